@@ -1,0 +1,92 @@
+/*
+ * agnes_ops.h -- C ABI of the operators that a model trained on prepared
+ * hyperbatches needs next to them: learned node embeddings (lookup and
+ * gradient), distillation from a teacher's top logits (loss and gradient), and
+ * feature rows in microscaled 4-bit floating point (quantisation, and their
+ * product with 4-bit weights).  They need no ctx.  The paper (arXiv
+ * 2601.01473) has no counterpart; the student it trains is the user's model.
+ *
+ * Conventions, beside those of agnes.h: all work of a call is enqueued on
+ * cuda_stream, nothing is allocated and nothing waited for; arrays are device
+ * memory of one GPU, and the call runs on that GPU.  No output may overlap
+ * an input or another output unless an entry says so.  A call with nothing to
+ * compute (no rows) returns AGNES_OK.  On failure agnes_last_error(NULL) gives
+ * a message.  Every call can be captured into a CUDA graph.
+ *
+ * Element types are AGNES_F32, AGNES_F16 or AGNES_BF16, each argument's own;
+ * arithmetic is in fp32 and each output value is rounded once, to nearest even.
+ * Strides are in elements (bytes for 4-bit rows) and may exceed the row's
+ * length; a row's elements are adjacent.
+ *
+ * status: an optional int32 in device memory.  What a kernel finds wrong with
+ * its data is ORed into it (AGNES_OP_*): the caller clears it, and reads it when
+ * it next waits for the stream.
+ */
+#ifndef AGNES_OPS_H
+#define AGNES_OPS_H
+
+#include "agnes.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define AGNES_BF16 2 /* agnes_dtype of the operators: bfloat16 */
+
+#define AGNES_OP_BAD_INDEX 1 /* an id or index at or past the end of its range */
+#define AGNES_OP_TIMEOUT 2   /* a kernel's bounded wait ran out: its output is undefined */
+
+/* out[t] = scale * table[ids[t]] for n tokens (for example the nodes of a
+ * minibatch).  A negative id selects no row: zeros.  So does an id >= rows,
+ * which also sets AGNES_OP_BAD_INDEX.
+ *  table   rows x dim of table_dtype, table_stride apart; 0 <= rows < 2^31,
+ *          1 <= dim < 2^31.
+ *  ids     n ids of ids_bits (32 or 64) bits; 0 <= n < 2^31.
+ *  out     n x dim of out_dtype, out_stride apart.
+ * Errors: EINVAL, ERANGE (a size above these limits, or n * dim above 2^40),
+ * ECUDA. */
+agnes_status agnes_embedding_lookup(const void* table, int32_t table_dtype, int64_t rows,
+                                    int64_t table_stride, int64_t dim, const void* ids,
+                                    int32_t ids_bits, int64_t n, float scale, void* out,
+                                    int32_t out_dtype, int64_t out_stride, int32_t* status,
+                                    void* cuda_stream);
+
+/* The gradient of agnes_embedding_lookup to the table, from the gradients of
+ * its n output rows: d[v] = scale * sum_{t: ids[t] = v} grad[t].  Tokens are
+ * sorted by id (stably) and each row's tokens summed in fp32 in an order that
+ * depends on n and the ids only: the result is the same, bit by bit, each time.
+ * Negative ids have no gradient, nor have ids >= rows, which also set
+ * AGNES_OP_BAD_INDEX.
+ *  grad    n x dim of grad_dtype, grad_stride apart.
+ *  out     dense: rows x dim of out_dtype, contiguous; every row is written
+ *          (zeros where no token selects it).
+ *  workspace  at least agnes_embedding_grad_workspace bytes, 256-byte aligned;
+ *          its contents are not kept.
+ * Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_embedding_grad(const void* grad, int32_t grad_dtype, int64_t grad_stride,
+                                  const void* ids, int32_t ids_bits, int64_t n, int64_t rows,
+                                  int64_t dim, float scale, void* out, int32_t out_dtype,
+                                  void* workspace, int64_t workspace_bytes, int32_t* status,
+                                  void* cuda_stream);
+
+/* The same gradient, of the selected rows only, for tables too large for a
+ * dense one: with c distinct ids in [0, rows),
+ *  out_ids   n int32: the c ids in ascending order, then -1;
+ *  out       n x dim of out_dtype, contiguous: their rows of d, then zeros;
+ *  count     one int32: c.
+ * The sizes do not depend on the data, so a training step needs no read-back.
+ * Arguments and errors as agnes_embedding_grad. */
+agnes_status agnes_embedding_grad_rows(const void* grad, int32_t grad_dtype, int64_t grad_stride,
+                                       const void* ids, int32_t ids_bits, int64_t n, int64_t rows,
+                                       int64_t dim, float scale, int32_t* out_ids, void* out,
+                                       int32_t out_dtype, int32_t* count, void* workspace,
+                                       int64_t workspace_bytes, int32_t* status,
+                                       void* cuda_stream);
+
+/* Bytes of workspace that both take for n tokens of dim values. */
+agnes_status agnes_embedding_grad_workspace(int64_t n, int64_t dim, int64_t* bytes);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

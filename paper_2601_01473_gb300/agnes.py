@@ -120,8 +120,8 @@ class _GraphInfo(ctypes.Structure):
     ]
 
 
-# Exported entry points and their argument types (mirrors include/agnes.h).
-_P = ctypes.c_void_p
+# Exported entry points and their argument types (mirrors include/*.h).
+_P, _I32, _I64, _F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 SIGNATURES = {
     "agnes_load_graph": ([ctypes.POINTER(_GraphDesc), ctypes.c_int, _P, ctypes.POINTER(_P)],
                          ctypes.c_int),
@@ -147,6 +147,14 @@ SIGNATURES = {
                                ctypes.c_int64, _P, _P, ctypes.c_int32, _P, ctypes.c_int32,
                                ctypes.c_int64, _P], ctypes.c_int),
     "agnes_free": ([_P], ctypes.c_int),
+    # include/agnes_ops.h (called by ops.py)
+    "agnes_embedding_lookup": ([_P, _I32, _I64, _I64, _I64, _P, _I32, _I64, _F32, _P, _I32, _I64,
+                                _P, _P], ctypes.c_int),
+    "agnes_embedding_grad": ([_P, _I32, _I64, _P, _I32, _I64, _I64, _I64, _F32, _P, _I32, _P, _I64,
+                              _P, _P], ctypes.c_int),
+    "agnes_embedding_grad_rows": ([_P, _I32, _I64, _P, _I32, _I64, _I64, _I64, _F32, _P, _P, _I32,
+                                   _P, _P, _I64, _P, _P], ctypes.c_int),
+    "agnes_embedding_grad_workspace": ([_I64, _I64, ctypes.POINTER(_I64)], ctypes.c_int),
     "agnes_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "agnes_last_error": ([_P], ctypes.c_char_p),
 }

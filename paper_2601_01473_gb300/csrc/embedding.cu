@@ -1,0 +1,894 @@
+// embedding.cu -- rows of a learned embedding table, scaled, for a list of node
+// ids, and the gradient of that lookup to the table (include/agnes_ops.h).
+//
+//   out[t] = scale * table[ids[t]]          d[v] = scale * sum_{ids[t] = v} grad[t]
+//
+// The gradient sorts the tokens by id, so that each row's tokens are adjacent,
+// and sums them without atomics: cut into chunks of equal length, whatever the
+// ids' distribution, a chunk writes the rows that lie within it and leaves its
+// part of a row that spans chunks in the workspace; a last kernel joins those.
+#include <type_traits>
+
+#include "ops_common.cuh"
+
+namespace agnes {
+
+namespace {
+
+// ---- lookup -----------------------------------------------------------------
+
+constexpr int kLookupThreads = 256;
+constexpr int kLookupItems = 4;  // vectors per thread, loaded before the first is stored
+constexpr int kLookupBlock = kLookupThreads * kLookupItems;
+
+// A block takes kLookupBlock vectors of kVec elements of the output in order.
+// vpr: vectors per row; inv_vpr = ceil(2^32 / vpr) where vpr < kLookupBlock.
+template <typename TIn, typename TOut, typename Id, int kVec>
+__global__ void __launch_bounds__(kLookupThreads)
+lookup_kernel(const TIn* __restrict__ table, int64_t rows, int64_t table_stride, int32_t vpr,
+              uint32_t inv_vpr, const Id* __restrict__ ids, int64_t n, float scale,
+              TOut* __restrict__ out, int64_t out_stride, int32_t* status) {
+  const int64_t first = (int64_t)blockIdx.x * kLookupBlock;
+  const int64_t t0 = first / vpr;
+  const uint32_t c0 = (uint32_t)(first - t0 * vpr);
+  int64_t token[kLookupItems], id[kLookupItems];
+  uint32_t col[kLookupItems];
+#pragma unroll
+  for (int u = 0; u < kLookupItems; ++u) {
+    // the row within the block: below 2 kLookupBlock / vpr + 1, and the product
+    // with the inverse is exact as q * vpr < 2^32
+    const uint32_t q = c0 + threadIdx.x + u * kLookupThreads;
+    uint32_t r;
+    if (vpr == 1)
+      r = q;
+    else if (vpr < kLookupBlock)
+      r = __umulhi(q, inv_vpr);
+    else
+      r = q >= (uint32_t)vpr;
+    col[u] = q - r * (uint32_t)vpr;
+    token[u] = t0 + r;
+    id[u] = token[u] < n ? (int64_t)__ldg(ids + token[u]) : -1;
+  }
+  Vec<TIn, kVec> x[kLookupItems];
+#pragma unroll
+  for (int u = 0; u < kLookupItems; ++u) {
+    if (id[u] >= 0 && id[u] < rows)
+      x[u] = *(const Vec<TIn, kVec>*)(table + id[u] * table_stride + (int64_t)col[u] * kVec);
+    else
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) x[u].v[e] = from_f32<TIn>(0.f);
+  }
+#pragma unroll
+  for (int u = 0; u < kLookupItems; ++u) {
+    if (token[u] >= n) continue;
+    const bool real = id[u] >= 0 && id[u] < rows;
+    Vec<TOut, kVec> y;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      y.v[e] = from_f32<TOut>(real ? to_f32(x[u].v[e]) * scale : 0.f);
+    *(Vec<TOut, kVec>*)(out + token[u] * out_stride + (int64_t)col[u] * kVec) = y;
+    if (id[u] >= rows && col[u] == 0) op_flag(status, AGNES_OP_BAD_INDEX);
+  }
+}
+
+// ---- the stable sort of the tokens by id -------------------------------------
+//
+// Least significant digit first, kDigits at most 2^kMaxBits, three launches a
+// pass: each CTA counts the digits of its run of tokens; the counts of one
+// digit are scanned over the CTAs; each CTA puts its tokens in their places,
+// in order.  Keys are ids in [0, rows), and `rows` for the tokens that select
+// none.
+
+constexpr int kSortThreads = 512;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortItems = 8;
+constexpr int kSortTile = kSortThreads * kSortItems;
+constexpr int kMaxBits = 9;
+constexpr int kMaxDigits = 1 << kMaxBits;
+constexpr int kSortMaxCtas = 304;
+
+template <typename Id>
+__device__ __forceinline__ uint32_t key_of(Id id, int64_t rows, int32_t* status) {
+  if (id < 0) return (uint32_t)rows;
+  if ((int64_t)id >= rows) {
+    op_flag(status, AGNES_OP_BAD_INDEX);
+    return (uint32_t)rows;
+  }
+  return (uint32_t)id;
+}
+
+// Where a pass reads its keys: the caller's ids (the first pass), or the last
+// pass's.
+template <typename Id>
+struct FromIds {
+  const Id* ids;
+  int64_t rows;
+  int32_t* status;
+  __device__ uint32_t key(int64_t i) const { return key_of(__ldg(ids + i), rows, status); }
+  __device__ int32_t token(int64_t i) const { return (int32_t)i; }
+};
+struct FromPass {
+  const uint32_t* keys;
+  const int32_t* tokens;
+  __device__ uint32_t key(int64_t i) const { return keys[i]; }
+  __device__ int32_t token(int64_t i) const { return tokens[i]; }
+};
+
+struct Run {
+  int64_t begin, end;
+};
+
+// CTA b's run of tokens: whole tiles.
+__device__ __forceinline__ Run run_of(int64_t n, int b, int ctas) {
+  const int64_t tiles = (n + kSortTile - 1) / kSortTile;
+  const int64_t lo = tiles * b / ctas * kSortTile, hi = tiles * (b + 1) / ctas * kSortTile;
+  return {lo, hi < n ? hi : n};
+}
+
+// counts[digit * ctas + cta]
+template <typename Src>
+__global__ void __launch_bounds__(kSortThreads)
+sort_count_kernel(Src src, int64_t n, int shift, int digits, int32_t* __restrict__ counts) {
+  __shared__ int32_t hist[kMaxDigits];
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) hist[d] = 0;
+  __syncthreads();
+  const Run run = run_of(n, blockIdx.x, gridDim.x);
+  for (int64_t base = run.begin; base < run.end; base += kSortTile) {
+#pragma unroll
+    for (int u = 0; u < kSortItems; ++u) {
+      const int64_t i = base + u * kSortThreads + threadIdx.x;
+      const bool in = i < run.end;
+      const int d = in ? (int)(src.key(i) >> shift) & (digits - 1) : -1;
+      const unsigned peers = __match_any_sync(0xffffffffu, d);
+      if (in && lane_id() == __ffs(peers) - 1) atomicAdd(hist + d, __popc(peers));
+    }
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kSortThreads)
+    counts[(int64_t)d * gridDim.x + blockIdx.x] = hist[d];
+}
+
+// A warp per digit: its counts become their exclusive prefix over the CTAs, and
+// totals[digit] their sum.
+__global__ void __launch_bounds__(256)
+sort_scan_kernel(int32_t* __restrict__ counts, int ctas, int digits, int32_t* __restrict__ totals) {
+  const int d = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (d >= digits) return;
+  int32_t* row = counts + (int64_t)d * ctas;
+  int32_t carry = 0;
+  for (int b = 0; b < ctas; b += 32) {
+    const int i = b + lane_id();
+    const int32_t v = i < ctas ? row[i] : 0;
+    const int32_t incl = warp_incl_scan(v);
+    if (i < ctas) row[i] = carry + incl - v;
+    carry += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane_id() == 0) totals[d] = carry;
+}
+
+struct SortSmem {
+  int32_t warp_hist[kSortWarps][kMaxDigits];
+  int32_t base[kMaxDigits];  // where the next token of each digit goes
+  int32_t warp_total[kSortWarps];
+};
+
+// base[d] = the exclusive prefix over the digits of total(d), plus extra(d).
+template <typename Total, typename Extra>
+__device__ __forceinline__ void digit_bases(SortSmem& s, int digits, Total total, Extra extra) {
+  const int d = threadIdx.x;  // kSortThreads >= kMaxDigits
+  const int32_t v = d < digits ? total(d) : 0;
+  const int32_t incl = warp_incl_scan(v);
+  if (lane_id() == 31) s.warp_total[d >> 5] = incl;
+  __syncthreads();
+  int32_t before = 0;
+  for (int w = 0; w < d >> 5; ++w) before += s.warp_total[w];
+  if (d < digits) s.base[d] = before + incl - v + extra(d);
+}
+static_assert(kSortThreads >= kMaxDigits, "a thread per digit");
+
+// The places of a tile's tokens, in order: warp w holds tokens w * 256 + u * 32
+// + lane.  s.base moves on by the tile's counts.  All threads take part; a
+// token out of the run has digit -1.
+__device__ __forceinline__ void tile_places(SortSmem& s, int digits, const int (&digit)[kSortItems],
+                                            int32_t (&place)[kSortItems]) {
+  const int warp = threadIdx.x >> 5;
+  for (int i = threadIdx.x; i < kSortWarps * kMaxDigits; i += kSortThreads)
+    (&s.warp_hist[0][0])[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kSortItems; ++u) {
+    const unsigned peers = __match_any_sync(0xffffffffu, digit[u]);
+    int32_t old = 0;
+    if (digit[u] >= 0) old = s.warp_hist[warp][digit[u]];
+    place[u] = old + __popc(peers & ((1u << lane_id()) - 1u));
+    __syncwarp();
+    if (digit[u] >= 0 && lane_id() == __ffs(peers) - 1)
+      s.warp_hist[warp][digit[u]] = old + __popc(peers);
+    __syncwarp();
+  }
+  __syncthreads();
+  const int d = threadIdx.x;
+  if (d < digits) {
+    int32_t at = s.base[d];
+    for (int w = 0; w < kSortWarps; ++w) {
+      const int32_t c = s.warp_hist[w][d];
+      s.warp_hist[w][d] = at;
+      at += c;
+    }
+    s.base[d] = at;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kSortItems; ++u)
+    if (digit[u] >= 0) place[u] += s.warp_hist[warp][digit[u]];
+}
+
+template <typename Src>
+__global__ void __launch_bounds__(kSortThreads)
+sort_place_kernel(Src src, int64_t n, int shift, int digits, const int32_t* __restrict__ counts,
+                  const int32_t* __restrict__ totals, uint32_t* __restrict__ keys,
+                  int32_t* __restrict__ tokens) {
+  __shared__ SortSmem s;
+  digit_bases(s, digits, [&](int d) { return totals[d]; },
+              [&](int d) { return counts[(int64_t)d * gridDim.x + blockIdx.x]; });
+  const Run run = run_of(n, blockIdx.x, gridDim.x);
+  const int first = (threadIdx.x >> 5) * 32 * kSortItems + lane_id();
+  for (int64_t base = run.begin; base < run.end; base += kSortTile) {
+    uint32_t key[kSortItems];
+    int32_t token[kSortItems], place[kSortItems];
+    int digit[kSortItems];
+#pragma unroll
+    for (int u = 0; u < kSortItems; ++u) {
+      const int64_t i = base + first + u * 32;
+      const bool in = i < run.end;
+      key[u] = in ? src.key(i) : 0;
+      token[u] = in ? src.token(i) : 0;
+      digit[u] = in ? (int)(key[u] >> shift) & (digits - 1) : -1;
+    }
+    __syncthreads();  // the bases, and the last tile's places, have been read
+    tile_places(s, digits, digit, place);
+#pragma unroll
+    for (int u = 0; u < kSortItems; ++u) {
+      if (digit[u] < 0) continue;
+      keys[place[u]] = key[u];
+      tokens[place[u]] = token[u];
+    }
+  }
+}
+
+// Up to kSortTile tokens in one CTA, every pass in shared memory.
+template <typename Id>
+__global__ void __launch_bounds__(kSortThreads)
+sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __restrict__ keys,
+                  int32_t* __restrict__ tokens) {
+  extern __shared__ __align__(16) uint8_t small_smem[];
+  SortSmem& s = *(SortSmem*)small_smem;
+  uint32_t* skey = (uint32_t*)(small_smem + sizeof(SortSmem));
+  int32_t* stoken = (int32_t*)(skey + kSortTile);
+  const int first = (threadIdx.x >> 5) * 32 * kSortItems + lane_id();
+  const int digits = 1 << bits;
+  uint32_t key[kSortItems];
+  int32_t token[kSortItems], place[kSortItems];
+#pragma unroll
+  for (int u = 0; u < kSortItems; ++u) {
+    const int i = first + u * 32;
+    key[u] = i < n ? src.key(i) : 0;
+    token[u] = i;
+  }
+  for (int p = 0; p < passes; ++p) {
+    int digit[kSortItems];
+#pragma unroll
+    for (int u = 0; u < kSortItems; ++u)
+      digit[u] = first + u * 32 < n ? (int)(key[u] >> (p * bits)) & (digits - 1) : -1;
+    // the digits' totals: counted with base = 0, then placed
+    if (threadIdx.x < digits) s.base[threadIdx.x] = 0;
+    __syncthreads();
+    tile_places(s, digits, digit, place);  // ends with base[d] = the digit's count
+    __syncthreads();
+    const int32_t count = threadIdx.x < digits ? s.base[threadIdx.x] : 0;
+    __syncthreads();
+    digit_bases(s, digits, [&](int) { return count; }, [](int) { return 0; });
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortItems; ++u) {
+      if (digit[u] < 0) continue;
+      const int32_t at = s.base[digit[u]] + place[u];
+      skey[at] = key[u];
+      stoken[at] = token[u];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortItems; ++u) {
+      const int i = first + u * 32;
+      if (i < n) {
+        key[u] = skey[i];
+        token[u] = stoken[i];
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int u = 0; u < kSortItems; ++u) {
+    const int i = first + u * 32;
+    if (i < n) {
+      keys[i] = key[u];
+      tokens[i] = token[u];
+    }
+  }
+}
+constexpr size_t kSmallSmem = sizeof(SortSmem) + 8 * kSortTile;
+
+// ---- sums over the sorted tokens ----------------------------------------------
+
+constexpr int kSumThreads = 256;
+
+// heads[b] = the number of distinct ids that begin among the sorted tokens
+// [b * span, (b + 1) * span).
+__global__ void __launch_bounds__(kSumThreads)
+count_heads_kernel(const uint32_t* __restrict__ keys, int64_t n, uint32_t rows, int span,
+                   int32_t* __restrict__ heads) {
+  __shared__ int32_t total;
+  if (threadIdx.x == 0) total = 0;
+  __syncthreads();
+  const int64_t lo = (int64_t)blockIdx.x * span, hi = min(n, lo + span);
+  int32_t mine = 0;
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kSumThreads) {
+    const uint32_t k = keys[i];
+    mine += k < rows && (i == 0 || keys[i - 1] != k);
+  }
+  mine = warp_sum(mine);
+  if (lane_id() == 0 && mine) atomicAdd(&total, mine);
+  __syncthreads();
+  if (threadIdx.x == 0) heads[blockIdx.x] = total;
+}
+
+struct SumArgs {
+  const uint32_t* keys;
+  const int32_t* tokens;
+  int64_t n;
+  uint32_t rows;
+  int32_t dim;
+  const void* grad;
+  int64_t grad_stride;
+  float scale;
+  void* out;
+  // the compact form (null: dense, row v of `out` is d[v])
+  const int32_t* heads;
+  int32_t* out_ids;
+  int32_t* count;
+  // a chunk's part of the row that it begins within (first) and of the row that
+  // it ends within (last): partial[(2 * chunk + which) * dim ..]
+  float* partial;
+  int32_t chunk;       // tokens per chunk
+  int64_t chunks;
+  int32_t cta_chunks;  // chunks per CTA
+};
+
+// The sum of heads[0 .. limit) for this CTA, and of all of them.
+__device__ __forceinline__ void prefix_of_heads(const int32_t* heads, int ctas, int limit,
+                                                int32_t* before, int32_t* all) {
+  __shared__ int32_t sum[2];
+  if (threadIdx.x < 2) sum[threadIdx.x] = 0;
+  __syncthreads();
+  int32_t b = 0, a = 0;
+  for (int i = threadIdx.x; i < ctas; i += kSumThreads) {
+    const int32_t h = heads[i];
+    a += h;
+    b += i < limit ? h : 0;
+  }
+  a = warp_sum(a);
+  b = warp_sum(b);
+  if (lane_id() == 0) {
+    atomicAdd(&sum[0], b);
+    atomicAdd(&sum[1], a);
+  }
+  __syncthreads();
+  *before = sum[0];
+  *all = sum[1];
+}
+
+// A group of kLanes lanes sums a chunk's rows for kLanes * kVec * kCols columns,
+// kAhead rows in flight.  blockIdx.y: which columns.
+template <typename TIn, typename TOut, int kVec, int kCols, int kLanes>
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
+  constexpr int kGroups = kSumThreads / kLanes;
+  constexpr int kAhead = 8 / kCols > 2 ? 8 / kCols : 2;
+  __shared__ int32_t group_heads[kGroups];
+  const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const int64_t chunk = (int64_t)blockIdx.x * kGroups + group;
+  const int64_t lo = min(a.n, chunk * a.chunk), hi = min(a.n, lo + a.chunk);
+  const int32_t col0 = blockIdx.y * kLanes * kVec * kCols + lane * kVec;
+  int32_t rank = -1;  // of the current row among the distinct ids
+  if (a.heads) {
+    int32_t before, all;
+    prefix_of_heads(a.heads, gridDim.x, blockIdx.x, &before, &all);
+    int32_t mine = 0;
+    for (int64_t i = lo + lane; i < hi; i += kLanes) {
+      const uint32_t k = a.keys[i];
+      mine += k < a.rows && (i == 0 || a.keys[i - 1] != k);
+    }
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d, kLanes);
+    if (lane == 0) group_heads[group] = mine;
+    __syncthreads();
+    rank = before - 1;
+    for (int g = 0; g < group; ++g) rank += group_heads[g];
+    // the zeros past the last row, the CTAs' shares of them in turn
+    const int64_t pad = a.n - all;
+    const int64_t p0 = all + pad * blockIdx.x / gridDim.x;
+    const int64_t p1 = all + pad * (blockIdx.x + 1) / gridDim.x;
+    if (blockIdx.y == 0) {
+      for (int64_t i = p0 + threadIdx.x; i < p1; i += kSumThreads) a.out_ids[i] = -1;
+      if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = all;
+    }
+    for (int64_t i = p0 + group; i < p1; i += kGroups) {
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) {
+        const int32_t col = col0 + c * kLanes * kVec;
+        if (col >= a.dim) break;
+        Vec<TOut, kVec> z;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) z.v[e] = from_f32<TOut>(0.f);
+        *(Vec<TOut, kVec>*)((TOut*)a.out + i * a.dim + col) = z;
+      }
+    }
+  }
+  if (lo >= hi) return;
+  float acc[kCols][kVec];
+  auto clear = [&] {
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) acc[c][e] = 0.f;
+  };
+  // the row that the tokens before i belong to is complete within the chunk, or
+  // its part goes to the workspace
+  auto put_row = [&](uint32_t key) {
+    const int64_t row = a.heads ? rank : (int64_t)key;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+      const int32_t col = col0 + c * kLanes * kVec;
+      if (col >= a.dim) break;
+      Vec<TOut, kVec> y;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) y.v[e] = from_f32<TOut>(acc[c][e] * a.scale);
+      *(Vec<TOut, kVec>*)((TOut*)a.out + row * a.dim + col) = y;
+    }
+  };
+  auto put_part = [&](int which) {
+    float* p = a.partial + (2 * chunk + which) * a.dim;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+      const int32_t col = col0 + c * kLanes * kVec;
+      if (col >= a.dim) break;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) p[col + e] = acc[c][e];
+    }
+  };
+  uint32_t key = a.keys[lo];
+  bool spans = lo > 0 && a.keys[lo - 1] == key;  // the current row began in an earlier chunk
+  auto begin_row = [&](uint32_t k) {
+    ++rank;
+    if (a.heads && k < a.rows && blockIdx.y == 0 && lane == 0) a.out_ids[rank] = (int32_t)k;
+  };
+  if (!spans && key < a.rows) begin_row(key);
+  clear();
+  for (int64_t i0 = lo; i0 < hi && key < a.rows; i0 += kAhead) {
+    uint32_t k[kAhead];
+    Vec<TIn, kVec> x[kAhead][kCols];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t i = min(i0 + u, hi - 1);
+      k[u] = i0 + u < hi ? a.keys[i] : a.rows;
+      const TIn* row = (const TIn*)a.grad + (int64_t)a.tokens[i] * a.grad_stride;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) {
+        const int32_t col = col0 + c * kLanes * kVec;
+        if (col < a.dim) {
+          x[u][c] = *(const Vec<TIn, kVec>*)(row + col);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x[u][c].v[e] = from_f32<TIn>(0.f);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (i0 + u >= hi) break;
+      if (k[u] != key) {
+        if (spans)
+          put_part(0);
+        else
+          put_row(key);
+        spans = false;
+        clear();
+        key = k[u];
+        if (key >= a.rows) break;
+        begin_row(key);
+      }
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          acc[c][e] += to_f32(x[u][c].v[e]);
+    }
+  }
+  if (key >= a.rows) return;
+  if (spans)
+    put_part(0);
+  else if (hi < a.n && a.keys[hi] == key)
+    put_part(1);
+  else
+    put_row(key);
+}
+
+// Rows that span chunks: a warp for each chunk in which such a row begins adds
+// the chunks' parts in order.  rank of the row: known from the chunk's heads.
+template <typename TOut>
+__global__ void __launch_bounds__(kSumThreads) join_kernel(SumArgs a) {
+  const int64_t chunk = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
+  if (chunk + 1 >= a.chunks) return;  // the last chunk's rows end in it
+  const int64_t lo = chunk * a.chunk, hi = lo + a.chunk;
+  const uint32_t key = a.keys[hi - 1];
+  if (key >= a.rows || a.keys[hi] != key) return;     // nothing goes on past the chunk
+  if (lo > 0 && a.keys[lo - 1] == key) return;        // it began in an earlier chunk
+  // the last chunk that begins with the key
+  int64_t last = chunk + 1, end = a.chunks;
+  while (end - last > 1) {
+    const int64_t mid = (last + end) / 2;
+    if (a.keys[mid * a.chunk] == key)
+      last = mid;
+    else
+      end = mid;
+  }
+  int64_t row = key;
+  if (a.heads) {  // the row is the last that begins at or before the chunk's end
+    int32_t r = 0;
+    const int cta = (int)(chunk / a.cta_chunks);
+    for (int i = lane_id(); i < cta; i += 32) r += a.heads[i];
+    for (int64_t i = (int64_t)cta * a.cta_chunks * a.chunk + lane_id(); i < hi; i += 32) {
+      const uint32_t k = a.keys[i];
+      r += k < a.rows && (i == 0 || a.keys[i - 1] != k);
+    }
+    row = warp_sum(r) - 1;
+  }
+  for (int32_t col = lane_id(); col < a.dim; col += 32) {
+    float acc = a.partial[(2 * chunk + 1) * a.dim + col];
+    for (int64_t c = chunk + 1; c <= last; ++c) acc += a.partial[2 * c * a.dim + col];
+    ((TOut*)a.out)[row * a.dim + col] = from_f32<TOut>(acc * a.scale);
+  }
+}
+
+// ---- host ------------------------------------------------------------------
+
+constexpr int64_t kMaxTokens = 0x7fffffff;
+constexpr int64_t kMaxCells = 1ll << 40;
+constexpr int kMaxChunks = 8192;
+constexpr int kMinChunk = 32;
+
+struct GradPlan {
+  int64_t chunk, chunks;
+  size_t keys[2], tokens[2], counts, totals, heads, partial, bytes;
+};
+
+GradPlan grad_plan(int64_t n, int64_t dim) {
+  GradPlan p;
+  p.chunk = ceil_div(ceil_div(n, kMaxChunks), kMinChunk) * kMinChunk;
+  if (p.chunk < kMinChunk) p.chunk = kMinChunk;
+  p.chunks = ceil_div(n, p.chunk);
+  size_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at += (size_t)((bytes + 255) / 256 * 256);
+    return here;
+  };
+  for (int i = 0; i < 2; ++i) {
+    p.keys[i] = take(4 * n);
+    p.tokens[i] = take(4 * n);
+  }
+  p.counts = take(4ll * kMaxDigits * kSortMaxCtas);
+  p.totals = take(4 * kMaxDigits);
+  p.heads = take(4 * (p.chunks + 1));
+  p.partial = take(8 * p.chunks * dim);
+  p.bytes = at;
+  return p;
+}
+
+template <typename Id>
+cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, const GradPlan& p,
+                        int32_t* status, int num_sms, cudaStream_t st, int* result) {
+  int bits = 1;
+  while ((1ll << bits) <= rows) ++bits;  // keys 0 .. rows
+  const int passes = (int)ceil_div(bits, kMaxBits);
+  const int pass_bits = (int)ceil_div(bits, passes);
+  const int digits = 1 << pass_bits;
+  const FromIds<Id> ids_src{ids, rows, status};
+  const auto keys = [&](int i) { return (uint32_t*)(ws + p.keys[i]); };
+  const auto tokens = [&](int i) { return (int32_t*)(ws + p.tokens[i]); };
+  if (n <= kSortTile) {
+    const cudaError_t e = cudaFuncSetAttribute(
+        sort_small_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
+    if (e != cudaSuccess) return e;
+    sort_small_kernel<Id><<<1, kSortThreads, kSmallSmem, st>>>(ids_src, (int)n, passes, pass_bits,
+                                                               keys(0), tokens(0));
+    *result = 0;
+    return cudaGetLastError();
+  }
+  const int64_t tiles = ceil_div(n, kSortTile);
+  int ctas = 2 * num_sms < kSortMaxCtas ? 2 * num_sms : kSortMaxCtas;
+  if (tiles < ctas) ctas = (int)tiles;
+  int32_t* counts = (int32_t*)(ws + p.counts);
+  int32_t* totals = (int32_t*)(ws + p.totals);
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * pass_bits, to = pass & 1;
+    const FromPass from{keys(to ^ 1), tokens(to ^ 1)};
+    if (pass == 0)
+      sort_count_kernel<<<ctas, kSortThreads, 0, st>>>(ids_src, n, shift, digits, counts);
+    else
+      sort_count_kernel<<<ctas, kSortThreads, 0, st>>>(from, n, shift, digits, counts);
+    sort_scan_kernel<<<(digits + 7) / 8, 256, 0, st>>>(counts, ctas, digits, totals);
+    if (pass == 0)
+      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(ids_src, n, shift, digits, counts, totals,
+                                                       keys(to), tokens(to));
+    else
+      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(from, n, shift, digits, counts, totals,
+                                                       keys(to), tokens(to));
+    *result = to;
+  }
+  return cudaGetLastError();
+}
+
+template <typename TIn, typename TOut, int kVec, int kCols, int kLanes>
+cudaError_t launch_sum(SumArgs a, int32_t* heads, cudaStream_t st) {
+  constexpr int kGroups = kSumThreads / kLanes;
+  a.cta_chunks = kGroups;
+  const int64_t ctas = ceil_div(a.chunks, kGroups);
+  const int64_t cols = ceil_div(a.dim, kLanes * kVec * kCols);
+  if (cols > 65535) return cudaErrorInvalidConfiguration;
+  if (heads) {
+    a.heads = heads;
+    count_heads_kernel<<<(unsigned)ctas, kSumThreads, 0, st>>>(a.keys, a.n, a.rows,
+                                                               kGroups * a.chunk, heads);
+  }
+  sum_kernel<TIn, TOut, kVec, kCols, kLanes>
+      <<<dim3((unsigned)ctas, (unsigned)cols), kSumThreads, 0, st>>>(a);
+  if (a.chunks > 1)
+    join_kernel<TOut><<<(unsigned)ceil_div(a.chunks, kSumThreads / 32), kSumThreads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+// Lanes for a row of `vecs` vectors.
+template <typename TIn, typename TOut, int kVec>
+cudaError_t launch_sum_lanes(const SumArgs& a, int32_t* heads, cudaStream_t st) {
+  const int64_t vecs = ceil_div(a.dim, kVec);
+  if (vecs <= 4) return launch_sum<TIn, TOut, kVec, 1, 4>(a, heads, st);
+  if (vecs <= 16) return launch_sum<TIn, TOut, kVec, 1, 16>(a, heads, st);
+  if (kVec > 2 || vecs <= 32) return launch_sum<TIn, TOut, kVec, 1, 32>(a, heads, st);
+  return launch_sum<TIn, TOut, kVec, 4, 32>(a, heads, st);
+}
+
+// f(constant) for the widest vector of 8, 4, 2 or 1 elements (16 bytes at most of
+// either type) that divides the rows and to which both arrays are aligned.
+template <typename TA, typename TB, typename F>
+cudaError_t with_vector(int64_t dim, const void* a, int64_t a_stride, const void* b,
+                        int64_t b_stride, F&& f) {
+  constexpr int kWide = 16 / (sizeof(TA) > sizeof(TB) ? sizeof(TA) : sizeof(TB));
+  const auto fits = [&](int64_t v) {
+    return dim % v == 0 && aligned_rows(a, a_stride * (int64_t)sizeof(TA), v * sizeof(TA)) &&
+           aligned_rows(b, b_stride * (int64_t)sizeof(TB), v * sizeof(TB));
+  };
+  if (fits(kWide)) return f(std::integral_constant<int, kWide>());
+  if (fits(2)) return f(std::integral_constant<int, 2>());
+  return f(std::integral_constant<int, 1>());
+}
+
+// The checks that the lookup and the gradient share.
+agnes_status check_embedding(const char* op, int64_t rows, int64_t dim, int64_t n,
+                             int32_t ids_bits) {
+  if (rows < 0 || n < 0 || dim < 1)
+    return op_error(AGNES_EINVAL, "%s: rows %lld, dim %lld, n %lld", op, (long long)rows,
+                    (long long)dim, (long long)n);
+  if (rows > kMaxTokens || n > kMaxTokens || dim > kMaxTokens || (n && dim > kMaxCells / n) ||
+      (rows && dim > kMaxCells / rows))
+    return op_error(AGNES_ERANGE, "%s: rows %lld, dim %lld, n %lld are too large", op,
+                    (long long)rows, (long long)dim, (long long)n);
+  return op_index_bits(op, "ids", ids_bits);
+}
+
+struct GradCall {
+  const char* op;
+  const void* grad;
+  int32_t grad_dtype;
+  int64_t grad_stride;
+  const void* ids;
+  int32_t ids_bits;
+  int64_t n, rows, dim;
+  float scale;
+  void* out;
+  int32_t out_dtype;
+  int32_t* out_ids;  // the compact form's, with count
+  int32_t* count;
+  void* workspace;
+  int64_t workspace_bytes;
+  int32_t* status;
+  cudaStream_t st;
+};
+
+agnes_status embedding_grad(const GradCall& c, bool compact) {
+  const char* op = c.op;
+  OP_TRY(check_embedding(op, c.rows, c.dim, c.n, c.ids_bits));
+  OP_TRY(op_float_type(op, "grad", c.grad_dtype));
+  OP_TRY(op_float_type(op, "out", c.out_dtype));
+  if (c.n > 0 && c.grad_stride < c.dim)
+    return op_error(AGNES_EINVAL, "%s: grad_stride %lld is below dim %lld", op,
+                    (long long)c.grad_stride, (long long)c.dim);
+  const int64_t out_rows = compact ? c.n : c.rows;
+  int device = -1;
+  if (compact) {
+    OP_TRY(op_device_of(op, "count", c.count, &device));
+    OP_TRY(op_aligned(op, "count", c.count, 4));
+  } else if (out_rows == 0) {
+    return AGNES_OK;
+  } else {
+    OP_TRY(op_device_of(op, "out", c.out, &device));
+  }
+  if (out_rows > 0) {
+    OP_TRY(op_on_device(op, "out", c.out, device));
+    OP_TRY(op_aligned(op, "out", c.out, float_size(c.out_dtype)));
+  }
+  if (c.status) OP_TRY(op_on_device(op, "status", c.status, device));
+  DeviceGuard dg(device);
+  if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
+  if (c.n == 0) {
+    cudaError_t e;
+    if (compact)
+      e = cudaMemsetAsync(c.count, 0, 4, c.st);
+    else
+      e = cudaMemsetAsync(c.out, 0, (size_t)(c.rows * c.dim * float_size(c.out_dtype)), c.st);
+    return op_launched(op, e);
+  }
+  OP_TRY(op_on_device(op, "grad", c.grad, device));
+  OP_TRY(op_aligned(op, "grad", c.grad, float_size(c.grad_dtype)));
+  OP_TRY(op_on_device(op, "ids", c.ids, device));
+  OP_TRY(op_aligned(op, "ids", c.ids, c.ids_bits / 8));
+  if (compact) {
+    OP_TRY(op_on_device(op, "out_ids", c.out_ids, device));
+    OP_TRY(op_aligned(op, "out_ids", c.out_ids, 4));
+  }
+  OP_TRY(op_on_device(op, "workspace", c.workspace, device));
+  OP_TRY(op_aligned(op, "workspace", c.workspace, 256));
+  const GradPlan p = grad_plan(c.n, c.dim);
+  if (c.workspace_bytes < (int64_t)p.bytes)
+    return op_error(AGNES_EINVAL, "%s: a workspace of %lld bytes, %lld are needed", op,
+                    (long long)c.workspace_bytes, (long long)p.bytes);
+  uint8_t* ws = (uint8_t*)c.workspace;
+  int which = 0;
+  cudaError_t e = with_index_type(c.ids_bits, [&](auto id) {
+    using Id = typename decltype(id)::type;
+    return sort_tokens((const Id*)c.ids, c.n, c.rows, ws, p, c.status, op_num_sms(device), c.st,
+                       &which);
+  });
+  if (e != cudaSuccess) return op_launched(op, e);
+  if (!compact) {
+    e = cudaMemsetAsync(c.out, 0, (size_t)(c.rows * c.dim * float_size(c.out_dtype)), c.st);
+    if (e != cudaSuccess) return op_launched(op, e);
+  }
+  SumArgs a = {};
+  a.keys = (const uint32_t*)(ws + p.keys[which]);
+  a.tokens = (const int32_t*)(ws + p.tokens[which]);
+  a.n = c.n;
+  a.rows = (uint32_t)c.rows;
+  a.dim = (int32_t)c.dim;
+  a.grad = c.grad;
+  a.grad_stride = c.grad_stride;
+  a.scale = c.scale;
+  a.out = c.out;
+  a.out_ids = c.out_ids;
+  a.count = c.count;
+  a.partial = (float*)(ws + p.partial);
+  a.chunk = (int32_t)p.chunk;
+  a.chunks = p.chunks;
+  int32_t* heads = compact ? (int32_t*)(ws + p.heads) : nullptr;
+  e = with_float_type(c.grad_dtype, [&](auto tin) {
+    return with_float_type(c.out_dtype, [&](auto tout) {
+      using TIn = typename decltype(tin)::type;
+      using TOut = typename decltype(tout)::type;
+      return with_vector<TIn, TOut>(c.dim, c.grad, c.grad_stride, c.out, c.dim, [&](auto v) {
+        return launch_sum_lanes<TIn, TOut, decltype(v)::value>(a, heads, c.st);
+      });
+    });
+  });
+  return op_launched(op, e);
+}
+
+}  // namespace
+
+}  // namespace agnes
+
+using namespace agnes;
+
+extern "C" {
+
+agnes_status agnes_embedding_lookup(const void* table, int32_t table_dtype, int64_t rows,
+                                    int64_t table_stride, int64_t dim, const void* ids,
+                                    int32_t ids_bits, int64_t n, float scale, void* out,
+                                    int32_t out_dtype, int64_t out_stride, int32_t* status,
+                                    void* cuda_stream) {
+  const char* op = "agnes_embedding_lookup";
+  OP_TRY(check_embedding(op, rows, dim, n, ids_bits));
+  OP_TRY(op_float_type(op, "table", table_dtype));
+  OP_TRY(op_float_type(op, "out", out_dtype));
+  if ((rows > 1 && table_stride < dim) || (n > 1 && out_stride < dim))
+    return op_error(AGNES_EINVAL, "%s: table_stride %lld or out_stride %lld is below dim %lld", op,
+                    (long long)table_stride, (long long)out_stride, (long long)dim);
+  if (n == 0) return AGNES_OK;
+  int device = -1;
+  OP_TRY(op_device_of(op, "out", out, &device));
+  if (rows > 0) OP_TRY(op_on_device(op, "table", table, device));
+  OP_TRY(op_on_device(op, "ids", ids, device));
+  OP_TRY(op_aligned(op, "table", table, float_size(table_dtype)));
+  OP_TRY(op_aligned(op, "out", out, float_size(out_dtype)));
+  OP_TRY(op_aligned(op, "ids", ids, ids_bits / 8));
+  if (status) OP_TRY(op_on_device(op, "status", status, device));
+  DeviceGuard dg(device);
+  if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  bool too_many = false;
+  const cudaError_t e = with_float_type(table_dtype, [&](auto tin) {
+    return with_float_type(out_dtype, [&](auto tout) {
+      using TIn = typename decltype(tin)::type;
+      using TOut = typename decltype(tout)::type;
+      return with_vector<TIn, TOut>(dim, table, table_stride, out, out_stride, [&](auto v) {
+        constexpr int kVec = decltype(v)::value;
+        const int64_t vpr = dim / kVec, blocks = ceil_div(n * vpr, kLookupBlock);
+        if (blocks > kMaxTokens) {
+          too_many = true;
+          return cudaSuccess;
+        }
+        const uint32_t inv = (uint32_t)(((1ull << 32) + vpr - 1) / vpr);
+        return with_index_type(ids_bits, [&](auto id) {
+          using Id = typename decltype(id)::type;
+          lookup_kernel<TIn, TOut, Id, kVec><<<(unsigned)blocks, kLookupThreads, 0, st>>>(
+              (const TIn*)table, rows, table_stride, (int32_t)vpr, inv, (const Id*)ids, n, scale,
+              (TOut*)out, out_stride, status);
+          return cudaGetLastError();
+        });
+      });
+    });
+  });
+  if (too_many) return op_error(AGNES_ERANGE, "%s: n * dim is too large", op);
+  return op_launched(op, e);
+}
+
+agnes_status agnes_embedding_grad(const void* grad, int32_t grad_dtype, int64_t grad_stride,
+                                  const void* ids, int32_t ids_bits, int64_t n, int64_t rows,
+                                  int64_t dim, float scale, void* out, int32_t out_dtype,
+                                  void* workspace, int64_t workspace_bytes, int32_t* status,
+                                  void* cuda_stream) {
+  return embedding_grad({"agnes_embedding_grad", grad, grad_dtype, grad_stride, ids, ids_bits, n,
+                         rows, dim, scale, out, out_dtype, nullptr, nullptr, workspace,
+                         workspace_bytes, status, (cudaStream_t)cuda_stream},
+                        false);
+}
+
+agnes_status agnes_embedding_grad_rows(const void* grad, int32_t grad_dtype, int64_t grad_stride,
+                                       const void* ids, int32_t ids_bits, int64_t n, int64_t rows,
+                                       int64_t dim, float scale, int32_t* out_ids, void* out,
+                                       int32_t out_dtype, int32_t* count, void* workspace,
+                                       int64_t workspace_bytes, int32_t* status,
+                                       void* cuda_stream) {
+  return embedding_grad({"agnes_embedding_grad_rows", grad, grad_dtype, grad_stride, ids, ids_bits,
+                         n, rows, dim, scale, out, out_dtype, out_ids, count, workspace,
+                         workspace_bytes, status, (cudaStream_t)cuda_stream},
+                        true);
+}
+
+agnes_status agnes_embedding_grad_workspace(int64_t n, int64_t dim, int64_t* bytes) {
+  const char* op = "agnes_embedding_grad_workspace";
+  if (!bytes) return op_error(AGNES_EINVAL, "%s: bytes is NULL", op);
+  OP_TRY(check_embedding(op, 0, dim, n, 32));
+  *bytes = (int64_t)grad_plan(n, dim).bytes;
+  return AGNES_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,106 @@
+// ops_common.cuh -- what the operators of include/agnes_ops.h share: element
+// types, vectors of elements, and the host's checks of arguments.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/agnes_ops.h"
+#include "common.cuh"
+#include "internal.h"
+
+namespace agnes {
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// One rounding, to nearest even.
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) {
+  return x;
+}
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float x) {
+  return __float2half_rn(x);
+}
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) {
+  return __float2bfloat16_rn(x);
+}
+
+// N elements that are loaded and stored as one access of N * sizeof(T) bytes.
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Vec {
+  T v[N];
+};
+
+// One of an operator's float types, as a type.
+template <typename T>
+struct TypeTag {
+  using type = T;
+};
+
+// f(TypeTag<T>) for the type of an agnes_dtype code that has been checked.
+template <typename F>
+cudaError_t with_float_type(int32_t dtype, F&& f) {
+  switch (dtype) {
+    case AGNES_F32: return f(TypeTag<float>());
+    case AGNES_F16: return f(TypeTag<__half>());
+    default: return f(TypeTag<__nv_bfloat16>());
+  }
+}
+
+template <typename F>
+cudaError_t with_index_type(int32_t bits, F&& f) {
+  return bits == 32 ? f(TypeTag<int32_t>()) : f(TypeTag<int64_t>());
+}
+
+inline bool is_float_type(int32_t dtype) {
+  return dtype == AGNES_F32 || dtype == AGNES_F16 || dtype == AGNES_BF16;
+}
+
+inline int64_t float_size(int32_t dtype) { return dtype == AGNES_F32 ? 4 : 2; }
+
+// Whether p and every stride bytes after it are multiples of `bytes`.
+inline bool aligned_rows(const void* p, int64_t stride_bytes, int64_t bytes) {
+  return (uintptr_t)p % (uintptr_t)bytes == 0 && stride_bytes % bytes == 0;
+}
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---- argument checks (ops.cu); each records a message for
+// agnes_last_error(NULL) when it fails ----------------------------------------
+
+agnes_status op_error(agnes_status s, const char* fmt, ...);
+
+// `p` is memory that the current or some other device can address as its own;
+// *device receives which.
+agnes_status op_device_of(const char* op, const char* name, const void* p, int* device);
+// `p` lies in the memory of `device`.
+agnes_status op_on_device(const char* op, const char* name, const void* p, int device);
+agnes_status op_float_type(const char* op, const char* name, int32_t dtype);
+agnes_status op_index_bits(const char* op, const char* name, int32_t bits);
+// `p` is aligned to one element of `size` bytes.
+agnes_status op_aligned(const char* op, const char* name, const void* p, int64_t size);
+// The launch's error, as a status.
+agnes_status op_launched(const char* op, cudaError_t e);
+// Multiprocessors of `device` (looked up once for each device).
+int op_num_sms(int device);
+
+#define OP_TRY(call)                          \
+  do {                                        \
+    const agnes_status op_s_ = (call);        \
+    if (op_s_ != AGNES_OK) return op_s_;      \
+  } while (0)
+
+// Sets bits of the caller's status word, where there is one.
+__device__ __forceinline__ void op_flag(int32_t* status, int32_t bits) {
+  if (status) atomicOr(status, bits);
+}
+
+}  // namespace agnes

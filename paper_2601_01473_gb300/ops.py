@@ -1,0 +1,224 @@
+"""The operators of a model that is trained on prepared hyperbatches
+(include/agnes_ops.h): learned node embeddings with their gradient,
+distillation from a teacher's top logits, and feature rows in microscaled 4-bit
+floating point.  Argument marshalling only; each call runs the library's CUDA
+kernels on the current stream (or ``stream``) and returns without waiting.
+
+What a kernel finds wrong with its data (an id past the end of its table, a wait
+that ran out) is kept on the device, in the int32 tensor ``status`` if one is
+given and else in one per device that ``check()`` reads and clears.
+
+With ``stream``, the results belong to that stream, and the inputs' memory is
+kept until it has come past the call; the inputs' values have to be there by
+then (order the stream after the one that makes them).
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from typing import NamedTuple
+
+import torch
+
+from .agnes import AgnesError, lib
+
+_FLOATS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_INDEXES = {torch.int32: 32, torch.int64: 64}
+BAD_INDEX, TIMEOUT = 1, 2  # AGNES_OP_*
+
+_status = {}  # device index -> int32 [1]
+
+
+class RowGrad(NamedTuple):
+    """The gradient of the selected rows of a table."""
+    ids: torch.Tensor    # int32 [n]: the distinct ids in ascending order, then -1
+    rows: torch.Tensor   # [n, dim]: their gradients, then zeros
+    count: torch.Tensor  # int32 [1]: how many
+
+
+def _streamed(op):
+    @functools.wraps(op)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return op(*args, **kw)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(stream):
+            result = op(*args, **kw)
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(stream)
+        return result
+    return call
+
+
+def _check(rc: int) -> None:
+    if rc != 0:
+        msg = lib().agnes_last_error(None)
+        raise AgnesError(rc, msg.decode() if msg else "")
+
+
+def _stream(device) -> int | None:
+    return torch.cuda.current_stream(device).cuda_stream or None
+
+
+def _status_word(status, device) -> int:
+    if status is None:
+        status = _status.get(device.index)
+        if status is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the first call on a device cannot be captured without a "
+                                   "status tensor")
+            status = torch.zeros(1, dtype=torch.int32, device=device)
+            torch.cuda.current_stream(device).synchronize()
+            _status[device.index] = status
+    elif status.dtype != torch.int32 or status.numel() < 1:
+        raise TypeError("status must be an int32 tensor")
+    elif status.device != device:
+        raise ValueError(f"status must be on {device}")
+    return status.data_ptr()
+
+
+def check(device=None) -> None:
+    """Waits for the device and raises AgnesError for what its kernels have found
+    wrong since the last check (calls without a ``status`` of their own)."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else \
+        torch.device(device)
+    index = torch.cuda.current_device() if device.index is None else device.index
+    torch.cuda.synchronize(index)
+    if index not in _status:
+        return
+    found = int(_status[index])
+    if not found:
+        return
+    _status[index].zero_()
+    torch.cuda.synchronize(index)
+    if found & TIMEOUT:
+        raise AgnesError(6, "a kernel's bounded wait ran out")
+    raise AgnesError(1, "an id or index is at or past the end of its range")
+
+
+def _rows(name: str, t: torch.Tensor, device=None) -> torch.Tensor:
+    """A matrix of floats whose rows' elements are adjacent."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _FLOATS:
+        raise TypeError(f"{name} must be a 2-D float32, float16 or bfloat16 tensor")
+    if t.numel() and ((t.shape[1] > 1 and t.stride(1) != 1)
+                      or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+        raise ValueError(f"{name} must have adjacent elements in each row")
+    return _on(name, t, device)
+
+
+def _on(name: str, t: torch.Tensor, device) -> torch.Tensor:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a CUDA device")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    return t
+
+
+def _stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _ids(name: str, t: torch.Tensor, device) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or t.dtype not in _INDEXES:
+        raise TypeError(f"{name} must be an int32 or int64 tensor")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return _on(name, t, device)
+
+
+def _float_type(dtype) -> int:
+    if dtype not in _FLOATS:
+        raise TypeError(f"{dtype} is not float32, float16 or bfloat16")
+    return _FLOATS[dtype]
+
+
+def _output(out, shape, dtype, device, name="out"):
+    """(tensor, stride) of an output: the caller's `out`, or a new one."""
+    if out is None:
+        _float_type(dtype)
+        return torch.empty(shape, dtype=dtype, device=device)
+    _rows(name, out, device)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(out.shape)}")
+    return out
+
+
+# ---- embeddings -------------------------------------------------------------------------
+
+
+@_streamed
+def embedding_lookup(table, ids, scale: float = 1.0, out_dtype=None, out=None, status=None):
+    """``scale * table[ids]`` (agnes_embedding_lookup): the rows of ``table``
+    [rows, dim] for ``ids`` of any shape, as [*ids.shape, dim] of ``out_dtype`` (the
+    table's by default).  A negative id gives zeros.  ``out``: [ids.numel(), dim],
+    its rows adjacent or not, written instead of a new tensor and returned."""
+    device = _rows("table", table).device
+    _ids("ids", ids, device)
+    n, dim = ids.numel(), table.shape[1]
+    y = _output(out, (n, dim), out_dtype or table.dtype, device)
+    if out is not None and out_dtype not in (None, out.dtype):
+        raise TypeError("out has another type than out_dtype")
+    _check(lib().agnes_embedding_lookup(
+        table.data_ptr(), _FLOATS[table.dtype], table.shape[0], _stride(table), dim,
+        ids.data_ptr(), _INDEXES[ids.dtype], n, scale, y.data_ptr(), _FLOATS[y.dtype], _stride(y),
+        _status_word(status, device), _stream(device)))
+    return y if out is not None or ids.dim() == 1 else y.view(*ids.shape, dim)
+
+
+def _grad_arguments(grad, ids):
+    device = _rows("grad", grad).device
+    _ids("ids", ids, device)
+    if ids.numel() != grad.shape[0]:
+        raise ValueError(f"{ids.numel()} ids for {grad.shape[0]} rows of grad")
+    return device
+
+
+def _grad_workspace(n, dim, device):
+    need = ctypes.c_int64()
+    _check(lib().agnes_embedding_grad_workspace(n, dim, ctypes.byref(need)))
+    return torch.empty(need.value, dtype=torch.uint8, device=device)
+
+
+@_streamed
+def embedding_grad(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=None, out=None,
+                   status=None):
+    """The gradient of ``embedding_lookup`` to the whole table (agnes_embedding_grad):
+    [num_rows, dim] of ``out_dtype`` (grad's by default), row v the scaled sum of the
+    rows of ``grad`` [n, dim] whose id (``ids``, n of any shape) is v, zeros where
+    there is none.  ``out``: written instead of a new tensor; contiguous."""
+    device = _grad_arguments(grad, ids)
+    n, dim = grad.shape
+    y = _output(out, (num_rows, dim), out_dtype or grad.dtype, device)
+    if out is not None and out_dtype not in (None, out.dtype):
+        raise TypeError("out has another type than out_dtype")
+    if not y.is_contiguous():
+        raise ValueError("out must be contiguous")
+    ws = _grad_workspace(n, dim, device)
+    _check(lib().agnes_embedding_grad(
+        grad.data_ptr(), _FLOATS[grad.dtype], _stride(grad), ids.data_ptr(), _INDEXES[ids.dtype],
+        n, num_rows, dim, scale, y.data_ptr(), _FLOATS[y.dtype], ws.data_ptr(), ws.numel(),
+        _status_word(status, device), _stream(device)))
+    return y
+
+
+@_streamed
+def embedding_grad_rows(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=None,
+                        status=None) -> RowGrad:
+    """The same gradient for the selected rows only (agnes_embedding_grad_rows), for
+    tables too large for a dense one.  Its shapes do not depend on the ids, so
+    ``table.index_add_(0, g.ids.clamp(min=0), g.rows, alpha=-lr)`` needs no read-back:
+    the rows past ``count`` are zeros."""
+    device = _grad_arguments(grad, ids)
+    n, dim = grad.shape
+    rows = _output(None, (n, dim), out_dtype or grad.dtype, device)
+    out_ids = torch.empty(n, dtype=torch.int32, device=device)
+    count = torch.empty(1, dtype=torch.int32, device=device)
+    ws = _grad_workspace(n, dim, device)
+    _check(lib().agnes_embedding_grad_rows(
+        grad.data_ptr(), _FLOATS[grad.dtype], _stride(grad), ids.data_ptr(), _INDEXES[ids.dtype],
+        n, num_rows, dim, scale, out_ids.data_ptr(), rows.data_ptr(), _FLOATS[rows.dtype],
+        count.data_ptr(), ws.data_ptr(), ws.numel(), _status_word(status, device),
+        _stream(device)))
+    return RowGrad(out_ids, rows, count)

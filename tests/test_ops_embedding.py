@@ -1,0 +1,316 @@
+"""Embedding lookup and its gradient (include/agnes_ops.h) against their
+formulas in 64 bits."""
+import pytest
+import torch
+
+from ops_support import FLOATS, U32, assert_within, gen, rounding
+from paper_2601_01473_gb300 import AgnesError, ops
+
+
+def _lookup_ref(table, ids, scale):
+    ids = ids.reshape(-1).long()
+    ref = torch.zeros((ids.numel(), table.shape[1]), dtype=torch.float64)
+    real = (ids >= 0) & (ids < table.shape[0])
+    ref[real] = table[ids[real]].double() * scale
+    return ref
+
+
+def _grad_ref(grad, ids, rows, scale):
+    """(d, sum of magnitudes, tokens) of every row of the table."""
+    ids = ids.reshape(-1).long()
+    real = (ids >= 0) & (ids < rows)
+    d = torch.zeros((rows, grad.shape[1]), dtype=torch.float64)
+    size = torch.zeros_like(d)
+    d.index_add_(0, ids[real], grad[real].double() * scale)
+    size.index_add_(0, ids[real], grad[real].double().abs() * abs(scale))
+    return d, size, torch.bincount(ids[real], minlength=rows).double()[:, None]
+
+
+def _grad_bound(d, size, tokens, dtype):
+    # a sum of m terms in fp32, in any order, the scale's rounding and the product's
+    return (tokens + 3) * U32 * size * 1.01 + rounding(d, dtype) * 1.01
+
+
+# ---- refusals (no GPU needed) ---------------------------------------------------------
+
+def test_arguments_are_checked_before_any_device_is_used():
+    table, ids = torch.zeros(4, 8), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="CUDA device"):
+        ops.embedding_lookup(table, ids)
+    with pytest.raises(TypeError, match="2-D"):
+        ops.embedding_lookup(table[0], ids)
+    with pytest.raises(TypeError, match="2-D"):
+        ops.embedding_lookup(table.double(), ids)
+    with pytest.raises(TypeError, match="2-D"):
+        ops.embedding_grad(torch.zeros(3, dtype=torch.int8), ids, 4)
+
+
+def test_the_c_entries_refuse_bad_arguments_without_a_device():
+    import ctypes
+
+    from paper_2601_01473_gb300 import build
+    build.build()
+    L = ops.lib()
+    need = ctypes.c_int64()
+    assert L.agnes_embedding_grad_workspace(10, 0, ctypes.byref(need)) == 1
+    assert L.agnes_embedding_grad_workspace(10, 4, None) == 1
+    assert L.agnes_embedding_grad_workspace(1 << 31, 4, ctypes.byref(need)) == 2
+    assert L.agnes_embedding_grad_workspace(1000, 4, ctypes.byref(need)) == 0
+    assert need.value >= 16 * 1000
+    args = [None, 0, 10, 8, 8, None, 32, 3, 1.0, None, 0, 8, None, None]
+    assert L.agnes_embedding_lookup(*args) == 1
+    assert b"NULL" in L.agnes_last_error(None)
+    for at, value, status in ((1, 7, 1), (10, -1, 1), (6, 16, 1), (4, 0, 1), (2, -1, 1), (7, -1, 1),
+                              (3, 7, 1), (11, 7, 1), (2, 1 << 31, 2), (7, 1 << 31, 2)):
+        bad = list(args)
+        bad[at] = value
+        assert L.agnes_embedding_lookup(*bad) == status, (at, value)
+    args[7] = 0  # nothing to do
+    assert L.agnes_embedding_lookup(*args) == 0
+
+
+# ---- lookup --------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tin", FLOATS)
+@pytest.mark.parametrize("tout", FLOATS)
+@pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (5, 3, 7), (1000, 77, 128), (333, 1000, 130),
+                                        (9, 5, 1000), (3, 4, 5001), (2048, 10, 2)])
+def test_lookup(cuda_device, tin, tout, n, rows, dim):
+    g = gen(n + dim)
+    table = torch.randn(rows, dim, generator=g).to(tin)
+    ids = torch.randint(-1, rows, (n,), generator=g, dtype=torch.int64)
+    for scale in (1.0, 11.25):
+        got = ops.embedding_lookup(table.to(cuda_device), ids.to(cuda_device), scale,
+                                   out_dtype=tout)
+        ref = _lookup_ref(table, ids, scale)
+        assert got.dtype == tout
+        # both scales are exact in fp32: the product's rounding, then the output's
+        assert_within(got, ref, ref.abs() * U32 + rounding(ref, tout) * 1.01)
+    ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+def test_lookup_strides_shapes_and_views(cuda_device, index):
+    g = gen(3)
+    wide = torch.randn(50, 3 * 40 + 1, generator=g)
+    ids = torch.randint(-1, 50, (4, 6), generator=g, dtype=index)
+    for first in (0, 1, 3):  # alignments of the rows' starts
+        table = wide.to(cuda_device)[:, first:first + 40]
+        out = torch.full((24, 100), 7.0, device=cuda_device)
+        got = ops.embedding_lookup(table, ids.to(cuda_device), 2.0, out=out[:, 5:45])
+        assert got.data_ptr() == out[:, 5:45].data_ptr()
+        assert torch.equal(out[:, 5:45].cpu(), _lookup_ref(table.cpu(), ids, 2.0).float())
+        assert (out[:, :5] == 7).all() and (out[:, 45:] == 7).all()
+        assert ops.embedding_lookup(table, ids.to(cuda_device)).shape == (4, 6, 40)
+    ops.check()
+
+
+@pytest.mark.gpu
+def test_lookup_special_values_and_empty(cuda_device):
+    table = torch.tensor([[float("inf"), float("nan"), -0.0, 65504.0]], device=cuda_device)
+    ids = torch.tensor([0, -1, -5], device=cuda_device)
+    got = ops.embedding_lookup(table, ids, 2.0, out_dtype=torch.float16).cpu()
+    assert got[0, 0] == float("inf") and got[0, 1].isnan() and got[0, 3] == float("inf")
+    assert torch.equal(got[1:], torch.zeros(2, 4, dtype=torch.float16))
+    assert ops.embedding_lookup(table, ids[:0]).shape == (0, 4)
+    assert (ops.embedding_lookup(table[:0], ids[1:]) == 0).all()
+    ops.check()
+
+
+@pytest.mark.gpu
+def test_lookup_past_the_end_is_reported(cuda_device):
+    table = torch.ones(10, 16, device=cuda_device)
+    for bad in (10, 2 ** 31 - 1):
+        ids = torch.tensor([3, bad, 9], device=cuda_device)
+        status = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+        got = ops.embedding_lookup(table, ids, status=status)
+        assert got.sum(1).tolist() == [16, 0, 16]
+        assert int(status) == ops.BAD_INDEX
+        ops.embedding_lookup(table, ids)
+        with pytest.raises(AgnesError, match="past the end"):
+            ops.check()
+        ops.check()  # cleared
+    huge = torch.tensor([2 ** 40], device=cuda_device)
+    assert (ops.embedding_lookup(table, huge) == 0).all()
+    with pytest.raises(AgnesError):
+        ops.check()
+
+
+@pytest.mark.gpu
+def test_lookup_offsets_past_32_bits(cuda_device):
+    rows, dim = 40_000_000, 128  # 5.1e9 elements
+    table = torch.empty(rows, dim, dtype=torch.float16, device=cuda_device)
+    ids = torch.tensor([0, 1, 16_777_216, 33_554_432, rows - 1], device=cuda_device)
+    want = torch.randn(5, dim, generator=gen(5)).half().to(cuda_device)
+    table[ids] = want
+    assert torch.equal(ops.embedding_lookup(table, ids), want)
+
+
+# ---- gradient --------------------------------------------------------------------------
+
+def _case(n, rows, dim, tin, skew, seed, index=torch.int32, padding=True):
+    g = gen(seed)
+    grad = torch.randn(n, dim, generator=g).to(tin)
+    u = torch.rand(n, generator=g, dtype=torch.float64)
+    ids = ((u ** skew) * rows).long().clamp(max=rows - 1) * 7919 % rows
+    if padding:
+        ids[torch.rand(n, generator=g) < 0.05] = -1
+    return grad, ids.to(index)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tin", FLOATS)
+@pytest.mark.parametrize("tout", FLOATS)
+@pytest.mark.parametrize("n,rows,dim,skew", [
+    (1, 1, 1, 1), (2, 5, 3, 1), (31, 7, 130, 1), (33, 1000, 16, 1), (64, 1, 33, 1),
+    (4096, 50, 24, 2), (4097, 5000, 8, 1), (9000, 3, 130, 1), (20000, 40000, 65, 3),
+    (100_000, 100, 9, 4)])
+def test_gradient(cuda_device, tin, tout, n, rows, dim, skew):
+    scale = 1.5
+    grad, ids = _case(n, rows, dim, tin, skew, n + dim)
+    d, size, tokens = _grad_ref(grad, ids, rows, scale)
+    bound = _grad_bound(d, size, tokens, tout)
+    dense = ops.embedding_grad(grad.to(cuda_device), ids.to(cuda_device), rows, scale,
+                               out_dtype=tout)
+    assert dense.dtype == tout
+    assert_within(dense, d, bound)
+    r = ops.embedding_grad_rows(grad.to(cuda_device), ids.to(cuda_device), rows, scale,
+                                out_dtype=tout)
+    hit = torch.nonzero(tokens[:, 0])[:, 0]
+    c = hit.numel()
+    assert r.count.tolist() == [c]
+    assert torch.equal(r.ids[:c].cpu().long(), hit) and (r.ids[c:] == -1).all()
+    assert torch.equal(r.rows[:c].cpu(), dense.cpu()[hit])  # the same sums, bit by bit
+    assert (r.rows[c:] == 0).all()
+    ops.check()
+
+
+@pytest.mark.gpu
+def test_gradient_of_a_large_table_and_wide_ids(cuda_device):
+    for rows in (2 ** 31 - 1, 10_000_000):
+        grad, ids = _case(30_000, rows, 12, torch.float32, 2, 5, torch.int64)
+        ids[17] = rows - 1
+        r = ops.embedding_grad_rows(grad.to(cuda_device), ids.to(cuda_device), rows)
+        real = ids >= 0
+        node, where = torch.unique(ids[real], return_inverse=True)
+        c = node.numel()
+        assert r.count.tolist() == [c] and torch.equal(r.ids[:c].cpu().long(), node)
+        d = torch.zeros((c, 12), dtype=torch.float64)
+        size = torch.zeros_like(d)
+        d.index_add_(0, where, grad[real].double())
+        size.index_add_(0, where, grad[real].double().abs())
+        tokens = torch.bincount(where).double()[:, None]
+        assert_within(r.rows[:c], d, _grad_bound(d, size, tokens, torch.float32))
+    ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 5000, 50_000])
+def test_gradient_without_any_real_id(cuda_device, n):
+    grad = torch.full((n, 10), float("nan"), device=cuda_device)
+    ids = torch.full((n,), -1, dtype=torch.int32, device=cuda_device)
+    assert (ops.embedding_grad(grad, ids, 20) == 0).all()
+    r = ops.embedding_grad_rows(grad, ids, 20)
+    assert r.count.tolist() == [0] and (r.ids == -1).all() and (r.rows == 0).all()
+    ops.check()
+
+
+@pytest.mark.gpu
+def test_gradient_of_nothing(cuda_device):
+    grad = torch.zeros(0, 10, device=cuda_device)
+    ids = torch.zeros(0, dtype=torch.int64, device=cuda_device)
+    assert (ops.embedding_grad(grad, ids, 20) == 0).all()
+    r = ops.embedding_grad_rows(grad, ids, 20)
+    assert r.count.tolist() == [0] and r.rows.shape == (0, 10)
+    assert ops.embedding_grad(grad, ids, 0).shape == (0, 10)
+
+
+@pytest.mark.gpu
+def test_gradient_past_the_end_is_left_out_and_reported(cuda_device):
+    for n in (6, 6000):
+        grad = torch.ones(n, 4, device=cuda_device)
+        ids = torch.full((n,), 3, device=cuda_device)
+        ids[1], ids[4] = 10, 2 ** 35
+        got = ops.embedding_grad(grad, ids, 10)
+        with pytest.raises(AgnesError, match="past the end"):
+            ops.check()
+        assert got[3].tolist() == [n - 2.0] * 4 and got.sum() == 4 * (n - 2)
+
+
+@pytest.mark.gpu
+def test_gradient_is_the_same_each_time_and_on_any_stream(cuda_device):
+    grad, ids = _case(200_000, 1000, 40, torch.float16, 4, 9)
+    grad, ids = grad.to(cuda_device), ids.to(cuda_device)
+    first = ops.embedding_grad(grad, ids, 1000, out_dtype=torch.float32)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        again = ops.embedding_grad(grad, ids, 1000, out_dtype=torch.float32, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(first, again)
+
+
+@pytest.mark.gpu
+def test_gradient_in_a_cuda_graph(cuda_device):
+    grad, ids = _case(10_000, 500, 32, torch.float32, 2, 11)
+    grad, ids = grad.to(cuda_device), ids.to(cuda_device)
+    ops.embedding_grad(grad, ids, 500)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ops.embedding_grad(grad, ids, 500)
+    grad.mul_(-2)
+    graph.replay()
+    assert torch.equal(got, ops.embedding_grad(grad, ids, 500))
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences(cuda_device):
+    """d(sum of g * lookup) / d table[v], by central differences in the table."""
+    rows, dim = 6, 5
+    g = gen(2)
+    table = torch.randn(rows, dim, generator=g)
+    ids = torch.tensor([0, 3, 3, -1, 5, 3, 0], dtype=torch.int32)
+    out_grad = torch.randn(7, dim, generator=g)
+    scale, h = 3.0, 0.5  # linear in the table: the step only scales the rounding
+    got = ops.embedding_grad(out_grad.to(cuda_device), ids.to(cuda_device), rows, scale).cpu()
+
+    def value(t):
+        y = ops.embedding_lookup(t.to(cuda_device), ids.to(cuda_device), scale).cpu()
+        return (y.double() * out_grad.double()).sum()
+
+    for v in range(rows):
+        for c in range(dim):
+            up, down = table.clone(), table.clone()
+            up[v, c] += h
+            down[v, c] -= h
+            step = float(up[v, c].double() - down[v, c].double())
+            slope = float(value(up) - value(down)) / step
+            # the lookups round to fp32: 21 products of about 10, over the step
+            assert abs(slope - float(got[v, c])) <= 21 * 10 * 2 * U32 * 4 / step + 1e-5
+
+
+@pytest.mark.gpu
+def test_refusals_on_the_device(cuda_device):
+    table = torch.zeros(10, 8, device=cuda_device)
+    ids = torch.zeros(4, dtype=torch.int32, device=cuda_device)
+    with pytest.raises(TypeError):
+        ops.embedding_lookup(table, ids.float())
+    with pytest.raises(TypeError):
+        ops.embedding_lookup(table, ids, out_dtype=torch.float64)
+    with pytest.raises(ValueError, match="contiguous"):
+        ops.embedding_lookup(table, torch.zeros(8, dtype=torch.int32, device=cuda_device)[::2])
+    with pytest.raises(ValueError, match="adjacent"):
+        ops.embedding_lookup(table.t(), ids)
+    with pytest.raises(ValueError, match="CUDA device"):
+        ops.embedding_lookup(table, ids.cpu())
+    with pytest.raises(ValueError, match="must be"):
+        ops.embedding_lookup(table, ids, out=torch.zeros(5, 8, device=cuda_device))
+    with pytest.raises(ValueError, match="rows of grad"):
+        ops.embedding_grad(torch.zeros(3, 8, device=cuda_device), ids, 10)
+    with pytest.raises(RuntimeError):  # a negative number of rows
+        ops.embedding_grad(torch.zeros(4, 8, device=cuda_device), ids, -1)
+    with pytest.raises(ValueError, match="contiguous"):
+        ops.embedding_grad(torch.zeros(4, 8, device=cuda_device), ids, 10,
+                           out=torch.zeros(10, 16, device=cuda_device)[:, :8])

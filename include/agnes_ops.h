@@ -86,6 +86,62 @@ agnes_status agnes_embedding_grad_rows(const void* grad, int32_t grad_dtype, int
 /* Bytes of workspace that both take for n tokens of dim values. */
 agnes_status agnes_embedding_grad_workspace(int64_t n, int64_t dim, int64_t* bytes);
 
+/* The loss of a student's logits against a teacher's top logits, row by row:
+ * with p = softmax(teacher / T) over the row's entries, q = softmax(logits / T)
+ * over all classes,
+ *   loss = T^2 sum_k p_k (ln p_k - ln q[index_k]).
+ * An entry with a negative index is absent; so is one with an index >= classes,
+ * which also sets AGNES_OP_BAD_INDEX.  Entries of a row that name the same class
+ * each count.  A row without an entry (or with teacher logits of -inf only), and
+ * one whose logits are all -inf, has loss 0 and gradient 0.  A logit of -inf has
+ * q = 0: the loss is +inf where p is not 0 there.  Where a logit or a present
+ * teacher logit is NaN or +inf, the row's loss and gradient are NaN.
+ * A label is the entry (label, 0) with top = 1 and T = 1: its loss is the cross
+ * entropy, and label -1 is ignored.
+ *  logits   rows x classes of logits_dtype, logits_stride apart;
+ *           1 <= classes <= AGNES_DISTILL_MAX_CLASSES.
+ *  teacher  rows x top of teacher_dtype, contiguous; 0 <= top <=
+ *           AGNES_DISTILL_MAX_TOP.
+ *  index    rows x top of index_bits (32 or 64) bits, contiguous.
+ *  temperature  T > 0.
+ *  loss     rows floats.
+ *  stats    rows x 2 floats, 8-byte aligned: each row's largest logit and its
+ *           sum of exp((x - largest) / T), for agnes_distill_grad.
+ * Errors: EINVAL, ERANGE, ECUDA. */
+#define AGNES_DISTILL_MAX_TOP 512
+#define AGNES_DISTILL_MAX_CLASSES (1 << 30)
+agnes_status agnes_distill_loss(const void* logits, int32_t logits_dtype, int64_t logits_stride,
+                                int64_t rows, int64_t classes, const void* teacher,
+                                int32_t teacher_dtype, const void* index, int32_t index_bits,
+                                int64_t top, float temperature, float* loss, float* stats,
+                                int32_t* status, void* cuda_stream);
+
+/* Its gradient to the logits, with the loss of row r weighted by
+ * w_r = weight_scale * weight[r] (weight NULL: weight_scale):
+ *   out[r][v] = w_r T (q_v sum_k p_k - sum_{k: index_k = v} p_k).
+ *  stats    as agnes_distill_loss left it for the same arguments.
+ *  out      rows x classes of out_dtype, out_stride apart.  It may be the logits
+ *           themselves (the same address, type and stride).
+ * Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_distill_grad(const void* logits, int32_t logits_dtype, int64_t logits_stride,
+                                int64_t rows, int64_t classes, const void* teacher,
+                                int32_t teacher_dtype, const void* index, int32_t index_bits,
+                                int64_t top, float temperature, const float* stats,
+                                const float* weight, float weight_scale, void* out,
+                                int32_t out_dtype, int64_t out_stride, int32_t* status,
+                                void* cuda_stream);
+
+/* Both in one call, for a training step that knows its rows' weights: the
+ * logits are read from memory once (up to 8 CTAs' shared memory a row, 1.6 MB).
+ * Arguments, in-place use and errors as above. */
+agnes_status agnes_distill_loss_grad(const void* logits, int32_t logits_dtype,
+                                     int64_t logits_stride, int64_t rows, int64_t classes,
+                                     const void* teacher, int32_t teacher_dtype, const void* index,
+                                     int32_t index_bits, int64_t top, float temperature,
+                                     const float* weight, float weight_scale, float* loss,
+                                     void* out, int32_t out_dtype, int64_t out_stride,
+                                     int32_t* status, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

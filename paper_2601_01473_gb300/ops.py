@@ -222,3 +222,81 @@ def embedding_grad_rows(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=
         count.data_ptr(), ws.data_ptr(), ws.numel(), _status_word(status, device),
         _stream(device)))
     return RowGrad(out_ids, rows, count)
+
+
+# ---- distillation -------------------------------------------------------------------------
+
+
+def _distill_arguments(logits, teacher, index):
+    device = _rows("logits", logits).device
+    _rows("teacher", teacher, device)
+    _ids("index", index, device)
+    if not teacher.is_contiguous():
+        raise ValueError("teacher must be contiguous")
+    if teacher.shape[0] != logits.shape[0] or index.shape != teacher.shape:
+        raise ValueError(f"teacher {tuple(teacher.shape)} and index {tuple(index.shape)} must be "
+                         f"[{logits.shape[0]}, top]")
+    return device, (logits.data_ptr(), _FLOATS[logits.dtype], _stride(logits), logits.shape[0],
+                    logits.shape[1], teacher.data_ptr(), _FLOATS[teacher.dtype], index.data_ptr(),
+                    _INDEXES[index.dtype], teacher.shape[1])
+
+
+def _weight_arguments(weight, rows, device):
+    if not isinstance(weight, torch.Tensor):
+        return None, float(weight)
+    if weight.dtype != torch.float32 or weight.shape != (rows,) or not weight.is_contiguous():
+        raise TypeError(f"weight must be a number or a contiguous float32 tensor [{rows}]")
+    return _on("weight", weight, device).data_ptr(), 1.0
+
+
+@_streamed
+def distill_loss(logits, teacher, index, temperature: float = 1.0, status=None):
+    """Each row's loss against the teacher's top logits (agnes_distill_loss):
+    ``logits`` [rows, classes], ``teacher`` [rows, top] with their classes ``index``
+    (negative: absent).  Returns (loss float32 [rows], stats float32 [rows, 2]);
+    ``distill_grad`` takes the stats."""
+    device, arguments = _distill_arguments(logits, teacher, index)
+    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=device)
+    stats = torch.empty((logits.shape[0], 2), dtype=torch.float32, device=device)
+    _check(lib().agnes_distill_loss(*arguments, temperature, loss.data_ptr(), stats.data_ptr(),
+                                    _status_word(status, device), _stream(device)))
+    return loss, stats
+
+
+@_streamed
+def distill_grad(logits, teacher, index, stats, weight=1.0, temperature: float = 1.0,
+                 out_dtype=None, out=None, status=None):
+    """The gradient of sum(weight * loss) to the logits (agnes_distill_grad):
+    ``weight`` a number or float32 [rows], ``stats`` from ``distill_loss``.  ``out``:
+    written instead of a new tensor of ``out_dtype`` (the logits' by default); it may
+    be ``logits``."""
+    device, arguments = _distill_arguments(logits, teacher, index)
+    if stats.dtype != torch.float32 or stats.shape != (logits.shape[0], 2) or \
+            not stats.is_contiguous():
+        raise TypeError("stats must be what distill_loss returned")
+    _on("stats", stats, device)
+    w, scale = _weight_arguments(weight, logits.shape[0], device)
+    y = _output(out, logits.shape, out_dtype or logits.dtype, device)
+    if out is not None and out_dtype not in (None, out.dtype):
+        raise TypeError("out has another type than out_dtype")
+    _check(lib().agnes_distill_grad(*arguments, temperature, stats.data_ptr(), w, scale,
+                                    y.data_ptr(), _FLOATS[y.dtype], _stride(y),
+                                    _status_word(status, device), _stream(device)))
+    return y
+
+
+@_streamed
+def distill_loss_grad(logits, teacher, index, weight=1.0, temperature: float = 1.0,
+                      out_dtype=None, out=None, status=None):
+    """(loss, gradient) in one call, the logits read once (agnes_distill_loss_grad);
+    arguments as for ``distill_loss`` and ``distill_grad``."""
+    device, arguments = _distill_arguments(logits, teacher, index)
+    w, scale = _weight_arguments(weight, logits.shape[0], device)
+    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=device)
+    y = _output(out, logits.shape, out_dtype or logits.dtype, device)
+    if out is not None and out_dtype not in (None, out.dtype):
+        raise TypeError("out has another type than out_dtype")
+    _check(lib().agnes_distill_loss_grad(*arguments, temperature, w, scale, loss.data_ptr(),
+                                         y.data_ptr(), _FLOATS[y.dtype], _stride(y),
+                                         _status_word(status, device), _stream(device)))
+    return loss, y

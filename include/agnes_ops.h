@@ -142,6 +142,45 @@ agnes_status agnes_distill_loss_grad(const void* logits, int32_t logits_dtype,
                                      void* out, int32_t out_dtype, int64_t out_stride,
                                      int32_t* status, void* cuda_stream);
 
+/* Rows in microscaled 4-bit floating point (OCP MX, MXFP4).  Blocks of 32
+ * values share a scale 2^(byte - 127), byte - 127 = floor(log2(largest magnitude))
+ * - 2 and at least -127; each value is a 4-bit code, sign and magnitude of 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 (codes 0 to 7, the sign in bit 3) times the scale.  A row of
+ * dim values is mx4_row_bytes(dim) bytes: with b = ceil(dim / 32), 16 b bytes of
+ * codes (the even value in a byte's low half; codes past dim are 0), b scale
+ * bytes, and zeros up to a multiple of 16 bytes.  Rows are 16-byte aligned, a
+ * multiple of 16 bytes apart.  So a matrix of them can be loaded as a graph's
+ * features (row_bytes / 2 "fp16" values a row): they are gathered byte for byte. */
+agnes_status agnes_mx4_row_bytes(int64_t dim, int64_t* bytes);
+
+/* Rounds rows of dim values of dtype (stride apart) to 4-bit rows (out_stride
+ * bytes apart): each value to the nearest magnitude, ties to the even code, above
+ * 6 scales to 6.  A block with an infinity or NaN gets scale byte 255 and codes
+ * 0: it stands for NaN.  Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_mx4_quantize(const void* x, int32_t dtype, int64_t stride, int64_t rows,
+                                int64_t dim, void* out, int64_t out_stride, void* cuda_stream);
+
+/* The values that 4-bit rows (stride bytes apart) stand for, rounded to dtype.
+ * Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_mx4_dequantize(const void* x, int64_t stride, int64_t rows, int64_t dim,
+                                  void* out, int32_t dtype, int64_t out_stride,
+                                  void* cuda_stream);
+
+/* out[r][j] = sum_i x[r][i] w[j][i] (+ bias[j]): rows of 4-bit values times 4-bit
+ * weights, for example a model's first layer over gathered rows.  Products are
+ * exact and summed in fp32 on the tensor cores (tcgen05, block-scaled).
+ *  x      rows 4-bit rows of dim values, x_stride bytes apart.
+ *  w      width 4-bit rows of dim values, w_stride bytes apart.
+ *  bias   width floats, or NULL.
+ *  out    rows x width of out_dtype, out_stride apart.
+ *  status AGNES_OP_TIMEOUT where a wait inside the kernel ran out.
+ * 0 <= rows, 0 <= width < 2^31 - 255; 1 <= dim <= 2^26.
+ * Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_mx4_linear(const void* x, int64_t x_stride, int64_t rows, const void* w,
+                              int64_t w_stride, int64_t width, int64_t dim, const float* bias,
+                              void* out, int32_t out_dtype, int64_t out_stride, int32_t* status,
+                              void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -160,6 +160,11 @@ SIGNATURES = {
                             _F32, _P, _I32, _I64, _P, _P], ctypes.c_int),
     "agnes_distill_loss_grad": ([_P, _I32, _I64, _I64, _I64, _P, _I32, _P, _I32, _I64, _F32, _P,
                                  _F32, _P, _P, _I32, _I64, _P, _P], ctypes.c_int),
+    "agnes_mx4_row_bytes": ([_I64, ctypes.POINTER(_I64)], ctypes.c_int),
+    "agnes_mx4_quantize": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _P], ctypes.c_int),
+    "agnes_mx4_dequantize": ([_P, _I64, _I64, _I64, _P, _I32, _I64, _P], ctypes.c_int),
+    "agnes_mx4_linear": ([_P, _I64, _I64, _P, _I64, _I64, _I64, _P, _P, _I32, _I64, _P, _P],
+                         ctypes.c_int),
     "agnes_embedding_grad_workspace": ([_I64, _I64, ctypes.POINTER(_I64)], ctypes.c_int),
     "agnes_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "agnes_last_error": ([_P], ctypes.c_char_p),

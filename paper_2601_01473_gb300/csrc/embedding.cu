@@ -19,34 +19,21 @@ namespace {
 
 constexpr int kLookupThreads = 256;
 constexpr int kLookupItems = 4;  // vectors per thread, loaded before the first is stored
-constexpr int kLookupBlock = kLookupThreads * kLookupItems;
+static_assert(kLookupThreads * kLookupItems == kFlat, "a block's vectors");
 
-// A block takes kLookupBlock vectors of kVec elements of the output in order.
-// vpr: vectors per row; inv_vpr = ceil(2^32 / vpr) where vpr < kLookupBlock.
+// A block takes kFlat vectors of kVec elements of the output in order.  vpr:
+// vectors per row.
 template <typename TIn, typename TOut, typename Id, int kVec>
 __global__ void __launch_bounds__(kLookupThreads)
 lookup_kernel(const TIn* __restrict__ table, int64_t rows, int64_t table_stride, int32_t vpr,
               uint32_t inv_vpr, const Id* __restrict__ ids, int64_t n, float scale,
               TOut* __restrict__ out, int64_t out_stride, int32_t* status) {
-  const int64_t first = (int64_t)blockIdx.x * kLookupBlock;
-  const int64_t t0 = first / vpr;
-  const uint32_t c0 = (uint32_t)(first - t0 * vpr);
+  const FlatRows flat(blockIdx.x, vpr, inv_vpr);
   int64_t token[kLookupItems], id[kLookupItems];
   uint32_t col[kLookupItems];
 #pragma unroll
   for (int u = 0; u < kLookupItems; ++u) {
-    // the row within the block: below 2 kLookupBlock / vpr + 1, and the product
-    // with the inverse is exact as q * vpr < 2^32
-    const uint32_t q = c0 + threadIdx.x + u * kLookupThreads;
-    uint32_t r;
-    if (vpr == 1)
-      r = q;
-    else if (vpr < kLookupBlock)
-      r = __umulhi(q, inv_vpr);
-    else
-      r = q >= (uint32_t)vpr;
-    col[u] = q - r * (uint32_t)vpr;
-    token[u] = t0 + r;
+    flat.at(threadIdx.x + u * kLookupThreads, &token[u], &col[u]);
     id[u] = token[u] < n ? (int64_t)__ldg(ids + token[u]) : -1;
   }
   Vec<TIn, kVec> x[kLookupItems];
@@ -840,16 +827,15 @@ agnes_status agnes_embedding_lookup(const void* table, int32_t table_dtype, int6
       using TOut = typename decltype(tout)::type;
       return with_vector<TIn, TOut>(dim, table, table_stride, out, out_stride, [&](auto v) {
         constexpr int kVec = decltype(v)::value;
-        const int64_t vpr = dim / kVec, blocks = ceil_div(n * vpr, kLookupBlock);
+        const int64_t vpr = dim / kVec, blocks = ceil_div(n * vpr, kFlat);
         if (blocks > kMaxTokens) {
           too_many = true;
           return cudaSuccess;
         }
-        const uint32_t inv = (uint32_t)(((1ull << 32) + vpr - 1) / vpr);
         return with_index_type(ids_bits, [&](auto id) {
           using Id = typename decltype(id)::type;
           lookup_kernel<TIn, TOut, Id, kVec><<<(unsigned)blocks, kLookupThreads, 0, st>>>(
-              (const TIn*)table, rows, table_stride, (int32_t)vpr, inv, (const Id*)ids, n, scale,
+              (const TIn*)table, rows, table_stride, (int32_t)vpr, flat_inverse(vpr), (const Id*)ids, n, scale,
               (TOut*)out, out_stride, status);
           return cudaGetLastError();
         });

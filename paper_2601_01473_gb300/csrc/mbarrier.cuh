@@ -41,7 +41,7 @@ constexpr int kMbarFastPolls = 64;
 constexpr int kMbarSlowPolls = 1 << 24;
 constexpr uint64_t kMbarWaitNs = 1000000000;
 
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
   const uint64_t start = global_ns();
   for (int it = 0; it < kMbarSlowPolls; ++it) {
     if (mbar_poll(bar, parity)) return true;

@@ -1,0 +1,251 @@
+// mx4.cu -- rows to microscaled 4-bit floating point and back
+// (include/agnes_ops.h; the format is in mx4.cuh).
+//
+// A thread takes eight values, so four threads share a block of 32: its largest
+// magnitude is found by two exchanges within the warp.  Magnitudes are compared
+// as bit patterns, which order as the numbers do and put what is not finite on
+// top.
+#include <type_traits>
+
+#include "mx4.cuh"
+#include "ops_common.cuh"
+
+namespace agnes {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kItems = kFlat / kThreads;  // groups of eight values per thread
+
+// The eight values from column col0 of a row, zeros past its end; kWide: the row
+// is 16-byte aligned and a whole number of eights.
+template <typename T, bool kWide>
+__device__ __forceinline__ void load8(const T* row, int32_t col0, int32_t dim, float (&f)[8]) {
+  if constexpr (kWide) {
+    constexpr int kN = 16 / sizeof(T);
+#pragma unroll
+    for (int h = 0; h < 8 / kN; ++h) {
+      Vec<T, kN> v;
+      if (col0 < dim) {
+        v = *(const Vec<T, kN>*)(row + col0 + h * kN);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v.v[e] = from_f32<T>(0.f);
+      }
+#pragma unroll
+      for (int e = 0; e < kN; ++e) f[h * kN + e] = to_f32(v.v[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = col0 + e < dim ? to_f32(row[col0 + e]) : 0.f;
+  }
+}
+
+// groups: 4 * blocks, groups of eight values per row.
+template <typename T, bool kWide>
+__global__ void __launch_bounds__(kThreads)
+quantize_kernel(const T* __restrict__ x, int64_t rows, int64_t stride, int32_t dim, int32_t groups,
+                uint32_t inv_groups, uint8_t* __restrict__ out, int64_t out_stride,
+                int32_t row_bytes) {
+  const FlatRows flat(blockIdx.x, groups, inv_groups);
+  int64_t row[kItems];
+  uint32_t group[kItems];
+  float f[kItems][8];
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    flat.at(threadIdx.x + u * kThreads, &row[u], &group[u]);
+    if (row[u] < rows) {
+      load8<T, kWide>(x + row[u] * stride, (int32_t)group[u] * 8, dim, f[u]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[u][e] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[u][e]) & 0x7fffffffu);
+    // a block's four groups are in four lanes: a row has a multiple of four
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t exponent = top >> 23;  // floor(log2) + 127 of a normal magnitude
+    const bool fine = exponent < 255;
+    const uint32_t byte = !fine ? 255u : exponent > 2 ? exponent - 2 : 0u;
+    // 1 / scale = 2^(127 - byte): a normal number, so the products are exact
+    // where they are not far below the smallest step
+    const float inv = fine ? __uint_as_float((254u - byte) << 23) : 0.f;
+    uint32_t codes = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+      codes |= mx4_codes(f[u][e] * inv, f[u][e + 1] * inv) << (4 * e);
+    if (!fine) codes = 0;
+    if (row[u] >= rows) continue;
+    uint8_t* to = out + row[u] * out_stride;
+    *(uint32_t*)(to + group[u] * 4) = codes;
+    const int32_t blocks = groups >> 2;
+    if ((group[u] & 3) == 0) to[blocks * 16 + (group[u] >> 2)] = (uint8_t)byte;
+    if (group[u] == 0)
+      for (int32_t b = blocks * 17; b < row_bytes; ++b) to[b] = 0;
+  }
+}
+
+template <typename T, bool kWide>
+__global__ void __launch_bounds__(kThreads)
+dequantize_kernel(const uint8_t* __restrict__ x, int64_t rows, int64_t stride, int32_t dim,
+                  int32_t groups, uint32_t inv_groups, T* __restrict__ out, int64_t out_stride) {
+  const FlatRows flat(blockIdx.x, groups, inv_groups);
+  const int32_t blocks = (dim + kMxBlock - 1) / kMxBlock;
+  int64_t row[kItems];
+  uint32_t group[kItems], codes[kItems], byte[kItems];
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    flat.at(threadIdx.x + u * kThreads, &row[u], &group[u]);
+    codes[u] = byte[u] = 0;
+    if (row[u] < rows) {
+      const uint8_t* from = x + row[u] * stride;
+      codes[u] = __ldg((const uint32_t*)from + group[u]);
+      byte[u] = __ldg(from + (int64_t)blocks * 16 + (group[u] >> 2));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    if (row[u] >= rows) continue;
+    const float scale = mx4_scale(byte[u]);
+    __half2 h[4];
+    mx4_values(codes[u], h);
+    T y[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = __half22float2(h[e]);
+      y[2 * e] = from_f32<T>(f.x * scale);
+      y[2 * e + 1] = from_f32<T>(f.y * scale);
+    }
+    T* to = out + row[u] * out_stride + (int64_t)group[u] * 8;
+    if constexpr (kWide) {
+      constexpr int kN = 16 / sizeof(T);
+#pragma unroll
+      for (int p = 0; p < 8 / kN; ++p) {
+        Vec<T, kN> v;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v.v[e] = y[p * kN + e];
+        ((Vec<T, kN>*)to)[p] = v;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if ((int32_t)group[u] * 8 + e < dim) to[e] = y[e];
+    }
+  }
+}
+
+constexpr int64_t kMaxDim = 1 << 26;  // 2^26 / 32 blocks of 17 bytes fit 32 bits
+constexpr int64_t kMaxRows = 0x7fffffff - 255;
+
+agnes_status check_rows(const char* op, int64_t rows, int64_t dim, int64_t stride,
+                        int64_t packed_stride) {
+  if (rows < 0 || dim < 1)
+    return op_error(AGNES_EINVAL, "%s: rows %lld, dim %lld", op, (long long)rows, (long long)dim);
+  if (rows > kMaxRows || dim > kMaxDim)
+    return op_error(AGNES_ERANGE, "%s: rows %lld, dim %lld are too large", op, (long long)rows,
+                    (long long)dim);
+  if (rows > 1 && stride < dim)
+    return op_error(AGNES_EINVAL, "%s: a stride of %lld is below dim %lld", op, (long long)stride,
+                    (long long)dim);
+  return mx4_check_stride(op, "packed", rows, dim, packed_stride);
+}
+
+// f(rows per call's groups, inverse, blocks) after the sizes' checks.
+struct MxGrid {
+  int32_t groups;
+  uint32_t inv;
+  int64_t ctas;
+};
+
+MxGrid mx_grid(int64_t rows, int64_t groups) {
+  return {(int32_t)groups, flat_inverse(groups), ceil_div(rows * groups, kFlat)};
+}
+
+}  // namespace
+
+agnes_status mx4_check_stride(const char* op, const char* name, int64_t rows, int64_t dim,
+                              int64_t stride) {
+  if (rows > 1 && (stride < mx4_row_bytes(dim) || stride % 16))
+    return op_error(AGNES_EINVAL,
+                    "%s: a stride of %lld bytes of %s is not a multiple of 16 of at least %lld", op,
+                    (long long)stride, name, (long long)mx4_row_bytes(dim));
+  return AGNES_OK;
+}
+
+}  // namespace agnes
+
+using namespace agnes;
+
+extern "C" {
+
+agnes_status agnes_mx4_row_bytes(int64_t dim, int64_t* bytes) {
+  const char* op = "agnes_mx4_row_bytes";
+  if (!bytes) return op_error(AGNES_EINVAL, "%s: bytes is NULL", op);
+  OP_TRY(check_rows(op, 0, dim, dim, 0));
+  *bytes = mx4_row_bytes(dim);
+  return AGNES_OK;
+}
+
+agnes_status agnes_mx4_quantize(const void* x, int32_t dtype, int64_t stride, int64_t rows,
+                                int64_t dim, void* out, int64_t out_stride, void* cuda_stream) {
+  const char* op = "agnes_mx4_quantize";
+  OP_TRY(check_rows(op, rows, dim, stride, out_stride));
+  OP_TRY(op_float_type(op, "x", dtype));
+  if (rows == 0) return AGNES_OK;
+  int device = -1;
+  OP_TRY(op_device_of(op, "x", x, &device));
+  OP_TRY(op_on_device(op, "out", out, device));
+  OP_TRY(op_aligned(op, "x", x, float_size(dtype)));
+  OP_TRY(op_aligned(op, "out", out, 16));
+  DeviceGuard dg(device);
+  if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
+  const MxGrid g = mx_grid(rows, 4 * mx4_blocks(dim));
+  if (g.ctas > 0x7fffffff) return op_error(AGNES_ERANGE, "%s: rows * dim is too large", op);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = with_float_type(dtype, [&](auto t) {
+    using T = typename decltype(t)::type;
+    const bool wide = dim % 8 == 0 && aligned_rows(x, rows > 1 ? stride * (int64_t)sizeof(T) : 0, 16);
+    (wide ? quantize_kernel<T, true> : quantize_kernel<T, false>)<<<(unsigned)g.ctas, kThreads, 0,
+                                                                    st>>>(
+        (const T*)x, rows, stride, (int32_t)dim, g.groups, g.inv, (uint8_t*)out, out_stride,
+        (int32_t)mx4_row_bytes(dim));
+    return cudaGetLastError();
+  });
+  return op_launched(op, e);
+}
+
+agnes_status agnes_mx4_dequantize(const void* x, int64_t stride, int64_t rows, int64_t dim,
+                                  void* out, int32_t dtype, int64_t out_stride,
+                                  void* cuda_stream) {
+  const char* op = "agnes_mx4_dequantize";
+  OP_TRY(check_rows(op, rows, dim, out_stride, stride));
+  OP_TRY(op_float_type(op, "out", dtype));
+  if (rows == 0) return AGNES_OK;
+  int device = -1;
+  OP_TRY(op_device_of(op, "x", x, &device));
+  OP_TRY(op_on_device(op, "out", out, device));
+  OP_TRY(op_aligned(op, "x", x, 16));
+  OP_TRY(op_aligned(op, "out", out, float_size(dtype)));
+  DeviceGuard dg(device);
+  if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
+  const MxGrid g = mx_grid(rows, ceil_div(dim, 8));
+  if (g.ctas > 0x7fffffff) return op_error(AGNES_ERANGE, "%s: rows * dim is too large", op);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = with_float_type(dtype, [&](auto t) {
+    using T = typename decltype(t)::type;
+    const bool wide =
+        dim % 8 == 0 && aligned_rows(out, rows > 1 ? out_stride * (int64_t)sizeof(T) : 0, 16);
+    (wide ? dequantize_kernel<T, true> : dequantize_kernel<T, false>)<<<(unsigned)g.ctas, kThreads,
+                                                                        0, st>>>(
+        (const uint8_t*)x, rows, stride, (int32_t)dim, g.groups, g.inv, (T*)out, out_stride);
+    return cudaGetLastError();
+  });
+  return op_launched(op, e);
+}
+
+}  // extern "C"

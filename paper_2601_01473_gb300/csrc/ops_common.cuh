@@ -39,6 +39,37 @@ struct alignas(sizeof(T) * N) Vec {
   T v[N];
 };
 
+// A block of kFlat consecutive items of rows of `per_row` items each, row after
+// row: where an item is.  Items are numbered from the block's first.
+constexpr int kFlat = 1024;
+struct FlatRows {
+  int64_t row0;
+  uint32_t col0, per_row, inv;
+
+  // inv = ceil(2^32 / per_row), from the host (flat_inverse)
+  __device__ FlatRows(int64_t block, int32_t per_row_, uint32_t inv_)
+      : per_row((uint32_t)per_row_), inv(inv_) {
+    const int64_t first = block * kFlat;
+    row0 = first / per_row_;
+    col0 = (uint32_t)(first - row0 * per_row_);
+  }
+  __device__ void at(uint32_t item, int64_t* row, uint32_t* col) const {
+    const uint32_t q = col0 + item;  // < per_row + kFlat
+    uint32_t r;
+    if (per_row == 1)
+      r = q;
+    else if (per_row < kFlat)
+      r = __umulhi(q, inv);  // q / per_row: exact, as q * per_row < 2^32
+    else
+      r = q >= per_row;
+    *row = row0 + r;
+    *col = q - r * per_row;
+  }
+};
+inline uint32_t flat_inverse(int64_t per_row) {
+  return (uint32_t)(((1ull << 32) + (uint64_t)per_row - 1) / (uint64_t)per_row);
+}
+
 // One of an operator's float types, as a type.
 template <typename T>
 struct TypeTag {
@@ -89,6 +120,9 @@ agnes_status op_index_bits(const char* op, const char* name, int32_t bits);
 agnes_status op_aligned(const char* op, const char* name, const void* p, int64_t size);
 // The launch's error, as a status.
 agnes_status op_launched(const char* op, cudaError_t e);
+// A stride in bytes between 4-bit rows of dim values (mx4.cu).
+agnes_status mx4_check_stride(const char* op, const char* name, int64_t rows, int64_t dim,
+                              int64_t stride);
 // Multiprocessors of `device` (looked up once for each device).
 int op_num_sms(int device);
 

@@ -300,3 +300,80 @@ def distill_loss_grad(logits, teacher, index, weight=1.0, temperature: float = 1
                                          y.data_ptr(), _FLOATS[y.dtype], _stride(y),
                                          _status_word(status, device), _stream(device)))
     return loss, y
+
+
+# ---- 4-bit rows -----------------------------------------------------------------------------
+
+
+def mx4_row_bytes(dim: int) -> int:
+    """Bytes of a 4-bit row of ``dim`` values (agnes_mx4_row_bytes)."""
+    need = ctypes.c_int64()
+    _check(lib().agnes_mx4_row_bytes(dim, ctypes.byref(need)))
+    return need.value
+
+
+def _packed(name, t, dim, device=None):
+    """A matrix of 4-bit rows: uint8 [rows, mx4_row_bytes(dim)], or the same bytes as
+    float16 or float32 "features", as a graph gathers them."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or \
+            t.dtype not in (torch.uint8, torch.float16, torch.float32):
+        raise TypeError(f"{name} must be a 2-D tensor of 4-bit rows")
+    size = t.element_size()
+    if dim < 1 or t.shape[1] * size != (dim + 31) // 32 * 17 + -((dim + 31) // 32 * 17) % 16:
+        raise ValueError(f"{name} has rows of {t.shape[1] * size} bytes, not those of {dim} values")
+    if t.numel() and (t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+        raise ValueError(f"{name} must have adjacent bytes in each row")
+    return _on(name, t, device)
+
+
+def _stride_bytes(t) -> int:
+    return _stride(t) * t.element_size()
+
+
+@_streamed
+def mx4_quantize(x, out=None):
+    """Rows of ``x`` [rows, dim] rounded to microscaled 4-bit rows (agnes_mx4_quantize):
+    uint8 [rows, mx4_row_bytes(dim)].  ``.view(torch.float16)`` of them makes a graph's
+    features."""
+    device = _rows("x", x).device
+    rows, dim = x.shape
+    if out is None:
+        out = torch.empty((rows, mx4_row_bytes(dim)), dtype=torch.uint8, device=device)
+    else:
+        _packed("out", out, dim, device)
+        if out.shape[0] != rows:
+            raise ValueError(f"out has {out.shape[0]} rows, not {rows}")
+    _check(lib().agnes_mx4_quantize(x.data_ptr(), _FLOATS[x.dtype], _stride(x), rows, dim,
+                                    out.data_ptr(), _stride_bytes(out), _stream(device)))
+    return out
+
+
+@_streamed
+def mx4_dequantize(x, dim: int, out_dtype=torch.float32, out=None):
+    """The values [rows, dim] that 4-bit rows stand for (agnes_mx4_dequantize)."""
+    device = _packed("x", x, dim).device
+    y = _output(out, (x.shape[0], dim), out_dtype if out is None else out.dtype, device)
+    _check(lib().agnes_mx4_dequantize(x.data_ptr(), _stride_bytes(x), x.shape[0], dim,
+                                      y.data_ptr(), _FLOATS[y.dtype], _stride(y),
+                                      _stream(device)))
+    return y
+
+
+@_streamed
+def mx4_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, status=None):
+    """``x @ w.T + bias`` of 4-bit rows (agnes_mx4_linear): ``x`` [rows, bytes], for example a
+    minibatch's gathered features, ``w`` [width, bytes], both of ``dim`` values a row;
+    ``bias`` float32 [width] or None.  Returns [rows, width]."""
+    device = _packed("x", x, dim).device
+    _packed("w", w, dim, device)
+    rows, width = x.shape[0], w.shape[0]
+    if bias is not None:
+        if bias.dtype != torch.float32 or bias.shape != (width,) or not bias.is_contiguous():
+            raise TypeError(f"bias must be a contiguous float32 tensor [{width}]")
+        _on("bias", bias, device)
+    y = _output(out, (rows, width), out_dtype if out is None else out.dtype, device)
+    _check(lib().agnes_mx4_linear(
+        x.data_ptr(), _stride_bytes(x), rows, w.data_ptr(), _stride_bytes(w), width, dim,
+        bias.data_ptr() if bias is not None else None, y.data_ptr(), _FLOATS[y.dtype], _stride(y),
+        _status_word(status, device), _stream(device)))
+    return y

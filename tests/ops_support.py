@@ -16,11 +16,15 @@ def rounding(ref, dtype):
 
 
 def assert_within(got, ref, bound):
-    """|got - ref| <= bound, element by element; ref and bound in 64 bits."""
+    """|got - ref| <= bound, element by element; ref and bound in 64 bits.  What is
+    past got's type's largest number by half a unit rounds to infinity."""
+    most = torch.finfo(got.dtype).max if got.dtype in _UNIT else float("inf")
+    over = most * (1 + _UNIT[got.dtype][0] / 2) if got.dtype in _UNIT else most
     got, ref, bound = got.double().cpu(), ref.cpu(), bound.cpu()
     assert got.shape == ref.shape
     off = (got - ref).abs()
-    bad = ~(off <= bound)
+    infinite = got.isinf() & (got.sign() == ref.sign()) & (ref.abs() + bound >= over)
+    bad = ~((off <= bound) | infinite)
     assert not bad.any(), (f"{int(bad.sum())} of {bad.numel()} off, the worst by "
                            f"{float((off - bound)[bad].max()) if bad.any() else 0:.3g}")
 

@@ -40,7 +40,7 @@ extern "C" {
  * minibatch).  A negative id selects no row: zeros.  So does an id >= rows,
  * which also sets AGNES_OP_BAD_INDEX.
  *  table   rows x dim of table_dtype, table_stride apart; 0 <= rows < 2^31,
- *          1 <= dim < 2^31.
+ *          1 <= dim <= 2^22.
  *  ids     n ids of ids_bits (32 or 64) bits; 0 <= n < 2^31.
  *  out     n x dim of out_dtype, out_stride apart.
  * Errors: EINVAL, ERANGE (a size above these limits, or n * dim above 2^40),

@@ -364,14 +364,16 @@ Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int n
 }
 
 template <typename T, typename TOut, int kMode>
-cudaError_t launch_distill(DistillArgs a, int64_t rows, int num_sms, cudaStream_t st) {
-  const Shape s = distill_shape(rows, a.classes, sizeof(T), kMode, num_sms);
+cudaError_t launch_distill(DistillArgs a, int64_t rows, int device, cudaStream_t st) {
+  const Shape s = distill_shape(rows, a.classes, sizeof(T), kMode, op_num_sms(device));
   a.slice = s.slice;
   a.keep = s.keep;
   const auto kernel = distill_kernel<T, TOut, kMode>;
-  cudaError_t e =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)(sizeof(DistillSmem) + (kMode == kStep ? kMaxKeep : 0)));
+  static OncePerDevice once;
+  cudaError_t e = once.run(device, [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)(sizeof(DistillSmem) + (kMode == kStep ? kMaxKeep : 0)));
+  });
   if (e != cudaSuccess) return e;
   // rows over two grid dimensions of 65,535 at most; an exact cover, row by row
   for (int64_t r0 = 0; r0 < rows;) {
@@ -495,14 +497,13 @@ agnes_status distill(const DistillCall& c) {
   a.out = c.out;
   a.out_stride = c.out_stride;
   a.status = c.status;
-  const int sms = op_num_sms(device);
   const cudaError_t e = with_float_type(c.logits_dtype, [&](auto tin) {
     using T = typename decltype(tin)::type;
-    if (c.mode == kLoss) return launch_distill<T, T, kLoss>(a, c.rows, sms, c.st);
+    if (c.mode == kLoss) return launch_distill<T, T, kLoss>(a, c.rows, device, c.st);
     return with_float_type(c.out_dtype, [&](auto tout) {
       using TOut = typename decltype(tout)::type;
-      if (c.mode == kGrad) return launch_distill<T, TOut, kGrad>(a, c.rows, sms, c.st);
-      return launch_distill<T, TOut, kStep>(a, c.rows, sms, c.st);
+      if (c.mode == kGrad) return launch_distill<T, TOut, kGrad>(a, c.rows, device, c.st);
+      return launch_distill<T, TOut, kStep>(a, c.rows, device, c.st);
     });
   });
   return op_launched(op, e);

@@ -68,11 +68,13 @@ lookup_kernel(const TIn* __restrict__ table, int64_t rows, int64_t table_stride,
 
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortItems = 8;
+constexpr int kSortItems = 4;
 constexpr int kSortTile = kSortThreads * kSortItems;
+constexpr int kSmallItems = 8;  // where one CTA sorts them all
+constexpr int kSmallTile = kSortThreads * kSmallItems;
 constexpr int kMaxBits = 9;
 constexpr int kMaxDigits = 1 << kMaxBits;
-constexpr int kSortMaxCtas = 304;
+constexpr int kSortMaxCtas = 608;
 
 template <typename Id>
 __device__ __forceinline__ uint32_t key_of(Id id, int64_t rows, int32_t* status) {
@@ -125,9 +127,7 @@ sort_count_kernel(Src src, int64_t n, int shift, int digits, int32_t* __restrict
     for (int u = 0; u < kSortItems; ++u) {
       const int64_t i = base + u * kSortThreads + threadIdx.x;
       const bool in = i < run.end;
-      const int d = in ? (int)(src.key(i) >> shift) & (digits - 1) : -1;
-      const unsigned peers = __match_any_sync(0xffffffffu, d);
-      if (in && lane_id() == __ffs(peers) - 1) atomicAdd(hist + d, __popc(peers));
+      if (in) atomicAdd(hist + ((src.key(i) >> shift) & (uint32_t)(digits - 1)), 1);
     }
   }
   __syncthreads();
@@ -173,18 +173,30 @@ __device__ __forceinline__ void digit_bases(SortSmem& s, int digits, Total total
 }
 static_assert(kSortThreads >= kMaxDigits, "a thread per digit");
 
-// The places of a tile's tokens, in order: warp w holds tokens w * 256 + u * 32
-// + lane.  s.base moves on by the tile's counts.  All threads take part; a
+// The lanes with this lane's digit, by a ballot for each of its bits.
+__device__ __forceinline__ unsigned same_digit(int digit, int bits) {
+  unsigned peers = __ballot_sync(0xffffffffu, digit >= 0);
+  for (int b = 0; b < bits; ++b) {
+    const bool set = (digit >> b) & 1;
+    const unsigned with = __ballot_sync(0xffffffffu, set);
+    peers &= set ? with : ~with;
+  }
+  return peers;
+}
+
+// The places of a tile's tokens, in order: warp w holds tokens w * 32 * kItems +
+// u * 32 + lane.  s.base moves on by the tile's counts.  All threads take part; a
 // token out of the run has digit -1.
-__device__ __forceinline__ void tile_places(SortSmem& s, int digits, const int (&digit)[kSortItems],
-                                            int32_t (&place)[kSortItems]) {
-  const int warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < kSortWarps * kMaxDigits; i += kSortThreads)
-    (&s.warp_hist[0][0])[i] = 0;
+template <int kItems>
+__device__ __forceinline__ void tile_places(SortSmem& s, int bits, const int (&digit)[kItems],
+                                            int32_t (&place)[kItems]) {
+  const int warp = threadIdx.x >> 5, digits = 1 << bits;
+  if (threadIdx.x < digits)
+    for (int w = 0; w < kSortWarps; ++w) s.warp_hist[w][threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u) {
-    const unsigned peers = __match_any_sync(0xffffffffu, digit[u]);
+  for (int u = 0; u < kItems; ++u) {
+    const unsigned peers = same_digit(digit[u], bits);
     int32_t old = 0;
     if (digit[u] >= 0) old = s.warp_hist[warp][digit[u]];
     place[u] = old + __popc(peers & ((1u << lane_id()) - 1u));
@@ -206,16 +218,17 @@ __device__ __forceinline__ void tile_places(SortSmem& s, int digits, const int (
   }
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u)
+  for (int u = 0; u < kItems; ++u)
     if (digit[u] >= 0) place[u] += s.warp_hist[warp][digit[u]];
 }
 
 template <typename Src>
 __global__ void __launch_bounds__(kSortThreads)
-sort_place_kernel(Src src, int64_t n, int shift, int digits, const int32_t* __restrict__ counts,
+sort_place_kernel(Src src, int64_t n, int shift, int bits, const int32_t* __restrict__ counts,
                   const int32_t* __restrict__ totals, uint32_t* __restrict__ keys,
                   int32_t* __restrict__ tokens) {
   __shared__ SortSmem s;
+  const int digits = 1 << bits;
   digit_bases(s, digits, [&](int d) { return totals[d]; },
               [&](int d) { return counts[(int64_t)d * gridDim.x + blockIdx.x]; });
   const Run run = run_of(n, blockIdx.x, gridDim.x);
@@ -233,7 +246,7 @@ sort_place_kernel(Src src, int64_t n, int shift, int digits, const int32_t* __re
       digit[u] = in ? (int)(key[u] >> shift) & (digits - 1) : -1;
     }
     __syncthreads();  // the bases, and the last tile's places, have been read
-    tile_places(s, digits, digit, place);
+    tile_places(s, bits, digit, place);
 #pragma unroll
     for (int u = 0; u < kSortItems; ++u) {
       if (digit[u] < 0) continue;
@@ -243,7 +256,7 @@ sort_place_kernel(Src src, int64_t n, int shift, int digits, const int32_t* __re
   }
 }
 
-// Up to kSortTile tokens in one CTA, every pass in shared memory.
+// Up to kSmallTile tokens in one CTA, every pass in shared memory.
 template <typename Id>
 __global__ void __launch_bounds__(kSortThreads)
 sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __restrict__ keys,
@@ -251,33 +264,33 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
   extern __shared__ __align__(16) uint8_t small_smem[];
   SortSmem& s = *(SortSmem*)small_smem;
   uint32_t* skey = (uint32_t*)(small_smem + sizeof(SortSmem));
-  int32_t* stoken = (int32_t*)(skey + kSortTile);
-  const int first = (threadIdx.x >> 5) * 32 * kSortItems + lane_id();
+  int32_t* stoken = (int32_t*)(skey + kSmallTile);
+  const int first = (threadIdx.x >> 5) * 32 * kSmallItems + lane_id();
   const int digits = 1 << bits;
-  uint32_t key[kSortItems];
-  int32_t token[kSortItems], place[kSortItems];
+  uint32_t key[kSmallItems];
+  int32_t token[kSmallItems], place[kSmallItems];
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u) {
+  for (int u = 0; u < kSmallItems; ++u) {
     const int i = first + u * 32;
     key[u] = i < n ? src.key(i) : 0;
     token[u] = i;
   }
   for (int p = 0; p < passes; ++p) {
-    int digit[kSortItems];
+    int digit[kSmallItems];
 #pragma unroll
-    for (int u = 0; u < kSortItems; ++u)
+    for (int u = 0; u < kSmallItems; ++u)
       digit[u] = first + u * 32 < n ? (int)(key[u] >> (p * bits)) & (digits - 1) : -1;
     // the digits' totals: counted with base = 0, then placed
     if (threadIdx.x < digits) s.base[threadIdx.x] = 0;
     __syncthreads();
-    tile_places(s, digits, digit, place);  // ends with base[d] = the digit's count
+    tile_places(s, bits, digit, place);  // ends with base[d] = the digit's count
     __syncthreads();
     const int32_t count = threadIdx.x < digits ? s.base[threadIdx.x] : 0;
     __syncthreads();
     digit_bases(s, digits, [&](int) { return count; }, [](int) { return 0; });
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kSortItems; ++u) {
+    for (int u = 0; u < kSmallItems; ++u) {
       if (digit[u] < 0) continue;
       const int32_t at = s.base[digit[u]] + place[u];
       skey[at] = key[u];
@@ -285,7 +298,7 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kSortItems; ++u) {
+    for (int u = 0; u < kSmallItems; ++u) {
       const int i = first + u * 32;
       if (i < n) {
         key[u] = skey[i];
@@ -295,7 +308,7 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
     __syncthreads();
   }
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u) {
+  for (int u = 0; u < kSmallItems; ++u) {
     const int i = first + u * 32;
     if (i < n) {
       keys[i] = key[u];
@@ -303,11 +316,12 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
     }
   }
 }
-constexpr size_t kSmallSmem = sizeof(SortSmem) + 8 * kSortTile;
+constexpr size_t kSmallSmem = sizeof(SortSmem) + 8 * kSmallTile;
 
 // ---- sums over the sorted tokens ----------------------------------------------
 
 constexpr int kSumThreads = 256;
+constexpr uint32_t kPastChunk = 0xffffffffu;  // no id
 
 // heads[b] = the number of distinct ids that begin among the sorted tokens
 // [b * span, (b + 1) * span).
@@ -343,12 +357,18 @@ struct SumArgs {
   const int32_t* heads;
   int32_t* out_ids;
   int32_t* count;
-  // a chunk's part of the row that it begins within (first) and of the row that
-  // it ends within (last): partial[(2 * chunk + which) * dim ..]
+  int32_t* rank_of;  // per chunk: which row of `out` its part 1 belongs to
+  // a chunk's part of the row that it begins within (which = 0) and of the row that
+  // it ends within (1): partial[(2 * chunk + which) * part_dim ..]
   float* partial;
-  int32_t chunk;       // tokens per chunk
+  int32_t part_dim;    // dim up to a multiple of 4
+  int32_t chunk;       // tokens per chunk, a multiple of kMinChunk
   int64_t chunks;
-  int32_t cta_chunks;  // chunks per CTA
+
+  __device__ float* part(int64_t c, int which) const {
+    return partial + (2 * c + which) * part_dim;
+  }
+  __device__ uint32_t first_key(int64_t c) const { return keys[c * chunk]; }
 };
 
 // The sum of heads[0 .. limit) for this CTA, and of all of them.
@@ -375,13 +395,17 @@ __device__ __forceinline__ void prefix_of_heads(const int32_t* heads, int ctas, 
 }
 
 // A group of kLanes lanes sums a chunk's rows for kLanes * kVec * kCols columns,
-// kAhead rows in flight.  blockIdx.y: which columns.
+// kAhead rows in flight.  blockIdx.y: which columns.  Each lane holds one token's key
+// and place, and they pass them around, so that a row's load waits for no other.
 template <typename TIn, typename TOut, int kVec, int kCols, int kLanes>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
   constexpr int kGroups = kSumThreads / kLanes;
-  constexpr int kAhead = 8 / kCols > 2 ? 8 / kCols : 2;
+  constexpr int kAhead = kCols > 1 || kLanes < 8 ? 4 : 8;
   __shared__ int32_t group_heads[kGroups];
   const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const unsigned lanes = kLanes == 32 ? 0xffffffffu
+                                      : ((1u << (kLanes & 31)) - 1u)
+                                            << (threadIdx.x % 32 / kLanes * kLanes);
   const int64_t chunk = (int64_t)blockIdx.x * kGroups + group;
   const int64_t lo = min(a.n, chunk * a.chunk), hi = min(a.n, lo + a.chunk);
   const int32_t col0 = blockIdx.y * kLanes * kVec * kCols + lane * kVec;
@@ -394,6 +418,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
       const uint32_t k = a.keys[i];
       mine += k < a.rows && (i == 0 || a.keys[i - 1] != k);
     }
+    __syncwarp();
 #pragma unroll
     for (int d = kLanes / 2; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d, kLanes);
     if (lane == 0) group_heads[group] = mine;
@@ -421,6 +446,10 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
     }
   }
   if (lo >= hi) return;
+  uint32_t key = a.keys[lo];
+  if (key >= a.rows) return;  // padding only
+  const bool goes_on = hi < a.n && a.keys[hi] == a.keys[hi - 1];  // past the chunk
+  bool spans = lo > 0 && a.keys[lo - 1] == key;  // the current row began in an earlier chunk
   float acc[kCols][kVec];
   auto clear = [&] {
 #pragma unroll
@@ -428,10 +457,8 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) acc[c][e] = 0.f;
   };
-  // the row that the tokens before i belong to is complete within the chunk, or
-  // its part goes to the workspace
-  auto put_row = [&](uint32_t key) {
-    const int64_t row = a.heads ? rank : (int64_t)key;
+  auto put_row = [&](uint32_t k) {
+    const int64_t row = a.heads ? rank : (int64_t)k;
 #pragma unroll
     for (int c = 0; c < kCols; ++c) {
       const int32_t col = col0 + c * kLanes * kVec;
@@ -443,106 +470,227 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
     }
   };
   auto put_part = [&](int which) {
-    float* p = a.partial + (2 * chunk + which) * a.dim;
+    constexpr int kN = kVec < 4 ? kVec : 4;
+    float* p = a.part(chunk, which);
 #pragma unroll
     for (int c = 0; c < kCols; ++c) {
       const int32_t col = col0 + c * kLanes * kVec;
       if (col >= a.dim) break;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) p[col + e] = acc[c][e];
+      for (int h = 0; h < kVec / kN; ++h) {
+        Vec<float, kN> y;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) y.v[e] = acc[c][h * kN + e];
+        *(Vec<float, kN>*)(p + col + h * kN) = y;
+      }
     }
   };
-  uint32_t key = a.keys[lo];
-  bool spans = lo > 0 && a.keys[lo - 1] == key;  // the current row began in an earlier chunk
   auto begin_row = [&](uint32_t k) {
     ++rank;
-    if (a.heads && k < a.rows && blockIdx.y == 0 && lane == 0) a.out_ids[rank] = (int32_t)k;
+    if (a.heads && blockIdx.y == 0 && lane == 0) a.out_ids[rank] = (int32_t)k;
   };
-  if (!spans && key < a.rows) begin_row(key);
+  if (!spans) begin_row(key);
   clear();
-  for (int64_t i0 = lo; i0 < hi && key < a.rows; i0 += kAhead) {
-    uint32_t k[kAhead];
-    Vec<TIn, kVec> x[kAhead][kCols];
+  uint32_t next_key = lo + lane < hi ? a.keys[lo + lane] : kPastChunk;
+  int32_t next_token = lo + lane < hi ? a.tokens[lo + lane] : -1;
+  for (int64_t base = lo; base < hi && key < a.rows; base += kLanes) {
+    const uint32_t held_key = next_key;
+    const int32_t held_token = next_token;
+    const int64_t next = base + kLanes + lane;
+    next_key = next < hi ? a.keys[next] : kPastChunk;
+    next_token = next < hi ? a.tokens[next] : -1;
+#pragma unroll 1
+    for (int i0 = 0; i0 < kLanes; i0 += kAhead) {
+      Vec<TIn, kVec> x[kAhead][kCols];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int64_t i = min(i0 + u, hi - 1);
-      k[u] = i0 + u < hi ? a.keys[i] : a.rows;
-      const TIn* row = (const TIn*)a.grad + (int64_t)a.tokens[i] * a.grad_stride;
+      for (int u = 0; u < kAhead; ++u) {
+        const int32_t token = __shfl_sync(lanes, held_token, i0 + u, kLanes);
+        const TIn* row = (const TIn*)a.grad + (int64_t)token * a.grad_stride;
 #pragma unroll
-      for (int c = 0; c < kCols; ++c) {
-        const int32_t col = col0 + c * kLanes * kVec;
-        if (col < a.dim) {
-          x[u][c] = *(const Vec<TIn, kVec>*)(row + col);
-        } else {
+        for (int c = 0; c < kCols; ++c) {
+          const int32_t col = col0 + c * kLanes * kVec;
+          if (token >= 0 && col < a.dim) {
+            x[u][c] = *(const Vec<TIn, kVec>*)(row + col);
+          } else {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) x[u][c].v[e] = from_f32<TIn>(0.f);
+            for (int e = 0; e < kVec; ++e) x[u][c].v[e] = from_f32<TIn>(0.f);
+          }
         }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (i0 + u >= hi) break;
-      if (k[u] != key) {
-        if (spans)
-          put_part(0);
-        else
-          put_row(key);
-        spans = false;
-        clear();
-        key = k[u];
-        if (key >= a.rows) break;
-        begin_row(key);
+      for (int u = 0; u < kAhead; ++u) {
+        const uint32_t k = __shfl_sync(lanes, held_key, i0 + u, kLanes);
+        if (k != key && key < a.rows && k != kPastChunk) {
+          if (spans)
+            put_part(0);
+          else
+            put_row(key);
+          spans = false;
+          clear();
+          key = k;
+          if (key < a.rows) begin_row(key);
+        }
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) acc[c][e] += to_f32(x[u][c].v[e]);
       }
-#pragma unroll
-      for (int c = 0; c < kCols; ++c)
-#pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          acc[c][e] += to_f32(x[u][c].v[e]);
     }
   }
   if (key >= a.rows) return;
   if (spans)
     put_part(0);
-  else if (hi < a.n && a.keys[hi] == key)
-    put_part(1);
-  else
+  else if (!goes_on)
     put_row(key);
+  else {
+    put_part(1);
+    if (a.heads && blockIdx.y == 0 && lane == 0) a.rank_of[chunk] = rank;
+  }
 }
 
-// Rows that span chunks: a warp for each chunk in which such a row begins adds
-// the chunks' parts in order.  rank of the row: known from the chunk's heads.
-template <typename TOut>
-__global__ void __launch_bounds__(kSumThreads) join_kernel(SumArgs a) {
-  const int64_t chunk = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
-  if (chunk + 1 >= a.chunks) return;  // the last chunk's rows end in it
-  const int64_t lo = chunk * a.chunk, hi = lo + a.chunk;
-  const uint32_t key = a.keys[hi - 1];
-  if (key >= a.rows || a.keys[hi] != key) return;     // nothing goes on past the chunk
-  if (lo > 0 && a.keys[lo - 1] == key) return;        // it began in an earlier chunk
-  // the last chunk that begins with the key
-  int64_t last = chunk + 1, end = a.chunks;
-  while (end - last > 1) {
-    const int64_t mid = (last + end) / 2;
-    if (a.keys[mid * a.chunk] == key)
-      last = mid;
-    else
-      end = mid;
+// Rows that span chunks.  Such a row has part 1 of the chunk in which it begins and
+// part 0 of each later one.  Where kFold chunks from a multiple of kFold on are all
+// within one row, their parts are first summed into the first one's (fold_kernel),
+// so that a row of any length has few parts left.
+constexpr int kFold = 64;
+constexpr int kJoinCols = 128;  // columns per CTA, four to a lane
+
+__device__ __forceinline__ void add4(float4& s, const float4& x) {
+  s.x += x.x;
+  s.y += x.y;
+  s.z += x.z;
+  s.w += x.w;
+}
+
+// The sum over i in [first, count) in steps of `step` of item(i)'s four columns.
+template <typename Item>
+__device__ __forceinline__ float4 sum_items(int64_t first, int64_t count, int step, Item item) {
+  constexpr int kAhead = 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  int64_t i = first;
+  for (; i + (kAhead - 1) * step < count; i += kAhead * step) {
+    float4 x[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) x[u] = *(const float4*)item(i + u * step);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) add4(s, x[u]);
   }
-  int64_t row = key;
-  if (a.heads) {  // the row is the last that begins at or before the chunk's end
-    int32_t r = 0;
-    const int cta = (int)(chunk / a.cta_chunks);
-    for (int i = lane_id(); i < cta; i += 32) r += a.heads[i];
-    for (int64_t i = (int64_t)cta * a.cta_chunks * a.chunk + lane_id(); i < hi; i += 32) {
-      const uint32_t k = a.keys[i];
-      r += k < a.rows && (i == 0 || a.keys[i - 1] != k);
+  for (; i < count; i += step) add4(s, *(const float4*)item(i));
+  return s;
+}
+
+constexpr int kFoldThreads = 256;
+
+__global__ void __launch_bounds__(kFoldThreads) fold_kernel(SumArgs a) {
+  __shared__ float4 part[kFoldThreads / 32][32];
+  const int64_t c0 = (int64_t)blockIdx.x * kFold;
+  if (c0 == 0 || c0 + kFold > a.chunks) return;
+  const uint32_t key = a.keys[c0 * a.chunk - 1];
+  if (key >= a.rows || a.first_key(c0 + kFold - 1) != key) return;
+  const int warp = threadIdx.x >> 5;
+  const int32_t col = blockIdx.y * kJoinCols + lane_id() * 4;
+  const bool in = col < a.part_dim;
+  if (in)
+    part[warp][lane_id()] = sum_items(warp, kFold, kFoldThreads / 32,
+                                      [&](int64_t i) { return a.part(c0 + i, 0) + col; });
+  __syncthreads();
+  if (warp == 0 && in) {
+    float4 s = part[0][lane_id()];
+    for (int w = 1; w < kFoldThreads / 32; ++w) add4(s, part[w][lane_id()]);
+    *(float4*)(a.part(c0, 0) + col) = s;
+  }
+}
+
+// The parts of the row that begins in chunk `own` and goes on to chunk `last`.
+struct Parts {
+  int64_t own, last, count;
+  int64_t fold0, folds;  // the first folded chunk, and how many runs of kFold
+
+  __device__ Parts() {}
+  __device__ Parts(int64_t own_, int64_t last_) : own(own_), last(last_) {
+    fold0 = (own + kFold) / kFold * kFold;  // the first multiple of kFold past own
+    folds = last + 1 > fold0 ? (last + 1 - fold0) / kFold : 0;
+    count = last - own + 1 - folds * (kFold - 1);
+  }
+  __device__ const float* at(const SumArgs& a, int64_t i) const {
+    if (i == 0) return a.part(own, 1);
+    int64_t c = own + i;
+    if (folds > 0 && c > fold0) {
+      const int64_t f = c - fold0;  // folded runs count as one
+      c = f < folds ? fold0 + f * kFold : fold0 + folds * kFold + (f - folds);
     }
-    row = warp_sum(r) - 1;
+    return a.part(c, 0);
   }
-  for (int32_t col = lane_id(); col < a.dim; col += 32) {
-    float acc = a.partial[(2 * chunk + 1) * a.dim + col];
-    for (int64_t c = chunk + 1; c <= last; ++c) acc += a.partial[2 * c * a.dim + col];
-    ((TOut*)a.out)[row * a.dim + col] = from_f32<TOut>(acc * a.scale);
+};
+
+constexpr int kJoinThreads = 512;
+constexpr int kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinAlone = 32;  // parts that a warp sums by itself
+
+// A warp for each chunk in which a row begins that goes on past it; the CTA
+// together where the row has many parts.
+template <typename TOut>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(SumArgs a) {
+  __shared__ Parts all[kJoinWarps];
+  __shared__ int64_t row_of[kJoinWarps];
+  __shared__ float4 part[kJoinWarps][32];
+  const int warp = threadIdx.x >> 5, lane = lane_id();
+  const int64_t chunk = (int64_t)blockIdx.x * kJoinWarps + warp;
+  const int32_t col = blockIdx.y * kJoinCols + lane * 4;
+  const auto put = [&](int64_t row, const float4& s) {
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.dim) ((TOut*)a.out)[row * a.dim + col + e] = from_f32<TOut>(v[e] * a.scale);
+  };
+  int64_t many = -1;  // the row, where the CTA sums it
+  Parts parts;
+  if (chunk + 1 < a.chunks) {  // the last chunk's rows end in it
+    const int64_t lo = chunk * a.chunk, hi = lo + a.chunk;
+    const uint32_t key = a.keys[hi - 1];
+    if (key < a.rows && a.keys[hi] == key && !(lo > 0 && a.keys[lo - 1] == key)) {
+      // the last chunk that begins with the key: most rows end in the next one
+      int64_t last = chunk + 1, end = chunk + 2;
+      while (end < a.chunks && a.first_key(end) == key) {
+        last = end;
+        end = last + 2 * (last - chunk);
+      }
+      if (end > a.chunks) end = a.chunks;
+      while (end - last > 1) {
+        const int64_t mid = (last + end) / 2;
+        if (a.first_key(mid) == key)
+          last = mid;
+        else
+          end = mid;
+      }
+      const int64_t row = a.heads ? (int64_t)a.rank_of[chunk] : (int64_t)key;
+      parts = Parts(chunk, last);
+      if (parts.count > kJoinAlone) {
+        many = row;
+      } else if (col < a.part_dim) {
+        put(row, sum_items(0, parts.count, 1, [&](int64_t i) { return parts.at(a, i) + col; }));
+      }
+    }
+  }
+  if (lane == 0) {
+    row_of[warp] = many;
+    all[warp] = parts;
+  }
+  if (!__syncthreads_or(many >= 0)) return;
+  for (int o = 0; o < kJoinWarps; ++o) {
+    const int64_t row = row_of[o];
+    if (row < 0) continue;
+    const Parts p = all[o];
+    if (col < a.part_dim)
+      part[warp][lane] =
+          sum_items(warp, p.count, kJoinWarps, [&](int64_t i) { return p.at(a, i) + col; });
+    __syncthreads();
+    if (warp == 0 && col < a.part_dim) {
+      float4 s = part[0][lane];
+      for (int w = 1; w < kJoinWarps; ++w) add4(s, part[w][lane]);
+      put(row, s);
+    }
+    __syncthreads();
   }
 }
 
@@ -550,12 +698,13 @@ __global__ void __launch_bounds__(kSumThreads) join_kernel(SumArgs a) {
 
 constexpr int64_t kMaxTokens = 0x7fffffff;
 constexpr int64_t kMaxCells = 1ll << 40;
-constexpr int kMaxChunks = 8192;
+constexpr int64_t kMaxDim = 1 << 22;  // its column tiles fit a grid's second dimension
+constexpr int kMaxChunks = 32768;
 constexpr int kMinChunk = 32;
 
 struct GradPlan {
   int64_t chunk, chunks;
-  size_t keys[2], tokens[2], counts, totals, heads, partial, bytes;
+  size_t keys[2], tokens[2], counts, totals, heads, rank_of, partial, bytes;
 };
 
 GradPlan grad_plan(int64_t n, int64_t dim) {
@@ -575,15 +724,16 @@ GradPlan grad_plan(int64_t n, int64_t dim) {
   }
   p.counts = take(4ll * kMaxDigits * kSortMaxCtas);
   p.totals = take(4 * kMaxDigits);
-  p.heads = take(4 * (p.chunks + 1));
-  p.partial = take(8 * p.chunks * dim);
+  p.heads = take(4 * p.chunks);
+  p.rank_of = take(4 * p.chunks);
+  p.partial = take(8 * p.chunks * (ceil_div(dim, 4) * 4));
   p.bytes = at;
   return p;
 }
 
 template <typename Id>
 cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, const GradPlan& p,
-                        int32_t* status, int num_sms, cudaStream_t st, int* result) {
+                        int32_t* status, int device, cudaStream_t st, int* result) {
   int bits = 1;
   while ((1ll << bits) <= rows) ++bits;  // keys 0 .. rows
   const int passes = (int)ceil_div(bits, kMaxBits);
@@ -592,9 +742,12 @@ cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, con
   const FromIds<Id> ids_src{ids, rows, status};
   const auto keys = [&](int i) { return (uint32_t*)(ws + p.keys[i]); };
   const auto tokens = [&](int i) { return (int32_t*)(ws + p.tokens[i]); };
-  if (n <= kSortTile) {
-    const cudaError_t e = cudaFuncSetAttribute(
-        sort_small_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
+  if (n <= kSmallTile) {
+    static OncePerDevice once;
+    const cudaError_t e = once.run(device, [] {
+      return cudaFuncSetAttribute(sort_small_kernel<Id>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
+    });
     if (e != cudaSuccess) return e;
     sort_small_kernel<Id><<<1, kSortThreads, kSmallSmem, st>>>(ids_src, (int)n, passes, pass_bits,
                                                                keys(0), tokens(0));
@@ -602,7 +755,8 @@ cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, con
     return cudaGetLastError();
   }
   const int64_t tiles = ceil_div(n, kSortTile);
-  int ctas = 2 * num_sms < kSortMaxCtas ? 2 * num_sms : kSortMaxCtas;
+  const int num_sms = op_num_sms(device);
+  int ctas = 4 * num_sms < kSortMaxCtas ? 4 * num_sms : kSortMaxCtas;
   if (tiles < ctas) ctas = (int)tiles;
   int32_t* counts = (int32_t*)(ws + p.counts);
   int32_t* totals = (int32_t*)(ws + p.totals);
@@ -615,10 +769,10 @@ cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, con
       sort_count_kernel<<<ctas, kSortThreads, 0, st>>>(from, n, shift, digits, counts);
     sort_scan_kernel<<<(digits + 7) / 8, 256, 0, st>>>(counts, ctas, digits, totals);
     if (pass == 0)
-      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(ids_src, n, shift, digits, counts, totals,
+      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(ids_src, n, shift, pass_bits, counts, totals,
                                                        keys(to), tokens(to));
     else
-      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(from, n, shift, digits, counts, totals,
+      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(from, n, shift, pass_bits, counts, totals,
                                                        keys(to), tokens(to));
     *result = to;
   }
@@ -628,10 +782,8 @@ cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, con
 template <typename TIn, typename TOut, int kVec, int kCols, int kLanes>
 cudaError_t launch_sum(SumArgs a, int32_t* heads, cudaStream_t st) {
   constexpr int kGroups = kSumThreads / kLanes;
-  a.cta_chunks = kGroups;
   const int64_t ctas = ceil_div(a.chunks, kGroups);
   const int64_t cols = ceil_div(a.dim, kLanes * kVec * kCols);
-  if (cols > 65535) return cudaErrorInvalidConfiguration;
   if (heads) {
     a.heads = heads;
     count_heads_kernel<<<(unsigned)ctas, kSumThreads, 0, st>>>(a.keys, a.n, a.rows,
@@ -639,8 +791,12 @@ cudaError_t launch_sum(SumArgs a, int32_t* heads, cudaStream_t st) {
   }
   sum_kernel<TIn, TOut, kVec, kCols, kLanes>
       <<<dim3((unsigned)ctas, (unsigned)cols), kSumThreads, 0, st>>>(a);
+  const unsigned join_cols = (unsigned)ceil_div(a.dim, kJoinCols);
+  if (a.chunks > kFold)
+    fold_kernel<<<dim3((unsigned)(a.chunks / kFold), join_cols), kFoldThreads, 0, st>>>(a);
   if (a.chunks > 1)
-    join_kernel<TOut><<<(unsigned)ceil_div(a.chunks, kSumThreads / 32), kSumThreads, 0, st>>>(a);
+    join_kernel<TOut><<<dim3((unsigned)ceil_div(a.chunks, kJoinWarps), join_cols), kJoinThreads, 0,
+                        st>>>(a);
   return cudaGetLastError();
 }
 
@@ -650,8 +806,9 @@ cudaError_t launch_sum_lanes(const SumArgs& a, int32_t* heads, cudaStream_t st) 
   const int64_t vecs = ceil_div(a.dim, kVec);
   if (vecs <= 4) return launch_sum<TIn, TOut, kVec, 1, 4>(a, heads, st);
   if (vecs <= 16) return launch_sum<TIn, TOut, kVec, 1, 16>(a, heads, st);
-  if (kVec > 2 || vecs <= 32) return launch_sum<TIn, TOut, kVec, 1, 32>(a, heads, st);
-  return launch_sum<TIn, TOut, kVec, 4, 32>(a, heads, st);
+  if constexpr (kVec <= 2)
+    if (vecs > 32) return launch_sum<TIn, TOut, kVec, 4, 32>(a, heads, st);
+  return launch_sum<TIn, TOut, kVec, 1, 32>(a, heads, st);
 }
 
 // f(constant) for the widest vector of 8, 4, 2 or 1 elements (16 bytes at most of
@@ -675,7 +832,7 @@ agnes_status check_embedding(const char* op, int64_t rows, int64_t dim, int64_t 
   if (rows < 0 || n < 0 || dim < 1)
     return op_error(AGNES_EINVAL, "%s: rows %lld, dim %lld, n %lld", op, (long long)rows,
                     (long long)dim, (long long)n);
-  if (rows > kMaxTokens || n > kMaxTokens || dim > kMaxTokens || (n && dim > kMaxCells / n) ||
+  if (rows > kMaxTokens || n > kMaxTokens || dim > kMaxDim || (n && dim > kMaxCells / n) ||
       (rows && dim > kMaxCells / rows))
     return op_error(AGNES_ERANGE, "%s: rows %lld, dim %lld, n %lld are too large", op,
                     (long long)rows, (long long)dim, (long long)n);
@@ -752,7 +909,7 @@ agnes_status embedding_grad(const GradCall& c, bool compact) {
   int which = 0;
   cudaError_t e = with_index_type(c.ids_bits, [&](auto id) {
     using Id = typename decltype(id)::type;
-    return sort_tokens((const Id*)c.ids, c.n, c.rows, ws, p, c.status, op_num_sms(device), c.st,
+    return sort_tokens((const Id*)c.ids, c.n, c.rows, ws, p, c.status, device, c.st,
                        &which);
   });
   if (e != cudaSuccess) return op_launched(op, e);
@@ -772,7 +929,9 @@ agnes_status embedding_grad(const GradCall& c, bool compact) {
   a.out = c.out;
   a.out_ids = c.out_ids;
   a.count = c.count;
+  a.rank_of = (int32_t*)(ws + p.rank_of);
   a.partial = (float*)(ws + p.partial);
+  a.part_dim = (int32_t)(ceil_div(c.dim, 4) * 4);
   a.chunk = (int32_t)p.chunk;
   a.chunks = p.chunks;
   int32_t* heads = compact ? (int32_t*)(ws + p.heads) : nullptr;

@@ -487,7 +487,7 @@ bool map_rows(EncodeTiled encode, CUtensorMap* map, const void* p, int64_t bytes
 
 template <typename TOut>
 cudaError_t launch_linear(const void* x, int64_t x_stride, const void* w, int64_t w_stride,
-                          const LinearArgs& a, int num_sms, cudaStream_t st) {
+                          const LinearArgs& a, int device, cudaStream_t st) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return cudaErrorNotSupported;
   const int64_t codes = (int64_t)a.blocks * 16;
@@ -502,10 +502,14 @@ cudaError_t launch_linear(const void* x, int64_t x_stride, const void* w, int64_
       !map_rows(encode, &ws, wb + codes, a.blocks, a.width, w_stride, kScaleRun,
                 CU_TENSOR_MAP_SWIZZLE_NONE))
     return cudaErrorInvalidValue;
-  const cudaError_t e = cudaFuncSetAttribute(
-      linear_kernel<TOut>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+  static OncePerDevice once;
+  const cudaError_t e = once.run(device, [] {
+    return cudaFuncSetAttribute(linear_kernel<TOut>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)kSmemBytes);
+  });
   if (e != cudaSuccess) return e;
   const int64_t tiles = ceil_div(a.rows, kTile) * ceil_div(a.width, kTile);
+  const int num_sms = op_num_sms(device);
   linear_kernel<TOut><<<(unsigned)(tiles < num_sms ? tiles : num_sms), kThreads, kSmemBytes, st>>>(
       xc, xs, wc, ws, a);
   return cudaGetLastError();
@@ -513,14 +517,17 @@ cudaError_t launch_linear(const void* x, int64_t x_stride, const void* w, int64_
 
 template <typename TOut, int kRows>
 cudaError_t launch_few(const void* x, int64_t x_stride, const void* w, int64_t w_stride,
-                       const LinearArgs& a, int num_sms, cudaStream_t st) {
+                       const LinearArgs& a, int device, cudaStream_t st) {
   int lanes = 1;
   while (lanes < 32 && lanes < a.blocks) lanes *= 2;
   const int64_t ctas = ceil_div(a.width, kFewThreads / lanes);
   const size_t smem = few_smem(kRows, a.blocks);
-  const cudaError_t e =
-      cudaFuncSetAttribute(linear_few_kernel<TOut, kRows>,
-                           cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+  const int num_sms = op_num_sms(device);
+  static OncePerDevice once;
+  const cudaError_t e = once.run(device, [] {
+    return cudaFuncSetAttribute(linear_few_kernel<TOut, kRows>,
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+  });
   if (e != cudaSuccess) return e;
   linear_few_kernel<TOut, kRows>
       <<<(unsigned)(ctas < 8 * num_sms ? ctas : 8 * num_sms), kFewThreads, smem, st>>>(
@@ -581,18 +588,17 @@ extern "C" agnes_status agnes_mx4_linear(const void* x, int64_t x_stride, int64_
   // a single row has no next one: any stride will do
   if (rows == 1) x_stride = mx4_row_bytes(dim);
   if (width == 1) w_stride = mx4_row_bytes(dim);
-  const int sms = op_num_sms(device);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const cudaError_t e = with_float_type(out_dtype, [&](auto t) {
     using TOut = typename decltype(t)::type;
     if (rows <= kFewRows && few_smem(rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8,
                                      a.blocks) <= kFewSmem) {
-      if (rows == 1) return launch_few<TOut, 1>(x, x_stride, w, w_stride, a, sms, st);
-      if (rows == 2) return launch_few<TOut, 2>(x, x_stride, w, w_stride, a, sms, st);
-      if (rows <= 4) return launch_few<TOut, 4>(x, x_stride, w, w_stride, a, sms, st);
-      return launch_few<TOut, 8>(x, x_stride, w, w_stride, a, sms, st);
+      if (rows == 1) return launch_few<TOut, 1>(x, x_stride, w, w_stride, a, device, st);
+      if (rows == 2) return launch_few<TOut, 2>(x, x_stride, w, w_stride, a, device, st);
+      if (rows <= 4) return launch_few<TOut, 4>(x, x_stride, w, w_stride, a, device, st);
+      return launch_few<TOut, 8>(x, x_stride, w, w_stride, a, device, st);
     }
-    return launch_linear<TOut>(x, x_stride, w, w_stride, a, sms, st);
+    return launch_linear<TOut>(x, x_stride, w, w_stride, a, device, st);
   });
   return op_launched(op, e);
 }

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/agnes_ops.h"
 #include "common.cuh"
 #include "internal.h"
@@ -125,6 +127,23 @@ agnes_status mx4_check_stride(const char* op, const char* name, int64_t rows, in
                               int64_t stride);
 // Multiprocessors of `device` (looked up once for each device).
 int op_num_sms(int device);
+
+// What a kernel needs set once on each device (its shared-memory limit) before its
+// first launch there.
+class OncePerDevice {
+ public:
+  template <typename F>
+  cudaError_t run(int device, F&& f) {
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done_.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    const cudaError_t e = f();
+    if (e == cudaSuccess && device < 64) done_.fetch_or(bit, std::memory_order_release);
+    return e;
+  }
+
+ private:
+  std::atomic<uint64_t> done_{0};
+};
 
 #define OP_TRY(call)                          \
   do {                                        \

@@ -62,6 +62,13 @@ def _stream(device) -> int | None:
     return torch.cuda.current_stream(device).cuda_stream or None
 
 
+# the same number without a Stream object around it (2 us of host time a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+if _raw_stream is not None:
+    def _stream(device) -> int | None:  # noqa: F811
+        return _raw_stream(device.index) or None
+
+
 def _status_word(status, device) -> int:
     if status is None:
         status = _status.get(device.index)
@@ -98,51 +105,55 @@ def check(device=None) -> None:
     raise AgnesError(1, "an id or index is at or past the end of its range")
 
 
-def _rows(name: str, t: torch.Tensor, device=None) -> torch.Tensor:
-    """A matrix of floats whose rows' elements are adjacent."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _FLOATS:
+def _rows(name: str, t: torch.Tensor, device=None):
+    """(device, rows, columns, row stride) of a matrix of floats whose rows' elements
+    are adjacent."""
+    if not isinstance(t, torch.Tensor) or t.ndim != 2 or t.dtype not in _FLOATS:
         raise TypeError(f"{name} must be a 2-D float32, float16 or bfloat16 tensor")
-    if t.numel() and ((t.shape[1] > 1 and t.stride(1) != 1)
-                      or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+    n, dim = t.shape
+    step, unit = t.stride()
+    if n <= 1:
+        step = dim  # there is no next row
+    if (unit != 1 and dim > 1 or step < dim) and n and dim:
         raise ValueError(f"{name} must have adjacent elements in each row")
-    return _on(name, t, device)
+    return _on(name, t, device), n, dim, step
 
 
-def _on(name: str, t: torch.Tensor, device) -> torch.Tensor:
+def _on(name: str, t: torch.Tensor, device):
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a CUDA device")
-    if device is not None and t.device != device:
+    if device is None:
+        return t.device
+    if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    return t
+    return device
 
 
-def _stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-def _ids(name: str, t: torch.Tensor, device) -> torch.Tensor:
-    if not isinstance(t, torch.Tensor) or t.dtype not in _INDEXES:
+def _ids(name: str, t: torch.Tensor, device) -> int:
+    """The bits of a contiguous tensor of indexes."""
+    bits = _INDEXES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if bits is None:
         raise TypeError(f"{name} must be an int32 or int64 tensor")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return _on(name, t, device)
+    _on(name, t, device)
+    return bits
 
 
-def _float_type(dtype) -> int:
-    if dtype not in _FLOATS:
-        raise TypeError(f"{dtype} is not float32, float16 or bfloat16")
-    return _FLOATS[dtype]
-
-
-def _output(out, shape, dtype, device, name="out"):
-    """(tensor, stride) of an output: the caller's `out`, or a new one."""
+def _output(out, n, dim, dtype, device):
+    """(tensor, its type's code, row stride) of an output [n, dim]: the caller's `out`,
+    or a new one of `dtype`."""
     if out is None:
-        _float_type(dtype)
-        return torch.empty(shape, dtype=dtype, device=device)
-    _rows(name, out, device)
-    if tuple(out.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(out.shape)}")
-    return out
+        code = _FLOATS.get(dtype)
+        if code is None:
+            raise TypeError(f"{dtype} is not float32, float16 or bfloat16")
+        return torch.empty((n, dim), dtype=dtype, device=device), code, dim
+    _, rows, cols, step = _rows("out", out, device)
+    if (rows, cols) != (n, dim):
+        raise ValueError(f"out must be {(n, dim)}, not {(rows, cols)}")
+    if dtype is not None and dtype != out.dtype:
+        raise TypeError("out has another type than out_dtype")
+    return out, _FLOATS[out.dtype], step
 
 
 # ---- embeddings -------------------------------------------------------------------------
@@ -154,31 +165,27 @@ def embedding_lookup(table, ids, scale: float = 1.0, out_dtype=None, out=None, s
     [rows, dim] for ``ids`` of any shape, as [*ids.shape, dim] of ``out_dtype`` (the
     table's by default).  A negative id gives zeros.  ``out``: [ids.numel(), dim],
     its rows adjacent or not, written instead of a new tensor and returned."""
-    device = _rows("table", table).device
-    _ids("ids", ids, device)
-    n, dim = ids.numel(), table.shape[1]
-    y = _output(out, (n, dim), out_dtype or table.dtype, device)
-    if out is not None and out_dtype not in (None, out.dtype):
-        raise TypeError("out has another type than out_dtype")
+    device, rows, dim, step = _rows("table", table)
+    bits = _ids("ids", ids, device)
+    n = ids.numel()
+    if out is None and out_dtype is None:
+        out_dtype = table.dtype
+    y, code, out_step = _output(out, n, dim, out_dtype, device)
     _check(lib().agnes_embedding_lookup(
-        table.data_ptr(), _FLOATS[table.dtype], table.shape[0], _stride(table), dim,
-        ids.data_ptr(), _INDEXES[ids.dtype], n, scale, y.data_ptr(), _FLOATS[y.dtype], _stride(y),
-        _status_word(status, device), _stream(device)))
-    return y if out is not None or ids.dim() == 1 else y.view(*ids.shape, dim)
+        table.data_ptr(), _FLOATS[table.dtype], rows, step, dim, ids.data_ptr(), bits, n, scale,
+        y.data_ptr(), code, out_step, _status_word(status, device), _stream(device)))
+    return y if out is not None or ids.ndim == 1 else y.view(*ids.shape, dim)
 
 
 def _grad_arguments(grad, ids):
-    device = _rows("grad", grad).device
-    _ids("ids", ids, device)
-    if ids.numel() != grad.shape[0]:
-        raise ValueError(f"{ids.numel()} ids for {grad.shape[0]} rows of grad")
-    return device
-
-
-def _grad_workspace(n, dim, device):
+    device, n, dim, step = _rows("grad", grad)
+    bits = _ids("ids", ids, device)
+    if ids.numel() != n:
+        raise ValueError(f"{ids.numel()} ids for {n} rows of grad")
     need = ctypes.c_int64()
     _check(lib().agnes_embedding_grad_workspace(n, dim, ctypes.byref(need)))
-    return torch.empty(need.value, dtype=torch.uint8, device=device)
+    ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+    return device, n, dim, ws, (grad.data_ptr(), _FLOATS[grad.dtype], step, ids.data_ptr(), bits, n)
 
 
 @_streamed
@@ -188,17 +195,14 @@ def embedding_grad(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=None,
     [num_rows, dim] of ``out_dtype`` (grad's by default), row v the scaled sum of the
     rows of ``grad`` [n, dim] whose id (``ids``, n of any shape) is v, zeros where
     there is none.  ``out``: written instead of a new tensor; contiguous."""
-    device = _grad_arguments(grad, ids)
-    n, dim = grad.shape
-    y = _output(out, (num_rows, dim), out_dtype or grad.dtype, device)
-    if out is not None and out_dtype not in (None, out.dtype):
-        raise TypeError("out has another type than out_dtype")
-    if not y.is_contiguous():
+    device, n, dim, ws, arguments = _grad_arguments(grad, ids)
+    if out is None and out_dtype is None:
+        out_dtype = grad.dtype
+    y, code, step = _output(out, num_rows, dim, out_dtype, device)
+    if step != dim:
         raise ValueError("out must be contiguous")
-    ws = _grad_workspace(n, dim, device)
     _check(lib().agnes_embedding_grad(
-        grad.data_ptr(), _FLOATS[grad.dtype], _stride(grad), ids.data_ptr(), _INDEXES[ids.dtype],
-        n, num_rows, dim, scale, y.data_ptr(), _FLOATS[y.dtype], ws.data_ptr(), ws.numel(),
+        *arguments, num_rows, dim, scale, y.data_ptr(), code, ws.data_ptr(), ws.numel(),
         _status_word(status, device), _stream(device)))
     return y
 
@@ -210,15 +214,12 @@ def embedding_grad_rows(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=
     tables too large for a dense one.  Its shapes do not depend on the ids, so
     ``table.index_add_(0, g.ids.clamp(min=0), g.rows, alpha=-lr)`` needs no read-back:
     the rows past ``count`` are zeros."""
-    device = _grad_arguments(grad, ids)
-    n, dim = grad.shape
-    rows = _output(None, (n, dim), out_dtype or grad.dtype, device)
+    device, n, dim, ws, arguments = _grad_arguments(grad, ids)
+    rows, code, _ = _output(None, n, dim, out_dtype or grad.dtype, device)
     out_ids = torch.empty(n, dtype=torch.int32, device=device)
     count = torch.empty(1, dtype=torch.int32, device=device)
-    ws = _grad_workspace(n, dim, device)
     _check(lib().agnes_embedding_grad_rows(
-        grad.data_ptr(), _FLOATS[grad.dtype], _stride(grad), ids.data_ptr(), _INDEXES[ids.dtype],
-        n, num_rows, dim, scale, out_ids.data_ptr(), rows.data_ptr(), _FLOATS[rows.dtype],
+        *arguments, num_rows, dim, scale, out_ids.data_ptr(), rows.data_ptr(), code,
         count.data_ptr(), ws.data_ptr(), ws.numel(), _status_word(status, device),
         _stream(device)))
     return RowGrad(out_ids, rows, count)
@@ -228,17 +229,17 @@ def embedding_grad_rows(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=
 
 
 def _distill_arguments(logits, teacher, index):
-    device = _rows("logits", logits).device
-    _rows("teacher", teacher, device)
-    _ids("index", index, device)
-    if not teacher.is_contiguous():
+    device, n, classes, step = _rows("logits", logits)
+    _, rows, top, teacher_step = _rows("teacher", teacher, device)
+    bits = _ids("index", index, device)
+    if teacher_step != top and rows and top:
         raise ValueError("teacher must be contiguous")
-    if teacher.shape[0] != logits.shape[0] or index.shape != teacher.shape:
+    if rows != n or index.shape != teacher.shape:
         raise ValueError(f"teacher {tuple(teacher.shape)} and index {tuple(index.shape)} must be "
-                         f"[{logits.shape[0]}, top]")
-    return device, (logits.data_ptr(), _FLOATS[logits.dtype], _stride(logits), logits.shape[0],
-                    logits.shape[1], teacher.data_ptr(), _FLOATS[teacher.dtype], index.data_ptr(),
-                    _INDEXES[index.dtype], teacher.shape[1])
+                         f"[{n}, top]")
+    return device, n, classes, (
+        logits.data_ptr(), _FLOATS[logits.dtype], step, n, classes, teacher.data_ptr(),
+        _FLOATS[teacher.dtype], index.data_ptr(), bits, top)
 
 
 def _weight_arguments(weight, rows, device):
@@ -246,7 +247,8 @@ def _weight_arguments(weight, rows, device):
         return None, float(weight)
     if weight.dtype != torch.float32 or weight.shape != (rows,) or not weight.is_contiguous():
         raise TypeError(f"weight must be a number or a contiguous float32 tensor [{rows}]")
-    return _on("weight", weight, device).data_ptr(), 1.0
+    _on("weight", weight, device)
+    return weight.data_ptr(), 1.0
 
 
 @_streamed
@@ -255,9 +257,9 @@ def distill_loss(logits, teacher, index, temperature: float = 1.0, status=None):
     ``logits`` [rows, classes], ``teacher`` [rows, top] with their classes ``index``
     (negative: absent).  Returns (loss float32 [rows], stats float32 [rows, 2]);
     ``distill_grad`` takes the stats."""
-    device, arguments = _distill_arguments(logits, teacher, index)
-    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=device)
-    stats = torch.empty((logits.shape[0], 2), dtype=torch.float32, device=device)
+    device, n, _, arguments = _distill_arguments(logits, teacher, index)
+    loss = torch.empty(n, dtype=torch.float32, device=device)
+    stats = torch.empty((n, 2), dtype=torch.float32, device=device)
     _check(lib().agnes_distill_loss(*arguments, temperature, loss.data_ptr(), stats.data_ptr(),
                                     _status_word(status, device), _stream(device)))
     return loss, stats
@@ -270,18 +272,17 @@ def distill_grad(logits, teacher, index, stats, weight=1.0, temperature: float =
     ``weight`` a number or float32 [rows], ``stats`` from ``distill_loss``.  ``out``:
     written instead of a new tensor of ``out_dtype`` (the logits' by default); it may
     be ``logits``."""
-    device, arguments = _distill_arguments(logits, teacher, index)
-    if stats.dtype != torch.float32 or stats.shape != (logits.shape[0], 2) or \
-            not stats.is_contiguous():
+    device, n, classes, arguments = _distill_arguments(logits, teacher, index)
+    if stats.dtype != torch.float32 or stats.shape != (n, 2) or not stats.is_contiguous():
         raise TypeError("stats must be what distill_loss returned")
     _on("stats", stats, device)
-    w, scale = _weight_arguments(weight, logits.shape[0], device)
-    y = _output(out, logits.shape, out_dtype or logits.dtype, device)
-    if out is not None and out_dtype not in (None, out.dtype):
-        raise TypeError("out has another type than out_dtype")
-    _check(lib().agnes_distill_grad(*arguments, temperature, stats.data_ptr(), w, scale,
-                                    y.data_ptr(), _FLOATS[y.dtype], _stride(y),
-                                    _status_word(status, device), _stream(device)))
+    w, w_scale = _weight_arguments(weight, n, device)
+    if out is None and out_dtype is None:
+        out_dtype = logits.dtype
+    y, code, step = _output(out, n, classes, out_dtype, device)
+    _check(lib().agnes_distill_grad(*arguments, temperature, stats.data_ptr(), w, w_scale,
+                                    y.data_ptr(), code, step, _status_word(status, device),
+                                    _stream(device)))
     return y
 
 
@@ -290,15 +291,15 @@ def distill_loss_grad(logits, teacher, index, weight=1.0, temperature: float = 1
                       out_dtype=None, out=None, status=None):
     """(loss, gradient) in one call, the logits read once (agnes_distill_loss_grad);
     arguments as for ``distill_loss`` and ``distill_grad``."""
-    device, arguments = _distill_arguments(logits, teacher, index)
-    w, scale = _weight_arguments(weight, logits.shape[0], device)
-    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=device)
-    y = _output(out, logits.shape, out_dtype or logits.dtype, device)
-    if out is not None and out_dtype not in (None, out.dtype):
-        raise TypeError("out has another type than out_dtype")
-    _check(lib().agnes_distill_loss_grad(*arguments, temperature, w, scale, loss.data_ptr(),
-                                         y.data_ptr(), _FLOATS[y.dtype], _stride(y),
-                                         _status_word(status, device), _stream(device)))
+    device, n, classes, arguments = _distill_arguments(logits, teacher, index)
+    w, w_scale = _weight_arguments(weight, n, device)
+    loss = torch.empty(n, dtype=torch.float32, device=device)
+    if out is None and out_dtype is None:
+        out_dtype = logits.dtype
+    y, code, step = _output(out, n, classes, out_dtype, device)
+    _check(lib().agnes_distill_loss_grad(*arguments, temperature, w, w_scale, loss.data_ptr(),
+                                         y.data_ptr(), code, step, _status_word(status, device),
+                                         _stream(device)))
     return loss, y
 
 
@@ -313,21 +314,22 @@ def mx4_row_bytes(dim: int) -> int:
 
 
 def _packed(name, t, dim, device=None):
-    """A matrix of 4-bit rows: uint8 [rows, mx4_row_bytes(dim)], or the same bytes as
-    float16 or float32 "features", as a graph gathers them."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or \
+    """(device, rows, row stride in bytes) of a matrix of 4-bit rows: uint8
+    [rows, mx4_row_bytes(dim)], or the same bytes as float16 or float32 "features", as a
+    graph gathers them."""
+    if not isinstance(t, torch.Tensor) or t.ndim != 2 or \
             t.dtype not in (torch.uint8, torch.float16, torch.float32):
         raise TypeError(f"{name} must be a 2-D tensor of 4-bit rows")
+    n, cols = t.shape
+    step, unit = t.stride()
     size = t.element_size()
-    if dim < 1 or t.shape[1] * size != (dim + 31) // 32 * 17 + -((dim + 31) // 32 * 17) % 16:
-        raise ValueError(f"{name} has rows of {t.shape[1] * size} bytes, not those of {dim} values")
-    if t.numel() and (t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+    if dim < 1 or cols * size != ((dim + 31) // 32 * 17 + 15) // 16 * 16:
+        raise ValueError(f"{name} has rows of {cols * size} bytes, not those of {dim} values")
+    if n <= 1:
+        step = cols  # there is no next row
+    if (unit != 1 or step < cols) and n:
         raise ValueError(f"{name} must have adjacent bytes in each row")
-    return _on(name, t, device)
-
-
-def _stride_bytes(t) -> int:
-    return _stride(t) * t.element_size()
+    return _on(name, t, device), n, step * size
 
 
 @_streamed
@@ -335,26 +337,25 @@ def mx4_quantize(x, out=None):
     """Rows of ``x`` [rows, dim] rounded to microscaled 4-bit rows (agnes_mx4_quantize):
     uint8 [rows, mx4_row_bytes(dim)].  ``.view(torch.float16)`` of them makes a graph's
     features."""
-    device = _rows("x", x).device
-    rows, dim = x.shape
+    device, rows, dim, step = _rows("x", x)
     if out is None:
-        out = torch.empty((rows, mx4_row_bytes(dim)), dtype=torch.uint8, device=device)
+        out_step = mx4_row_bytes(dim)
+        out = torch.empty((rows, out_step), dtype=torch.uint8, device=device)
     else:
-        _packed("out", out, dim, device)
-        if out.shape[0] != rows:
-            raise ValueError(f"out has {out.shape[0]} rows, not {rows}")
-    _check(lib().agnes_mx4_quantize(x.data_ptr(), _FLOATS[x.dtype], _stride(x), rows, dim,
-                                    out.data_ptr(), _stride_bytes(out), _stream(device)))
+        _, n, out_step = _packed("out", out, dim, device)
+        if n != rows:
+            raise ValueError(f"out has {n} rows, not {rows}")
+    _check(lib().agnes_mx4_quantize(x.data_ptr(), _FLOATS[x.dtype], step, rows, dim,
+                                    out.data_ptr(), out_step, _stream(device)))
     return out
 
 
 @_streamed
 def mx4_dequantize(x, dim: int, out_dtype=torch.float32, out=None):
     """The values [rows, dim] that 4-bit rows stand for (agnes_mx4_dequantize)."""
-    device = _packed("x", x, dim).device
-    y = _output(out, (x.shape[0], dim), out_dtype if out is None else out.dtype, device)
-    _check(lib().agnes_mx4_dequantize(x.data_ptr(), _stride_bytes(x), x.shape[0], dim,
-                                      y.data_ptr(), _FLOATS[y.dtype], _stride(y),
+    device, rows, step = _packed("x", x, dim)
+    y, code, out_step = _output(out, rows, dim, out_dtype if out is None else None, device)
+    _check(lib().agnes_mx4_dequantize(x.data_ptr(), step, rows, dim, y.data_ptr(), code, out_step,
                                       _stream(device)))
     return y
 
@@ -364,16 +365,16 @@ def mx4_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, sta
     """``x @ w.T + bias`` of 4-bit rows (agnes_mx4_linear): ``x`` [rows, bytes], for example a
     minibatch's gathered features, ``w`` [width, bytes], both of ``dim`` values a row;
     ``bias`` float32 [width] or None.  Returns [rows, width]."""
-    device = _packed("x", x, dim).device
-    _packed("w", w, dim, device)
-    rows, width = x.shape[0], w.shape[0]
+    device, rows, step = _packed("x", x, dim)
+    _, width, w_step = _packed("w", w, dim, device)
+    at = None
     if bias is not None:
         if bias.dtype != torch.float32 or bias.shape != (width,) or not bias.is_contiguous():
             raise TypeError(f"bias must be a contiguous float32 tensor [{width}]")
         _on("bias", bias, device)
-    y = _output(out, (rows, width), out_dtype if out is None else out.dtype, device)
-    _check(lib().agnes_mx4_linear(
-        x.data_ptr(), _stride_bytes(x), rows, w.data_ptr(), _stride_bytes(w), width, dim,
-        bias.data_ptr() if bias is not None else None, y.data_ptr(), _FLOATS[y.dtype], _stride(y),
-        _status_word(status, device), _stream(device)))
+        at = bias.data_ptr()
+    y, code, out_step = _output(out, rows, width, out_dtype if out is None else None, device)
+    _check(lib().agnes_mx4_linear(x.data_ptr(), step, rows, w.data_ptr(), w_step, width, dim, at,
+                                  y.data_ptr(), code, out_step, _status_word(status, device),
+                                  _stream(device)))
     return y

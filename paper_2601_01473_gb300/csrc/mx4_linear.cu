@@ -35,18 +35,29 @@ constexpr int kCodeBytes = kTile * kStageBytesK;
 constexpr int kScaleRun = 16;     // scale bytes the TMA brings per row, for two stages
 constexpr int kScaleBytes = kTile * kScaleRun;
 constexpr int kStageBytes = 2 * kCodeBytes + 2 * kScaleBytes;
-constexpr int kStages = 5;
+constexpr int kStages = 4;
 constexpr int kScaleCols = 16;    // tensor-memory columns of a stage's scales
 constexpr int kScaleCol0 = 2 * kTile;  // after two accumulators
 constexpr int kTmemCols = 512;
-// warps: 0-3 epilogue, 4-7 scales, 8 producer, 9 MMA
-constexpr int kScaleWarp0 = 4;
-constexpr int kProducerWarp = 8;
-constexpr int kMmaWarp = 9;
-constexpr int kThreads = 320;
+// warps: 0-7 epilogue (two to a quarter of tensor memory's lanes, half the columns
+// each), 8-11 scales, 12 producer, 13 MMA
+constexpr int kEpilogueWarps = 8;
+constexpr int kEpilogueCols = kTile / (kEpilogueWarps / 4);
+constexpr int kScaleWarp0 = kEpilogueWarps;
+constexpr int kProducerWarp = kScaleWarp0 + 4;
+constexpr int kMmaWarp = kProducerWarp + 1;
+constexpr int kThreads = 32 * (kMmaWarp + 1);
 constexpr int kBars = 3 * kStages + 5;
-constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + 1024 + 8 * kBars + 16;
-static_assert(kStageBytes % 1024 == 0, "the swizzled tiles stay 1024-byte aligned");
+// An epilogue warp's output on its way to memory: 32 rows of 128 bytes, twice.
+constexpr int kOutBytes = 32 * 128;
+constexpr int kOutBuffers = 2;
+constexpr int kOutStage = kEpilogueWarps * kOutBuffers * kOutBytes;
+constexpr size_t kSmemBytes =
+    (size_t)kStages * kStageBytes + kOutStage + 1024 + 8 * kBars + 16;
+static_assert(kStageBytes % 1024 == 0 && kOutBytes % 1024 == 0,
+              "the swizzled tiles stay 1024-byte aligned");
+static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
+static_assert(kEpilogueCols % 64 == 0, "whole groups of the widest output");
 static_assert(kScaleCol0 + kStages * kScaleCols <= kTmemCols, "tensor memory");
 
 struct LinearArgs {
@@ -55,6 +66,8 @@ struct LinearArgs {
   const float* bias;
   void* out;
   int64_t out_stride;
+  bool tma_out;    // the output's rows suit the TMA
+  bool bias_wide;  // there is a bias, 16-byte aligned
   int32_t* status;
 };
 
@@ -161,40 +174,69 @@ struct Ring {
   }
 };
 
-// 32 columns of a row of the output from column c0 on.
+// 32 columns of a row of the output from column c0 on, for rows that do not suit
+// the TMA.
 template <typename TOut>
 __device__ __forceinline__ void store_columns(const LinearArgs& a, TOut* row, int64_t c0,
-                                              const uint32_t (&v)[32], bool wide) {
-  if (wide && c0 + 32 <= a.width) {
-    constexpr int kN = 16 / sizeof(TOut);
+                                              const uint32_t (&v)[32]) {
 #pragma unroll
-    for (int q = 0; q < 32 / kN; ++q) {
-      Vec<TOut, kN> y;
-#pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        const float b = a.bias ? __ldg(a.bias + c0 + q * kN + e) : 0.f;
-        y.v[e] = from_f32<TOut>(__uint_as_float(v[q * kN + e]) + b);
-      }
-      *(Vec<TOut, kN>*)(row + c0 + q * kN) = y;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      if (c0 + e >= a.width) break;
-      const float b = a.bias ? __ldg(a.bias + c0 + e) : 0.f;
-      row[c0 + e] = from_f32<TOut>(__uint_as_float(v[e]) + b);
-    }
+  for (int e = 0; e < 32; ++e) {
+    if (c0 + e >= a.width) break;
+    const float b = a.bias ? __ldg(a.bias + c0 + e) : 0.f;
+    row[c0 + e] = from_f32<TOut>(__uint_as_float(v[e]) + b);
   }
+}
+
+// 32 columns of a lane's row into its warp's buffer, from byte `first` of its 128 on:
+// 16-byte pieces permuted by the row as the TMA's 128-byte swizzle has them, so that
+// eight lanes' pieces lie in different banks.
+template <typename TOut>
+__device__ __forceinline__ void stage_columns(const LinearArgs& a, uint8_t* buffer, int lane,
+                                              int first, int64_t c0, const uint32_t (&v)[32]) {
+  constexpr int kN = 16 / sizeof(TOut);
+  float f[32];
+#pragma unroll
+  for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
+  if (a.bias_wide) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+      const float4 b = __ldg((const float4*)(a.bias + c0 + e));
+      f[e] += b.x;
+      f[e + 1] += b.y;
+      f[e + 2] += b.z;
+      f[e + 3] += b.w;
+    }
+  } else if (a.bias) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) f[e] += __ldg(a.bias + c0 + e);
+  }
+#pragma unroll
+  for (int q = 0; q < 32 / kN; ++q) {
+    Vec<TOut, kN> y;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) y.v[e] = from_f32<TOut>(f[q * kN + e]);
+    *(Vec<TOut, kN>*)(buffer + lane * 128 + (((first / 16 + q) ^ (lane & 7)) << 4)) = y;
+  }
+}
+
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, int32_t x, int32_t y,
+                                          uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                   map),
+               "r"(x), "r"(y), "r"(src)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
 template <typename TOut>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant__ CUtensorMap x_scales,
               const __grid_constant__ CUtensorMap w_codes, const __grid_constant__ CUtensorMap w_scales,
-              const LinearArgs a) {
+              const __grid_constant__ CUtensorMap out_map, const LinearArgs a) {
   extern __shared__ uint8_t raw[];
   uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
-  uint64_t* bars = (uint64_t*)(smem + (size_t)kStages * kStageBytes);
+  uint8_t* out_stage = smem + (size_t)kStages * kStageBytes;
+  uint64_t* bars = (uint64_t*)(out_stage + kOutStage);
   uint32_t* tmem_slot = (uint32_t*)(bars + kBars);
   const Bars bar = {smem_addr(bars)};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -213,7 +255,7 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
     }
     for (int d = 0; d < 2; ++d) {
       mbar_init(bar.done(d), 1);
-      mbar_init(bar.taken(d), 4);
+      mbar_init(bar.taken(d), kEpilogueWarps);
     }
     mbar_init(bar.drained(), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -326,7 +368,9 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
       }
     }
   } else {
-    const bool wide = (uintptr_t)a.out % 16 == 0 && a.out_stride * (int64_t)sizeof(TOut) % 16 == 0;
+    constexpr int kGroup = 128 / sizeof(TOut);  // columns of a staged buffer
+    uint8_t* mine = out_stage + warp * kOutBuffers * kOutBytes;
+    int buffer = 0;
     Ring acc;
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
       const int d = acc.slot;
@@ -335,20 +379,42 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
         break;
       }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int64_t row = t / tiles_n * kTile + warp * 32 + lane;
-      const int64_t n0 = t % tiles_n * kTile;
-      TOut* to = (TOut*)a.out + row * a.out_stride;
-      for (int c = 0; c < kTile; c += 32) {
-        if (n0 + c >= a.width) break;
-        uint32_t v[32];
-        tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)(d * kTile + c), v);
-        if (row < a.rows) store_columns<TOut>(a, to, n0 + c, v, wide);
+      const int64_t row0 = t / tiles_n * kTile + (warp & 3) * 32;
+      const int64_t n0 = t % tiles_n * kTile + (warp >> 2) * kEpilogueCols;
+      const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
+                            (uint32_t)(d * kTile + (warp >> 2) * kEpilogueCols);
+      for (int c = 0; c < kEpilogueCols && n0 + c < a.width; c += kGroup) {
+        // whole groups only: at a ragged end the TMA writes up to a 16-byte boundary
+        const bool staged = a.tma_out && n0 + c + kGroup <= a.width;
+        if (staged) {  // the store before the last has read the buffer
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          __syncwarp();
+        }
+#pragma unroll
+        for (int h = 0; h < kGroup / 32; ++h) {
+          uint32_t v[32];
+          tmem_load32(from + (uint32_t)(c + h * 32), v);
+          if (staged)
+            stage_columns<TOut>(a, mine + buffer * kOutBytes, lane, h * 64, n0 + c + h * 32, v);
+          else if (row0 + lane < a.rows)
+            store_columns<TOut>(a, (TOut*)a.out + (row0 + lane) * a.out_stride, n0 + c + h * 32, v);
+        }
+        if (staged) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0 && row0 < a.rows)  // rows past the end are left out
+            tma_store(&out_map, (int32_t)(n0 + c), (int32_t)row0,
+                      smem_addr(mine + buffer * kOutBytes));
+          buffer ^= 1;
+        }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(bar.taken(d));
       acc.next(2);
     }
+    // the stores in flight have read shared memory before the CTA leaves
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
   }
   if (!ok) op_flag(a.status, AGNES_OP_TIMEOUT);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -472,35 +538,51 @@ EncodeTiled encode_tiled() {
   return (EncodeTiled)fn;
 }
 
-// `rows` rows of `bytes` bytes, `stride` bytes apart, in boxes of kTile rows x
-// box_bytes; zeros past either end.
-bool map_rows(EncodeTiled encode, CUtensorMap* map, const void* p, int64_t bytes, int64_t rows,
-              int64_t stride, int box_bytes, CUtensorMapSwizzle swizzle) {
-  const cuuint64_t size[2] = {(cuuint64_t)bytes, (cuuint64_t)rows};
+// `rows` rows of `cols` elements of `type`, `stride` bytes apart, in boxes of
+// box_rows x box_cols; zeros past either end.
+bool map_rows(EncodeTiled encode, CUtensorMap* map, CUtensorMapDataType type, const void* p,
+              int64_t cols, int64_t rows, int64_t stride, int box_cols, int box_rows,
+              CUtensorMapSwizzle swizzle) {
+  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)stride};
-  const cuuint32_t box[2] = {(cuuint32_t)box_bytes, (cuuint32_t)kTile};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
   const cuuint32_t step[2] = {1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)p, size, strides, box, step,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+  return encode(map, type, 2, (void*)p, size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <typename T>
+constexpr CUtensorMapDataType kMapType = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+template <>
+constexpr CUtensorMapDataType kMapType<__half> = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+template <>
+constexpr CUtensorMapDataType kMapType<__nv_bfloat16> = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+
 template <typename TOut>
 cudaError_t launch_linear(const void* x, int64_t x_stride, const void* w, int64_t w_stride,
-                          const LinearArgs& a, int device, cudaStream_t st) {
+                          LinearArgs a, int device, cudaStream_t st) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return cudaErrorNotSupported;
   const int64_t codes = (int64_t)a.blocks * 16;
   const uint8_t *xb = (const uint8_t*)x, *wb = (const uint8_t*)w;
-  CUtensorMap xc, xs, wc, ws;
-  if (!map_rows(encode, &xc, xb, codes, a.rows, x_stride, kStageBytesK,
-                CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !map_rows(encode, &xs, xb + codes, a.blocks, a.rows, x_stride, kScaleRun,
-                CU_TENSOR_MAP_SWIZZLE_NONE) ||
-      !map_rows(encode, &wc, wb, codes, a.width, w_stride, kStageBytesK,
-                CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !map_rows(encode, &ws, wb + codes, a.blocks, a.width, w_stride, kScaleRun,
-                CU_TENSOR_MAP_SWIZZLE_NONE))
+  CUtensorMap xc, xs, wc, ws, out = {};
+  const auto bytes = [&](CUtensorMap* map, const void* p, int64_t cols, int64_t rows,
+                         int64_t stride, int box, CUtensorMapSwizzle swizzle) {
+    return map_rows(encode, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, p, cols, rows, stride, box, kTile,
+                    swizzle);
+  };
+  if (!bytes(&xc, xb, codes, a.rows, x_stride, kStageBytesK, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !bytes(&xs, xb + codes, a.blocks, a.rows, x_stride, kScaleRun,
+             CU_TENSOR_MAP_SWIZZLE_NONE) ||
+      !bytes(&wc, wb, codes, a.width, w_stride, kStageBytesK, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !bytes(&ws, wb + codes, a.blocks, a.width, w_stride, kScaleRun, CU_TENSOR_MAP_SWIZZLE_NONE))
+    return cudaErrorInvalidValue;
+  const int64_t out_bytes = a.out_stride * (int64_t)sizeof(TOut);
+  a.tma_out = aligned_rows(a.out, out_bytes, 16) && out_bytes < (1ll << 40);
+  if (a.tma_out &&
+      !map_rows(encode, &out, kMapType<TOut>, a.out, a.width, a.rows, out_bytes,
+                (int)(128 / sizeof(TOut)), 32, CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
   static OncePerDevice once;
   const cudaError_t e = once.run(device, [] {
@@ -511,7 +593,7 @@ cudaError_t launch_linear(const void* x, int64_t x_stride, const void* w, int64_
   const int64_t tiles = ceil_div(a.rows, kTile) * ceil_div(a.width, kTile);
   const int num_sms = op_num_sms(device);
   linear_kernel<TOut><<<(unsigned)(tiles < num_sms ? tiles : num_sms), kThreads, kSmemBytes, st>>>(
-      xc, xs, wc, ws, a);
+      xc, xs, wc, ws, out, a);
   return cudaGetLastError();
 }
 
@@ -582,12 +664,14 @@ extern "C" agnes_status agnes_mx4_linear(const void* x, int64_t x_stride, int64_
   a.width = width;
   a.blocks = (int32_t)mx4_blocks(dim);
   a.bias = bias;
+  a.bias_wide = bias && (uintptr_t)bias % 16 == 0;
   a.out = out;
   a.out_stride = out_stride;
   a.status = status;
   // a single row has no next one: any stride will do
   if (rows == 1) x_stride = mx4_row_bytes(dim);
   if (width == 1) w_stride = mx4_row_bytes(dim);
+  if (rows == 1) a.out_stride = width;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const cudaError_t e = with_float_type(out_dtype, [&](auto t) {
     using TOut = typename decltype(t)::type;

@@ -4,14 +4,20 @@
 // Many rows: the block-scaled tensor-core product (tcgen05.mma kind::mxf4), which
 // takes e2m1 codes from shared memory and the blocks' scale bytes from tensor
 // memory.  Persistent CTAs, one per SM, over output tiles of 128 x 128:
-//   the producer      has the TMA copy a stage: 256 codes of 128 rows of x and of
-//                     w, and the 16-byte runs that hold their scale bytes;
-//   the scale warps   put the stage's scale bytes from shared into tensor
-//                     memory: lane l of each quarter, column g, holds those of
-//                     row 32 g + l for four blocks;
+//   the producer      has the TMA copy a stage: 256 codes of 128 rows of x and of w;
+//   the scale warps   load the rows' scale bytes, a thread to a row and 512 values
+//                     at a time, pass them round through shared memory, and put
+//                     them into tensor memory: lane l of each quarter, column g,
+//                     holds those of row 32 g + l for four blocks;
 //   the MMA warp      issues the stage's products (K = 64 each) into one of two
 //                     accumulators;
-//   the epilogue warps read the accumulator, add the bias, round and store.
+//   the epilogue warps read the accumulator, add the bias, round, and have the TMA
+//                     store it from shared memory.
+// Rows of up to 512 values: a CTA keeps to one tile of columns and its weights stay in
+// shared and tensor memory, so a tile costs the copy of x's rows alone.  (The TMA
+// takes about 5 cycles a row, however short: with w's rows copied for each tile, and
+// the scale bytes by it too, those requests took all the time, 786,432 rows of 128 to
+// 256 columns 116 us.)
 // Every wait is bounded (mbarrier.cuh).  Rows and columns past the matrices' ends
 // come as zeros from the TMA.
 //
@@ -32,13 +38,24 @@ namespace {
 constexpr int kTile = 128;        // rows, and columns, of an output tile
 constexpr int kStageBytesK = 128;  // bytes of codes of a row per stage: 256 values
 constexpr int kCodeBytes = kTile * kStageBytesK;
-constexpr int kScaleRun = 16;     // scale bytes the TMA brings per row, for two stages
+// The ring: stages of x's codes and w's, or of x's alone beside w's resident ones.
+constexpr int kSharedSlots = 4;
+constexpr int kResidentStages = 2;
+constexpr int kResidentSlots = 6;
+constexpr int kMaxSlots = kResidentSlots;
+constexpr int kRingBytes = 8 * kCodeBytes;
+static_assert(kSharedSlots * 2 == 8 && kResidentSlots + kResidentStages == 8, "the ring");
+// Scale bytes on their way: 16 of each row of x and w, twice.
+constexpr int kScaleRun = 16;  // of a row, for two stages
 constexpr int kScaleBytes = kTile * kScaleRun;
-constexpr int kStageBytes = 2 * kCodeBytes + 2 * kScaleBytes;
-constexpr int kStages = 4;
-constexpr int kScaleCols = 16;    // tensor-memory columns of a stage's scales
-constexpr int kScaleCol0 = 2 * kTile;  // after two accumulators
+constexpr int kScaleStage = 4 * kScaleBytes;
+// Tensor memory: two accumulators, each slot's scales (x's eight columns, w's
+// eight), the resident w's.
+constexpr int kScaleCols = 16;
+constexpr int kScaleCol0 = 2 * kTile;
+constexpr int kResidentCol0 = kScaleCol0 + kMaxSlots * kScaleCols;
 constexpr int kTmemCols = 512;
+static_assert(kResidentCol0 + kResidentStages * 8 <= kTmemCols, "tensor memory");
 // warps: 0-7 epilogue (two to a quarter of tensor memory's lanes, half the columns
 // each), 8-11 scales, 12 producer, 13 MMA
 constexpr int kEpilogueWarps = 8;
@@ -47,25 +64,28 @@ constexpr int kScaleWarp0 = kEpilogueWarps;
 constexpr int kProducerWarp = kScaleWarp0 + 4;
 constexpr int kMmaWarp = kProducerWarp + 1;
 constexpr int kThreads = 32 * (kMmaWarp + 1);
-constexpr int kBars = 3 * kStages + 5;
+static_assert(kScaleWarp0 % 4 == 0, "a scale warp's quarter is its place among the four");
+static_assert(kEpilogueCols % 64 == 0, "whole groups of the widest output");
 // An epilogue warp's output on its way to memory: 32 rows of 128 bytes, twice.
 constexpr int kOutBytes = 32 * 128;
 constexpr int kOutBuffers = 2;
 constexpr int kOutStage = kEpilogueWarps * kOutBuffers * kOutBytes;
+constexpr int kBars = 3 * kMaxSlots + 9;
 constexpr size_t kSmemBytes =
-    (size_t)kStages * kStageBytes + kOutStage + 1024 + 8 * kBars + 16;
-static_assert(kStageBytes % 1024 == 0 && kOutBytes % 1024 == 0,
+    (size_t)kRingBytes + kOutStage + kScaleStage + 1024 + 8 * kBars + 16;
+static_assert(kCodeBytes % 1024 == 0 && kOutBytes % 1024 == 0,
               "the swizzled tiles stay 1024-byte aligned");
 static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
-static_assert(kEpilogueCols % 64 == 0, "whole groups of the widest output");
-static_assert(kScaleCol0 + kStages * kScaleCols <= kTmemCols, "tensor memory");
 
 struct LinearArgs {
+  const uint8_t *x, *w;
+  int64_t x_stride, w_stride;
   int64_t rows, width;
   int32_t blocks;  // of 32 values
   const float* bias;
   void* out;
   int64_t out_stride;
+  bool resident;   // w's stages stay in shared memory: a CTA keeps to one tile of columns
   bool tma_out;    // the output's rows suit the TMA
   bool bias_wide;  // there is a bias, 16-byte aligned
   int32_t* status;
@@ -138,27 +158,33 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&v)[16]) {
+__device__ __forceinline__ void tmem_store8(uint32_t addr, const uint32_t* v) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
-      "%11, %12, %13, %14, %15, %16};" ::"r"(addr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-      "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
       : "memory");
+}
+
+__device__ __forceinline__ void tmem_store_wait() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
-// The mbarriers: full[s] (the TMA has brought stage s), scaled[s] (its scales are in
+// The mbarriers: full[s] (the TMA has brought slot s), scaled[s] (its scales are in
 // tensor memory), empty[s] (its products are done); done[d] / taken[d] of the
-// accumulators; drained, when the MMA warp gives up.
+// accumulators; staged[b] (the scale warps have filled buffer b); w_full / w_scaled of
+// the resident weights; drained, when the MMA warp gives up.
 struct Bars {
   uint32_t base;
-  __device__ uint32_t full(int s) const { return base + 8u * (uint32_t)s; }
-  __device__ uint32_t scaled(int s) const { return base + 8u * (uint32_t)(kStages + s); }
-  __device__ uint32_t empty(int s) const { return base + 8u * (uint32_t)(2 * kStages + s); }
-  __device__ uint32_t done(int d) const { return base + 8u * (uint32_t)(3 * kStages + d); }
-  __device__ uint32_t taken(int d) const { return base + 8u * (uint32_t)(3 * kStages + 2 + d); }
-  __device__ uint32_t drained() const { return base + 8u * (uint32_t)(3 * kStages + 4); }
+  __device__ uint32_t at(int i) const { return base + 8u * (uint32_t)i; }
+  __device__ uint32_t full(int s) const { return at(s); }
+  __device__ uint32_t scaled(int s) const { return at(kMaxSlots + s); }
+  __device__ uint32_t empty(int s) const { return at(2 * kMaxSlots + s); }
+  __device__ uint32_t done(int d) const { return at(3 * kMaxSlots + d); }
+  __device__ uint32_t taken(int d) const { return at(3 * kMaxSlots + 2 + d); }
+  __device__ uint32_t staged(int b) const { return at(3 * kMaxSlots + 4 + b); }
+  __device__ uint32_t w_full() const { return at(3 * kMaxSlots + 6); }
+  __device__ uint32_t w_scaled() const { return at(3 * kMaxSlots + 7); }
+  __device__ uint32_t drained() const { return at(3 * kMaxSlots + 8); }
 };
 
 struct Ring {
@@ -173,6 +199,77 @@ struct Ring {
     }
   }
 };
+
+// The output tiles of a CTA, every gridDim.x-th: columns change fastest, so they stay
+// the same where the grid is a multiple of the tiles across.
+struct Tiles {
+  int64_t m, n;  // tile coordinates
+  int64_t tiles_n, tiles_m, step_m, step_n;
+  __device__ explicit Tiles(const LinearArgs& a) {
+    tiles_n = (a.width + kTile - 1) / kTile;
+    tiles_m = (a.rows + kTile - 1) / kTile;
+    m = blockIdx.x / tiles_n;
+    n = blockIdx.x - m * tiles_n;
+    step_m = gridDim.x / tiles_n;
+    step_n = gridDim.x - step_m * tiles_n;
+  }
+  __device__ bool any() const { return m < tiles_m; }
+  __device__ void next() {
+    m += step_m;
+    n += step_n;
+    if (n >= tiles_n) {
+      n -= tiles_n;
+      ++m;
+    }
+  }
+};
+
+// The scale bytes of two stages of a row, zeros past the matrix and past the row's
+// blocks (the bytes there are not the row's).
+__device__ __forceinline__ uint4 scale_run(const uint8_t* p, int64_t stride, int64_t row,
+                                           int64_t rows, int32_t blocks, int pair) {
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (row >= rows) return v;
+  v = __ldg((const uint4*)(p + row * stride + (int64_t)blocks * 16) + pair);
+  const int left = blocks - pair * kScaleRun;
+  if (left < kScaleRun) {
+    const auto keep = [&](uint32_t word, int first) {
+      const int n = left - first;
+      return n >= 4 ? word : n <= 0 ? 0u : word & ((1u << (8 * n)) - 1u);
+    };
+    v = make_uint4(keep(v.x, 0), keep(v.y, 4), keep(v.z, 8), keep(v.w, 12));
+  }
+  return v;
+}
+
+// A stage's scales of 128 rows, from their runs, as the eight columns of a lane: four
+// blocks' bytes of rows 32 g + lane (g = 0 .. 3), then of the next four blocks.
+__device__ __forceinline__ void scale_columns(const uint8_t* runs, int lane, int half,
+                                              uint32_t* v) {
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const uint2 b = *(const uint2*)(runs + (32 * g + lane) * kScaleRun + half * 8);
+    v[g] = b.x;
+    v[4 + g] = b.y;
+  }
+}
+
+// The bias of 32 columns from c0 on, all within the width.
+__device__ __forceinline__ void load_bias(const LinearArgs& a, int64_t c0, float (&b)[32]) {
+  if (a.bias_wide) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+      const float4 v = __ldg((const float4*)(a.bias + c0 + e));
+      b[e] = v.x;
+      b[e + 1] = v.y;
+      b[e + 2] = v.z;
+      b[e + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) b[e] = a.bias ? __ldg(a.bias + c0 + e) : 0.f;
+  }
+}
 
 // 32 columns of a row of the output from column c0 on, for rows that do not suit
 // the TMA.
@@ -191,30 +288,15 @@ __device__ __forceinline__ void store_columns(const LinearArgs& a, TOut* row, in
 // 16-byte pieces permuted by the row as the TMA's 128-byte swizzle has them, so that
 // eight lanes' pieces lie in different banks.
 template <typename TOut>
-__device__ __forceinline__ void stage_columns(const LinearArgs& a, uint8_t* buffer, int lane,
-                                              int first, int64_t c0, const uint32_t (&v)[32]) {
+__device__ __forceinline__ void stage_columns(uint8_t* buffer, int lane, int first,
+                                              const uint32_t (&v)[32], const float (&b)[32]) {
   constexpr int kN = 16 / sizeof(TOut);
-  float f[32];
-#pragma unroll
-  for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
-  if (a.bias_wide) {
-#pragma unroll
-    for (int e = 0; e < 32; e += 4) {
-      const float4 b = __ldg((const float4*)(a.bias + c0 + e));
-      f[e] += b.x;
-      f[e + 1] += b.y;
-      f[e + 2] += b.z;
-      f[e + 3] += b.w;
-    }
-  } else if (a.bias) {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) f[e] += __ldg(a.bias + c0 + e);
-  }
 #pragma unroll
   for (int q = 0; q < 32 / kN; ++q) {
     Vec<TOut, kN> y;
 #pragma unroll
-    for (int e = 0; e < kN; ++e) y.v[e] = from_f32<TOut>(f[q * kN + e]);
+    for (int e = 0; e < kN; ++e)
+      y.v[e] = from_f32<TOut>(__uint_as_float(v[q * kN + e]) + b[q * kN + e]);
     *(Vec<TOut, kN>*)(buffer + lane * 128 + (((first / 16 + q) ^ (lane & 7)) << 4)) = y;
   }
 }
@@ -230,13 +312,13 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, int32_t x, int
 
 template <typename TOut>
 __global__ void __launch_bounds__(kThreads, 1)
-linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant__ CUtensorMap x_scales,
-              const __grid_constant__ CUtensorMap w_codes, const __grid_constant__ CUtensorMap w_scales,
+linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant__ CUtensorMap w_codes,
               const __grid_constant__ CUtensorMap out_map, const LinearArgs a) {
   extern __shared__ uint8_t raw[];
   uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
-  uint8_t* out_stage = smem + (size_t)kStages * kStageBytes;
-  uint64_t* bars = (uint64_t*)(out_stage + kOutStage);
+  uint8_t* out_stage = smem + kRingBytes;
+  uint8_t* scale_stage = out_stage + kOutStage;
+  uint64_t* bars = (uint64_t*)(scale_stage + kScaleStage);
   uint32_t* tmem_slot = (uint32_t*)(bars + kBars);
   const Bars bar = {smem_addr(bars)};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -248,7 +330,7 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < kMaxSlots; ++s) {
       mbar_init(bar.full(s), 1);
       mbar_init(bar.scaled(s), 4);
       mbar_init(bar.empty(s), 1);
@@ -256,7 +338,10 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
     for (int d = 0; d < 2; ++d) {
       mbar_init(bar.done(d), 1);
       mbar_init(bar.taken(d), kEpilogueWarps);
+      mbar_init(bar.staged(d), 4);
     }
+    mbar_init(bar.w_full(), 1);
+    mbar_init(bar.w_scaled(), 4);
     mbar_init(bar.drained(), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -264,46 +349,55 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_slot;
-  const int64_t tiles_n = (a.width + kTile - 1) / kTile;
-  const int64_t tiles = (a.rows + kTile - 1) / kTile * tiles_n;
+  Tiles t(a);
   const int stages = (a.blocks + 7) / 8;  // of 256 values, per tile
   const int steps = (a.blocks + 1) / 2;   // products of 64 values, per tile
+  const bool resident = a.resident;
+  const int slots = resident ? kResidentSlots : kSharedSlots;
+  const int slot_bytes = resident ? kCodeBytes : 2 * kCodeBytes;
+  const uint32_t ring_at = smem_addr(smem);
+  const uint32_t w_ring_at = ring_at + kResidentSlots * kCodeBytes;  // the resident stages
   bool ok = true;
 
   if (warp == kProducerWarp) {
     if (lane == 0) {
+      if (resident) {
+        mbar_expect(bar.w_full(), (uint32_t)(stages * kCodeBytes));
+        for (int k = 0; k < stages; ++k)
+          tma_load(w_ring_at + (uint32_t)(k * kCodeBytes), &w_codes, k * kStageBytesK,
+                   (int32_t)(t.n * kTile), bar.w_full());
+      }
       Ring ring;
       int64_t issued = 0;
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-        const int32_t m0 = (int32_t)(t / tiles_n * kTile), n0 = (int32_t)(t % tiles_n * kTile);
+      for (; ok && t.any(); t.next()) {
+        const int32_t m0 = (int32_t)(t.m * kTile), n0 = (int32_t)(t.n * kTile);
         for (int k = 0; k < stages; ++k) {
           const int s = ring.slot;
           if (!ring.first && !mbar_wait(bar.empty(s), ring.parity ^ 1u)) {
             ok = false;
             break;
           }
-          const uint32_t at = smem_addr(smem) + (uint32_t)(s * kStageBytes);
-          mbar_expect(bar.full(s), kStageBytes);
+          const uint32_t at = ring_at + (uint32_t)(s * slot_bytes);
+          mbar_expect(bar.full(s), (uint32_t)slot_bytes);
           tma_load(at, &x_codes, k * kStageBytesK, m0, bar.full(s));
-          tma_load(at + kCodeBytes, &w_codes, k * kStageBytesK, n0, bar.full(s));
-          // two stages' scale bytes: the copy starts on a 16-byte boundary
-          tma_load(at + 2 * kCodeBytes, &x_scales, k / 2 * kScaleRun, m0, bar.full(s));
-          tma_load(at + 2 * kCodeBytes + kScaleBytes, &w_scales, k / 2 * kScaleRun, n0,
-                   bar.full(s));
-          ring.next(kStages);
+          if (!resident)
+            tma_load(at + kCodeBytes, &w_codes, k * kStageBytesK, n0, bar.full(s));
+          ring.next(slots);
           ++issued;
         }
       }
       if (!ok) {  // the copies in flight land before the CTA may leave
+        if (resident) mbar_wait(bar.w_full(), 0);
         Ring r;
-        for (int64_t i = 0; i < issued; ++i, r.next(kStages))
-          if (i + kStages >= issued) mbar_wait(bar.full(r.slot), r.parity);
+        for (int64_t i = 0; i < issued; ++i, r.next(slots))
+          if (i + slots >= issued) mbar_wait(bar.full(r.slot), r.parity);
       }
     }
   } else if (warp == kMmaWarp) {
     if (lane == 0) {
+      if (resident) ok = mbar_wait(bar.w_full(), 0) && mbar_wait(bar.w_scaled(), 0);
       Ring ring, acc;
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      for (; ok && t.any(); t.next()) {
         const int d = acc.slot;
         if (!acc.first && !mbar_wait(bar.taken(d), acc.parity ^ 1u)) {
           ok = false;
@@ -316,17 +410,19 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
             break;
           }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t x_at = smem_addr(smem) + (uint32_t)(s * kStageBytes);
-          const uint32_t w_at = x_at + kCodeBytes;
-          const uint32_t scale = tmem + kScaleCol0 + (uint32_t)(s * kScaleCols);
+          const uint32_t x_at = ring_at + (uint32_t)(s * slot_bytes);
+          const uint32_t w_at =
+              resident ? w_ring_at + (uint32_t)(k * kCodeBytes) : x_at + kCodeBytes;
+          const uint32_t x_scale = tmem + kScaleCol0 + (uint32_t)(s * kScaleCols);
+          const uint32_t w_scale = resident ? tmem + kResidentCol0 + (uint32_t)(k * 8) : x_scale + 8u;
           const int n = min(4, steps - 4 * k);
           for (int i = 0; i < n; ++i)
             mma_mx4(tmem + (uint32_t)(d * kTile), operand_desc(x_at + 32u * (uint32_t)i),
                     operand_desc(w_at + 32u * (uint32_t)i), mx4_idesc(i & 1),
-                    scale + 4u * (uint32_t)(i >> 1), scale + 8u + 4u * (uint32_t)(i >> 1),
+                    x_scale + 4u * (uint32_t)(i >> 1), w_scale + 4u * (uint32_t)(i >> 1),
                     k > 0 || i > 0);
           mma_commit(bar.empty(s));
-          ring.next(kStages);
+          ring.next(slots);
         }
         if (!ok) break;
         mma_commit(bar.done(d));
@@ -338,33 +434,80 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
       }
     }
   } else if (warp >= kScaleWarp0) {
-    // columns of a stage: x's first four blocks, x's next four, w's likewise; four
-    // columns each, column g for rows 32 g .. 32 g + 31
-    const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
+    const int r = tid - 32 * kScaleWarp0;  // this thread's row of the tile
+    const uint32_t quarter = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const int pairs = (stages + 1) / 2;
+    uint32_t v[8];
+    Ring buffer;  // of the two that the runs are passed round in
+    // this thread's runs are there for all four warps; false when the time is up
+    const auto pass_round = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar.staged(buffer.slot));
+      return __all_sync(0xffffffffu, mbar_wait(bar.staged(buffer.slot), buffer.parity)) != 0;
+    };
+    if (resident) {  // one pair at most
+      *(uint4*)(scale_stage + r * kScaleRun) =
+          scale_run(a.w, a.w_stride, t.n * kTile + r, a.width, a.blocks, 0);
+      ok = pass_round();
+      if (ok) {
+        for (int k = 0; k < stages; ++k) {
+          scale_columns(scale_stage, lane, k, v);
+          tmem_store8(quarter + kResidentCol0 + (uint32_t)(k * 8), v);
+        }
+        tmem_store_wait();
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar.w_scaled());
+        buffer.next(2);
+      }
+    }
     Ring ring;
-    for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-      for (int k = 0; k < stages; ++k) {
-        const int s = ring.slot;
-        if (!__all_sync(0xffffffffu, mbar_wait(bar.full(s), ring.parity))) {
+    Tiles ahead = t;  // the loads are a pair ahead
+    int ahead_pair = 0;
+    uint4 x_run = make_uint4(0, 0, 0, 0), w_run = x_run;
+    const auto load = [&] {
+      if (!ahead.any()) return;
+      x_run = scale_run(a.x, a.x_stride, ahead.m * kTile + r, a.rows, a.blocks, ahead_pair);
+      if (!resident)
+        w_run = scale_run(a.w, a.w_stride, ahead.n * kTile + r, a.width, a.blocks, ahead_pair);
+      if (++ahead_pair == pairs) {
+        ahead_pair = 0;
+        ahead.next();
+      }
+    };
+    load();
+    for (; ok && t.any(); t.next()) {
+      for (int p = 0; ok && p < pairs; ++p) {
+        uint8_t* runs = scale_stage + buffer.slot * 2 * kScaleBytes;
+        *(uint4*)(runs + r * kScaleRun) = x_run;
+        if (!resident) *(uint4*)(runs + kScaleBytes + r * kScaleRun) = w_run;
+        load();
+        if (!pass_round()) {
           ok = false;
           break;
         }
-        const uint8_t* at = smem + s * kStageBytes + 2 * kCodeBytes + (k & 1) * 8;
-        uint32_t v[16];
-#pragma unroll
-        for (int o = 0; o < 2; ++o)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const uint2 b =
-                *(const uint2*)(at + o * kScaleBytes + (32 * g + lane) * kScaleRun);
-            v[8 * o + g] = b.x;
-            v[8 * o + 4 + g] = b.y;
+        for (int k = 2 * p; k < min(2 * p + 2, stages); ++k) {
+          const int s = ring.slot;
+          if (!ring.first &&
+              !__all_sync(0xffffffffu, mbar_wait(bar.empty(s), ring.parity ^ 1u))) {
+            ok = false;
+            break;
           }
-        tmem_store16(tmem + quarter + kScaleCol0 + (uint32_t)(s * kScaleCols), v);
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar.scaled(s));
-        ring.next(kStages);
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t to = quarter + kScaleCol0 + (uint32_t)(s * kScaleCols);
+          scale_columns(runs, lane, k & 1, v);
+          tmem_store8(to, v);
+          if (!resident) {
+            scale_columns(runs + kScaleBytes, lane, k & 1, v);
+            tmem_store8(to + 8u, v);
+          }
+          tmem_store_wait();
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar.scaled(s));
+          ring.next(slots);
+        }
+        buffer.next(2);
       }
     }
   } else {
@@ -372,15 +515,15 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
     uint8_t* mine = out_stage + warp * kOutBuffers * kOutBytes;
     int buffer = 0;
     Ring acc;
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    for (; t.any(); t.next()) {
       const int d = acc.slot;
       if (!__all_sync(0xffffffffu, mbar_wait(bar.done(d), acc.parity))) {
         ok = false;
         break;
       }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int64_t row0 = t / tiles_n * kTile + (warp & 3) * 32;
-      const int64_t n0 = t % tiles_n * kTile + (warp >> 2) * kEpilogueCols;
+      const int64_t row0 = t.m * kTile + (warp & 3) * 32;
+      const int64_t n0 = t.n * kTile + (warp >> 2) * kEpilogueCols;
       const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
                             (uint32_t)(d * kTile + (warp >> 2) * kEpilogueCols);
       for (int c = 0; c < kEpilogueCols && n0 + c < a.width; c += kGroup) {
@@ -393,9 +536,11 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
 #pragma unroll
         for (int h = 0; h < kGroup / 32; ++h) {
           uint32_t v[32];
+          float b[32];
+          if (staged) load_bias(a, n0 + c + h * 32, b);  // on its way with the accumulator's
           tmem_load32(from + (uint32_t)(c + h * 32), v);
           if (staged)
-            stage_columns<TOut>(a, mine + buffer * kOutBytes, lane, h * 64, n0 + c + h * 32, v);
+            stage_columns<TOut>(mine + buffer * kOutBytes, lane, h * 64, v, b);
           else if (row0 + lane < a.rows)
             store_columns<TOut>(a, (TOut*)a.out + (row0 + lane) * a.out_stride, n0 + c + h * 32, v);
         }
@@ -441,8 +586,7 @@ size_t few_smem(int64_t rows, int64_t blocks) { return (size_t)(rows * blocks * 
 // kLanes lanes per column of the output.
 template <typename TOut, int kRows>
 __global__ void __launch_bounds__(kFewThreads)
-linear_few_kernel(const uint8_t* __restrict__ x, int64_t x_stride, const uint8_t* __restrict__ w,
-                  int64_t w_stride, int lanes, const LinearArgs a) {
+linear_few_kernel(int lanes, const LinearArgs a) {
   extern __shared__ __align__(16) uint8_t few_raw[];
   uint4* values = (uint4*)few_raw;
   float* scales = (float*)(values + (size_t)kRows * 4 * a.blocks);
@@ -451,8 +595,8 @@ linear_few_kernel(const uint8_t* __restrict__ x, int64_t x_stride, const uint8_t
     uint4 codes = make_uint4(0, 0, 0, 0);
     uint32_t byte = 0;
     if (r < a.rows) {
-      codes = __ldg((const uint4*)(x + r * x_stride) + b);
-      byte = __ldg(x + r * x_stride + (int64_t)a.blocks * 16 + b);
+      codes = __ldg((const uint4*)(a.x + r * a.x_stride) + b);
+      byte = __ldg(a.x + r * a.x_stride + (int64_t)a.blocks * 16 + b);
     }
     const uint32_t word[4] = {codes.x, codes.y, codes.z, codes.w};
 #pragma unroll
@@ -472,7 +616,7 @@ linear_few_kernel(const uint8_t* __restrict__ x, int64_t x_stride, const uint8_t
 #pragma unroll
     for (int r = 0; r < kRows; ++r) sum[r] = 0.f;
     if (j < a.width) {
-      const uint8_t* row = w + j * w_stride;
+      const uint8_t* row = a.w + j * a.w_stride;
       for (int b = lane; b < a.blocks; b += lanes) {
         const uint4 codes = __ldg((const uint4*)row + b);
         const float scale = mx4_scale(__ldg(row + (int64_t)a.blocks * 16 + b));
@@ -560,28 +704,21 @@ template <>
 constexpr CUtensorMapDataType kMapType<__nv_bfloat16> = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 
 template <typename TOut>
-cudaError_t launch_linear(const void* x, int64_t x_stride, const void* w, int64_t w_stride,
-                          LinearArgs a, int device, cudaStream_t st) {
+cudaError_t launch_linear(LinearArgs a, int device, cudaStream_t st) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return cudaErrorNotSupported;
   const int64_t codes = (int64_t)a.blocks * 16;
-  const uint8_t *xb = (const uint8_t*)x, *wb = (const uint8_t*)w;
-  CUtensorMap xc, xs, wc, ws, out = {};
-  const auto bytes = [&](CUtensorMap* map, const void* p, int64_t cols, int64_t rows,
-                         int64_t stride, int box, CUtensorMapSwizzle swizzle) {
-    return map_rows(encode, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, p, cols, rows, stride, box, kTile,
-                    swizzle);
+  CUtensorMap x_map, w_map, out_map = {};
+  const auto codes_map = [&](CUtensorMap* map, const uint8_t* p, int64_t rows, int64_t stride) {
+    return map_rows(encode, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, p, codes, rows, stride,
+                    kStageBytesK, kTile, CU_TENSOR_MAP_SWIZZLE_128B);
   };
-  if (!bytes(&xc, xb, codes, a.rows, x_stride, kStageBytesK, CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !bytes(&xs, xb + codes, a.blocks, a.rows, x_stride, kScaleRun,
-             CU_TENSOR_MAP_SWIZZLE_NONE) ||
-      !bytes(&wc, wb, codes, a.width, w_stride, kStageBytesK, CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !bytes(&ws, wb + codes, a.blocks, a.width, w_stride, kScaleRun, CU_TENSOR_MAP_SWIZZLE_NONE))
+  if (!codes_map(&x_map, a.x, a.rows, a.x_stride) || !codes_map(&w_map, a.w, a.width, a.w_stride))
     return cudaErrorInvalidValue;
   const int64_t out_bytes = a.out_stride * (int64_t)sizeof(TOut);
   a.tma_out = aligned_rows(a.out, out_bytes, 16) && out_bytes < (1ll << 40);
   if (a.tma_out &&
-      !map_rows(encode, &out, kMapType<TOut>, a.out, a.width, a.rows, out_bytes,
+      !map_rows(encode, &out_map, kMapType<TOut>, a.out, a.width, a.rows, out_bytes,
                 (int)(128 / sizeof(TOut)), 32, CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
   static OncePerDevice once;
@@ -590,16 +727,18 @@ cudaError_t launch_linear(const void* x, int64_t x_stride, const void* w, int64_
                                 (int)kSmemBytes);
   });
   if (e != cudaSuccess) return e;
-  const int64_t tiles = ceil_div(a.rows, kTile) * ceil_div(a.width, kTile);
   const int num_sms = op_num_sms(device);
-  linear_kernel<TOut><<<(unsigned)(tiles < num_sms ? tiles : num_sms), kThreads, kSmemBytes, st>>>(
-      xc, xs, wc, ws, out, a);
+  const int64_t tiles_m = ceil_div(a.rows, kTile), tiles_n = ceil_div(a.width, kTile);
+  a.resident = ceil_div(a.blocks, 8) <= kResidentStages && tiles_n <= num_sms;
+  int64_t grid = num_sms;
+  if (a.resident) grid = num_sms / tiles_n * tiles_n;  // a CTA's columns stay the same
+  if (tiles_m <= grid / tiles_n) grid = tiles_m * tiles_n;
+  linear_kernel<TOut><<<(unsigned)grid, kThreads, kSmemBytes, st>>>(x_map, w_map, out_map, a);
   return cudaGetLastError();
 }
 
 template <typename TOut, int kRows>
-cudaError_t launch_few(const void* x, int64_t x_stride, const void* w, int64_t w_stride,
-                       const LinearArgs& a, int device, cudaStream_t st) {
+cudaError_t launch_few(const LinearArgs& a, int device, cudaStream_t st) {
   int lanes = 1;
   while (lanes < 32 && lanes < a.blocks) lanes *= 2;
   const int64_t ctas = ceil_div(a.width, kFewThreads / lanes);
@@ -613,7 +752,7 @@ cudaError_t launch_few(const void* x, int64_t x_stride, const void* w, int64_t w
   if (e != cudaSuccess) return e;
   linear_few_kernel<TOut, kRows>
       <<<(unsigned)(ctas < 8 * num_sms ? ctas : 8 * num_sms), kFewThreads, smem, st>>>(
-          (const uint8_t*)x, x_stride, (const uint8_t*)w, w_stride, lanes, a);
+          lanes, a);
   return cudaGetLastError();
 }
 
@@ -669,20 +808,22 @@ extern "C" agnes_status agnes_mx4_linear(const void* x, int64_t x_stride, int64_
   a.out_stride = out_stride;
   a.status = status;
   // a single row has no next one: any stride will do
-  if (rows == 1) x_stride = mx4_row_bytes(dim);
-  if (width == 1) w_stride = mx4_row_bytes(dim);
+  a.x = (const uint8_t*)x;
+  a.w = (const uint8_t*)w;
+  a.x_stride = rows > 1 ? x_stride : mx4_row_bytes(dim);
+  a.w_stride = width > 1 ? w_stride : mx4_row_bytes(dim);
   if (rows == 1) a.out_stride = width;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const cudaError_t e = with_float_type(out_dtype, [&](auto t) {
     using TOut = typename decltype(t)::type;
     if (rows <= kFewRows && few_smem(rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8,
                                      a.blocks) <= kFewSmem) {
-      if (rows == 1) return launch_few<TOut, 1>(x, x_stride, w, w_stride, a, device, st);
-      if (rows == 2) return launch_few<TOut, 2>(x, x_stride, w, w_stride, a, device, st);
-      if (rows <= 4) return launch_few<TOut, 4>(x, x_stride, w, w_stride, a, device, st);
-      return launch_few<TOut, 8>(x, x_stride, w, w_stride, a, device, st);
+      if (rows == 1) return launch_few<TOut, 1>(a, device, st);
+      if (rows == 2) return launch_few<TOut, 2>(a, device, st);
+      if (rows <= 4) return launch_few<TOut, 4>(a, device, st);
+      return launch_few<TOut, 8>(a, device, st);
     }
-    return launch_linear<TOut>(x, x_stride, w, w_stride, a, device, st);
+    return launch_linear<TOut>(a, device, st);
   });
   return op_launched(op, e);
 }

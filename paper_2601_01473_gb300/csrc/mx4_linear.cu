@@ -49,6 +49,7 @@ static_assert(kSharedSlots * 2 == 8 && kResidentSlots + kResidentStages == 8, "t
 constexpr int kScaleRun = 16;  // of a row, for two stages
 constexpr int kScaleBytes = kTile * kScaleRun;
 constexpr int kScaleStage = 4 * kScaleBytes;
+constexpr int kRunsAhead = 4;
 // Tensor memory: two accumulators, each slot's scales (x's eight columns, w's
 // eight), the resident w's.
 constexpr int kScaleCols = 16;
@@ -143,11 +144,14 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
       : "memory");
 }
 
+// The wait is part of the same statement: apart, arithmetic on the values may be
+// moved before it.
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, "
       "%10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
-      "%26, %27, %28, %29, %30, %31}, [%32];"
+      "%26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
         "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
         "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
@@ -155,7 +159,6 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
         "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
       : "r"(addr)
       : "memory");
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
 __device__ __forceinline__ void tmem_store8(uint32_t addr, const uint32_t* v) {
@@ -462,26 +465,36 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
       }
     }
     Ring ring;
-    Tiles ahead = t;  // the loads are a pair ahead
+    // the runs are loaded kRunsAhead pairs ahead: one pair is less than a trip to memory
+    Tiles ahead = t;
     int ahead_pair = 0;
-    uint4 x_run = make_uint4(0, 0, 0, 0), w_run = x_run;
-    const auto load = [&] {
+    uint4 x_run[kRunsAhead], w_run[kRunsAhead];
+    const auto load = [&](uint4& x, uint4& w) {
       if (!ahead.any()) return;
-      x_run = scale_run(a.x, a.x_stride, ahead.m * kTile + r, a.rows, a.blocks, ahead_pair);
+      x = scale_run(a.x, a.x_stride, ahead.m * kTile + r, a.rows, a.blocks, ahead_pair);
       if (!resident)
-        w_run = scale_run(a.w, a.w_stride, ahead.n * kTile + r, a.width, a.blocks, ahead_pair);
+        w = scale_run(a.w, a.w_stride, ahead.n * kTile + r, a.width, a.blocks, ahead_pair);
       if (++ahead_pair == pairs) {
         ahead_pair = 0;
         ahead.next();
       }
     };
-    load();
+#pragma unroll
+    for (int q = 0; q < kRunsAhead; ++q) {
+      x_run[q] = w_run[q] = make_uint4(0, 0, 0, 0);
+      load(x_run[q], w_run[q]);
+    }
     for (; ok && t.any(); t.next()) {
       for (int p = 0; ok && p < pairs; ++p) {
         uint8_t* runs = scale_stage + buffer.slot * 2 * kScaleBytes;
-        *(uint4*)(runs + r * kScaleRun) = x_run;
-        if (!resident) *(uint4*)(runs + kScaleBytes + r * kScaleRun) = w_run;
-        load();
+        *(uint4*)(runs + r * kScaleRun) = x_run[0];
+        if (!resident) *(uint4*)(runs + kScaleBytes + r * kScaleRun) = w_run[0];
+#pragma unroll
+        for (int q = 1; q < kRunsAhead; ++q) {
+          x_run[q - 1] = x_run[q];
+          w_run[q - 1] = w_run[q];
+        }
+        load(x_run[kRunsAhead - 1], w_run[kRunsAhead - 1]);
         if (!pass_round()) {
           ok = false;
           break;
@@ -526,7 +539,10 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
       const int64_t n0 = t.n * kTile + (warp >> 2) * kEpilogueCols;
       const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
                             (uint32_t)(d * kTile + (warp >> 2) * kEpilogueCols);
-      for (int c = 0; c < kEpilogueCols && n0 + c < a.width; c += kGroup) {
+      // a warp whose rows are all past the end has nothing to store, and its buffers
+      // may still be on their way
+      const int cols = row0 < a.rows ? kEpilogueCols : 0;
+      for (int c = 0; c < cols && n0 + c < a.width; c += kGroup) {
         // whole groups only: at a ragged end the TMA writes up to a 16-byte boundary
         const bool staged = a.tma_out && n0 + c + kGroup <= a.width;
         if (staged) {  // the store before the last has read the buffer
@@ -547,7 +563,7 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
         if (staged) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0 && row0 < a.rows)  // rows past the end are left out
+          if (lane == 0)  // rows past the end are left out
             tma_store(&out_map, (int32_t)(n0 + c), (int32_t)row0,
                       smem_addr(mine + buffer * kOutBytes));
           buffer ^= 1;

@@ -276,3 +276,23 @@ def test_a_graph_gathers_4bit_rows_unchanged(cuda_device):
         assert torch.equal(mb.feats.view(torch.uint8), packed[mb.nodes.long()])
         assert torch.equal(ops.mx4_linear(mb.feats, w, dim), whole[mb.nodes.long()])
     ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", FLOATS)
+def test_product_of_a_ragged_last_tile_each_time(cuda_device, out):
+    """The CTA that ends with a tile of fewer rows stores the whole of the one before:
+    the warps without rows in the last tile leave their buffers alone."""
+    rows, width, dim = 40_000, 256, 128
+    x = ops.mx4_quantize(_values(rows, dim, 1).to(cuda_device))
+    w = ops.mx4_quantize(_values(width, dim, 2).to(cuda_device))
+    b = torch.ones(width, device=cuda_device)
+    got = torch.empty(rows, width, dtype=out, device=cuda_device)
+    ops.mx4_linear(x, w, dim, b, out=got)
+    first = got.clone()
+    differ = torch.zeros((), dtype=torch.int64, device=cuda_device)
+    for _ in range(2000):
+        got.zero_()
+        ops.mx4_linear(x, w, dim, b, out=got)
+        differ += (got != first).sum()
+    assert int(differ) == 0

@@ -6,11 +6,10 @@
 // memory.  Persistent CTAs, one per SM, over output tiles of 128 x 128:
 //   the producer      has the TMA copy a stage: 256 codes of 128 rows of x and of w;
 //   the scale warps   load the rows' scale bytes, a thread to a row and 512 values
-//                     at a time, pass them round through shared memory, and put
-//                     them into tensor memory: lane l of each quarter, column g,
-//                     holds those of row 32 g + l for four blocks;
-//   the MMA warp      issues the stage's products (K = 64 each) into one of two
-//                     accumulators;
+//                     at a time, and lay them out in shared memory as tensor memory
+//                     takes them: four blocks' bytes of row 32 g + l in lane l, column g;
+//   the MMA warp      has the scales copied to tensor memory (tcgen05.cp) and issues
+//                     the stage's products (K = 64 each) into one of two accumulators;
 //   the epilogue warps read the accumulator, add the bias, round, and have the TMA
 //                     store it from shared memory.
 // Rows of up to 512 values: a CTA keeps to one tile of columns and its weights stay in
@@ -45,11 +44,13 @@ constexpr int kResidentSlots = 6;
 constexpr int kMaxSlots = kResidentSlots;
 constexpr int kRingBytes = 8 * kCodeBytes;
 static_assert(kSharedSlots * 2 == 8 && kResidentSlots + kResidentStages == 8, "the ring");
-// Scale bytes on their way: 16 of each row of x and w, twice.
-constexpr int kScaleRun = 16;  // of a row, for two stages
-constexpr int kScaleBytes = kTile * kScaleRun;
-constexpr int kScaleStage = 4 * kScaleBytes;
-constexpr int kRunsAhead = 4;
+// Scale bytes: a thread loads 16 of its row, for two stages; a stage of 128 rows is
+// two words a row, in two blocks of 512 bytes.
+constexpr int kScaleRun = 16;
+constexpr int kScaleBlock = kTile * 4;
+constexpr int kScaleBytes = 2 * kScaleBlock;
+constexpr int kScaleStage = (2 * kMaxSlots + kResidentStages) * kScaleBytes;
+constexpr int kRunsAhead = 4;  // runs on their way to a thread, further than a trip to memory
 // Tensor memory: two accumulators, each slot's scales (x's eight columns, w's
 // eight), the resident w's.
 constexpr int kScaleCols = 16;
@@ -71,7 +72,7 @@ static_assert(kEpilogueCols % 64 == 0, "whole groups of the widest output");
 constexpr int kOutBytes = 32 * 128;
 constexpr int kOutBuffers = 2;
 constexpr int kOutStage = kEpilogueWarps * kOutBuffers * kOutBytes;
-constexpr int kBars = 3 * kMaxSlots + 9;
+constexpr int kBars = 3 * kMaxSlots + 7;
 constexpr size_t kSmemBytes =
     (size_t)kRingBytes + kOutStage + kScaleStage + 1024 + 8 * kBars + 16;
 static_assert(kCodeBytes % 1024 == 0 && kOutBytes % 1024 == 0,
@@ -161,21 +162,18 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
       : "memory");
 }
 
-__device__ __forceinline__ void tmem_store8(uint32_t addr, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-      : "memory");
+// A block of 512 bytes from shared memory to four columns of all four quarters of
+// tensor memory: lane l takes 16 bytes.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t to, uint32_t from) {
+  // no swizzle; groups of eight lanes' 16 bytes are 128 bytes apart (bits 32-45)
+  const uint64_t desc =
+      (uint64_t)((from & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
 }
 
-__device__ __forceinline__ void tmem_store_wait() {
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-}
-
-// The mbarriers: full[s] (the TMA has brought slot s), scaled[s] (its scales are in
-// tensor memory), empty[s] (its products are done); done[d] / taken[d] of the
-// accumulators; staged[b] (the scale warps have filled buffer b); w_full / w_scaled of
-// the resident weights; drained, when the MMA warp gives up.
+// The mbarriers: full[s] (the TMA has brought slot s), scaled[s] (its scales are laid
+// out), empty[s] (its products are done); done[d] / taken[d] of the accumulators;
+// w_full / w_scaled of the resident weights; drained, when the MMA warp gives up.
 struct Bars {
   uint32_t base;
   __device__ uint32_t at(int i) const { return base + 8u * (uint32_t)i; }
@@ -184,10 +182,9 @@ struct Bars {
   __device__ uint32_t empty(int s) const { return at(2 * kMaxSlots + s); }
   __device__ uint32_t done(int d) const { return at(3 * kMaxSlots + d); }
   __device__ uint32_t taken(int d) const { return at(3 * kMaxSlots + 2 + d); }
-  __device__ uint32_t staged(int b) const { return at(3 * kMaxSlots + 4 + b); }
-  __device__ uint32_t w_full() const { return at(3 * kMaxSlots + 6); }
-  __device__ uint32_t w_scaled() const { return at(3 * kMaxSlots + 7); }
-  __device__ uint32_t drained() const { return at(3 * kMaxSlots + 8); }
+  __device__ uint32_t w_full() const { return at(3 * kMaxSlots + 4); }
+  __device__ uint32_t w_scaled() const { return at(3 * kMaxSlots + 5); }
+  __device__ uint32_t drained() const { return at(3 * kMaxSlots + 6); }
 };
 
 struct Ring {
@@ -245,16 +242,12 @@ __device__ __forceinline__ uint4 scale_run(const uint8_t* p, int64_t stride, int
   return v;
 }
 
-// A stage's scales of 128 rows, from their runs, as the eight columns of a lane: four
-// blocks' bytes of rows 32 g + lane (g = 0 .. 3), then of the next four blocks.
-__device__ __forceinline__ void scale_columns(const uint8_t* runs, int lane, int half,
-                                              uint32_t* v) {
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const uint2 b = *(const uint2*)(runs + (32 * g + lane) * kScaleRun + half * 8);
-    v[g] = b.x;
-    v[4 + g] = b.y;
-  }
+// A row's two words of a stage to their blocks.
+__device__ __forceinline__ void put_scales(uint8_t* blocks, int r, uint32_t first,
+                                           uint32_t second) {
+  uint8_t* to = blocks + (r & 31) * 16 + (r >> 5) * 4;
+  *(uint32_t*)to = first;
+  *(uint32_t*)(to + kScaleBlock) = second;
 }
 
 // The bias of 32 columns from c0 on, all within the width.
@@ -341,7 +334,6 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
     for (int d = 0; d < 2; ++d) {
       mbar_init(bar.done(d), 1);
       mbar_init(bar.taken(d), kEpilogueWarps);
-      mbar_init(bar.staged(d), 4);
     }
     mbar_init(bar.w_full(), 1);
     mbar_init(bar.w_scaled(), 4);
@@ -360,6 +352,7 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
   const int slot_bytes = resident ? kCodeBytes : 2 * kCodeBytes;
   const uint32_t ring_at = smem_addr(smem);
   const uint32_t w_ring_at = ring_at + kResidentSlots * kCodeBytes;  // the resident stages
+  uint8_t* w_scale_stage = scale_stage + 2 * kMaxSlots * kScaleBytes;
   bool ok = true;
 
   if (warp == kProducerWarp) {
@@ -398,7 +391,13 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
     }
   } else if (warp == kMmaWarp) {
     if (lane == 0) {
-      if (resident) ok = mbar_wait(bar.w_full(), 0) && mbar_wait(bar.w_scaled(), 0);
+      if (resident) {
+        ok = mbar_wait(bar.w_full(), 0) && mbar_wait(bar.w_scaled(), 0);
+        if (ok)
+          for (int c = 0; c < 2 * stages; ++c)
+            tmem_copy_scales(tmem + kResidentCol0 + (uint32_t)(c * 4),
+                             smem_addr(w_scale_stage + c * kScaleBlock));
+      }
       Ring ring, acc;
       for (; ok && t.any(); t.next()) {
         const int d = acc.slot;
@@ -419,6 +418,13 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
           const uint32_t x_scale = tmem + kScaleCol0 + (uint32_t)(s * kScaleCols);
           const uint32_t w_scale = resident ? tmem + kResidentCol0 + (uint32_t)(k * 8) : x_scale + 8u;
           const int n = min(4, steps - 4 * k);
+          const uint32_t scales = smem_addr(scale_stage + s * 2 * kScaleBytes);
+          for (int c = 0; c < (n + 1) / 2; ++c) {
+            tmem_copy_scales(x_scale + 4u * (uint32_t)c, scales + (uint32_t)(c * kScaleBlock));
+            if (!resident)
+              tmem_copy_scales(w_scale + 4u * (uint32_t)c,
+                               scales + (uint32_t)(kScaleBytes + c * kScaleBlock));
+          }
           for (int i = 0; i < n; ++i)
             mma_mx4(tmem + (uint32_t)(d * kTile), operand_desc(x_at + 32u * (uint32_t)i),
                     operand_desc(w_at + 32u * (uint32_t)i), mx4_idesc(i & 1),
@@ -438,37 +444,21 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
     }
   } else if (warp >= kScaleWarp0) {
     const int r = tid - 32 * kScaleWarp0;  // this thread's row of the tile
-    const uint32_t quarter = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const int pairs = (stages + 1) / 2;
-    uint32_t v[8];
-    Ring buffer;  // of the two that the runs are passed round in
-    // this thread's runs are there for all four warps; false when the time is up
-    const auto pass_round = [&] {
+    // what the tensor core reads has been written, for the thread that waits for `b`
+    const auto tell = [&](uint32_t b) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar.staged(buffer.slot));
-      return __all_sync(0xffffffffu, mbar_wait(bar.staged(buffer.slot), buffer.parity)) != 0;
+      if (lane == 0) mbar_arrive(b);
     };
     if (resident) {  // one pair at most
-      *(uint4*)(scale_stage + r * kScaleRun) =
-          scale_run(a.w, a.w_stride, t.n * kTile + r, a.width, a.blocks, 0);
-      ok = pass_round();
-      if (ok) {
-        for (int k = 0; k < stages; ++k) {
-          scale_columns(scale_stage, lane, k, v);
-          tmem_store8(quarter + kResidentCol0 + (uint32_t)(k * 8), v);
-        }
-        tmem_store_wait();
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar.w_scaled());
-        buffer.next(2);
-      }
+      const uint4 v = scale_run(a.w, a.w_stride, t.n * kTile + r, a.width, a.blocks, 0);
+      put_scales(w_scale_stage, r, v.x, v.y);
+      put_scales(w_scale_stage + kScaleBytes, r, v.z, v.w);
+      tell(bar.w_scaled());
     }
-    Ring ring;
-    // the runs are loaded kRunsAhead pairs ahead: one pair is less than a trip to memory
     Tiles ahead = t;
     int ahead_pair = 0;
-    uint4 x_run[kRunsAhead], w_run[kRunsAhead];
     const auto load = [&](uint4& x, uint4& w) {
       if (!ahead.any()) return;
       x = scale_run(a.x, a.x_stride, ahead.m * kTile + r, a.rows, a.blocks, ahead_pair);
@@ -479,48 +469,40 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
         ahead.next();
       }
     };
+    uint4 x_run[kRunsAhead], w_run[kRunsAhead];
 #pragma unroll
     for (int q = 0; q < kRunsAhead; ++q) {
       x_run[q] = w_run[q] = make_uint4(0, 0, 0, 0);
       load(x_run[q], w_run[q]);
     }
-    for (; ok && t.any(); t.next()) {
-      for (int p = 0; ok && p < pairs; ++p) {
-        uint8_t* runs = scale_stage + buffer.slot * 2 * kScaleBytes;
-        *(uint4*)(runs + r * kScaleRun) = x_run[0];
-        if (!resident) *(uint4*)(runs + kScaleBytes + r * kScaleRun) = w_run[0];
+    Ring ring;
+    int p = 0;
+    while (ok && t.any()) {
+      // unrolled, so that a run stays in its registers until it is used
 #pragma unroll
-        for (int q = 1; q < kRunsAhead; ++q) {
-          x_run[q - 1] = x_run[q];
-          w_run[q - 1] = w_run[q];
-        }
-        load(x_run[kRunsAhead - 1], w_run[kRunsAhead - 1]);
-        if (!pass_round()) {
-          ok = false;
-          break;
-        }
-        for (int k = 2 * p; k < min(2 * p + 2, stages); ++k) {
+      for (int q = 0; q < kRunsAhead; ++q) {
+        if (!ok || !t.any()) break;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (2 * p + h >= stages) break;
           const int s = ring.slot;
           if (!ring.first &&
               !__all_sync(0xffffffffu, mbar_wait(bar.empty(s), ring.parity ^ 1u))) {
             ok = false;
             break;
           }
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t to = quarter + kScaleCol0 + (uint32_t)(s * kScaleCols);
-          scale_columns(runs, lane, k & 1, v);
-          tmem_store8(to, v);
-          if (!resident) {
-            scale_columns(runs + kScaleBytes, lane, k & 1, v);
-            tmem_store8(to + 8u, v);
-          }
-          tmem_store_wait();
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar.scaled(s));
+          uint8_t* to = scale_stage + s * 2 * kScaleBytes;
+          const uint4 &x = x_run[q], &w = w_run[q];
+          put_scales(to, r, h ? x.z : x.x, h ? x.w : x.y);
+          if (!resident) put_scales(to + kScaleBytes, r, h ? w.z : w.x, h ? w.w : w.y);
+          tell(bar.scaled(s));
           ring.next(slots);
         }
-        buffer.next(2);
+        load(x_run[q], w_run[q]);
+        if (++p == pairs) {
+          p = 0;
+          t.next();
+        }
       }
     }
   } else {

@@ -13,10 +13,14 @@
 //   the epilogue warps read the accumulator, add the bias, round, and have the TMA
 //                     store it from shared memory.
 // Rows of up to 512 values: a CTA keeps to one tile of columns and its weights stay in
-// shared and tensor memory, so a tile costs the copy of x's rows alone.  (The TMA
-// takes about 5 cycles a row, however short: with w's rows copied for each tile, and
-// the scale bytes by it too, those requests took all the time, 786,432 rows of 128 to
-// 256 columns 116 us.)
+// shared and tensor memory, so a tile costs the copy of x's rows alone.
+//
+// Short rows are bound by the output's stores: 786,432 rows of 128 to 256 columns in
+// fp16 take 92 us, a memset of the same 402 MB 102 us.  Long rows are bound by the
+// operands' way from L2 (64 values of x or w meet 128 of the other): 6,000 x 1024 to
+// 4096 columns 35 us, 1430 TFLOP/s.  Tried without gain: two tiles of columns to each
+// stage of x with three accumulators taken in turn by the two sets of epilogue warps
+// (93 us; long rows 15% slower), three sets (97 us).
 // Every wait is bounded (mbarrier.cuh).  Rows and columns past the matrices' ends
 // come as zeros from the TMA.
 //
@@ -250,9 +254,10 @@ __device__ __forceinline__ void put_scales(uint8_t* blocks, int r, uint32_t firs
   *(uint32_t*)(to + kScaleBlock) = second;
 }
 
-// The bias of 32 columns from c0 on, all within the width.
+// The bias of 32 columns from c0 on; of those past the width, zeros.
 __device__ __forceinline__ void load_bias(const LinearArgs& a, int64_t c0, float (&b)[32]) {
-  if (a.bias_wide) {
+  const bool full = c0 + 32 <= a.width;
+  if (a.bias_wide && full) {
 #pragma unroll
     for (int e = 0; e < 32; e += 4) {
       const float4 v = __ldg((const float4*)(a.bias + c0 + e));
@@ -261,22 +266,13 @@ __device__ __forceinline__ void load_bias(const LinearArgs& a, int64_t c0, float
       b[e + 2] = v.z;
       b[e + 3] = v.w;
     }
+  } else if (!a.bias) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) b[e] = 0.f;
   } else {
+    const int left = full ? 32 : (int)(a.width - c0);
 #pragma unroll
-    for (int e = 0; e < 32; ++e) b[e] = a.bias ? __ldg(a.bias + c0 + e) : 0.f;
-  }
-}
-
-// 32 columns of a row of the output from column c0 on, for rows that do not suit
-// the TMA.
-template <typename TOut>
-__device__ __forceinline__ void store_columns(const LinearArgs& a, TOut* row, int64_t c0,
-                                              const uint32_t (&v)[32]) {
-#pragma unroll
-  for (int e = 0; e < 32; ++e) {
-    if (c0 + e >= a.width) break;
-    const float b = a.bias ? __ldg(a.bias + c0 + e) : 0.f;
-    row[c0 + e] = from_f32<TOut>(__uint_as_float(v[e]) + b);
+    for (int e = 0; e < 32; ++e) b[e] = e < left ? __ldg(a.bias + c0 + e) : 0.f;
   }
 }
 
@@ -297,13 +293,31 @@ __device__ __forceinline__ void stage_columns(uint8_t* buffer, int lane, int fir
   }
 }
 
+// A warp's buffer to `rows` rows of the output from `to` on, `cols` columns each: for rows
+// that do not suit the TMA and for ragged ends.  A row at a time, its elements side by
+// side.
+template <typename TOut>
+__device__ __forceinline__ void store_rows(const uint8_t* buffer, int lane, TOut* to,
+                                           int64_t stride, int rows, int cols) {
+  constexpr int kGroup = 128 / sizeof(TOut);
+#pragma unroll 4
+  for (int r = 0; r < rows; ++r) {
+#pragma unroll
+    for (int e = 0; e < kGroup; e += 32) {
+      const int byte = (e + lane) * (int)sizeof(TOut);
+      if (e + lane < cols)
+        to[r * stride + e + lane] = *(const TOut*)(buffer + r * 128 +
+                                                   (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
+    }
+  }
+}
+
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, int32_t x, int32_t y,
                                           uint32_t src) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
                    map),
                "r"(x), "r"(y), "r"(src)
                : "memory");
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
 template <typename TOut>
@@ -525,31 +539,35 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
       // may still be on their way
       const int cols = row0 < a.rows ? kEpilogueCols : 0;
       for (int c = 0; c < cols && n0 + c < a.width; c += kGroup) {
-        // whole groups only: at a ragged end the TMA writes up to a 16-byte boundary
-        const bool staged = a.tma_out && n0 + c + kGroup <= a.width;
-        if (staged) {  // the store before the last has read the buffer
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          __syncwarp();
-        }
+        // the store before the last has read the buffer
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
 #pragma unroll
         for (int h = 0; h < kGroup / 32; ++h) {
           uint32_t v[32];
           float b[32];
-          if (staged) load_bias(a, n0 + c + h * 32, b);  // on its way with the accumulator's
+          load_bias(a, n0 + c + h * 32, b);  // on its way with the accumulator's
           tmem_load32(from + (uint32_t)(c + h * 32), v);
-          if (staged)
-            stage_columns<TOut>(mine + buffer * kOutBytes, lane, h * 64, v, b);
-          else if (row0 + lane < a.rows)
-            store_columns<TOut>(a, (TOut*)a.out + (row0 + lane) * a.out_stride, n0 + c + h * 32, v);
+          stage_columns<TOut>(mine + buffer * kOutBytes, lane, h * 64, v, b);
         }
-        if (staged) {
+        // whole groups only: at a ragged end the TMA writes up to a 16-byte boundary
+        if (a.tma_out && n0 + c + kGroup <= a.width) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0)  // rows past the end are left out
             tma_store(&out_map, (int32_t)(n0 + c), (int32_t)row0,
                       smem_addr(mine + buffer * kOutBytes));
-          buffer ^= 1;
+        } else {
+          __syncwarp();
+          const int64_t rows = a.rows - row0, left = a.width - n0 - c;
+          store_rows<TOut>(mine + buffer * kOutBytes, lane,
+                           (TOut*)a.out + row0 * a.out_stride + n0 + c, a.out_stride,
+                           rows < 32 ? (int)rows : 32, left < kGroup ? (int)left : kGroup);
+          __syncwarp();
         }
+        // a group for each use of a buffer, an empty one too, so that the wait's count holds
+        if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        buffer ^= 1;
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();

@@ -22,7 +22,8 @@ namespace agnes {
 namespace {
 
 constexpr int kMaxTop = AGNES_DISTILL_MAX_TOP;
-constexpr int kMaxThreads = 512;
+constexpr int kMaxReaders = 512;
+constexpr int kMaxThreads = kMaxReaders + 32;
 constexpr int kMaxCluster = 8;
 constexpr float kNegInf = -__builtin_huge_valf();
 
@@ -83,39 +84,114 @@ __device__ __forceinline__ MaxSum warp_join(MaxSum x, float c) {
   return x;
 }
 
+// Pairs of floats, for the packed instructions (each half rounded as by a single one).
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t p) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+  return f;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Two elements of a vector as a pair of floats.
+__device__ __forceinline__ uint64_t pair_of(const float* v) { return pack2(v[0], v[1]); }
+__device__ __forceinline__ uint64_t pair_of(const __half* v) {
+  const float2 f = __half22float2(*(const __half2*)v);
+  return pack2(f.x, f.y);
+}
+__device__ __forceinline__ uint64_t pair_of(const __nv_bfloat16* v) {
+  const float2 f = __bfloat1622float2(*(const __nv_bfloat162*)v);
+  return pack2(f.x, f.y);
+}
+__device__ __forceinline__ void put_pair(float* to, float2 f) {
+  to[0] = f.x;
+  to[1] = f.y;
+}
+__device__ __forceinline__ void put_pair(__half* to, float2 f) {
+  *(__half2*)to = __float22half2_rn(f);
+}
+__device__ __forceinline__ void put_pair(__nv_bfloat16* to, float2 f) {
+  *(__nv_bfloat162*)to = __float22bfloat162_rn(f);
+}
+
+// The largest of a vector's elements; a NaN is not looked at.
+__device__ __forceinline__ float largest(const Vec<float, 4>& x) {
+  return fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3]));
+}
+__device__ __forceinline__ float largest(const Vec<__half, 8>& x) {
+  const __half2* h = (const __half2*)x.v;
+  const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ float largest(const Vec<__nv_bfloat16, 8>& x) {
+  const __nv_bfloat162* h = (const __nv_bfloat162*)x.v;
+  const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
   return x;
 }
 
-template <typename T, int kN>
-__device__ __forceinline__ void take(MaxSum& r, const Vec<T, kN>& x, float c) {
-  float f[kN], m = r.m;
-#pragma unroll
-  for (int e = 0; e < kN; ++e) {
-    f[e] = to_f32(x.v[e]);
-    m = fmaxf(m, f[e]);
+// A thread's running maximum, and the sum as a pair.
+struct Running {
+  float m;
+  uint64_t s;
+
+  __device__ void raise(float top, float c) {  // a larger maximum
+    if (top > m) {
+      const float scale = exp2_fast((m - top) * c);
+      s = mul2(s, pack2(scale, scale));
+      m = top;
+    }
   }
-  const float z = above(m);
-  float s = 0.f;
+  template <typename T, int kN>
+  __device__ void take(const Vec<T, kN>& x, float c) {
+    raise(largest(x), c);
+    const float z = -above(m);
+    const uint64_t z2 = pack2(z, z), c2 = pack2(c, c);
 #pragma unroll
-  for (int e = 0; e < kN; ++e) s += exp2_fast((f[e] - z) * c);
-  r.s = r.s * exp2_fast((r.m - z) * c) + s;
-  r.m = m;
-}
+    for (int e = 0; e < kN; e += 2) {
+      const float2 f = unpack2(mul2(add2(pair_of(x.v + e), z2), c2));
+      s = add2(s, pack2(exp2_fast(f.x), exp2_fast(f.y)));
+    }
+  }
+  __device__ void take_one(float f, float c) {
+    raise(f, c);
+    s = add2(s, pack2(exp2_fast((f - above(m)) * c), 0.f));
+  }
+  __device__ MaxSum sum() const {
+    const float2 f = unpack2(s);
+    return {m, f.x + f.y};
+  }
+};
 
 struct alignas(16) DistillSmem {  // the kept slice follows it, in 16-byte vectors
   float p[kMaxTop];
   int32_t index[kMaxTop];  // -1: absent
   float x[kMaxTop];        // the student's logit at index (rank 0)
-  MaxSum part[kMaxThreads / 32];
+  MaxSum part[32];         // the readers' warps'
   MaxSum joined;           // this CTA's
   float mass;              // sum of p: 1, or 0 without a teacher entry
 };
 static_assert(sizeof(DistillSmem) % 16 == 0, "what follows is 16-byte aligned");
 
-// Warp 0: the teacher's distribution of the row.
+// A warp: the teacher's distribution of the row.
 __device__ __forceinline__ void teacher_row(const DistillArgs& a, int64_t row, float c,
                                             DistillSmem& s) {
   const int lane = lane_id();
@@ -149,7 +225,7 @@ __device__ __forceinline__ void teacher_row(const DistillArgs& a, int64_t row, f
   if (lane == 0) s.mass = some ? sum * inv : 0.f;
 }
 
-// Warp 0: the row's loss.
+// A warp: the row's loss.
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const DistillSmem& s, MaxSum q) {
   const float inv_t = 1.f / a.temperature, log_s = logf(q.s);
   float sum = 0.f;
@@ -178,10 +254,9 @@ struct Cut {
 
 template <typename T>
 __device__ __forceinline__ MaxSum read_slice(const T* x, const Cut<T>& cut, T* kept,
-                                             bool keep, float c) {
+                                             bool keep, int tid, int threads, float c) {
   constexpr int kN = Cut<T>::kN, kAhead = 4;
-  MaxSum r = {kNegInf, 0.f};
-  const int tid = threadIdx.x, threads = blockDim.x;
+  Running r = {kNegInf, pack2(0.f, 0.f)};
   const Vec<T, kN>* body = (const Vec<T, kN>*)(x + cut.head);
   Vec<T, kN>* kept_body = (Vec<T, kN>*)(kept + cut.shift + cut.head);
   int32_t j = tid;
@@ -192,22 +267,22 @@ __device__ __forceinline__ MaxSum read_slice(const T* x, const Cut<T>& cut, T* k
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (keep) kept_body[j + u * threads] = v[u];
-      take<T, kN>(r, v[u], c);
+      r.take(v[u], c);
     }
   }
   for (; j < cut.body; j += threads) {
     const Vec<T, kN> v = body[j];
     if (keep) kept_body[j] = v;
-    take<T, kN>(r, v, c);
+    r.take(v, c);
   }
   const auto one = [&](int32_t i) {
-    const Vec<T, 1> v = {x[i]};
-    if (keep) kept[cut.shift + i] = v.v[0];
-    take<T, 1>(r, v, c);
+    const T v = x[i];
+    if (keep) kept[cut.shift + i] = v;
+    r.take_one(to_f32(v), c);
   };
   if (tid < cut.head) one(tid);
   if (tid < cut.n - cut.tail0()) one(cut.tail0() + tid);
-  return r;
+  return r.sum();
 }
 
 // out = factor * 2^((x - m) c) for the slice, from shared memory or from x.
@@ -221,7 +296,7 @@ __device__ __forceinline__ void write_slice(const T* x, const Cut<T>& cut, const
   const auto value = [&](T v) {
     return from_f32<TOut>(zero ? 0.f : factor * exp2_fast((to_f32(v) - m) * c));
   };
-  if ((uintptr_t)(out + cut.head) % kPart != 0) {
+  if (zero || (uintptr_t)(out + cut.head) % kPart != 0) {
     for (int32_t i = tid; i < cut.n; i += threads)
       out[i] = value(keep ? kept[cut.shift + i] : x[i]);
     return;
@@ -234,7 +309,12 @@ __device__ __forceinline__ void write_slice(const T* x, const Cut<T>& cut, const
     for (int h = 0; h < kN / kPartN; ++h) {
       Vec<TOut, kPartN> y;
 #pragma unroll
-      for (int e = 0; e < kPartN; ++e) y.v[e] = value(v.v[h * kPartN + e]);
+      for (int e = 0; e < kPartN; e += 2) {
+        const float2 f =
+            unpack2(mul2(add2(pair_of(v.v + h * kPartN + e), pack2(-m, -m)), pack2(c, c)));
+        put_pair(y.v + e, unpack2(mul2(pack2(exp2_fast(f.x), exp2_fast(f.y)),
+                                       pack2(factor, factor))));
+      }
       *(Vec<TOut, kPartN>*)(out + cut.head + j * kN + h * kPartN) = y;
     }
   }
@@ -257,23 +337,26 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillArgs a) {
   const int32_t v0 = min(a.classes, rank * a.slice);
   const int32_t n = min(a.classes, v0 + a.slice) - v0;
   const Cut<T> cut(x_row + v0, n);
-  if (tid < 32) {
+  // the last warp reads the teacher's entries, the others the slice
+  const int readers = (int)blockDim.x - 32;
+  MaxSum q = {kNegInf, 0.f};
+  if (tid >= readers) {
     teacher_row(a, row, c, s);
     if (kMode != kGrad && rank == 0)
-      for (int k = tid; k < a.top; k += 32)
+      for (int k = tid - readers; k < a.top; k += 32)
         s.x[k] = s.index[k] >= 0 ? to_f32(x_row[s.index[k]]) : 0.f;
+  } else if (kMode != kGrad) {
+    q = warp_join(read_slice<T>(x_row + v0, cut, kept, a.keep, tid, readers, c), c);
+    if (lane_id() == 0) s.part[tid >> 5] = q;
   }
-  MaxSum q;
+  __syncthreads();
   if (kMode == kGrad) {
     const float2 st = a.stats[row];
     q = {st.x, st.y};
-    __syncthreads();
   } else {
-    q = warp_join(read_slice<T>(x_row + v0, cut, kept, a.keep, c), c);
-    if (lane_id() == 0) s.part[tid >> 5] = q;
-    __syncthreads();
-    q = s.part[0];
-    for (int w = 1; w < (int)(blockDim.x >> 5); ++w) q = join(q, s.part[w], c);
+    q = {kNegInf, 0.f};
+    if (lane_id() < readers >> 5) q = s.part[lane_id()];
+    q = warp_join(q, c);
     if (ranks > 1) {
       cg::cluster_group cluster = cg::this_cluster();
       if (tid == 0) s.joined = q;
@@ -356,7 +439,7 @@ Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int n
   }
   s.ranks = (int)ranks;
   s.slice = (int32_t)slice_of(ranks);
-  s.threads = s.slice <= 2048 ? 128 : s.slice <= 8192 ? 256 : kMaxThreads;
+  s.threads = 32 + (s.slice <= 2048 ? 128 : s.slice <= 8192 ? 256 : kMaxReaders);
   const size_t kept = (size_t)(s.slice * size + 32);
   s.keep = mode == kStep && kept <= kMaxKeep;
   s.smem = sizeof(DistillSmem) + (s.keep ? kept : 0);

@@ -1,10 +1,10 @@
 // mx4.cu -- rows to microscaled 4-bit floating point and back
 // (include/agnes_ops.h; the format is in mx4.cuh).
 //
-// A thread takes eight values, so four threads share a block of 32: its largest
-// magnitude is found by two exchanges within the warp.  Magnitudes are compared
-// as bit patterns, which order as the numbers do and put what is not finite on
-// top.
+// Bound by memory where the instructions leave it: a thread takes 16 values, so that
+// two share a block of 32, whose largest magnitude takes one exchange.  Magnitudes are
+// compared as bit patterns, which order as the numbers do and put what is not finite on
+// top, two 16-bit ones at once.
 #include <type_traits>
 
 #include "mx4.cuh"
@@ -15,91 +15,129 @@ namespace agnes {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kItems = kFlat / kThreads;  // groups of eight values per thread
+constexpr int kItems = kFlat / kThreads;  // groups of eight values per thread, to dequantise
+constexpr int kQuantThreads = 512;
+constexpr int kQuantItems = kFlat / kQuantThreads;  // groups of sixteen, to quantise
 
-// The eight values from column col0 of a row, zeros past its end; kWide: the row
-// is 16-byte aligned and a whole number of eights.
+// Sixteen values of a row.
+template <typename T>
+struct Sixteen {
+  static constexpr int kWords = 16 * sizeof(T) / 4;
+  uint32_t w[kWords];
+};
+
+// From column col0 of a row on, zeros past its end; kWide: rows are 16-byte aligned
+// and a whole number of eights.
 template <typename T, bool kWide>
-__device__ __forceinline__ void load8(const T* row, int32_t col0, int32_t dim, float (&f)[8]) {
+__device__ __forceinline__ void load16(const T* row, int32_t col0, int32_t dim, Sixteen<T>& x) {
   if constexpr (kWide) {
     constexpr int kN = 16 / sizeof(T);
 #pragma unroll
-    for (int h = 0; h < 8 / kN; ++h) {
-      Vec<T, kN> v;
-      if (col0 < dim) {
-        v = *(const Vec<T, kN>*)(row + col0 + h * kN);
-      } else {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) v.v[e] = from_f32<T>(0.f);
-      }
-#pragma unroll
-      for (int e = 0; e < kN; ++e) f[h * kN + e] = to_f32(v.v[e]);
+    for (int h = 0; h < 16 / kN; ++h) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (col0 + h * kN < dim) v = __ldg((const uint4*)(row + col0 + h * kN));
+      x.w[4 * h] = v.x;
+      x.w[4 * h + 1] = v.y;
+      x.w[4 * h + 2] = v.z;
+      x.w[4 * h + 3] = v.w;
     }
   } else {
+    T* e = (T*)x.w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = col0 + e < dim ? to_f32(row[col0 + e]) : 0.f;
+    for (int i = 0; i < 16; ++i) e[i] = col0 + i < dim ? row[col0 + i] : from_f32<T>(0.f);
   }
 }
 
-// groups: 4 * blocks, groups of eight values per row.  kWords: a multiple of 16, so that
-// sixteen lanes hold four whole blocks of a row and their scales are stored as a word (a
-// byte each, and the padding by bytes: 2M fp16 rows of 128 values 233 us, by words HERE).
+// The largest magnitude, as the bits of a float.
+__device__ __forceinline__ uint32_t top_of(const Sixteen<float>& x) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, x.w[i] & 0x7fffffffu);
+  return top;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t top_of(const Sixteen<T>& x) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = __vmaxu2(top, x.w[i] & 0x7fff7fffu);
+  const uint16_t bits = (uint16_t)max(top & 0xffffu, top >> 16);
+  return __float_as_uint(to_f32(*(const T*)&bits));
+}
+
+// Values 2 i and 2 i + 1.
+__device__ __forceinline__ float2 two_of(const Sixteen<float>& x, int i) {
+  return make_float2(__uint_as_float(x.w[2 * i]), __uint_as_float(x.w[2 * i + 1]));
+}
+__device__ __forceinline__ float2 two_of(const Sixteen<__half>& x, int i) {
+  return __half22float2(*(const __half2*)&x.w[i]);
+}
+__device__ __forceinline__ float2 two_of(const Sixteen<__nv_bfloat16>& x, int i) {
+  return make_float2(__uint_as_float(x.w[i] << 16), __uint_as_float(x.w[i] & 0xffff0000u));
+}
+
+// groups: 2 * blocks, groups of sixteen values per row.  kWords: a multiple of 8, so that
+// eight lanes hold four whole blocks of a row and their scales are stored as a word
+// (2M fp16 rows of 128 values, groups of eight: a byte each, and the padding by bytes,
+// 233 us; by words 215; by groups of sixteen 96).
 template <typename T, bool kWide, bool kWords>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kQuantThreads)
 quantize_kernel(const T* __restrict__ x, int64_t rows, int64_t stride, int32_t dim, int32_t groups,
                 uint32_t inv_groups, uint8_t* __restrict__ out, int64_t out_stride,
                 int32_t row_bytes) {
   const FlatRows flat(blockIdx.x, groups, inv_groups);
-  int64_t row[kItems];
-  uint32_t group[kItems];
-  float f[kItems][8];
+  int64_t row[kQuantItems];
+  uint32_t group[kQuantItems];
+  Sixteen<T> v[kQuantItems];
 #pragma unroll
-  for (int u = 0; u < kItems; ++u) {
-    flat.at(threadIdx.x + u * kThreads, &row[u], &group[u]);
+  for (int u = 0; u < kQuantItems; ++u) {
+    flat.at(threadIdx.x + u * kQuantThreads, &row[u], &group[u]);
     if (row[u] < rows) {
-      load8<T, kWide>(x + row[u] * stride, (int32_t)group[u] * 8, dim, f[u]);
+      load16<T, kWide>(x + row[u] * stride, (int32_t)group[u] * 16, dim, v[u]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[u][e] = 0.f;
+      for (int i = 0; i < Sixteen<T>::kWords; ++i) v[u].w[i] = 0;
     }
   }
 #pragma unroll
-  for (int u = 0; u < kItems; ++u) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[u][e]) & 0x7fffffffu);
-    // a block's four groups are in four lanes: a row has a multiple of four
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  for (int u = 0; u < kQuantItems; ++u) {
+    uint32_t top = top_of(v[u]);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));  // a row has an even number
     const uint32_t exponent = top >> 23;  // floor(log2) + 127 of a normal magnitude
     const bool fine = exponent < 255;
     const uint32_t byte = !fine ? 255u : exponent > 2 ? exponent - 2 : 0u;
     // 1 / scale = 2^(127 - byte): a normal number, so the products are exact
     // where they are not far below the smallest step
     const float inv = fine ? __uint_as_float((254u - byte) << 23) : 0.f;
-    uint32_t codes = 0;
+    uint32_t codes[2];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2)
-      codes |= mx4_codes(f[u][e] * inv, f[u][e + 1] * inv) << (4 * e);
-    if (!fine) codes = 0;
+    for (int h = 0; h < 2; ++h) {
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 t = two_of(v[u], 4 * h + i);
+        f[2 * i] = t.x * inv;
+        f[2 * i + 1] = t.y * inv;
+      }
+      codes[h] = fine ? mx4_codes8(f) : 0u;
+    }
     uint32_t word = 0;
-    if constexpr (kWords) {  // four blocks' scales, from lanes 0, 4, 8 and 12 of sixteen
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        word |= __shfl_sync(0xffffffffu, byte, 4 * q, 16) << (8 * q);
+    if constexpr (kWords) {  // four blocks' scales, of eight lanes
+      word = byte << (4 * (threadIdx.x & 6));
+      word |= __shfl_xor_sync(0xffffffffu, word, 2);
+      word |= __shfl_xor_sync(0xffffffffu, word, 4);
     }
     if (row[u] >= rows) continue;
     uint8_t* to = out + row[u] * out_stride;
-    *(uint32_t*)(to + group[u] * 4) = codes;
-    const int32_t blocks = groups >> 2;
+    *(uint2*)(to + group[u] * 8) = make_uint2(codes[0], codes[1]);
+    const int32_t blocks = groups >> 1;
     if constexpr (kWords) {
-      if ((group[u] & 15) == 0) *(uint32_t*)(to + blocks * 16 + (group[u] >> 2)) = word;
-      // the padding, by the lanes after the last whole word's
-      const uint32_t pad = blocks * 17 + (group[u] & 15) * 4;
-      if (group[u] >= (uint32_t)groups - 16 && pad < (uint32_t)row_bytes)
+      if ((group[u] & 7) == 0) *(uint32_t*)(to + blocks * 16 + (group[u] >> 1)) = word;
+      // the padding: three words at most, by the row's last lanes
+      const uint32_t pad = blocks * 17 + (group[u] & 7) * 4;
+      if (group[u] >= (uint32_t)groups - 8 && pad < (uint32_t)row_bytes)
         *(uint32_t*)(to + pad) = 0;
     } else {
-      if ((group[u] & 3) == 0) to[blocks * 16 + (group[u] >> 2)] = (uint8_t)byte;
+      if ((group[u] & 1) == 0) to[blocks * 16 + (group[u] >> 1)] = (uint8_t)byte;
       if (group[u] == 0)
         for (int32_t b = blocks * 17; b < row_bytes; ++b) to[b] = 0;
     }
@@ -220,18 +258,18 @@ agnes_status agnes_mx4_quantize(const void* x, int32_t dtype, int64_t stride, in
   OP_TRY(op_aligned(op, "out", out, 16));
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
-  const MxGrid g = mx_grid(rows, 4 * mx4_blocks(dim));
+  const MxGrid g = mx_grid(rows, 2 * mx4_blocks(dim));
   if (g.ctas > 0x7fffffff) return op_error(AGNES_ERANGE, "%s: rows * dim is too large", op);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const cudaError_t e = with_float_type(dtype, [&](auto t) {
     using T = typename decltype(t)::type;
     const bool wide = dim % 8 == 0 && aligned_rows(x, rows > 1 ? stride * (int64_t)sizeof(T) : 0, 16);
-    const bool words = g.groups % 16 == 0;
+    const bool words = g.groups % 8 == 0;
     const auto kernel = wide ? (words ? quantize_kernel<T, true, true>
                                       : quantize_kernel<T, true, false>)
                              : (words ? quantize_kernel<T, false, true>
                                       : quantize_kernel<T, false, false>);
-    kernel<<<(unsigned)g.ctas, kThreads, 0, st>>>(
+    kernel<<<(unsigned)g.ctas, kQuantThreads, 0, st>>>(
         (const T*)x, rows, stride, (int32_t)dim, g.groups, g.inv, (uint8_t*)out, out_stride,
         (int32_t)mx4_row_bytes(dim));
     return cudaGetLastError();

@@ -19,14 +19,18 @@ __device__ __forceinline__ float mx4_scale(uint32_t byte) {
   return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fffffffu : byte << 23);
 }
 
-// Two codes from two floats, to nearest even, beyond 6 to 6; `lo` in the low half.
-__device__ __forceinline__ uint32_t mx4_codes(float lo, float hi) {
+// Eight codes from floats, each to nearest even, beyond 6 to 6; the first in the lowest
+// bits.
+__device__ __forceinline__ uint32_t mx4_codes8(const float (&f)[8]) {
   uint32_t r;
-  asm("{\n\t.reg .b8 q;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 q, %2, %1;\n\t"
-      "cvt.u32.u8 %0, q;\n\t}"
+  asm("{\n\t.reg .b8 q0, q1, q2, q3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 q0, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 q1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 q2, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 q3, %8, %7;\n\t"
+      "mov.b32 %0, {q0, q1, q2, q3};\n\t}"
       : "=r"(r)
-      : "f"(lo), "f"(hi));
+      : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
   return r;
 }
 

@@ -40,6 +40,7 @@ struct DistillArgs {
   int32_t index_bits;
   int32_t top;
   float temperature;
+  float c;        // log2(e) / T
   float* loss;    // R
   float2* stats;  // R: (M, S); written by kLoss, read by kGrad
   const float* weight;  // R, or null: 1
@@ -75,13 +76,13 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c) {
   return {m, a.s * exp2_fast((a.m - z) * c) + b.s * exp2_fast((b.m - z) * c)};
 }
 
+// The join over a warp's lanes: the largest maximum first, so that a lane's sum is
+// scaled once.
 __device__ __forceinline__ MaxSum warp_join(MaxSum x, float c) {
+  float m = x.m;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    const MaxSum y = {__shfl_xor_sync(0xffffffffu, x.m, d), __shfl_xor_sync(0xffffffffu, x.s, d)};
-    x = join(x, y, c);
-  }
-  return x;
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  return {m, warp_sum(x.s * exp2_fast((x.m - above(m)) * c))};
 }
 
 // Pairs of floats, for the packed instructions (each half rounded as by a single one).
@@ -184,7 +185,7 @@ struct Running {
 struct alignas(16) DistillSmem {  // the kept slice follows it, in 16-byte vectors
   float p[kMaxTop];
   int32_t index[kMaxTop];  // -1: absent
-  float x[kMaxTop];        // the student's logit at index (rank 0)
+  float x[kMaxTop];        // the student's logit at index
   MaxSum part[32];         // the readers' warps'
   MaxSum joined;           // this CTA's
   float mass;              // sum of p: 1, or 0 without a teacher entry
@@ -303,6 +304,7 @@ __device__ __forceinline__ void write_slice(const T* x, const Cut<T>& cut, const
   }
   const Vec<T, kN>* body =
       (const Vec<T, kN>*)(keep ? kept + cut.shift + cut.head : x + cut.head);
+#pragma unroll 2
   for (int32_t j = tid; j < cut.body; j += threads) {
     const Vec<T, kN> v = body[j];
 #pragma unroll
@@ -332,7 +334,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillArgs a) {
   const int64_t row = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
   const int rank = blockIdx.x, ranks = gridDim.x;
   const int tid = threadIdx.x;
-  const float c = 1.4426950408889634f / a.temperature;  // log2(e) / T
+  const float c = a.c;
   const T* x_row = (const T*)a.logits + row * a.stride;
   const int32_t v0 = min(a.classes, rank * a.slice);
   const int32_t n = min(a.classes, v0 + a.slice) - v0;
@@ -342,9 +344,12 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillArgs a) {
   MaxSum q = {kNegInf, 0.f};
   if (tid >= readers) {
     teacher_row(a, row, c, s);
-    if (kMode != kGrad && rank == 0)
-      for (int k = tid - readers; k < a.top; k += 32)
-        s.x[k] = s.index[k] >= 0 ? to_f32(x_row[s.index[k]]) : 0.f;
+    // of all classes for the loss, else of this slice's: others' may be overwritten
+    const bool all = kMode != kGrad && rank == 0;
+    for (int k = tid - readers; k < a.top; k += 32) {
+      const int32_t v = s.index[k];
+      s.x[k] = v >= 0 && (all || (v >= v0 && v < v0 + n)) ? to_f32(x_row[v]) : 0.f;
+    }
   } else if (kMode != kGrad) {
     q = warp_join(read_slice<T>(x_row + v0, cut, kept, a.keep, tid, readers, c), c);
     if (lane_id() == 0) s.part[tid >> 5] = q;
@@ -378,35 +383,22 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillArgs a) {
     const bool zero = s.mass == 0.f || q.s == 0.f;
     TOut* out = (TOut*)a.out + row * a.out_stride + v0;
     const float inv = 1.f / q.s, factor = coef * s.mass * inv;
-    // the logits at the entries' classes of this slice, before they may be overwritten
     const bool keep = kMode == kStep && a.keep;
-    float xk[(kMaxTop + 127) / 128];
-#pragma unroll
-    for (int u = 0; u < (kMaxTop + 127) / 128; ++u) {
-      const int k = tid + u * blockDim.x;
-      const int32_t v = k < a.top ? s.index[k] - v0 : -1;
-      xk[u] = v >= 0 && v < n ? to_f32(keep ? kept[cut.shift + v] : x_row[v0 + v]) : 0.f;
-    }
-    __syncthreads();
     write_slice<T, TOut>(x_row + v0, cut, kept, keep, out, q.m, factor, c, zero);
     __syncthreads();
-    if (!zero) {
-#pragma unroll
-      for (int u = 0; u < (kMaxTop + 127) / 128; ++u) {
-        const int k = tid + u * blockDim.x;
-        const int32_t v = k < a.top ? s.index[k] - v0 : -1;
-        if (v < 0 || v >= n) continue;
-        // the class's whole mass, by the first of the entries that name it
-        float p = 0.f;
-        bool first = true;
-        for (int j = 0; j < a.top; ++j) {
-          if (s.index[j] != v + v0) continue;
-          p += s.p[j];
-          first &= j >= k;
-        }
-        if (first)
-          out[v] = from_f32<TOut>(coef * (s.mass * inv * exp2_fast((xk[u] - q.m) * c) - p));
+    for (int k = tid; k < a.top && !zero; k += blockDim.x) {
+      const int32_t v = s.index[k] - v0;
+      if (s.index[k] < 0 || v < 0 || v >= n) continue;
+      // the class's whole mass, by the first of the entries that name it
+      float p = 0.f;
+      bool first = true;
+      for (int j = 0; j < a.top; ++j) {
+        if (s.index[j] != v + v0) continue;
+        p += s.p[j];
+        first &= j >= k;
       }
+      if (first)
+        out[v] = from_f32<TOut>(coef * (s.mass * inv * exp2_fast((s.x[k] - q.m) * c) - p));
     }
   }
   if (kMode != kGrad && ranks > 1) cg::this_cluster().sync();  // the others have read s.joined
@@ -573,6 +565,7 @@ agnes_status distill(const DistillCall& c) {
   a.index_bits = c.index_bits;
   a.top = (int32_t)c.top;
   a.temperature = c.temperature;
+  a.c = (float)(1.4426950408889634 / (double)c.temperature);
   a.loss = c.loss;
   a.stats = (float2*)c.stats;
   a.weight = c.weight;

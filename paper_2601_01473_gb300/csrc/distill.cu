@@ -7,12 +7,13 @@
 //
 // One pass over the row keeps a running maximum M and sum S of exp((x - M) / T).
 // A cluster of CTAs shares a row, each a slice of it, and joins (M, S) through
-// distributed shared memory; a step that also wants the gradient keeps its slice
-// in shared memory, so that the logits are read from memory once.  The gradient
-// is written as if the teacher had no entry, and then the few entries' classes
-// once more.
+// distributed shared memory.  A slice is copied to shared memory by a few bulk copies
+// that are all on their way from the start, and a step that also wants the gradient
+// takes it from there, so that the logits are read from memory once.  The gradient is
+// written as if the teacher had no entry, and then the few entries' classes once more.
 #include <cooperative_groups.h>
 
+#include "mbarrier.cuh"
 #include "ops_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -22,9 +23,10 @@ namespace agnes {
 namespace {
 
 constexpr int kMaxTop = AGNES_DISTILL_MAX_TOP;
-constexpr int kMaxReaders = 512;
+constexpr int kMaxReaders = 384;
 constexpr int kMaxThreads = kMaxReaders + 32;
 constexpr int kMaxCluster = 8;
+constexpr int kCopies = 8;  // bulk copies of a slice
 constexpr float kNegInf = -__builtin_huge_valf();
 
 enum Mode { kLoss, kGrad, kStep };
@@ -47,7 +49,7 @@ struct DistillArgs {
   float weight_scale;
   void* out;
   int64_t out_stride;
-  bool keep;  // the slice stays in shared memory
+  bool keep;  // the slice fits shared memory
   int32_t* status;
 };
 
@@ -182,39 +184,39 @@ struct Running {
   }
 };
 
-struct alignas(16) DistillSmem {  // the kept slice follows it, in 16-byte vectors
-  float p[kMaxTop];
-  int32_t index[kMaxTop];  // -1: absent
-  float x[kMaxTop];        // the student's logit at index
-  MaxSum part[32];         // the readers' warps'
-  MaxSum joined;           // this CTA's
-  float mass;              // sum of p: 1, or 0 without a teacher entry
+// The teacher's entries of a row, in shared memory.
+struct Entries {
+  float* p;        // the teacher's distribution
+  int32_t* index;  // -1: absent
+  float* x;        // the student's logit at index
 };
-static_assert(sizeof(DistillSmem) % 16 == 0, "what follows is 16-byte aligned");
 
-// A warp: the teacher's distribution of the row.
-__device__ __forceinline__ void teacher_row(const DistillArgs& a, int64_t row, float c,
-                                            DistillSmem& s) {
+// A warp: the entries of a row, and the logits at their classes in [lo, hi).  Returns
+// the sum of p: 1, or 0 without an entry.
+template <typename T>
+__device__ __forceinline__ float teacher_row(const DistillArgs& a, int64_t row, const T* x_row,
+                                             int32_t lo, int32_t hi, const Entries& s) {
   const int lane = lane_id();
   float top = kNegInf;
   bool bad = false;
   for (int k = lane; k < a.top; k += 32) {
     const int64_t i = row * a.top + k;
+    const float t = load_teacher(a, i);  // on its way with the index
     const int64_t v = a.index_bits == 32 ? (int64_t)__ldg((const int32_t*)a.index + i)
                                          : __ldg((const int64_t*)a.index + i);
     const bool in = v >= 0 && v < a.classes;
     bad |= v >= a.classes;
     s.index[k] = in ? (int32_t)v : -1;
-    const float t = in ? load_teacher(a, i) : kNegInf;
-    s.p[k] = t;
-    top = fmaxf(top, t);
+    s.x[k] = in && v >= lo && v < hi ? to_f32(x_row[v]) : 0.f;
+    s.p[k] = in ? t : kNegInf;
+    top = fmaxf(top, s.p[k]);
   }
   if (bad) op_flag(a.status, AGNES_OP_BAD_INDEX);
   top = warp_max(top);
   const float z = above(top);
   float sum = 0.f;
   for (int k = lane; k < a.top; k += 32) {
-    const float e = s.index[k] < 0 ? 0.f : exp2_fast((s.p[k] - z) * c);
+    const float e = s.index[k] < 0 ? 0.f : exp2_fast((s.p[k] - z) * a.c);
     s.p[k] = e;
     sum += e;
   }
@@ -223,11 +225,32 @@ __device__ __forceinline__ void teacher_row(const DistillArgs& a, int64_t row, f
   const bool some = !(sum == 0.f);
   const float inv = some ? 1.f / sum : 0.f;
   for (int k = lane; k < a.top; k += 32) s.p[k] *= inv;
-  if (lane == 0) s.mass = some ? sum * inv : 0.f;
+  return some ? sum * inv : 0.f;
+}
+
+// A warp: whether two entries name the same class.  `table`: `slots` words, a power of
+// two of at least twice the entries.
+__device__ __forceinline__ bool repeated(const DistillArgs& a, const Entries& s, int32_t* table,
+                                         int slots) {
+  const int lane = lane_id();
+  for (int i = lane; i < slots; i += 32) table[i] = -1;
+  __syncwarp();
+  bool twice = false;
+  for (int k = lane; k < a.top; k += 32) {
+    const int32_t v = s.index[k];
+    if (v < 0) continue;
+    uint32_t at = (uint32_t)v * 2654435761u >> 16;
+    for (int n = 0; n < slots; ++n, ++at) {
+      const int32_t old = atomicCAS(table + (at & (uint32_t)(slots - 1)), -1, v);
+      twice |= old == v;
+      if (old == -1 || old == v) break;
+    }
+  }
+  return __any_sync(0xffffffffu, twice);
 }
 
 // A warp: the row's loss.
-__device__ __forceinline__ float row_loss(const DistillArgs& a, const DistillSmem& s, MaxSum q) {
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& s, MaxSum q) {
   const float inv_t = 1.f / a.temperature, log_s = logf(q.s);
   float sum = 0.f;
   for (int k = lane_id(); k < a.top; k += 32) {
@@ -237,6 +260,47 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const DistillSme
   }
   return warp_sum(sum) * a.temperature * a.temperature;
 }
+
+// The entries' classes in [v0, v0 + n) once more: out = coef (mass q - p), where p is
+// the class's whole mass, by the first of the entries that name it.
+template <typename TOut>
+__device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries& s, bool twice,
+                                            TOut* out, int32_t v0, int32_t n, MaxSum q, float coef,
+                                            float mass_inv, int tid, int threads) {
+  for (int k = tid; k < a.top; k += threads) {
+    const int32_t v = s.index[k] - v0;
+    if (s.index[k] < 0 || v < 0 || v >= n) continue;
+    float p = s.p[k];
+    if (twice) {
+      bool first = true;
+      p = 0.f;
+      for (int j = 0; j < a.top; ++j) {
+        if (s.index[j] != v + v0) continue;
+        p += s.p[j];
+        first &= j >= k;
+      }
+      if (!first) continue;
+    }
+    out[v] = from_f32<TOut>(coef * (mass_inv * exp2_fast((s.x[k] - q.m) * a.c) - p));
+  }
+}
+
+constexpr int kTable = 2 * kMaxTop;
+
+struct alignas(16) DistillSmem {  // the kept slice follows it, in 16-byte vectors
+  float p[kMaxTop];
+  int32_t index[kMaxTop];
+  float x[kMaxTop];
+  int32_t table[kTable];
+  MaxSum part[32];         // the readers' warps'
+  MaxSum joined;           // this CTA's
+  uint64_t bars[kCopies];  // the copies of the slice
+  float mass;
+  float weight;
+  float2 stats;
+  bool twice;
+};
+static_assert(sizeof(DistillSmem) % 16 == 0, "what follows is 16-byte aligned");
 
 // The vectors of a slice: `head` elements up to the first 16-byte boundary, then
 // `body` whole vectors, then the rest.
@@ -253,47 +317,105 @@ struct Cut {
   __device__ int32_t tail0() const { return head + body * kN; }
 };
 
+// The copies of a slice's body: `step` vectors each, a multiple of the readers.
+struct Copies {
+  int32_t step, count;
+  __device__ Copies(int32_t body, int readers) {
+    step = (body + kCopies * readers - 1) / (kCopies * readers) * readers;
+    count = step > 0 ? (body + step - 1) / step : 0;
+  }
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) {
+  return (uint32_t)__cvta_generic_to_shared(p);
+}
+
+// One thread: has the whole body copied to shared memory.
 template <typename T>
-__device__ __forceinline__ MaxSum read_slice(const T* x, const Cut<T>& cut, T* kept,
-                                             bool keep, int tid, int threads, float c) {
+__device__ __forceinline__ void start_copies(const T* x, const Cut<T>& cut, T* kept,
+                                             const Copies& copies, uint64_t* bars) {
+  for (int i = 0; i < copies.count; ++i) mbar_init(smem_addr(bars + i), 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  for (int i = 0; i < copies.count; ++i) {
+    const int32_t first = i * copies.step;
+    const uint32_t bytes = 16u * (uint32_t)min(copies.step, cut.body - first);
+    const uint32_t bar = smem_addr(bars + i);
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+                 : "memory");
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+            "r"(smem_addr(kept + cut.shift + cut.head) + 16u * (uint32_t)first),
+        "l"(x + cut.head + (int64_t)first * Cut<T>::kN), "r"(bytes), "r"(bar)
+        : "memory");
+  }
+}
+
+// Waits for copy i; a wait that ran out is reported and tried once more, as the CTA
+// may not leave before its copies have landed.
+__device__ __forceinline__ void wait_copy(uint64_t* bars, int i, int32_t* status) {
+  const uint32_t bar = smem_addr(bars + i);
+  if (mbar_wait(bar, 0)) return;
+  op_flag(status, AGNES_OP_TIMEOUT);
+  mbar_wait(bar, 0);
+}
+
+// A slice's few elements before and after its body to shared memory.
+template <typename T, typename F>
+__device__ __forceinline__ void ragged_ends(const T* x, const Cut<T>& cut, int tid, F&& f) {
+  if (tid < cut.head) f(tid, x[tid]);
+  const int32_t i = cut.tail0() + tid;
+  if (i < cut.n) f(i, x[i]);
+}
+
+// A reader's share of a slice in shared memory.
+template <typename T>
+__device__ __forceinline__ MaxSum read_kept(const T* x, const Cut<T>& cut, T* kept,
+                                            const Copies& copies, uint64_t* bars, int tid,
+                                            int threads, float c, int32_t* status) {
+  constexpr int kN = Cut<T>::kN;
+  Running r = {kNegInf, pack2(0.f, 0.f)};
+  ragged_ends(x, cut, tid, [&](int32_t i, T v) {
+    kept[cut.shift + i] = v;
+    r.take_one(to_f32(v), c);
+  });
+  const Vec<T, kN>* body = (const Vec<T, kN>*)(kept + cut.shift + cut.head);
+  for (int i = 0; i < copies.count; ++i) {
+    wait_copy(bars, i, status);
+    const int32_t end = min(cut.body, (i + 1) * copies.step);
+#pragma unroll 2
+    for (int32_t j = i * copies.step + tid; j < end; j += threads) r.take(body[j], c);
+  }
+  return r.sum();
+}
+
+// The same from memory, for slices that do not fit.
+template <typename T>
+__device__ __forceinline__ MaxSum read_slice(const T* x, const Cut<T>& cut, int tid, int threads,
+                                             float c) {
   constexpr int kN = Cut<T>::kN, kAhead = 4;
   Running r = {kNegInf, pack2(0.f, 0.f)};
   const Vec<T, kN>* body = (const Vec<T, kN>*)(x + cut.head);
-  Vec<T, kN>* kept_body = (Vec<T, kN>*)(kept + cut.shift + cut.head);
   int32_t j = tid;
   for (; j + (kAhead - 1) * threads < cut.body; j += kAhead * threads) {
     Vec<T, kN> v[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) v[u] = body[j + u * threads];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (keep) kept_body[j + u * threads] = v[u];
-      r.take(v[u], c);
-    }
+    for (int u = 0; u < kAhead; ++u) r.take(v[u], c);
   }
-  for (; j < cut.body; j += threads) {
-    const Vec<T, kN> v = body[j];
-    if (keep) kept_body[j] = v;
-    r.take(v, c);
-  }
-  const auto one = [&](int32_t i) {
-    const T v = x[i];
-    if (keep) kept[cut.shift + i] = v;
-    r.take_one(to_f32(v), c);
-  };
-  if (tid < cut.head) one(tid);
-  if (tid < cut.n - cut.tail0()) one(cut.tail0() + tid);
+  for (; j < cut.body; j += threads) r.take(body[j], c);
+  ragged_ends(x, cut, tid, [&](int32_t, T v) { r.take_one(to_f32(v), c); });
   return r.sum();
 }
 
 // out = factor * 2^((x - m) c) for the slice, from shared memory or from x.
 template <typename T, typename TOut>
 __device__ __forceinline__ void write_slice(const T* x, const Cut<T>& cut, const T* kept, bool keep,
-                                            TOut* out, float m, float factor, float c, bool zero) {
+                                            TOut* out, float m, float factor, float c, bool zero,
+                                            int tid, int threads) {
   constexpr int kN = Cut<T>::kN;
   constexpr int kOutBytes = kN * sizeof(TOut), kPart = kOutBytes > 16 ? 16 : kOutBytes;
   constexpr int kPartN = kPart / (int)sizeof(TOut);
-  const int tid = threadIdx.x, threads = blockDim.x;
   const auto value = [&](T v) {
     return from_f32<TOut>(zero ? 0.f : factor * exp2_fast((to_f32(v) - m) * c));
   };
@@ -341,23 +463,40 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillArgs a) {
   const Cut<T> cut(x_row + v0, n);
   // the last warp reads the teacher's entries, the others the slice
   const int readers = (int)blockDim.x - 32;
+  const Copies copies(cut.body, readers);
+  if (a.keep) {
+    if (tid == 0) start_copies(x_row + v0, cut, kept, copies, s.bars);
+    __syncthreads();
+  }
+  const Entries entries = {s.p, s.index, s.x};
   MaxSum q = {kNegInf, 0.f};
   if (tid >= readers) {
-    teacher_row(a, row, c, s);
-    // of all classes for the loss, else of this slice's: others' may be overwritten
-    const bool all = kMode != kGrad && rank == 0;
-    for (int k = tid - readers; k < a.top; k += 32) {
-      const int32_t v = s.index[k];
-      s.x[k] = v >= 0 && (all || (v >= v0 && v < v0 + n)) ? to_f32(x_row[v]) : 0.f;
+    const int lane = tid - readers;
+    if (lane == 0 && kMode != kLoss) {
+      s.weight = a.weight ? __ldg(a.weight + row) : 1.f;
+      if (kMode == kGrad) s.stats = a.stats[row];
     }
-  } else if (kMode != kGrad) {
-    q = warp_join(read_slice<T>(x_row + v0, cut, kept, a.keep, tid, readers, c), c);
+    // the logits of all classes for the loss, else of this slice: others' may be
+    // overwritten
+    const bool all = kMode != kGrad && rank == 0;
+    const float mass =
+        teacher_row(a, row, x_row, all ? 0 : v0, all ? a.classes : v0 + n, entries);
+    const bool twice = kMode != kLoss && repeated(a, entries, s.table, kTable);
+    if (lane == 0) {
+      s.mass = mass;
+      s.twice = twice;
+    }
+  } else if (kMode == kGrad) {
+    if (a.keep) ragged_ends(x_row + v0, cut, tid, [&](int32_t i, T v) { kept[cut.shift + i] = v; });
+  } else {
+    q = a.keep ? read_kept(x_row + v0, cut, kept, copies, s.bars, tid, readers, c, a.status)
+               : read_slice(x_row + v0, cut, tid, readers, c);
+    q = warp_join(q, c);
     if (lane_id() == 0) s.part[tid >> 5] = q;
   }
   __syncthreads();
   if (kMode == kGrad) {
-    const float2 st = a.stats[row];
-    q = {st.x, st.y};
+    q = {s.stats.x, s.stats.y};
   } else {
     q = {kNegInf, 0.f};
     if (lane_id() < readers >> 5) q = s.part[lane_id()];
@@ -369,39 +508,80 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillArgs a) {
       q = *cluster.map_shared_rank(&s.joined, 0);
       for (int r = 1; r < ranks; ++r) q = join(q, *cluster.map_shared_rank(&s.joined, r), c);
     }
-    if (rank == 0 && tid < 32) {
+    if (rank == 0 && tid >= readers) {
       const bool some = s.mass != 0.f && q.s != 0.f;  // s = 0: every logit is -inf
-      const float loss = some ? row_loss(a, s, q) : 0.f;
-      if (tid == 0) {
+      const float loss = some ? row_loss(a, entries, q) : 0.f;
+      if (tid == readers) {
         a.loss[row] = loss;
         if (kMode == kLoss) a.stats[row] = make_float2(q.m, q.s);
       }
     }
   }
   if (kMode != kLoss) {
-    const float coef = (a.weight ? a.weight[row] : 1.f) * a.weight_scale * a.temperature;
+    const float coef = s.weight * a.weight_scale * a.temperature;
     const bool zero = s.mass == 0.f || q.s == 0.f;
     TOut* out = (TOut*)a.out + row * a.out_stride + v0;
-    const float inv = 1.f / q.s, factor = coef * s.mass * inv;
-    const bool keep = kMode == kStep && a.keep;
-    write_slice<T, TOut>(x_row + v0, cut, kept, keep, out, q.m, factor, c, zero);
+    const float mass_inv = s.mass / q.s;
+    if (kMode == kGrad && a.keep)
+      for (int i = 0; i < copies.count; ++i) wait_copy(s.bars, i, a.status);
+    write_slice<T, TOut>(x_row + v0, cut, kept, a.keep, out, q.m, coef * mass_inv, c, zero, tid,
+                         blockDim.x);
     __syncthreads();
-    for (int k = tid; k < a.top && !zero; k += blockDim.x) {
-      const int32_t v = s.index[k] - v0;
-      if (s.index[k] < 0 || v < 0 || v >= n) continue;
-      // the class's whole mass, by the first of the entries that name it
-      float p = 0.f;
-      bool first = true;
-      for (int j = 0; j < a.top; ++j) {
-        if (s.index[j] != v + v0) continue;
-        p += s.p[j];
-        first &= j >= k;
-      }
-      if (first)
-        out[v] = from_f32<TOut>(coef * (s.mass * inv * exp2_fast((s.x[k] - q.m) * c) - p));
-    }
+    if (!zero)
+      put_entries(a, entries, s.twice, out, v0, n, q, coef, mass_inv, tid, blockDim.x);
   }
   if (kMode != kGrad && ranks > 1) cg::this_cluster().sync();  // the others have read s.joined
+}
+
+// Short rows, a warp to each: nothing to join but its lanes, and no barrier.  The row is
+// read again for the gradient, from L1 or L2.
+constexpr int kShortWarps = 8;
+
+__host__ __device__ inline int short_slots(int top) {  // of a row's table
+  int n = 32;
+  while (n < 2 * top) n *= 2;
+  return n;
+}
+
+template <typename T, typename TOut, int kMode>
+__global__ void __launch_bounds__(32 * kShortWarps) distill_short_kernel(DistillArgs a,
+                                                                         int64_t rows) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = lane_id();
+  const int64_t row = (int64_t)blockIdx.x * kShortWarps + warp;
+  if (row >= rows) return;
+  const int slots = kMode == kLoss ? 0 : short_slots(a.top);
+  float* const mine = (float*)smem + warp * (3 * a.top + slots);
+  const Entries entries = {mine, (int32_t*)(mine + a.top), mine + 2 * a.top};
+  const T* x = (const T*)a.logits + row * a.stride;
+  const Cut<T> cut(x, a.classes);
+  MaxSum q;
+  if (kMode == kGrad) {
+    const float2 st = a.stats[row];
+    q = {st.x, st.y};
+  } else {
+    q = warp_join(read_slice(x, cut, lane, 32, a.c), a.c);
+  }
+  const float mass = teacher_row(a, row, x, 0, a.classes, entries);
+  const bool zero = mass == 0.f || q.s == 0.f;
+  __syncwarp();
+  if (kMode != kGrad) {
+    const float loss = zero ? 0.f : row_loss(a, entries, q);
+    if (lane == 0) {
+      a.loss[row] = loss;
+      if (kMode == kLoss) a.stats[row] = make_float2(q.m, q.s);
+    }
+  }
+  if (kMode != kLoss) {
+    const bool twice = repeated(a, entries, (int32_t*)(mine + 3 * a.top), slots);
+    const float coef = (a.weight ? __ldg(a.weight + row) : 1.f) * a.weight_scale * a.temperature;
+    TOut* out = (TOut*)a.out + row * a.out_stride;
+    const float mass_inv = mass / q.s;
+    write_slice<T, TOut>(x, cut, nullptr, false, out, q.m, coef * mass_inv, a.c, zero, lane, 32);
+    __syncwarp();
+    if (!zero)
+      put_entries(a, entries, twice, out, 0, a.classes, q, coef, mass_inv, lane, 32);
+  }
 }
 
 // ---- host ------------------------------------------------------------------
@@ -415,12 +595,18 @@ struct Shape {
   size_t smem;
 };
 
+// How a row is cut.  A CTA's barriers, joins and trips to memory for the entries take
+// microseconds beside its slice, so CTAs that share an SM hide one another's: two of
+// 100 KB where the slice is kept for the gradient (8192 rows of 50,000 bf16 classes, a
+// step: 310 us, 396 with four of 50 KB), eight of 26 KB where nothing is joined (the
+// gradient alone: 360 us, 502 with 32 KB and twice the threads).  Threads by what is
+// left for each: 4096 rows of 10,007 fp16 classes, a step: 256 50 us, 384 75, 512 76.
 Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int num_sms) {
   Shape s = {};
   const auto slice_of = [&](int64_t ranks) { return ceil_div(ceil_div(classes, ranks), 64) * 64; };
   int64_t ranks = 1;
   if (mode == kGrad) {
-    while (slice_of(ranks) * size > 64 * 1024 ||
+    while (slice_of(ranks) * size > 26 * 1024 ||
            (rows * ranks < 4 * num_sms && slice_of(ranks) > 4096))
       ranks *= 2;
   } else {
@@ -431,15 +617,35 @@ Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int n
   }
   s.ranks = (int)ranks;
   s.slice = (int32_t)slice_of(ranks);
-  s.threads = 32 + (s.slice <= 2048 ? 128 : s.slice <= 8192 ? 256 : kMaxReaders);
+  s.threads = 32 + (s.slice <= 2048 ? 128 : s.slice <= 20000 ? 256 : kMaxReaders);
   const size_t kept = (size_t)(s.slice * size + 32);
-  s.keep = mode == kStep && kept <= kMaxKeep;
+  s.keep = kept <= kMaxKeep;
   s.smem = sizeof(DistillSmem) + (s.keep ? kept : 0);
   return s;
 }
 
+// A warp reads a few vectors at a time, so longer rows are a warp's only where every SM
+// has warps enough.
+bool is_short(int64_t rows, int64_t classes, int num_sms) {
+  return classes <= 512 || (classes <= 4096 && rows >= 8 * num_sms);
+}
+
 template <typename T, typename TOut, int kMode>
 cudaError_t launch_distill(DistillArgs a, int64_t rows, int device, cudaStream_t st) {
+  if (is_short(rows, a.classes, op_num_sms(device))) {
+    const size_t smem =
+        4 * kShortWarps * (size_t)(3 * a.top + (kMode == kLoss ? 0 : short_slots(a.top)));
+    static OncePerDevice once;
+    const cudaError_t e = once.run(device, [] {
+      return cudaFuncSetAttribute(distill_short_kernel<T, TOut, kMode>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  4 * kShortWarps * (3 * kMaxTop + short_slots(kMaxTop)));
+    });
+    if (e != cudaSuccess) return e;
+    distill_short_kernel<T, TOut, kMode>
+        <<<(unsigned)ceil_div(rows, kShortWarps), 32 * kShortWarps, smem, st>>>(a, rows);
+    return cudaGetLastError();
+  }
   const Shape s = distill_shape(rows, a.classes, sizeof(T), kMode, op_num_sms(device));
   a.slice = s.slice;
   a.keep = s.keep;
@@ -447,7 +653,7 @@ cudaError_t launch_distill(DistillArgs a, int64_t rows, int device, cudaStream_t
   static OncePerDevice once;
   cudaError_t e = once.run(device, [&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)(sizeof(DistillSmem) + (kMode == kStep ? kMaxKeep : 0)));
+                                (int)(sizeof(DistillSmem) + kMaxKeep));
   });
   if (e != cudaSuccess) return e;
   // rows over two grid dimensions of 65,535 at most; an exact cover, row by row

@@ -25,6 +25,8 @@ namespace {
 constexpr int kMaxTop = AGNES_DISTILL_MAX_TOP;
 constexpr int kMaxReaders = 384;
 constexpr int kMaxThreads = kMaxReaders + 32;
+constexpr int kGradThreads = 256 + 32;  // of the gradient alone, whose slices are small
+constexpr int kGradCtas = 7;            // that share an SM
 constexpr int kMaxCluster = 8;
 constexpr int kCopies = 8;  // bulk copies of a slice
 constexpr float kNegInf = -__builtin_huge_valf();
@@ -449,7 +451,9 @@ __device__ __forceinline__ void write_slice(const T* x, const Cut<T>& cut, const
 
 // grid: (CTAs per row, rows); kLoss and kStep: a row's CTAs are a cluster.
 template <typename T, typename TOut, int kMode>
-__global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillArgs a) {
+__global__ void __launch_bounds__(kMode == kGrad ? kGradThreads : kMaxThreads,
+                                  kMode == kGrad ? kGradCtas : 2)
+distill_kernel(DistillArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   DistillSmem& s = *(DistillSmem*)smem;
   T* kept = (T*)(smem + sizeof(DistillSmem));
@@ -587,6 +591,9 @@ __global__ void __launch_bounds__(32 * kShortWarps) distill_short_kernel(Distill
 // ---- host ------------------------------------------------------------------
 
 constexpr size_t kMaxKeep = 200 * 1024;  // of a slice in shared memory
+constexpr int64_t kGradSlice = 26 * 1024;
+constexpr int kMidSlice = 20000;  // classes that 256 threads read
+static_assert(kGradSlice / 2 <= kMidSlice, "the gradient alone runs 256 threads at most");
 
 struct Shape {
   int threads, ranks;
@@ -606,7 +613,7 @@ Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int n
   const auto slice_of = [&](int64_t ranks) { return ceil_div(ceil_div(classes, ranks), 64) * 64; };
   int64_t ranks = 1;
   if (mode == kGrad) {
-    while (slice_of(ranks) * size > 26 * 1024 ||
+    while (slice_of(ranks) * size > kGradSlice ||
            (rows * ranks < 4 * num_sms && slice_of(ranks) > 4096))
       ranks *= 2;
   } else {
@@ -617,7 +624,7 @@ Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int n
   }
   s.ranks = (int)ranks;
   s.slice = (int32_t)slice_of(ranks);
-  s.threads = 32 + (s.slice <= 2048 ? 128 : s.slice <= 20000 ? 256 : kMaxReaders);
+  s.threads = 32 + (s.slice <= 2048 ? 128 : s.slice <= kMidSlice ? 256 : kMaxReaders);
   const size_t kept = (size_t)(s.slice * size + 32);
   s.keep = kept <= kMaxKeep;
   s.smem = sizeof(DistillSmem) + (s.keep ? kept : 0);

@@ -264,11 +264,12 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& s
 }
 
 // The entries' classes in [v0, v0 + n) once more: out = coef (mass q - p), where p is
-// the class's whole mass, by the first of the entries that name it.
-template <typename TOut>
+// the class's whole mass, by the first of the entries that name it.  logit(k, v - v0): the
+// student's logit at entry k's class.
+template <typename TOut, typename Logit>
 __device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries& s, bool twice,
                                             TOut* out, int32_t v0, int32_t n, MaxSum q, float coef,
-                                            float mass_inv, int tid, int threads) {
+                                            float mass_inv, int tid, int threads, Logit logit) {
   for (int k = tid; k < a.top; k += threads) {
     const int32_t v = s.index[k] - v0;
     if (s.index[k] < 0 || v < 0 || v >= n) continue;
@@ -283,11 +284,17 @@ __device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries&
       }
       if (!first) continue;
     }
-    out[v] = from_f32<TOut>(coef * (mass_inv * exp2_fast((s.x[k] - q.m) * a.c) - p));
+    out[v] = from_f32<TOut>(coef * (mass_inv * exp2_fast((logit(k, v) - q.m) * a.c) - p));
   }
 }
 
 constexpr int kTable = 2 * kMaxTop;
+__host__ __device__ inline int table_slots(int top) {  // of a row's table
+  int n = 32;
+  while (n < 2 * top) n *= 2;
+  return n;
+}
+
 
 struct alignas(16) DistillSmem {  // the kept slice follows it, in 16-byte vectors
   float p[kMaxTop];
@@ -480,12 +487,12 @@ distill_kernel(DistillArgs a) {
       s.weight = a.weight ? __ldg(a.weight + row) : 1.f;
       if (kMode == kGrad) s.stats = a.stats[row];
     }
-    // the logits of all classes for the loss, else of this slice: others' may be
-    // overwritten
+    // the logits of all classes for the loss, else of this slice (others' may be
+    // overwritten) unless it is kept
     const bool all = kMode != kGrad && rank == 0;
-    const float mass =
-        teacher_row(a, row, x_row, all ? 0 : v0, all ? a.classes : v0 + n, entries);
-    const bool twice = kMode != kLoss && repeated(a, entries, s.table, kTable);
+    const float mass = teacher_row(a, row, x_row, all ? 0 : v0,
+                                   all ? a.classes : a.keep ? v0 : v0 + n, entries);
+    const bool twice = kMode != kLoss && repeated(a, entries, s.table, table_slots(a.top));
     if (lane == 0) {
       s.mass = mass;
       s.twice = twice;
@@ -532,7 +539,8 @@ distill_kernel(DistillArgs a) {
                          blockDim.x);
     __syncthreads();
     if (!zero)
-      put_entries(a, entries, s.twice, out, v0, n, q, coef, mass_inv, tid, blockDim.x);
+      put_entries(a, entries, s.twice, out, v0, n, q, coef, mass_inv, tid, blockDim.x,
+                  [&](int k, int32_t v) { return a.keep ? to_f32(kept[cut.shift + v]) : s.x[k]; });
   }
   if (kMode != kGrad && ranks > 1) cg::this_cluster().sync();  // the others have read s.joined
 }
@@ -541,12 +549,6 @@ distill_kernel(DistillArgs a) {
 // read again for the gradient, from L1 or L2.
 constexpr int kShortWarps = 8;
 
-__host__ __device__ inline int short_slots(int top) {  // of a row's table
-  int n = 32;
-  while (n < 2 * top) n *= 2;
-  return n;
-}
-
 template <typename T, typename TOut, int kMode>
 __global__ void __launch_bounds__(32 * kShortWarps) distill_short_kernel(DistillArgs a,
                                                                          int64_t rows) {
@@ -554,7 +556,7 @@ __global__ void __launch_bounds__(32 * kShortWarps) distill_short_kernel(Distill
   const int warp = threadIdx.x >> 5, lane = lane_id();
   const int64_t row = (int64_t)blockIdx.x * kShortWarps + warp;
   if (row >= rows) return;
-  const int slots = kMode == kLoss ? 0 : short_slots(a.top);
+  const int slots = kMode == kLoss ? 0 : table_slots(a.top);
   float* const mine = (float*)smem + warp * (3 * a.top + slots);
   const Entries entries = {mine, (int32_t*)(mine + a.top), mine + 2 * a.top};
   const T* x = (const T*)a.logits + row * a.stride;
@@ -584,7 +586,8 @@ __global__ void __launch_bounds__(32 * kShortWarps) distill_short_kernel(Distill
     write_slice<T, TOut>(x, cut, nullptr, false, out, q.m, coef * mass_inv, a.c, zero, lane, 32);
     __syncwarp();
     if (!zero)
-      put_entries(a, entries, twice, out, 0, a.classes, q, coef, mass_inv, lane, 32);
+      put_entries(a, entries, twice, out, 0, a.classes, q, coef, mass_inv, lane, 32,
+                  [&](int k, int32_t) { return entries.x[k]; });
   }
 }
 
@@ -641,12 +644,12 @@ template <typename T, typename TOut, int kMode>
 cudaError_t launch_distill(DistillArgs a, int64_t rows, int device, cudaStream_t st) {
   if (is_short(rows, a.classes, op_num_sms(device))) {
     const size_t smem =
-        4 * kShortWarps * (size_t)(3 * a.top + (kMode == kLoss ? 0 : short_slots(a.top)));
+        4 * kShortWarps * (size_t)(3 * a.top + (kMode == kLoss ? 0 : table_slots(a.top)));
     static OncePerDevice once;
     const cudaError_t e = once.run(device, [] {
       return cudaFuncSetAttribute(distill_short_kernel<T, TOut, kMode>,
                                   cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  4 * kShortWarps * (3 * kMaxTop + short_slots(kMaxTop)));
+                                  4 * kShortWarps * (3 * kMaxTop + table_slots(kMaxTop)));
     });
     if (e != cudaSuccess) return e;
     distill_short_kernel<T, TOut, kMode>

@@ -118,6 +118,8 @@ __device__ __forceinline__ Run run_of(int64_t n, int b, int ctas) {
 template <typename Src>
 __global__ void __launch_bounds__(kSortThreads)
 sort_count_kernel(Src src, int64_t n, int shift, int digits, int32_t* __restrict__ counts) {
+  grid_dep_wait();
+  let_next_start();
   __shared__ int32_t hist[kMaxDigits];
   for (int d = threadIdx.x; d < digits; d += kSortThreads) hist[d] = 0;
   __syncthreads();
@@ -139,6 +141,8 @@ sort_count_kernel(Src src, int64_t n, int shift, int digits, int32_t* __restrict
 // totals[digit] their sum.
 __global__ void __launch_bounds__(256)
 sort_scan_kernel(int32_t* __restrict__ counts, int ctas, int digits, int32_t* __restrict__ totals) {
+  grid_dep_wait();
+  let_next_start();
   const int d = blockIdx.x * 8 + (threadIdx.x >> 5);
   if (d >= digits) return;
   int32_t* row = counts + (int64_t)d * ctas;
@@ -227,6 +231,8 @@ __global__ void __launch_bounds__(kSortThreads)
 sort_place_kernel(Src src, int64_t n, int shift, int bits, const int32_t* __restrict__ counts,
                   const int32_t* __restrict__ totals, uint32_t* __restrict__ keys,
                   int32_t* __restrict__ tokens) {
+  grid_dep_wait();
+  let_next_start();
   __shared__ SortSmem s;
   const int digits = 1 << bits;
   digit_bases(s, digits, [&](int d) { return totals[d]; },
@@ -256,11 +262,17 @@ sort_place_kernel(Src src, int64_t n, int shift, int bits, const int32_t* __rest
   }
 }
 
-// Up to kSmallTile tokens in one CTA, every pass in shared memory.
+constexpr int kMinChunk = 32;
+constexpr int kRunChunks = 128;  // chunks whose ranks one CTA counts
+static_assert(kSmallTile <= kMinChunk * kRunChunks, "the small sort's tokens are one run");
+
+// Up to kSmallTile tokens in one CTA, every pass in shared memory; with rank_of and
+// heads, what count_heads_kernel finds, too (chunks of kMinChunk tokens, one run).
 template <typename Id>
 __global__ void __launch_bounds__(kSortThreads)
 sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __restrict__ keys,
-                  int32_t* __restrict__ tokens) {
+                  int32_t* __restrict__ tokens, int32_t* __restrict__ rank_of,
+                  int32_t* __restrict__ heads) {
   extern __shared__ __align__(16) uint8_t small_smem[];
   SortSmem& s = *(SortSmem*)small_smem;
   uint32_t* skey = (uint32_t*)(small_smem + sizeof(SortSmem));
@@ -315,6 +327,27 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
       tokens[i] = token[u];
     }
   }
+  if (!heads) return;
+  // s.base: the ids that begin in each chunk, then their prefix
+  const int chunks = (n + kMinChunk - 1) / kMinChunk;
+  for (int c = threadIdx.x >> 5; c < chunks; c += kSortWarps) {
+    const int i = c * kMinChunk + lane_id();
+    const uint32_t k = i < n ? skey[i] : 0;
+    const bool head = i < n && k < (uint32_t)src.rows && (i == 0 || skey[i - 1] != k);
+    const int count = __popc(__ballot_sync(0xffffffffu, head));
+    if (lane_id() == 0) s.base[c] = count;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  int32_t before = 0;
+  for (int c0 = 0; c0 < chunks; c0 += 32) {
+    const int c = c0 + lane_id();
+    const int32_t count = c < chunks ? s.base[c] : 0;
+    const int32_t incl = warp_incl_scan(count);
+    if (c < chunks) rank_of[c] = before + incl - count;
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane_id() == 0) heads[0] = before;
 }
 constexpr size_t kSmallSmem = sizeof(SortSmem) + 8 * kSmallTile;
 
@@ -323,13 +356,13 @@ constexpr size_t kSmallSmem = sizeof(SortSmem) + 8 * kSmallTile;
 constexpr int kSumThreads = 256;
 constexpr uint32_t kPastChunk = 0xffffffffu;  // no id
 
-constexpr int kRunChunks = 128;  // chunks whose ranks one CTA counts
-
 // rank_of[c] = the number of distinct ids that begin in the chunks of c's run before
 // c; heads[r] = those that begin in run r.  A warp to a chunk.
 __global__ void __launch_bounds__(1024)
 count_heads_kernel(const uint32_t* __restrict__ keys, int64_t n, uint32_t rows, int32_t chunk,
                    int64_t chunks, int32_t* __restrict__ rank_of, int32_t* __restrict__ heads) {
+  grid_dep_wait();
+  let_next_start();
   __shared__ int32_t count[kRunChunks], warp_total[4];
   const int warp = threadIdx.x >> 5, lane = lane_id();
   const int64_t c0 = (int64_t)blockIdx.x * kRunChunks;
@@ -427,6 +460,8 @@ __device__ __forceinline__ void prefix_of_heads(const int32_t* heads, int runs, 
 // and add; lanes and tokens without a value load a valid one and store nothing.
 template <typename TIn, typename TOut, int kVec, int kCols, int kLanes>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
+  grid_dep_wait();
+  let_next_start();
   constexpr int kGroups = kSumThreads / kLanes;
   constexpr int kDepth = kCols > 1 ? 2 : 4;
   constexpr int kTileCols = kLanes * kVec * kCols;
@@ -623,6 +658,8 @@ __device__ __forceinline__ float4 sum_items(int64_t first, int64_t count, int st
 constexpr int kFoldThreads = 256;
 
 __global__ void __launch_bounds__(kFoldThreads) fold_kernel(SumArgs a) {
+  grid_dep_wait();
+  let_next_start();
   __shared__ float4 part[kFoldThreads / 32][32];
   const int64_t c0 = (int64_t)blockIdx.x * kFold;
   if (c0 == 0 || c0 + kFold > a.chunks) return;
@@ -672,6 +709,8 @@ constexpr int kJoinAlone = 32;  // parts that a warp sums by itself
 // together where the row has many parts.
 template <typename TOut>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(SumArgs a) {
+  grid_dep_wait();
+  let_next_start();
   __shared__ Parts all[kJoinWarps];
   __shared__ int64_t row_of[kJoinWarps];
   __shared__ float4 part[kJoinWarps][32];
@@ -741,7 +780,6 @@ constexpr int64_t kMaxTokens = 0x7fffffff;
 constexpr int64_t kMaxCells = 1ll << 40;
 constexpr int64_t kMaxDim = 1 << 22;  // its column tiles fit a grid's second dimension
 constexpr int kMaxChunks = 32768;
-constexpr int kMinChunk = 32;
 
 struct GradPlan {
   int64_t chunk, chunks;
@@ -775,7 +813,7 @@ GradPlan grad_plan(int64_t n, int64_t dim) {
 
 template <typename Id>
 cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, const GradPlan& p,
-                        int32_t* status, int device, cudaStream_t st, int* result) {
+                        int32_t* status, int32_t* heads, int device, cudaStream_t st, int* result) {
   int bits = 1;
   while ((1ll << bits) <= rows) ++bits;  // keys 0 .. rows
   const int passes = (int)ceil_div(bits, kMaxBits);
@@ -792,7 +830,8 @@ cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, con
     });
     if (e != cudaSuccess) return e;
     sort_small_kernel<Id><<<1, kSortThreads, kSmallSmem, st>>>(ids_src, (int)n, passes, pass_bits,
-                                                               keys(0), tokens(0));
+                                                               keys(0), tokens(0),
+                                                               (int32_t*)(ws + p.rank_of), heads);
     *result = 0;
     return cudaGetLastError();
   }
@@ -802,23 +841,30 @@ cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, con
   if (tiles < ctas) ctas = (int)tiles;
   int32_t* counts = (int32_t*)(ws + p.counts);
   int32_t* totals = (int32_t*)(ws + p.totals);
-  for (int pass = 0; pass < passes; ++pass) {
+  cudaError_t e = cudaSuccess;
+  for (int pass = 0; pass < passes && e == cudaSuccess; ++pass) {
     const int shift = pass * pass_bits, to = pass & 1;
     const FromPass from{keys(to ^ 1), tokens(to ^ 1)};
-    if (pass == 0)
+    if (pass == 0) {
+      // after whatever the caller's stream ran before
       sort_count_kernel<<<ctas, kSortThreads, 0, st>>>(ids_src, n, shift, digits, counts);
-    else
-      sort_count_kernel<<<ctas, kSortThreads, 0, st>>>(from, n, shift, digits, counts);
-    sort_scan_kernel<<<(digits + 7) / 8, 256, 0, st>>>(counts, ctas, digits, totals);
+      e = cudaGetLastError();
+    } else {
+      e = launch_next(sort_count_kernel<FromPass>, ctas, kSortThreads, 0, st, from, n, shift,
+                      digits, counts);
+    }
+    if (e == cudaSuccess)
+      e = launch_next(sort_scan_kernel, (digits + 7) / 8, 256, 0, st, counts, ctas, digits, totals);
+    if (e != cudaSuccess) break;
     if (pass == 0)
-      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(ids_src, n, shift, pass_bits, counts, totals,
-                                                       keys(to), tokens(to));
+      e = launch_next(sort_place_kernel<FromIds<Id>>, ctas, kSortThreads, 0, st, ids_src, n, shift,
+                      pass_bits, counts, totals, keys(to), tokens(to));
     else
-      sort_place_kernel<<<ctas, kSortThreads, 0, st>>>(from, n, shift, pass_bits, counts, totals,
-                                                       keys(to), tokens(to));
+      e = launch_next(sort_place_kernel<FromPass>, ctas, kSortThreads, 0, st, from, n, shift,
+                      pass_bits, counts, totals, keys(to), tokens(to));
     *result = to;
   }
-  return cudaGetLastError();
+  return e;
 }
 
 template <typename TIn, typename TOut, int kVec, int kCols, int kLanes>
@@ -829,18 +875,22 @@ cudaError_t launch_sum(SumArgs a, int32_t* heads, cudaStream_t st) {
   if (heads) {
     a.heads = heads;
     a.runs = (int32_t)ceil_div(a.chunks, kRunChunks);
-    count_heads_kernel<<<(unsigned)a.runs, 1024, 0, st>>>(a.keys, a.n, a.rows, a.chunk, a.chunks,
-                                                          a.rank_of, heads);
+    if (a.n > kSmallTile) {  // else the sort has counted them
+      const cudaError_t e = launch_next(count_heads_kernel, (unsigned)a.runs, 1024, 0, st, a.keys,
+                                        a.n, a.rows, a.chunk, a.chunks, a.rank_of, heads);
+      if (e != cudaSuccess) return e;
+    }
   }
-  sum_kernel<TIn, TOut, kVec, kCols, kLanes>
-      <<<dim3((unsigned)ctas, (unsigned)cols), kSumThreads, 0, st>>>(a);
+  cudaError_t e = launch_next(sum_kernel<TIn, TOut, kVec, kCols, kLanes>,
+                              dim3((unsigned)ctas, (unsigned)cols), kSumThreads, 0, st, a);
   const unsigned join_cols = (unsigned)ceil_div(a.dim, kJoinCols);
-  if (a.chunks > kFold)
-    fold_kernel<<<dim3((unsigned)(a.chunks / kFold), join_cols), kFoldThreads, 0, st>>>(a);
-  if (a.chunks > 1)
-    join_kernel<TOut><<<dim3((unsigned)ceil_div(a.chunks, kJoinWarps), join_cols), kJoinThreads, 0,
-                        st>>>(a);
-  return cudaGetLastError();
+  if (e == cudaSuccess && a.chunks > kFold)
+    e = launch_next(fold_kernel, dim3((unsigned)(a.chunks / kFold), join_cols), kFoldThreads, 0, st,
+                    a);
+  if (e == cudaSuccess && a.chunks > 1)
+    e = launch_next(join_kernel<TOut>, dim3((unsigned)ceil_div(a.chunks, kJoinWarps), join_cols),
+                    kJoinThreads, 0, st, a);
+  return e;
 }
 
 // A warp to a row where the row has 32 columns or more: half a warp to a row has
@@ -959,17 +1009,19 @@ agnes_status embedding_grad(const GradCall& c, bool compact) {
     return op_error(AGNES_EINVAL, "%s: a workspace of %lld bytes, %lld are needed", op,
                     (long long)c.workspace_bytes, (long long)p.bytes);
   uint8_t* ws = (uint8_t*)c.workspace;
+  int32_t* heads = compact ? (int32_t*)(ws + p.heads) : nullptr;
   int which = 0;
+  if (!compact) {  // before the kernels, which then follow one another
+    const cudaError_t e =
+        cudaMemsetAsync(c.out, 0, (size_t)(c.rows * c.dim * float_size(c.out_dtype)), c.st);
+    if (e != cudaSuccess) return op_launched(op, e);
+  }
   cudaError_t e = with_index_type(c.ids_bits, [&](auto id) {
     using Id = typename decltype(id)::type;
-    return sort_tokens((const Id*)c.ids, c.n, c.rows, ws, p, c.status, device, c.st,
+    return sort_tokens((const Id*)c.ids, c.n, c.rows, ws, p, c.status, heads, device, c.st,
                        &which);
   });
   if (e != cudaSuccess) return op_launched(op, e);
-  if (!compact) {
-    e = cudaMemsetAsync(c.out, 0, (size_t)(c.rows * c.dim * float_size(c.out_dtype)), c.st);
-    if (e != cudaSuccess) return op_launched(op, e);
-  }
   SumArgs a = {};
   a.keys = (const uint32_t*)(ws + p.keys[which]);
   a.tokens = (const int32_t*)(ws + p.tokens[which]);
@@ -988,7 +1040,6 @@ agnes_status embedding_grad(const GradCall& c, bool compact) {
   a.part_dim = (int32_t)(ceil_div(c.dim, 4) * 4);
   a.chunk = (int32_t)p.chunk;
   a.chunks = p.chunks;
-  int32_t* heads = compact ? (int32_t*)(ws + p.heads) : nullptr;
   e = with_float_type(c.grad_dtype, [&](auto tin) {
     return with_float_type(c.out_dtype, [&](auto tout) {
       using TIn = typename decltype(tin)::type;

@@ -106,6 +106,30 @@ inline bool aligned_rows(const void* p, int64_t stride_bytes, int64_t bytes) {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Launches a kernel whose predecessor on the stream is the kernel before it in the same
+// call, ahead of that one's completion: its CTAs are set up meanwhile and wait in
+// grid_dep_wait(), which has to be the kernel's first statement.
+template <typename... Params, typename... Args>
+cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem,
+                        cudaStream_t st, Args&&... args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
+// Lets the next kernel's CTAs be set up from here on.
+__device__ __forceinline__ void let_next_start() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // ---- argument checks (ops.cu); each records a message for
 // agnes_last_error(NULL) when it fails ----------------------------------------
 

@@ -177,14 +177,19 @@ def embedding_lookup(table, ids, scale: float = 1.0, out_dtype=None, out=None, s
     return y if out is not None or ids.ndim == 1 else y.view(*ids.shape, dim)
 
 
+@functools.lru_cache(maxsize=1024)
+def _grad_workspace(n, dim) -> int:
+    need = ctypes.c_int64()
+    _check(lib().agnes_embedding_grad_workspace(n, dim, ctypes.byref(need)))
+    return need.value
+
+
 def _grad_arguments(grad, ids):
     device, n, dim, step = _rows("grad", grad)
     bits = _ids("ids", ids, device)
     if ids.numel() != n:
         raise ValueError(f"{ids.numel()} ids for {n} rows of grad")
-    need = ctypes.c_int64()
-    _check(lib().agnes_embedding_grad_workspace(n, dim, ctypes.byref(need)))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+    ws = torch.empty(_grad_workspace(n, dim), dtype=torch.uint8, device=device)
     return device, n, dim, ws, (grad.data_ptr(), _FLOATS[grad.dtype], step, ids.data_ptr(), bits, n)
 
 

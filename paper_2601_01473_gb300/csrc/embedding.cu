@@ -66,12 +66,11 @@ lookup_kernel(const TIn* __restrict__ table, int64_t rows, int64_t table_stride,
 // in order.  Keys are ids in [0, rows), and `rows` for the tokens that select
 // none.
 
-constexpr int kSortThreads = 512;
+constexpr int kSortThreads = 256;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortItems = 4;
+constexpr int kSortItems = 8;
 constexpr int kSortTile = kSortThreads * kSortItems;
-constexpr int kSmallItems = 8;  // where one CTA sorts them all
-constexpr int kSmallTile = kSortThreads * kSmallItems;
+constexpr int kSmallTile = kSortThreads * 16;  // where one CTA sorts them all
 constexpr int kMaxBits = 9;
 constexpr int kMaxDigits = 1 << kMaxBits;
 constexpr int kSortMaxCtas = 608;
@@ -138,7 +137,11 @@ sort_count_kernel(Src src, int64_t n, int shift, int digits, int32_t* __restrict
 }
 
 // A warp per digit: its counts become their exclusive prefix over the CTAs, and
-// totals[digit] their sum.
+// totals[digit] their sum.  A lane takes neighbouring CTAs' counts, all on their way at
+// once.
+constexpr int kScanItems = kSortMaxCtas / 32;
+static_assert(kSortMaxCtas % 32 == 0, "whole lanes");
+
 __global__ void __launch_bounds__(256)
 sort_scan_kernel(int32_t* __restrict__ counts, int ctas, int digits, int32_t* __restrict__ totals) {
   grid_dep_wait();
@@ -146,36 +149,51 @@ sort_scan_kernel(int32_t* __restrict__ counts, int ctas, int digits, int32_t* __
   const int d = blockIdx.x * 8 + (threadIdx.x >> 5);
   if (d >= digits) return;
   int32_t* row = counts + (int64_t)d * ctas;
-  int32_t carry = 0;
-  for (int b = 0; b < ctas; b += 32) {
-    const int i = b + lane_id();
-    const int32_t v = i < ctas ? row[i] : 0;
-    const int32_t incl = warp_incl_scan(v);
-    if (i < ctas) row[i] = carry + incl - v;
-    carry += __shfl_sync(0xffffffffu, incl, 31);
+  const int per = (ctas + 31) / 32, first = lane_id() * per;
+  int32_t v[kScanItems], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kScanItems; ++j) v[j] = j < per && first + j < ctas ? row[first + j] : 0;
+#pragma unroll
+  for (int j = 0; j < kScanItems; ++j) sum += v[j];
+  const int32_t incl = warp_incl_scan(sum);
+  int32_t at = incl - sum;
+#pragma unroll
+  for (int j = 0; j < kScanItems; ++j) {
+    if (j < per && first + j < ctas) row[first + j] = at;
+    at += v[j];
   }
-  if (lane_id() == 0) totals[d] = carry;
+  if (lane_id() == 31) totals[d] = incl;
 }
 
-struct SortSmem {
+struct alignas(16) SortSmem {
   int32_t warp_hist[kSortWarps][kMaxDigits];
-  int32_t base[kMaxDigits];  // where the next token of each digit goes
+  int32_t base[kMaxDigits];   // where the next token of each digit goes
+  int32_t delta[kMaxDigits];  // from a token's place in its tile to where it goes
   int32_t warp_total[kSortWarps];
 };
 
-// base[d] = the exclusive prefix over the digits of total(d), plus extra(d).
+// base[d] = the exclusive prefix over the digits of total(d), plus extra(d).  A thread
+// has digits 2 t and 2 t + 1.
+constexpr int kThreadDigits = kMaxDigits / kSortThreads;
+static_assert(kThreadDigits == 2, "two digits to a thread");
+
 template <typename Total, typename Extra>
 __device__ __forceinline__ void digit_bases(SortSmem& s, int digits, Total total, Extra extra) {
-  const int d = threadIdx.x;  // kSortThreads >= kMaxDigits
-  const int32_t v = d < digits ? total(d) : 0;
-  const int32_t incl = warp_incl_scan(v);
-  if (lane_id() == 31) s.warp_total[d >> 5] = incl;
+  const int t = threadIdx.x, d = 2 * t;
+  const bool in = d < digits;  // an even number
+  const int32_t first = in ? total(d) : 0, second = in ? total(d + 1) : 0;
+  const int32_t more = in ? extra(d) : 0, more2 = in ? extra(d + 1) : 0;
+  const int32_t incl = warp_incl_scan(first + second);
+  if (lane_id() == 31) s.warp_total[t >> 5] = incl;
   __syncthreads();
-  int32_t before = 0;
-  for (int w = 0; w < d >> 5; ++w) before += s.warp_total[w];
-  if (d < digits) s.base[d] = before + incl - v + extra(d);
+  int32_t before = incl - first - second;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) before += w < t >> 5 ? s.warp_total[w] : 0;
+  if (in) {
+    s.base[d] = before + more;
+    s.base[d + 1] = before + first + more2;
+  }
 }
-static_assert(kSortThreads >= kMaxDigits, "a thread per digit");
 
 // The lanes with this lane's digit, by a ballot for each of its bits.
 __device__ __forceinline__ unsigned same_digit(int digit, int bits) {
@@ -188,15 +206,17 @@ __device__ __forceinline__ unsigned same_digit(int digit, int bits) {
   return peers;
 }
 
-// The places of a tile's tokens, in order: warp w holds tokens w * 32 * kItems +
-// u * 32 + lane.  s.base moves on by the tile's counts.  All threads take part; a
+// The places of a tile's tokens among themselves, sorted by digit, in order: warp w
+// holds tokens w * 32 * kItems + u * 32 + lane.  s.delta: what leads from there to where
+// the digit's tokens go; s.base moves on by the tile's counts.  All threads take part; a
 // token out of the run has digit -1.
 template <int kItems>
 __device__ __forceinline__ void tile_places(SortSmem& s, int bits, const int (&digit)[kItems],
                                             int32_t (&place)[kItems]) {
   const int warp = threadIdx.x >> 5, digits = 1 << bits;
-  if (threadIdx.x < digits)
-    for (int w = 0; w < kSortWarps; ++w) s.warp_hist[w][threadIdx.x] = 0;
+  for (int d = threadIdx.x; d < digits; d += kSortThreads)
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) s.warp_hist[w][d] = 0;
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < kItems; ++u) {
@@ -210,15 +230,34 @@ __device__ __forceinline__ void tile_places(SortSmem& s, int bits, const int (&d
     __syncwarp();
   }
   __syncthreads();
-  const int d = threadIdx.x;
-  if (d < digits) {
-    int32_t at = s.base[d];
+  const int d = 2 * threadIdx.x;
+  const bool in = d < digits;  // an even number
+  int2 c[kSortWarps], sum = make_int2(0, 0);
+  if (in) {
+#pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      const int32_t c = s.warp_hist[w][d];
-      s.warp_hist[w][d] = at;
-      at += c;
+      c[w] = *(const int2*)&s.warp_hist[w][d];
+      sum.x += c[w].x;
+      sum.y += c[w].y;
     }
-    s.base[d] = at;
+  }
+  const int32_t incl = warp_incl_scan(sum.x + sum.y);
+  if (lane_id() == 31) s.warp_total[warp] = incl;
+  __syncthreads();
+  int32_t before = incl - sum.x - sum.y;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) before += w < warp ? s.warp_total[w] : 0;
+  if (in) {
+    int2 at = make_int2(before, before + sum.x);
+    const int2 base = *(const int2*)&s.base[d];
+    *(int2*)&s.delta[d] = make_int2(base.x - at.x, base.y - at.y);
+    *(int2*)&s.base[d] = make_int2(base.x + sum.x, base.y + sum.y);
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+      *(int2*)&s.warp_hist[w][d] = at;
+      at.x += c[w].x;
+      at.y += c[w].y;
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -234,6 +273,9 @@ sort_place_kernel(Src src, int64_t n, int shift, int bits, const int32_t* __rest
   grid_dep_wait();
   let_next_start();
   __shared__ SortSmem s;
+  // a tile's tokens in the order of their digits, so that those of one digit are stored
+  // side by side
+  __shared__ uint2 sorted[kSortTile];
   const int digits = 1 << bits;
   digit_bases(s, digits, [&](int d) { return totals[d]; },
               [&](int d) { return counts[(int64_t)d * gridDim.x + blockIdx.x]; });
@@ -254,10 +296,15 @@ sort_place_kernel(Src src, int64_t n, int shift, int bits, const int32_t* __rest
     __syncthreads();  // the bases, and the last tile's places, have been read
     tile_places(s, bits, digit, place);
 #pragma unroll
-    for (int u = 0; u < kSortItems; ++u) {
-      if (digit[u] < 0) continue;
-      keys[place[u]] = key[u];
-      tokens[place[u]] = token[u];
+    for (int u = 0; u < kSortItems; ++u)
+      if (digit[u] >= 0) sorted[place[u]] = make_uint2(key[u], (uint32_t)token[u]);
+    __syncthreads();
+    const int count = (int)min((int64_t)kSortTile, run.end - base);
+    for (int i = threadIdx.x; i < count; i += kSortThreads) {
+      const uint2 e = sorted[i];
+      const int32_t to = i + s.delta[(e.x >> shift) & (uint32_t)(digits - 1)];
+      keys[to] = e.x;
+      tokens[to] = (int32_t)e.y;
     }
   }
 }
@@ -268,7 +315,7 @@ static_assert(kSmallTile <= kMinChunk * kRunChunks, "the small sort's tokens are
 
 // Up to kSmallTile tokens in one CTA, every pass in shared memory; with rank_of and
 // heads, what count_heads_kernel finds, too (chunks of kMinChunk tokens, one run).
-template <typename Id>
+template <typename Id, int kSmallItems>
 __global__ void __launch_bounds__(kSortThreads)
 sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __restrict__ keys,
                   int32_t* __restrict__ tokens, int32_t* __restrict__ rank_of,
@@ -279,6 +326,7 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
   int32_t* stoken = (int32_t*)(skey + kSmallTile);
   const int first = (threadIdx.x >> 5) * 32 * kSmallItems + lane_id();
   const int digits = 1 << bits;
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) s.base[d] = 0;
   uint32_t key[kSmallItems];
   int32_t token[kSmallItems], place[kSmallItems];
 #pragma unroll
@@ -292,21 +340,12 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
 #pragma unroll
     for (int u = 0; u < kSmallItems; ++u)
       digit[u] = first + u * 32 < n ? (int)(key[u] >> (p * bits)) & (digits - 1) : -1;
-    // the digits' totals: counted with base = 0, then placed
-    if (threadIdx.x < digits) s.base[threadIdx.x] = 0;
-    __syncthreads();
-    tile_places(s, bits, digit, place);  // ends with base[d] = the digit's count
-    __syncthreads();
-    const int32_t count = threadIdx.x < digits ? s.base[threadIdx.x] : 0;
-    __syncthreads();
-    digit_bases(s, digits, [&](int) { return count; }, [](int) { return 0; });
-    __syncthreads();
+    tile_places(s, bits, digit, place);
 #pragma unroll
     for (int u = 0; u < kSmallItems; ++u) {
       if (digit[u] < 0) continue;
-      const int32_t at = s.base[digit[u]] + place[u];
-      skey[at] = key[u];
-      stoken[at] = token[u];
+      skey[place[u]] = key[u];
+      stoken[place[u]] = token[u];
     }
     __syncthreads();
 #pragma unroll
@@ -355,6 +394,7 @@ constexpr size_t kSmallSmem = sizeof(SortSmem) + 8 * kSmallTile;
 
 constexpr int kSumThreads = 256;
 constexpr uint32_t kPastChunk = 0xffffffffu;  // no id
+constexpr int32_t kNoPart = -1, kAllOfIt = -2;  // instead of a row
 
 // rank_of[c] = the number of distinct ids that begin in the chunks of c's run before
 // c; heads[r] = those that begin in run r.  A warp to a chunk.
@@ -406,9 +446,9 @@ struct SumArgs {
   int32_t runs;
   int32_t* out_ids;
   int32_t* count;
-  // per chunk: ids that begin in its run before it; then, which row of `out` its
-  // part 1 belongs to
-  int32_t* rank_of;
+  int32_t* rank_of;  // per chunk: ids that begin in its run before it
+  // per chunk: which row of `out` its part 1 belongs to, kNoPart, or kAllOfIt where the
+  // whole chunk is in the middle of a row
   int32_t* row_of;
   // a chunk's part of the row that it begins within (which = 0) and of the row that
   // it ends within (1): partial[(2 * chunk + which) * part_dim ..]
@@ -518,7 +558,13 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
   }
   if (lo >= hi) return;
   uint32_t key = __shfl_sync(lanes, held_key, 0, kLanes);
-  if (key >= a.rows) return;  // padding only
+  const auto leave = [&](int32_t what) {
+    if (blockIdx.y == 0 && lane == 0) a.row_of[chunk] = what;
+  };
+  if (key >= a.rows) {  // padding only
+    leave(kNoPart);
+    return;
+  }
   const bool goes_on = hi < a.n && a.keys[hi] == a.keys[hi - 1];  // past the chunk
   bool spans = lo > 0 && a.keys[lo - 1] == key;  // the current row began in an earlier chunk
 
@@ -603,7 +649,10 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
         spans = false;
         clear();
         key = __shfl_sync(lanes, held_key, at0 + d, kLanes);
-        if (key >= a.rows) return;  // the rest is padding
+        if (key >= a.rows) {  // the rest is padding
+          leave(kNoPart);
+          return;
+        }
         row = a.heads ? rank : key;
         ++rank;
       }
@@ -616,12 +665,11 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a) {
   }
   if (spans)
     put_part(0);
-  else if (!goes_on)
-    put_row(row);
-  else {
+  else if (goes_on)
     put_part(1);
-    if (a.heads && blockIdx.y == 0 && lane == 0) a.row_of[chunk] = (int32_t)row;
-  }
+  else
+    put_row(row);
+  leave(!goes_on ? kNoPart : spans ? kAllOfIt : (int32_t)row);
 }
 
 // Rows that span chunks.  Such a row has part 1 of the chunk in which it begins and
@@ -725,32 +773,21 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(SumArgs a) {
   };
   int64_t many = -1;  // the row, where the CTA sums it
   Parts parts;
-  if (chunk + 1 < a.chunks) {  // the last chunk's rows end in it
-    const int64_t lo = chunk * a.chunk, hi = lo + a.chunk;
-    const uint32_t key = a.keys[hi - 1];
-    if (key < a.rows && a.keys[hi] == key && !(lo > 0 && a.keys[lo - 1] == key)) {
-      // the last chunk that begins with the key: most rows end in the next one
-      int64_t last = chunk + 1, end = chunk + 2;
-      while (end < a.chunks && a.first_key(end) == key) {
-        last = end;
-        end = last + 2 * (last - chunk);
-      }
-      if (end > a.chunks) end = a.chunks;
-      while (end - last > 1) {
-        const int64_t mid = (last + end) / 2;
-        if (a.first_key(mid) == key)
-          last = mid;
-        else
-          end = mid;
-      }
-      const int64_t row = a.heads ? (int64_t)a.row_of[chunk] : (int64_t)key;
-      parts = Parts(chunk, last);
-      if (parts.count > kJoinAlone) {
-        many = row;
-      } else if (col < a.part_dim) {
-        put(row, sum_items(0, parts.count, 1, [&](int64_t i) { return parts.at(a, i) + col; }));
-      }
+  const int32_t row = chunk < a.chunks ? a.row_of[chunk] : kNoPart;
+  if (row >= 0) {
+    // the last chunk of the row: the first after this one that it does not fill
+    int64_t last = chunk + 1;
+    unsigned ends = 0;
+    for (; !ends; last += 32) {
+      const int64_t c = last + lane;
+      ends = __ballot_sync(0xffffffffu, c >= a.chunks || a.row_of[c] != kAllOfIt);
     }
+    last += __ffs(ends) - 33;
+    parts = Parts(chunk, last);
+    if (parts.count > kJoinAlone)
+      many = row;
+    else if (col < a.part_dim)
+      put(row, sum_items(0, parts.count, 1, [&](int64_t i) { return parts.at(a, i) + col; }));
   }
   if (lane == 0) {
     row_of[warp] = many;
@@ -823,17 +860,23 @@ cudaError_t sort_tokens(const Id* ids, int64_t n, int64_t rows, uint8_t* ws, con
   const auto keys = [&](int i) { return (uint32_t*)(ws + p.keys[i]); };
   const auto tokens = [&](int i) { return (int32_t*)(ws + p.tokens[i]); };
   if (n <= kSmallTile) {
-    static OncePerDevice once;
-    const cudaError_t e = once.run(device, [] {
-      return cudaFuncSetAttribute(sort_small_kernel<Id>,
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
-    });
-    if (e != cudaSuccess) return e;
-    sort_small_kernel<Id><<<1, kSortThreads, kSmallSmem, st>>>(ids_src, (int)n, passes, pass_bits,
-                                                               keys(0), tokens(0),
-                                                               (int32_t*)(ws + p.rank_of), heads);
+    const auto run = [&](auto items) {
+      constexpr int kItems = decltype(items)::value;
+      static OncePerDevice once;
+      const cudaError_t e = once.run(device, [] {
+        return cudaFuncSetAttribute(sort_small_kernel<Id, kItems>,
+                                    cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
+      });
+      if (e != cudaSuccess) return e;
+      sort_small_kernel<Id, kItems><<<1, kSortThreads, kSmallSmem, st>>>(
+          ids_src, (int)n, passes, pass_bits, keys(0), tokens(0), (int32_t*)(ws + p.rank_of),
+          heads);
+      return cudaGetLastError();
+    };
     *result = 0;
-    return cudaGetLastError();
+    if (n <= 4 * kSortThreads) return run(std::integral_constant<int, 4>());
+    if (n <= 8 * kSortThreads) return run(std::integral_constant<int, 8>());
+    return run(std::integral_constant<int, 16>());
   }
   const int64_t tiles = ceil_div(n, kSortTile);
   const int num_sms = op_num_sms(device);

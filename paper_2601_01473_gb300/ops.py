@@ -36,26 +36,21 @@ class RowGrad(NamedTuple):
     count: torch.Tensor  # int32 [1]: how many
 
 
-def _streamed(op):
-    @functools.wraps(op)
-    def call(*args, stream=None, **kw):
-        if stream is None:
-            return op(*args, **kw)
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream))
-        with torch.cuda.stream(stream):
-            result = op(*args, **kw)
-        for t in (*args, *kw.values()):
-            if isinstance(t, torch.Tensor) and t.is_cuda:
-                t.record_stream(stream)
-        return result
-    return call
+def _on_stream(stream, op, *args):
+    """op(*args) with ``stream`` current."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(stream):
+        result = op(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            t.record_stream(stream)
+    return result
 
 
-def _check(rc: int) -> None:
-    if rc != 0:
-        msg = lib().agnes_last_error(None)
-        raise AgnesError(rc, msg.decode() if msg else "")
+def _failed(rc: int):
+    msg = lib().agnes_last_error(None)
+    raise AgnesError(rc, msg.decode() if msg else "")
 
 
 def _stream(device) -> int | None:
@@ -116,7 +111,9 @@ def _rows(name: str, t: torch.Tensor, device=None):
         step = dim  # there is no next row
     if (unit != 1 and dim > 1 or step < dim) and n and dim:
         raise ValueError(f"{name} must have adjacent elements in each row")
-    return _on(name, t, device), n, dim, step
+    if device is not None or not t.is_cuda:
+        return _on(name, t, device), n, dim, step
+    return t.device, n, dim, step
 
 
 def _on(name: str, t: torch.Tensor, device):
@@ -159,28 +156,34 @@ def _output(out, n, dim, dtype, device):
 # ---- embeddings -------------------------------------------------------------------------
 
 
-@_streamed
-def embedding_lookup(table, ids, scale: float = 1.0, out_dtype=None, out=None, status=None):
+def embedding_lookup(table, ids, scale: float = 1.0, out_dtype=None, out=None, status=None,
+                     stream=None):
     """``scale * table[ids]`` (agnes_embedding_lookup): the rows of ``table``
     [rows, dim] for ``ids`` of any shape, as [*ids.shape, dim] of ``out_dtype`` (the
     table's by default).  A negative id gives zeros.  ``out``: [ids.numel(), dim],
     its rows adjacent or not, written instead of a new tensor and returned."""
+    if stream is not None:
+        return _on_stream(stream, embedding_lookup, table, ids, scale, out_dtype, out, status)
     device, rows, dim, step = _rows("table", table)
     bits = _ids("ids", ids, device)
     n = ids.numel()
     if out is None and out_dtype is None:
         out_dtype = table.dtype
     y, code, out_step = _output(out, n, dim, out_dtype, device)
-    _check(lib().agnes_embedding_lookup(
+    rc = lib().agnes_embedding_lookup(
         table.data_ptr(), _FLOATS[table.dtype], rows, step, dim, ids.data_ptr(), bits, n, scale,
-        y.data_ptr(), code, out_step, _status_word(status, device), _stream(device)))
+        y.data_ptr(), code, out_step, _status_word(status, device), _stream(device))
+    if rc:
+        _failed(rc)
     return y if out is not None or ids.ndim == 1 else y.view(*ids.shape, dim)
 
 
 @functools.lru_cache(maxsize=1024)
 def _grad_workspace(n, dim) -> int:
     need = ctypes.c_int64()
-    _check(lib().agnes_embedding_grad_workspace(n, dim, ctypes.byref(need)))
+    rc = lib().agnes_embedding_grad_workspace(n, dim, ctypes.byref(need))
+    if rc:
+        _failed(rc)
     return need.value
 
 
@@ -193,40 +196,48 @@ def _grad_arguments(grad, ids):
     return device, n, dim, ws, (grad.data_ptr(), _FLOATS[grad.dtype], step, ids.data_ptr(), bits, n)
 
 
-@_streamed
 def embedding_grad(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=None, out=None,
-                   status=None):
+                   status=None, stream=None):
     """The gradient of ``embedding_lookup`` to the whole table (agnes_embedding_grad):
     [num_rows, dim] of ``out_dtype`` (grad's by default), row v the scaled sum of the
     rows of ``grad`` [n, dim] whose id (``ids``, n of any shape) is v, zeros where
     there is none.  ``out``: written instead of a new tensor; contiguous."""
+    if stream is not None:
+        return _on_stream(stream, embedding_grad, grad, ids, num_rows, scale, out_dtype, out,
+                          status)
     device, n, dim, ws, arguments = _grad_arguments(grad, ids)
     if out is None and out_dtype is None:
         out_dtype = grad.dtype
     y, code, step = _output(out, num_rows, dim, out_dtype, device)
     if step != dim:
         raise ValueError("out must be contiguous")
-    _check(lib().agnes_embedding_grad(
+    rc = lib().agnes_embedding_grad(
         *arguments, num_rows, dim, scale, y.data_ptr(), code, ws.data_ptr(), ws.numel(),
-        _status_word(status, device), _stream(device)))
+        _status_word(status, device), _stream(device))
+    if rc:
+        _failed(rc)
     return y
 
 
-@_streamed
-def embedding_grad_rows(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=None,
-                        status=None) -> RowGrad:
+def embedding_grad_rows(grad, ids, num_rows: int, scale: float = 1.0, out_dtype=None, status=None,
+                        stream=None) -> RowGrad:
     """The same gradient for the selected rows only (agnes_embedding_grad_rows), for
     tables too large for a dense one.  Its shapes do not depend on the ids, so
     ``table.index_add_(0, g.ids.clamp(min=0), g.rows, alpha=-lr)`` needs no read-back:
     the rows past ``count`` are zeros."""
+    if stream is not None:
+        return _on_stream(stream, embedding_grad_rows, grad, ids, num_rows, scale, out_dtype,
+                          status)
     device, n, dim, ws, arguments = _grad_arguments(grad, ids)
     rows, code, _ = _output(None, n, dim, out_dtype or grad.dtype, device)
     out_ids = torch.empty(n, dtype=torch.int32, device=device)
     count = torch.empty(1, dtype=torch.int32, device=device)
-    _check(lib().agnes_embedding_grad_rows(
+    rc = lib().agnes_embedding_grad_rows(
         *arguments, num_rows, dim, scale, out_ids.data_ptr(), rows.data_ptr(), code,
         count.data_ptr(), ws.data_ptr(), ws.numel(), _status_word(status, device),
-        _stream(device)))
+        _stream(device))
+    if rc:
+        _failed(rc)
     return RowGrad(out_ids, rows, count)
 
 
@@ -256,27 +267,32 @@ def _weight_arguments(weight, rows, device):
     return weight.data_ptr(), 1.0
 
 
-@_streamed
-def distill_loss(logits, teacher, index, temperature: float = 1.0, status=None):
+def distill_loss(logits, teacher, index, temperature: float = 1.0, status=None, stream=None):
     """Each row's loss against the teacher's top logits (agnes_distill_loss):
     ``logits`` [rows, classes], ``teacher`` [rows, top] with their classes ``index``
     (negative: absent).  Returns (loss float32 [rows], stats float32 [rows, 2]);
     ``distill_grad`` takes the stats."""
+    if stream is not None:
+        return _on_stream(stream, distill_loss, logits, teacher, index, temperature, status)
     device, n, _, arguments = _distill_arguments(logits, teacher, index)
     loss = torch.empty(n, dtype=torch.float32, device=device)
     stats = torch.empty((n, 2), dtype=torch.float32, device=device)
-    _check(lib().agnes_distill_loss(*arguments, temperature, loss.data_ptr(), stats.data_ptr(),
-                                    _status_word(status, device), _stream(device)))
+    rc = lib().agnes_distill_loss(*arguments, temperature, loss.data_ptr(), stats.data_ptr(),
+                                  _status_word(status, device), _stream(device))
+    if rc:
+        _failed(rc)
     return loss, stats
 
 
-@_streamed
 def distill_grad(logits, teacher, index, stats, weight=1.0, temperature: float = 1.0,
-                 out_dtype=None, out=None, status=None):
+                 out_dtype=None, out=None, status=None, stream=None):
     """The gradient of sum(weight * loss) to the logits (agnes_distill_grad):
     ``weight`` a number or float32 [rows], ``stats`` from ``distill_loss``.  ``out``:
     written instead of a new tensor of ``out_dtype`` (the logits' by default); it may
     be ``logits``."""
+    if stream is not None:
+        return _on_stream(stream, distill_grad, logits, teacher, index, stats, weight,
+                          temperature, out_dtype, out, status)
     device, n, classes, arguments = _distill_arguments(logits, teacher, index)
     if stats.dtype != torch.float32 or stats.shape != (n, 2) or not stats.is_contiguous():
         raise TypeError("stats must be what distill_loss returned")
@@ -285,26 +301,32 @@ def distill_grad(logits, teacher, index, stats, weight=1.0, temperature: float =
     if out is None and out_dtype is None:
         out_dtype = logits.dtype
     y, code, step = _output(out, n, classes, out_dtype, device)
-    _check(lib().agnes_distill_grad(*arguments, temperature, stats.data_ptr(), w, w_scale,
-                                    y.data_ptr(), code, step, _status_word(status, device),
-                                    _stream(device)))
+    rc = lib().agnes_distill_grad(*arguments, temperature, stats.data_ptr(), w, w_scale,
+                                  y.data_ptr(), code, step, _status_word(status, device),
+                                  _stream(device))
+    if rc:
+        _failed(rc)
     return y
 
 
-@_streamed
-def distill_loss_grad(logits, teacher, index, weight=1.0, temperature: float = 1.0,
-                      out_dtype=None, out=None, status=None):
+def distill_loss_grad(logits, teacher, index, weight=1.0, temperature: float = 1.0, out_dtype=None,
+                      out=None, status=None, stream=None):
     """(loss, gradient) in one call, the logits read once (agnes_distill_loss_grad);
     arguments as for ``distill_loss`` and ``distill_grad``."""
+    if stream is not None:
+        return _on_stream(stream, distill_loss_grad, logits, teacher, index, weight, temperature,
+                          out_dtype, out, status)
     device, n, classes, arguments = _distill_arguments(logits, teacher, index)
     w, w_scale = _weight_arguments(weight, n, device)
     loss = torch.empty(n, dtype=torch.float32, device=device)
     if out is None and out_dtype is None:
         out_dtype = logits.dtype
     y, code, step = _output(out, n, classes, out_dtype, device)
-    _check(lib().agnes_distill_loss_grad(*arguments, temperature, w, w_scale, loss.data_ptr(),
-                                         y.data_ptr(), code, step, _status_word(status, device),
-                                         _stream(device)))
+    rc = lib().agnes_distill_loss_grad(*arguments, temperature, w, w_scale, loss.data_ptr(),
+                                       y.data_ptr(), code, step, _status_word(status, device),
+                                       _stream(device))
+    if rc:
+        _failed(rc)
     return loss, y
 
 
@@ -314,7 +336,9 @@ def distill_loss_grad(logits, teacher, index, weight=1.0, temperature: float = 1
 def mx4_row_bytes(dim: int) -> int:
     """Bytes of a 4-bit row of ``dim`` values (agnes_mx4_row_bytes)."""
     need = ctypes.c_int64()
-    _check(lib().agnes_mx4_row_bytes(dim, ctypes.byref(need)))
+    rc = lib().agnes_mx4_row_bytes(dim, ctypes.byref(need))
+    if rc:
+        _failed(rc)
     return need.value
 
 
@@ -337,11 +361,12 @@ def _packed(name, t, dim, device=None):
     return _on(name, t, device), n, step * size
 
 
-@_streamed
-def mx4_quantize(x, out=None):
+def mx4_quantize(x, out=None, stream=None):
     """Rows of ``x`` [rows, dim] rounded to microscaled 4-bit rows (agnes_mx4_quantize):
     uint8 [rows, mx4_row_bytes(dim)].  ``.view(torch.float16)`` of them makes a graph's
     features."""
+    if stream is not None:
+        return _on_stream(stream, mx4_quantize, x, out)
     device, rows, dim, step = _rows("x", x)
     if out is None:
         out_step = mx4_row_bytes(dim)
@@ -350,26 +375,33 @@ def mx4_quantize(x, out=None):
         _, n, out_step = _packed("out", out, dim, device)
         if n != rows:
             raise ValueError(f"out has {n} rows, not {rows}")
-    _check(lib().agnes_mx4_quantize(x.data_ptr(), _FLOATS[x.dtype], step, rows, dim,
-                                    out.data_ptr(), out_step, _stream(device)))
+    rc = lib().agnes_mx4_quantize(x.data_ptr(), _FLOATS[x.dtype], step, rows, dim,
+                                  out.data_ptr(), out_step, _stream(device))
+    if rc:
+        _failed(rc)
     return out
 
 
-@_streamed
-def mx4_dequantize(x, dim: int, out_dtype=torch.float32, out=None):
+def mx4_dequantize(x, dim: int, out_dtype=torch.float32, out=None, stream=None):
     """The values [rows, dim] that 4-bit rows stand for (agnes_mx4_dequantize)."""
+    if stream is not None:
+        return _on_stream(stream, mx4_dequantize, x, dim, out_dtype, out)
     device, rows, step = _packed("x", x, dim)
     y, code, out_step = _output(out, rows, dim, out_dtype if out is None else None, device)
-    _check(lib().agnes_mx4_dequantize(x.data_ptr(), step, rows, dim, y.data_ptr(), code, out_step,
-                                      _stream(device)))
+    rc = lib().agnes_mx4_dequantize(x.data_ptr(), step, rows, dim, y.data_ptr(), code, out_step,
+                                    _stream(device))
+    if rc:
+        _failed(rc)
     return y
 
 
-@_streamed
-def mx4_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, status=None):
+def mx4_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, status=None,
+               stream=None):
     """``x @ w.T + bias`` of 4-bit rows (agnes_mx4_linear): ``x`` [rows, bytes], for example a
     minibatch's gathered features, ``w`` [width, bytes], both of ``dim`` values a row;
     ``bias`` float32 [width] or None.  Returns [rows, width]."""
+    if stream is not None:
+        return _on_stream(stream, mx4_linear, x, w, dim, bias, out_dtype, out, status)
     device, rows, step = _packed("x", x, dim)
     _, width, w_step = _packed("w", w, dim, device)
     at = None
@@ -379,7 +411,9 @@ def mx4_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, sta
         _on("bias", bias, device)
         at = bias.data_ptr()
     y, code, out_step = _output(out, rows, width, out_dtype if out is None else None, device)
-    _check(lib().agnes_mx4_linear(x.data_ptr(), step, rows, w.data_ptr(), w_step, width, dim, at,
-                                  y.data_ptr(), code, out_step, _status_word(status, device),
-                                  _stream(device)))
+    rc = lib().agnes_mx4_linear(x.data_ptr(), step, rows, w.data_ptr(), w_step, width, dim, at,
+                                y.data_ptr(), code, out_step, _status_word(status, device),
+                                _stream(device))
+    if rc:
+        _failed(rc)
     return y

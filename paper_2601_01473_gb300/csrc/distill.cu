@@ -251,14 +251,16 @@ __device__ __forceinline__ bool repeated(const DistillArgs& a, const Entries& s,
   return __any_sync(0xffffffffu, twice);
 }
 
-// A warp: the row's loss.
-__device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& s, MaxSum q) {
+// A warp: the row's loss.  logit(k): the student's logit at entry k's class.
+template <typename Logit>
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& s, MaxSum q,
+                                          Logit logit) {
   const float inv_t = 1.f / a.temperature, log_s = logf(q.s);
   float sum = 0.f;
   for (int k = lane_id(); k < a.top; k += 32) {
     const float p = s.p[k];
     if (p != 0.f && s.index[k] >= 0)
-      sum += p * (logf(p) - ((s.x[k] - q.m) * inv_t - log_s));
+      sum += p * (logf(p) - ((logit(k) - q.m) * inv_t - log_s));
   }
   return warp_sum(sum) * a.temperature * a.temperature;
 }
@@ -480,6 +482,7 @@ distill_kernel(DistillArgs a) {
     __syncthreads();
   }
   const Entries entries = {s.p, s.index, s.x};
+  const bool whole = a.keep && ranks == 1;  // the whole row is kept
   MaxSum q = {kNegInf, 0.f};
   if (tid >= readers) {
     const int lane = tid - readers;
@@ -488,8 +491,8 @@ distill_kernel(DistillArgs a) {
       if (kMode == kGrad) s.stats = a.stats[row];
     }
     // the logits of all classes for the loss, else of this slice (others' may be
-    // overwritten) unless it is kept
-    const bool all = kMode != kGrad && rank == 0;
+    // overwritten); none that are kept
+    const bool all = kMode != kGrad && rank == 0 && !whole;
     const float mass = teacher_row(a, row, x_row, all ? 0 : v0,
                                    all ? a.classes : a.keep ? v0 : v0 + n, entries);
     const bool twice = kMode != kLoss && repeated(a, entries, s.table, table_slots(a.top));
@@ -521,7 +524,12 @@ distill_kernel(DistillArgs a) {
     }
     if (rank == 0 && tid >= readers) {
       const bool some = s.mass != 0.f && q.s != 0.f;  // s = 0: every logit is -inf
-      const float loss = some ? row_loss(a, entries, q) : 0.f;
+      const float loss =
+          some ? row_loss(a, entries, q,
+                          [&](int k) {
+                            return whole ? to_f32(kept[cut.shift + s.index[k]]) : s.x[k];
+                          })
+               : 0.f;
       if (tid == readers) {
         a.loss[row] = loss;
         if (kMode == kLoss) a.stats[row] = make_float2(q.m, q.s);
@@ -572,7 +580,8 @@ __global__ void __launch_bounds__(32 * kShortWarps) distill_short_kernel(Distill
   const bool zero = mass == 0.f || q.s == 0.f;
   __syncwarp();
   if (kMode != kGrad) {
-    const float loss = zero ? 0.f : row_loss(a, entries, q);
+    const float loss =
+        zero ? 0.f : row_loss(a, entries, q, [&](int k) { return entries.x[k]; });
     if (lane == 0) {
       a.loss[row] = loss;
       if (kMode == kLoss) a.stats[row] = make_float2(q.m, q.s);

@@ -318,3 +318,26 @@ def test_refusals_on_the_device(cuda_device):
     with pytest.raises(TypeError, match="out"):
         ops.distill_loss_grad(x, t, at, out=torch.zeros(2, 5, device=cuda_device),
                               out_dtype=torch.float16)
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits(cuda_device):
+    R, V, K = 60_000, 50_000, 4  # 3e9 logits
+    x = torch.zeros(R, V, dtype=torch.float16, device=cuda_device)
+    part, t, at, w = _case(5, V, K, torch.float16, torch.float32, 31)
+    rows = torch.tensor([0, 1, 42_949, 42_950, R - 1], device=cuda_device)
+    x[rows] = part.to(cuda_device)
+    teacher = torch.zeros(R, K, device=cuda_device)
+    index = torch.full((R, K), -1, dtype=torch.int32, device=cuda_device)
+    weight = torch.ones(R, device=cuda_device)
+    teacher[rows], index[rows], weight[rows] = (v.to(cuda_device) for v in (t, at, w))
+    ref_loss, ref_grad, loss_bound, grad_bound = _reference(part, t, at, 2.0, w)
+    bound = grad_bound + 1.01 * rounding(ref_grad.abs() + grad_bound, x.dtype)
+    _, stats = ops.distill_loss(x, teacher, index, 2.0)
+    grad = ops.distill_grad(x, teacher, index, stats, weight, 2.0)
+    assert_within(grad[rows], ref_grad, bound)
+    del grad
+    loss, grad = ops.distill_loss_grad(x, teacher, index, weight, 2.0, out=x)  # in place
+    assert_within(loss[rows], ref_loss, loss_bound)
+    assert_within(grad[rows], ref_grad, bound)
+    assert (loss.sum() - loss[rows].sum()).abs() == 0

@@ -314,3 +314,31 @@ def test_refusals_on_the_device(cuda_device):
     with pytest.raises(ValueError, match="contiguous"):
         ops.embedding_grad(torch.zeros(4, 8, device=cuda_device), ids, 10,
                            out=torch.zeros(10, 16, device=cuda_device)[:, :8])
+
+
+@pytest.mark.gpu
+def test_gradient_offsets_past_32_bits(cuda_device):
+    rows, dim, n = 20_000_000, 128, 40_000  # 2.6e9 values of the dense gradient
+    grad, ids = _case(n, rows, dim, torch.float16, 1, 6)
+    ids[:3] = torch.tensor([0, rows - 1, 16_777_217])
+    d = ops.embedding_grad(grad.to(cuda_device), ids.to(cuda_device), rows)
+    r = ops.embedding_grad_rows(grad.to(cuda_device), ids.to(cuda_device), rows)
+    c = int(r.count)
+    assert torch.equal(d[r.ids[:c].long()], r.rows[:c])
+    assert int((d != 0).any(1).sum()) == c
+    where = int((r.ids[:c] == rows - 1).nonzero())
+    mine = grad[ids == rows - 1].double().sum(0)
+    assert_within(r.rows[where], mine, rounding(mine, torch.float16) + n * U32)
+
+
+@pytest.mark.gpu
+def test_a_gradient_with_more_rows_than_an_index_of_elements(cuda_device):
+    n, dim = 18_000_000, 128  # 2.3e9 values of the tokens' gradients
+    grad = torch.zeros(n, dim, dtype=torch.float16, device=cuda_device)
+    grad[-1], grad[0], grad[16_777_216] = 3, 5, 7
+    ids = torch.zeros(n, dtype=torch.int32, device=cuda_device)
+    ids[n // 2:] = 9
+    d = ops.embedding_grad(grad, ids, 10, out_dtype=torch.float32)
+    want = torch.zeros(10, dim)
+    want[0], want[9] = 5, 10
+    assert torch.equal(d.cpu(), want)

@@ -296,3 +296,38 @@ def test_product_of_a_ragged_last_tile_each_time(cuda_device, out):
         ops.mx4_linear(x, w, dim, b, out=got)
         differ += (got != first).sum()
     assert int(differ) == 0
+
+
+@pytest.mark.gpu
+def test_products_on_two_streams_at_once(cuda_device):
+    """Kernels that each want all of an SM's tensor memory, side by side."""
+    cases = []
+    for seed, (rows, width, dim) in enumerate([(40_000, 256, 128), (9000, 500, 640)]):
+        x = ops.mx4_quantize(_values(rows, dim, seed).to(cuda_device))
+        w = ops.mx4_quantize(_values(width, dim, seed + 9).to(cuda_device))
+        cases.append((x, w, dim, ops.mx4_linear(x, w, dim), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [[ops.mx4_linear(x, w, dim, stream=stream) for x, w, dim, _, stream in cases]
+           for _ in range(20)]
+    torch.cuda.synchronize()
+    for outs in got:
+        for out, (_, _, _, ref, _) in zip(outs, cases):
+            assert torch.equal(out, ref)
+    ops.check()
+
+
+@pytest.mark.gpu
+def test_product_offsets_past_32_bits(cuda_device):
+    rows, width, dim = 9_000_000, 256, 32  # 2.3e9 values of the output
+    part = reference_rows(_values(7, dim, 3))
+    x = torch.zeros(rows, row_bytes(dim), dtype=torch.uint8, device=cuda_device)
+    at = torch.tensor([0, 1, 8_388_607, 8_388_608, 8_388_609, rows - 2, rows - 1],
+                      device=cuda_device)
+    x[at] = part.to(cuda_device)
+    w = reference_rows(_values(width, dim, 4))
+    y = ops.mx4_linear(x, w.to(cuda_device), dim, out_dtype=torch.float16)
+    xv, wv = reference_values(part, dim), reference_values(w, dim)
+    ref, size = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    assert_within(y[at], ref, (dim + 2) * 2 * U32 * size + 1.01 * rounding(ref, y.dtype) + 1e-30)
+    assert int((y != 0).any(1).sum()) <= 7
+    ops.check()

@@ -313,8 +313,14 @@ constexpr int kMinChunk = 32;
 constexpr int kRunChunks = 128;  // chunks whose ranks one CTA counts
 static_assert(kSmallTile <= kMinChunk * kRunChunks, "the small sort's tokens are one run");
 
+// Tokens per chunk where one CTA sorts them: fewer where there are few, so that their
+// rows are summed by more warps, but always one run of chunks.
+__host__ __device__ inline int small_chunk(int64_t n) {
+  return n <= 8 * kRunChunks ? 8 : n <= 16 * kRunChunks ? 16 : kMinChunk;
+}
+
 // Up to kSmallTile tokens in one CTA, every pass in shared memory; with rank_of and
-// heads, what count_heads_kernel finds, too (chunks of kMinChunk tokens, one run).
+// heads, what count_heads_kernel finds, too (one run of chunks of small_chunk(n)).
 template <typename Id, int kSmallItems>
 __global__ void __launch_bounds__(kSortThreads)
 sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __restrict__ keys,
@@ -367,14 +373,16 @@ sort_small_kernel(FromIds<Id> src, int n, int passes, int bits, uint32_t* __rest
     }
   }
   if (!heads) return;
-  // s.base: the ids that begin in each chunk, then their prefix
-  const int chunks = (n + kMinChunk - 1) / kMinChunk;
-  for (int c = threadIdx.x >> 5; c < chunks; c += kSortWarps) {
-    const int i = c * kMinChunk + lane_id();
+  // s.base: the ids that begin in each chunk
+  const int chunk = small_chunk(n), chunks = (n + chunk - 1) / chunk, each = 32 / chunk;
+  for (int g = threadIdx.x >> 5; g * 32 < n; g += kSortWarps) {  // 32 tokens, `each` chunks
+    const int i = g * 32 + lane_id();
     const uint32_t k = i < n ? skey[i] : 0;
     const bool head = i < n && k < (uint32_t)src.rows && (i == 0 || skey[i - 1] != k);
-    const int count = __popc(__ballot_sync(0xffffffffu, head));
-    if (lane_id() == 0) s.base[c] = count;
+    const unsigned heads_here = __ballot_sync(0xffffffffu, head);
+    if (lane_id() < each)
+      s.base[g * each + lane_id()] =
+          __popc(heads_here >> (lane_id() * chunk) & (0xffffffffu >> (32 - chunk)));
   }
   __syncthreads();
   if (threadIdx.x >= 32) return;
@@ -454,7 +462,7 @@ struct SumArgs {
   // it ends within (1): partial[(2 * chunk + which) * part_dim ..]
   float* partial;
   int32_t part_dim;    // dim up to a multiple of 4
-  int32_t chunk;       // tokens per chunk, a multiple of kMinChunk
+  int32_t chunk;       // tokens per chunk
   int64_t chunks;
 
   __device__ float* part(int64_t c, int which) const {
@@ -831,6 +839,7 @@ GradPlan grad_plan(int64_t n, int64_t dim) {
   GradPlan p;
   p.chunk = ceil_div(ceil_div(n, kMaxChunks), kMinChunk) * kMinChunk;
   if (p.chunk < kMinChunk) p.chunk = kMinChunk;
+  if (n <= kSmallTile) p.chunk = small_chunk(n);
   p.chunks = ceil_div(n, p.chunk);
   size_t at = 0;
   const auto take = [&](int64_t bytes) {
@@ -931,7 +940,7 @@ cudaError_t launch_sum(SumArgs a, int32_t* heads, cudaStream_t st) {
   cudaError_t e = launch_next(sum_kernel<TIn, TOut, kVec, kCols, kLanes>,
                               dim3((unsigned)ctas, (unsigned)cols), kSumThreads, 0, st, a);
   const unsigned join_cols = (unsigned)ceil_div(a.dim, kJoinCols);
-  if (e == cudaSuccess && a.chunks > kFold)
+  if (e == cudaSuccess && a.chunks >= 2 * kFold)  // a whole run after the first
     e = launch_next(fold_kernel, dim3((unsigned)(a.chunks / kFold), join_cols), kFoldThreads, 0, st,
                     a);
   if (e == cudaSuccess && a.chunks > 1)

@@ -342,3 +342,34 @@ def test_a_gradient_with_more_rows_than_an_index_of_elements(cuda_device):
     want = torch.zeros(10, dim)
     want[0], want[9] = 5, 10
     assert torch.equal(d.cpu(), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [7, 8, 9, 255, 1023, 1024, 1025, 2047, 2048, 2049, 4095, 4096, 4097,
+                               4128, 8191, 8192, 8193])
+@pytest.mark.parametrize("rows", [1, 3, 200, 2 ** 20])
+def test_gradient_at_the_ends_of_its_chunks(cuda_device, n, rows):
+    grad, ids = _case(n, rows, 20, torch.float32, 2, n)
+    d, size, tokens = _grad_ref(grad, ids, rows, 1.0)
+    r = ops.embedding_grad_rows(grad.to(cuda_device), ids.to(cuda_device), rows)
+    hit = torch.nonzero(tokens[:, 0])[:, 0]
+    c = hit.numel()
+    assert r.count.tolist() == [c]
+    assert torch.equal(r.ids[:c].cpu().long(), hit) and (r.ids[c:] == -1).all()
+    assert_within(r.rows[:c], d[hit], _grad_bound(d, size, tokens, torch.float32)[hit])
+    assert (r.rows[c:] == 0).all()
+    ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [5000, 130 * 32, 200_000])
+def test_gradient_of_one_row_from_any_token_to_the_next_row(cuda_device, n):
+    """A row that fills runs of chunks, beginning and ending within, at and past their ends."""
+    for first, last in ((0, n), (1, n - 1), (31, n - 32), (32, n - 31), (64 * 32, n), (0, 64 * 32),
+                        (63, 129 * 32 + 5)):
+        last = min(last, n)
+        ids = torch.zeros(n, dtype=torch.int32)
+        ids[first:last], ids[last:] = 1, 2
+        grad = torch.ones(n, 6)
+        d = ops.embedding_grad(grad.to(cuda_device), ids.to(cuda_device), 3)
+        assert d[:, 0].tolist() == [first, last - first, n - last] and (d == d[:, :1]).all()

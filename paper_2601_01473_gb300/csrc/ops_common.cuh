@@ -68,6 +68,26 @@ struct FlatRows {
     *col = q - r * per_row;
   }
 };
+// A CTA's share of a contiguous matrix taken as one run of elements: kFlatRun of them
+// from element block * kFlatRun on; where element `first` + i of it is.
+constexpr int kFlatRun = 8192;
+struct FlatRun {
+  int64_t row0;
+  uint32_t col0, dim, inv;
+
+  __device__ FlatRun(int64_t block, int32_t dim_, uint32_t inv_) : dim((uint32_t)dim_), inv(inv_) {
+    const int64_t first = block * kFlatRun;
+    row0 = first / dim_;
+    col0 = (uint32_t)(first - row0 * dim_);
+  }
+  __device__ void at(uint32_t i, int64_t* row, uint32_t* col) const {
+    const uint32_t q = col0 + i;  // < dim + kFlatRun
+    // q / dim: exact, as q * dim < 2^32 where dim < kFlatRun
+    const uint32_t r = dim == 1 ? q : dim < kFlatRun ? __umulhi(q, inv) : q >= dim;
+    *row = row0 + r;
+    *col = q - r * dim;
+  }
+};
 inline uint32_t flat_inverse(int64_t per_row) {
   return (uint32_t)(((1ull << 32) + (uint64_t)per_row - 1) / (uint64_t)per_row);
 }

@@ -373,3 +373,25 @@ def test_gradient_of_one_row_from_any_token_to_the_next_row(cuda_device, n):
         grad = torch.ones(n, 6)
         d = ops.embedding_grad(grad.to(cuda_device), ids.to(cuda_device), 3)
         assert d[:, 0].tolist() == [first, last - first, n - last] and (d == d[:, :1]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [8, 9, 11, 31, 301, 1023, 8191, 8192, 8193, 20_011])
+@pytest.mark.parametrize("tin,tout", [(torch.float16, torch.float16),
+                                      (torch.float32, torch.float32),
+                                      (torch.bfloat16, torch.float32),
+                                      (torch.float32, torch.float16)])
+def test_lookup_of_rows_that_no_vector_divides(cuda_device, dim, tin, tout):
+    g = gen(dim)
+    table = torch.randn(50, dim, generator=g).to(tin)
+    for n in (1, 3, 2 + 40_000 // dim):
+        ids = torch.randint(-2, 53, (n,), generator=g, dtype=torch.int32)
+        status = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+        got = ops.embedding_lookup(table.to(cuda_device), ids.to(cuda_device), 2.0, out_dtype=tout,
+                                   status=status)
+        ref = _lookup_ref(table, ids, 2.0)
+        assert_within(got, ref, rounding(ref, tout) * 1.01)
+        assert int(status) == (ops.BAD_INDEX if (ids >= 50).any() else 0)
+    empty = ops.embedding_lookup(table[:0].to(cuda_device),
+                                 torch.tensor([-1, -1], device=cuda_device))
+    assert (empty == 0).all()

@@ -331,3 +331,13 @@ def test_product_offsets_past_32_bits(cuda_device):
     assert_within(y[at], ref, (dim + 2) * 2 * U32 * size + 1.01 * rounding(ref, y.dtype) + 1e-30)
     assert int((y != 0).any(1).sum()) <= 7
     ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [8, 9, 15, 31, 33, 39, 63, 301, 8191, 8193, 12_345])
+@pytest.mark.parametrize("out", FLOATS)
+def test_back_from_rows_that_are_not_whole_eights(cuda_device, dim, out):
+    for rows in (1, 2, 3 + 30_000 // dim):
+        packed = reference_rows(_values(rows, dim, rows))
+        got = ops.mx4_dequantize(packed.to(cuda_device), dim, out_dtype=out).cpu()
+        assert torch.equal(got, reference_values(packed, dim).to(out))

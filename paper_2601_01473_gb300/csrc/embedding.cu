@@ -560,8 +560,11 @@ __device__ __forceinline__ void prefix_of_heads(const int32_t* heads, int runs, 
 
 // A group of kLanes lanes sums a chunk's rows for kLanes * kVec * kCols columns.
 // blockIdx.y: which columns.  Each lane holds the key and place of one token of this
-// round of kLanes tokens and of the next round, whose rows it asks for in L2; from
-// there kDepth rows are on their way at any time.
+// round of kLanes tokens and of the next round; kDepth rows are on their way at any
+// time.  Rows that are loaded two bytes at a time are asked for in L2 when their token
+// is known (498,000 fp16 rows of 301: 238 us, 271 without); others are not, as whole
+// 128-byte lines come that are partly not theirs or not there any more when they are
+// used (1.17M of 128: 221 us, 237 with; 234,000 fp32 rows of 640: 252 and 306).
 //
 // Bound by instructions as much as by memory, so a token costs as few as possible:
 // where rows begin is a mask, found for a round at once; an address is one multiply
@@ -602,10 +605,11 @@ __global__ void __launch_bounds__(kSumThreads, kCols > 4 ? 3 : 6) sum_kernel(Sum
     if (k >= a.rows) return;
     const char* row = (const char*)a.grad + (uint64_t)token * in_bytes +
                       (int64_t)tile_col * (int64_t)sizeof(TIn);
-    for (int32_t b = 0; b < tile_bytes; b += 128)
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(row + b));
+    if constexpr (kVec == 1)
+      for (int32_t b = 0; b < tile_bytes; b += 128)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(row + b));
   };
-  // the rows are on their way while the ranks are found
+  // before the ranks: the chain from a token to its row is the longest
   uint32_t held_key, next_key, held_token, next_token;
   fetch(lo + lane, held_key, held_token);
   fetch(lo + kLanes + lane, next_key, next_token);
@@ -888,7 +892,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(SumArgs a) {
 constexpr int64_t kMaxTokens = 0x7fffffff;
 constexpr int64_t kMaxCells = 1ll << 40;
 constexpr int64_t kMaxDim = 1 << 22;  // its column tiles fit a grid's second dimension
-constexpr int kMaxChunks = 32768;
+constexpr int kMaxChunks = 65536;
 
 struct GradPlan {
   int64_t chunk, chunks;
@@ -1020,9 +1024,14 @@ cudaError_t launch_sum_lanes(const SumArgs& a, int32_t* heads, cudaStream_t st) 
     if (a.dim <= 4) return launch_sum<TIn, TOut, 1, 1, 4>(a, heads, st);
     if (a.dim <= 16) return launch_sum<TIn, TOut, 1, 1, 16>(a, heads, st);
   }
+  const int64_t need = ceil_div(a.dim, 32 * kVec);  // columns a lane
   if constexpr (kVec <= 2) {
-    if (a.dim > 128 * kVec) return launch_sum<TIn, TOut, kVec, 10, 32>(a, heads, st);
-    if (a.dim > 32 * kVec) return launch_sum<TIn, TOut, kVec, 4, 32>(a, heads, st);
+    if (need > 5) return launch_sum<TIn, TOut, kVec, 10, 32>(a, heads, st);
+    if (need > 2) return launch_sum<TIn, TOut, kVec, 5, 32>(a, heads, st);
+    if (need > 1) return launch_sum<TIn, TOut, kVec, 2, 32>(a, heads, st);
+  } else {
+    if (need == 2) return launch_sum<TIn, TOut, kVec, 2, 32>(a, heads, st);
+    if (need == 3) return launch_sum<TIn, TOut, kVec, 3, 32>(a, heads, st);
   }
   return launch_sum<TIn, TOut, kVec, 1, 32>(a, heads, st);
 }

@@ -617,9 +617,10 @@ struct Shape {
 // How a row is cut.  A CTA's barriers, joins and trips to memory for the entries take
 // microseconds beside its slice, so CTAs that share an SM hide one another's: two of
 // 100 KB where the slice is kept for the gradient (8192 rows of 50,000 bf16 classes, a
-// step: 310 us, 396 with four of 50 KB), eight of 26 KB where nothing is joined (the
-// gradient alone: 360 us, 502 with 32 KB and twice the threads).  Threads by what is
-// left for each: 4096 rows of 10,007 fp16 classes, a step: 256 50 us, 384 75, 512 76.
+// step: 305 us, 396 with four of 50 KB), eight of 26 KB where nothing is joined (the
+// gradient alone: 303 us, 370 with 64 KB).  Threads by what is left for each, and where
+// every SM has CTAs enough: 4096 rows of 10,007 fp16 classes, a step: 128 42 us, 256 58,
+// 512 76; 64 rows of 131,072 want 256.
 Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int num_sms) {
   Shape s = {};
   const auto slice_of = [&](int64_t ranks) { return ceil_div(ceil_div(classes, ranks), 64) * 64; };
@@ -636,22 +637,28 @@ Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int n
   }
   s.ranks = (int)ranks;
   s.slice = (int32_t)slice_of(ranks);
-  s.threads = 32 + (s.slice <= 2048 ? 128 : s.slice <= kMidSlice ? 256 : kMaxReaders);
+  s.threads = 32 + (s.slice <= 2048 || (s.slice <= 16384 && rows >= 4 * num_sms) ? 128
+                    : s.slice <= kMidSlice                                        ? 256
+                                                                                  : kMaxReaders);
   const size_t kept = (size_t)(s.slice * size + 32);
   s.keep = kept <= kMaxKeep;
   s.smem = sizeof(DistillSmem) + (s.keep ? kept : 0);
   return s;
 }
 
-// A warp reads a few vectors at a time, so longer rows are a warp's only where every SM
-// has warps enough.
-bool is_short(int64_t rows, int64_t classes, int num_sms) {
-  return classes <= 512 || (classes <= 4096 && rows >= 8 * num_sms);
+// Whether a row is a warp's.  A warp reads a few vectors at a time, so only very short
+// rows are where there are too few of them to fill the SMs.  With the gradient, up to
+// 8192 classes (4096 rows of 6000 fp16 classes, a step: 30 us, 34 by CTAs; of 10,007: 56
+// and 42); for the loss alone, which reads each row once, up to 65,536 (8192 rows of
+// 50,000 bf16 classes: 145 us, 188 by CTAs).
+bool is_short(int64_t rows, int64_t classes, int mode, int num_sms) {
+  const int64_t most = mode == kLoss ? 65536 : 8192;
+  return classes <= 512 || (classes <= most && rows >= 8 * num_sms);
 }
 
 template <typename T, typename TOut, int kMode>
 cudaError_t launch_distill(DistillArgs a, int64_t rows, int device, cudaStream_t st) {
-  if (is_short(rows, a.classes, op_num_sms(device))) {
+  if (is_short(rows, a.classes, kMode, op_num_sms(device))) {
     const size_t smem =
         4 * kShortWarps * (size_t)(3 * a.top + (kMode == kLoss ? 0 : table_slots(a.top)));
     static OncePerDevice once;

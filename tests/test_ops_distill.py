@@ -124,6 +124,32 @@ def test_types(cuda_device, dtype, tdtype, out, index):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("V", [513, 4001, 8192, 8193, 16_385])
+def test_many_rows_of_more_classes(cuda_device, dtype, V):
+    _check(cuda_device, *_case(1300, V, 7, dtype, torch.float32, V), 1.5)
+
+
+@pytest.mark.gpu
+def test_many_rows_of_many_classes(cuda_device):
+    """Rows that are a warp's for the loss alone, at both ends of what is, checked against the
+    same rows taken a few at a time."""
+    for V in (65_536, 65_537):
+        g = torch.Generator(device=cuda_device).manual_seed(V)
+        x = torch.randn(1300, V, generator=g, device=cuda_device).half()
+        t = torch.randn(1300, 5, generator=g, device=cuda_device)
+        at = torch.randint(0, V, (1300, 5), generator=g, device=cuda_device)
+        loss, stats = ops.distill_loss(x, t, at, 2.0)
+        for part in (slice(0, 4), slice(1296, 1300)):
+            ref, _, bound, _ = _reference(x[part].cpu(), t[part].cpu(), at[part].cpu(), 2.0,
+                                          torch.ones(4))
+            assert_within(loss[part], ref, bound)
+            few, few_stats = ops.distill_loss(x[part], t[part], at[part], 2.0)
+            assert_within(few, ref, bound)
+            assert torch.equal(stats[part, 0], few_stats[:, 0])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows", [200, 2000, 70_000])
 def test_many_rows(cuda_device, rows):
     _check(cuda_device, *_case(rows, 40, 4, torch.float16, torch.float32, 8), 2.0)

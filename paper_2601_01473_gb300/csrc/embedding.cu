@@ -569,10 +569,10 @@ __device__ __forceinline__ void prefix_of_heads(const int32_t* heads, int runs, 
 // Bound by instructions as much as by memory, so a token costs as few as possible:
 // where rows begin is a mask, found for a round at once; an address is one multiply
 // and add; lanes and tokens without a value load a valid one and store nothing.  Warps
-// hide the loads' latency better than rows in flight: two rows each and six CTAs an SM
-// (three for ten columns a lane), 1.0M fp16 rows of 128 over 10M nodes 202 us, 300,001 x
-// 301 bf16 140; four rows and what registers allow 214 and 146; eight CTAs, which spill,
-// 238 and 200.
+// hide the loads' latency better than rows in flight: with two rows each and six CTAs an
+// SM (three for ten columns a lane) this kernel takes 108 us of 1.0M fp16 rows of 128
+// over 10M nodes and 70 of 300,001 x 301 bf16; with four rows and as many CTAs as the
+// registers allow 118 and 76.
 template <typename TIn, typename TOut, int kVec, int kCols, int kLanes>
 __global__ void __launch_bounds__(kSumThreads, kCols > 4 ? 3 : 6) sum_kernel(SumArgs a) {
   grid_dep_wait();
@@ -765,7 +765,7 @@ __device__ __forceinline__ void add4(float4& s, const float4& x) {
 // The sum over i in [first, count) in steps of `step` of item(i)'s four columns.
 template <typename Item>
 __device__ __forceinline__ float4 sum_items(int64_t first, int64_t count, int step, Item item) {
-  constexpr int kAhead = 4;
+  constexpr int kAhead = 8;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   int64_t i = first;
   for (; i + (kAhead - 1) * step < count; i += kAhead * step) {
@@ -855,12 +855,22 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(SumArgs a) {
   if (row >= 0) {
     // the last chunk of the row: the first after this one that it does not fill
     int64_t last = chunk + 1;
-    unsigned ends = 0;
-    for (; !ends; last += 32) {
-      const int64_t c = last + lane;
-      ends = __ballot_sync(0xffffffffu, c >= a.chunks || a.row_of[c] != kAllOfIt);
+    const int64_t c = last + lane;
+    const unsigned ends =
+        __ballot_sync(0xffffffffu, c >= a.chunks || a.row_of[c] != kAllOfIt);
+    if (ends) {
+      last += __ffs(ends) - 1;
+    } else {  // a long row: the last chunk that begins with its key
+      const uint32_t key = a.first_key(last);
+      int64_t end = a.chunks;
+      while (end - last > 1) {
+        const int64_t mid = (last + end) / 2;
+        if (a.first_key(mid) == key)
+          last = mid;
+        else
+          end = mid;
+      }
     }
-    last += __ffs(ends) - 33;
     parts = Parts(chunk, last);
     if (parts.count > kJoinAlone)
       many = row;
@@ -1017,7 +1027,8 @@ cudaError_t launch_sum(SumArgs a, int32_t* heads, cudaStream_t st) {
 
 // A warp to a row where the row has 32 columns or more: half a warp to a row has
 // the two halves end their rows at different tokens, one after the other (1.0M fp16
-// rows of 128: 4 columns a lane 258 us, 8 a lane in half a warp 265).
+// rows of 128, the whole gradient at the time: 4 columns a lane 258 us, 8 a lane in half
+// a warp 265).  More columns a lane where a row is longer, as few as it needs.
 template <typename TIn, typename TOut, int kVec>
 cudaError_t launch_sum_lanes(const SumArgs& a, int32_t* heads, cudaStream_t st) {
   if constexpr (kVec > 1) {

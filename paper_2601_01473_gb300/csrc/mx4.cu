@@ -329,7 +329,8 @@ agnes_status agnes_mx4_quantize(const void* x, int32_t dtype, int64_t stride, in
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const cudaError_t e = with_float_type(dtype, [&](auto t) {
     using T = typename decltype(t)::type;
-    const bool wide = dim % 8 == 0 && aligned_rows(x, rows > 1 ? stride * (int64_t)sizeof(T) : 0, 16);
+    const bool wide =
+        dim % 8 == 0 && aligned_rows(x, rows > 1 ? stride * (int64_t)sizeof(T) : 0, 16);
     const bool words = g.groups % 8 == 0;
     const auto kernel = wide ? (words ? quantize_kernel<T, true, true>
                                       : quantize_kernel<T, true, false>)

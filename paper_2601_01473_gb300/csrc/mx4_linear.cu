@@ -322,7 +322,8 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, int32_t x, int
 
 template <typename TOut>
 __global__ void __launch_bounds__(kThreads, 1)
-linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant__ CUtensorMap w_codes,
+linear_kernel(const __grid_constant__ CUtensorMap x_codes,
+              const __grid_constant__ CUtensorMap w_codes,
               const __grid_constant__ CUtensorMap out_map, const LinearArgs a) {
   extern __shared__ uint8_t raw[];
   uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
@@ -430,7 +431,8 @@ linear_kernel(const __grid_constant__ CUtensorMap x_codes, const __grid_constant
           const uint32_t w_at =
               resident ? w_ring_at + (uint32_t)(k * kCodeBytes) : x_at + kCodeBytes;
           const uint32_t x_scale = tmem + kScaleCol0 + (uint32_t)(s * kScaleCols);
-          const uint32_t w_scale = resident ? tmem + kResidentCol0 + (uint32_t)(k * 8) : x_scale + 8u;
+          const uint32_t w_scale =
+              resident ? tmem + kResidentCol0 + (uint32_t)(k * 8) : x_scale + 8u;
           const int n = min(4, steps - 4 * k);
           const uint32_t scales = smem_addr(scale_stage + s * 2 * kScaleBytes);
           for (int c = 0; c < (n + 1) / 2; ++c) {

@@ -164,6 +164,14 @@ def test_rows_past_shared_memory(cuda_device, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("V", [350_003, 409_088, 409_217, 818_688])
+def test_rows_that_fill_shared_memory(cuda_device, dtype, V):
+    """Slices up to the most that a CTA keeps, and just past it."""
+    _check(cuda_device, *_case(2, V, 9, dtype, dtype, V), 2.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", FLOATS)
 def test_strides_and_alignments(cuda_device, dtype):
     R, V, K = 4, 1000, 6
     x, t, at, w = _case(R, V, K, dtype, torch.float32, 21)

@@ -660,7 +660,11 @@ linear_few_kernel(int lanes, const LinearArgs a) {
             const float2 f = __half22float2(acc);
             dot += f.x + f.y;
           }
-          sum[r] += dot * scales[r * a.blocks + b] * scale;
+          // the smaller scale first: |dot| <= 1152 and a multiple of 1/4, so that product is
+          // exact (2^-129 at the least) or no larger than the whole one
+          const float other = scales[r * a.blocks + b];
+          const bool less = other < scale;  // a NaN is a factor either way
+          sum[r] += dot * (less ? other : scale) * (less ? scale : other);
         }
       }
     }

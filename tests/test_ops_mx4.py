@@ -341,3 +341,48 @@ def test_back_from_rows_that_are_not_whole_eights(cuda_device, dim, out):
         packed = reference_rows(_values(rows, dim, rows))
         got = ops.mx4_dequantize(packed.to(cuda_device), dim, out_dtype=out).cpu()
         assert torch.equal(got, reference_values(packed, dim).to(out))
+
+
+def _product_of_values(dev, xv, wv, out=torch.float32):
+    """(product, its value in 64 bits, the bound of the difference) of xv and wv in 4 bits."""
+    dim = xv.shape[1]
+    x, w = reference_rows(xv), reference_rows(wv)
+    xv, wv = reference_values(x, dim), reference_values(w, dim)
+    ref, size = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    got = ops.mx4_linear(x.to(dev), w.to(dev), dim, out_dtype=out)
+    return got, ref, (dim + 2) * 2 * U32 * size + 1.01 * rounding(ref, out) + 1e-30
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 2, 4, 8, 9, 150])
+@pytest.mark.parametrize("large,small,used", [(2.0 ** 126, 2.0 ** -20, 96), (3.4e38, 0.1, 8),
+                                              (2.0 ** 120, 2.0 ** -120, 96)])
+def test_a_finite_product_of_far_apart_scales_is_finite(cuda_device, rows, large, small, used):
+    """Whichever side has the large values, and where blocks cancel one another.  The sum of the
+    magnitudes is in fp32's range, and so is every partial sum."""
+    g = gen(rows)
+    dim, width = 96, 20
+    column = torch.arange(dim)
+    sign = torch.where(column < 32, 1.0, -1.0)
+    sign[(column < 32 - used // 2) | (column >= 32 + used // 2)] = 0
+    for x_scale, w_scale in ((large, small), (small, large)):
+        xv = (torch.rand(rows, dim, generator=g) / 2 + 0.5) * x_scale * sign
+        wv = (torch.rand(width, dim, generator=g) / 2 + 0.5) * w_scale
+        wv[1] *= -1
+        assert xv.abs().max() * wv.abs().max() * used < 3e38
+        got, ref, bound = _product_of_values(cuda_device, xv, wv)
+        assert got.isfinite().all()
+        assert_within(got, ref, bound)
+    ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [2, 150])
+def test_a_product_past_fp32_is_infinite(cuda_device, rows):
+    xv = torch.full((rows, 64), 2.0 ** 100)
+    wv = torch.full((3, 64), 2.0 ** 100)
+    wv[1] *= -1
+    wv[2] = 0
+    got = ops.mx4_linear(*(ops.mx4_quantize(v.to(cuda_device)) for v in (xv, wv)), 64).cpu()
+    assert (got[:, 0] == math.inf).all() and (got[:, 1] == -math.inf).all()
+    assert (got[:, 2] == 0).all()

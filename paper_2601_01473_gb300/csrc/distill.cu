@@ -251,18 +251,21 @@ __device__ __forceinline__ bool repeated(const DistillArgs& a, const Entries& s,
   return __any_sync(0xffffffffu, twice);
 }
 
-// A warp: the row's loss.  logit(k): the student's logit at entry k's class.
+// A warp: the row's loss.  logit(k): the student's logit at entry k's class.  As
+//   2 T sum_k p_k (T/2 (ln p_k + ln S) - (x_k / 2 - M / 2)),
+// whose terms leave fp32 only where the loss does: x_k - M itself may, and over T it does for
+// a class that is masked by its type's lowest value.
 template <typename Logit>
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& s, MaxSum q,
                                           Logit logit) {
-  const float inv_t = 1.f / a.temperature, log_s = logf(q.s);
+  const float half_t = 0.5f * a.temperature, half_m = 0.5f * q.m, log_s = logf(q.s);
   float sum = 0.f;
   for (int k = lane_id(); k < a.top; k += 32) {
     const float p = s.p[k];
     if (p != 0.f && s.index[k] >= 0)
-      sum += p * (logf(p) - ((logit(k) - q.m) * inv_t - log_s));
+      sum += p * (half_t * (logf(p) + log_s) - (0.5f * logit(k) - half_m));
   }
-  return warp_sum(sum) * a.temperature * a.temperature;
+  return warp_sum(sum) * (2.f * a.temperature);
 }
 
 // The entries' classes in [v0, v0 + n) once more: out = coef (mass q - p), where p is

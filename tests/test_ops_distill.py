@@ -375,3 +375,23 @@ def test_offsets_past_32_bits(cuda_device):
     assert_within(loss[rows], ref_loss, loss_bound)
     assert_within(grad[rows], ref_grad, bound)
     assert (loss.sum() - loss[rows].sum()).abs() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("V", [6, 5000, 60_000])
+@pytest.mark.parametrize("T", [0.25, 0.5, 2.0])
+def test_a_teacher_of_classes_masked_by_the_lowest_value(cuda_device, dtype, V, T):
+    """The loss is large and finite wherever the formula's is: differences of logits beyond the
+    type's range, over T, and T^2 of it do not leave fp32 on the way."""
+    x, t, at, w = _case(4, V, 4, dtype, torch.float32, V)
+    at[:] = torch.tensor([1, 2, 4, 5], dtype=at.dtype)
+    lowest, most = torch.finfo(dtype).min, torch.finfo(dtype).max
+    x[:, 3:] = lowest                # two of the teacher's classes
+    x[1, 0] = most / 4               # and the others are far below the largest
+    x[2, 0] = most
+    t[3, 2:] = t[3, :2].max() - 40 * T  # almost nothing on the masked ones
+    _check(cuda_device, x, t, at, w, T)
+    ref = _reference(x, t, at, T, w)[0]
+    got = ops.distill_loss(*(v.to(cuda_device) for v in (x, t, at)), T)[0].cpu()
+    assert got.isfinite()[ref < 3e38].all()

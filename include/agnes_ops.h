@@ -18,7 +18,7 @@
  * Strides are in elements (bytes for 4-bit rows) and may exceed the row's
  * length; a row's elements are adjacent.
  *
- * status: an optional int32 in device memory.  What a kernel finds wrong with
+ * status: an optional int32 (4-byte aligned) in device memory.  What a kernel finds wrong with
  * its data is ORed into it (AGNES_OP_*): the caller clears it, and reads it when
  * it next waits for the stream.
  */

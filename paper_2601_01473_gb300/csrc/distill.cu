@@ -787,7 +787,7 @@ agnes_status distill(const DistillCall& c) {
                               (c.rows > 1 && c.out_stride != c.logits_stride)))
       return op_error(AGNES_EINVAL, "%s: out in place of logits has another type or stride", op);
   }
-  if (c.status) OP_TRY(op_on_device(op, "status", c.status, device));
+  OP_TRY(op_status(op, c.status, device));
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
   DistillArgs a = {};

@@ -1123,7 +1123,7 @@ agnes_status embedding_grad(const GradCall& c, bool compact) {
     OP_TRY(op_on_device(op, "out", c.out, device));
     OP_TRY(op_aligned(op, "out", c.out, float_size(c.out_dtype)));
   }
-  if (c.status) OP_TRY(op_on_device(op, "status", c.status, device));
+  OP_TRY(op_status(op, c.status, device));
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
   if (c.n == 0) {
@@ -1220,7 +1220,7 @@ agnes_status agnes_embedding_lookup(const void* table, int32_t table_dtype, int6
   OP_TRY(op_aligned(op, "table", table, float_size(table_dtype)));
   OP_TRY(op_aligned(op, "out", out, float_size(out_dtype)));
   OP_TRY(op_aligned(op, "ids", ids, ids_bits / 8));
-  if (status) OP_TRY(op_on_device(op, "status", status, device));
+  OP_TRY(op_status(op, status, device));
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
   const cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -817,7 +817,7 @@ extern "C" agnes_status agnes_mx4_linear(const void* x, int64_t x_stride, int64_
     OP_TRY(op_on_device(op, "bias", bias, device));
     OP_TRY(op_aligned(op, "bias", bias, 4));
   }
-  if (status) OP_TRY(op_on_device(op, "status", status, device));
+  OP_TRY(op_status(op, status, device));
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
   LinearArgs a = {};

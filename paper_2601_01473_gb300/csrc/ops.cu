@@ -61,6 +61,12 @@ agnes_status op_aligned(const char* op, const char* name, const void* p, int64_t
   return AGNES_OK;
 }
 
+agnes_status op_status(const char* op, const int32_t* status, int device) {
+  if (!status) return AGNES_OK;
+  OP_TRY(op_on_device(op, "status", status, device));
+  return op_aligned(op, "status", status, 4);
+}
+
 agnes_status op_launched(const char* op, cudaError_t e) {
   if (e == cudaSuccess) return AGNES_OK;
   return op_error(e == cudaErrorMemoryAllocation ? AGNES_ENOMEM : AGNES_ECUDA, "%s: %s", op,

@@ -164,6 +164,8 @@ agnes_status op_float_type(const char* op, const char* name, int32_t dtype);
 agnes_status op_index_bits(const char* op, const char* name, int32_t bits);
 // `p` is aligned to one element of `size` bytes.
 agnes_status op_aligned(const char* op, const char* name, const void* p, int64_t size);
+// The caller's status word, if there is one: on `device`, and aligned for an atomic.
+agnes_status op_status(const char* op, const int32_t* status, int device);
 // The launch's error, as a status.
 agnes_status op_launched(const char* op, cudaError_t e);
 // A stride in bytes between 4-bit rows of dim values (mx4.cu).

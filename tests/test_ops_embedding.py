@@ -395,3 +395,30 @@ def test_lookup_of_rows_that_no_vector_divides(cuda_device, dim, tin, tout):
     empty = ops.embedding_lookup(table[:0].to(cuda_device),
                                  torch.tensor([-1, -1], device=cuda_device))
     assert (empty == 0).all()
+
+
+@pytest.mark.gpu
+def test_a_status_that_is_not_aligned_is_refused(cuda_device):
+    """By every C entry that takes one, on the host."""
+    z = torch.zeros(4096, dtype=torch.uint8, device=cuda_device)
+    p, L = z.data_ptr(), ops.lib()
+    for off in (1, 2, 3):
+        bad = p + 2048 + off
+        for call in (
+                lambda: L.agnes_embedding_lookup(p, 0, 4, 8, 8, p, 32, 3, 1.0, p + 512, 0, 8, bad,
+                                                 None),
+                lambda: L.agnes_embedding_grad(p, 0, 8, p, 32, 3, 4, 8, 1.0, p + 512, 0, p + 1024,
+                                               1024, bad, None),
+                lambda: L.agnes_embedding_grad_rows(p, 0, 8, p, 32, 3, 4, 8, 1.0, p + 512, p + 768,
+                                                    0, p + 896, p + 1024, 1024, bad, None),
+                lambda: L.agnes_distill_loss(p, 0, 5, 2, 5, p, 0, p, 32, 1, 1.0, p + 512, p + 768,
+                                             bad, None),
+                lambda: L.agnes_distill_grad(p, 0, 5, 2, 5, p, 0, p, 32, 1, 1.0, p + 512, None, 1.0,
+                                             p + 768, 0, 5, bad, None),
+                lambda: L.agnes_distill_loss_grad(p, 0, 5, 2, 5, p, 0, p, 32, 1, 1.0, None, 1.0,
+                                                  p + 512, p + 768, 0, 5, bad, None),
+                lambda: L.agnes_mx4_linear(p, 32, 3, p, 32, 4, 32, None, p + 512, 0, 4, bad, None)):
+            assert call() == 1
+            assert b"status is not aligned" in L.agnes_last_error(None)
+    torch.cuda.synchronize()
+    assert (z == 0).all()

@@ -8,9 +8,10 @@ What a kernel finds wrong with its data (an id past the end of its table, a wait
 that ran out) is kept on the device, in the int32 tensor ``status`` if one is
 given and else in one per device that ``check()`` reads and clears.
 
-With ``stream``, the results belong to that stream, and the inputs' memory is
-kept until it has come past the call; the inputs' values have to be there by
-then (order the stream after the one that makes them).
+With ``stream`` (a Stream or a handle, of the arguments' device), the results
+belong to that stream, and the inputs' memory is kept until it has come past the
+call; the inputs' values have to be there by then (order the stream after the one
+that makes them).
 """
 from __future__ import annotations
 
@@ -36,15 +37,25 @@ class RowGrad(NamedTuple):
     count: torch.Tensor  # int32 [1]: how many
 
 
-def _on_stream(stream, op, *args):
-    """op(*args) with ``stream`` current."""
+def _stream_of(stream, device):
+    """``stream``, a Stream or a handle, as a stream of ``device``."""
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream))
+        return torch.cuda.ExternalStream(int(stream), device=device)
+    if stream.device != device:
+        raise ValueError(f"the stream is {stream.device}'s, the arguments are on {device}")
+    return stream
+
+
+def _on_stream(stream, op, *args):
+    """op(*args) with ``stream`` current on the arguments' device."""
+    tensors = [t for t in args if isinstance(t, torch.Tensor) and t.is_cuda]
+    if not tensors:
+        return op(*args)  # which refuses them
+    stream = _stream_of(stream, tensors[0].device)
     with torch.cuda.stream(stream):
         result = op(*args)
-    for t in args:
-        if isinstance(t, torch.Tensor) and t.is_cuda:
-            t.record_stream(stream)
+    for t in tensors:
+        t.record_stream(stream)
     return result
 
 

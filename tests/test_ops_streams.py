@@ -1,0 +1,60 @@
+"""Which stream an operator's call runs on (paper_2601_01473_gb300/ops.py)."""
+import contextlib
+
+import pytest
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+
+from paper_2601_01473_gb300 import ops
+
+
+class _Stream:
+    def __init__(self, handle, device=None):
+        self.cuda_stream, self.device = handle, device
+
+
+def test_a_stream_is_one_of_the_arguments_device(monkeypatch):
+    """Without a GPU: a handle becomes a stream of the tensors' device whatever device is
+    current, and a stream of another device is refused."""
+    ran_on, kept_for = [], []
+    monkeypatch.setattr(torch.cuda, "Stream", _Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", _Stream)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: ran_on.append(s) or contextlib.nullcontext())
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: kept_for.append(s))
+    with FakeTensorMode():
+        tensors = [torch.empty(3, device=f"cuda:{i}") for i in range(2)]
+    for t in tensors:
+        for stream in (77, _Stream(77, t.device)):
+            assert ops._on_stream(stream, lambda *args: args, 1.5, t, None) == (1.5, t, None)
+            assert ran_on[-1].cuda_stream == 77 and ran_on[-1].device == t.device
+            assert kept_for[-1] is ran_on[-1]
+    with pytest.raises(ValueError, match="cuda:1.*cuda:0"):
+        ops._on_stream(_Stream(5, tensors[1].device), lambda *args: args, tensors[0])
+
+
+def test_arguments_off_the_gpu_are_refused_with_a_stream_too():
+    with pytest.raises(ValueError, match="CUDA device"):
+        ops.embedding_lookup(torch.zeros(4, 8), torch.zeros(3, dtype=torch.int32), stream=0)
+    with pytest.raises(TypeError, match="2-D"):
+        ops.mx4_quantize(None, stream=0)
+
+
+@pytest.mark.gpu
+def test_a_call_is_ordered_by_the_stream_that_is_named(cuda_device):
+    """By its object and by its handle: what a stream has before the call is there for it, and
+    what it has after sees its results."""
+    for named in (lambda s: s, lambda s: s.cuda_stream):
+        stream = torch.cuda.Stream()
+        table = torch.zeros(4_000_000, 64, device=cuda_device)
+        ids = torch.full((100_000,), 3_999_999, dtype=torch.int32, device=cuda_device)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            for v in range(1, 9):
+                table.fill_(v)
+        got = ops.embedding_lookup(table, ids, stream=named(stream))
+        with torch.cuda.stream(stream):
+            table.fill_(-1)
+            total = got.sum()
+        torch.cuda.synchronize()
+        assert float(total) == 8 * 64 * 100_000
+    ops.check()

@@ -203,6 +203,14 @@ def _stream_handle(stream, device=None) -> int | None:
     return int(stream) or None
 
 
+def _stream_of_handle(handle, device):
+    """The stream of a handle; none is the default stream's, of which ExternalStream would
+    make another stream."""
+    if not handle:
+        return torch.cuda.default_stream(device)
+    return torch.cuda.ExternalStream(handle, device=device)
+
+
 def _int32_table(ptr: int, rows: int, cols: int):
     """A copy of rows x cols int32 values in host memory."""
     return np.frombuffer(bytearray(ctypes.string_at(ptr, 4 * rows * cols)),
@@ -377,8 +385,7 @@ class Graph:
         ones (_copied); for a program that does not fetch, or changes streams,
         an event follows every 64 of them."""
         if self._copying and (handle != self._copy_stream or len(self._copying) >= 64):
-            stream = torch.cuda.ExternalStream(self._copy_stream or 0, self.device)
-            with torch.cuda.stream(stream):
+            with torch.cuda.stream(_stream_of_handle(self._copy_stream, self.device)):
                 if not torch.cuda.is_current_stream_capturing():
                     event = torch.cuda.Event()
                     event.record()

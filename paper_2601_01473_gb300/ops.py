@@ -21,7 +21,7 @@ from typing import NamedTuple
 
 import torch
 
-from .agnes import AgnesError, lib
+from .agnes import AgnesError, _stream_of_handle, lib
 
 _FLOATS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _INDEXES = {torch.int32: 32, torch.int64: 64}
@@ -40,7 +40,7 @@ class RowGrad(NamedTuple):
 def _stream_of(stream, device):
     """``stream``, a Stream or a handle, as a stream of ``device``."""
     if not isinstance(stream, torch.cuda.Stream):
-        return torch.cuda.ExternalStream(int(stream), device=device)
+        return _stream_of_handle(int(stream), device)
     if stream.device != device:
         raise ValueError(f"the stream is {stream.device}'s, the arguments are on {device}")
     return stream

@@ -1,11 +1,12 @@
 """Which stream an operator's call runs on (paper_2601_01473_gb300/ops.py)."""
+import collections
 import contextlib
 
 import pytest
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
 
-from paper_2601_01473_gb300 import ops
+from paper_2601_01473_gb300 import Graph, ops
 
 
 class _Stream:
@@ -57,4 +58,60 @@ def test_a_call_is_ordered_by_the_stream_that_is_named(cuda_device):
             total = got.sum()
         torch.cuda.synchronize()
         assert float(total) == 8 * 64 * 100_000
+    ops.check()
+
+
+def test_no_handle_is_the_default_stream(monkeypatch):
+    """Without a GPU: torch makes a stream of its own of an ExternalStream without a handle."""
+    device = torch.device("cuda", 1)
+    default = _Stream(0, device)
+    monkeypatch.setattr(torch.cuda, "Stream", _Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", _Stream)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda d: default if d == device else None)
+    assert ops._stream_of(0, device) is default
+    assert ops._stream_of(5, device) is not default
+
+    # a graph's host targets, prepared on the default stream and not yet fetched: the event
+    # that they are kept for is one of that stream
+    current, recorded = [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        current.append(stream)
+        yield
+        current.pop()
+
+    class Event:
+        def record(self):
+            recorded.append(current[-1])
+
+        def query(self):
+            return False
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "Event", Event)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    g = Graph.__new__(Graph)
+    g.device, g._ctx = device, None
+    g._prepares, g._copy_stream, g._copying, g._held = 0, None, collections.deque(), \
+        collections.deque()
+    for _ in range(65):
+        g._hold_until_copied(object(), None)
+    assert recorded == [default]
+    g._hold_until_copied(object(), 7)  # another stream from here on
+    assert recorded == [default, default]
+    g._hold_until_copied(object(), None)
+    assert recorded[2].cuda_stream == 7 and recorded[2].device == device
+
+
+@pytest.mark.gpu
+def test_a_call_is_ordered_by_the_default_stream_by_its_handle(cuda_device):
+    table = torch.zeros(4_000_000, 64, device=cuda_device)
+    ids = torch.full((100_000,), 3_999_999, dtype=torch.int32, device=cuda_device)
+    torch.cuda.synchronize()
+    for v in range(1, 9):
+        table.fill_(v)
+    got = ops.embedding_lookup(table, ids, stream=0)
+    table.fill_(-1)
+    assert float(got.sum()) == 8 * 64 * 100_000
     ops.check()

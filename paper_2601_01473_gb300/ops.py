@@ -82,7 +82,8 @@ def _status_word(status, device) -> int:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("the first call on a device cannot be captured without a "
                                    "status tensor")
-            status = torch.zeros(1, dtype=torch.int32, device=device)
+            with torch.inference_mode(False):  # else check() may not clear it
+                status = torch.zeros(1, dtype=torch.int32, device=device)
             torch.cuda.current_stream(device).synchronize()
             _status[device.index] = status
     elif status.dtype != torch.int32 or status.numel() < 1:

@@ -422,3 +422,15 @@ def test_a_status_that_is_not_aligned_is_refused(cuda_device):
             assert b"status is not aligned" in L.agnes_last_error(None)
     torch.cuda.synchronize()
     assert (z == 0).all()
+
+
+@pytest.mark.gpu
+def test_a_first_call_in_inference_mode_leaves_a_status_that_can_be_cleared(cuda_device,
+                                                                            monkeypatch):
+    monkeypatch.setattr(ops, "_status", {})
+    table, ids = torch.ones(10, 16, device=cuda_device), torch.tensor([10], device=cuda_device)
+    with torch.inference_mode():
+        ops.embedding_lookup(table, ids)
+    with pytest.raises(AgnesError, match="past the end"):
+        ops.check()
+    ops.check()  # cleared

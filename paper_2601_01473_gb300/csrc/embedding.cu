@@ -145,6 +145,16 @@ __device__ __forceinline__ uint32_t key_of(Id id, int64_t rows, int32_t* status)
   return (uint32_t)id;
 }
 
+// What the gradient of a table without rows has to do: every id that selects a row is past
+// its end.
+template <typename Id>
+__global__ void __launch_bounds__(kSortThreads)
+any_id_kernel(const Id* __restrict__ ids, int64_t n, int32_t* status) {
+  const int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x;
+  if (__syncthreads_or(i < n && ids[i] >= 0) && threadIdx.x == 0)
+    op_flag(status, AGNES_OP_BAD_INDEX);
+}
+
 // Where a pass reads its keys: the caller's ids (the first pass), or the last
 // pass's.
 template <typename Id>
@@ -1098,6 +1108,24 @@ struct GradCall {
   cudaStream_t st;
 };
 
+// The dense gradient of a table without rows: nothing to write, ids past its end to report.
+agnes_status report_ids(const GradCall& c) {
+  const char* op = c.op;
+  if (c.n == 0 || !c.status) return AGNES_OK;
+  int device = -1;
+  OP_TRY(op_device_of(op, "ids", c.ids, &device));
+  OP_TRY(op_aligned(op, "ids", c.ids, c.ids_bits / 8));
+  OP_TRY(op_status(op, c.status, device));
+  DeviceGuard dg(device);
+  if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
+  return op_launched(op, with_index_type(c.ids_bits, [&](auto id) {
+    using Id = typename decltype(id)::type;
+    any_id_kernel<Id><<<(unsigned)ceil_div(c.n, kSortThreads), kSortThreads, 0, c.st>>>(
+        (const Id*)c.ids, c.n, c.status);
+    return cudaGetLastError();
+  }));
+}
+
 agnes_status embedding_grad(const GradCall& c, bool compact) {
   const char* op = c.op;
   OP_TRY(check_embedding(op, c.rows, c.dim, c.n, c.ids_bits));
@@ -1115,7 +1143,7 @@ agnes_status embedding_grad(const GradCall& c, bool compact) {
     OP_TRY(op_device_of(op, "count", c.count, &device));
     OP_TRY(op_aligned(op, "count", c.count, 4));
   } else if (out_rows == 0) {
-    return AGNES_OK;
+    return report_ids(c);
   } else {
     OP_TRY(op_device_of(op, "out", c.out, &device));
   }

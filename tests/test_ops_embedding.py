@@ -434,3 +434,28 @@ def test_a_first_call_in_inference_mode_leaves_a_status_that_can_be_cleared(cuda
     with pytest.raises(AgnesError, match="past the end"):
         ops.check()
     ops.check()  # cleared
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+def test_gradient_of_a_table_without_rows_reports_ids(cuda_device, index):
+    for n in (1, 300, 70_000):
+        grad = torch.ones(n, 4, device=cuda_device)
+        ids = torch.full((n,), -1, dtype=index, device=cuda_device)
+        status = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+        assert ops.embedding_grad(grad, ids, 0, status=status).shape == (0, 4)
+        assert int(status) == 0
+        ids[n - 1] = 0
+        ops.embedding_grad(grad, ids, 0, status=status)
+        assert int(status) == ops.BAD_INDEX
+        ops.embedding_grad(grad, ids, 0)
+        with pytest.raises(AgnesError, match="past the end"):
+            ops.check()
+    # by the C entry: ids and the status alone, and without a status nothing
+    L, ids = ops.lib(), torch.zeros(8, dtype=index, device=cuda_device)
+    bits, p = 8 * ids.element_size(), status.data_ptr()
+    for at, rc in ((p, 0), (None, 0), (p + 2, 1)):
+        assert L.agnes_embedding_grad(None, 0, 4, ids.data_ptr(), bits, 8, 0, 4, 1.0, None, 0, None,
+                                      0, at, None) == rc
+    assert L.agnes_embedding_grad(None, 0, 4, None, bits, 8, 0, 4, 1.0, None, 0, None, 0, p,
+                                  None) == 1

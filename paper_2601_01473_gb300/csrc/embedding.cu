@@ -1252,7 +1252,6 @@ agnes_status agnes_embedding_lookup(const void* table, int32_t table_dtype, int6
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  bool too_many = false;
   const cudaError_t e = with_float_type(table_dtype, [&](auto tin) {
     return with_float_type(out_dtype, [&](auto tout) {
       using TIn = typename decltype(tin)::type;
@@ -1271,22 +1270,17 @@ agnes_status agnes_embedding_lookup(const void* table, int32_t table_dtype, int6
             return cudaGetLastError();
           });
         }
-        const int64_t vpr = dim / kVec, blocks = ceil_div(n * vpr, kFlat);
-        if (blocks > kMaxTokens) {
-          too_many = true;
-          return cudaSuccess;
-        }
+        const int64_t vpr = dim / kVec, blocks = ceil_div(n * vpr, kFlat);  // 2^30 at most
         return with_index_type(ids_bits, [&](auto id) {
           using Id = typename decltype(id)::type;
           lookup_kernel<TIn, TOut, Id, kVec><<<(unsigned)blocks, kLookupThreads, 0, st>>>(
-              (const TIn*)table, rows, table_stride, (int32_t)vpr, flat_inverse(vpr), (const Id*)ids, n, scale,
-              (TOut*)out, out_stride, status);
+              (const TIn*)table, rows, table_stride, (int32_t)vpr, flat_inverse(vpr),
+              (const Id*)ids, n, scale, (TOut*)out, out_stride, status);
           return cudaGetLastError();
         });
       });
     });
   });
-  if (too_many) return op_error(AGNES_ERANGE, "%s: n * dim is too large", op);
   return op_launched(op, e);
 }
 

@@ -459,3 +459,52 @@ def test_gradient_of_a_table_without_rows_reports_ids(cuda_device, index):
                                       0, at, None) == rc
     assert L.agnes_embedding_grad(None, 0, 4, None, bits, 8, 0, 4, 1.0, None, 0, None, 0, p,
                                   None) == 1
+
+
+# The widest vector that divides the rows, and how many of them a lane and a column tile take,
+# follow from dim: every kernel of the sums, and grids of one and of several column tiles.
+_DIMS = {8: [256, 512, 768, 1024, 1296], 4: [128, 256, 300, 384, 516, 640],
+         2: [66, 130, 302, 322, 642], 1: [33, 65, 161, 301, 321, 643]}
+_SUMS = [(tin, tout, dim) for tin, tout in
+         [(torch.float16, torch.float16), (torch.bfloat16, torch.bfloat16),
+          (torch.float32, torch.float32), (torch.bfloat16, torch.float32)]
+         for vec, dims in _DIMS.items() for dim in dims
+         if vec <= 16 // max(tin.itemsize, tout.itemsize)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tin,tout,dim", _SUMS)
+def test_gradient_of_longer_rows(cuda_device, tin, tout, dim):
+    for n, rows, skew in ((600, 40, 2), (9000, 60, 4)):  # rows within, across and over chunks
+        grad, ids = _case(n, rows, dim, tin, skew, n + dim)
+        d, size, tokens = _grad_ref(grad, ids, rows, 1.5)
+        hit = torch.nonzero(tokens[:, 0])[:, 0]
+        c = hit.numel()
+        wide = torch.full((n, dim + 24), float("nan"), dtype=tin, device=cuda_device)
+        wide[:, 8:8 + dim] = grad.to(cuda_device)
+        odd = torch.full((n, dim + 3), float("nan"), dtype=tin, device=cuda_device)
+        odd[:, 1:1 + dim] = grad.to(cuda_device)
+        for x in (grad.to(cuda_device), wide[:, 8:8 + dim], odd[:, 1:1 + dim]):
+            dense = ops.embedding_grad(x, ids.to(cuda_device), rows, 1.5, out_dtype=tout)
+            assert_within(dense, d, _grad_bound(d, size, tokens, tout))
+            r = ops.embedding_grad_rows(x, ids.to(cuda_device), rows, 1.5, out_dtype=tout)
+            assert r.count.tolist() == [c]
+            assert torch.equal(r.ids[:c].cpu().long(), hit) and (r.ids[c:] == -1).all()
+            assert torch.equal(r.rows[:c].cpu(), dense.cpu()[hit])
+            assert (r.rows[c:] == 0).all()
+    ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("dim", [9, 41, 301])
+def test_lookup_of_strided_rows_that_no_vector_divides(cuda_device, dtype, dim):
+    g = gen(dim)
+    wide = torch.randn(50, dim + 7, generator=g).to(dtype)
+    for first in (0, 1, 6):
+        ids = torch.randint(-1, 50, (2 + 30_000 // dim,), generator=g, dtype=torch.int32)
+        got = ops.embedding_lookup(wide.to(cuda_device)[:, first:first + dim],
+                                   ids.to(cuda_device), 2.0)
+        ref = _lookup_ref(wide[:, first:first + dim], ids, 2.0)
+        assert_within(got, ref, rounding(ref, dtype) * 1.01)
+    ops.check()

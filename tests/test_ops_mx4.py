@@ -386,3 +386,33 @@ def test_a_product_past_fp32_is_infinite(cuda_device, rows):
     got = ops.mx4_linear(*(ops.mx4_quantize(v.to(cuda_device)) for v in (xv, wv)), 64).cpu()
     assert (got[:, 0] == math.inf).all() and (got[:, 1] == -math.inf).all()
     assert (got[:, 2] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", FLOATS)
+@pytest.mark.parametrize("rows,width,dim", [(20_000, 600, 500), (9000, 900, 640),
+                                            (9000, 900, 1024), (20_000, 500, 1100)])
+def test_product_of_several_tiles_a_cta(cuda_device, out, rows, width, dim):
+    """Rows of two stages and more, odd and even, over more tiles than there are CTAs."""
+    x = ops.mx4_quantize(_values(rows, dim, 1).to(cuda_device))
+    w = ops.mx4_quantize(_values(width, dim, 2).to(cuda_device))
+    b = torch.randn(width, generator=gen(3))
+    got = ops.mx4_linear(x, w, dim, b.to(cuda_device), out_dtype=out)
+    xv, wv = (reference_values(v.cpu(), dim).to(cuda_device) for v in (x, w))
+    ref, size = xv @ wv.t() + b.to(cuda_device).double(), xv.abs() @ wv.abs().t()
+    size += b.to(cuda_device).double().abs()
+    assert_within(got, ref, (dim + 2) * 2 * U32 * size + 1.01 * rounding(ref, out) + 1e-30)
+    ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", FLOATS)
+@pytest.mark.parametrize("dim", [9, 33, 301])
+def test_back_from_strided_rows_that_are_not_whole_eights(cuda_device, out, dim):
+    """Rows apart, and bytes between them that would be NaN if they were read as scales."""
+    rows, n = 700, row_bytes(dim)
+    packed = reference_rows(_values(rows, dim, dim))
+    wide = torch.full((rows, n + 48), 255, dtype=torch.uint8, device=cuda_device)
+    wide[:, 16:16 + n] = packed.to(cuda_device)
+    got = ops.mx4_dequantize(wide[:, 16:16 + n], dim, out_dtype=out).cpu()
+    assert torch.equal(got, reference_values(packed, dim).to(out))

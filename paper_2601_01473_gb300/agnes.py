@@ -470,7 +470,8 @@ class Graph:
     def wait(self, stream=None) -> None:
         """Orders ``stream`` (default: the current stream) after every
         hyperbatch still in flight (agnes_wait_hyperbatches)."""
-        _check(lib().agnes_wait_hyperbatches(self._ctx, _stream_handle(stream)), self._ctx)
+        _check(lib().agnes_wait_hyperbatches(self._ctx,
+                                             _stream_handle(stream, self.device)), self._ctx)
 
     def sage_mean_layer(self, hop: int, x: torch.Tensor, w: torch.Tensor, bias=None,
                         out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
@@ -494,7 +495,7 @@ class Graph:
         _check(lib().agnes_sage_mean_layer(
             self._ctx, hop, x.data_ptr(), _DTYPES[x.dtype], rows, d_in, w.data_ptr(),
             bias.data_ptr() if bias is not None else None, d_out, out.data_ptr(),
-            _DTYPES[out_dtype], out.shape[1], _stream_handle(stream)), self._ctx)
+            _DTYPES[out_dtype], out.shape[1], _stream_handle(stream, self.device)), self._ctx)
         return out
 
     def sizes(self, j: int) -> dict:

@@ -115,3 +115,31 @@ def test_a_call_is_ordered_by_the_default_stream_by_its_handle(cuda_device):
     table.fill_(-1)
     assert float(got.sum()) == 8 * 64 * 100_000
     ops.check()
+
+
+def test_a_graphs_default_stream_is_its_devices(monkeypatch):
+    """Without a GPU: whatever device is current, as for prepare."""
+    from paper_2601_01473_gb300 import agnes
+    seen = []
+
+    class Lib:
+        def agnes_wait_hyperbatches(self, ctx, handle):
+            seen.append(handle)
+            return 0
+
+        def agnes_sage_mean_layer(self, *args):
+            seen.append(args[-1])
+            return 0
+
+    device = torch.device("cuda", 1)
+    monkeypatch.setattr(agnes, "lib", Lib)
+    monkeypatch.setattr(torch.cuda, "Stream", _Stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: _Stream(9 if d == device else 4))
+    g = Graph.__new__(Graph)
+    g.device, g._ctx = device, None
+    g.fetch_all = lambda: type("Hyperbatch", (), {"node_size": torch.ones(2, 3)})
+    g.wait()
+    g.sage_mean_layer(0, torch.zeros(3, 2, 4), torch.zeros(2, 8, dtype=torch.float16))
+    assert seen == [9, 9]
+    g.wait(_Stream(6, device))
+    assert seen[2] == 6

@@ -131,9 +131,11 @@ agnes_status agnes_distill_grad(const void* logits, int32_t logits_dtype, int64_
                                 int32_t out_dtype, int64_t out_stride, int32_t* status,
                                 void* cuda_stream);
 
-/* Both in one call, for a training step that knows its rows' weights: the
- * logits are read from memory once (up to 8 CTAs' shared memory a row, 1.6 MB).
- * Arguments, in-place use and errors as above. */
+/* Both in one call, for a training step that knows its rows' weights.  Rows of
+ * up to 1.6 MB (8 CTAs' shared memory) are kept there and read from memory once;
+ * short ones (up to 512 classes, 8192 where rows are many) are read twice, the
+ * second time from L2 as far as it holds them.  Arguments, in-place use and
+ * errors as above. */
 agnes_status agnes_distill_loss_grad(const void* logits, int32_t logits_dtype,
                                      int64_t logits_stride, int64_t rows, int64_t classes,
                                      const void* teacher, int32_t teacher_dtype, const void* index,

@@ -557,7 +557,8 @@ distill_kernel(DistillArgs a) {
 }
 
 // Short rows, a warp to each: nothing to join but its lanes, and no barrier.  The row is
-// read again for the gradient, from L1 or L2.
+// read again for the gradient: from L1 or L2 as far as they hold the rows in flight, from
+// memory past that (fp32 rows of 8192 classes and many of them, is_short).
 constexpr int kShortWarps = 8;
 
 template <typename T, typename TOut, int kMode>
@@ -623,7 +624,8 @@ struct Shape {
 // step: 305 us, 396 with four of 50 KB), eight of 26 KB where nothing is joined (the
 // gradient alone: 303 us, 370 with 64 KB).  Threads by what is left for each, and where
 // every SM has CTAs enough: 4096 rows of 10,007 fp16 classes, a step: 128 42 us, 256 58,
-// 512 76; 64 rows of 131,072 want 256.
+// 512 76; 64 rows of 131,072 want 256.  The limits lie between those shapes and were not
+// measured one by one.
 Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int num_sms) {
   Shape s = {};
   const auto slice_of = [&](int64_t ranks) { return ceil_div(ceil_div(classes, ranks), 64) * 64; };
@@ -653,7 +655,10 @@ Shape distill_shape(int64_t rows, int64_t classes, int64_t size, int mode, int n
 // rows are where there are too few of them to fill the SMs.  With the gradient, up to
 // 8192 classes (4096 rows of 6000 fp16 classes, a step: 30 us, 34 by CTAs; of 10,007: 56
 // and 42); for the loss alone, which reads each row once, up to 65,536 (8192 rows of
-// 50,000 bf16 classes: 145 us, 188 by CTAs).
+// 50,000 bf16 classes: 145 us, 188 by CTAs).  The limit is in classes, and fp32 rows of
+// many classes, which are twice as long, would be better off by CTAs: a step of 16,384 rows
+// of 1000 42 us (88 by CTAs) and of 2000 67 (95), but of 8192 rows of 4096 77 (63), of 6000
+// 120 (70), of 8192 159 (89); in fp16 of 4096 35 (54), of 6000 58 (62), of 8192 80 (71).
 bool is_short(int64_t rows, int64_t classes, int mode, int num_sms) {
   const int64_t most = mode == kLoss ? 65536 : 8192;
   return classes <= 512 || (classes <= most && rows >= 8 * num_sms);

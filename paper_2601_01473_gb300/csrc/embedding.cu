@@ -1038,7 +1038,11 @@ cudaError_t launch_sum(SumArgs a, int32_t* heads, cudaStream_t st) {
 // A warp to a row where the row has 32 columns or more: half a warp to a row has
 // the two halves end their rows at different tokens, one after the other (1.0M fp16
 // rows of 128, the whole gradient at the time: 4 columns a lane 258 us, 8 a lane in half
-// a warp 265).  More columns a lane where a row is longer, as few as it needs.
+// a warp 265).  More columns a lane where a row is longer: of vectors of one or two
+// elements 1, 2, 5 or 10, whichever is the first that covers the row (10 covers 301 single
+// elements; lanes past the row's end load its first column and store nothing), of wider
+// ones 1, 2 or 3.  What is longer takes several column tiles, each with a pass of its own
+// over the tokens, of wide vectors with one column a lane (not measured against more).
 template <typename TIn, typename TOut, int kVec>
 cudaError_t launch_sum_lanes(const SumArgs& a, int32_t* heads, cudaStream_t st) {
   if constexpr (kVec > 1) {

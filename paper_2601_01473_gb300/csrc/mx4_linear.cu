@@ -13,12 +13,16 @@
 //   the epilogue warps read the accumulator, add the bias, round, and have the TMA
 //                     store it from shared memory.
 // Rows of up to 512 values: a CTA keeps to one tile of columns and its weights stay in
-// shared and tensor memory, so a tile costs the copy of x's rows alone.
+// shared and tensor memory, so a tile costs the copy of x's rows alone; the grid is then a
+// multiple of the tiles across, which leaves SMs idle where those are many (launch_linear).
 //
 // Short rows are bound by the output's stores: 786,432 rows of 128 to 256 columns in
-// fp16 take 92 us, a memset of the same 402 MB 102 us.  Long rows are bound by the
-// operands' way from L2 (64 values of x or w meet 128 of the other): 6,000 x 1024 to
-// 4096 columns 35 us, 1430 TFLOP/s.  Tried without gain: two tiles of columns to each
+// fp16 take 92 us, a memset of the same 402 MB 102 us.  Longer rows are bound by no rate:
+// 6,000 x 1024 to 4096 columns take 35 us, 1430 TFLOP/s, with the tensor pipe active 16% of
+// the time, L2 at 17% of its rate and DRAM at 2%; 100,000 x 300 to 600 columns 51 us with
+// 10%, 19% and 19%.  What is left is how long a tile's chain of stages takes: the copies and
+// scales on their way, the products, the epilogue, of which a CTA has few at a time.
+// Tried without gain: two tiles of columns to each
 // stage of x with three accumulators taken in turn by the two sets of epilogue warps
 // (93 us; long rows 15% slower), three sets (97 us).
 // Every wait is bounded (mbarrier.cuh).  Rows and columns past the matrices' ends
@@ -751,6 +755,11 @@ cudaError_t launch_linear(LinearArgs a, int device, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int num_sms = op_num_sms(device);
   const int64_t tiles_m = ceil_div(a.rows, kTile), tiles_n = ceil_div(a.width, kTile);
+  // Resident or not, 50,000 rows to fp16 (us): of 128 values to 256 columns 13 and 17, 3328
+  // 86 and 109, 6656 183 and 210, 9856 (77 of the 152 SMs at work) 338 and 311; of 512
+  // values to 3328 columns 130 and 113, 6656 308 and 216, 9856 606 and 317; 100,000 rows of
+  // 300 to 600 51 and 54.  So a narrower rule would serve wide outputs better, those of
+  // rows of two stages above all.
   a.resident = ceil_div(a.blocks, 8) <= kResidentStages && tiles_n <= num_sms;
   int64_t grid = num_sms;
   if (a.resident) grid = num_sms / tiles_n * tiles_n;  // a CTA's columns stay the same

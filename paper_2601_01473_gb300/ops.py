@@ -2,7 +2,9 @@
 (include/agnes_ops.h): learned node embeddings with their gradient,
 distillation from a teacher's top logits, and feature rows in microscaled 4-bit
 floating point.  Argument marshalling only; each call runs the library's CUDA
-kernels on the current stream (or ``stream``) and returns without waiting.
+kernels on the current stream (or ``stream``) and returns without waiting.  Results
+are no part of autograd's graph, whatever the arguments require: a training step calls
+the gradients itself, or from the backward of its own ``autograd.Function``.
 
 What a kernel finds wrong with its data (an id past the end of its table, a wait
 that ran out) is kept on the device, in the int32 tensor ``status`` if one is

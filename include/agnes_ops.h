@@ -1,9 +1,11 @@
 /*
  * agnes_ops.h -- C ABI of the operators that a model trained on prepared
  * hyperbatches needs next to them: learned node embeddings (lookup and
- * gradient), distillation from a teacher's top logits (loss and gradient), and
+ * gradient), distillation from a teacher's top logits (loss and gradient),
  * feature rows in microscaled 4-bit floating point (quantisation, and their
- * product with 4-bit weights).  They need no ctx.  The paper (arXiv
+ * product with 4-bit weights), and for deeper models rows in 8 bits (their
+ * product with 8-bit weights and its gradients, nonlinearities that keep their
+ * input in 8 bits) and the norms around a residual block.  They need no ctx.  The paper (arXiv
  * 2601.01473) has no counterpart; the student it trains is the user's model.
  *
  * Conventions, beside those of agnes.h: all work of a call is enqueued on
@@ -15,7 +17,7 @@
  *
  * Element types are AGNES_F32, AGNES_F16 or AGNES_BF16, each argument's own;
  * arithmetic is in fp32 and each output value is rounded once, to nearest even.
- * Strides are in elements (bytes for 4-bit rows) and may exceed the row's
+ * Strides are in elements (bytes for 4-bit and 8-bit rows) and may exceed the row's
  * length; a row's elements are adjacent.
  *
  * status: an optional int32 (4-byte aligned) in device memory.  What a kernel finds wrong with
@@ -182,6 +184,166 @@ agnes_status agnes_mx4_linear(const void* x, int64_t x_stride, int64_t rows, con
                               int64_t w_stride, int64_t width, int64_t dim, const float* bias,
                               void* out, int32_t out_dtype, int64_t out_stride, int32_t* status,
                               void* cuda_stream);
+
+/* Rows in 8 bits, for features and for activations that are kept for a backward
+ * pass.  A row of dim values is int8_row_bytes(dim) bytes: dim whole numbers q
+ * from -127 to 127, zeros, and in the last four bytes of a multiple of 16 a scale
+ * s (fp32); it stands for q s.  Rows are 16-byte aligned, a multiple of 16 bytes
+ * apart.  So a matrix of them can be loaded as a graph's features (row_bytes / 2
+ * "fp16" values a row): they are gathered byte for byte.  1 <= dim <= 2^17,
+ * 0 <= rows < 2^31 - 255. */
+#define AGNES_INT8_ROWS 3 /* an output's type: 8-bit rows, its stride in bytes */
+agnes_status agnes_int8_row_bytes(int64_t dim, int64_t* bytes);
+
+/* Rounds rows of dim values of dtype (stride apart) to 8-bit rows (out_stride
+ * bytes apart): s is the row's largest magnitude / 127 in fp32, rounded up to
+ * eight significant bits (a bfloat16 value), and q = round(x (1 / s)), the inverse
+ * and the product in fp32, to nearest even.  A row whose largest magnitude is
+ * below 2^-100 is zeros with scale 0; one with an infinity or NaN gets scale NaN
+ * and zeros: it stands for NaN.  Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_int8_quantize(const void* x, int32_t dtype, int64_t stride, int64_t rows,
+                                 int64_t dim, void* out, int64_t out_stride, void* cuda_stream);
+
+/* The values that 8-bit rows (stride bytes apart) stand for, rounded to dtype.  As
+ * s is rounded up, 127 s may lie past the type's largest number where the row did
+ * not: such a value becomes that number.  Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_int8_dequantize(const void* x, int64_t stride, int64_t rows, int64_t dim,
+                                   void* out, int32_t dtype, int64_t out_stride,
+                                   void* cuda_stream);
+
+/* out[r][j] = sum_i x[r][i] w[j][i] (+ bias[j]): 8-bit rows times 8-bit weights,
+ * with a scale for each row of x (a token) and each row of w (a channel):
+ * s_x[r] s_w[j] times the sum of the whole numbers' products.  That sum is exact
+ * up to 2^24 and in fp32 beyond (for up to AGNES_INT8_FEW_ROWS rows always exact).
+ *  x      rows 8-bit rows of dim values, x_stride bytes apart.
+ *  w      width 8-bit rows of dim values, w_stride bytes apart.
+ *  bias   width floats, or NULL.
+ *  out    rows x width of out_dtype, out_stride apart.
+ *  workspace  at least agnes_int8_linear_workspace bytes, 256-byte aligned (NULL
+ *         where that is 0); its contents are not kept.
+ *  status AGNES_OP_TIMEOUT where a wait inside the kernel ran out.
+ * 0 <= rows, 0 <= width < 2^31 - 255.  Errors: EINVAL, ERANGE, ECUDA. */
+#define AGNES_INT8_FEW_ROWS 8
+agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, const void* w,
+                               int64_t w_stride, int64_t width, int64_t dim, const float* bias,
+                               void* out, int32_t out_dtype, int64_t out_stride, void* workspace,
+                               int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+agnes_status agnes_int8_linear_workspace(int64_t rows, int64_t width, int64_t dim, int64_t* bytes);
+
+/* The gradient of agnes_int8_linear to the weights, from the rows that the layer
+ * keeps in 8 bits, and to the bias:
+ *   out[j][i] = sum_r grad[r][j] x[r][i],  dbias[j] = sum_r grad[r][j].
+ * Products are exact to 2^-24, sums are in fp32 over an order that depends on the
+ * sizes only: the result is the same, bit by bit, each time.
+ *  grad   rows x width of grad_dtype, grad_stride apart.
+ *  out    width x dim of out_dtype, out_stride apart (zeros where rows is 0).
+ *  dbias  width floats, or NULL.
+ *  workspace  at least agnes_int8_linear_grad_weight_workspace bytes, 256-byte
+ *         aligned; its contents are not kept.
+ * Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_int8_linear_grad_weight(const void* grad, int32_t grad_dtype,
+                                           int64_t grad_stride, int64_t rows, int64_t width,
+                                           const void* x, int64_t x_stride, int64_t dim, void* out,
+                                           int32_t out_dtype, int64_t out_stride, float* dbias,
+                                           void* workspace, int64_t workspace_bytes,
+                                           int32_t* status, void* cuda_stream);
+agnes_status agnes_int8_linear_grad_weight_workspace(int64_t rows, int64_t width, int64_t dim,
+                                                     int32_t grad_dtype, int64_t* bytes);
+
+/* The gradient of agnes_int8_linear to its input: out[r][i] = sum_j grad[r][j] w[j][i].
+ *  out    rows x dim of out_dtype, out_stride apart.
+ *  workspace  at least agnes_int8_linear_grad_input_workspace bytes, 256-byte
+ *         aligned; its contents are not kept.
+ * Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
+                                          int64_t grad_stride, int64_t rows, int64_t width,
+                                          const void* w, int64_t w_stride, int64_t dim, void* out,
+                                          int32_t out_dtype, int64_t out_stride, void* workspace,
+                                          int64_t workspace_bytes, int32_t* status,
+                                          void* cuda_stream);
+agnes_status agnes_int8_linear_grad_input_workspace(int64_t rows, int64_t width, int64_t dim,
+                                                    int32_t grad_dtype, int64_t* bytes);
+
+/* A nonlinearity, gated or not, that keeps its input in 8 bits for its backward
+ * pass: out = f(x), or f(x[:, :dim]) x[:, dim:] where gated (x has 2 dim columns
+ * then).  f is relu, silu (v / (1 + exp -v)) or gelu (v Phi(v)).
+ *  x      rows x dim (2 dim) of dtype, stride apart.
+ *  out    rows x dim of the same type, out_stride apart; or, with out_dtype
+ *         AGNES_INT8_ROWS, 8-bit rows out_stride bytes apart, for a layer that
+ *         takes them.
+ *  kept   8-bit rows of x, kept_stride bytes apart; where gated the two halves are
+ *         rows of their own side by side (2 int8_row_bytes(dim) bytes).  NULL: not
+ *         kept (serving).
+ * Errors: EINVAL, ERANGE, ECUDA. */
+#define AGNES_F_RELU 0
+#define AGNES_F_SILU 1
+#define AGNES_F_GELU 2
+agnes_status agnes_activation(const void* x, int32_t dtype, int64_t stride, int64_t rows,
+                              int64_t dim, int32_t f, int32_t gated, void* out, int32_t out_dtype,
+                              int64_t out_stride, void* kept, int64_t kept_stride,
+                              void* cuda_stream);
+
+/* Its gradient to x at the kept values k: grad f'(k), or where gated grad f'(k_1) k_2
+ * and grad f(k_1) side by side.  relu' is 0 at 0.  A kept row that stands for NaN
+ * has a gradient of NaN.
+ *  grad   rows x dim of grad_dtype, grad_stride apart.
+ *  out    rows x dim (2 dim) of out_dtype, out_stride apart.
+ * Errors: EINVAL, ERANGE, ECUDA. */
+agnes_status agnes_activation_grad(const void* grad, int32_t grad_dtype, int64_t grad_stride,
+                                   const void* kept, int64_t kept_stride, int64_t rows, int64_t dim,
+                                   int32_t f, int32_t gated, void* out, int32_t out_dtype,
+                                   int64_t out_stride, void* cuda_stream);
+
+/* The step between two blocks of a residual network.  With N(v) = v / sqrt(mean v^2
+ * + eps) (AGNES_NORM_RMS) or (v - mean v) / sqrt(var v + eps) (AGNES_NORM_LAYER) of
+ * a row,
+ *   u    = N(branch) after + after_bias, or branch where after is NULL
+ *   sum  = x + scale gate u, rounded to x's type
+ *   next = N(sum) before + before_bias, of the rounded sum.
+ * branch NULL: next of x itself, and no sum.  before NULL: no next.
+ *  x, sum        rows x dim of x_dtype: branch's type, or fp32.
+ *  branch, next  rows x dim of branch_dtype (next_dtype the same, or AGNES_INT8_ROWS:
+ *                8-bit rows, next_stride bytes apart).
+ *  gate          none, dim floats for all rows (AGNES_GATE_COLUMNS), or rows x dim
+ *                of branch_dtype, gate_stride apart (AGNES_GATE_ROWS).
+ *  after, after_bias, before, before_bias  dim floats each; a bias needs its norm.
+ *  sum may be x itself (the same address and stride).
+ * 0 <= rows < 2^31 - 2047, 1 <= dim <= 8192.  Errors: EINVAL, ERANGE, ECUDA. */
+#define AGNES_NORM_RMS 0
+#define AGNES_NORM_LAYER 1
+#define AGNES_GATE_NONE 0
+#define AGNES_GATE_COLUMNS 1
+#define AGNES_GATE_ROWS 2
+agnes_status agnes_residual_norm(const void* x, int32_t x_dtype, int64_t x_stride,
+                                 const void* branch, int32_t branch_dtype, int64_t branch_stride,
+                                 int64_t rows, int64_t dim, const void* gate, int32_t gate_kind,
+                                 int64_t gate_stride, float scale, const float* after,
+                                 const float* after_bias, const float* before,
+                                 const float* before_bias, int32_t kind, float eps, void* sum,
+                                 int64_t sum_stride, void* next, int32_t next_dtype,
+                                 int64_t next_stride, void* cuda_stream);
+
+/* Its gradients, from those of next (d_next, branch's type) and of sum (d_sum, x's
+ * type; NULL: none), and from sum as the forward pass rounded it (x where branch is
+ * NULL).
+ *  dx        rows x dim of x_dtype;  dbranch  rows x dim of branch_dtype.
+ *  dgate     dim floats or rows x dim of branch_dtype, as the gate is.
+ *  dafter, dafter_bias, dbefore, dbefore_bias  dim floats each, or NULL: not computed.
+ * The sums over rows are in fp32, in an order that depends on the sizes and the device
+ * only.
+ *  workspace  at least agnes_residual_norm_grad_workspace bytes, 256-byte aligned; its
+ *         contents are not kept.
+ * Other arguments, limits and errors as agnes_residual_norm. */
+agnes_status agnes_residual_norm_grad(
+    const void* d_next, int64_t d_next_stride, const void* d_sum, int64_t d_sum_stride,
+    const void* sum, int32_t x_dtype, int64_t sum_stride, const void* branch, int32_t branch_dtype,
+    int64_t branch_stride, int64_t rows, int64_t dim, const void* gate, int32_t gate_kind,
+    int64_t gate_stride, float scale, const float* after, const float* after_bias,
+    const float* before, int32_t kind, float eps, void* dx, int64_t dx_stride, void* dbranch,
+    int64_t dbranch_stride, void* dgate, int64_t dgate_stride, float* dafter, float* dafter_bias,
+    float* dbefore, float* dbefore_bias, void* workspace, int64_t workspace_bytes,
+    void* cuda_stream);
+agnes_status agnes_residual_norm_grad_workspace(int64_t rows, int64_t dim, int64_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -165,6 +165,30 @@ SIGNATURES = {
     "agnes_mx4_dequantize": ([_P, _I64, _I64, _I64, _P, _I32, _I64, _P], ctypes.c_int),
     "agnes_mx4_linear": ([_P, _I64, _I64, _P, _I64, _I64, _I64, _P, _P, _I32, _I64, _P, _P],
                          ctypes.c_int),
+    "agnes_int8_row_bytes": ([_I64, ctypes.POINTER(_I64)], ctypes.c_int),
+    "agnes_int8_quantize": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _P], ctypes.c_int),
+    "agnes_int8_dequantize": ([_P, _I64, _I64, _I64, _P, _I32, _I64, _P], ctypes.c_int),
+    "agnes_int8_linear": ([_P, _I64, _I64, _P, _I64, _I64, _I64, _P, _P, _I32, _I64, _P, _I64, _P,
+                           _P], ctypes.c_int),
+    "agnes_int8_linear_workspace": ([_I64, _I64, _I64, ctypes.POINTER(_I64)], ctypes.c_int),
+    "agnes_int8_linear_grad_weight": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64,
+                                       _P, _P, _I64, _P, _P], ctypes.c_int),
+    "agnes_int8_linear_grad_weight_workspace": ([_I64, _I64, _I64, _I32, ctypes.POINTER(_I64)],
+                                                ctypes.c_int),
+    "agnes_int8_linear_grad_input": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64,
+                                      _P, _I64, _P, _P], ctypes.c_int),
+    "agnes_int8_linear_grad_input_workspace": ([_I64, _I64, _I64, _I32, ctypes.POINTER(_I64)],
+                                               ctypes.c_int),
+    "agnes_activation": ([_P, _I32, _I64, _I64, _I64, _I32, _I32, _P, _I32, _I64, _P, _I64, _P],
+                         ctypes.c_int),
+    "agnes_activation_grad": ([_P, _I32, _I64, _P, _I64, _I64, _I64, _I32, _I32, _P, _I32, _I64,
+                               _P], ctypes.c_int),
+    "agnes_residual_norm": ([_P, _I32, _I64, _P, _I32, _I64, _I64, _I64, _P, _I32, _I64, _F32, _P,
+                             _P, _P, _P, _I32, _F32, _P, _I64, _P, _I32, _I64, _P], ctypes.c_int),
+    "agnes_residual_norm_grad": ([_P, _I64, _P, _I64, _P, _I32, _I64, _P, _I32, _I64, _I64, _I64,
+                                  _P, _I32, _I64, _F32, _P, _P, _P, _I32, _F32, _P, _I64, _P, _I64,
+                                  _P, _I64, _P, _P, _P, _P, _P, _I64, _P], ctypes.c_int),
+    "agnes_residual_norm_grad_workspace": ([_I64, _I64, ctypes.POINTER(_I64)], ctypes.c_int),
     "agnes_embedding_grad_workspace": ([_I64, _I64, ctypes.POINTER(_I64)], ctypes.c_int),
     "agnes_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "agnes_last_error": ([_P], ctypes.c_char_p),

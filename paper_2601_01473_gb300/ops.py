@@ -1,7 +1,9 @@
 """The operators of a model that is trained on prepared hyperbatches
 (include/agnes_ops.h): learned node embeddings with their gradient,
-distillation from a teacher's top logits, and feature rows in microscaled 4-bit
-floating point.  Argument marshalling only; each call runs the library's CUDA
+distillation from a teacher's top logits, feature rows in microscaled 4-bit
+floating point, and for deeper models rows in 8 bits with their product and its
+gradients, nonlinearities that keep their input in 8 bits, and the norms around a
+residual block.  Argument marshalling only; each call runs the library's CUDA
 kernels on the current stream (or ``stream``) and returns without waiting.  Results
 are no part of autograd's graph, whatever the arguments require: a training step calls
 the gradients itself, or from the backward of its own ``autograd.Function``.
@@ -28,6 +30,10 @@ from .agnes import AgnesError, _stream_of_handle, lib
 _FLOATS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _INDEXES = {torch.int32: 32, torch.int64: 64}
 BAD_INDEX, TIMEOUT = 1, 2  # AGNES_OP_*
+_INT8_ROWS = 3  # AGNES_INT8_ROWS
+_NONLINEAR = {"relu": 0, "silu": 1, "gelu": 2}  # AGNES_F_*
+_NORMS = {"rms": 0, "layer": 1}  # AGNES_NORM_*
+_NO_GATE, _GATE_COLUMNS, _GATE_ROWS = 0, 1, 2  # AGNES_GATE_*
 
 _status = {}  # device index -> int32 [1]
 
@@ -37,6 +43,29 @@ class RowGrad(NamedTuple):
     ids: torch.Tensor    # int32 [n]: the distinct ids in ascending order, then -1
     rows: torch.Tensor   # [n, dim]: their gradients, then zeros
     count: torch.Tensor  # int32 [1]: how many
+
+
+class NormOutput(NamedTuple):
+    """What goes into the next block."""
+    sum: torch.Tensor | None    # the residual with the block's output added
+    next: torch.Tensor | None   # its norm
+
+
+class NormGrad(NamedTuple):
+    """The gradients to what entered ``residual_norm``; None for what did not."""
+    x: torch.Tensor
+    branch: torch.Tensor | None
+    gate: torch.Tensor | None
+    after: torch.Tensor | None
+    after_bias: torch.Tensor | None
+    before: torch.Tensor | None
+    before_bias: torch.Tensor | None
+
+
+class LinearGrad(NamedTuple):
+    """The gradients to a layer's weights and bias."""
+    weight: torch.Tensor        # [width, dim]
+    bias: torch.Tensor | None   # float32 [width]
 
 
 def _stream_of(stream, device):
@@ -431,3 +460,362 @@ def mx4_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, sta
     if rc:
         _failed(rc)
     return y
+
+
+# ---- 8-bit rows -----------------------------------------------------------------------------
+
+
+def int8_row_bytes(dim: int) -> int:
+    """Bytes of an 8-bit row of ``dim`` values (agnes_int8_row_bytes)."""
+    need = ctypes.c_int64()
+    rc = lib().agnes_int8_row_bytes(dim, ctypes.byref(need))
+    if rc:
+        _failed(rc)
+    return need.value
+
+
+def _rows8(name, t, dim, device=None, halves=1):
+    """(device, rows, row stride in bytes) of a matrix of 8-bit rows: uint8
+    [rows, int8_row_bytes(dim)], or the same bytes as float16 or float32 "features", as a
+    graph gathers them; ``halves`` of them side by side."""
+    if not isinstance(t, torch.Tensor) or t.ndim != 2 or \
+            t.dtype not in (torch.uint8, torch.float16, torch.float32):
+        raise TypeError(f"{name} must be a 2-D tensor of 8-bit rows")
+    n, cols = t.shape
+    step, unit = t.stride()
+    size = t.element_size()
+    if dim < 1 or cols * size != halves * ((dim + 19) // 16 * 16):
+        raise ValueError(f"{name} has rows of {cols * size} bytes, not those of {dim} values")
+    if n <= 1:
+        step = cols  # there is no next row
+    if (unit != 1 or step < cols) and n:
+        raise ValueError(f"{name} must have adjacent bytes in each row")
+    return _on(name, t, device), n, step * size
+
+
+def _new_rows8(rows, dim, device, halves=1):
+    step = halves * int8_row_bytes(dim)
+    return torch.empty((rows, step), dtype=torch.uint8, device=device), step
+
+
+def int8_quantize(x, out=None, stream=None):
+    """Rows of ``x`` [rows, dim] rounded to 8-bit rows (agnes_int8_quantize): uint8
+    [rows, int8_row_bytes(dim)].  Activations, and weights [width, dim] of
+    ``int8_linear``; ``.view(torch.float16)`` of them makes a graph's features."""
+    if stream is not None:
+        return _on_stream(stream, int8_quantize, x, out)
+    device, rows, dim, step = _rows("x", x)
+    if out is None:
+        out, out_step = _new_rows8(rows, dim, device)
+    else:
+        _, n, out_step = _rows8("out", out, dim, device)
+        if n != rows:
+            raise ValueError(f"out has {n} rows, not {rows}")
+    rc = lib().agnes_int8_quantize(x.data_ptr(), _FLOATS[x.dtype], step, rows, dim,
+                                   out.data_ptr(), out_step, _stream(device))
+    if rc:
+        _failed(rc)
+    return out
+
+
+def int8_dequantize(x, dim: int, out_dtype=torch.float32, out=None, stream=None):
+    """The values [rows, dim] that 8-bit rows stand for (agnes_int8_dequantize)."""
+    if stream is not None:
+        return _on_stream(stream, int8_dequantize, x, dim, out_dtype, out)
+    device, rows, step = _rows8("x", x, dim)
+    y, code, out_step = _output(out, rows, dim, out_dtype if out is None else None, device)
+    rc = lib().agnes_int8_dequantize(x.data_ptr(), step, rows, dim, y.data_ptr(), code, out_step,
+                                     _stream(device))
+    if rc:
+        _failed(rc)
+    return y
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(entry, *sizes) -> int:
+    need = ctypes.c_int64()
+    rc = getattr(lib(), entry)(*sizes, ctypes.byref(need))
+    if rc:
+        _failed(rc)
+    return need.value
+
+
+def _workspace(device, entry, *sizes):
+    """(the tensor that holds it, its address, its bytes); None where none is needed."""
+    n = _workspace_bytes(entry, *sizes)
+    if n == 0:
+        return None, None, 0
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), n
+
+
+def int8_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, status=None,
+                stream=None):
+    """``x @ w.T + bias`` of 8-bit rows (agnes_int8_linear): ``x`` [rows, bytes], for example a
+    minibatch's gathered features or ``int8_quantize`` of activations, ``w`` [width, bytes],
+    both of ``dim`` values a row; ``bias`` float32 [width] or None.  Returns [rows, width]."""
+    if stream is not None:
+        return _on_stream(stream, int8_linear, x, w, dim, bias, out_dtype, out, status)
+    device, rows, step = _rows8("x", x, dim)
+    _, width, w_step = _rows8("w", w, dim, device)
+    at = _vector("bias", bias, width, device)
+    y, code, out_step = _output(out, rows, width, out_dtype if out is None else None, device)
+    ws, ws_at, ws_bytes = _workspace(device, "agnes_int8_linear_workspace", rows, width, dim)
+    rc = lib().agnes_int8_linear(x.data_ptr(), step, rows, w.data_ptr(), w_step, width, dim, at,
+                                 y.data_ptr(), code, out_step, ws_at, ws_bytes,
+                                 _status_word(status, device), _stream(device))
+    if rc:
+        _failed(rc)
+    return y
+
+
+def int8_linear_grad_weight(grad, x, dim: int, bias: bool = True, out_dtype=torch.float32,
+                            out=None, status=None, stream=None) -> LinearGrad:
+    """The gradient of ``int8_linear`` to its weights and bias
+    (agnes_int8_linear_grad_weight), from ``grad`` [rows, width] and the rows ``x`` that the
+    layer kept in 8 bits: (``grad.T @ x`` [width, dim], ``grad.sum(0)`` or None)."""
+    if stream is not None:
+        return _on_stream(stream, int8_linear_grad_weight, grad, x, dim, bias, out_dtype, out,
+                          status)
+    device, rows, width, step = _rows("grad", grad)
+    _, n, x_step = _rows8("x", x, dim, device)
+    if n != rows:
+        raise ValueError(f"x has {n} rows, grad {rows}")
+    y, code, out_step = _output(out, width, dim, out_dtype if out is None else None, device)
+    db = torch.empty(width, dtype=torch.float32, device=device) if bias else None
+    kind = _FLOATS[grad.dtype]
+    ws, ws_at, ws_bytes = _workspace(device, "agnes_int8_linear_grad_weight_workspace", rows,
+                                     width, dim, kind)
+    rc = lib().agnes_int8_linear_grad_weight(
+        grad.data_ptr(), kind, step, rows, width, x.data_ptr(), x_step, dim, y.data_ptr(), code,
+        out_step, db.data_ptr() if bias else None, ws_at, ws_bytes, _status_word(status, device),
+        _stream(device))
+    if rc:
+        _failed(rc)
+    return LinearGrad(y, db)
+
+
+def int8_linear_grad_input(grad, w, dim: int, out_dtype=None, out=None, status=None, stream=None):
+    """The gradient of ``int8_linear`` to its input (agnes_int8_linear_grad_input):
+    ``grad @ w`` [rows, dim] of ``out_dtype`` (grad's by default), from ``grad``
+    [rows, width] and the 8-bit weights ``w``."""
+    if stream is not None:
+        return _on_stream(stream, int8_linear_grad_input, grad, w, dim, out_dtype, out, status)
+    device, rows, width, step = _rows("grad", grad)
+    _, n, w_step = _rows8("w", w, dim, device)
+    if n != width:
+        raise ValueError(f"w has {n} rows, grad {width} columns")
+    if out is None and out_dtype is None:
+        out_dtype = grad.dtype
+    y, code, out_step = _output(out, rows, dim, out_dtype, device)
+    kind = _FLOATS[grad.dtype]
+    ws, ws_at, ws_bytes = _workspace(device, "agnes_int8_linear_grad_input_workspace", rows, width,
+                                     dim, kind)
+    rc = lib().agnes_int8_linear_grad_input(
+        grad.data_ptr(), kind, step, rows, width, w.data_ptr(), w_step, dim, y.data_ptr(), code,
+        out_step, ws_at, ws_bytes, _status_word(status, device), _stream(device))
+    if rc:
+        _failed(rc)
+    return y
+
+
+# ---- nonlinearities kept in 8 bits ----------------------------------------------------------
+
+
+def _nonlinear(f) -> int:
+    code = _NONLINEAR.get(f)
+    if code is None:
+        raise ValueError(f"f must be one of {', '.join(_NONLINEAR)}, not {f!r}")
+    return code
+
+
+def activation(x, f: str = "silu", gated: bool = False, keep: bool = True, rows8: bool = False,
+               stream=None):
+    """``f(x)``, or ``f(x[:, :dim]) * x[:, dim:]`` where ``gated``, with f "relu", "silu" or
+    "gelu" (agnes_activation).  Returns (y, kept): y [rows, dim] of x's type, or with
+    ``rows8`` as 8-bit rows for ``int8_linear``; kept is x in 8 bits, for
+    ``activation_grad``, or None without ``keep`` (serving)."""
+    if stream is not None:
+        return _on_stream(stream, activation, x, f, gated, keep, rows8)
+    device, rows, cols, step = _rows("x", x)
+    code = _nonlinear(f)
+    if gated and (cols % 2 or not cols):
+        raise ValueError(f"x must have two halves, not {cols} columns")
+    dim, halves = (cols // 2, 2) if gated else (cols, 1)
+    if rows8:
+        y, out_step = _new_rows8(rows, dim, device)
+    else:
+        y, out_step = torch.empty((rows, dim), dtype=x.dtype, device=device), dim
+    kept, kept_step = _new_rows8(rows, dim, device, halves) if keep else (None, 0)
+    rc = lib().agnes_activation(
+        x.data_ptr(), _FLOATS[x.dtype], step, rows, dim, code, int(gated), y.data_ptr(),
+        _INT8_ROWS if rows8 else _FLOATS[x.dtype], out_step, kept.data_ptr() if keep else None,
+        kept_step, _stream(device))
+    if rc:
+        _failed(rc)
+    return y, kept
+
+
+def activation_grad(grad, kept, f: str = "silu", gated: bool = False, out_dtype=None, out=None,
+                    stream=None):
+    """The gradient of ``activation`` to x, from ``grad`` [rows, dim] and what it kept
+    (agnes_activation_grad): [rows, dim], or [rows, 2 * dim] where ``gated``, of
+    ``out_dtype`` (grad's by default)."""
+    if stream is not None:
+        return _on_stream(stream, activation_grad, grad, kept, f, gated, out_dtype, out)
+    device, rows, dim, step = _rows("grad", grad)
+    code, halves = _nonlinear(f), 2 if gated else 1
+    _, n, kept_step = _rows8("kept", kept, dim, device, halves)
+    if n != rows:
+        raise ValueError(f"kept has {n} rows, grad {rows}")
+    if out is None and out_dtype is None:
+        out_dtype = grad.dtype
+    y, out_code, out_step = _output(out, rows, halves * dim, out_dtype, device)
+    rc = lib().agnes_activation_grad(
+        grad.data_ptr(), _FLOATS[grad.dtype], step, kept.data_ptr(), kept_step, rows, dim, code,
+        int(gated), y.data_ptr(), out_code, out_step, _stream(device))
+    if rc:
+        _failed(rc)
+    return y
+
+
+# ---- norms around a residual block ----------------------------------------------------------
+
+
+def _vector(name, t, n, device):
+    """The address of a float32 vector [n], or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.shape != (n,) or \
+            not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous float32 tensor [{n}]")
+    _on(name, t, device)
+    return t.data_ptr()
+
+
+def _matrix(name, t, rows, dim, dtype, device):
+    """(address, row stride) of a matrix [rows, dim] of ``dtype``."""
+    _, n, cols, step = _rows(name, t, device)
+    if (n, cols) != (rows, dim) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {(rows, dim)} of {dtype}, not {tuple(t.shape)} of "
+                         f"{t.dtype}")
+    return t.data_ptr(), step
+
+
+def _gate_arguments(gate, rows, dim, dtype, device):
+    """(address, kind, row stride)"""
+    if gate is None:
+        return None, _NO_GATE, 0
+    if isinstance(gate, torch.Tensor) and gate.ndim == 1:
+        return _vector("gate", gate, dim, device), _GATE_COLUMNS, 0
+    at, step = _matrix("gate", gate, rows, dim, dtype, device)
+    return at, _GATE_ROWS, step
+
+
+def _norm_kind(kind) -> int:
+    code = _NORMS.get(kind)
+    if code is None:
+        raise ValueError(f"kind must be one of {', '.join(_NORMS)}, not {kind!r}")
+    return code
+
+
+def residual_norm(x, branch=None, gate=None, scale: float = 1.0, after=None, after_bias=None,
+                  before=None, before_bias=None, kind: str = "rms", eps: float = 1e-5,
+                  rows8: bool = False, next_dtype=None, out=None, stream=None) -> NormOutput:
+    """The step between two blocks of a residual network (agnes_residual_norm): the block's
+    output ``branch`` [rows, dim] normalised (where ``after`` is given), gated, scaled and
+    added to the residual ``x``, and the sum normalised for the next block (where ``before``
+    is given).  Returns (sum, next).
+
+    ``x`` has branch's type or is float32, and so is sum; ``next`` has branch's type, or is
+    8-bit rows with ``rows8``.  ``gate``: float32 [dim], or [rows, dim] of branch's type.
+    ``after``, ``before`` and their biases: float32 [dim].  ``kind``: "rms" or "layer".
+    Without a branch, sum is x and next its norm, of ``next_dtype`` (x's by default).
+    ``out``: sum, written instead of a new tensor; it may be ``x``."""
+    if stream is not None:
+        return _on_stream(stream, residual_norm, x, branch, gate, scale, after, after_bias, before,
+                          before_bias, kind, eps, rows8, next_dtype, out)
+    device, rows, dim, step = _rows("x", x)
+    if branch is None:
+        b_at, b_step, b_type = None, 0, next_dtype or x.dtype
+        if out is not None:
+            raise ValueError("out without a branch: there is no new sum")
+        if b_type not in _FLOATS:
+            raise TypeError(f"{b_type} is not float32, float16 or bfloat16")
+    else:
+        b_type = branch.dtype if isinstance(branch, torch.Tensor) else None
+        b_at, b_step = _matrix("branch", branch, rows, dim, b_type, device)
+        if next_dtype not in (None, b_type):
+            raise TypeError("next has branch's type")
+    g_at, g_kind, g_step = _gate_arguments(gate, rows, dim, b_type, device)
+    total, sum_step = x, step
+    if branch is not None:
+        total, _, sum_step = _output(out, rows, dim, x.dtype, device)
+    code, n, n_step, n_type = _FLOATS[b_type], None, 0, 0
+    if before is not None:
+        if rows8:
+            n, n_step = _new_rows8(rows, dim, device)
+            n_type = _INT8_ROWS
+        else:
+            n, n_step, n_type = torch.empty((rows, dim), dtype=b_type, device=device), dim, code
+    rc = lib().agnes_residual_norm(
+        x.data_ptr(), _FLOATS[x.dtype], step, b_at, code, b_step, rows, dim, g_at, g_kind, g_step,
+        scale, _vector("after", after, dim, device), _vector("after_bias", after_bias, dim, device),
+        _vector("before", before, dim, device), _vector("before_bias", before_bias, dim, device),
+        _norm_kind(kind), eps, total.data_ptr(), sum_step, n.data_ptr() if n is not None else None,
+        n_type, n_step, _stream(device))
+    if rc:
+        _failed(rc)
+    return NormOutput(total, n)
+
+
+def residual_norm_grad(grad_next, grad_sum, sum, branch=None, gate=None, scale: float = 1.0,
+                       after=None, after_bias=None, before=None, before_bias=None,
+                       kind: str = "rms", eps: float = 1e-5, stream=None) -> NormGrad:
+    """The gradients of ``residual_norm`` (agnes_residual_norm_grad): ``grad_next`` (branch's
+    type; None without ``before``) and ``grad_sum`` (sum's type, or None) are those of its
+    results, ``sum`` is the sum that it returned (x without a branch); the others as they
+    were."""
+    if stream is not None:
+        return _on_stream(stream, residual_norm_grad, grad_next, grad_sum, sum, branch, gate, scale,
+                          after, after_bias, before, before_bias, kind, eps)
+    device, rows, dim, step = _rows("sum", sum)
+    if branch is not None:
+        b_type = branch.dtype if isinstance(branch, torch.Tensor) else None
+        b_at, b_step = _matrix("branch", branch, rows, dim, b_type, device)
+    else:
+        b_at, b_step = None, 0
+        b_type = grad_next.dtype if isinstance(grad_next, torch.Tensor) else None
+    if (grad_next is None) != (before is None):
+        raise ValueError("grad_next goes with before")
+    dn_at, dn_step = (None, 0) if grad_next is None else \
+        _matrix("grad_next", grad_next, rows, dim, b_type, device)
+    ds_at, ds_step = (None, 0) if grad_sum is None else \
+        _matrix("grad_sum", grad_sum, rows, dim, sum.dtype, device)
+    g_at, g_kind, g_step = _gate_arguments(gate, rows, dim, b_type, device)
+    vectors = [_vector(name, v, dim, device) for name, v in
+               (("after", after), ("after_bias", after_bias), ("before", before),
+                ("before_bias", before_bias))]
+
+    def matrix(dtype):
+        return torch.empty((rows, dim), dtype=dtype, device=device)
+
+    def like(v):
+        return None if v is None else torch.empty(dim, dtype=torch.float32, device=device)
+
+    dx, db = matrix(sum.dtype), None if branch is None else matrix(b_type)
+    dgate = matrix(b_type) if g_kind == _GATE_ROWS else like(gate)
+    sums = [like(v) for v in (after, after_bias, before, before_bias)]
+    ws, ws_at, ws_bytes = _workspace(device, "agnes_residual_norm_grad_workspace", rows, dim)
+
+    def at(t):
+        return None if t is None else t.data_ptr()
+
+    rc = lib().agnes_residual_norm_grad(
+        dn_at, dn_step, ds_at, ds_step, sum.data_ptr(), _FLOATS[sum.dtype], step, b_at,
+        _FLOATS.get(b_type, -1), b_step, rows, dim, g_at, g_kind, g_step, scale, *vectors[:3],
+        _norm_kind(kind), eps, dx.data_ptr(), dim, at(db), dim, at(dgate), dim,
+        *(at(t) for t in sums), ws_at, ws_bytes, _stream(device))
+    if rc:
+        _failed(rc)
+    return NormGrad(dx, db, dgate, *sums)

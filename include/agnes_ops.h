@@ -213,8 +213,8 @@ agnes_status agnes_int8_dequantize(const void* x, int64_t stride, int64_t rows, 
 
 /* out[r][j] = sum_i x[r][i] w[j][i] (+ bias[j]): 8-bit rows times 8-bit weights,
  * with a scale for each row of x (a token) and each row of w (a channel):
- * s_x[r] s_w[j] times the sum of the whole numbers' products.  That sum is exact
- * up to 2^24 and in fp32 beyond (for up to AGNES_INT8_FEW_ROWS rows always exact).
+ * s_x[r] s_w[j] times the sum of the whole numbers' products, which is exact up to
+ * 2^24 and in fp32 beyond.
  *  x      rows 8-bit rows of dim values, x_stride bytes apart.
  *  w      width 8-bit rows of dim values, w_stride bytes apart.
  *  bias   width floats, or NULL.
@@ -222,7 +222,8 @@ agnes_status agnes_int8_dequantize(const void* x, int64_t stride, int64_t rows, 
  *  workspace  at least agnes_int8_linear_workspace bytes, 256-byte aligned (NULL
  *         where that is 0); its contents are not kept.
  *  status AGNES_OP_TIMEOUT where a wait inside the kernel ran out.
- * 0 <= rows, 0 <= width < 2^31 - 255.  Errors: EINVAL, ERANGE, ECUDA. */
+ * 0 <= rows, 0 <= width < 2^29 (here and in the gradients).
+ * Errors: EINVAL, ERANGE, ECUDA. */
 #define AGNES_INT8_FEW_ROWS 8
 agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, const void* w,
                                int64_t w_stride, int64_t width, int64_t dim, const float* bias,
@@ -233,13 +234,15 @@ agnes_status agnes_int8_linear_workspace(int64_t rows, int64_t width, int64_t di
 /* The gradient of agnes_int8_linear to the weights, from the rows that the layer
  * keeps in 8 bits, and to the bias:
  *   out[j][i] = sum_r grad[r][j] x[r][i],  dbias[j] = sum_r grad[r][j].
- * Products are exact to 2^-24, sums are in fp32 over an order that depends on the
+ * Products are exact to 2^-21, sums are in fp32 over an order that depends on the
  * sizes only: the result is the same, bit by bit, each time.
  *  grad   rows x width of grad_dtype, grad_stride apart.
  *  out    width x dim of out_dtype, out_stride apart (zeros where rows is 0).
  *  dbias  width floats, or NULL.
  *  workspace  at least agnes_int8_linear_grad_weight_workspace bytes, 256-byte
- *         aligned; its contents are not kept.
+ *         aligned; its contents are not kept.  `direct` of that entry: 1 where grad is
+ *         bfloat16, 16-byte aligned and its rows a multiple of 16 bytes apart, so that it
+ *         is read as it is; else 0.
  * Errors: EINVAL, ERANGE, ECUDA. */
 agnes_status agnes_int8_linear_grad_weight(const void* grad, int32_t grad_dtype,
                                            int64_t grad_stride, int64_t rows, int64_t width,
@@ -248,12 +251,13 @@ agnes_status agnes_int8_linear_grad_weight(const void* grad, int32_t grad_dtype,
                                            void* workspace, int64_t workspace_bytes,
                                            int32_t* status, void* cuda_stream);
 agnes_status agnes_int8_linear_grad_weight_workspace(int64_t rows, int64_t width, int64_t dim,
-                                                     int32_t grad_dtype, int64_t* bytes);
+                                                     int32_t grad_dtype, int32_t direct,
+                                                     int64_t* bytes);
 
 /* The gradient of agnes_int8_linear to its input: out[r][i] = sum_j grad[r][j] w[j][i].
  *  out    rows x dim of out_dtype, out_stride apart.
  *  workspace  at least agnes_int8_linear_grad_input_workspace bytes, 256-byte
- *         aligned; its contents are not kept.
+ *         aligned; its contents are not kept.  `direct` as above.
  * Errors: EINVAL, ERANGE, ECUDA. */
 agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
                                           int64_t grad_stride, int64_t rows, int64_t width,
@@ -262,7 +266,8 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
                                           int64_t workspace_bytes, int32_t* status,
                                           void* cuda_stream);
 agnes_status agnes_int8_linear_grad_input_workspace(int64_t rows, int64_t width, int64_t dim,
-                                                    int32_t grad_dtype, int64_t* bytes);
+                                                    int32_t grad_dtype, int32_t direct,
+                                                    int64_t* bytes);
 
 /* A nonlinearity, gated or not, that keeps its input in 8 bits for its backward
  * pass: out = f(x), or f(x[:, :dim]) x[:, dim:] where gated (x has 2 dim columns

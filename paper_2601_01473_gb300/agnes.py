@@ -173,11 +173,11 @@ SIGNATURES = {
     "agnes_int8_linear_workspace": ([_I64, _I64, _I64, ctypes.POINTER(_I64)], ctypes.c_int),
     "agnes_int8_linear_grad_weight": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64,
                                        _P, _P, _I64, _P, _P], ctypes.c_int),
-    "agnes_int8_linear_grad_weight_workspace": ([_I64, _I64, _I64, _I32, ctypes.POINTER(_I64)],
+    "agnes_int8_linear_grad_weight_workspace": ([_I64, _I64, _I64, _I32, _I32, ctypes.POINTER(_I64)],
                                                 ctypes.c_int),
     "agnes_int8_linear_grad_input": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64,
                                       _P, _I64, _P, _P], ctypes.c_int),
-    "agnes_int8_linear_grad_input_workspace": ([_I64, _I64, _I64, _I32, ctypes.POINTER(_I64)],
+    "agnes_int8_linear_grad_input_workspace": ([_I64, _I64, _I64, _I32, _I32, ctypes.POINTER(_I64)],
                                                ctypes.c_int),
     "agnes_activation": ([_P, _I32, _I64, _I64, _I64, _I32, _I32, _P, _I32, _I64, _P, _I64, _P],
                          ctypes.c_int),

@@ -1,0 +1,530 @@
+// int8_grad_weight.cu -- the gradient of the product of 8-bit rows and 8-bit weights to the
+// weights and the bias (include/agnes_ops.h; the format is in int8.cuh):
+//
+//   dw[j][i] = sum_r grad[r][j] s[r] q[r][i],  dbias[j] = sum_r grad[r][j]
+//
+// The rows are the contraction, so both operands are taken as they lie in memory, a row of
+// shared memory to a row (MN-major).  A scaled whole number is exactly the sum of two
+// bfloat16 values, its leading eight bits and the rest; the two matrices lie side by side,
+// so that one product of 128 x 256 makes both sums and reads the gradient once.
+//
+// A CTA takes a tile of 128 x 128 of the output and a share of the rows:
+//   the producer      has the TMA copy slices of 64 rows, the gradient's terms and the whole
+//                     numbers as they are;
+//   the convert warps scale the whole numbers and write both terms;
+//   the MMA warp      issues the products into one of two accumulators, `chain` slices each;
+//   the epilogue warps add the accumulators up in registers and write a partial tile;
+//   the bias warps    add the gradient's columns up, of the first tile of columns.
+// Tensor memory's sums are cut off, not rounded, after each product: over a hyperbatch's rows
+// in one chain that bias would reach 1e-5 of the result, so chains are short.  A second
+// kernel adds the shares' tiles up in order, so the result is the same each time.
+#include <type_traits>
+
+#include "int8_product.cuh"
+
+namespace agnes {
+
+namespace {
+
+constexpr int kTile = 128;
+constexpr int kSlice = 64;  // rows to a stage
+constexpr int kEpilogueWarps = 8;
+constexpr int kConvertWarp0 = kEpilogueWarps, kConvertWarps = 4;
+constexpr int kProducerWarp = kConvertWarp0 + kConvertWarps;
+constexpr int kMmaWarp = kProducerWarp + 1;
+constexpr int kBiasWarp0 = kMmaWarp + 1, kBiasWarps = 2;
+constexpr int kThreads = 32 * (kBiasWarp0 + kBiasWarps);
+constexpr int kBox = kSlice * 128;           // 64 columns of a slice in 16 bits
+constexpr int kGradBytes = 2 * kBox;         // a term of the gradient
+constexpr int kValueBytes = 4 * kBox;        // the scaled whole numbers' two terms
+constexpr int kRawBytes = kSlice * kTile;
+constexpr int kMaxSlots = 4;
+constexpr int kBars = 3 * kMaxSlots + 5;
+constexpr int kSmemLimit = 232448;
+constexpr int kRingBytes = kSmemLimit - 1024 - 8 * kBars - 16;
+constexpr int kTmemCols = 512;
+constexpr int kTileValues = kTile * kTile;
+constexpr int kSms = 152;  // that the rows are shared out for: a GB300's
+
+struct WeightArgs {
+  int64_t rows, width;
+  int32_t dim, row_bytes;
+  const uint8_t* x;
+  int64_t x_stride;
+  int32_t ta;
+  int32_t slices;             // of all rows
+  int32_t tiles_j, tiles_i;   // of the output, along width and dim
+  int32_t splits, per_split;  // shares of the rows, slices of one
+  int32_t chain;
+  float* partial;             // [split][tile][kTileValues], as the threads hold them
+  float* bias_partial;        // [split][width], or null
+  void* out;
+  int64_t out_stride;
+  float* dbias;
+  int32_t slots, slot_bytes;
+  int32_t* status;
+};
+
+// full[s] (the TMA has brought slot s), ready[s] (both terms are written), empty[s] (nobody
+// reads it any more); done[d] / taken[d] of the accumulators; drained, when the MMA warp
+// gives up.
+struct WeightBars {
+  uint32_t base;
+  __device__ uint32_t at(int i) const { return base + 8u * (uint32_t)i; }
+  __device__ uint32_t full(int s) const { return at(s); }
+  __device__ uint32_t ready(int s) const { return at(kMaxSlots + s); }
+  __device__ uint32_t empty(int s) const { return at(2 * kMaxSlots + s); }
+  __device__ uint32_t done(int d) const { return at(3 * kMaxSlots + d); }
+  __device__ uint32_t taken(int d) const { return at(3 * kMaxSlots + 2 + d); }
+  __device__ uint32_t drained() const { return at(3 * kMaxSlots + 4); }
+};
+
+// Eight values from four pairs of fp32: their upper halves, which are all of them.
+__device__ __forceinline__ uint4 upper8(const float* v) {
+  const auto pair = [&](int i) {
+    return __byte_perm(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), 0x7632);
+  };
+  return make_uint4(pair(0), pair(2), pair(4), pair(6));
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+weight_kernel(const __grid_constant__ CUtensorMap grad_map,
+              const __grid_constant__ CUtensorMap x_map, const WeightArgs a) {
+  grid_dep_wait();
+  constexpr uint32_t kIdesc = idesc_16bit(true, true, kTile, 2 * kTile);
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+  uint64_t* bars = (uint64_t*)(smem + a.slots * a.slot_bytes);
+  uint32_t* tmem_slot = (uint32_t*)(bars + kBars);
+  const WeightBars bar = {smem_addr(bars)};
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // this CTA's tile and share
+  const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
+  const int64_t tile = blockIdx.x % tiles, split = blockIdx.x / tiles;
+  const int32_t tile_i = (int32_t)(tile % a.tiles_i);
+  const int64_t j0 = tile / a.tiles_i * kTile;
+  const int32_t i0 = tile_i * kTile;
+  const int32_t k0 = (int32_t)split * a.per_split, k1 = min(k0 + a.per_split, a.slices);
+  const bool bias = a.bias_partial && tile_i == 0;
+  if (warp == kMmaWarp) tmem_alloc(tmem_slot, kTmemCols);
+  if (tid == 0) {
+    for (int s = 0; s < kMaxSlots; ++s) {
+      mbar_init(bar.full(s), 1);
+      mbar_init(bar.ready(s), kConvertWarps);
+      mbar_init(bar.empty(s), 1 + (bias ? kBiasWarps : 0));
+    }
+    for (int d = 0; d < 2; ++d) {
+      mbar_init(bar.done(d), 1);
+      mbar_init(bar.taken(d), kEpilogueWarps);
+    }
+    mbar_init(bar.drained(), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t ring_at = smem_addr(smem);
+  // in a slot: the gradient's terms, the scaled whole numbers', the whole numbers
+  const uint32_t value_off = (uint32_t)(a.ta * kGradBytes), raw_off = value_off + kValueBytes;
+  bool ok = true;
+  Ring ring;
+
+  if (warp == kProducerWarp) {
+    if (lane == 0) {
+      int64_t issued = 0;
+      for (int32_t k = k0; k < k1; ++k) {
+        const int s = ring.slot;
+        if (!ring.first && !mbar_wait(bar.empty(s), ring.parity ^ 1u)) {
+          ok = false;
+          break;
+        }
+        const uint32_t at = ring_at + (uint32_t)(s * a.slot_bytes);
+        mbar_expect(bar.full(s), (uint32_t)(a.ta * kGradBytes + kRawBytes));
+        // Past the last row a term's slice runs into the next term, which is finite there
+        // and meets whole numbers of zero.
+        for (int p = 0; p < a.ta; ++p)
+          for (int b = 0; b < 2; ++b)
+            tma_load(at + (uint32_t)(p * kGradBytes + b * kBox), &grad_map,
+                     (int32_t)(j0 + b * 64), (int32_t)(p * a.rows + (int64_t)k * kSlice),
+                     bar.full(s));
+        tma_load(at + raw_off, &x_map, i0, (int32_t)((int64_t)k * kSlice), bar.full(s));
+        ring.next(a.slots);
+        ++issued;
+      }
+      if (!ok) {  // the copies in flight land before the CTA may leave
+        Ring r;
+        for (int64_t i = 0; i < issued; ++i, r.next(a.slots))
+          if (i + a.slots >= issued) mbar_wait(bar.full(r.slot), r.parity);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    if (lane == 0) {
+      Ring acc;
+      for (int32_t c0 = k0; ok && c0 < k1; c0 += a.chain) {
+        const int d = acc.slot;
+        if (!acc.first && !mbar_wait(bar.taken(d), acc.parity ^ 1u)) {
+          ok = false;
+          break;
+        }
+        tcgen05_fence_after();
+        const uint32_t to = tmem + (uint32_t)(d * 2 * kTile);
+        uint32_t accumulate = 0;
+        for (int32_t k = c0; k < min(c0 + a.chain, k1); ++k) {
+          const int s = ring.slot;
+          if (!mbar_wait(bar.full(s), ring.parity) || !mbar_wait(bar.ready(s), ring.parity)) {
+            ok = false;
+            break;
+          }
+          tcgen05_fence_after();
+          const uint32_t at = ring_at + (uint32_t)(s * a.slot_bytes);
+          const int64_t left = a.rows - (int64_t)k * kSlice;
+          const int n = left < kSlice ? (int)((left + 15) / 16) : kSlice / 16;
+          for (int i = 0; i < n; ++i)
+            for (int p = 0; p < a.ta; ++p) {
+              mma_16bit(to, operand_desc_mn(at + (uint32_t)(p * kGradBytes + i * 2048), kBox),
+                        operand_desc_mn(at + value_off + (uint32_t)(i * 2048), kBox), kIdesc,
+                        accumulate);
+              accumulate = 1;
+            }
+          mma_commit(bar.empty(s));
+          ring.next(a.slots);
+        }
+        if (!ok) break;
+        mma_commit(bar.done(d));
+        acc.next(2);
+      }
+      if (!ok) {  // the products in flight end before the tensor memory is freed
+        mma_commit(bar.drained());
+        mbar_wait(bar.drained(), 0);
+      }
+    }
+  } else if (warp >= kBiasWarp0) {
+    if (bias) {
+      // two columns to a lane, in a row's 16-byte pieces as the TMA's swizzle has them
+      const int b = warp - kBiasWarp0, piece = lane >> 2, byte = (lane & 3) * 4;
+      float sum[2] = {0.f, 0.f};
+      for (int32_t k = k0; k < k1; ++k) {
+        const int s = ring.slot;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar.full(s), ring.parity))) {
+          ok = false;
+          break;
+        }
+        const uint8_t* from = smem + s * a.slot_bytes + b * kBox;
+        const int64_t left = a.rows - (int64_t)k * kSlice;
+        const int n = left < kSlice ? (int)left : kSlice;
+        float part[2] = {0.f, 0.f};
+        for (int p = 0; p < a.ta; ++p)
+#pragma unroll 16
+          for (int r = 0; r < n; ++r) {
+            const uint32_t v = *(const uint32_t*)(from + p * kGradBytes + r * 128 +
+                                                  ((piece ^ (r & 7)) << 4) + byte);
+            part[0] += __uint_as_float(v << 16);
+            part[1] += __uint_as_float(v & 0xffff0000u);
+          }
+        sum[0] += part[0];
+        sum[1] += part[1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar.empty(s));
+        ring.next(a.slots);
+      }
+      const int64_t j = j0 + b * 64 + lane * 2;
+      float* to = a.bias_partial + split * a.width;
+      if (j < a.width) to[j] = sum[0];
+      if (j + 1 < a.width) to[j + 1] = sum[1];
+    }
+  } else if (warp >= kConvertWarp0) {
+    // a thread to 64 values of a row: neighbouring threads to neighbouring rows, whose
+    // pieces lie in different banks
+    const int t = tid - 32 * kConvertWarp0, half = t >> 6, r = t & 63;
+    const auto scale_of = [&](int32_t k) {
+      const int64_t row = (int64_t)k * kSlice + r;
+      return k < k1 && row < a.rows
+                 ? __ldg((const float*)(a.x + row * a.x_stride + a.row_bytes - 4)) : 0.f;
+    };
+    float next = scale_of(k0);
+    for (int32_t k = k0; k < k1; ++k) {
+      const int s = ring.slot;
+      const float scale = next;
+      next = scale_of(k + 1);
+      if (!__all_sync(0xffffffffu, mbar_wait(bar.full(s), ring.parity))) {
+        ok = false;
+        break;
+      }
+      uint8_t* slot = smem + s * a.slot_bytes;
+      const uint8_t* from = slot + raw_off + r * kTile;
+      uint8_t* to = slot + value_off + half * kBox + r * 128;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint4 w = *(const uint4*)(from + (((4 * half + c) ^ (r & 7)) << 4));
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float hi[8], lo[8];
+          int8_values4(word[2 * h], hi);
+          int8_values4(word[2 * h + 1], hi + 4);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) int8_split(hi[e] * scale, hi[e], lo[e]);
+          const int at = ((2 * c + h) ^ (r & 7)) << 4;
+          *(uint4*)(to + at) = upper8(hi);
+          *(uint4*)(to + 2 * kBox + at) = upper8(lo);
+        }
+      }
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar.ready(s));
+      ring.next(a.slots);
+    }
+  } else {
+    constexpr int kHalf = kTile / 2;
+    const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
+                              (uint32_t)((warp >> 2) * kHalf);
+    float total[kHalf];
+#pragma unroll
+    for (int e = 0; e < kHalf; ++e) total[e] = 0.f;
+    Ring acc;
+    for (int32_t c0 = k0; c0 < k1; c0 += a.chain) {
+      const int d = acc.slot;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar.done(d), acc.parity))) {
+        ok = false;
+        break;
+      }
+      tcgen05_fence_after();
+#pragma unroll
+      for (int c = 0; c < 2 * kHalf; c += 32) {  // the leading bits' sums, then the rest's
+        uint32_t v[32];
+        tmem_load32(lanes_at + (uint32_t)(d * 2 * kTile + c % kHalf + c / kHalf * kTile), v);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) total[c % kHalf + e] += __uint_as_float(v[e]);
+      }
+      tcgen05_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar.taken(d));
+      acc.next(2);
+    }
+    float4* to = (float4*)(a.partial + (split * tiles + tile) * kTileValues) + warp * 16 * 32;
+#pragma unroll
+    for (int c = 0; c < kHalf / 4; ++c)
+      to[c * 32 + lane] = make_float4(total[4 * c], total[4 * c + 1], total[4 * c + 2],
+                                      total[4 * c + 3]);
+  }
+  if (!ok) op_flag(a.status, AGNES_OP_TIMEOUT);
+  tcgen05_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tcgen05_fence_after();
+    tmem_free(tmem, kTmemCols);
+  }
+}
+
+// The shares' tiles added up: 32 rows x 16 columns of a tile to a CTA, their shares dealt
+// out to kJoinShares threads each, whose sums are added in order.
+constexpr int kJoinShares = 4;
+constexpr int kJoinQuads = 4;  // groups of four columns
+template <typename TOut>
+__global__ void __launch_bounds__(32 * kJoinQuads * kJoinShares)
+join_kernel(const WeightArgs a) {
+  grid_dep_wait();
+  __shared__ float4 sums[kJoinShares][kJoinQuads][32];
+  const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) % kJoinQuads;
+  const int share = (threadIdx.x >> 5) / kJoinQuads;
+  const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
+  const int64_t tile = blockIdx.x / 32;
+  const int part = blockIdx.x % 32, warp = part / 4, c = part % 4 * kJoinQuads + quad;
+  const float4* from = (const float4*)(a.partial + tile * kTileValues) + (warp * 16 + c) * 32 + lane;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = share; s < a.splits; s += kJoinShares) {
+    const float4 p = from[(int64_t)s * tiles * (kTileValues / 4)];
+    v.x += p.x;
+    v.y += p.y;
+    v.z += p.z;
+    v.w += p.w;
+  }
+  sums[share][quad][lane] = v;
+  __syncthreads();
+  // a row's 16 columns to neighbouring threads
+  const int t = threadIdx.x;
+  const int64_t j = tile / a.tiles_i * kTile + (warp & 3) * 32 + t / 16;
+  const int32_t i = (int32_t)(tile % a.tiles_i) * kTile + (warp >> 2) * 64 + part % 4 * 16 + t % 16;
+  if (j < a.width && i < a.dim) {
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < kJoinShares; ++s) sum += ((const float*)&sums[s][t % 16 / 4][t / 16])[t % 4];
+    ((TOut*)a.out)[j * a.out_stride + i] = from_f32<TOut>(sum);
+  }
+}
+
+__global__ void __launch_bounds__(256) bias_join_kernel(const WeightArgs a) {
+  grid_dep_wait();
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= a.width) return;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) sum += a.bias_partial[(int64_t)s * a.width + j];
+  a.dbias[j] = sum;
+}
+
+// How the rows are shared out, and the workspace: partial tiles, partial biases, and the
+// gradient's terms where it cannot be taken as it is.
+struct WeightSpace {
+  int64_t slices, tiles_j, tiles_i, splits, per_split, wpad, bias, grad, bytes;
+  WeightSpace(int64_t rows, int64_t width, int64_t dim, int32_t dtype, bool direct) {
+    slices = ceil_div(rows, kSlice);
+    tiles_j = ceil_div(width, kTile);
+    tiles_i = ceil_div(dim, kTile);
+    wpad = ceil_div(width, 8) * 8;
+    const int64_t tiles = tiles_j * tiles_i;
+    // one CTA to an SM: shares so that the last turn is as full as the others
+    splits = 1;
+    if (tiles > 0 && slices > 0) {
+      double best = 0;
+      for (int64_t s = 1; s <= slices && s * tiles <= 8 * kSms + tiles; ++s) {
+        const int64_t per = ceil_div(slices, s), used = ceil_div(slices, per);
+        // a share costs some slices' time besides, for its start and its partial tile
+        const double turns = (double)(ceil_div(used * tiles, kSms) * (per + 6));
+        if (s == 1 || turns < best) {
+          best = turns;
+          splits = used;
+        }
+      }
+    }
+    per_split = slices ? ceil_div(slices, splits) : 0;
+    bias = ceil_div(splits * tiles * kTileValues * 4, 256) * 256;
+    grad = bias + ceil_div(splits * width * 4, 256) * 256;
+    bytes = rows > 0 && width > 0 ? grad + (direct ? 0 : grad_terms(dtype) * rows * wpad * 2) : 0;
+  }
+  void shape(WeightArgs& a) const {
+    a.slices = (int32_t)slices;
+    a.tiles_j = (int32_t)tiles_j;
+    a.tiles_i = (int32_t)tiles_i;
+    a.splits = (int32_t)splits;
+    a.per_split = (int32_t)per_split;
+  }
+};
+
+template <typename TOut>
+cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, int device,
+                          cudaStream_t st) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return cudaErrorNotSupported;
+  CUtensorMap grad_map, x_map;
+  if (!map_rows(encode, &grad_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, grad, a.width, a.ta * a.rows,
+                grad_stride, 64, kSlice, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !map_rows(encode, &x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.x, a.dim, a.rows, a.x_stride, kTile,
+                kSlice, CU_TENSOR_MAP_SWIZZLE_128B))
+    return cudaErrorInvalidValue;
+  static OncePerDevice once;
+  cudaError_t e = once.run(device, [] {
+    return cudaFuncSetAttribute(weight_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                kSmemLimit);
+  });
+  if (e != cudaSuccess) return e;
+  a.chain = 8 / a.ta;
+  a.slot_bytes = a.ta * kGradBytes + kValueBytes + kRawBytes;
+  const int slots = kRingBytes / a.slot_bytes;
+  a.slots = slots < kMaxSlots ? slots : kMaxSlots;
+  const size_t smem = (size_t)kSmemLimit - kRingBytes + (size_t)a.slots * a.slot_bytes;
+  const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
+  e = launch_next(weight_kernel, dim3((unsigned)(tiles * a.splits)), (unsigned)kThreads, smem, st,
+                  grad_map, x_map, a);
+  if (e != cudaSuccess) return e;
+  e = launch_next(join_kernel<TOut>, dim3((unsigned)(tiles * 32)),
+                  32 * kJoinQuads * kJoinShares, 0, st, a);
+  if (e != cudaSuccess || !a.dbias) return e;
+  return launch_next(bias_join_kernel, dim3((unsigned)ceil_div(a.width, 256)), 256, 0, st, a);
+}
+
+}  // namespace
+
+}  // namespace agnes
+
+using namespace agnes;
+
+extern "C" {
+
+agnes_status agnes_int8_linear_grad_weight_workspace(int64_t rows, int64_t width, int64_t dim,
+                                                     int32_t grad_dtype, int32_t direct,
+                                                     int64_t* bytes) {
+  const char* op = "agnes_int8_linear_grad_weight_workspace";
+  if (!bytes) return op_error(AGNES_EINVAL, "%s: bytes is NULL", op);
+  OP_TRY(product_check_sizes(op, rows, width, dim));
+  OP_TRY(op_float_type(op, "grad", grad_dtype));
+  OP_TRY(check_direct(op, grad_dtype, direct));
+  *bytes = WeightSpace(rows, width, dim, grad_dtype, direct).bytes;
+  return AGNES_OK;
+}
+
+agnes_status agnes_int8_linear_grad_weight(const void* grad, int32_t grad_dtype,
+                                           int64_t grad_stride, int64_t rows, int64_t width,
+                                           const void* x, int64_t x_stride, int64_t dim, void* out,
+                                           int32_t out_dtype, int64_t out_stride, float* dbias,
+                                           void* workspace, int64_t workspace_bytes,
+                                           int32_t* status, void* cuda_stream) {
+  const char* op = "agnes_int8_linear_grad_weight";
+  OP_TRY(product_check_sizes(op, rows, width, dim));
+  OP_TRY(op_float_type(op, "grad", grad_dtype));
+  OP_TRY(op_float_type(op, "out", out_dtype));
+  OP_TRY(product_check_step(op, "grad", rows, width, grad_stride));
+  OP_TRY(int8_check_stride(op, "x", rows, dim, x_stride));
+  OP_TRY(product_check_step(op, "out", width, dim, out_stride));
+  if (width == 0) return AGNES_OK;
+  int device = -1;
+  OP_TRY(op_device_of(op, "out", out, &device));
+  OP_TRY(op_aligned(op, "out", out, float_size(out_dtype)));
+  if (dbias) {
+    OP_TRY(op_on_device(op, "dbias", dbias, device));
+    OP_TRY(op_aligned(op, "dbias", dbias, 4));
+  }
+  if (rows > 0) {
+    OP_TRY(op_on_device(op, "grad", grad, device));
+    OP_TRY(op_on_device(op, "x", x, device));
+    OP_TRY(op_aligned(op, "grad", grad, float_size(grad_dtype)));
+    OP_TRY(op_aligned(op, "x", x, 16));
+  }
+  OP_TRY(op_status(op, status, device));
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const int64_t out_step = width > 1 ? out_stride : dim;
+  if (rows == 0) {  // sums over no rows
+    DeviceGuard dg(device);
+    if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
+    const size_t size = (size_t)float_size(out_dtype);
+    OP_TRY(op_launched(op, cudaMemset2DAsync(out, (size_t)out_step * size, 0, (size_t)dim * size,
+                                             (size_t)width, st)));
+    return dbias ? op_launched(op, cudaMemsetAsync(dbias, 0, (size_t)width * 4, st)) : AGNES_OK;
+  }
+  const int64_t step = rows > 1 ? grad_stride : width;
+  const bool direct = takes_grad(grad, grad_dtype, rows > 1 ? grad_stride : 0);
+  const WeightSpace space(rows, width, dim, grad_dtype, direct);
+  OP_TRY(product_check_workspace(op, workspace, workspace_bytes, space.bytes, device));
+  DeviceGuard dg(device);
+  if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
+  const void* a = grad;
+  int64_t a_stride = rows > 1 ? step * 2 : space.wpad * 2;
+  if (!direct) {
+    __nv_bfloat16* terms = (__nv_bfloat16*)((uint8_t*)workspace + space.grad);
+    OP_TRY(op_launched(op, split_grad(grad, grad_dtype, step, rows, width, terms, space.wpad, st)));
+    a = terms;
+    a_stride = space.wpad * 2;
+  }
+  WeightArgs w = {};
+  w.rows = rows;
+  w.width = width;
+  w.dim = (int32_t)dim;
+  w.x = (const uint8_t*)x;
+  w.x_stride = rows > 1 ? x_stride : int8_row_bytes(dim);
+  w.row_bytes = (int32_t)int8_row_bytes(dim);
+  w.ta = direct ? 1 : grad_terms(grad_dtype);
+  w.partial = (float*)workspace;
+  w.bias_partial = dbias ? (float*)((uint8_t*)workspace + space.bias) : nullptr;
+  w.out = out;
+  w.out_stride = out_step;
+  w.dbias = dbias;
+  w.status = status;
+  space.shape(w);
+  return op_launched(op, with_float_type(out_dtype, [&](auto t) {
+    return launch_weight<typename decltype(t)::type>(w, a, a_stride, device, st);
+  }));
+}
+
+}  // extern "C"

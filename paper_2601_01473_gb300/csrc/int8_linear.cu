@@ -1,15 +1,17 @@
-// int8_linear.cu -- 8-bit rows times 8-bit weights, and the gradients of that product
-// (include/agnes_ops.h; the format is in int8.cuh).
+// int8_linear.cu -- 8-bit rows times 8-bit weights, and the gradient of that product to the
+// rows (include/agnes_ops.h; the format is in int8.cuh; the gradient to the weights is in
+// int8_grad_weight.cu).
 //
 //   out[r][j] = s_x[r] s_w[j] sum_i q_x[r][i] q_w[j][i] + bias[j]
-//   dw[j][i]  = sum_r grad[r][j] s_x[r] q_x[r][i]
 //   dx[r][i]  = sum_j grad[r][j] s_w[j] q_w[j][i]
 //
 // Few rows: the weights' bytes count, so a group of lanes takes a column's whole numbers,
 // four products an instruction, for all rows.
-// Otherwise tiles of 64 x 64 outputs, 4 x 4 to a thread, over slices of 16 staged in
-// shared memory as fp32; sums of 4096 products in fp32, those in 64 bits.
-#include "int8.cuh"
+// Otherwise the tensor cores (tcgen05.mma), in 16-bit operands: whole numbers are exact in
+// fp16, and a scaled one is the sum of two bfloat16 values (int8.cuh).
+#include <type_traits>
+
+#include "int8_product.cuh"
 
 namespace agnes {
 
@@ -96,117 +98,549 @@ linear_few_kernel(int lanes, const LinearArgs a) {
   }
 }
 
+// ---- operands in 16 bits --------------------------------------------------------
+
+constexpr int kPrepThreads = 256;
+
+// Whole numbers as fp16, `kpad` to a row, and the rows' scales.
+__global__ void __launch_bounds__(kPrepThreads)
+expand_kernel(const uint8_t* __restrict__ q, int64_t stride, int64_t rows, int32_t dim,
+              int32_t row_bytes, int32_t groups, uint32_t inv_groups, __half* __restrict__ out,
+              int64_t kpad, float* __restrict__ scales) {
+  const FlatRows flat(blockIdx.x, groups, inv_groups);
+#pragma unroll
+  for (int u = 0; u < kFlat / kPrepThreads; ++u) {
+    int64_t row;
+    uint32_t g;
+    flat.at(threadIdx.x + u * kPrepThreads, &row, &g);
+    if (row >= rows) continue;
+    const uint8_t* from = q + row * stride;
+    float v[8];
+    const uint2 w = *(const uint2*)(from + g * 8);
+    int8_values4(w.x, v);
+    int8_values4(w.y, v + 4);
+    store_vec<__half, 8>(out + row * kpad + g * 8, v);  // past dim: not looked at
+    if (scales && g == 0) scales[row] = *(const float*)(from + row_bytes - 4);
+  }
+}
+
+// The weights' values, transposed and as sums of two bfloat16 values: term t of column i of
+// row j at out[(t * dim + i) * wpad + j].
+constexpr int kTransTile = 64;
+__global__ void __launch_bounds__(kPrepThreads)
+transpose_kernel(const uint8_t* __restrict__ q, int64_t stride, int64_t width, int32_t dim,
+                 int32_t row_bytes, __nv_bfloat16* __restrict__ out, int64_t wpad) {
+  __shared__ __align__(16) uint8_t tile[kTransTile][kTransTile + 16];
+  __shared__ float scale[kTransTile];
+  const int64_t j0 = (int64_t)blockIdx.x * kTransTile;
+  const int32_t i0 = (int32_t)blockIdx.y * kTransTile;
+  {
+    const int j = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (j0 + j < width && i0 + c < row_bytes) v = *(const uint4*)(q + (j0 + j) * stride + i0 + c);
+    *(uint4*)&tile[j][c] = v;
+    if (c == 0) scale[j] = j0 + j < width ? *(const float*)(q + (j0 + j) * stride + row_bytes - 4) : 0.f;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int i = threadIdx.x / 4, j = (threadIdx.x % 4 * 2 + u) * 8;
+    if (i0 + i >= dim || j0 + j >= wpad) continue;
+    float hi[8], lo[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) int8_split((float)(int8_t)tile[j + e][i] * scale[j + e], hi[e], lo[e]);
+    __nv_bfloat16* to = out + (int64_t)(i0 + i) * wpad + j0 + j;
+    store_vec<__nv_bfloat16, 8>(to, hi);
+    store_vec<__nv_bfloat16, 8>(to + (int64_t)dim * wpad, lo);
+  }
+}
+
 // ---- tiles ----------------------------------------------------------------------
 
-constexpr int kTile = 64, kSlice = 16, kChunk = 4096;
+// Warps: 0-7 epilogue (two to a quarter of tensor memory's lanes, half the columns each),
+// 8-11 whole numbers to fp16, 12 producer, 13 MMA.
+constexpr int kTileM = 128;
+constexpr int kSliceK = 64;  // of the contraction to a stage: 128 bytes in 16 bits
+constexpr int kEpilogueWarps = 8;
+constexpr int kConvertWarp0 = kEpilogueWarps, kConvertWarps = 4;
+constexpr int kProducerWarp = kConvertWarp0 + kConvertWarps;
+constexpr int kMmaWarp = kProducerWarp + 1;
+constexpr int kTileThreads = 32 * (kMmaWarp + 1);
+constexpr int kOperandBytes = kTileM * 128;  // of one term of A
+constexpr int kRawBytes = kTileM * kSliceK;
+constexpr int kMaxSlots = 8;
+constexpr int kOutBytes = 32 * 128;  // an epilogue warp's output on its way to memory
+constexpr int kTileBars = 3 * kMaxSlots + 6;
+constexpr int kSmemLimit = 232448;
+constexpr int kTileSmem = kSmemLimit - 1024 - 8 * kTileBars - 16;  // for the buffers
 
-// out[m][n] = sum_k A(m, k) B(n, k), A and B functions of two indexes.
-template <typename A, typename B, typename Out>
-__device__ __forceinline__ void tile_product(int64_t M, int64_t N, int64_t K, A&& fa, B&& fb,
-                                             Out&& out) {
-  __shared__ float sa[kSlice][kTile + 4], sb[kSlice][kTile + 4];
-  const int64_t m0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
-  const int tm = threadIdx.x / 16 * 4, tn = threadIdx.x % 16 * 4;
-  double total[4][4] = {};
-  float sum[4][4] = {};
-  for (int64_t k0 = 0; k0 < K; k0 += kSlice) {
-    for (int i = threadIdx.x; i < kTile * kSlice; i += 256) {
-      const int r = i / kSlice, k = i % kSlice;
-      sa[k][r] = m0 + r < M && k0 + k < K ? fa(m0 + r, k0 + k) : 0.f;
-      sb[k][r] = n0 + r < N && k0 + k < K ? fb(n0 + r, k0 + k) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kSlice; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[i][j] = fmaf(sa[k][tm + i], sb[k][tn + j], sum[i][j]);
-    __syncthreads();
-    if (k0 % kChunk == kChunk - kSlice || k0 + kSlice >= K) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          total[i][j] += sum[i][j];
-          sum[i][j] = 0.f;
-        }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (m0 + tm + i < M && n0 + tn + j < N) out(m0 + tm + i, n0 + tn + j, total[i][j]);
-}
-
-template <typename TOut>
-__global__ void __launch_bounds__(256) linear_kernel(const LinearArgs a) {
-  const int end = a.row_bytes - 4;
-  tile_product(
-      a.rows, a.width, a.dim,
-      [&](int64_t r, int64_t i) { return (float)(int8_t)a.x[r * a.x_stride + i]; },
-      [&](int64_t j, int64_t i) { return (float)(int8_t)a.w[j * a.w_stride + i]; },
-      [&](int64_t r, int64_t j, double v) {
-        const float sx = *(const float*)(a.x + r * a.x_stride + end);
-        const float sw = *(const float*)(a.w + j * a.w_stride + end);
-        ((TOut*)a.out)[r * a.out_stride + j] =
-            from_f32<TOut>(scaled((float)v, sx, sw) + (a.bias ? a.bias[j] : 0.f));
-      });
-}
-
-struct GradArgs {
-  const void* grad;
-  int64_t grad_stride, rows, width;
-  const uint8_t* q;  // x's rows, or w's
-  int64_t q_stride;
-  int32_t dim, row_bytes;
+struct TileArgs {
+  int64_t rows, cols;  // of the output
+  int32_t steps;       // slices of the contraction
+  int32_t last;        // products of 16 in the last one
+  int32_t ta, tb;      // terms of A and of B
+  int32_t limit;       // of the terms' products those with a + b < limit count
+  int32_t chain;       // slices that one accumulator sums
+  const uint8_t* x;    // rows whose scales the output takes, or null
+  int64_t x_stride;
+  int32_t row_bytes;
+  const float *col_scale, *bias;
   void* out;
   int64_t out_stride;
-  float* dbias;
+  int32_t slots, slot_bytes, out_buffers;
+  bool resident;  // B's slices stay in shared memory: a CTA keeps to one tile of columns
+  bool tma_out;
+  int32_t* status;
 };
 
-template <typename TGrad, typename TOut>
-__global__ void __launch_bounds__(256) grad_weight_kernel(const GradArgs a) {
-  const int end = a.row_bytes - 4;
-  tile_product(
-      a.width, a.dim, a.rows,
-      [&](int64_t j, int64_t r) {
-        return to_f32(((const TGrad*)a.grad)[r * a.grad_stride + j]);
-      },
-      [&](int64_t i, int64_t r) {
-        const uint8_t* row = a.q + r * a.q_stride;
-        return (float)(int8_t)row[i] * *(const float*)(row + end);
-      },
-      [&](int64_t j, int64_t i, double v) {
-        ((TOut*)a.out)[j * a.out_stride + i] = from_f32<TOut>((float)v);
-      });
+// The output tiles of a CTA, every gridDim.x-th, columns fastest.
+struct TileWalk {
+  int64_t m, n, tiles_m, tiles_n, step_m, step_n;
+  __device__ TileWalk(const TileArgs& a, int cols) {
+    tiles_n = (a.cols + cols - 1) / cols;
+    tiles_m = (a.rows + kTileM - 1) / kTileM;
+    m = blockIdx.x / tiles_n;
+    n = blockIdx.x - m * tiles_n;
+    step_m = gridDim.x / tiles_n;
+    step_n = gridDim.x - step_m * tiles_n;
+  }
+  __device__ bool any() const { return m < tiles_m; }
+  __device__ void next() {
+    m += step_m;
+    n += step_n;
+    if (n >= tiles_n) {
+      n -= tiles_n;
+      ++m;
+    }
+  }
+};
+
+// The mbarriers: full[s] (the TMA has brought slot s), ready[s] (A's whole numbers are fp16),
+// empty[s] (its products are done); done[d] / taken[d] of the accumulators; b_full of the
+// resident B; drained, when the MMA warp gives up.
+struct TileBars {
+  uint32_t base;
+  __device__ uint32_t at(int i) const { return base + 8u * (uint32_t)i; }
+  __device__ uint32_t full(int s) const { return at(s); }
+  __device__ uint32_t ready(int s) const { return at(kMaxSlots + s); }
+  __device__ uint32_t empty(int s) const { return at(2 * kMaxSlots + s); }
+  __device__ uint32_t done(int d) const { return at(3 * kMaxSlots + d); }
+  __device__ uint32_t taken(int d) const { return at(3 * kMaxSlots + 2 + d); }
+  __device__ uint32_t b_full() const { return at(3 * kMaxSlots + 4); }
+  __device__ uint32_t drained() const { return at(3 * kMaxSlots + 5); }
+};
+
+// 32 values from c0 on of a vector over the columns; `fill` past its end or where there is
+// none.
+__device__ __forceinline__ void load_columns(const float* p, int64_t c0, int64_t cols, float fill,
+                                             float (&b)[32]) {
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) b[e] = fill;
+  } else if (c0 + 32 <= cols && (uintptr_t)p % 16 == 0) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+      const float4 v = __ldg((const float4*)(p + c0 + e));
+      b[e] = v.x;
+      b[e + 1] = v.y;
+      b[e + 2] = v.z;
+      b[e + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) b[e] = c0 + e < cols ? __ldg(p + c0 + e) : fill;
+  }
 }
 
-template <typename TGrad>
-__global__ void __launch_bounds__(256) grad_bias_kernel(const GradArgs a) {
-  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (j >= a.width) return;
-  double sum = 0;
-  for (int64_t r = 0; r < a.rows; ++r) sum += to_f32(((const TGrad*)a.grad)[r * a.grad_stride + j]);
-  a.dbias[j] = (float)sum;
+// 32 columns of a lane's row into its warp's buffer, from byte `first` of its 128 on, in
+// 16-byte pieces permuted as the TMA's 128-byte swizzle has them.
+template <typename TOut>
+__device__ __forceinline__ void stage_values(uint8_t* buffer, int lane, int first,
+                                             const float (&v)[32]) {
+  constexpr int kN = 16 / sizeof(TOut);
+#pragma unroll
+  for (int q = 0; q < 32 / kN; ++q) {
+    Vec<TOut, kN> y;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) y.v[e] = from_f32<TOut>(v[q * kN + e]);
+    *(Vec<TOut, kN>*)(buffer + lane * 128 + (((first / 16 + q) ^ (lane & 7)) << 4)) = y;
+  }
 }
 
-template <typename TGrad, typename TOut>
-__global__ void __launch_bounds__(256) grad_input_kernel(const GradArgs a) {
-  const int end = a.row_bytes - 4;
-  tile_product(
-      a.rows, a.dim, a.width,
-      [&](int64_t r, int64_t j) {
-        return to_f32(((const TGrad*)a.grad)[r * a.grad_stride + j]);
-      },
-      [&](int64_t i, int64_t j) {
-        const uint8_t* row = a.q + j * a.q_stride;
-        return (float)(int8_t)row[i] * *(const float*)(row + end);
-      },
-      [&](int64_t r, int64_t i, double v) {
-        ((TOut*)a.out)[r * a.out_stride + i] = from_f32<TOut>((float)v);
-      });
+// Four whole numbers as two pairs of fp16, in order: 1024 + (q + 128) are the bytes of the
+// word xor 0x80, each under 0x64.
+__device__ __forceinline__ uint2 int8_halves4(uint32_t word) {
+  word ^= 0x80808080u;
+  const uint32_t low = __byte_perm(word, 0x64646464u, 0x4140);
+  const uint32_t high = __byte_perm(word, 0x64646464u, 0x4342);
+  const __half2 offset = __half2half2(__ushort_as_half(0x6480));  // 1152
+  const __half2 a = __hsub2(*(const __half2*)&low, offset);
+  const __half2 b = __hsub2(*(const __half2*)&high, offset);
+  return make_uint2(*(const uint32_t*)&a, *(const uint32_t*)&b);
+}
+
+// out = A B^T over tiles of 128 x kCols.  kConvert: A is 8-bit rows, brought as they are and
+// made fp16 in shared memory, and B fp16; else both are bfloat16, of several terms each.
+// kDrain: an accumulator sums `chain` slices, and the epilogue warps add those up in
+// registers: tensor memory's sums are cut off, not rounded, after each product, which adds
+// up over long chains.
+template <typename TOut, bool kConvert, int kCols, bool kDrain>
+__global__ void __launch_bounds__(kTileThreads, 1)
+tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+            const __grid_constant__ CUtensorMap out_map, const TileArgs a) {
+  grid_dep_wait();
+  constexpr int kHalf = kCols / 2;  // columns of an epilogue warp
+  constexpr int kTmemCols = 2 * kCols;
+  constexpr uint32_t kIdesc = idesc_16bit(!kConvert, false, kTileM, kCols);
+  constexpr uint32_t kBBytes = kCols * 128;
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+  uint8_t* resident_b = smem + a.slots * a.slot_bytes;
+  uint8_t* out_stage =
+      resident_b + (a.resident ? a.steps * a.tb * (int)kBBytes : 0);
+  uint64_t* bars = (uint64_t*)(out_stage + kEpilogueWarps * a.out_buffers * kOutBytes);
+  uint32_t* tmem_slot = (uint32_t*)(bars + kTileBars);
+  const TileBars bar = {smem_addr(bars)};
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (warp == kMmaWarp) tmem_alloc(tmem_slot, kTmemCols);
+  if (tid == 0) {
+    for (int s = 0; s < kMaxSlots; ++s) {
+      mbar_init(bar.full(s), 1);
+      mbar_init(bar.ready(s), kConvertWarps);
+      mbar_init(bar.empty(s), 1);
+    }
+    for (int d = 0; d < 2; ++d) {
+      mbar_init(bar.done(d), 1);
+      mbar_init(bar.taken(d), kEpilogueWarps);
+    }
+    mbar_init(bar.b_full(), 1);
+    mbar_init(bar.drained(), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  TileWalk t(a, kCols);
+  const int slots = a.slots;
+  const uint32_t ring_at = smem_addr(smem), resident_at = smem_addr(resident_b);
+  // in a slot: A's terms, B's (unless they are resident), A's raw bytes
+  const uint32_t b_off = (uint32_t)(a.ta * kOperandBytes);
+  const uint32_t raw_off = b_off + (a.resident ? 0u : (uint32_t)a.tb * kBBytes);
+  bool ok = true;
+
+  if (warp == kProducerWarp) {
+    if (lane == 0) {
+      if (a.resident) {
+        mbar_expect(bar.b_full(), (uint32_t)(a.steps * a.tb) * kBBytes);
+        for (int k = 0; k < a.steps; ++k)
+          for (int b = 0; b < a.tb; ++b)
+            tma_load(resident_at + (uint32_t)(k * a.tb + b) * kBBytes, &b_map, k * kSliceK,
+                     (int32_t)(b * a.cols + t.n * kCols), bar.b_full());
+      }
+      const uint32_t bytes = (kConvert ? (uint32_t)kRawBytes : b_off) +
+                             (a.resident ? 0u : (uint32_t)a.tb * kBBytes);
+      Ring ring;
+      int64_t issued = 0;
+      for (; ok && t.any(); t.next()) {
+        for (int k = 0; k < a.steps; ++k) {
+          const int s = ring.slot;
+          if (!ring.first && !mbar_wait(bar.empty(s), ring.parity ^ 1u)) {
+            ok = false;
+            break;
+          }
+          const uint32_t at = ring_at + (uint32_t)(s * a.slot_bytes);
+          mbar_expect(bar.full(s), bytes);
+          if constexpr (kConvert) {
+            tma_load(at + raw_off, &a_map, k * kSliceK, (int32_t)(t.m * kTileM), bar.full(s));
+          } else {
+            for (int i = 0; i < a.ta; ++i)
+              tma_load(at + (uint32_t)(i * kOperandBytes), &a_map, k * kSliceK,
+                       (int32_t)(i * a.rows + t.m * kTileM), bar.full(s));
+          }
+          if (!a.resident)
+            for (int i = 0; i < a.tb; ++i)
+              tma_load(at + b_off + (uint32_t)i * kBBytes, &b_map, k * kSliceK,
+                       (int32_t)(i * a.cols + t.n * kCols), bar.full(s));
+          ring.next(slots);
+          ++issued;
+        }
+      }
+      if (!ok) {  // the copies in flight land before the CTA may leave
+        if (a.resident) mbar_wait(bar.b_full(), 0);
+        Ring r;
+        for (int64_t i = 0; i < issued; ++i, r.next(slots))
+          if (i + slots >= issued) mbar_wait(bar.full(r.slot), r.parity);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    if (lane == 0) {
+      if (a.resident) ok = mbar_wait(bar.b_full(), 0);
+      Ring ring, acc;
+      for (; ok && t.any(); t.next()) {
+        for (int k0 = 0; ok && k0 < a.steps; k0 += a.chain) {
+          const int d = acc.slot;
+          if (!acc.first && !mbar_wait(bar.taken(d), acc.parity ^ 1u)) {
+            ok = false;
+            break;
+          }
+          tcgen05_fence_after();
+          const uint32_t to = tmem + (uint32_t)(d * kCols);
+          uint32_t accumulate = 0;
+          const int k1 = min(k0 + a.chain, a.steps);
+          for (int k = k0; k < k1; ++k) {
+            const int s = ring.slot;
+            if (!mbar_wait(bar.full(s), ring.parity) ||
+                (kConvert && !mbar_wait(bar.ready(s), ring.parity))) {
+              ok = false;
+              break;
+            }
+            tcgen05_fence_after();
+            const uint32_t a_at = ring_at + (uint32_t)(s * a.slot_bytes);
+            const uint32_t b_at =
+                a.resident ? resident_at + (uint32_t)(k * a.tb) * kBBytes : a_at + b_off;
+            const int n = k + 1 == a.steps ? a.last : kSliceK / 16;
+            for (int i = 0; i < n; ++i) {
+              if constexpr (kConvert) {
+                mma_16bit(to, operand_desc(a_at + 32u * (uint32_t)i),
+                          operand_desc(b_at + 32u * (uint32_t)i), kIdesc, accumulate);
+                accumulate = 1;
+              } else {
+                for (int p = 0; p < a.ta; ++p)
+                  for (int q = 0; q < a.tb && p + q < a.limit; ++q) {
+                    mma_16bit(to,
+                              operand_desc(a_at + (uint32_t)(p * kOperandBytes) + 32u * (uint32_t)i),
+                              operand_desc(b_at + (uint32_t)q * kBBytes + 32u * (uint32_t)i), kIdesc,
+                              accumulate);
+                    accumulate = 1;
+                  }
+              }
+            }
+            mma_commit(bar.empty(s));
+            ring.next(slots);
+          }
+          if (!ok) break;
+          mma_commit(bar.done(d));
+          acc.next(2);
+        }
+      }
+      if (!ok) {  // the products in flight end before the tensor memory is freed
+        mma_commit(bar.drained());
+        mbar_wait(bar.drained(), 0);
+      }
+    }
+  } else if (warp >= kConvertWarp0) {
+    if constexpr (kConvert) {
+      const int r = tid - 32 * kConvertWarp0;  // this thread's row of the tile
+      Ring ring;
+      for (; ok && t.any(); t.next()) {
+        for (int k = 0; k < a.steps; ++k) {
+          const int s = ring.slot;
+          if (!__all_sync(0xffffffffu, mbar_wait(bar.full(s), ring.parity))) {
+            ok = false;
+            break;
+          }
+          uint8_t* slot = smem + s * a.slot_bytes;
+          const uint8_t* from = slot + raw_off + r * kSliceK;
+          uint4 v[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c)  // the TMA's 64-byte swizzle
+            v[c] = *(const uint4*)(from + ((c ^ ((r >> 1) & 3)) << 4));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint2 p0 = int8_halves4(v[c].x), p1 = int8_halves4(v[c].y);
+            const uint2 p2 = int8_halves4(v[c].z), p3 = int8_halves4(v[c].w);
+            *(uint4*)(slot + r * 128 + (((2 * c) ^ (r & 7)) << 4)) =
+                make_uint4(p0.x, p0.y, p1.x, p1.y);
+            *(uint4*)(slot + r * 128 + (((2 * c + 1) ^ (r & 7)) << 4)) =
+                make_uint4(p2.x, p2.y, p3.x, p3.y);
+          }
+          fence_async_proxy();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar.ready(s));
+          ring.next(slots);
+        }
+      }
+    }
+  } else {
+    constexpr int kGroup = 128 / sizeof(TOut);  // columns of a staged buffer
+    uint8_t* mine = out_stage + warp * a.out_buffers * kOutBytes;
+    int buffer = 0;
+    Ring acc;
+    for (; ok && t.any(); t.next()) {
+      const int64_t row0 = t.m * kTileM + (warp & 3) * 32;
+      const int64_t n0 = t.n * kCols + (warp >> 2) * kHalf;
+      // a warp whose rows are all past the end has nothing to store, and its buffers may
+      // still be on their way
+      const int cols = row0 < a.rows ? kHalf : 0;
+      const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
+                                (uint32_t)((warp >> 2) * kHalf);
+      float scale = 1.f;
+      if (kConvert && row0 + lane < a.rows)
+        scale = __ldg((const float*)(a.x + (row0 + lane) * a.x_stride + a.row_bytes - 4));
+      // neither a sum (up to 2^31) times such a scale nor that times a column's overflows
+      // unless the whole does
+      const bool plain = __all_sync(0xffffffffu, !(scale > 0x1p90f) && !(scale < 0x1p-90f));
+      float total[kDrain ? kHalf : 1];
+      if constexpr (kDrain) {
+#pragma unroll
+        for (int e = 0; e < kHalf; ++e) total[e] = 0.f;
+      }
+      uint32_t from = 0;
+      for (int k0 = 0; k0 < a.steps; k0 += a.chain) {
+        const int d = acc.slot;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar.done(d), acc.parity))) {
+          ok = false;
+          break;
+        }
+        tcgen05_fence_after();
+        from = lanes_at + (uint32_t)(d * kCols);
+        if constexpr (kDrain) {
+#pragma unroll
+          for (int c = 0; c < kHalf; c += 32) {
+            uint32_t v[32];
+            tmem_load32(from + (uint32_t)c, v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) total[c + e] += __uint_as_float(v[e]);
+          }
+          tcgen05_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar.taken(d));
+        }
+        acc.next(2);
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int c = 0; c < kHalf; c += kGroup) {
+        if (c >= cols || n0 + c >= a.cols) break;
+        // an earlier store has read the buffer
+        if (lane == 0) {
+          if (a.out_buffers == 2)
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          else
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        }
+        __syncwarp();
+        uint8_t* to = mine + buffer * kOutBytes;
+#pragma unroll
+        for (int h = 0; h < kGroup; h += 32) {
+          float y[32];
+          if constexpr (kDrain) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) y[e] = total[c + h + e];
+          } else {
+            uint32_t v[32];
+            tmem_load32(from + (uint32_t)(c + h), v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(v[e]);
+          }
+          if constexpr (kConvert) {
+            float w[32], b[32];
+            load_columns(a.col_scale, n0 + c + h, a.cols, 0.f, w);
+            load_columns(a.bias, n0 + c + h, a.cols, 0.f, b);
+            if (plain) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) y[e] = fmaf(y[e] * scale, w[e], b[e]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) y[e] = scaled(y[e], scale, w[e]) + b[e];
+            }
+          }
+          stage_values<TOut>(to, lane, h * (int)sizeof(TOut), y);
+        }
+        // whole groups only: at a ragged end the TMA writes up to a 16-byte boundary
+        if (a.tma_out && n0 + c + kGroup <= a.cols) {
+          fence_async_proxy();
+          __syncwarp();
+          if (lane == 0)  // rows past the end are left out
+            tma_store(&out_map, (int32_t)(n0 + c), (int32_t)row0, smem_addr(to));
+        } else {
+          __syncwarp();
+          const int64_t rows = a.rows - row0, left = a.cols - n0 - c;
+          store_rows<TOut>(to, lane, (TOut*)a.out + row0 * a.out_stride + n0 + c, a.out_stride,
+                           rows < 32 ? (int)rows : 32, left < kGroup ? (int)left : kGroup);
+          __syncwarp();
+        }
+        // a group for each use of a buffer, an empty one too, so that the wait's count holds
+        if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        if (a.out_buffers == 2) buffer ^= 1;
+      }
+      if constexpr (!kDrain) {
+        tcgen05_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar.taken(acc.slot ^ 1));
+      }
+    }
+    // the stores in flight have read shared memory before the CTA leaves
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  }
+  if (!ok) op_flag(a.status, AGNES_OP_TIMEOUT);
+  tcgen05_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tcgen05_fence_after();
+    tmem_free(tmem, kTmemCols);
+  }
+}
+
+// What a launch of tile_kernel is given: operands in 16 bits, `k` values to a row.
+struct TileOperands {
+  const void *a, *b;  // A of kConvert: 8-bit rows
+  int64_t a_stride, b_stride;  // in bytes
+  int64_t k;
+};
+
+template <typename TOut, bool kConvert, int kCols, bool kDrain>
+cudaError_t launch_tiles(TileArgs a, const TileOperands& o, int device, cudaStream_t st) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return cudaErrorNotSupported;
+  CUtensorMap a_map, b_map, out_map = {};
+  const CUtensorMapDataType type = kConvert ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                            : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const bool mapped =
+      (kConvert ? map_rows(encode, &a_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, o.a, o.k, a.rows,
+                           o.a_stride, kSliceK, kTileM, CU_TENSOR_MAP_SWIZZLE_64B)
+                : map_rows(encode, &a_map, type, o.a, o.k, a.ta * a.rows, o.a_stride, kSliceK,
+                           kTileM, CU_TENSOR_MAP_SWIZZLE_128B)) &&
+      map_rows(encode, &b_map, type, o.b, o.k, a.tb * a.cols, o.b_stride, kSliceK, kCols,
+               CU_TENSOR_MAP_SWIZZLE_128B);
+  if (!mapped) return cudaErrorInvalidValue;
+  const int64_t out_bytes = a.out_stride * (int64_t)sizeof(TOut);
+  a.tma_out = aligned_rows(a.out, out_bytes, 16) && out_bytes < (1ll << 40);
+  if (a.tma_out &&
+      !map_rows(encode, &out_map, kMapType<TOut>, a.out, a.cols, a.rows, out_bytes,
+                (int)(128 / sizeof(TOut)), 32, CU_TENSOR_MAP_SWIZZLE_128B))
+    return cudaErrorInvalidValue;
+  static OncePerDevice once;
+  const cudaError_t e = once.run(device, [] {
+    return cudaFuncSetAttribute(tile_kernel<TOut, kConvert, kCols, kDrain>,
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+  });
+  if (e != cudaSuccess) return e;
+  a.steps = (int32_t)ceil_div(o.k, kSliceK);
+  a.last = (int32_t)ceil_div(o.k - (int64_t)(a.steps - 1) * kSliceK, 16);
+  if (!kDrain) a.chain = a.steps;
+  const int num_sms = op_num_sms(device);
+  const int64_t tiles_m = ceil_div(a.rows, kTileM), tiles_n = ceil_div(a.cols, kCols);
+  const int b_slice = a.tb * kCols * 128;
+  const int a_slice = a.ta * kOperandBytes + (kConvert ? kRawBytes : 0);
+  a.resident = tiles_n <= num_sms &&
+               (int64_t)a.steps * b_slice + 3 * a_slice + kEpilogueWarps * kOutBytes <= kTileSmem;
+  a.slot_bytes = a_slice + (a.resident ? 0 : b_slice);
+  const int fixed = a.resident ? a.steps * b_slice : 0;
+  const auto slots_with = [&](int buffers) {
+    return (kTileSmem - fixed - kEpilogueWarps * buffers * kOutBytes) / a.slot_bytes;
+  };
+  a.out_buffers = slots_with(2) >= 4 ? 2 : 1;
+  const int slots = slots_with(a.out_buffers);
+  a.slots = slots < kMaxSlots ? slots : kMaxSlots;
+  const size_t smem = (size_t)kSmemLimit - kTileSmem + (size_t)a.slots * a.slot_bytes + fixed +
+                      (size_t)kEpilogueWarps * a.out_buffers * kOutBytes;
+  int64_t grid = num_sms;
+  if (a.resident) grid = num_sms / tiles_n * tiles_n;  // a CTA's columns stay the same
+  if (tiles_m <= grid / tiles_n) grid = tiles_m * tiles_n;
+  return launch_next(tile_kernel<TOut, kConvert, kCols, kDrain>, dim3((unsigned)grid),
+                     (unsigned)kTileThreads, smem, st, a_map, b_map, out_map, a);
 }
 
 template <typename TOut, int kRows>
@@ -220,26 +654,121 @@ cudaError_t launch_few(const LinearArgs& a, int device, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-agnes_status check_sizes(const char* op, int64_t rows, int64_t width, int64_t dim) {
+// The forward pass' workspace: the weights as fp16, then their scales.
+struct LinearSpace {
+  int64_t kpad, scales, bytes;
+  LinearSpace(int64_t rows, int64_t width, int64_t dim) {
+    const bool tiles = rows > AGNES_INT8_FEW_ROWS && width > 0;
+    kpad = ceil_div(dim, 8) * 8;
+    scales = ceil_div(width * kpad * 2, 256) * 256;
+    bytes = tiles ? scales + width * 4 : 0;
+  }
+};
+
+// The backward pass': the transposed weights' two terms, then the gradient's where it cannot
+// be taken as it is.
+struct GradInputSpace {
+  int64_t wpad, grad, bytes;
+  GradInputSpace(int64_t rows, int64_t width, int64_t dim, int32_t dtype, bool direct) {
+    wpad = ceil_div(width, 8) * 8;
+    grad = ceil_div(2 * dim * wpad * 2, 256) * 256;
+    bytes = rows > 0 && width > 0 ? grad + (direct ? 0 : grad_terms(dtype) * rows * wpad * 2) : 0;
+  }
+};
+
+template <typename TOut, bool kConvert>
+cudaError_t launch_product(const TileArgs& a, const TileOperands& o, bool drain, int device,
+                           cudaStream_t st) {
+  if (drain) return launch_tiles<TOut, kConvert, 128, true>(a, o, device, st);
+  if (a.cols <= 128) return launch_tiles<TOut, kConvert, 128, false>(a, o, device, st);
+  return launch_tiles<TOut, kConvert, 256, false>(a, o, device, st);
+}
+
+template <typename TOut>
+cudaError_t launch_linear(const LinearArgs& l, void* workspace, int32_t* status, int device,
+                          cudaStream_t st) {
+  const LinearSpace space(l.rows, l.width, l.dim);
+  __half* w = (__half*)workspace;
+  float* scales = (float*)((uint8_t*)workspace + space.scales);
+  const int64_t groups = space.kpad / 8;
+  expand_kernel<<<(unsigned)ceil_div(l.width * groups, kFlat), kPrepThreads, 0, st>>>(
+      l.w, l.w_stride, l.width, l.dim, l.row_bytes, (int32_t)groups, flat_inverse(groups), w,
+      space.kpad, scales);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  TileArgs a = {};
+  a.rows = l.rows;
+  a.cols = l.width;
+  a.ta = a.tb = a.limit = 1;
+  a.chain = 16;  // 1024 products, whose sum of whole numbers is exact
+  a.x = l.x;
+  a.x_stride = l.x_stride;
+  a.row_bytes = l.row_bytes;
+  a.col_scale = scales;
+  a.bias = l.bias;
+  a.out = l.out;
+  a.out_stride = l.out_stride;
+  a.status = status;
+  const TileOperands o = {l.x, w, l.x_stride, space.kpad * 2, l.dim};
+  // 16-bit outputs keep nothing of what a chain of 32,768 products loses
+  const bool drain = l.dim > (sizeof(TOut) == 4 ? 1024 : 32768);
+  return launch_product<TOut, true>(a, o, drain, device, st);
+}
+
+// One value of a row to a lane and turn; see split_grad.
+template <typename T>
+__global__ void __launch_bounds__(kPrepThreads)
+split_kernel(const T* __restrict__ x, int64_t stride, int64_t rows, int64_t width,
+             __nv_bfloat16* __restrict__ out, int64_t wpad) {
+  const int64_t step = (int64_t)gridDim.x * kPrepThreads, total = rows * width;
+  for (int64_t i = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; i < total; i += step) {
+    const int64_t r = i / width, c = i - r * width;
+    const float v = to_f32(x[r * stride + c]);
+    float hi, mid, lo;
+    int8_split(v, hi, mid);
+    __nv_bfloat16* to = out + r * wpad + c;
+    to[0] = __float2bfloat16_rn(hi);
+    if constexpr (sizeof(T) == 4) {
+      int8_split(mid, mid, lo);
+      to[2 * rows * wpad] = __float2bfloat16_rn(lo);
+    }
+    if constexpr (!std::is_same<T, __nv_bfloat16>::value) to[rows * wpad] = __float2bfloat16_rn(mid);
+  }
+}
+
+}  // namespace
+
+cudaError_t split_grad(const void* grad, int32_t dtype, int64_t stride, int64_t rows,
+                       int64_t width, __nv_bfloat16* out, int64_t wpad, cudaStream_t st) {
+  return with_float_type(dtype, [&](auto t) {
+    using T = typename decltype(t)::type;
+    const int64_t ctas = ceil_div(rows * width, 4 * kPrepThreads);
+    split_kernel<T><<<(unsigned)(ctas < 65536 ? ctas : 65536), kPrepThreads, 0, st>>>(
+        (const T*)grad, stride, rows, width, out, wpad);
+    return cudaGetLastError();
+  });
+}
+
+agnes_status product_check_sizes(const char* op, int64_t rows, int64_t width, int64_t dim) {
   if (rows < 0 || width < 0 || dim < 1)
     return op_error(AGNES_EINVAL, "%s: rows %lld, width %lld, dim %lld", op, (long long)rows,
                     (long long)width, (long long)dim);
-  if (rows > kInt8MaxRows || width > kInt8MaxRows || dim > kInt8MaxDim)
+  if (rows >= kProductMaxRows || width >= kProductMaxRows || dim > kInt8MaxDim)
     return op_error(AGNES_ERANGE, "%s: rows %lld, width %lld, dim %lld are too large", op,
                     (long long)rows, (long long)width, (long long)dim);
   return AGNES_OK;
 }
 
-agnes_status check_step(const char* op, const char* name, int64_t rows, int64_t cols,
-                        int64_t stride) {
+agnes_status product_check_step(const char* op, const char* name, int64_t rows, int64_t cols,
+                                int64_t stride) {
   if (rows > 1 && stride < cols)
     return op_error(AGNES_EINVAL, "%s: a stride of %lld of %s is below %lld", op, (long long)stride,
                     name, (long long)cols);
   return AGNES_OK;
 }
 
-agnes_status check_workspace(const char* op, const void* p, int64_t bytes, int64_t need,
-                             int device) {
+agnes_status product_check_workspace(const char* op, const void* p, int64_t bytes, int64_t need,
+                                     int device) {
   if (need == 0) return AGNES_OK;
   OP_TRY(op_on_device(op, "workspace", p, device));
   OP_TRY(op_aligned(op, "workspace", p, 256));
@@ -249,15 +778,11 @@ agnes_status check_workspace(const char* op, const void* p, int64_t bytes, int64
   return AGNES_OK;
 }
 
-int64_t linear_workspace(int64_t, int64_t, int64_t) { return 0; }
-int64_t grad_weight_workspace(int64_t, int64_t, int64_t, int32_t) { return 0; }
-int64_t grad_input_workspace(int64_t, int64_t, int64_t, int32_t) { return 0; }
-
-dim3 tile_grid(int64_t m, int64_t n) {
-  return dim3((unsigned)ceil_div(m, kTile), (unsigned)ceil_div(n, kTile));
+agnes_status check_direct(const char* op, int32_t grad_dtype, int32_t direct) {
+  if ((direct != 0 && direct != 1) || (direct && grad_dtype != AGNES_BF16))
+    return op_error(AGNES_EINVAL, "%s: direct is %d", op, direct);
+  return AGNES_OK;
 }
-
-}  // namespace
 
 }  // namespace agnes
 
@@ -269,8 +794,8 @@ agnes_status agnes_int8_linear_workspace(int64_t rows, int64_t width, int64_t di
                                          int64_t* bytes) {
   const char* op = "agnes_int8_linear_workspace";
   if (!bytes) return op_error(AGNES_EINVAL, "%s: bytes is NULL", op);
-  OP_TRY(check_sizes(op, rows, width, dim));
-  *bytes = linear_workspace(rows, width, dim);
+  OP_TRY(product_check_sizes(op, rows, width, dim));
+  *bytes = LinearSpace(rows, width, dim).bytes;
   return AGNES_OK;
 }
 
@@ -279,11 +804,11 @@ agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, co
                                void* out, int32_t out_dtype, int64_t out_stride, void* workspace,
                                int64_t workspace_bytes, int32_t* status, void* cuda_stream) {
   const char* op = "agnes_int8_linear";
-  OP_TRY(check_sizes(op, rows, width, dim));
+  OP_TRY(product_check_sizes(op, rows, width, dim));
   OP_TRY(op_float_type(op, "out", out_dtype));
   OP_TRY(int8_check_stride(op, "x", rows, dim, x_stride));
   OP_TRY(int8_check_stride(op, "w", width, dim, w_stride));
-  OP_TRY(check_step(op, "out", rows, width, out_stride));
+  OP_TRY(product_check_step(op, "out", rows, width, out_stride));
   if (rows == 0 || width == 0) return AGNES_OK;
   int device = -1;
   OP_TRY(op_device_of(op, "x", x, &device));
@@ -297,7 +822,7 @@ agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, co
     OP_TRY(op_aligned(op, "bias", bias, 4));
   }
   OP_TRY(op_status(op, status, device));
-  OP_TRY(check_workspace(op, workspace, workspace_bytes, linear_workspace(rows, width, dim),
+  OP_TRY(product_check_workspace(op, workspace, workspace_bytes, LinearSpace(rows, width, dim).bytes,
                          device));
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
@@ -321,84 +846,19 @@ agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, co
     if (rows == 2) return launch_few<TOut, 2>(a, device, st);
     if (rows <= 4) return launch_few<TOut, 4>(a, device, st);
     if (rows <= AGNES_INT8_FEW_ROWS) return launch_few<TOut, 8>(a, device, st);
-    linear_kernel<TOut><<<tile_grid(rows, width), 256, 0, st>>>(a);
-    return cudaGetLastError();
-  }));
-}
-
-agnes_status agnes_int8_linear_grad_weight_workspace(int64_t rows, int64_t width, int64_t dim,
-                                                     int32_t grad_dtype, int64_t* bytes) {
-  const char* op = "agnes_int8_linear_grad_weight_workspace";
-  if (!bytes) return op_error(AGNES_EINVAL, "%s: bytes is NULL", op);
-  OP_TRY(check_sizes(op, rows, width, dim));
-  OP_TRY(op_float_type(op, "grad", grad_dtype));
-  *bytes = grad_weight_workspace(rows, width, dim, grad_dtype);
-  return AGNES_OK;
-}
-
-agnes_status agnes_int8_linear_grad_weight(const void* grad, int32_t grad_dtype,
-                                           int64_t grad_stride, int64_t rows, int64_t width,
-                                           const void* x, int64_t x_stride, int64_t dim, void* out,
-                                           int32_t out_dtype, int64_t out_stride, float* dbias,
-                                           void* workspace, int64_t workspace_bytes,
-                                           int32_t* status, void* cuda_stream) {
-  const char* op = "agnes_int8_linear_grad_weight";
-  OP_TRY(check_sizes(op, rows, width, dim));
-  OP_TRY(op_float_type(op, "grad", grad_dtype));
-  OP_TRY(op_float_type(op, "out", out_dtype));
-  OP_TRY(check_step(op, "grad", rows, width, grad_stride));
-  OP_TRY(int8_check_stride(op, "x", rows, dim, x_stride));
-  OP_TRY(check_step(op, "out", width, dim, out_stride));
-  if (width == 0) return AGNES_OK;
-  int device = -1;
-  OP_TRY(op_device_of(op, "out", out, &device));
-  OP_TRY(op_aligned(op, "out", out, float_size(out_dtype)));
-  if (dbias) {
-    OP_TRY(op_on_device(op, "dbias", dbias, device));
-    OP_TRY(op_aligned(op, "dbias", dbias, 4));
-  }
-  if (rows > 0) {
-    OP_TRY(op_on_device(op, "grad", grad, device));
-    OP_TRY(op_on_device(op, "x", x, device));
-    OP_TRY(op_aligned(op, "grad", grad, float_size(grad_dtype)));
-    OP_TRY(op_aligned(op, "x", x, 16));
-  }
-  OP_TRY(op_status(op, status, device));
-  OP_TRY(check_workspace(op, workspace, workspace_bytes,
-                         grad_weight_workspace(rows, width, dim, grad_dtype), device));
-  DeviceGuard dg(device);
-  if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
-  GradArgs a = {};
-  a.grad = grad;
-  a.rows = rows;
-  a.width = width;
-  a.q = (const uint8_t*)x;
-  a.dim = (int32_t)dim;
-  a.row_bytes = (int32_t)int8_row_bytes(dim);
-  a.out = out;
-  a.dbias = dbias;
-  a.grad_stride = rows > 1 ? grad_stride : width;
-  a.q_stride = rows > 1 ? x_stride : a.row_bytes;
-  a.out_stride = width > 1 ? out_stride : dim;
-  const cudaStream_t st = (cudaStream_t)cuda_stream;
-  return op_launched(op, with_float_type(grad_dtype, [&](auto t) {
-    using TGrad = typename decltype(t)::type;
-    if (dbias) grad_bias_kernel<TGrad><<<(unsigned)ceil_div(width, 256), 256, 0, st>>>(a);
-    return with_float_type(out_dtype, [&](auto o) {
-      using TOut = typename decltype(o)::type;
-      grad_weight_kernel<TGrad, TOut><<<tile_grid(width, dim), 256, 0, st>>>(a);
-      return cudaGetLastError();
-    });
+    return launch_linear<TOut>(a, workspace, status, device, st);
   }));
 }
 
 agnes_status agnes_int8_linear_grad_input_workspace(int64_t rows, int64_t width, int64_t dim,
-                                                    int32_t grad_dtype, int64_t* bytes) {
+                                                    int32_t grad_dtype, int32_t direct,
+                                                    int64_t* bytes) {
   const char* op = "agnes_int8_linear_grad_input_workspace";
   if (!bytes) return op_error(AGNES_EINVAL, "%s: bytes is NULL", op);
-  OP_TRY(check_sizes(op, rows, width, dim));
+  OP_TRY(product_check_sizes(op, rows, width, dim));
   OP_TRY(op_float_type(op, "grad", grad_dtype));
-  *bytes = grad_input_workspace(rows, width, dim, grad_dtype);
+  OP_TRY(check_direct(op, grad_dtype, direct));
+  *bytes = GradInputSpace(rows, width, dim, grad_dtype, direct).bytes;
   return AGNES_OK;
 }
 
@@ -409,12 +869,12 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
                                           int64_t workspace_bytes, int32_t* status,
                                           void* cuda_stream) {
   const char* op = "agnes_int8_linear_grad_input";
-  OP_TRY(check_sizes(op, rows, width, dim));
+  OP_TRY(product_check_sizes(op, rows, width, dim));
   OP_TRY(op_float_type(op, "grad", grad_dtype));
   OP_TRY(op_float_type(op, "out", out_dtype));
-  OP_TRY(check_step(op, "grad", rows, width, grad_stride));
+  OP_TRY(product_check_step(op, "grad", rows, width, grad_stride));
   OP_TRY(int8_check_stride(op, "w", width, dim, w_stride));
-  OP_TRY(check_step(op, "out", rows, dim, out_stride));
+  OP_TRY(product_check_step(op, "out", rows, dim, out_stride));
   if (rows == 0) return AGNES_OK;
   int device = -1;
   OP_TRY(op_device_of(op, "out", out, &device));
@@ -426,29 +886,50 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
     OP_TRY(op_aligned(op, "w", w, 16));
   }
   OP_TRY(op_status(op, status, device));
-  OP_TRY(check_workspace(op, workspace, workspace_bytes,
-                         grad_input_workspace(rows, width, dim, grad_dtype), device));
+  const int64_t step = rows > 1 ? grad_stride : width;
+  const bool direct = takes_grad(grad, grad_dtype, rows > 1 ? grad_stride : 0);
+  const GradInputSpace space(rows, width, dim, grad_dtype, direct);
+  OP_TRY(product_check_workspace(op, workspace, workspace_bytes, space.bytes, device));
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
-  GradArgs a = {};
-  a.grad = grad;
-  a.rows = rows;
-  a.width = width;
-  a.q = (const uint8_t*)w;
-  a.dim = (int32_t)dim;
-  a.row_bytes = (int32_t)int8_row_bytes(dim);
-  a.out = out;
-  a.grad_stride = rows > 1 ? grad_stride : width;
-  a.q_stride = width > 1 ? w_stride : a.row_bytes;
-  a.out_stride = rows > 1 ? out_stride : dim;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  return op_launched(op, with_float_type(grad_dtype, [&](auto t) {
-    using TGrad = typename decltype(t)::type;
-    return with_float_type(out_dtype, [&](auto o) {
-      using TOut = typename decltype(o)::type;
-      grad_input_kernel<TGrad, TOut><<<tile_grid(rows, dim), 256, 0, st>>>(a);
-      return cudaGetLastError();
-    });
+  const int64_t out_step = rows > 1 ? out_stride : dim;
+  if (width == 0)  // a sum over nothing
+    return op_launched(op, cudaMemset2DAsync(out, (size_t)(out_step * float_size(out_dtype)), 0,
+                                             (size_t)(dim * float_size(out_dtype)), (size_t)rows,
+                                             st));
+  __nv_bfloat16* wt = (__nv_bfloat16*)workspace;
+  __nv_bfloat16* terms = (__nv_bfloat16*)((uint8_t*)workspace + space.grad);
+  const int64_t row_bytes = int8_row_bytes(dim);
+  transpose_kernel<<<dim3((unsigned)ceil_div(width, kTransTile), (unsigned)ceil_div(dim, kTransTile)),
+                     kPrepThreads, 0, st>>>((const uint8_t*)w, width > 1 ? w_stride : row_bytes,
+                                            width, (int32_t)dim, (int32_t)row_bytes, wt,
+                                            space.wpad);
+  OP_TRY(op_launched(op, cudaGetLastError()));
+  TileOperands o = {grad, wt, rows > 1 ? step * 2 : space.wpad * 2, space.wpad * 2, width};
+  TileArgs a = {};
+  a.ta = 1;
+  if (!direct) {
+    a.ta = grad_terms(grad_dtype);
+    OP_TRY(op_launched(op, split_grad(grad, grad_dtype, step, rows, width, terms, space.wpad, st)));
+    o.a = terms;
+    o.a_stride = space.wpad * 2;
+  }
+  a.rows = rows;
+  a.cols = dim;
+  a.tb = 2;
+  a.limit = 3;  // all products of terms but the third's with the second, below 2^-21 of the whole
+  a.out = out;
+  a.out_stride = out_step;
+  a.status = status;
+  return op_launched(op, with_float_type(out_dtype, [&](auto t) {
+    using TOut = typename decltype(t)::type;
+    // some 48 products of 16 to an accumulator where the sum stays in fp32; 16-bit outputs
+    // keep nothing of what a chain of some thousand loses
+    const int per_slice = 4 * (a.ta == 1 ? 2 : a.ta == 2 ? 4 : 5);
+    a.chain = 48 / per_slice > 0 ? 48 / per_slice : 1;
+    const bool drain = sizeof(TOut) == 4 || width > 16384;
+    return launch_product<TOut, false>(a, o, drain, device, st);
   }));
 }
 

@@ -1,0 +1,42 @@
+// int8_product.cuh -- what the products of 8-bit rows share: the checks of their arguments,
+// and operands as sums of bfloat16 values.
+#pragma once
+
+#include "int8.cuh"
+#include "tcgen05.cuh"
+
+namespace agnes {
+
+// The terms of a gradient lie below one another, and the TMA's coordinates are 32-bit.
+constexpr int64_t kProductMaxRows = 1 << 29;
+
+// A value of up to 16 significant bits as two bfloat16 ones, the first its leading eight
+// bits; what is not finite is the first alone.
+__device__ __forceinline__ void int8_split(float v, float& hi, float& lo) {
+  hi = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  lo = fabsf(hi) <= 3.4e38f ? v - hi : 0.f;
+}
+
+// How many such terms a gradient's type takes: all of its bits.
+inline int grad_terms(int32_t dtype) {
+  return dtype == AGNES_F32 ? 3 : dtype == AGNES_F16 ? 2 : 1;
+}
+
+// Whether the TMA can take a gradient as it is: bfloat16, 16-byte aligned rows.
+inline bool takes_grad(const void* grad, int32_t dtype, int64_t stride) {
+  return dtype == AGNES_BF16 && aligned_rows(grad, stride * 2, 16) && stride * 2 < (1ll << 40);
+}
+
+// rows x width values of dtype, stride apart, as grad_terms(dtype) bfloat16 matrices one
+// after the other, their rows wpad apart (int8_linear.cu).
+cudaError_t split_grad(const void* grad, int32_t dtype, int64_t stride, int64_t rows,
+                       int64_t width, __nv_bfloat16* out, int64_t wpad, cudaStream_t st);
+
+agnes_status product_check_sizes(const char* op, int64_t rows, int64_t width, int64_t dim);
+agnes_status product_check_step(const char* op, const char* name, int64_t rows, int64_t cols,
+                                int64_t stride);
+agnes_status product_check_workspace(const char* op, const void* p, int64_t bytes, int64_t need,
+                                     int device);
+agnes_status check_direct(const char* op, int32_t grad_dtype, int32_t direct);
+
+}  // namespace agnes

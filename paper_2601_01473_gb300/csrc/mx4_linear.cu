@@ -30,13 +30,8 @@
 //
 // Few rows: the weights' bytes count and there is little to multiply, so a warp's
 // lanes take a block of 32 weights each, for all rows.
-#include <cuda.h>
-
-#include <atomic>
-
-#include "mbarrier.cuh"
 #include "mx4.cuh"
-#include "ops_common.cuh"
+#include "tcgen05.cuh"
 
 namespace agnes {
 
@@ -101,31 +96,6 @@ struct LinearArgs {
   int32_t* status;
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) {
-  return (uint32_t)__cvta_generic_to_shared(p);
-}
-
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
-               : "memory");
-}
-
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y,
-                                         uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-
-// A K-major operand with 128-byte swizzle: atoms of 8 rows x 128 bytes, 1024 bytes
-// apart (bits 32-45), descriptor version 1 (bits 46-48), swizzle mode 2 (bits 61-63).
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         (1ull << 46) | (2ull << 61);
-}
-
 // Instruction descriptor of kind::mxf4: e2m1 operands (bits 7-9 and 10-11 = 1), both
 // K-major, N >> 3 at bits 17-22, scales of type ue8m0 (bit 23), M >> 7 at bits
 // 27-28, K = 64 (bit 31 = 0).  Of the four scale bytes of a tensor-memory word a
@@ -144,29 +114,6 @@ __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint
       "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], "
       "[%5], p;\n\t}" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
-      : "memory");
-}
-
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-      : "memory");
-}
-
-// The wait is part of the same statement: apart, arithmetic on the values may be
-// moved before it.
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, "
-      "%10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
-      "%26, %27, %28, %29, %30, %31}, [%32];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
-        "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
-        "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
-        "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]),
-        "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-      : "r"(addr)
       : "memory");
 }
 
@@ -193,19 +140,6 @@ struct Bars {
   __device__ uint32_t w_full() const { return at(3 * kMaxSlots + 4); }
   __device__ uint32_t w_scaled() const { return at(3 * kMaxSlots + 5); }
   __device__ uint32_t drained() const { return at(3 * kMaxSlots + 6); }
-};
-
-struct Ring {
-  int slot = 0;
-  uint32_t parity = 0;  // of the phase that this use completes
-  bool first = true;    // no earlier use to wait for
-  __device__ void next(int n) {
-    if (++slot == n) {
-      slot = 0;
-      parity ^= 1u;
-      first = false;
-    }
-  }
 };
 
 // The output tiles of a CTA, every gridDim.x-th: columns change fastest, so they stay
@@ -295,33 +229,6 @@ __device__ __forceinline__ void stage_columns(uint8_t* buffer, int lane, int fir
       y.v[e] = from_f32<TOut>(__uint_as_float(v[q * kN + e]) + b[q * kN + e]);
     *(Vec<TOut, kN>*)(buffer + lane * 128 + (((first / 16 + q) ^ (lane & 7)) << 4)) = y;
   }
-}
-
-// A warp's buffer to `rows` rows of the output from `to` on, `cols` columns each: for rows
-// that do not suit the TMA and for ragged ends.  A row at a time, its elements side by
-// side.
-template <typename TOut>
-__device__ __forceinline__ void store_rows(const uint8_t* buffer, int lane, TOut* to,
-                                           int64_t stride, int rows, int cols) {
-  constexpr int kGroup = 128 / sizeof(TOut);
-#pragma unroll 4
-  for (int r = 0; r < rows; ++r) {
-#pragma unroll
-    for (int e = 0; e < kGroup; e += 32) {
-      const int byte = (e + lane) * (int)sizeof(TOut);
-      if (e + lane < cols)
-        to[r * stride + e + lane] = *(const TOut*)(buffer + r * 128 +
-                                                   (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
-    }
-  }
-}
-
-__device__ __forceinline__ void tma_store(const CUtensorMap* map, int32_t x, int32_t y,
-                                          uint32_t src) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
-                   map),
-               "r"(x), "r"(y), "r"(src)
-               : "memory");
 }
 
 template <typename TOut>
@@ -686,48 +593,6 @@ linear_few_kernel(int lanes, const LinearArgs a) {
 }
 
 // ---- host ----------------------------------------------------------------------
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                 const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-  static std::atomic<void*> known{nullptr};
-  void* fn = known.load(std::memory_order_acquire);
-  if (!fn) {
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault,
-                                         &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      return nullptr;
-    }
-    known.store(fn, std::memory_order_release);
-  }
-  return (EncodeTiled)fn;
-}
-
-// `rows` rows of `cols` elements of `type`, `stride` bytes apart, in boxes of
-// box_rows x box_cols; zeros past either end.
-bool map_rows(EncodeTiled encode, CUtensorMap* map, CUtensorMapDataType type, const void* p,
-              int64_t cols, int64_t rows, int64_t stride, int box_cols, int box_rows,
-              CUtensorMapSwizzle swizzle) {
-  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)stride};
-  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
-  const cuuint32_t step[2] = {1, 1};
-  return encode(map, type, 2, (void*)p, size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-template <typename T>
-constexpr CUtensorMapDataType kMapType = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
-template <>
-constexpr CUtensorMapDataType kMapType<__half> = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-template <>
-constexpr CUtensorMapDataType kMapType<__nv_bfloat16> = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 
 template <typename TOut>
 cudaError_t launch_linear(LinearArgs a, int device, cudaStream_t st) {

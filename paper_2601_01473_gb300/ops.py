@@ -569,6 +569,12 @@ def int8_linear(x, w, dim: int, bias=None, out_dtype=torch.float32, out=None, st
     return y
 
 
+def _direct(grad, rows, step) -> int:
+    """Whether the kernels can read a gradient as it is."""
+    return int(grad.dtype == torch.bfloat16 and grad.data_ptr() % 16 == 0
+               and (rows <= 1 or step * 2 % 16 == 0 and step * 2 < 1 << 40))
+
+
 def int8_linear_grad_weight(grad, x, dim: int, bias: bool = True, out_dtype=torch.float32,
                             out=None, status=None, stream=None) -> LinearGrad:
     """The gradient of ``int8_linear`` to its weights and bias
@@ -585,7 +591,7 @@ def int8_linear_grad_weight(grad, x, dim: int, bias: bool = True, out_dtype=torc
     db = torch.empty(width, dtype=torch.float32, device=device) if bias else None
     kind = _FLOATS[grad.dtype]
     ws, ws_at, ws_bytes = _workspace(device, "agnes_int8_linear_grad_weight_workspace", rows,
-                                     width, dim, kind)
+                                     width, dim, kind, _direct(grad, rows, step))
     rc = lib().agnes_int8_linear_grad_weight(
         grad.data_ptr(), kind, step, rows, width, x.data_ptr(), x_step, dim, y.data_ptr(), code,
         out_step, db.data_ptr() if bias else None, ws_at, ws_bytes, _status_word(status, device),
@@ -610,7 +616,7 @@ def int8_linear_grad_input(grad, w, dim: int, out_dtype=None, out=None, status=N
     y, code, out_step = _output(out, rows, dim, out_dtype, device)
     kind = _FLOATS[grad.dtype]
     ws, ws_at, ws_bytes = _workspace(device, "agnes_int8_linear_grad_input_workspace", rows, width,
-                                     dim, kind)
+                                     dim, kind, _direct(grad, rows, step))
     rc = lib().agnes_int8_linear_grad_input(
         grad.data_ptr(), kind, step, rows, width, w.data_ptr(), w_step, dim, y.data_ptr(), code,
         out_step, ws_at, ws_bytes, _status_word(status, device), _stream(device))

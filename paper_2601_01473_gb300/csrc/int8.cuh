@@ -56,22 +56,18 @@ __device__ __forceinline__ void int8_values4(uint32_t word, float* q) {
     q[e] = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7540 + e)) - 8388736.f;
 }
 
-// A thread's part of a row, to 8-bit rows at `to`; the group's threads write the row's
-// zeros and scale besides.
+// Vector i of a thread's part of a row, to an 8-bit row at `to`; the group's threads write
+// the row's zeros and scale besides.
 template <int kVec, int kPer>
 __device__ __forceinline__ void int8_store(const RowPart<kVec, kPer>& part, uint8_t* to, bool valid,
-                                           const float (&v)[kVec * kPer], const Int8Scale& s) {
-  if (!valid) return;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int32_t c = part.col(i);
-    if (c >= part.dim) break;
-    if constexpr (kVec == 1) {
-      to[c] = s.fine ? (uint8_t)int8_code(v[i], s) : 0;
-    } else {
-      static_assert(kVec == 8, "8 bytes a store");
-      *(uint2*)(to + c) = make_uint2(int8_codes4(v + i * 8, s), int8_codes4(v + i * 8 + 4, s));
-    }
+                                           int i, const float* v, const Int8Scale& s) {
+  const int32_t c = part.col(i);
+  if (!valid || c >= part.dim) return;
+  if constexpr (kVec == 1) {
+    to[c] = s.fine ? (uint8_t)int8_code(v[0], s) : 0;
+  } else {
+    static_assert(kVec == 8, "8 bytes a store");
+    *(uint2*)(to + c) = make_uint2(int8_codes4(v, s), int8_codes4(v + 4, s));
   }
 }
 __device__ __forceinline__ void int8_store_end(uint8_t* to, int32_t dim, int lane, int lanes,
@@ -82,25 +78,30 @@ __device__ __forceinline__ void int8_store_end(uint8_t* to, int32_t dim, int lan
   if (lane == 0) *(float*)(to + end) = s.scale;
 }
 
-// A thread's part of an 8-bit row as whole numbers; zeros where there is none.
+// A thread's part of an 8-bit row as it lies in memory.
 template <int kVec, int kPer>
-__device__ __forceinline__ void int8_load(const RowPart<kVec, kPer>& part, const uint8_t* row,
-                                          bool valid, float (&q)[kVec * kPer]) {
+struct Int8Regs {
+  uint2 w[kPer];
+  __device__ void load(const RowPart<kVec, kPer>& part, const uint8_t* row, bool valid) {
+    static_assert(kVec == 8, "8 bytes a load");
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int32_t c = part.col(i);
-    if (!valid || c >= part.dim) {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) q[i * kVec + e] = 0.f;
-    } else if constexpr (kVec == 1) {
-      q[i] = (float)(int8_t)row[c];
-    } else {
-      static_assert(kVec == 8, "8 bytes a load");
-      const uint2 w = *(const uint2*)(row + c);
-      int8_values4(w.x, q + i * 8);
-      int8_values4(w.y, q + i * 8 + 4);
-    }
+    for (int i = 0; i < kPer; ++i)
+      w[i] = valid && part.has(i) ? *(const uint2*)(row + part.col(i)) : make_uint2(0, 0);
   }
-}
+  __device__ void get(int i, float* q) const {
+    int8_values4(w[i].x, q);
+    int8_values4(w[i].y, q + 4);
+  }
+};
+template <int kPer>
+struct Int8Regs<1, kPer> {
+  int8_t q[kPer];
+  __device__ void load(const RowPart<1, kPer>& part, const uint8_t* row, bool valid) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      q[i] = valid && part.has(i) ? (int8_t)row[part.col(i)] : (int8_t)0;
+  }
+  __device__ void get(int i, float* f) const { f[0] = (float)q[i]; }
+};
 
 }  // namespace agnes

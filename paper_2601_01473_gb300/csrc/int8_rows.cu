@@ -10,114 +10,195 @@ namespace agnes {
 
 namespace {
 
-constexpr int kElems = 8;  // values of a row to a thread at a time
+constexpr int kElems = 16;   // values of a row to a thread at a time
+constexpr int kLanes = 512;  // threads to a row at most
+constexpr int kBackLanes = 256;
 
 struct KeepArgs {
   const void* x;
   int64_t stride, rows;
   int32_t dim;       // of a half where gated
-  int32_t lanes, groups;
-  int32_t f;         // AGNES_F_*, or -1: no nonlinearity
-  bool gated;        // rows of 2 dim values
-  bool out_rows8;
-  void* out;         // may be null where f is -1
+  int32_t lanes, log_lanes, groups;
+  int32_t f;         // AGNES_F_*
+  void* out;
   int64_t out_stride;
   uint8_t* kept;     // may be null
   int64_t kept_stride;
 };
 
-// f(v), and its derivative where one is asked for.
-template <bool kSlope>
+// The normal distribution function and its density at v, for results of 16 bits:
+// Phi(-a) = exp(-a^2 / 2) t Q(t), t = 1 / (1 + 0.21 a), with Q of degree 8 fitted to the
+// scaled complementary error function over 0 <= a <= 14, to 2^-25.9 of it.  The square's
+// own rounding is put back into the exponential.  (normcdff and a second exponential: gelu of
+// 131,072 x 1024 bf16 278 us forward and 537 backward.)
+__device__ __forceinline__ void normal_fit(float v, float* phi, float* density) {
+  const float a = fminf(fabsf(v), 16.f);
+  const float t = __fdividef(1.f, fmaf(0.21f, a, 1.f));
+  float q = -0.07165663f;
+  q = fmaf(q, t, 0.28359011f);
+  q = fmaf(q, t, -0.33025661f);
+  q = fmaf(q, t, 0.34940478f);
+  q = fmaf(q, t, -0.09392789f);
+  q = fmaf(q, t, 0.12487392f);
+  q = fmaf(q, t, 0.06919184f);
+  q = fmaf(q, t, 0.0850689f);
+  q = fmaf(q, t, 0.08371157f);
+  const float square = a * a, rest = fmaf(a, a, -square);
+  float e = __expf(-0.5f * square);
+  e = fmaf(e, -0.5f * rest, e);
+  const float tail = e * t * q;
+  *phi = v < 0.f ? tail : 1.f - tail;
+  *density = e * 0.3989422804f;  // 1 / sqrt(2 pi)
+}
+
+// f(v), and its derivative where one is asked for; kFit: for results of 16 bits.
+template <bool kSlope, bool kFit>
 __device__ __forceinline__ float nonlinear(int32_t f, float v, float* slope) {
   if (f == AGNES_F_RELU) {
     if (kSlope) *slope = v > 0.f ? 1.f : v <= 0.f ? 0.f : v;
     return v < 0.f ? 0.f : v;
   }
   if (f == AGNES_F_SILU) {
-    const float p = __fdividef(1.f, 1.f + expf(-v));
+    const float p = __fdividef(1.f, 1.f + (kFit ? __expf(-v) : expf(-v)));
     if (kSlope) *slope = p * fmaf(v, 1.f - p, 1.f);
     return v * p;
   }
-  const float p = normcdff(v);
-  if (kSlope) *slope = fmaf(v * 0.3989422804f, expf(-0.5f * v * v), p);  // 1 / sqrt(2 pi)
+  float p, density;
+  if constexpr (kFit) {
+    normal_fit(v, &p, &density);
+  } else {
+    p = normcdff(v);
+    if (kSlope) density = expf(-0.5f * v * v) * 0.3989422804f;
+  }
+  if (kSlope) *slope = fmaf(v, density, p);
   return v * p;
+}
+
+// f with the kind as a constant, chosen once for all of a thread's values.
+template <typename F>
+__device__ __forceinline__ void with_kind(int32_t kind, F&& f) {
+  if (kind == AGNES_F_RELU)
+    f(std::integral_constant<int32_t, AGNES_F_RELU>());
+  else if (kind == AGNES_F_SILU)
+    f(std::integral_constant<int32_t, AGNES_F_SILU>());
+  else
+    f(std::integral_constant<int32_t, AGNES_F_GELU>());
 }
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-template <typename T, int kVec, bool kLoop>
-__global__ void __launch_bounds__(kRowLanesMax)
+// What is made of a row: 8-bit rows alone, a nonlinearity, or a gated one.
+enum { kRound, kPlain, kGated };
+
+template <typename T, int kMode, bool kOut8, int kVec, bool kLoop>
+__global__ void __launch_bounds__(kLanes, kVec == 1 ? 1 : 2)
 keep_kernel(const KeepArgs a) {
   constexpr int kPer = kElems / kVec;
+  constexpr bool kFit = sizeof(T) == 2;
   __shared__ RowScratch scratch;
   int turn = 0;
-  const int group = threadIdx.x / a.lanes, lane = threadIdx.x - group * a.lanes;
+  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
   const int64_t row = (int64_t)blockIdx.x * a.groups + group;
   const bool valid = row < a.rows;
   const T* x = (const T*)a.x + row * a.stride;
   const int32_t chunk = a.lanes * kElems;
-  float v[kElems], u[kElems], y[kElems];
-  // columns c0 on of the row, and what is made of them
-  const auto load = [&](int32_t c0) {
-    const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
-    part.load(x + c0, valid, v);
-    if (a.gated) part.load(x + a.dim + c0, valid, u);
-    if (a.f < 0) return;
-#pragma unroll
-    for (int e = 0; e < kElems; ++e) {
-      y[e] = nonlinear<false>(a.f, v[e], nullptr);
-      if (a.gated) y[e] *= u[e];
-    }
-  };
+  const bool keep = kMode == kRound || a.kept;
+  uint8_t* to8 = (uint8_t*)a.out + row * a.out_stride;
+  T* to = (T*)a.out + row * a.out_stride;
+  RowRegs<T, kVec, kPer> v, u;
+  float y[kOut8 ? kElems : 1];
   uint32_t top[3] = {0, 0, 0};
-  const bool tops = a.kept || a.out_rows8;
-  if (kLoop || tops || a.f >= 0) {
-    for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
-      load(c0);
-      if (!tops) break;
+  // The values are made of the row once: those of a type that is stored as it is go out at
+  // once, those that are rounded to 8 bits wait for their largest magnitude.
+  for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
+    const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
+    v.load(part, x + c0, valid);
+    if constexpr (kMode == kGated) u.load(part, x + a.dim + c0, valid);
+    if (keep) {
+      top[0] = max(top[0], v.top());
+      if constexpr (kMode == kGated) top[1] = max(top[1], u.top());
+    }
+    if constexpr (kMode != kRound) {
+      with_kind(a.f, [&](auto kind) {
 #pragma unroll
-      for (int e = 0; e < kElems; ++e) {
-        top[0] = max(top[0], magnitude(v[e]));
-        if (a.gated) top[1] = max(top[1], magnitude(u[e]));
-        if (a.out_rows8) top[2] = max(top[2], magnitude(y[e]));
-      }
+        for (int i = 0; i < kPer; ++i) {
+          float f[kVec], g[kVec];
+          v.get(i, f);
+          if constexpr (kMode == kGated) u.get(i, g);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            f[e] = nonlinear<false, kFit>(kind, f[e], nullptr);
+            if constexpr (kMode == kGated) f[e] *= g[e];
+            if constexpr (kOut8) {
+              y[i * kVec + e] = f[e];
+              top[2] = max(top[2], magnitude(f[e]));
+            }
+          }
+          if constexpr (!kOut8) part.store_one(to + c0, valid, i, f);
+        }
+      });
     }
   }
-  Int8Scale s[3];
-  if (tops) {
+  if (!keep && !kOut8) return;
+  v.pin();
+  if constexpr (kMode == kGated) u.pin();
+  Int8Scale s = {}, s_gate = {}, s_out = {};
+  if constexpr (kMode == kRound) {
+    uint32_t one[1] = {top[0]};
+    group_reduce<MaxBits>(one, a.lanes, &scratch, turn);
+    s = int8_scale(one[0]);
+  } else {
     group_reduce<MaxBits>(top, a.lanes, &scratch, turn);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) s[k] = int8_scale(top[k]);
+    s = int8_scale(top[0]);
+    if constexpr (kMode == kGated) s_gate = int8_scale(top[1]);
+    if constexpr (kOut8) s_out = int8_scale(top[2]);
   }
   uint8_t* kept = a.kept + row * a.kept_stride;
   const int64_t half = int8_row_bytes(a.dim);
-  uint8_t* out8 = (uint8_t*)a.out + row * a.out_stride;
-  T* out = (T*)a.out + row * a.out_stride;
   for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
-    if (kLoop) load(c0);
     const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
-    if (a.kept) {
-      int8_store(part, kept + c0, valid, v, s[0]);
-      if (a.gated) int8_store(part, kept + half + c0, valid, u, s[1]);
+    if (kLoop) {
+      v.load(part, x + c0, valid);
+      if constexpr (kMode == kGated) u.load(part, x + a.dim + c0, valid);
     }
-    if (a.out_rows8)
-      int8_store(part, out8 + c0, valid, y, s[2]);
-    else if (a.f >= 0)
-      part.store(out + c0, valid, y);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      float f[kVec], g[kVec];
+      v.get(i, f);
+      if constexpr (kMode == kGated) u.get(i, g);
+      if (keep) {
+        int8_store(part, kept + c0, valid, i, f, s);
+        if constexpr (kMode == kGated) int8_store(part, kept + half + c0, valid, i, g, s_gate);
+      }
+      if constexpr (kOut8) {
+        if (kLoop) {
+          with_kind(a.f, [&](auto kind) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+              f[e] = nonlinear<false, kFit>(kind, f[e], nullptr);
+              if constexpr (kMode == kGated) f[e] *= g[e];
+            }
+          });
+          int8_store(part, to8 + c0, valid, i, f, s_out);
+        } else {
+          int8_store(part, to8, valid, i, y + i * kVec, s_out);
+        }
+      }
+    }
   }
-  if (a.kept) {
-    int8_store_end(kept, a.dim, lane, a.lanes, valid, s[0]);
-    if (a.gated) int8_store_end(kept + half, a.dim, lane, a.lanes, valid, s[1]);
+  if (keep) {
+    int8_store_end(kept, a.dim, lane, a.lanes, valid, s);
+    if constexpr (kMode == kGated)
+      int8_store_end(kept + half, a.dim, lane, a.lanes, valid, s_gate);
   }
-  if (a.out_rows8) int8_store_end(out8, a.dim, lane, a.lanes, valid, s[2]);
+  if constexpr (kOut8) int8_store_end(to8, a.dim, lane, a.lanes, valid, s_out);
 }
 
 struct BackArgs {
   const uint8_t* kept;
   int64_t kept_stride, rows;
-  int32_t dim, lanes, groups;
+  int32_t dim, lanes, log_lanes, groups;
   int32_t f;
-  bool gated;
   const void* grad;  // null: the kept values themselves
   int64_t grad_stride;
   void* out;
@@ -140,48 +221,78 @@ __device__ __forceinline__ float most_of<__nv_bfloat16>() {
   return 3.3895313892515355e38f;
 }
 
-// What 8-bit rows stand for, or the nonlinearity's gradient at it.
-template <typename TGrad, typename T, int kVec, bool kGrad>
-__global__ void __launch_bounds__(kRowLanesMax)
+// What 8-bit rows stand for.
+template <typename T, int kVec>
+__global__ void __launch_bounds__(kBackLanes, kVec == 1 ? 4 : 8)
+values_kernel(const BackArgs a) {
+  constexpr int kPer = kElems / kVec;
+  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
+  const int64_t row = (int64_t)blockIdx.x * a.groups + group;
+  if (row >= a.rows) return;
+  const uint8_t* kept = a.kept + row * a.kept_stride;
+  const float scale = *(const float*)(kept + int8_row_bytes(a.dim) - 4);
+  T* out = (T*)a.out + row * a.out_stride;
+  for (int32_t c0 = 0; c0 < a.dim; c0 += a.lanes * kElems) {
+    const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
+    Int8Regs<kVec, kPer> v;
+    v.load(part, kept + c0, true);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      float f[kVec];
+      v.get(i, f);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float most = most_of<T>(), y = f[e] * scale;
+        f[e] = y > most ? most : y < -most ? -most : y;
+      }
+      part.store_one(out + c0, true, i, f);
+    }
+  }
+}
+
+// The nonlinearity's gradient at them.
+template <typename TGrad, typename T, bool kGate, int kVec>
+__global__ void __launch_bounds__(kBackLanes, kVec == 1 ? 2 : 4)
 back_kernel(const BackArgs a) {
   constexpr int kPer = kElems / kVec;
-  const int group = threadIdx.x / a.lanes, lane = threadIdx.x - group * a.lanes;
+  constexpr bool kFit = sizeof(T) == 2;
+  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
   const int64_t row = (int64_t)blockIdx.x * a.groups + group;
-  const bool valid = row < a.rows;
-  if (!valid) return;
+  if (row >= a.rows) return;
   const uint8_t* kept = a.kept + row * a.kept_stride;
   const int64_t half = int8_row_bytes(a.dim);
   const float s0 = *(const float*)(kept + half - 4);
-  const float s1 = kGrad && a.gated ? *(const float*)(kept + 2 * half - 4) : 0.f;
+  const float s1 = kGate ? *(const float*)(kept + 2 * half - 4) : 0.f;
   T* out = (T*)a.out + row * a.out_stride;
   const TGrad* grad = (const TGrad*)a.grad + row * a.grad_stride;
   for (int32_t c0 = 0; c0 < a.dim; c0 += a.lanes * kElems) {
     const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
-    float v[kElems], u[kElems], d[kElems];
-    int8_load(part, kept + c0, true, v);
-    if constexpr (!kGrad) {
+    Int8Regs<kVec, kPer> v, u;
+    RowRegs<TGrad, kVec, kPer> d;
+    v.load(part, kept + c0, true);
+    if constexpr (kGate) u.load(part, kept + half + c0, true);
+    d.load(part, grad + c0, true);
+    with_kind(a.f, [&](auto kind) {
 #pragma unroll
-      for (int e = 0; e < kElems; ++e) {
-        const float most = most_of<T>(), y = v[e] * s0;
-        v[e] = y > most ? most : y < -most ? -most : y;
-      }
-      part.store(out + c0, true, v);
-    } else {
-      if (a.gated) int8_load(part, kept + half + c0, true, u);
-      part.load(grad + c0, true, d);
+      for (int i = 0; i < kPer; ++i) {
+        float f[kVec], g[kVec], h[kVec];
+        v.get(i, f);
+        d.get(i, h);
+        if constexpr (kGate) u.get(i, g);
 #pragma unroll
-      for (int e = 0; e < kElems; ++e) {
-        float slope;
-        const float y = nonlinear<true>(a.f, v[e] * s0, &slope);
-        v[e] = d[e] * slope;
-        if (a.gated) {
-          v[e] *= u[e] * s1;
-          u[e] = d[e] * y;
+        for (int e = 0; e < kVec; ++e) {
+          float slope;
+          const float y = nonlinear<true, kFit>(kind, f[e] * s0, &slope);
+          f[e] = h[e] * slope;
+          if constexpr (kGate) {
+            f[e] *= g[e] * s1;
+            g[e] = h[e] * y;
+          }
         }
+        part.store_one(out + c0, true, i, f);
+        if constexpr (kGate) part.store_one(out + a.dim + c0, true, i, g);
       }
-      part.store(out + c0, true, v);
-      if (a.gated) part.store(out + a.dim + c0, true, u);
-    }
+    });
   }
 }
 
@@ -216,35 +327,39 @@ agnes_status check_kept(const char* op, const char* name, int64_t rows, int64_t 
   return AGNES_OK;
 }
 
-template <typename T>
+template <typename T, int kMode, bool kOut8>
 cudaError_t launch_keep(KeepArgs a, cudaStream_t st) {
   const int64_t next = a.rows > 1 ? 1 : 0;  // a single row has no next one
   const bool aligned =
       aligned_rows(a.x, next * a.stride * (int64_t)sizeof(T), 16) &&
-      (a.f < 0 || a.out_rows8 || aligned_rows(a.out, next * a.out_stride * (int64_t)sizeof(T), 16));
-  const RowShape shape = row_shape(a.dim, kElems);
+      (kMode == kRound || kOut8 ||
+       aligned_rows(a.out, next * a.out_stride * (int64_t)sizeof(T), 16));
+  const RowShape shape = row_shape(a.dim, kElems, kLanes);
   a.lanes = shape.lanes;
+  a.log_lanes = shape.log_lanes;
   a.groups = shape.groups;
   const bool loop = a.dim > a.lanes * kElems;
-  const auto kernel = vec_of(a.dim, aligned) == 8
-                          ? (loop ? keep_kernel<T, 8, true> : keep_kernel<T, 8, false>)
-                          : (loop ? keep_kernel<T, 1, true> : keep_kernel<T, 1, false>);
+  const auto kernel = vec_of(a.dim, aligned) == 8 ? (loop ? keep_kernel<T, kMode, kOut8, 8, true>
+                                                          : keep_kernel<T, kMode, kOut8, 8, false>)
+                                                  : (loop ? keep_kernel<T, kMode, kOut8, 1, true>
+                                                          : keep_kernel<T, kMode, kOut8, 1, false>);
   kernel<<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), 0, st>>>(a);
   return cudaGetLastError();
 }
 
-template <typename TGrad, typename T, bool kGrad>
-cudaError_t launch_back(BackArgs a, cudaStream_t st) {
+// kernels[0] for vectors, [1] for single elements
+using BackKernel = void (*)(BackArgs);
+cudaError_t launch_back(const BackKernel (&kernels)[2], BackArgs a, int64_t grad_size,
+                        int64_t size, cudaStream_t st) {
   const int64_t next = a.rows > 1 ? 1 : 0;
-  const bool aligned =
-      aligned_rows(a.out, next * a.out_stride * (int64_t)sizeof(T), 16) &&
-      (!kGrad || aligned_rows(a.grad, next * a.grad_stride * (int64_t)sizeof(TGrad), 16));
-  const RowShape shape = row_shape(a.dim, kElems);
+  const bool aligned = aligned_rows(a.out, next * a.out_stride * size, 16) &&
+                       (!a.grad || aligned_rows(a.grad, next * a.grad_stride * grad_size, 16));
+  const RowShape shape = row_shape(a.dim, kElems, kBackLanes);
   a.lanes = shape.lanes;
+  a.log_lanes = shape.log_lanes;
   a.groups = shape.groups;
-  const auto kernel = vec_of(a.dim, aligned) == 8 ? back_kernel<TGrad, T, 8, kGrad>
-                                                  : back_kernel<TGrad, T, 1, kGrad>;
-  kernel<<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), 0, st>>>(a);
+  kernels[vec_of(a.dim, aligned) == 8 ? 0 : 1]
+      <<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), 0, st>>>(a);
   return cudaGetLastError();
 }
 
@@ -296,11 +411,10 @@ agnes_status agnes_int8_quantize(const void* x, int32_t dtype, int64_t stride, i
   a.stride = stride;
   a.rows = rows;
   a.dim = (int32_t)dim;
-  a.f = -1;
   a.kept = (uint8_t*)out;
   a.kept_stride = out_stride;
   return op_launched(op, with_float_type(dtype, [&](auto t) {
-    return launch_keep<typename decltype(t)::type>(a, (cudaStream_t)cuda_stream);
+    return launch_keep<typename decltype(t)::type, kRound, false>(a, (cudaStream_t)cuda_stream);
   }));
 }
 
@@ -329,7 +443,8 @@ agnes_status agnes_int8_dequantize(const void* x, int64_t stride, int64_t rows, 
   a.out_stride = out_stride;
   return op_launched(op, with_float_type(dtype, [&](auto t) {
     using T = typename decltype(t)::type;
-    return launch_back<T, T, false>(a, (cudaStream_t)cuda_stream);
+    const BackKernel kernels[2] = {values_kernel<T, 8>, values_kernel<T, 1>};
+    return launch_back(kernels, a, 0, sizeof(T), (cudaStream_t)cuda_stream);
   }));
 }
 
@@ -369,14 +484,16 @@ agnes_status agnes_activation(const void* x, int32_t dtype, int64_t stride, int6
   a.rows = rows;
   a.dim = (int32_t)dim;
   a.f = f;
-  a.gated = gated != 0;
-  a.out_rows8 = out_dtype == AGNES_INT8_ROWS;
   a.out = out;
   a.out_stride = out_stride;
   a.kept = (uint8_t*)kept;
   a.kept_stride = kept_stride;
   return op_launched(op, with_float_type(dtype, [&](auto t) {
-    return launch_keep<typename decltype(t)::type>(a, (cudaStream_t)cuda_stream);
+    using T = typename decltype(t)::type;
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (out_dtype == AGNES_INT8_ROWS)
+      return gated ? launch_keep<T, kGated, true>(a, st) : launch_keep<T, kPlain, true>(a, st);
+    return gated ? launch_keep<T, kGated, false>(a, st) : launch_keep<T, kPlain, false>(a, st);
   }));
 }
 
@@ -409,7 +526,6 @@ agnes_status agnes_activation_grad(const void* grad, int32_t grad_dtype, int64_t
   a.rows = rows;
   a.dim = (int32_t)dim;
   a.f = f;
-  a.gated = gated != 0;
   a.grad = grad;
   a.grad_stride = grad_stride;
   a.out = out;
@@ -417,7 +533,11 @@ agnes_status agnes_activation_grad(const void* grad, int32_t grad_dtype, int64_t
   return op_launched(op, with_float_type(grad_dtype, [&](auto t) {
     using TGrad = typename decltype(t)::type;
     return with_float_type(out_dtype, [&](auto o) {
-      return launch_back<TGrad, typename decltype(o)::type, true>(a, (cudaStream_t)cuda_stream);
+      using T = typename decltype(o)::type;
+      const BackKernel kernels[2][2] = {
+          {back_kernel<TGrad, T, false, 8>, back_kernel<TGrad, T, false, 1>},
+          {back_kernel<TGrad, T, true, 8>, back_kernel<TGrad, T, true, 1>}};
+      return launch_back(kernels[gated], a, sizeof(TGrad), sizeof(T), (cudaStream_t)cuda_stream);
     });
   }));
 }

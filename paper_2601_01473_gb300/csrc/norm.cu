@@ -178,7 +178,7 @@ norm_kernel(const NormArgs a) {
     group_reduce<MaxBits>(top, a.lanes, &scratch, r.turn);
     const Int8Scale s = int8_scale(top[0]);
     uint8_t* to = (uint8_t*)a.next + row * a.next_stride;
-    int8_store(r.part, to, valid, x, s);
+    for (int i = 0; i < kPer; ++i) int8_store(r.part, to, valid, i, x + i * kVec, s);
     int8_store_end(to, a.dim, lane, a.lanes, valid, s);
   } else {
     r.part.store((TBranch*)a.next + row * a.next_stride, valid, x);

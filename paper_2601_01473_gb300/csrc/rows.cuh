@@ -8,6 +8,8 @@
 // 256 threads, or a group's if that is more.
 #pragma once
 
+#include <type_traits>
+
 #include "ops_common.cuh"
 
 namespace agnes {
@@ -17,16 +19,20 @@ constexpr int kRowLanesMax = 1024;
 
 // How a launch spreads its rows.
 struct RowShape {
-  int32_t lanes;   // threads to a row
-  int32_t groups;  // rows of a CTA at a time
+  int32_t lanes, log_lanes;  // threads to a row
+  int32_t groups;            // rows of a CTA at a time
   unsigned threads() const { return (unsigned)(lanes * groups); }
 };
 
-// For rows of `cols` columns, `per_thread` of them to a thread.
-inline RowShape row_shape(int64_t cols, int per_thread) {
-  int32_t lanes = 1;
-  while (lanes < kRowLanesMax && (int64_t)lanes * per_thread < cols) lanes *= 2;
-  return {lanes, lanes < kRowThreads ? kRowThreads / lanes : 1};
+// For rows of `cols` columns, `per_thread` of them to a thread, `most` threads at most.
+inline RowShape row_shape(int64_t cols, int per_thread, int most = kRowLanesMax) {
+  RowShape s = {1, 0, 0};
+  while (s.lanes < most && (int64_t)s.lanes * per_thread < cols) {
+    s.lanes *= 2;
+    ++s.log_lanes;
+  }
+  s.groups = s.lanes < kRowThreads ? kRowThreads / s.lanes : 1;
+  return s;
 }
 
 template <typename T, int kVec>
@@ -79,8 +85,98 @@ struct RowPart {
     for (int i = 0; i < kPer; ++i)
       if (valid && col(i) < dim) store_vec<T, kVec>(row + col(i), v + i * kVec);
   }
+  // vector i
+  template <typename T>
+  __device__ void store_one(T* row, bool valid, int i, const float* v) const {
+    if (valid && col(i) < dim) store_vec<T, kVec>(row + col(i), v);
+  }
   // elements past the end hold zeros or what a row's arithmetic made of them
   __device__ bool has(int i) const { return col(i) < dim; }
+};
+
+// A thread's part of a row as it lies in memory: two 16-bit values to a register.
+template <typename T, int kVec, int kPer>
+struct RowRegs {
+  static constexpr int kWords = kVec * sizeof(T) / 4;
+  uint32_t w[kPer][kWords];
+
+  __device__ void load(const RowPart<kVec, kPer>& part, const T* row, bool valid) {
+    constexpr int kQuads = kWords / 4;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+#pragma unroll
+      for (int h = 0; h < kQuads; ++h) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (valid && part.has(i)) v = ((const uint4*)(row + part.col(i)))[h];
+        w[i][4 * h] = v.x;
+        w[i][4 * h + 1] = v.y;
+        w[i][4 * h + 2] = v.z;
+        w[i][4 * h + 3] = v.w;
+      }
+    }
+  }
+  // vector i
+  __device__ void get(int i, float* f) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) f[e] = __uint_as_float(w[i][e]);
+    } else if constexpr (std::is_same<T, __half>::value) {
+#pragma unroll
+      for (int e = 0; e < kWords; ++e) {
+        const float2 v = __half22float2(*(const __half2*)&w[i][e]);
+        f[2 * e] = v.x;
+        f[2 * e + 1] = v.y;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kWords; ++e) {
+        f[2 * e] = __uint_as_float(w[i][e] << 16);
+        f[2 * e + 1] = __uint_as_float(w[i][e] & 0xffff0000u);
+      }
+    }
+  }
+  // The largest magnitude, as the bits of a float.
+  __device__ uint32_t top() const {
+    uint32_t most = 0;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+#pragma unroll
+        for (int e = 0; e < kWords; ++e) most = max(most, w[i][e] & 0x7fffffffu);
+      return most;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+#pragma unroll
+        for (int e = 0; e < kWords; ++e) most = __vmaxu2(most, w[i][e] & 0x7fff7fffu);
+      const uint16_t bits = (uint16_t)max(most & 0xffffu, most >> 16);
+      return __float_as_uint(to_f32(*(const T*)&bits));
+    }
+  }
+  // Keeps the values as they are across this point, instead of what was made of them.
+  __device__ void pin() {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+#pragma unroll
+      for (int e = 0; e < kWords; ++e) asm volatile("" : "+r"(w[i][e]));
+  }
+};
+// Single elements, for rows that no vector divides.
+template <typename T, int kPer>
+struct RowRegs<T, 1, kPer> {
+  float v[kPer];
+
+  __device__ void load(const RowPart<1, kPer>& part, const T* row, bool valid) {
+    part.load(row, valid, v);
+  }
+  __device__ void get(int i, float* f) const { f[0] = v[i]; }
+  __device__ uint32_t top() const {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+    return most;
+  }
+  __device__ void pin() {}
 };
 
 struct SumOp {

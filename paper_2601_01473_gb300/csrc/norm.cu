@@ -22,14 +22,19 @@ namespace agnes {
 
 namespace {
 
-constexpr int kElems = 8;  // of a row to a thread
-constexpr int64_t kNormMaxDim = (int64_t)kRowLanesMax * kElems;
+constexpr int kElems = 16;       // of a row to a thread, forward; rows of up to
+constexpr int kShortElems = 8;   // kShortDim columns take fewer, and two rows at a time,
+constexpr int kShortDim = 256;   // and so does the backward pass, which has more to hold
+constexpr int kNormLanes = 512;  // threads to a row at most, forward
+constexpr int64_t kNormMaxDim = 8192;
+static_assert(kNormLanes * kElems >= kNormMaxDim && kRowLanesMax * kShortElems >= kNormMaxDim,
+              "a row in registers");
 constexpr int64_t kNormMaxRows = 0x7fffffff - 2047;
-constexpr int kSums = 5;  // before, before_bias, after, after_bias, gate
+constexpr int kSums = 5;  // of before, after, gate, before_bias and after_bias
 
 struct NormArgs {
   int64_t rows;
-  int32_t dim, lanes, groups;
+  int32_t dim, lanes, log_lanes, groups;
   const void *x, *branch, *gate;  // the backward pass has the sum as x
   int64_t x_stride, branch_stride, gate_stride;
   int32_t gate_kind;
@@ -50,225 +55,432 @@ struct NormArgs {
   int32_t sums;
 };
 
-struct RowStats {
-  float mean, inv;
+// Two values of fp32 in one register pair, for the packed arithmetic: each half is rounded
+// as by a single instruction.
+struct Two {
+  uint64_t p;
 };
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.p) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ Two both(float a) { return two(a, a); }
+__device__ __forceinline__ float2 apart(Two a) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(a.p));
+  return f;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.p) : "l"(a.p), "l"(b.p));
+  return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.p) : "l"(a.p), "l"(b.p));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.p) : "l"(a.p), "l"(b.p), "l"(c.p));
+  return r;
+}
 
+// A thread's values of a row: vector i's are pairs i * kVec / 2 on.
 template <int kVec, int kPer>
 struct NormRow {
-  static constexpr int kN = kVec * kPer;
+  static constexpr int kPairs = kVec * kPer / 2;
+  using Values = Two[kPairs];
   RowPart<kVec, kPer> part;
   RowScratch* scratch;
   int turn = 0;
+
+  template <typename T>
+  static __device__ void unpack(const RowRegs<T, kVec, kPer>& from, Values& v) {
+    float f[kVec * kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) from.get(i, f + i * kVec);
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) v[e] = two(f[2 * e], f[2 * e + 1]);
+  }
+  template <typename T>
+  __device__ void load(const T* row, bool valid, Values& v) const {
+    RowRegs<T, kVec, kPer> r;
+    r.load(part, row, valid);
+    unpack(r, v);
+  }
+  template <typename T>
+  __device__ void store(T* row, bool valid, const Values& v) const {
+    float f[kVec * kPer];
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) {
+      const float2 x = apart(v[e]);
+      f[2 * e] = x.x;
+      f[2 * e + 1] = x.y;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) part.store_one(row, valid, i, f + i * kVec);
+  }
+  // whether the elements of pair e are in the row: of single elements they are apart
+  __device__ bool has(int e, int half) const { return part.has((2 * e + half) / kVec); }
+
+  static __device__ float total(const Values& v) {
+    Two s = v[0];
+#pragma unroll
+    for (int e = 1; e < kPairs; ++e) s = s + v[e];
+    const float2 f = apart(s);
+    return f.x + f.y;
+  }
+  static __device__ float total(const Values& v, const Values& w) {
+    Two s = v[0] * w[0];
+#pragma unroll
+    for (int e = 1; e < kPairs; ++e) s = fma2(v[e], w[e], s);
+    const float2 f = apart(s);
+    return f.x + f.y;
+  }
 
   template <int kCount>
   __device__ void sum(float (&v)[kCount]) {
     group_reduce<SumOp>(v, part.lanes, scratch, turn);
   }
 
-  // v becomes N(v); zeros past the row's end
-  __device__ RowStats standard(float (&v)[kN], bool layer, float eps, float inv_dim) {
-    RowStats r = {0.f, 0.f};
+  // v becomes what it is without its mean (of AGNES_NORM_LAYER), zeros past the row's end;
+  // inv is 1 / the root.
+  template <int kRows>
+  __device__ void standard(Values (&v)[kRows], bool layer, float eps, float inv_dim,
+                           float (&inv)[kRows]) {
+    float s[kRows];
     if (layer) {
-      float s[1] = {0.f};
 #pragma unroll
-      for (int e = 0; e < kN; ++e) s[0] += v[e];
+      for (int r = 0; r < kRows; ++r) s[r] = total(v[r]);
       sum(s);
-      r.mean = s[0] * inv_dim;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
+      for (int r = 0; r < kRows; ++r) {
+        const float mean = -(s[r] * inv_dim);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[i * kVec + e] = part.has(i) ? v[i * kVec + e] - r.mean : 0.f;
+        for (int e = 0; e < kPairs; ++e)
+          v[r][e] = v[r][e] + two(has(e, 0) ? mean : 0.f, has(e, 1) ? mean : 0.f);
+      }
     }
-    float s[1] = {0.f};
 #pragma unroll
-    for (int e = 0; e < kN; ++e) s[0] = fmaf(v[e], v[e], s[0]);
+    for (int r = 0; r < kRows; ++r) s[r] = total(v[r], v[r]);
     sum(s);
-    r.inv = 1.f / sqrtf(fmaf(s[0], inv_dim, eps));
 #pragma unroll
-    for (int e = 0; e < kN; ++e) v[e] *= r.inv;
-    return r;
+    for (int r = 0; r < kRows; ++r) inv[r] = 1.f / sqrtf(fmaf(s[r], inv_dim, eps));
   }
 
   // A vector over the columns; `fill` where there is none.
-  __device__ void vector(const float* p, float fill, float (&v)[kN]) const {
+  __device__ void vector(const float* p, float fill, Values& v) const {
     if (p) {
-      part.load(p, true, v);
+      load(p, true, v);
     } else {
 #pragma unroll
-      for (int e = 0; e < kN; ++e) v[e] = fill;
+      for (int e = 0; e < kPairs; ++e) v[e] = both(fill);
     }
   }
 
   // the gradient to v of the gradient d to n = N(v)
-  __device__ void through(float (&d)[kN], const float (&n)[kN], bool layer, float inv,
-                          float inv_dim) {
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < kN; ++e) {
-      s[0] = fmaf(d[e], n[e], s[0]);
-      s[1] += d[e];
+  __device__ void through(Values& d, const Values& n, bool layer, float inv, float inv_dim) {
+    float along, mean = 0.f;
+    if (layer) {
+      float s[2] = {total(d, n), total(d)};
+      sum(s);
+      along = s[0];
+      mean = s[1] * inv_dim;
+    } else {
+      float s[1] = {total(d, n)};
+      sum(s);
+      along = s[0];
     }
-    sum(s);
-    const float along = s[0] * inv_dim, mean = layer ? s[1] * inv_dim : 0.f;
+    const Two a = both(-(along * inv_dim)), m = both(-mean), i = both(inv);
 #pragma unroll
-    for (int e = 0; e < kN; ++e) d[e] = (d[e] - mean - n[e] * along) * inv;
+    for (int e = 0; e < kPairs; ++e) d[e] = (fma2(n[e], a, d[e]) + m) * i;
   }
 };
 
-// A row times a gate's values, as gate_kind has them.
-template <typename TBranch, int kVec, int kPer>
-__device__ __forceinline__ void load_gate(const NormRow<kVec, kPer>& r, const NormArgs& a,
-                                          int64_t row, bool valid, float (&g)[kVec * kPer]) {
-  if (a.gate_kind == AGNES_GATE_ROWS)
-    r.part.load((const TBranch*)a.gate + row * a.gate_stride, valid, g);
-  else
-    r.vector(a.gate_kind == AGNES_GATE_COLUMNS ? (const float*)a.gate : nullptr, 1.f, g);
-}
-
-template <typename TX, typename TBranch, int kVec, int kPer>
-__global__ void __launch_bounds__(kRowLanesMax)
+// kRows rows to a group at a time: the vectors over the columns are loaded once for all of
+// them, and the exchanges of their sums overlap.
+template <typename TX, typename TBranch, int kVec, int kPer, int kRows>
+__global__ void __launch_bounds__(kNormLanes)
 norm_kernel(const NormArgs a) {
-  constexpr int kN = kVec * kPer;
+  using Row = NormRow<kVec, kPer>;
+  constexpr int kPairs = Row::kPairs;
   __shared__ RowScratch scratch;
-  const int group = threadIdx.x / a.lanes, lane = threadIdx.x - group * a.lanes;
-  NormRow<kVec, kPer> r = {{a.lanes, lane, a.dim}, &scratch};
-  const int64_t row = (int64_t)blockIdx.x * a.groups + group;
-  const bool valid = row < a.rows;
-  float x[kN];
-  r.part.load((const TX*)a.x + row * a.x_stride, valid, x);
+  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
+  Row n = {{a.lanes, lane, a.dim}, &scratch};
+  const int64_t row0 = ((int64_t)blockIdx.x * kRows) * a.groups + group;
+  RowRegs<TX, kVec, kPer> x_regs[kRows];
+  RowRegs<TBranch, kVec, kPer> b_regs[kRows], g_regs[kRows];
+  const auto row = [&](int r) { return row0 + (int64_t)r * a.groups; };
+  const bool gate_rows = a.gate_kind == AGNES_GATE_ROWS;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const bool valid = row(r) < a.rows;
+    x_regs[r].load(n.part, (const TX*)a.x + row(r) * a.x_stride, valid);
+    if (a.branch)
+      b_regs[r].load(n.part, (const TBranch*)a.branch + row(r) * a.branch_stride, valid);
+    if (gate_rows) g_regs[r].load(n.part, (const TBranch*)a.gate + row(r) * a.gate_stride, valid);
+  }
+  Two x[kRows][kPairs], w[kPairs], b[kPairs];
+  float inv[kRows];
   if (a.branch) {
-    float u[kN], w[kN];
-    r.part.load((const TBranch*)a.branch + row * a.branch_stride, valid, u);
+    Two u[kRows][kPairs];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) Row::unpack(b_regs[r], u[r]);
     if (a.after) {
-      r.standard(u, a.layer, a.eps, a.inv_dim);
-      r.vector(a.after, 1.f, w);
+      n.standard(u, a.layer, a.eps, a.inv_dim, inv);
+      n.vector(a.after, 1.f, w);
+      n.vector(a.after_bias, 0.f, b);
 #pragma unroll
-      for (int e = 0; e < kN; ++e) u[e] *= w[e];
-      if (a.after_bias) {
-        r.vector(a.after_bias, 0.f, w);
+      for (int r = 0; r < kRows; ++r)
 #pragma unroll
-        for (int e = 0; e < kN; ++e) u[e] += w[e];
+        for (int e = 0; e < kPairs; ++e) u[r][e] = fma2(u[r][e] * both(inv[r]), w[e], b[e]);
+    }
+    // scale gate
+    if (!gate_rows) {
+      n.vector(a.gate_kind == AGNES_GATE_COLUMNS ? (const float*)a.gate : nullptr, 1.f, w);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) w[e] = w[e] * both(a.scale);
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      if (gate_rows) {
+        Row::unpack(g_regs[r], w);
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) w[e] = w[e] * both(a.scale);
       }
-    }
-    if (a.gate_kind != AGNES_GATE_NONE) {
-      load_gate<TBranch>(r, a, row, valid, w);
+      Row::unpack(x_regs[r], x[r]);
 #pragma unroll
-      for (int e = 0; e < kN; ++e) u[e] *= w[e];
+      for (int e = 0; e < kPairs; ++e) {
+        const float2 f = apart(fma2(w[e], u[r][e], x[r][e]));
+        x[r][e] = two(to_f32(from_f32<TX>(f.x)), to_f32(from_f32<TX>(f.y)));
+      }
+      n.store((TX*)a.sum + row(r) * a.sum_stride, row(r) < a.rows, x[r]);
     }
+  } else {
 #pragma unroll
-    for (int e = 0; e < kN; ++e) x[e] = to_f32(from_f32<TX>(fmaf(a.scale, u[e], x[e])));
-    r.part.store((TX*)a.sum + row * a.sum_stride, valid, x);
+    for (int r = 0; r < kRows; ++r) Row::unpack(x_regs[r], x[r]);
   }
   if (!a.next) return;
-  float w[kN];
-  r.standard(x, a.layer, a.eps, a.inv_dim);
-  r.vector(a.before, 1.f, w);
+  n.standard(x, a.layer, a.eps, a.inv_dim, inv);
+  n.vector(a.before, 1.f, w);
+  n.vector(a.before_bias, 0.f, b);
 #pragma unroll
-  for (int e = 0; e < kN; ++e) x[e] *= w[e];
-  if (a.before_bias) {
-    r.vector(a.before_bias, 0.f, w);
+  for (int r = 0; r < kRows; ++r)
 #pragma unroll
-    for (int e = 0; e < kN; ++e) x[e] += w[e];
-  }
+    for (int e = 0; e < kPairs; ++e) x[r][e] = fma2(x[r][e] * both(inv[r]), w[e], b[e]);
   if (a.next_rows8) {
-    uint32_t top[1] = {0};
+    uint32_t top[kRows];
 #pragma unroll
-    for (int e = 0; e < kN; ++e) top[0] = max(top[0], __float_as_uint(x[e]) & 0x7fffffffu);
-    group_reduce<MaxBits>(top, a.lanes, &scratch, r.turn);
-    const Int8Scale s = int8_scale(top[0]);
-    uint8_t* to = (uint8_t*)a.next + row * a.next_stride;
-    for (int i = 0; i < kPer; ++i) int8_store(r.part, to, valid, i, x + i * kVec, s);
-    int8_store_end(to, a.dim, lane, a.lanes, valid, s);
+    for (int r = 0; r < kRows; ++r) {
+      top[r] = 0;
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        const float2 f = apart(x[r][e]);
+        top[r] = max(top[r], max(__float_as_uint(f.x) & 0x7fffffffu,
+                                 __float_as_uint(f.y) & 0x7fffffffu));
+      }
+    }
+    group_reduce<MaxBits>(top, a.lanes, &scratch, n.turn);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const Int8Scale s = int8_scale(top[r]);
+      uint8_t* to = (uint8_t*)a.next + row(r) * a.next_stride;
+      const bool valid = row(r) < a.rows;
+      float f[2 * kPairs];
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        const float2 v = apart(x[r][e]);
+        f[2 * e] = v.x;
+        f[2 * e + 1] = v.y;
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) int8_store(n.part, to, valid, i, f + i * kVec, s);
+      int8_store_end(to, a.dim, lane, a.lanes, valid, s);
+    }
   } else {
-    r.part.store((TBranch*)a.next + row * a.next_stride, valid, x);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      n.store((TBranch*)a.next + row(r) * a.next_stride, row(r) < a.rows, x[r]);
   }
 }
 
-// kThreads: the most that a CTA has.  A thread's sums stay in registers, of which a CTA of
-// 1024 has 64 a thread.
-template <typename TX, typename TBranch, int kVec, int kPer, int kThreads>
+// A thread's sums over the rows: in registers, or (kShared) in shared memory, where a thread
+// has too few of them.
+template <int kPairs, int kCount, bool kShared>
+struct Totals {
+  Two v[kShared ? 1 : kCount][kPairs];
+  float4* mine;  // [sum][quad][thread]
+  __device__ void init(float4* shared) {
+    mine = shared + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < kCount; ++k)
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        if constexpr (kShared) {
+          if (e % 2 == 0)
+            mine[(k * (kPairs / 2) + e / 2) * blockDim.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+          v[k][e] = both(0.f);
+        }
+      }
+  }
+  // of pairs e and e + 1
+  __device__ void add(int k, int e, Two a, Two b) {
+    if constexpr (kShared) {
+      float4* at = mine + (k * (kPairs / 2) + e / 2) * blockDim.x;
+      const float4 t = *at;
+      const float2 x = apart(a + two(t.x, t.y)), y = apart(b + two(t.z, t.w));
+      *at = make_float4(x.x, x.y, y.x, y.y);
+    } else {
+      v[k][e] = v[k][e] + a;
+      v[k][e + 1] = v[k][e + 1] + b;
+    }
+  }
+  __device__ void add_product(int k, int e, Two a, Two b, Two c, Two d) {
+    if constexpr (kShared) {
+      add(k, e, a * b, c * d);
+    } else {
+      v[k][e] = fma2(a, b, v[k][e]);
+      v[k][e + 1] = fma2(c, d, v[k][e + 1]);
+    }
+  }
+  __device__ float get(int k, int at) const {
+    if constexpr (kShared) {
+      return ((const float*)&mine[(k * (kPairs / 2) + at / 4) * blockDim.x])[at % 4];
+    } else {
+      const float2 f = apart(v[k][at / 2]);
+      return at & 1 ? f.y : f.x;
+    }
+  }
+};
+
+// Which sums there are, so that the others take no registers: of before, after and gate, or
+// of the biases too.
+enum { kBefore, kAfter, kGateSum, kBeforeBias, kAfterBias, kMostSums };
+
+// A row ahead: what a row needs is on its way while the one before it is worked on.
+template <typename TX, typename TBranch, int kVec, int kPer>
+struct GradRegs {
+  RowRegs<TX, kVec, kPer> x, d_sum;
+  RowRegs<TBranch, kVec, kPer> d_next, branch;
+  __device__ void load(const RowPart<kVec, kPer>& part, const NormArgs& a, int64_t row) {
+    const bool valid = row < a.rows;
+    if (a.d_sum) d_sum.load(part, (const TX*)a.d_sum + row * a.d_sum_stride, valid);
+    if (a.before) {
+      x.load(part, (const TX*)a.x + row * a.x_stride, valid);
+      d_next.load(part, (const TBranch*)a.d_next + row * a.d_next_stride, valid);
+    }
+    if (a.branch) branch.load(part, (const TBranch*)a.branch + row * a.branch_stride, valid);
+  }
+};
+
+template <typename TX, typename TBranch, int kVec, int kPer, int kThreads, bool kBias, bool kShared>
 __global__ void __launch_bounds__(kThreads)
 norm_grad_kernel(const NormArgs a) {
-  constexpr int kN = kVec * kPer;
+  using Row = NormRow<kVec, kPer>;
+  constexpr int kPairs = Row::kPairs;
+  constexpr int kCount = kBias ? kMostSums : kBeforeBias;
   __shared__ RowScratch scratch;
-  extern __shared__ float group_sums[];  // [groups][dim], where a CTA has several rows
-  const int group = threadIdx.x / a.lanes, lane = threadIdx.x - group * a.lanes;
-  NormRow<kVec, kPer> r = {{a.lanes, lane, a.dim}, &scratch};
-  float total[kSums][kN];
-#pragma unroll
-  for (int k = 0; k < kSums; ++k)
-#pragma unroll
-    for (int e = 0; e < kN; ++e) total[k][e] = 0.f;
+  extern __shared__ float4 grad_smem[];  // shared sums, or [groups][dim] of the end
+  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
+  Row r = {{a.lanes, lane, a.dim}, &scratch};
+  Totals<kPairs, kCount, kShared> total;
+  total.init(grad_smem);
   const int64_t step = (int64_t)gridDim.x * a.groups;
+  GradRegs<TX, TBranch, kVec, kPer> ahead;
+  ahead.load(r.part, a, (int64_t)blockIdx.x * a.groups + group);
   for (int64_t first = (int64_t)blockIdx.x * a.groups; first < a.rows; first += step) {
     const int64_t row = first + group;
     const bool valid = row < a.rows;
-    float d[kN], w[kN];
+    Two d[kPairs], w[kPairs], n[1][kPairs], branch[1][kPairs];
+    float inv[1];
     if (a.d_sum) {
-      r.part.load((const TX*)a.d_sum + row * a.d_sum_stride, valid, d);
+      Row::unpack(ahead.d_sum, d);
     } else {
 #pragma unroll
-      for (int e = 0; e < kN; ++e) d[e] = 0.f;
+      for (int e = 0; e < kPairs; ++e) d[e] = both(0.f);
     }
+    Two g[kPairs];
     if (a.before) {
-      float n[kN], g[kN];
-      r.part.load((const TX*)a.x + row * a.x_stride, valid, n);
-      r.part.load((const TBranch*)a.d_next + row * a.d_next_stride, valid, g);
-      const RowStats s = r.standard(n, a.layer, a.eps, a.inv_dim);
+      Row::unpack(ahead.x, n[0]);
+      Row::unpack(ahead.d_next, g);
+    }
+    if (a.branch) Row::unpack(ahead.branch, branch[0]);
+    ahead.load(r.part, a, row + step);
+    if (a.before) {
+      r.standard(n, a.layer, a.eps, a.inv_dim, inv);
       r.vector(a.before, 1.f, w);
 #pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        if (valid) {  // where there is no row and eps is 0, n is no number
-          total[0][e] = fmaf(g[e], n[e], total[0][e]);
-          total[1][e] += g[e];
+      for (int e = 0; e < kPairs; ++e) n[0][e] = n[0][e] * both(inv[0]);
+      if (valid) {  // where there is no row and eps is 0, n is no number
+#pragma unroll
+        for (int e = 0; e < kPairs; e += 2) {
+          total.add_product(kBefore, e, g[e], n[0][e], g[e + 1], n[0][e + 1]);
+          if constexpr (kBias) total.add(kBeforeBias, e, g[e], g[e + 1]);
         }
-        g[e] *= w[e];
       }
-      r.through(g, n, a.layer, s.inv, a.inv_dim);
 #pragma unroll
-      for (int e = 0; e < kN; ++e) d[e] += g[e];
+      for (int e = 0; e < kPairs; ++e) g[e] = g[e] * w[e];
+      r.through(g, n[0], a.layer, inv[0], a.inv_dim);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) d[e] = d[e] + g[e];
     }
-    r.part.store((TX*)a.dx + row * a.dx_stride, valid, d);
+    r.store((TX*)a.dx + row * a.dx_stride, valid, d);
     if (!a.branch) continue;
-    float n[kN], b[kN];
-    r.part.load((const TBranch*)a.branch + row * a.branch_stride, valid, n);
-    RowStats s = {0.f, 1.f};
-    if (a.after) s = r.standard(n, a.layer, a.eps, a.inv_dim);
+    if (a.after) {
+      r.standard(branch, a.layer, a.eps, a.inv_dim, inv);
 #pragma unroll
-    for (int e = 0; e < kN; ++e) d[e] *= a.scale;
+      for (int e = 0; e < kPairs; ++e) branch[0][e] = branch[0][e] * both(inv[0]);
+    }
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) d[e] = d[e] * both(a.scale);
     if (a.gate_kind != AGNES_GATE_NONE) {
       // u, then d u
       r.vector(a.after, 1.f, w);
+      Two b[kPairs];
       r.vector(a.after_bias, 0.f, b);
 #pragma unroll
-      for (int e = 0; e < kN; ++e) b[e] = d[e] * fmaf(n[e], w[e], b[e]);
-      load_gate<TBranch>(r, a, row, valid, w);
+      for (int e = 0; e < kPairs; ++e) b[e] = fma2(branch[0][e], w[e], b[e]);
       if (a.gate_kind == AGNES_GATE_ROWS) {
-        r.part.store((TBranch*)a.dgate + row * a.dgate_stride, valid, b);
-      } else if (valid) {
+        Two gate[kPairs];
+        r.load((const TBranch*)a.gate + row * a.gate_stride, valid, gate);
 #pragma unroll
-        for (int e = 0; e < kN; ++e) total[4][e] += b[e];
+        for (int e = 0; e < kPairs; ++e) {
+          b[e] = d[e] * b[e];
+          d[e] = d[e] * gate[e];
+        }
+        r.store((TBranch*)a.dgate + row * a.dgate_stride, valid, b);
+      } else {
+        if (valid) {
+#pragma unroll
+          for (int e = 0; e < kPairs; e += 2)
+            total.add_product(kGateSum, e, d[e], b[e], d[e + 1], b[e + 1]);
+        }
+        r.vector((const float*)a.gate, 1.f, b);
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) d[e] = d[e] * b[e];
       }
-#pragma unroll
-      for (int e = 0; e < kN; ++e) d[e] *= w[e];
     }
     if (a.after) {
       r.vector(a.after, 1.f, w);
+      if (valid) {
 #pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        if (valid) {
-          total[2][e] = fmaf(d[e], n[e], total[2][e]);
-          total[3][e] += d[e];
+        for (int e = 0; e < kPairs; e += 2) {
+          total.add_product(kAfter, e, d[e], branch[0][e], d[e + 1], branch[0][e + 1]);
+          if constexpr (kBias) total.add(kAfterBias, e, d[e], d[e + 1]);
         }
-        d[e] *= w[e];
       }
-      r.through(d, n, a.layer, s.inv, a.inv_dim);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) d[e] = d[e] * w[e];
+      r.through(d, branch[0], a.layer, inv[0], a.inv_dim);
     }
-    r.part.store((TBranch*)a.dbranch + row * a.dbranch_stride, valid, d);
+    r.store((TBranch*)a.dbranch + row * a.dbranch_stride, valid, d);
   }
   // a CTA's sums: its groups' added in order
-  for (int k = 0; k < kSums; ++k) {
+#pragma unroll
+  for (int k = 0; k < kCount; ++k) {
     if (a.slot[k] < 0) continue;
     float* to = a.partial + ((int64_t)blockIdx.x * a.sums + a.slot[k]) * a.dim;
     if (a.groups == 1) {
@@ -276,15 +488,16 @@ norm_grad_kernel(const NormArgs a) {
       for (int i = 0; i < kPer; ++i)
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
-          if (r.part.has(i)) to[r.part.col(i) + e] = total[k][i * kVec + e];
+          if (r.part.has(i)) to[r.part.col(i) + e] = total.get(k, i * kVec + e);
       continue;
     }
+    float* group_sums = (float*)grad_smem;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
 #pragma unroll
       for (int e = 0; e < kVec; ++e)
-        if (r.part.has(i)) group_sums[group * a.dim + r.part.col(i) + e] = total[k][i * kVec + e];
+        if (r.part.has(i)) group_sums[group * a.dim + r.part.col(i) + e] = total.get(k, i * kVec + e);
     __syncthreads();
     for (int c = threadIdx.x; c < a.dim; c += blockDim.x) {
       float sum = 0.f;
@@ -431,9 +644,9 @@ bool wide_inputs(const NormArgs& a, int64_t x_size, int64_t branch_size) {
       .ok();
 }
 
-void set_shape(NormArgs& a) {
-  const RowShape shape = row_shape(a.dim, kElems);
+void set_shape(NormArgs& a, const RowShape& shape) {
   a.lanes = shape.lanes;
+  a.log_lanes = shape.log_lanes;
   a.groups = shape.groups;
   a.inv_dim = 1.f / (float)a.dim;
 }
@@ -441,12 +654,38 @@ void set_shape(NormArgs& a) {
 // CTAs of the backward pass: each writes a row of partial sums, so no more than keep the
 // device busy.
 int64_t grad_ctas(int64_t rows, int64_t dim, int sms) {
-  const RowShape shape = row_shape(dim, kElems);
+  const RowShape shape = row_shape(dim, kShortElems);
   const int64_t ctas = ceil_div(rows, shape.groups);
-  const int64_t most = (int64_t)sms * (1024 / shape.threads());
+  // a thread's sums and the row ahead leave room for 512 threads to an SM
+  const int64_t most = (int64_t)sms * (shape.threads() <= 256 ? 2 : 1);
   return ctas < most ? ctas : most;
 }
 constexpr int kMostSms = 256;  // for the size of a workspace, whatever device it will be on
+
+// A sum's bytes of shared memory where the threads keep it there.
+size_t dim_smem(const NormArgs& a) { return (size_t)a.lanes * kShortElems * 4; }
+
+template <typename TX, typename TBranch, bool kBias>
+cudaError_t launch_grad(const NormArgs& a, bool wide, int64_t ctas, size_t smem, int device,
+                        cudaStream_t st) {
+  using Kernel = void (*)(NormArgs);
+  constexpr int kPer = kShortElems;
+  const Kernel long_rows = wide ? norm_grad_kernel<TX, TBranch, 8, 1, 1024, kBias, true>
+                                : norm_grad_kernel<TX, TBranch, 1, kPer, 1024, kBias, true>;
+  const Kernel kernel = a.lanes > 512 ? long_rows
+                        : wide        ? norm_grad_kernel<TX, TBranch, 8, 1, 512, kBias, false>
+                                      : norm_grad_kernel<TX, TBranch, 1, kPer, 512, kBias, false>;
+  if (a.lanes > 512) {
+    static OncePerDevice once[2];
+    const cudaError_t e = once[wide].run(device, [&] {
+      return cudaFuncSetAttribute(long_rows, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  kSums * kRowLanesMax * kShortElems * 4);
+    });
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<(unsigned)ctas, (unsigned)(a.lanes * a.groups), smem, st>>>(a);
+  return cudaGetLastError();
+}
 
 }  // namespace
 
@@ -508,7 +747,6 @@ agnes_status agnes_residual_norm(const void* x, int32_t x_dtype, int64_t x_strid
   }
   DeviceGuard dg(device);
   if (!dg.ok()) return op_error(AGNES_ECUDA, "%s: cudaSetDevice(%d) failed", op, device);
-  set_shape(a);
   const bool wide = wide_inputs(a, x_size, branch_size) &&
                     Wide(a)
                         .rows(branch ? sum : nullptr, sum_stride, x_size)
@@ -517,9 +755,12 @@ agnes_status agnes_residual_norm(const void* x, int32_t x_dtype, int64_t x_strid
   return op_launched(op, with_norm_types(x_dtype, branch_dtype, [&](auto tx, auto tb) {
     using TX = typename decltype(tx)::type;
     using TBranch = typename decltype(tb)::type;
-    const auto kernel =
-        wide ? norm_kernel<TX, TBranch, 8, 1> : norm_kernel<TX, TBranch, 1, kElems>;
-    kernel<<<(unsigned)ceil_div(rows, a.groups), (unsigned)(a.lanes * a.groups), 0,
+    const bool brief = wide && dim <= kShortDim;
+    set_shape(a, row_shape(dim, brief ? kShortElems : kElems, kNormLanes));
+    const auto kernel = brief  ? norm_kernel<TX, TBranch, 8, 1, 2>
+                        : wide ? norm_kernel<TX, TBranch, 8, 2, 1>
+                               : norm_kernel<TX, TBranch, 1, kElems, 1>;
+    kernel<<<(unsigned)ceil_div(rows, a.groups * (brief ? 2 : 1)), (unsigned)(a.lanes * a.groups), 0,
              (cudaStream_t)cuda_stream>>>(a);
     return cudaGetLastError();
   }));
@@ -575,9 +816,10 @@ agnes_status agnes_residual_norm_grad(
     return op_error(AGNES_EINVAL, "%s: dafter without after", op);
   if ((dbefore || dbefore_bias) && !before)
     return op_error(AGNES_EINVAL, "%s: dbefore without before", op);
-  float* const outs[kSums] = {dbefore, dbefore_bias, dafter, dafter_bias,
-                              gate_kind == AGNES_GATE_COLUMNS ? (float*)dgate : nullptr};
-  const char* const names[kSums] = {"dbefore", "dbefore_bias", "dafter", "dafter_bias", "dgate"};
+  float* const outs[kSums] = {dbefore, dafter,
+                              gate_kind == AGNES_GATE_COLUMNS ? (float*)dgate : nullptr,
+                              dbefore_bias, dafter_bias};
+  const char* const names[kSums] = {"dbefore", "dafter", "dgate", "dbefore_bias", "dafter_bias"};
   JoinArgs join = {};
   for (int k = 0; k < kSums; ++k) {
     a.slot[k] = outs[k] ? a.sums++ : -1;
@@ -622,7 +864,7 @@ agnes_status agnes_residual_norm_grad(
                       (long long)workspace_bytes, (long long)(ctas * a.sums * dim * 4));
   }
   a.partial = (float*)workspace;
-  set_shape(a);
+  set_shape(a, row_shape(dim, kShortElems));
   const int64_t x_size = float_size(x_dtype), branch_size = float_size(branch_dtype);
   const bool wide = wide_inputs(a, x_size, branch_size) &&
                     Wide(a)
@@ -633,16 +875,15 @@ agnes_status agnes_residual_norm_grad(
                         .rows(gate_kind == AGNES_GATE_ROWS ? dgate : nullptr, dgate_stride,
                               branch_size)
                         .ok();
-  const size_t smem = a.groups > 1 && a.sums ? (size_t)a.groups * dim * 4 : 0;
+  const bool biases = dbefore_bias || dafter_bias, shared = a.lanes > 512;
+  const size_t smem = shared          ? (size_t)(biases ? kSums : kBeforeBias) * dim_smem(a)
+                      : a.groups > 1 ? (size_t)a.groups * dim * 4
+                                      : 0;
   const cudaError_t e = with_norm_types(x_dtype, branch_dtype, [&](auto tx, auto tb) {
     using TX = typename decltype(tx)::type;
     using TBranch = typename decltype(tb)::type;
-    const auto kernel = a.lanes <= 512 ? (wide ? norm_grad_kernel<TX, TBranch, 8, 1, 512>
-                                               : norm_grad_kernel<TX, TBranch, 1, kElems, 512>)
-                                       : (wide ? norm_grad_kernel<TX, TBranch, 8, 1, 1024>
-                                               : norm_grad_kernel<TX, TBranch, 1, kElems, 1024>);
-    kernel<<<(unsigned)ctas, (unsigned)(a.lanes * a.groups), smem, st>>>(a);
-    return cudaGetLastError();
+    return biases ? launch_grad<TX, TBranch, true>(a, wide, ctas, smem, device, st)
+                  : launch_grad<TX, TBranch, false>(a, wide, ctas, smem, device, st);
   });
   OP_TRY(op_launched(op, e));
   if (!a.sums) return AGNES_OK;

@@ -180,13 +180,21 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
           const uint32_t at = ring_at + (uint32_t)(s * a.slot_bytes);
           const int64_t left = a.rows - (int64_t)k * kSlice;
           const int n = left < kSlice ? (int)((left + 15) / 16) : kSlice / 16;
-          for (int i = 0; i < n; ++i)
-            for (int p = 0; p < a.ta; ++p) {
-              mma_16bit(to, operand_desc_mn(at + (uint32_t)(p * kGradBytes + i * 2048), kBox),
-                        operand_desc_mn(at + value_off + (uint32_t)(i * 2048), kBox), kIdesc,
-                        accumulate);
-              accumulate = 1;
-            }
+          // descriptors are sums of constants: one thread issues all products
+          const uint64_t g0 = operand_desc_mn(at, kBox), v0 = operand_desc_mn(at + value_off, kBox);
+#pragma unroll
+          for (int i = 0; i < kSlice / 16; ++i) {
+            if (i >= n) break;
+            mma_16bit(to, g0 + (uint64_t)(i * 128), v0 + (uint64_t)(i * 128), kIdesc,
+                      accumulate | (uint32_t)(i > 0));
+            if (a.ta > 1)
+              mma_16bit(to, g0 + (uint64_t)(i * 128 + (kGradBytes >> 4)), v0 + (uint64_t)(i * 128),
+                        kIdesc, 1);
+            if (a.ta > 2)
+              mma_16bit(to, g0 + (uint64_t)(i * 128 + 2 * (kGradBytes >> 4)),
+                        v0 + (uint64_t)(i * 128), kIdesc, 1);
+          }
+          accumulate = 1;
           mma_commit(bar.empty(s));
           ring.next(a.slots);
         }

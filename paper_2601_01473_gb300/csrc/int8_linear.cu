@@ -179,7 +179,6 @@ struct TileArgs {
   int32_t steps;       // slices of the contraction
   int32_t last;        // products of 16 in the last one
   int32_t ta, tb;      // terms of A and of B
-  int32_t limit;       // of the terms' products those with a + b < limit count
   int32_t chain;       // slices that one accumulator sums
   const uint8_t* x;    // rows whose scales the output takes, or null
   int64_t x_stride;
@@ -277,6 +276,28 @@ __device__ __forceinline__ uint2 int8_halves4(uint32_t word) {
   const __half2 a = __hsub2(*(const __half2*)&low, offset);
   const __half2 b = __hsub2(*(const __half2*)&high, offset);
   return make_uint2(*(const uint32_t*)&a, *(const uint32_t*)&b);
+}
+
+// A slice's products, n of 16 for each two terms but the third with the second.  The thread
+// that issues them has one at a time to prepare, so their descriptors are sums of constants
+// (looked up term by term a product took some 250 cycles to issue, twice its own time).
+template <int kTermsA, int kTermsB, int kCols>
+__device__ __forceinline__ void slice_products(uint32_t to, uint32_t a_at, uint32_t b_at, int n,
+                                               uint32_t idesc, uint32_t accumulate) {
+  const uint64_t a0 = operand_desc(a_at), b0 = operand_desc(b_at);
+#pragma unroll
+  for (int i = 0; i < kSliceK / 16; ++i) {
+    if (i >= n) break;
+#pragma unroll
+    for (int p = 0; p < kTermsA; ++p)
+#pragma unroll
+      for (int q = 0; q < kTermsB; ++q) {
+        if (p + q >= 3) continue;
+        mma_16bit(to, a0 + (uint64_t)(p * (kOperandBytes >> 4) + 2 * i),
+                  b0 + (uint64_t)(q * (kCols * 128 >> 4) + 2 * i), idesc,
+                  accumulate | (uint32_t)(i + p + q > 0));
+      }
+  }
 }
 
 // out = A B^T over tiles of 128 x kCols.  kConvert: A is 8-bit rows, brought as they are and
@@ -400,22 +421,15 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
             const uint32_t b_at =
                 a.resident ? resident_at + (uint32_t)(k * a.tb) * kBBytes : a_at + b_off;
             const int n = k + 1 == a.steps ? a.last : kSliceK / 16;
-            for (int i = 0; i < n; ++i) {
-              if constexpr (kConvert) {
-                mma_16bit(to, operand_desc(a_at + 32u * (uint32_t)i),
-                          operand_desc(b_at + 32u * (uint32_t)i), kIdesc, accumulate);
-                accumulate = 1;
-              } else {
-                for (int p = 0; p < a.ta; ++p)
-                  for (int q = 0; q < a.tb && p + q < a.limit; ++q) {
-                    mma_16bit(to,
-                              operand_desc(a_at + (uint32_t)(p * kOperandBytes) + 32u * (uint32_t)i),
-                              operand_desc(b_at + (uint32_t)q * kBBytes + 32u * (uint32_t)i), kIdesc,
-                              accumulate);
-                    accumulate = 1;
-                  }
-              }
-            }
+            if (kConvert)
+              slice_products<1, 1, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+            else if (a.ta == 1)
+              slice_products<1, 2, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+            else if (a.ta == 2)
+              slice_products<2, 2, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+            else
+              slice_products<3, 2, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+            accumulate = 1;
             mma_commit(bar.empty(s));
             ring.next(slots);
           }
@@ -467,7 +481,18 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
     uint8_t* mine = out_stage + warp * a.out_buffers * kOutBytes;
     int buffer = 0;
     Ring acc;
+    // a tile ahead, as it is some trip away
+    const auto scale_of = [&](const TileWalk& at) {
+      const int64_t row = at.m * kTileM + (warp & 3) * 32 + lane;
+      return kConvert && at.any() && row < a.rows
+                 ? __ldg((const float*)(a.x + row * a.x_stride + a.row_bytes - 4)) : 1.f;
+    };
+    float next_scale = scale_of(t);
     for (; ok && t.any(); t.next()) {
+      const float scale = next_scale;
+      TileWalk after = t;
+      after.next();
+      next_scale = scale_of(after);
       const int64_t row0 = t.m * kTileM + (warp & 3) * 32;
       const int64_t n0 = t.n * kCols + (warp >> 2) * kHalf;
       // a warp whose rows are all past the end has nothing to store, and its buffers may
@@ -475,9 +500,6 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
       const int cols = row0 < a.rows ? kHalf : 0;
       const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
                                 (uint32_t)((warp >> 2) * kHalf);
-      float scale = 1.f;
-      if (kConvert && row0 + lane < a.rows)
-        scale = __ldg((const float*)(a.x + (row0 + lane) * a.x_stride + a.row_bytes - 4));
       // neither a sum (up to 2^31) times such a scale nor that times a column's overflows
       // unless the whole does
       const bool plain = __all_sync(0xffffffffu, !(scale > 0x1p90f) && !(scale < 0x1p-90f));
@@ -699,7 +721,7 @@ cudaError_t launch_linear(const LinearArgs& l, void* workspace, int32_t* status,
   TileArgs a = {};
   a.rows = l.rows;
   a.cols = l.width;
-  a.ta = a.tb = a.limit = 1;
+  a.ta = a.tb = 1;
   a.chain = 16;  // 1024 products, whose sum of whole numbers is exact
   a.x = l.x;
   a.x_stride = l.x_stride;
@@ -918,7 +940,6 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
   a.rows = rows;
   a.cols = dim;
   a.tb = 2;
-  a.limit = 3;  // all products of terms but the third's with the second, below 2^-21 of the whole
   a.out = out;
   a.out_stride = out_step;
   a.status = status;

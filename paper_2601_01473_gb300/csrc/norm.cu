@@ -87,8 +87,31 @@ __device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
   return r;
 }
 
-// A thread's values of a row: vector i's are pairs i * kVec / 2 on.
-template <int kVec, int kPer>
+// Two values rounded to T, as they are then.
+template <typename T>
+__device__ __forceinline__ Two rounded(Two a) {
+  const float2 f = apart(a);
+  if constexpr (std::is_same<T, __half>::value) {
+    const float2 r = __half22float2(__floats2half2_rn(f.x, f.y));
+    return two(r.x, r.y);
+  } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    const uint32_t w = *(const uint32_t*)&h;
+    return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  } else {
+    return a;
+  }
+}
+
+// 1 / sqrt(x): the estimate corrected once by its residual, where that is a number.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float y = rsqrtf(x), r = fmaf(-x * y, y, 1.f);
+  return r == r ? fmaf(0.5f * y, r, y) : y;
+}
+
+// A thread's values of a row: vector i's are pairs i * kVec / 2 on.  kLanes: threads to a row
+// where that is known.
+template <int kVec, int kPer, int kLanes = 0>
 struct NormRow {
   static constexpr int kPairs = kVec * kPer / 2;
   using Values = Two[kPairs];
@@ -142,7 +165,7 @@ struct NormRow {
 
   template <int kCount>
   __device__ void sum(float (&v)[kCount]) {
-    group_reduce<SumOp>(v, part.lanes, scratch, turn);
+    group_reduce<SumOp, kLanes>(v, part.lanes, scratch, turn);
   }
 
   // v becomes what it is without its mean (of AGNES_NORM_LAYER), zeros past the row's end;
@@ -167,7 +190,31 @@ struct NormRow {
     for (int r = 0; r < kRows; ++r) s[r] = total(v[r], v[r]);
     sum(s);
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) inv[r] = 1.f / sqrtf(fmaf(s[r], inv_dim, eps));
+    for (int r = 0; r < kRows; ++r) inv[r] = inverse_root(fmaf(s[r], inv_dim, eps));
+  }
+
+  // `standard` of two independent rows at once, either of which may be left out
+  __device__ void standard_of(Values& x, bool with_x, Values& y, bool with_y, bool layer,
+                              float eps, float inv_dim, float& inv_x, float& inv_y) {
+    float s[2] = {0.f, 0.f};
+    const auto centre = [&](Values& v, float sum) {
+      const float mean = -(sum * inv_dim);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e)
+        v[e] = v[e] + two(has(e, 0) ? mean : 0.f, has(e, 1) ? mean : 0.f);
+    };
+    if (layer) {
+      if (with_x) s[0] = total(x);
+      if (with_y) s[1] = total(y);
+      sum(s);
+      if (with_x) centre(x, s[0]);
+      if (with_y) centre(y, s[1]);
+    }
+    if (with_x) s[0] = total(x, x);
+    if (with_y) s[1] = total(y, y);
+    sum(s);
+    inv_x = inverse_root(fmaf(s[0], inv_dim, eps));
+    inv_y = inverse_root(fmaf(s[1], inv_dim, eps));
   }
 
   // A vector over the columns; `fill` where there is none.
@@ -201,10 +248,10 @@ struct NormRow {
 
 // kRows rows to a group at a time: the vectors over the columns are loaded once for all of
 // them, and the exchanges of their sums overlap.
-template <typename TX, typename TBranch, int kVec, int kPer, int kRows>
-__global__ void __launch_bounds__(kNormLanes)
+template <typename TX, typename TBranch, int kVec, int kPer, int kRows, int kLanes>
+__global__ void __launch_bounds__(kLanes ? kRowThreads : kNormLanes)
 norm_kernel(const NormArgs a) {
-  using Row = NormRow<kVec, kPer>;
+  using Row = NormRow<kVec, kPer, kLanes>;
   constexpr int kPairs = Row::kPairs;
   __shared__ RowScratch scratch;
   const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
@@ -252,10 +299,7 @@ norm_kernel(const NormArgs a) {
       }
       Row::unpack(x_regs[r], x[r]);
 #pragma unroll
-      for (int e = 0; e < kPairs; ++e) {
-        const float2 f = apart(fma2(w[e], u[r][e], x[r][e]));
-        x[r][e] = two(to_f32(from_f32<TX>(f.x)), to_f32(from_f32<TX>(f.y)));
-      }
+      for (int e = 0; e < kPairs; ++e) x[r][e] = rounded<TX>(fma2(w[e], u[r][e], x[r][e]));
       n.store((TX*)a.sum + row(r) * a.sum_stride, row(r) < a.rows, x[r]);
     }
   } else {
@@ -282,7 +326,7 @@ norm_kernel(const NormArgs a) {
                                  __float_as_uint(f.y) & 0x7fffffffu));
       }
     }
-    group_reduce<MaxBits>(top, a.lanes, &scratch, n.turn);
+    group_reduce<MaxBits, kLanes>(top, a.lanes, &scratch, n.turn);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       const Int8Scale s = int8_scale(top[r]);
@@ -376,10 +420,11 @@ struct GradRegs {
   }
 };
 
-template <typename TX, typename TBranch, int kVec, int kPer, int kThreads, bool kBias, bool kShared>
+template <typename TX, typename TBranch, int kVec, int kPer, int kThreads, bool kBias, bool kShared,
+          int kLanes>
 __global__ void __launch_bounds__(kThreads)
 norm_grad_kernel(const NormArgs a) {
-  using Row = NormRow<kVec, kPer>;
+  using Row = NormRow<kVec, kPer, kLanes>;
   constexpr int kPairs = Row::kPairs;
   constexpr int kCount = kBias ? kMostSums : kBeforeBias;
   __shared__ RowScratch scratch;
@@ -394,8 +439,8 @@ norm_grad_kernel(const NormArgs a) {
   for (int64_t first = (int64_t)blockIdx.x * a.groups; first < a.rows; first += step) {
     const int64_t row = first + group;
     const bool valid = row < a.rows;
-    Two d[kPairs], w[kPairs], n[1][kPairs], branch[1][kPairs];
-    float inv[1];
+    Two d[kPairs], w[kPairs], n[kPairs], branch[kPairs];
+    float inv, branch_inv;
     if (a.d_sum) {
       Row::unpack(ahead.d_sum, d);
     } else {
@@ -404,35 +449,34 @@ norm_grad_kernel(const NormArgs a) {
     }
     Two g[kPairs];
     if (a.before) {
-      Row::unpack(ahead.x, n[0]);
+      Row::unpack(ahead.x, n);
       Row::unpack(ahead.d_next, g);
     }
-    if (a.branch) Row::unpack(ahead.branch, branch[0]);
+    if (a.branch) Row::unpack(ahead.branch, branch);
     ahead.load(r.part, a, row + step);
+    r.standard_of(n, a.before, branch, a.after, a.layer, a.eps, a.inv_dim, inv, branch_inv);
     if (a.before) {
-      r.standard(n, a.layer, a.eps, a.inv_dim, inv);
       r.vector(a.before, 1.f, w);
 #pragma unroll
-      for (int e = 0; e < kPairs; ++e) n[0][e] = n[0][e] * both(inv[0]);
+      for (int e = 0; e < kPairs; ++e) n[e] = n[e] * both(inv);
       if (valid) {  // where there is no row and eps is 0, n is no number
 #pragma unroll
         for (int e = 0; e < kPairs; e += 2) {
-          total.add_product(kBefore, e, g[e], n[0][e], g[e + 1], n[0][e + 1]);
+          total.add_product(kBefore, e, g[e], n[e], g[e + 1], n[e + 1]);
           if constexpr (kBias) total.add(kBeforeBias, e, g[e], g[e + 1]);
         }
       }
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) g[e] = g[e] * w[e];
-      r.through(g, n[0], a.layer, inv[0], a.inv_dim);
+      r.through(g, n, a.layer, inv, a.inv_dim);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) d[e] = d[e] + g[e];
     }
     r.store((TX*)a.dx + row * a.dx_stride, valid, d);
     if (!a.branch) continue;
     if (a.after) {
-      r.standard(branch, a.layer, a.eps, a.inv_dim, inv);
 #pragma unroll
-      for (int e = 0; e < kPairs; ++e) branch[0][e] = branch[0][e] * both(inv[0]);
+      for (int e = 0; e < kPairs; ++e) branch[e] = branch[e] * both(branch_inv);
     }
 #pragma unroll
     for (int e = 0; e < kPairs; ++e) d[e] = d[e] * both(a.scale);
@@ -442,7 +486,7 @@ norm_grad_kernel(const NormArgs a) {
       Two b[kPairs];
       r.vector(a.after_bias, 0.f, b);
 #pragma unroll
-      for (int e = 0; e < kPairs; ++e) b[e] = fma2(branch[0][e], w[e], b[e]);
+      for (int e = 0; e < kPairs; ++e) b[e] = fma2(branch[e], w[e], b[e]);
       if (a.gate_kind == AGNES_GATE_ROWS) {
         Two gate[kPairs];
         r.load((const TBranch*)a.gate + row * a.gate_stride, valid, gate);
@@ -468,13 +512,13 @@ norm_grad_kernel(const NormArgs a) {
       if (valid) {
 #pragma unroll
         for (int e = 0; e < kPairs; e += 2) {
-          total.add_product(kAfter, e, d[e], branch[0][e], d[e + 1], branch[0][e + 1]);
+          total.add_product(kAfter, e, d[e], branch[e], d[e + 1], branch[e + 1]);
           if constexpr (kBias) total.add(kAfterBias, e, d[e], d[e + 1]);
         }
       }
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) d[e] = d[e] * w[e];
-      r.through(d, branch[0], a.layer, inv[0], a.inv_dim);
+      r.through(d, branch, a.layer, branch_inv, a.inv_dim);
     }
     r.store((TBranch*)a.dbranch + row * a.dbranch_stride, valid, d);
   }
@@ -644,6 +688,14 @@ bool wide_inputs(const NormArgs& a, int64_t x_size, int64_t branch_size) {
       .ok();
 }
 
+// Of rows of up to kShortDim columns, for kernels that know their threads to a row: 8, 16
+// or 32.
+RowShape short_shape(int64_t dim) {
+  RowShape s = row_shape(dim, kShortElems);
+  if (s.lanes < 8) s = {8, 3, kRowThreads / 8};
+  return s;
+}
+
 void set_shape(NormArgs& a, const RowShape& shape) {
   a.lanes = shape.lanes;
   a.log_lanes = shape.log_lanes;
@@ -654,7 +706,7 @@ void set_shape(NormArgs& a, const RowShape& shape) {
 // CTAs of the backward pass: each writes a row of partial sums, so no more than keep the
 // device busy.
 int64_t grad_ctas(int64_t rows, int64_t dim, int sms) {
-  const RowShape shape = row_shape(dim, kShortElems);
+  const RowShape shape = short_shape(dim);
   const int64_t ctas = ceil_div(rows, shape.groups);
   // a thread's sums and the row ahead leave room for 512 threads to an SM
   const int64_t most = (int64_t)sms * (shape.threads() <= 256 ? 2 : 1);
@@ -670,11 +722,14 @@ cudaError_t launch_grad(const NormArgs& a, bool wide, int64_t ctas, size_t smem,
                         cudaStream_t st) {
   using Kernel = void (*)(NormArgs);
   constexpr int kPer = kShortElems;
-  const Kernel long_rows = wide ? norm_grad_kernel<TX, TBranch, 8, 1, 1024, kBias, true>
-                                : norm_grad_kernel<TX, TBranch, 1, kPer, 1024, kBias, true>;
+  const Kernel long_rows = wide ? norm_grad_kernel<TX, TBranch, 8, 1, 1024, kBias, true, 0>
+                                : norm_grad_kernel<TX, TBranch, 1, kPer, 1024, kBias, true, 0>;
   const Kernel kernel = a.lanes > 512 ? long_rows
-                        : wide        ? norm_grad_kernel<TX, TBranch, 8, 1, 512, kBias, false>
-                                      : norm_grad_kernel<TX, TBranch, 1, kPer, 512, kBias, false>;
+                        : !wide ? norm_grad_kernel<TX, TBranch, 1, kPer, 512, kBias, false, 0>
+                        : a.lanes > 32  ? norm_grad_kernel<TX, TBranch, 8, 1, 512, kBias, false, 0>
+                        : a.lanes == 8  ? norm_grad_kernel<TX, TBranch, 8, 1, 256, kBias, false, 8>
+                        : a.lanes == 16 ? norm_grad_kernel<TX, TBranch, 8, 1, 256, kBias, false, 16>
+                                        : norm_grad_kernel<TX, TBranch, 8, 1, 256, kBias, false, 32>;
   if (a.lanes > 512) {
     static OncePerDevice once[2];
     const cudaError_t e = once[wide].run(device, [&] {
@@ -756,10 +811,12 @@ agnes_status agnes_residual_norm(const void* x, int32_t x_dtype, int64_t x_strid
     using TX = typename decltype(tx)::type;
     using TBranch = typename decltype(tb)::type;
     const bool brief = wide && dim <= kShortDim;
-    set_shape(a, row_shape(dim, brief ? kShortElems : kElems, kNormLanes));
-    const auto kernel = brief  ? norm_kernel<TX, TBranch, 8, 1, 2>
-                        : wide ? norm_kernel<TX, TBranch, 8, 2, 1>
-                               : norm_kernel<TX, TBranch, 1, kElems, 1>;
+    set_shape(a, brief ? short_shape(dim) : row_shape(dim, kElems, kNormLanes));
+    const auto kernel = !wide          ? norm_kernel<TX, TBranch, 1, kElems, 1, 0>
+                        : !brief       ? norm_kernel<TX, TBranch, 8, 2, 1, 0>
+                        : a.lanes == 8 ? norm_kernel<TX, TBranch, 8, 1, 2, 8>
+                        : a.lanes == 16 ? norm_kernel<TX, TBranch, 8, 1, 2, 16>
+                                        : norm_kernel<TX, TBranch, 8, 1, 2, 32>;
     kernel<<<(unsigned)ceil_div(rows, a.groups * (brief ? 2 : 1)), (unsigned)(a.lanes * a.groups), 0,
              (cudaStream_t)cuda_stream>>>(a);
     return cudaGetLastError();
@@ -864,7 +921,7 @@ agnes_status agnes_residual_norm_grad(
                       (long long)workspace_bytes, (long long)(ctas * a.sums * dim * 4));
   }
   a.partial = (float*)workspace;
-  set_shape(a, row_shape(dim, kShortElems));
+  set_shape(a, short_shape(dim));
   const int64_t x_size = float_size(x_dtype), branch_size = float_size(branch_dtype);
   const bool wide = wide_inputs(a, x_size, branch_size) &&
                     Wide(a)

@@ -193,22 +193,34 @@ struct MaxBits {  // of magnitudes as bit patterns, which order as the numbers d
 // Shared memory of the reductions: two sets in turn, so that one barrier is enough (the
 // next but one writes where everybody has read).
 struct RowScratch {
-  uint32_t words[2][3][32];
+  uint32_t words[2][4][32];
 };
 
-// v[k] over the threads of each group, for all of them; kN values at once, 3 at most.
-// Every thread of the CTA takes part.  The order of a sum depends on `lanes` alone.
-template <typename Op, int kN>
+// v[k] over the threads of each group, for all of them; kN values at once, 4 at most.
+// Every thread of the CTA takes part.  The order of a sum depends on `lanes` alone; kLanes
+// is that number where it is known, or 0.
+template <typename Op, int kLanes = 0, int kN>
 __device__ __forceinline__ void group_reduce(typename Op::type (&v)[kN], int lanes,
                                              RowScratch* scratch, int& turn) {
-  static_assert(kN <= 3, "RowScratch");
-  const int first = lanes < 32 ? lanes / 2 : 16;
-  for (int d = first; d > 0; d >>= 1) {
+  static_assert(kN <= 4, "RowScratch");
+  using V = typename Op::type;
+  const auto step = [&](int d) {
 #pragma unroll
     for (int k = 0; k < kN; ++k) v[k] = Op::of(v[k], __shfl_xor_sync(0xffffffffu, v[k], d));
+  };
+  if constexpr (kLanes > 0) {
+    static_assert(kLanes <= 32, "within a warp");
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) step(d);
+    return;
   }
-  if (lanes <= 32) return;
-  using V = typename Op::type;
+  if (lanes < 32) {
+    for (int d = lanes / 2; d > 0; d >>= 1) step(d);
+    return;
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) step(d);
+  if (lanes == 32) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = lanes >> 5;
   if (lane == 0) {
 #pragma unroll
@@ -217,15 +229,8 @@ __device__ __forceinline__ void group_reduce(typename Op::type (&v)[kN], int lan
   __syncthreads();
   const int from = warp & ~(warps - 1);
 #pragma unroll
-  for (int k = 0; k < kN; ++k)
-    v[k] = lane < warps ? *(const V*)&scratch->words[turn][k][from + lane] : Op::identity();
-  for (int d = warps / 2; d > 0; d >>= 1) {
-#pragma unroll
-    for (int k = 0; k < kN; ++k) v[k] = Op::of(v[k], __shfl_xor_sync(0xffffffffu, v[k], d));
-  }
-  // lanes past `warps` reduced identities among themselves
-#pragma unroll
-  for (int k = 0; k < kN; ++k) v[k] = __shfl_sync(0xffffffffu, v[k], 0);
+  for (int k = 0; k < kN; ++k) v[k] = *(const V*)&scratch->words[turn][k][from + (lane & (warps - 1))];
+  for (int d = warps / 2; d > 0; d >>= 1) step(d);
   turn ^= 1;
 }
 

@@ -79,14 +79,6 @@ struct WeightBars {
   __device__ uint32_t drained() const { return at(3 * kMaxSlots + 4); }
 };
 
-// Eight values from four pairs of fp32: their upper halves, which are all of them.
-__device__ __forceinline__ uint4 upper8(const float* v) {
-  const auto pair = [&](int i) {
-    return __byte_perm(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), 0x7632);
-  };
-  return make_uint4(pair(0), pair(2), pair(4), pair(6));
-}
-
 __global__ void __launch_bounds__(kThreads, 1)
 weight_kernel(const __grid_constant__ CUtensorMap grad_map,
               const __grid_constant__ CUtensorMap x_map, const WeightArgs a) {
@@ -262,20 +254,24 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
       uint8_t* slot = smem + s * a.slot_bytes;
       const uint8_t* from = slot + raw_off + r * kTile;
       uint8_t* to = slot + value_off + half * kBox + r * 128;
+      const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);  // exact: it has eight bits
+      uint4 w[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        w[c] = *(const uint4*)(from + (((4 * half + c) ^ (r & 7)) << 4));
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const uint4 w = *(const uint4*)(from + (((4 * half + c) ^ (r & 7)) << 4));
-        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+        uint2 hi[4], lo[4];
+        int8_terms4(w[c].x, s2, hi[0], lo[0]);
+        int8_terms4(w[c].y, s2, hi[1], lo[1]);
+        int8_terms4(w[c].z, s2, hi[2], lo[2]);
+        int8_terms4(w[c].w, s2, hi[3], lo[3]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float hi[8], lo[8];
-          int8_values4(word[2 * h], hi);
-          int8_values4(word[2 * h + 1], hi + 4);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) int8_split(hi[e] * scale, hi[e], lo[e]);
           const int at = ((2 * c + h) ^ (r & 7)) << 4;
-          *(uint4*)(to + at) = upper8(hi);
-          *(uint4*)(to + 2 * kBox + at) = upper8(lo);
+          *(uint4*)(to + at) = make_uint4(hi[2 * h].x, hi[2 * h].y, hi[2 * h + 1].x, hi[2 * h + 1].y);
+          *(uint4*)(to + 2 * kBox + at) =
+              make_uint4(lo[2 * h].x, lo[2 * h].y, lo[2 * h + 1].x, lo[2 * h + 1].y);
         }
       }
       fence_async_proxy();

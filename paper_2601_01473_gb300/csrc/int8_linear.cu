@@ -170,9 +170,13 @@ constexpr int kOperandBytes = kTileM * 128;  // of one term of A
 constexpr int kRawBytes = kTileM * kSliceK;
 constexpr int kMaxSlots = 8;
 constexpr int kOutBytes = 32 * 128;  // an epilogue warp's output on its way to memory
+constexpr int kColumnBytes = kEpilogueWarps * 2 * 128 * 4;  // the epilogue warps' scales and biases
 constexpr int kTileBars = 3 * kMaxSlots + 6;
 constexpr int kSmemLimit = 232448;
-constexpr int kTileSmem = kSmemLimit - 1024 - 8 * kTileBars - 16;  // for the buffers
+// Shared memory beside those (of kConvert alone) and the mbarriers.
+constexpr int tile_smem(bool convert) {
+  return kSmemLimit - 1024 - (convert ? kColumnBytes : 0) - 8 * kTileBars - 16;
+}
 
 struct TileArgs {
   int64_t rows, cols;  // of the output
@@ -229,27 +233,24 @@ struct TileBars {
   __device__ uint32_t drained() const { return at(3 * kMaxSlots + 5); }
 };
 
-// 32 values from c0 on of a vector over the columns; `fill` past its end or where there is
-// none.
-__device__ __forceinline__ void load_columns(const float* p, int64_t c0, int64_t cols, float fill,
-                                             float (&b)[32]) {
-  if (!p) {
+// A warp's columns of a vector, kHalf / 32 to a lane, from c0 on; zeros past its end or where
+// there is none.
+template <int kHalf>
+struct Columns {
+  float v[kHalf / 32];
+  __device__ void load(const float* p, int64_t c0, int64_t cols, bool any) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) b[e] = fill;
-  } else if (c0 + 32 <= cols && (uintptr_t)p % 16 == 0) {
-#pragma unroll
-    for (int e = 0; e < 32; e += 4) {
-      const float4 v = __ldg((const float4*)(p + c0 + e));
-      b[e] = v.x;
-      b[e + 1] = v.y;
-      b[e + 2] = v.z;
-      b[e + 3] = v.w;
+    for (int i = 0; i < kHalf / 32; ++i) {
+      const int64_t c = c0 + i * 32 + lane;
+      v[i] = p && any && c < cols ? __ldg(p + c) : 0.f;
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) b[e] = c0 + e < cols ? __ldg(p + c0 + e) : fill;
   }
-}
+  __device__ void put(float* to) const {
+#pragma unroll
+    for (int i = 0; i < kHalf / 32; ++i) to[i * 32 + (threadIdx.x & 31)] = v[i];
+  }
+};
 
 // 32 columns of a lane's row into its warp's buffer, from byte `first` of its 128 on, in
 // 16-byte pieces permuted as the TMA's 128-byte swizzle has them.
@@ -319,7 +320,8 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
   uint8_t* resident_b = smem + a.slots * a.slot_bytes;
   uint8_t* out_stage =
       resident_b + (a.resident ? a.steps * a.tb * (int)kBBytes : 0);
-  uint64_t* bars = (uint64_t*)(out_stage + kEpilogueWarps * a.out_buffers * kOutBytes);
+  float* column_stage = (float*)(out_stage + kEpilogueWarps * a.out_buffers * kOutBytes);
+  uint64_t* bars = (uint64_t*)((uint8_t*)column_stage + (kConvert ? kColumnBytes : 0));
   uint32_t* tmem_slot = (uint32_t*)(bars + kTileBars);
   const TileBars bar = {smem_addr(bars)};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -488,11 +490,30 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
                  ? __ldg((const float*)(a.x + row * a.x_stride + a.row_bytes - 4)) : 1.f;
     };
     float next_scale = scale_of(t);
+    // the columns' scales and biases, too, on their way to shared memory
+    float* my_scales = column_stage + warp * 256;
+    float* my_biases = my_scales + 128;
+    Columns<kHalf> next_scales, next_biases;
+    const auto columns_of = [&](const TileWalk& at) {
+      if constexpr (kConvert) {
+        const int64_t c0 = at.n * kCols + (warp >> 2) * kHalf;
+        next_scales.load(a.col_scale, c0, a.cols, at.any());
+        next_biases.load(a.bias, c0, a.cols, at.any());
+      }
+    };
+    columns_of(t);
     for (; ok && t.any(); t.next()) {
       const float scale = next_scale;
+      if constexpr (kConvert) {
+        __syncwarp();
+        next_scales.put(my_scales);
+        next_biases.put(my_biases);
+        __syncwarp();
+      }
       TileWalk after = t;
       after.next();
       next_scale = scale_of(after);
+      columns_of(after);
       const int64_t row0 = t.m * kTileM + (warp & 3) * 32;
       const int64_t n0 = t.n * kCols + (warp >> 2) * kHalf;
       // a warp whose rows are all past the end has nothing to store, and its buffers may
@@ -500,9 +521,13 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
       const int cols = row0 < a.rows ? kHalf : 0;
       const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
                                 (uint32_t)((warp >> 2) * kHalf);
-      // neither a sum (up to 2^31) times such a scale nor that times a column's overflows
-      // unless the whole does
-      const bool plain = __all_sync(0xffffffffu, !(scale > 0x1p90f) && !(scale < 0x1p-90f));
+      // A sum (up to 2^31) times a row's scale between 2^-90 and 2^90 does not leave fp32 unless
+      // the whole product does.  Another scale is taken in two, its power of two last: that
+      // costs a product more for each value, where a branch between the two took 18 us more of
+      // 786,432 x 128 to 256 and a choice for each value 45.
+      const float far = scale > 0x1p90f ? 0x1p60f : scale < 0x1p-90f ? 0x1p-60f : 1.f;
+      const float near = scale > 0x1p90f ? scale * 0x1p-60f : scale < 0x1p-90f ? scale * 0x1p60f
+                                                                               : scale;
       float total[kDrain ? kHalf : 1];
       if constexpr (kDrain) {
 #pragma unroll
@@ -532,7 +557,7 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
         acc.next(2);
       }
       if (!ok) break;
-#pragma unroll
+#pragma unroll(kDrain ? kHalf / kGroup : 1)
       for (int c = 0; c < kHalf; c += kGroup) {
         if (c >= cols || n0 + c >= a.cols) break;
         // an earlier store has read the buffer
@@ -557,15 +582,15 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
             for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(v[e]);
           }
           if constexpr (kConvert) {
-            float w[32], b[32];
-            load_columns(a.col_scale, n0 + c + h, a.cols, 0.f, w);
-            load_columns(a.bias, n0 + c + h, a.cols, 0.f, b);
-            if (plain) {
+const float4* w4 = (const float4*)(my_scales + c + h);
+            const float4* b4 = (const float4*)(my_biases + c + h);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) y[e] = fmaf(y[e] * scale, w[e], b[e]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) y[e] = scaled(y[e], scale, w[e]) + b[e];
+            for (int q = 0; q < 8; ++q) {
+              const float4 w = w4[q], b = b4[q];
+              y[4 * q] = fmaf(y[4 * q] * near * w.x, far, b.x);
+              y[4 * q + 1] = fmaf(y[4 * q + 1] * near * w.y, far, b.y);
+              y[4 * q + 2] = fmaf(y[4 * q + 2] * near * w.z, far, b.z);
+              y[4 * q + 3] = fmaf(y[4 * q + 3] * near * w.w, far, b.w);
             }
           }
           stage_values<TOut>(to, lane, h * (int)sizeof(TOut), y);
@@ -647,16 +672,16 @@ cudaError_t launch_tiles(TileArgs a, const TileOperands& o, int device, cudaStre
   const int b_slice = a.tb * kCols * 128;
   const int a_slice = a.ta * kOperandBytes + (kConvert ? kRawBytes : 0);
   a.resident = tiles_n <= num_sms &&
-               (int64_t)a.steps * b_slice + 3 * a_slice + kEpilogueWarps * kOutBytes <= kTileSmem;
+               (int64_t)a.steps * b_slice + 3 * a_slice + kEpilogueWarps * kOutBytes <= tile_smem(kConvert);
   a.slot_bytes = a_slice + (a.resident ? 0 : b_slice);
   const int fixed = a.resident ? a.steps * b_slice : 0;
   const auto slots_with = [&](int buffers) {
-    return (kTileSmem - fixed - kEpilogueWarps * buffers * kOutBytes) / a.slot_bytes;
+    return (tile_smem(kConvert) - fixed - kEpilogueWarps * buffers * kOutBytes) / a.slot_bytes;
   };
   a.out_buffers = slots_with(2) >= 4 ? 2 : 1;
   const int slots = slots_with(a.out_buffers);
   a.slots = slots < kMaxSlots ? slots : kMaxSlots;
-  const size_t smem = (size_t)kSmemLimit - kTileSmem + (size_t)a.slots * a.slot_bytes + fixed +
+  const size_t smem = (size_t)kSmemLimit - tile_smem(kConvert) + (size_t)a.slots * a.slot_bytes + fixed +
                       (size_t)kEpilogueWarps * a.out_buffers * kOutBytes;
   int64_t grid = num_sms;
   if (a.resident) grid = num_sms / tiles_n * tiles_n;  // a CTA's columns stay the same
@@ -737,24 +762,38 @@ cudaError_t launch_linear(const LinearArgs& l, void* workspace, int32_t* status,
   return launch_product<TOut, true>(a, o, drain, device, st);
 }
 
-// One value of a row to a lane and turn; see split_grad.
-template <typename T>
+// Eight values of a row to a thread; see split_grad.  kWide: rows that are 16-byte aligned and
+// whole eights.
+template <typename T, bool kWide>
 __global__ void __launch_bounds__(kPrepThreads)
 split_kernel(const T* __restrict__ x, int64_t stride, int64_t rows, int64_t width,
-             __nv_bfloat16* __restrict__ out, int64_t wpad) {
-  const int64_t step = (int64_t)gridDim.x * kPrepThreads, total = rows * width;
-  for (int64_t i = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; i < total; i += step) {
-    const int64_t r = i / width, c = i - r * width;
-    const float v = to_f32(x[r * stride + c]);
-    float hi, mid, lo;
-    int8_split(v, hi, mid);
-    __nv_bfloat16* to = out + r * wpad + c;
-    to[0] = __float2bfloat16_rn(hi);
-    if constexpr (sizeof(T) == 4) {
-      int8_split(mid, mid, lo);
-      to[2 * rows * wpad] = __float2bfloat16_rn(lo);
+             int32_t groups, uint32_t inv_groups, __nv_bfloat16* __restrict__ out, int64_t wpad) {
+  const FlatRows flat(blockIdx.x, groups, inv_groups);
+#pragma unroll
+  for (int u = 0; u < kFlat / kPrepThreads; ++u) {
+    int64_t row;
+    uint32_t g;
+    flat.at(threadIdx.x + u * kPrepThreads, &row, &g);
+    if (row >= rows) continue;
+    const T* from = x + row * stride + g * 8;
+    float v[8], rest[8];
+    if constexpr (kWide) {
+      load_vec<T, 8>(from, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (int64_t)g * 8 + e < width ? to_f32(from[e]) : 0.f;
     }
-    if constexpr (!std::is_same<T, __nv_bfloat16>::value) to[rows * wpad] = __float2bfloat16_rn(mid);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) int8_split(v[e], v[e], rest[e]);
+    __nv_bfloat16* to = out + row * wpad + g * 8;
+    store_vec<__nv_bfloat16, 8>(to, v);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) continue;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) int8_split(rest[e], rest[e], v[e]);
+      store_vec<__nv_bfloat16, 8>(to + 2 * rows * wpad, v);
+    }
+    store_vec<__nv_bfloat16, 8>(to + rows * wpad, rest);
   }
 }
 
@@ -764,9 +803,11 @@ cudaError_t split_grad(const void* grad, int32_t dtype, int64_t stride, int64_t 
                        int64_t width, __nv_bfloat16* out, int64_t wpad, cudaStream_t st) {
   return with_float_type(dtype, [&](auto t) {
     using T = typename decltype(t)::type;
-    const int64_t ctas = ceil_div(rows * width, 4 * kPrepThreads);
-    split_kernel<T><<<(unsigned)(ctas < 65536 ? ctas : 65536), kPrepThreads, 0, st>>>(
-        (const T*)grad, stride, rows, width, out, wpad);
+    const int64_t groups = wpad / 8;
+    const bool wide = width % 8 == 0 && aligned_rows(grad, stride * (int64_t)sizeof(T), 16);
+    (wide ? split_kernel<T, true> : split_kernel<T, false>)
+        <<<(unsigned)ceil_div(rows * groups, kFlat), kPrepThreads, 0, st>>>(
+            (const T*)grad, stride, rows, width, (int32_t)groups, flat_inverse(groups), out, wpad);
     return cudaGetLastError();
   });
 }

@@ -17,6 +17,28 @@ __device__ __forceinline__ void int8_split(float v, float& hi, float& lo) {
   lo = fabsf(hi) <= 3.4e38f ? v - hi : 0.f;
 }
 
+// Four whole numbers times a scale (a bfloat16 value, twice in `scale`) as pairs of bfloat16
+// terms: hi the rounded products, lo what they leave, exactly.  A byte is its lower seven
+// bits less 128 times its sign, and 128 + seven bits, 128 and 256 are bfloat16 bit patterns
+// of the byte's parts.
+__device__ __forceinline__ void int8_terms4(uint32_t word, __nv_bfloat162 scale, uint2& hi,
+                                            uint2& lo) {
+  const uint32_t size = word & 0x7f7f7f7fu, sign = word & 0x80808080u;
+  uint32_t* h = &hi.x;
+  uint32_t* l = &lo.x;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t pick = i ? 0x4342 : 0x4140;
+    const uint32_t a = __byte_perm(size, 0x43434343u, pick);
+    const uint32_t b = __byte_perm(sign, 0x43434343u, pick);
+    const __nv_bfloat162 q = __hsub2(*(const __nv_bfloat162*)&a, *(const __nv_bfloat162*)&b);
+    const __nv_bfloat162 top = __hmul2(q, scale);
+    const __nv_bfloat162 rest = __hfma2(q, scale, __hneg2(top));
+    h[i] = *(const uint32_t*)&top;
+    l[i] = *(const uint32_t*)&rest;
+  }
+}
+
 // How many such terms a gradient's type takes: all of its bits.
 inline int grad_terms(int32_t dtype) {
   return dtype == AGNES_F32 ? 3 : dtype == AGNES_F16 ? 2 : 1;

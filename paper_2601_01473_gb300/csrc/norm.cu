@@ -16,6 +16,8 @@
 // means leave.  For the sums over rows a thread keeps to its columns while its group goes
 // from row to row, each CTA writes one partial row, and a second kernel adds those up in
 // order: the result is the same each time.
+#include <algorithm>
+
 #include "int8.cuh"
 
 namespace agnes {
@@ -50,6 +52,7 @@ struct NormArgs {
   int64_t d_next_stride, d_sum_stride;
   void *dx, *dbranch, *dgate;
   int64_t dx_stride, dbranch_stride, dgate_stride;
+  int32_t stages, stage_off;  // of the copies ahead, and where they lie, in 16 bytes
   float* partial;      // [CTAs][sums][dim]
   int32_t slot[kSums];  // a sum's place among them, or -1
   int32_t sums;
@@ -400,29 +403,147 @@ struct Totals {
   }
 };
 
+// The vectors over the columns of the backward pass, in shared memory where there is room
+// beside the sums: a thread's of one vector are kElems / 4 quads, quad q of all threads to a
+// row side by side, zeros past the row's end.  What there is none of is ones, or zeros for
+// the bias.
+enum { kBeforeVector, kAfterVector, kAfterBiasVector, kGateVector, kVectors };
+template <int kVec, int kPer, int kLanes>
+struct ColumnVectors {
+  using Row = NormRow<kVec, kPer, kLanes>;
+  static constexpr int kQuads = kVec * kPer / 4;
+  float4* at;
+  __device__ void init(const NormArgs& a, const Row& r, float4* shared) {
+    at = shared;
+    if ((int)threadIdx.x >= a.lanes) return;  // one group's threads fill them
+    const float* const from[kVectors] = {
+        a.before, a.after, a.after_bias,
+        a.gate_kind == AGNES_GATE_COLUMNS ? (const float*)a.gate : nullptr};
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k) {
+      Two v[Row::kPairs];
+      r.vector(from[k], k == kAfterBiasVector ? 0.f : 1.f, v);
+#pragma unroll
+      for (int q = 0; q < kQuads; ++q) {
+        const float2 x = apart(v[2 * q]), y = apart(v[2 * q + 1]);
+        at[(k * kQuads + q) * a.lanes + r.part.lane] = make_float4(x.x, x.y, y.x, y.y);
+      }
+    }
+  }
+  __device__ void get(const Row& r, int k, typename Row::Values& v) const {
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+      const float4 x = at[(k * kQuads + q) * r.part.lanes + r.part.lane];
+      v[2 * q] = two(x.x, x.y);
+      v[2 * q + 1] = two(x.z, x.w);
+    }
+  }
+};
+
 // Which sums there are, so that the others take no registers: of before, after and gate, or
 // of the biases too.
 enum { kBefore, kAfter, kGateSum, kBeforeBias, kAfterBias, kMostSums };
 
-// A row ahead: what a row needs is on its way while the one before it is worked on.
-template <typename TX, typename TBranch, int kVec, int kPer>
-struct GradRegs {
-  RowRegs<TX, kVec, kPer> x, d_sum;
-  RowRegs<TBranch, kVec, kPer> d_next, branch;
-  __device__ void load(const RowPart<kVec, kPer>& part, const NormArgs& a, int64_t row) {
-    const bool valid = row < a.rows;
-    if (a.d_sum) d_sum.load(part, (const TX*)a.d_sum + row * a.d_sum_stride, valid);
-    if (a.before) {
-      x.load(part, (const TX*)a.x + row * a.x_stride, valid);
-      d_next.load(part, (const TBranch*)a.d_next + row * a.d_next_stride, valid);
+// What a row of the backward pass needs.  kAsync: it is on its way for some rows ahead, copied
+// to slots of shared memory that only the thread itself reads, of which there are `stages`.
+// Otherwise it is loaded when its row is due.
+template <typename TX, typename TBranch, int kVec, int kPer, bool kAsync, int kLanes>
+struct GradRow {
+  using Row = NormRow<kVec, kPer, kLanes>;
+  static constexpr int kX = sizeof(TX) / 2, kB = sizeof(TBranch) / 2;  // 16-byte pieces
+  enum { kPieces = 2 * (kX + kB) };
+  const NormArgs& a;
+  const RowPart<kVec, kPer>& part;
+  uint4* slots;  // this thread's: piece p of stage s at (s * kPieces + p) * blockDim.x
+  int stages;
+
+  template <typename T>
+  __device__ void copy(const void* from, int64_t row, int64_t stride, int slot, int piece) const {
+    constexpr int kBytes = kVec * sizeof(T), kAccess = kBytes < 16 ? kBytes : 16;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const bool there = from && row < a.rows && part.has(i);
+      const uint8_t* at = there ? (const uint8_t*)((const T*)from + row * stride + part.col(i))
+                                : (const uint8_t*)a.x;
+      const uint32_t bytes = there ? kAccess : 0;  // the others are zeros
+#pragma unroll
+      for (int h = 0; h < kBytes; h += kAccess) {
+        const int byte = i * kBytes + h;
+        const uint32_t to =
+            (uint32_t)__cvta_generic_to_shared(
+                slots + (slot * kPieces + piece + byte / 16) * (int)blockDim.x) + byte % 16;
+        if constexpr (kAccess == 16)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to),
+                       "l"(at + (there ? h : 0)), "r"(bytes)
+                       : "memory");
+        else
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to),
+                       "l"(at), "r"(bytes)
+                       : "memory");
+      }
     }
-    if (a.branch) branch.load(part, (const TBranch*)a.branch + row * a.branch_stride, valid);
+  }
+  // Starts a row's copies; one group each, of rows past the end too, so that the wait's count
+  // holds.
+  __device__ void start(int64_t row, int slot) const {
+    if constexpr (kAsync) {
+      if (row < a.rows) {
+        copy<TX>(a.before ? a.x : nullptr, row, a.x_stride, slot, 0);
+        copy<TX>(a.d_sum, row, a.d_sum_stride, slot, kX);
+        copy<TBranch>(a.before ? a.d_next : nullptr, row, a.d_next_stride, slot, 2 * kX);
+        copy<TBranch>(a.branch, row, a.branch_stride, slot, 2 * kX + kB);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  }
+  __device__ void wait() const {
+    if constexpr (kAsync) {
+      if (stages == 4)
+        asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else if (stages == 3)
+        asm volatile("cp.async.wait_group 2;" ::: "memory");
+      else  // there are two at least
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+    }
+  }
+  template <typename T>
+  __device__ void get(const void* from, int64_t row, int64_t stride, int slot, int piece,
+                      typename Row::Values& v) const {
+    if constexpr (kAsync) {
+      RowRegs<T, kVec, kPer> r;
+      uint32_t* words = &r.w[0][0];
+#pragma unroll
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        const uint4 q = slots[(slot * kPieces + piece + h) * (int)blockDim.x];
+        words[4 * h] = q.x;
+        words[4 * h + 1] = q.y;
+        words[4 * h + 2] = q.z;
+        words[4 * h + 3] = q.w;
+      }
+      Row::unpack(r, v);
+    } else {
+      RowRegs<T, kVec, kPer> r;
+      r.load(part, (const T*)from + row * stride, row < a.rows);
+      Row::unpack(r, v);
+    }
+  }
+  __device__ void x(int64_t row, int slot, typename Row::Values& v) const {
+    get<TX>(a.x, row, a.x_stride, slot, 0, v);
+  }
+  __device__ void d_sum(int64_t row, int slot, typename Row::Values& v) const {
+    get<TX>(a.d_sum, row, a.d_sum_stride, slot, kX, v);
+  }
+  __device__ void d_next(int64_t row, int slot, typename Row::Values& v) const {
+    get<TBranch>(a.d_next, row, a.d_next_stride, slot, 2 * kX, v);
+  }
+  __device__ void branch(int64_t row, int slot, typename Row::Values& v) const {
+    get<TBranch>(a.branch, row, a.branch_stride, slot, 2 * kX + kB, v);
   }
 };
 
 template <typename TX, typename TBranch, int kVec, int kPer, int kThreads, bool kBias, bool kShared,
           int kLanes>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 2 : 1)
 norm_grad_kernel(const NormArgs a) {
   using Row = NormRow<kVec, kPer, kLanes>;
   constexpr int kPairs = Row::kPairs;
@@ -433,30 +554,47 @@ norm_grad_kernel(const NormArgs a) {
   Row r = {{a.lanes, lane, a.dim}, &scratch};
   Totals<kPairs, kCount, kShared> total;
   total.init(grad_smem);
+  ColumnVectors<kVec, kPer, kLanes> columns;
+  if constexpr (!kShared) {
+    columns.init(a, r, grad_smem);
+    __syncthreads();
+  }
+  const auto vector = [&](int k, const float* p, float fill, Two (&v)[kPairs]) {
+    if constexpr (kShared)
+      r.vector(p, fill, v);
+    else
+      columns.get(r, k, v);
+  };
   const int64_t step = (int64_t)gridDim.x * a.groups;
-  GradRegs<TX, TBranch, kVec, kPer> ahead;
-  ahead.load(r.part, a, (int64_t)blockIdx.x * a.groups + group);
+  GradRow<TX, TBranch, kVec, kPer, kVec != 1 && !kShared, kLanes> in = {a, r.part, (uint4*)(grad_smem + a.stage_off) + threadIdx.x,
+                                         a.stages};
+  for (int k = 0; k + 1 < a.stages; ++k)
+    in.start((int64_t)blockIdx.x * a.groups + group + k * step, k);
+  int slot = 0, fill = a.stages - 1;
   for (int64_t first = (int64_t)blockIdx.x * a.groups; first < a.rows; first += step) {
     const int64_t row = first + group;
     const bool valid = row < a.rows;
     Two d[kPairs], w[kPairs], n[kPairs], branch[kPairs];
     float inv, branch_inv;
+    in.start(row + (a.stages - 1) * step, fill);
+    in.wait();
     if (a.d_sum) {
-      Row::unpack(ahead.d_sum, d);
+      in.d_sum(row, slot, d);
     } else {
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) d[e] = both(0.f);
     }
     Two g[kPairs];
     if (a.before) {
-      Row::unpack(ahead.x, n);
-      Row::unpack(ahead.d_next, g);
+      in.x(row, slot, n);
+      in.d_next(row, slot, g);
     }
-    if (a.branch) Row::unpack(ahead.branch, branch);
-    ahead.load(r.part, a, row + step);
+    if (a.branch) in.branch(row, slot, branch);
+    if (++slot == a.stages) slot = 0;
+    if (++fill == a.stages) fill = 0;
     r.standard_of(n, a.before, branch, a.after, a.layer, a.eps, a.inv_dim, inv, branch_inv);
     if (a.before) {
-      r.vector(a.before, 1.f, w);
+      vector(kBeforeVector, a.before, 1.f, w);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) n[e] = n[e] * both(inv);
       if (valid) {  // where there is no row and eps is 0, n is no number
@@ -482,9 +620,9 @@ norm_grad_kernel(const NormArgs a) {
     for (int e = 0; e < kPairs; ++e) d[e] = d[e] * both(a.scale);
     if (a.gate_kind != AGNES_GATE_NONE) {
       // u, then d u
-      r.vector(a.after, 1.f, w);
+      vector(kAfterVector, a.after, 1.f, w);
       Two b[kPairs];
-      r.vector(a.after_bias, 0.f, b);
+      vector(kAfterBiasVector, a.after_bias, 0.f, b);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) b[e] = fma2(branch[e], w[e], b[e]);
       if (a.gate_kind == AGNES_GATE_ROWS) {
@@ -502,13 +640,13 @@ norm_grad_kernel(const NormArgs a) {
           for (int e = 0; e < kPairs; e += 2)
             total.add_product(kGateSum, e, d[e], b[e], d[e + 1], b[e + 1]);
         }
-        r.vector((const float*)a.gate, 1.f, b);
+        vector(kGateVector, (const float*)a.gate, 1.f, b);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) d[e] = d[e] * b[e];
       }
     }
     if (a.after) {
-      r.vector(a.after, 1.f, w);
+      vector(kAfterVector, a.after, 1.f, w);
       if (valid) {
 #pragma unroll
         for (int e = 0; e < kPairs; e += 2) {
@@ -557,9 +695,9 @@ struct JoinArgs {
   float* out[kSums];  // by place
 };
 
-// A warp to 32 columns of a sum would wait for `parts` loads in a row: eight threads share
-// a column's parts, and add theirs up in order.
-constexpr int kJoinShares = 8;
+// A warp to 32 columns of a sum would wait for `parts` loads in a row: 32 threads share a
+// column's parts, and their sums are added up in order.
+constexpr int kJoinShares = 32;
 __global__ void __launch_bounds__(32 * kJoinShares)
 norm_join_kernel(const JoinArgs a) {
   grid_dep_wait();
@@ -568,6 +706,7 @@ norm_join_kernel(const JoinArgs a) {
   const int c = blockIdx.x * 32 + lane, k = blockIdx.y;
   float sum = 0.f;
   if (c < a.dim)
+#pragma unroll 4
     for (int p = share; p < a.parts; p += kJoinShares)
       sum += a.partial[((int64_t)p * a.sums + k) * a.dim + c];
   part_sum[share][lane] = sum;
@@ -718,26 +857,39 @@ constexpr int kMostSms = 256;  // for the size of a workspace, whatever device i
 size_t dim_smem(const NormArgs& a) { return (size_t)a.lanes * kShortElems * 4; }
 
 template <typename TX, typename TBranch, bool kBias>
-cudaError_t launch_grad(const NormArgs& a, bool wide, int64_t ctas, size_t smem, int device,
+cudaError_t launch_grad(NormArgs a, bool wide, int64_t ctas, size_t smem, int device,
                         cudaStream_t st) {
   using Kernel = void (*)(NormArgs);
   constexpr int kPer = kShortElems;
-  const Kernel long_rows = wide ? norm_grad_kernel<TX, TBranch, 8, 1, 1024, kBias, true, 0>
-                                : norm_grad_kernel<TX, TBranch, 1, kPer, 1024, kBias, true, 0>;
-  const Kernel kernel = a.lanes > 512 ? long_rows
-                        : !wide ? norm_grad_kernel<TX, TBranch, 1, kPer, 512, kBias, false, 0>
-                        : a.lanes > 32  ? norm_grad_kernel<TX, TBranch, 8, 1, 512, kBias, false, 0>
-                        : a.lanes == 8  ? norm_grad_kernel<TX, TBranch, 8, 1, 256, kBias, false, 8>
-                        : a.lanes == 16 ? norm_grad_kernel<TX, TBranch, 8, 1, 256, kBias, false, 16>
-                                        : norm_grad_kernel<TX, TBranch, 8, 1, 256, kBias, false, 32>;
-  if (a.lanes > 512) {
-    static OncePerDevice once[2];
-    const cudaError_t e = once[wide].run(device, [&] {
-      return cudaFuncSetAttribute(long_rows, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  kSums * kRowLanesMax * kShortElems * 4);
-    });
-    if (e != cudaSuccess) return e;
+  // With a residual in fp32 a thread has two vectors of four columns, so that each access of
+  // a warp is one run of memory (eight columns to a thread: 346 us of 16,384 x 4096, past L1,
+  // 328 through it).
+  constexpr int kV = sizeof(TX) == 4 ? 4 : 8, kP = kShortElems / kV;
+  const Kernel kernels[7] = {norm_grad_kernel<TX, TBranch, kV, kP, 1024, kBias, true, 0>,
+                             norm_grad_kernel<TX, TBranch, 1, kPer, 1024, kBias, true, 0>,
+                             norm_grad_kernel<TX, TBranch, 1, kPer, 512, kBias, false, 0>,
+                             norm_grad_kernel<TX, TBranch, kV, kP, 512, kBias, false, 0>,
+                             norm_grad_kernel<TX, TBranch, kV, kP, 256, kBias, false, 8>,
+                             norm_grad_kernel<TX, TBranch, kV, kP, 256, kBias, false, 16>,
+                             norm_grad_kernel<TX, TBranch, kV, kP, 256, kBias, false, 32>};
+  const int which = a.lanes > 512 ? (wide ? 0 : 1) : !wide ? 2 : a.lanes > 32 ? 3
+                    : a.lanes == 8 ? 4 : a.lanes == 16 ? 5 : 6;
+  const Kernel kernel = kernels[which];
+  // as many rows ahead as there is room for in the 227 KB of an SM's CTAs
+  a.stages = 1;
+  a.stage_off = (int32_t)ceil_div((int64_t)smem, 16);
+  if (which >= 3) {
+    const int threads = a.lanes * a.groups;
+    const size_t stage = (size_t)GradRow<TX, TBranch, kV, kP, true, 0>::kPieces * 16 * threads;
+    const size_t room = (threads <= 256 ? 110 : 224) * 1024 - (size_t)a.stage_off * 16;
+    a.stages = (int32_t)std::min((size_t)4, room / stage);
+    smem = (size_t)a.stage_off * 16 + a.stages * stage;
   }
+  static OncePerDevice once[7];
+  const cudaError_t e = once[which].run(device, [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
+  });
+  if (e != cudaSuccess) return e;
   kernel<<<(unsigned)ctas, (unsigned)(a.lanes * a.groups), smem, st>>>(a);
   return cudaGetLastError();
 }
@@ -933,9 +1085,10 @@ agnes_status agnes_residual_norm_grad(
                               branch_size)
                         .ok();
   const bool biases = dbefore_bias || dafter_bias, shared = a.lanes > 512;
-  const size_t smem = shared          ? (size_t)(biases ? kSums : kBeforeBias) * dim_smem(a)
-                      : a.groups > 1 ? (size_t)a.groups * dim * 4
-                                      : 0;
+  // the sums; or the vectors, and in their place a group's share of a sum at the end
+  const size_t smem = shared ? (size_t)(biases ? kSums : kBeforeBias) * dim_smem(a)
+                             : std::max((size_t)kVectors * dim_smem(a),
+                                        a.groups > 1 ? (size_t)a.groups * dim * 4 : 0);
   const cudaError_t e = with_norm_types(x_dtype, branch_dtype, [&](auto tx, auto tb) {
     using TX = typename decltype(tx)::type;
     using TBranch = typename decltype(tb)::type;

@@ -101,17 +101,16 @@ struct RowRegs {
   uint32_t w[kPer][kWords];
 
   __device__ void load(const RowPart<kVec, kPer>& part, const T* row, bool valid) {
-    constexpr int kQuads = kWords / 4;
+    constexpr int kPiece = kWords < 4 ? kWords : 4;  // words to an access
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
 #pragma unroll
-      for (int h = 0; h < kQuads; ++h) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (valid && part.has(i)) v = ((const uint4*)(row + part.col(i)))[h];
-        w[i][4 * h] = v.x;
-        w[i][4 * h + 1] = v.y;
-        w[i][4 * h + 2] = v.z;
-        w[i][4 * h + 3] = v.w;
+      for (int h = 0; h < kWords; h += kPiece) {
+        Vec<uint32_t, kPiece> v = {};
+        if (valid && part.has(i))
+          v = ((const Vec<uint32_t, kPiece>*)(row + part.col(i)))[h / kPiece];
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) w[i][h + e] = v.v[e];
       }
     }
   }

@@ -224,7 +224,6 @@ agnes_status agnes_int8_dequantize(const void* x, int64_t stride, int64_t rows, 
  *  status AGNES_OP_TIMEOUT where a wait inside the kernel ran out.
  * 0 <= rows, 0 <= width < 2^29 (here and in the gradients).
  * Errors: EINVAL, ERANGE, ECUDA. */
-#define AGNES_INT8_FEW_ROWS 8
 agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, const void* w,
                                int64_t w_stride, int64_t width, int64_t dim, const float* bias,
                                void* out, int32_t out_dtype, int64_t out_stride, void* workspace,

@@ -322,7 +322,8 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
 }
 
 // The shares' tiles added up: 32 rows x 16 columns of a tile to a CTA, their shares dealt
-// out to kJoinShares threads each, whose sums are added in order.
+// out to kJoinShares threads each, whose sums are added in order.  The CTAs behind the
+// tiles' have the bias.
 constexpr int kJoinShares = 4;
 constexpr int kJoinQuads = 4;  // groups of four columns
 template <typename TOut>
@@ -330,6 +331,15 @@ __global__ void __launch_bounds__(32 * kJoinQuads * kJoinShares)
 join_kernel(const WeightArgs a) {
   grid_dep_wait();
   __shared__ float4 sums[kJoinShares][kJoinQuads][32];
+  if (blockIdx.x >= a.tiles_j * a.tiles_i * 32) {
+    const int64_t j = (int64_t)(blockIdx.x - a.tiles_j * a.tiles_i * 32) * blockDim.x + threadIdx.x;
+    if (j >= a.width) return;
+    float sum = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s) sum += a.bias_partial[(int64_t)s * a.width + j];
+    a.dbias[j] = sum;
+    return;
+  }
   const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) % kJoinQuads;
   const int share = (threadIdx.x >> 5) / kJoinQuads;
   const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
@@ -357,16 +367,6 @@ join_kernel(const WeightArgs a) {
     for (int s = 0; s < kJoinShares; ++s) sum += ((const float*)&sums[s][t % 16 / 4][t / 16])[t % 4];
     ((TOut*)a.out)[j * a.out_stride + i] = from_f32<TOut>(sum);
   }
-}
-
-__global__ void __launch_bounds__(256) bias_join_kernel(const WeightArgs a) {
-  grid_dep_wait();
-  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (j >= a.width) return;
-  float sum = 0.f;
-#pragma unroll 8
-  for (int s = 0; s < a.splits; ++s) sum += a.bias_partial[(int64_t)s * a.width + j];
-  a.dbias[j] = sum;
 }
 
 // How the rows are shared out, and the workspace: partial tiles, partial biases, and the
@@ -433,10 +433,10 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, i
   e = launch_next(weight_kernel, dim3((unsigned)(tiles * a.splits)), (unsigned)kThreads, smem, st,
                   grad_map, x_map, a);
   if (e != cudaSuccess) return e;
-  e = launch_next(join_kernel<TOut>, dim3((unsigned)(tiles * 32)),
-                  32 * kJoinQuads * kJoinShares, 0, st, a);
-  if (e != cudaSuccess || !a.dbias) return e;
-  return launch_next(bias_join_kernel, dim3((unsigned)ceil_div(a.width, 256)), 256, 0, st, a);
+  constexpr int kJoinThreads = 32 * kJoinQuads * kJoinShares;
+  return launch_next(join_kernel<TOut>,
+                     dim3((unsigned)(tiles * 32 + (a.dbias ? ceil_div(a.width, kJoinThreads) : 0))),
+                     (unsigned)kJoinThreads, 0, st, a);
 }
 
 }  // namespace

@@ -19,6 +19,7 @@ namespace {
 
 // ---- few rows ------------------------------------------------------------------
 
+constexpr int kFewRows = 32;
 constexpr int kFewThreads = 256;
 constexpr int kFewCols = 2;  // of the output to a group of lanes at a time
 
@@ -127,13 +128,23 @@ expand_kernel(const uint8_t* __restrict__ q, int64_t stride, int64_t rows, int32
 // The weights' values, transposed and as sums of two bfloat16 values: term t of column i of
 // row j at out[(t * dim + i) * wpad + j].
 constexpr int kTransTile = 64;
-__global__ void __launch_bounds__(kPrepThreads)
-transpose_kernel(const uint8_t* __restrict__ q, int64_t stride, int64_t width, int32_t dim,
-                 int32_t row_bytes, __nv_bfloat16* __restrict__ out, int64_t wpad) {
+struct TransposeArgs {
+  const uint8_t* q;
+  int64_t stride, width;
+  int32_t dim, row_bytes;
+  __nv_bfloat16* out;
+  int64_t wpad;
+  int32_t tiles_i;
+};
+__device__ __forceinline__ void transpose_tile(const TransposeArgs& a, int64_t block) {
+  const uint8_t* q = a.q;
+  const int64_t stride = a.stride, width = a.width, wpad = a.wpad;
+  const int32_t dim = a.dim, row_bytes = a.row_bytes;
+  __nv_bfloat16* out = a.out;
   __shared__ __align__(16) uint8_t tile[kTransTile][kTransTile + 16];
   __shared__ float scale[kTransTile];
-  const int64_t j0 = (int64_t)blockIdx.x * kTransTile;
-  const int32_t i0 = (int32_t)blockIdx.y * kTransTile;
+  const int64_t j0 = block / a.tiles_i * kTransTile;
+  const int32_t i0 = (int32_t)(block % a.tiles_i) * kTransTile;
   {
     const int j = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
     uint4 v = make_uint4(0, 0, 0, 0);
@@ -153,6 +164,82 @@ transpose_kernel(const uint8_t* __restrict__ q, int64_t stride, int64_t width, i
     store_vec<__nv_bfloat16, 8>(to, hi);
     store_vec<__nv_bfloat16, 8>(to + (int64_t)dim * wpad, lo);
   }
+}
+
+// Eight values of a row to a thread; see split_grad.  kWide: rows that are 16-byte aligned and
+// whole eights.
+struct SplitArgs {
+  const void* x;
+  int64_t stride, rows, width;
+  int32_t groups;
+  uint32_t inv_groups;
+  __nv_bfloat16* out;
+  int64_t wpad;
+};
+template <typename T, bool kWide>
+__device__ __forceinline__ void split_rows(const SplitArgs& a, int64_t block) {
+  const T* x = (const T*)a.x;
+  const int64_t stride = a.stride, rows = a.rows, width = a.width, wpad = a.wpad;
+  __nv_bfloat16* out = a.out;
+  const FlatRows flat(block, a.groups, a.inv_groups);
+#pragma unroll
+  for (int u = 0; u < kFlat / kPrepThreads; ++u) {
+    int64_t row;
+    uint32_t g;
+    flat.at(threadIdx.x + u * kPrepThreads, &row, &g);
+    if (row >= rows) continue;
+    const T* from = x + row * stride + g * 8;
+    float v[8], rest[8];
+    if constexpr (kWide) {
+      load_vec<T, 8>(from, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (int64_t)g * 8 + e < width ? to_f32(from[e]) : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) int8_split(v[e], v[e], rest[e]);
+    __nv_bfloat16* to = out + row * wpad + g * 8;
+    store_vec<__nv_bfloat16, 8>(to, v);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) continue;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) int8_split(rest[e], rest[e], v[e]);
+      store_vec<__nv_bfloat16, 8>(to + 2 * rows * wpad, v);
+    }
+    store_vec<__nv_bfloat16, 8>(to + rows * wpad, rest);
+  }
+}
+
+// The operands of the backward pass in one launch: the first `transposes` CTAs have the
+// weights, the others the gradient.
+template <typename T, bool kWide>
+__global__ void __launch_bounds__(kPrepThreads)
+prepare_kernel(const TransposeArgs w, int64_t transposes, const SplitArgs g) {
+  if ((int64_t)blockIdx.x < transposes)
+    transpose_tile(w, blockIdx.x);
+  else
+    split_rows<T, kWide>(g, (int64_t)blockIdx.x - transposes);
+}
+
+// The weights where t.q is set; the gradient of `dtype` where g.x is.
+cudaError_t prepare_operands(TransposeArgs t, SplitArgs g, int32_t dtype, cudaStream_t st) {
+  int64_t transposes = 0, splits = 0;
+  if (t.q) {
+    t.tiles_i = (int32_t)ceil_div(t.dim, kTransTile);
+    transposes = ceil_div(t.width, kTransTile) * t.tiles_i;
+  }
+  if (g.x) {
+    g.groups = (int32_t)(g.wpad / 8);
+    g.inv_groups = flat_inverse(g.groups);
+    splits = ceil_div(g.rows * g.groups, kFlat);
+  }
+  return with_float_type(dtype, [&](auto tag) {
+    using T = typename decltype(tag)::type;
+    const bool wide = g.width % 8 == 0 && aligned_rows(g.x, g.stride * (int64_t)sizeof(T), 16);
+    (wide ? prepare_kernel<T, true> : prepare_kernel<T, false>)
+        <<<(unsigned)(transposes + splits), kPrepThreads, 0, st>>>(t, transposes, g);
+    return cudaGetLastError();
+  });
 }
 
 // ---- tiles ----------------------------------------------------------------------
@@ -705,7 +792,7 @@ cudaError_t launch_few(const LinearArgs& a, int device, cudaStream_t st) {
 struct LinearSpace {
   int64_t kpad, scales, bytes;
   LinearSpace(int64_t rows, int64_t width, int64_t dim) {
-    const bool tiles = rows > AGNES_INT8_FEW_ROWS && width > 0;
+    const bool tiles = rows > kFewRows && width > 0;
     kpad = ceil_div(dim, 8) * 8;
     scales = ceil_div(width * kpad * 2, 256) * 256;
     bytes = tiles ? scales + width * 4 : 0;
@@ -762,54 +849,11 @@ cudaError_t launch_linear(const LinearArgs& l, void* workspace, int32_t* status,
   return launch_product<TOut, true>(a, o, drain, device, st);
 }
 
-// Eight values of a row to a thread; see split_grad.  kWide: rows that are 16-byte aligned and
-// whole eights.
-template <typename T, bool kWide>
-__global__ void __launch_bounds__(kPrepThreads)
-split_kernel(const T* __restrict__ x, int64_t stride, int64_t rows, int64_t width,
-             int32_t groups, uint32_t inv_groups, __nv_bfloat16* __restrict__ out, int64_t wpad) {
-  const FlatRows flat(blockIdx.x, groups, inv_groups);
-#pragma unroll
-  for (int u = 0; u < kFlat / kPrepThreads; ++u) {
-    int64_t row;
-    uint32_t g;
-    flat.at(threadIdx.x + u * kPrepThreads, &row, &g);
-    if (row >= rows) continue;
-    const T* from = x + row * stride + g * 8;
-    float v[8], rest[8];
-    if constexpr (kWide) {
-      load_vec<T, 8>(from, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (int64_t)g * 8 + e < width ? to_f32(from[e]) : 0.f;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) int8_split(v[e], v[e], rest[e]);
-    __nv_bfloat16* to = out + row * wpad + g * 8;
-    store_vec<__nv_bfloat16, 8>(to, v);
-    if constexpr (std::is_same<T, __nv_bfloat16>::value) continue;
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) int8_split(rest[e], rest[e], v[e]);
-      store_vec<__nv_bfloat16, 8>(to + 2 * rows * wpad, v);
-    }
-    store_vec<__nv_bfloat16, 8>(to + rows * wpad, rest);
-  }
-}
-
 }  // namespace
 
 cudaError_t split_grad(const void* grad, int32_t dtype, int64_t stride, int64_t rows,
                        int64_t width, __nv_bfloat16* out, int64_t wpad, cudaStream_t st) {
-  return with_float_type(dtype, [&](auto t) {
-    using T = typename decltype(t)::type;
-    const int64_t groups = wpad / 8;
-    const bool wide = width % 8 == 0 && aligned_rows(grad, stride * (int64_t)sizeof(T), 16);
-    (wide ? split_kernel<T, true> : split_kernel<T, false>)
-        <<<(unsigned)ceil_div(rows * groups, kFlat), kPrepThreads, 0, st>>>(
-            (const T*)grad, stride, rows, width, (int32_t)groups, flat_inverse(groups), out, wpad);
-    return cudaGetLastError();
-  });
+  return prepare_operands({}, {grad, stride, rows, width, 0, 0, out, wpad}, dtype, st);
 }
 
 agnes_status product_check_sizes(const char* op, int64_t rows, int64_t width, int64_t dim) {
@@ -908,7 +952,9 @@ agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, co
     if (rows == 1) return launch_few<TOut, 1>(a, device, st);
     if (rows == 2) return launch_few<TOut, 2>(a, device, st);
     if (rows <= 4) return launch_few<TOut, 4>(a, device, st);
-    if (rows <= AGNES_INT8_FEW_ROWS) return launch_few<TOut, 8>(a, device, st);
+    if (rows <= 8) return launch_few<TOut, 8>(a, device, st);
+    if (rows <= 16) return launch_few<TOut, 16>(a, device, st);
+    if (rows <= kFewRows) return launch_few<TOut, 32>(a, device, st);
     return launch_linear<TOut>(a, workspace, status, device, st);
   }));
 }
@@ -964,20 +1010,19 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
   __nv_bfloat16* wt = (__nv_bfloat16*)workspace;
   __nv_bfloat16* terms = (__nv_bfloat16*)((uint8_t*)workspace + space.grad);
   const int64_t row_bytes = int8_row_bytes(dim);
-  transpose_kernel<<<dim3((unsigned)ceil_div(width, kTransTile), (unsigned)ceil_div(dim, kTransTile)),
-                     kPrepThreads, 0, st>>>((const uint8_t*)w, width > 1 ? w_stride : row_bytes,
-                                            width, (int32_t)dim, (int32_t)row_bytes, wt,
-                                            space.wpad);
-  OP_TRY(op_launched(op, cudaGetLastError()));
   TileOperands o = {grad, wt, rows > 1 ? step * 2 : space.wpad * 2, space.wpad * 2, width};
   TileArgs a = {};
   a.ta = 1;
+  const TransposeArgs t = {(const uint8_t*)w, width > 1 ? w_stride : row_bytes, width,
+                           (int32_t)dim, (int32_t)row_bytes, wt, space.wpad, 0};
+  SplitArgs g = {};
   if (!direct) {
     a.ta = grad_terms(grad_dtype);
-    OP_TRY(op_launched(op, split_grad(grad, grad_dtype, step, rows, width, terms, space.wpad, st)));
+    g = {grad, step, rows, width, 0, 0, terms, space.wpad};
     o.a = terms;
     o.a_stride = space.wpad * 2;
   }
+  OP_TRY(op_launched(op, prepare_operands(t, g, grad_dtype, st)));
   a.rows = rows;
   a.cols = dim;
   a.tb = 2;

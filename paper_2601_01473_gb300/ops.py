@@ -692,15 +692,19 @@ def _vector(name, t, n, device):
     """The address of a float32 vector [n], or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.shape != (n,) or \
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (n,) or \
             not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous float32 tensor [{n}]")
-    _on(name, t, device)
+    if t.device != device:
+        _on(name, t, device)
     return t.data_ptr()
 
 
 def _matrix(name, t, rows, dim, dtype, device):
     """(address, row stride) of a matrix [rows, dim] of ``dtype``."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and dtype in _FLOATS and \
+            t.shape == (rows, dim) and t.is_contiguous() and t.device == device and t.is_cuda:
+        return t.data_ptr(), dim
     _, n, cols, step = _rows(name, t, device)
     if (n, cols) != (rows, dim) or t.dtype != dtype:
         raise ValueError(f"{name} must be {(rows, dim)} of {dtype}, not {tuple(t.shape)} of "
@@ -799,29 +803,33 @@ def residual_norm_grad(grad_next, grad_sum, sum, branch=None, gate=None, scale: 
     ds_at, ds_step = (None, 0) if grad_sum is None else \
         _matrix("grad_sum", grad_sum, rows, dim, sum.dtype, device)
     g_at, g_kind, g_step = _gate_arguments(gate, rows, dim, b_type, device)
-    vectors = [_vector(name, v, dim, device) for name, v in
-               (("after", after), ("after_bias", after_bias), ("before", before),
-                ("before_bias", before_bias))]
-
-    def matrix(dtype):
-        return torch.empty((rows, dim), dtype=dtype, device=device)
-
-    def like(v):
-        return None if v is None else torch.empty(dim, dtype=torch.float32, device=device)
-
-    dx, db = matrix(sum.dtype), None if branch is None else matrix(b_type)
-    dgate = matrix(b_type) if g_kind == _GATE_ROWS else like(gate)
-    sums = [like(v) for v in (after, after_bias, before, before_bias)]
+    after_at = _vector("after", after, dim, device)
+    after_bias_at = _vector("after_bias", after_bias, dim, device)
+    before_at = _vector("before", before, dim, device)
+    _vector("before_bias", before_bias, dim, device)
+    dx = torch.empty((rows, dim), dtype=sum.dtype, device=device)
+    db = None if branch is None else torch.empty((rows, dim), dtype=b_type, device=device)
+    dgate = torch.empty((rows, dim), dtype=b_type, device=device) if g_kind == _GATE_ROWS else None
+    # the vectors' gradients are parts of one tensor
+    vectors = (gate if g_kind == _GATE_COLUMNS else None, after, after_bias, before, before_bias)
+    part = (dim + 3) // 4 * 4
+    buffer = torch.empty(5 * part, dtype=torch.float32, device=device)
+    at = buffer.data_ptr()
+    sums = [None if v is None else buffer.as_strided((dim,), (1,), k * part)
+            for k, v in enumerate(vectors)]
+    sum_at = [None if v is None else at + 4 * k * part for k, v in enumerate(vectors)]
     ws, ws_at, ws_bytes = _workspace(device, "agnes_residual_norm_grad_workspace", rows, dim)
-
-    def at(t):
-        return None if t is None else t.data_ptr()
-
+    if g_kind == _GATE_COLUMNS:
+        dgate = sums[0]
+        dgate_at = sum_at[0]
+    else:
+        dgate_at = None if dgate is None else dgate.data_ptr()
     rc = lib().agnes_residual_norm_grad(
         dn_at, dn_step, ds_at, ds_step, sum.data_ptr(), _FLOATS[sum.dtype], step, b_at,
-        _FLOATS.get(b_type, -1), b_step, rows, dim, g_at, g_kind, g_step, scale, *vectors[:3],
-        _norm_kind(kind), eps, dx.data_ptr(), dim, at(db), dim, at(dgate), dim,
-        *(at(t) for t in sums), ws_at, ws_bytes, _stream(device))
+        _FLOATS.get(b_type, -1), b_step, rows, dim, g_at, g_kind, g_step, scale, after_at,
+        after_bias_at, before_at, _norm_kind(kind), eps, dx.data_ptr(), dim,
+        None if db is None else db.data_ptr(), dim, dgate_at, dim, sum_at[1], sum_at[2],
+        sum_at[3], sum_at[4], ws_at, ws_bytes, _stream(device))
     if rc:
         _failed(rc)
-    return NormGrad(dx, db, dgate, *sums)
+    return NormGrad(dx, db, dgate, *sums[1:])

@@ -223,6 +223,13 @@ def test_product_of_few_rows(cuda_device, out, rows, width, dim):
     _product_check(cuda_device, rows, width, dim, out, rows % 2 == 0)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [9, 16, 17, 31, 32, 33, 64])
+@pytest.mark.parametrize("width,dim", [(1, 1), (70, 301), (257, 2048)])
+def test_product_of_some_rows(cuda_device, rows, width, dim):
+    _product_check(cuda_device, rows, width, dim, FLOATS[rows % 3], rows % 2 == 0)
+
+
 SIZES = [(9, 8, 32), (128, 128, 64), (128, 256, 128), (16, 1, 1), (129, 130, 33), (200, 96, 128),
          (1000, 257, 301), (130, 300, 1024), (64, 500, 4096), (40_000, 256, 128), (300, 17, 12),
          (257, 513, 80), (5000, 64, 520), (700, 1000, 2000)]

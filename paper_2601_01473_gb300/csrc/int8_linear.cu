@@ -283,16 +283,19 @@ struct TileArgs {
   int32_t* status;
 };
 
-// The output tiles of a CTA, every gridDim.x-th, columns fastest.
+// The output tiles of a CTA (or of a pair, kGroup = 2), every one of as many as there are
+// CTAs, columns fastest.
+template <int kGroup>
 struct TileWalk {
   int64_t m, n, tiles_m, tiles_n, step_m, step_n;
   __device__ TileWalk(const TileArgs& a, int cols) {
+    const uint32_t at = blockIdx.x / kGroup, count = gridDim.x / kGroup;
     tiles_n = (a.cols + cols - 1) / cols;
-    tiles_m = (a.rows + kTileM - 1) / kTileM;
-    m = blockIdx.x / tiles_n;
-    n = blockIdx.x - m * tiles_n;
-    step_m = gridDim.x / tiles_n;
-    step_n = gridDim.x - step_m * tiles_n;
+    tiles_m = (a.rows + kGroup * kTileM - 1) / (kGroup * kTileM);
+    m = at / tiles_n;
+    n = at - m * tiles_n;
+    step_m = count / tiles_n;
+    step_n = count - step_m * tiles_n;
   }
   __device__ bool any() const { return m < tiles_m; }
   __device__ void next() {
@@ -369,7 +372,7 @@ __device__ __forceinline__ uint2 int8_halves4(uint32_t word) {
 // A slice's products, n of 16 for each two terms but the third with the second.  The thread
 // that issues them has one at a time to prepare, so their descriptors are sums of constants
 // (looked up term by term a product took some 250 cycles to issue, twice its own time).
-template <int kTermsA, int kTermsB, int kCols>
+template <int kTermsA, int kTermsB, int kBRows, bool kPair>
 __device__ __forceinline__ void slice_products(uint32_t to, uint32_t a_at, uint32_t b_at, int n,
                                                uint32_t idesc, uint32_t accumulate) {
   const uint64_t a0 = operand_desc(a_at), b0 = operand_desc(b_at);
@@ -381,9 +384,13 @@ __device__ __forceinline__ void slice_products(uint32_t to, uint32_t a_at, uint3
 #pragma unroll
       for (int q = 0; q < kTermsB; ++q) {
         if (p + q >= 3) continue;
-        mma_16bit(to, a0 + (uint64_t)(p * (kOperandBytes >> 4) + 2 * i),
-                  b0 + (uint64_t)(q * (kCols * 128 >> 4) + 2 * i), idesc,
-                  accumulate | (uint32_t)(i + p + q > 0));
+        const uint64_t a = a0 + (uint64_t)(p * (kOperandBytes >> 4) + 2 * i);
+        const uint64_t b = b0 + (uint64_t)(q * (kBRows * 128 >> 4) + 2 * i);
+        const uint32_t more = accumulate | (uint32_t)(i + p + q > 0);
+        if constexpr (kPair)
+          mma_16bit_pair(to, a, b, idesc, more);
+        else
+          mma_16bit(to, a, b, idesc, more);
       }
   }
 }
@@ -393,15 +400,19 @@ __device__ __forceinline__ void slice_products(uint32_t to, uint32_t a_at, uint3
 // kDrain: an accumulator sums `chain` slices, and the epilogue warps add those up in
 // registers: tensor memory's sums are cut off, not rounded, after each product, which adds
 // up over long chains.
-template <typename TOut, bool kConvert, int kCols, bool kDrain>
+// kPair: two CTAs have a tile of 256 x kCols, each the rows and the output of its half and half
+// of B, so that B is copied and read once for both.
+template <typename TOut, bool kConvert, int kCols, bool kDrain, bool kPair>
 __global__ void __launch_bounds__(kTileThreads, 1)
 tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
             const __grid_constant__ CUtensorMap out_map, const TileArgs a) {
   grid_dep_wait();
   constexpr int kHalf = kCols / 2;  // columns of an epilogue warp
   constexpr int kTmemCols = 2 * kCols;
-  constexpr uint32_t kIdesc = idesc_16bit(!kConvert, false, kTileM, kCols);
-  constexpr uint32_t kBBytes = kCols * 128;
+  constexpr uint32_t kIdesc = idesc_16bit(!kConvert, false, kPair ? 2 * kTileM : kTileM, kCols);
+  constexpr int kBRows = kPair ? kCols / 2 : kCols;  // of B in this CTA
+  constexpr uint32_t kBBytes = kBRows * 128;
+  const uint32_t rank = kPair ? cluster_rank() : 0;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
   uint8_t* resident_b = smem + a.slots * a.slot_bytes;
@@ -412,16 +423,22 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
   uint32_t* tmem_slot = (uint32_t*)(bars + kTileBars);
   const TileBars bar = {smem_addr(bars)};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (warp == kMmaWarp) tmem_alloc(tmem_slot, kTmemCols);
+  if (warp == kMmaWarp) {
+    if constexpr (kPair)
+      tmem_alloc_pair(tmem_slot, kTmemCols);
+    else
+      tmem_alloc(tmem_slot, kTmemCols);
+  }
   if (tid == 0) {
+    constexpr int kBoth = kPair ? 2 : 1;  // a pair's first CTA is told by the warps of both
     for (int s = 0; s < kMaxSlots; ++s) {
       mbar_init(bar.full(s), 1);
-      mbar_init(bar.ready(s), kConvertWarps);
+      mbar_init(bar.ready(s), (kConvert ? kConvertWarps : 1) * kBoth);
       mbar_init(bar.empty(s), 1);
     }
     for (int d = 0; d < 2; ++d) {
       mbar_init(bar.done(d), 1);
-      mbar_init(bar.taken(d), kEpilogueWarps);
+      mbar_init(bar.taken(d), kEpilogueWarps * kBoth);
     }
     mbar_init(bar.b_full(), 1);
     mbar_init(bar.drained(), 1);
@@ -429,9 +446,21 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
   }
   tcgen05_fence_before();
   __syncthreads();
+  if constexpr (kPair) cluster_sync();  // the other CTA's barriers are there
   tcgen05_fence_after();
   const uint32_t tmem = *tmem_slot;
-  TileWalk t(a, kCols);
+  // for the thread that issues the products: of this CTA, or of the pair's first
+  const auto tell = [&](uint32_t b) {
+    if constexpr (kPair)
+      mbar_arrive_at(b, 0);
+    else
+      mbar_arrive(b);
+  };
+  using Walk = TileWalk<kPair ? 2 : 1>;
+  Walk t(a, kCols);
+  const auto first_row = [&](const Walk& at) {
+    return kPair ? (at.m * 2 + rank) * kTileM : at.m * kTileM;
+  };
   const int slots = a.slots;
   const uint32_t ring_at = smem_addr(smem), resident_at = smem_addr(resident_b);
   // in a slot: A's terms, B's (unless they are resident), A's raw bytes
@@ -446,7 +475,7 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
         for (int k = 0; k < a.steps; ++k)
           for (int b = 0; b < a.tb; ++b)
             tma_load(resident_at + (uint32_t)(k * a.tb + b) * kBBytes, &b_map, k * kSliceK,
-                     (int32_t)(b * a.cols + t.n * kCols), bar.b_full());
+                     (int32_t)(b * a.cols + t.n * kCols + rank * kBRows), bar.b_full());
       }
       const uint32_t bytes = (kConvert ? (uint32_t)kRawBytes : b_off) +
                              (a.resident ? 0u : (uint32_t)a.tb * kBBytes);
@@ -462,18 +491,24 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
           const uint32_t at = ring_at + (uint32_t)(s * a.slot_bytes);
           mbar_expect(bar.full(s), bytes);
           if constexpr (kConvert) {
-            tma_load(at + raw_off, &a_map, k * kSliceK, (int32_t)(t.m * kTileM), bar.full(s));
+            tma_load(at + raw_off, &a_map, k * kSliceK, (int32_t)first_row(t), bar.full(s));
           } else {
             for (int i = 0; i < a.ta; ++i)
               tma_load(at + (uint32_t)(i * kOperandBytes), &a_map, k * kSliceK,
-                       (int32_t)(i * a.rows + t.m * kTileM), bar.full(s));
+                       (int32_t)(i * a.rows + first_row(t)), bar.full(s));
           }
           if (!a.resident)
             for (int i = 0; i < a.tb; ++i)
               tma_load(at + b_off + (uint32_t)i * kBBytes, &b_map, k * kSliceK,
-                       (int32_t)(i * a.cols + t.n * kCols), bar.full(s));
+                       (int32_t)(i * a.cols + t.n * kCols + rank * kBRows), bar.full(s));
           ring.next(slots);
           ++issued;
+        }
+      }
+      if (kPair && ok) {  // the other CTA's last arrivals here land before this one may leave
+        for (int s = 0; ok && s < slots; ++s) {
+          ok = ring.first || mbar_wait(bar.empty(ring.slot), ring.parity ^ 1u);
+          ring.next(slots);
         }
       }
       if (!ok) {  // the copies in flight land before the CTA may leave
@@ -484,7 +519,13 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
       }
     }
   } else if (warp == kMmaWarp) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
+      const auto commit = [](uint32_t b) {
+        if constexpr (kPair)
+          mma_commit_pair(b);
+        else
+          mma_commit(b);
+      };
       if (a.resident) ok = mbar_wait(bar.b_full(), 0);
       Ring ring, acc;
       for (; ok && t.any(); t.next()) {
@@ -501,7 +542,7 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
           for (int k = k0; k < k1; ++k) {
             const int s = ring.slot;
             if (!mbar_wait(bar.full(s), ring.parity) ||
-                (kConvert && !mbar_wait(bar.ready(s), ring.parity))) {
+                ((kConvert || kPair) && !mbar_wait(bar.ready(s), ring.parity))) {
               ok = false;
               break;
             }
@@ -511,28 +552,44 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
                 a.resident ? resident_at + (uint32_t)(k * a.tb) * kBBytes : a_at + b_off;
             const int n = k + 1 == a.steps ? a.last : kSliceK / 16;
             if (kConvert)
-              slice_products<1, 1, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+              slice_products<1, 1, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
             else if (a.ta == 1)
-              slice_products<1, 2, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+              slice_products<1, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
             else if (a.ta == 2)
-              slice_products<2, 2, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+              slice_products<2, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
             else
-              slice_products<3, 2, kCols>(to, a_at, b_at, n, kIdesc, accumulate);
+              slice_products<3, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
             accumulate = 1;
-            mma_commit(bar.empty(s));
+            commit(bar.empty(s));
             ring.next(slots);
           }
           if (!ok) break;
-          mma_commit(bar.done(d));
+          commit(bar.done(d));
           acc.next(2);
         }
       }
       if (!ok) {  // the products in flight end before the tensor memory is freed
-        mma_commit(bar.drained());
+        commit(bar.drained());
         mbar_wait(bar.drained(), 0);
       }
     }
   } else if (warp >= kConvertWarp0) {
+    if constexpr (!kConvert && kPair) {
+      // one warp tells the pair's first CTA of this one's slices
+      if (warp == kConvertWarp0) {
+        Ring ring;
+        for (; ok && t.any(); t.next()) {
+          for (int k = 0; k < a.steps; ++k) {
+            if (!__all_sync(0xffffffffu, mbar_wait(bar.full(ring.slot), ring.parity))) {
+              ok = false;
+              break;
+            }
+            if (lane == 0) tell(bar.ready(ring.slot));
+            ring.next(slots);
+          }
+        }
+      }
+    }
     if constexpr (kConvert) {
       const int r = tid - 32 * kConvertWarp0;  // this thread's row of the tile
       Ring ring;
@@ -560,7 +617,7 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
           }
           fence_async_proxy();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar.ready(s));
+          if (lane == 0) tell(bar.ready(s));
           ring.next(slots);
         }
       }
@@ -571,8 +628,8 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
     int buffer = 0;
     Ring acc;
     // a tile ahead, as it is some trip away
-    const auto scale_of = [&](const TileWalk& at) {
-      const int64_t row = at.m * kTileM + (warp & 3) * 32 + lane;
+    const auto scale_of = [&](const Walk& at) {
+      const int64_t row = first_row(at) + (warp & 3) * 32 + lane;
       return kConvert && at.any() && row < a.rows
                  ? __ldg((const float*)(a.x + row * a.x_stride + a.row_bytes - 4)) : 1.f;
     };
@@ -581,7 +638,7 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
     float* my_scales = column_stage + warp * 256;
     float* my_biases = my_scales + 128;
     Columns<kHalf> next_scales, next_biases;
-    const auto columns_of = [&](const TileWalk& at) {
+    const auto columns_of = [&](const Walk& at) {
       if constexpr (kConvert) {
         const int64_t c0 = at.n * kCols + (warp >> 2) * kHalf;
         next_scales.load(a.col_scale, c0, a.cols, at.any());
@@ -597,11 +654,11 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
         next_biases.put(my_biases);
         __syncwarp();
       }
-      TileWalk after = t;
+      Walk after = t;
       after.next();
       next_scale = scale_of(after);
       columns_of(after);
-      const int64_t row0 = t.m * kTileM + (warp & 3) * 32;
+      const int64_t row0 = first_row(t) + (warp & 3) * 32;
       const int64_t n0 = t.n * kCols + (warp >> 2) * kHalf;
       // a warp whose rows are all past the end has nothing to store, and its buffers may
       // still be on their way
@@ -639,7 +696,7 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
           }
           tcgen05_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar.taken(d));
+          if (lane == 0) tell(bar.taken(d));
         }
         acc.next(2);
       }
@@ -702,7 +759,7 @@ const float4* w4 = (const float4*)(my_scales + c + h);
       if constexpr (!kDrain) {
         tcgen05_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar.taken(acc.slot ^ 1));
+        if (lane == 0) tell(bar.taken(acc.slot ^ 1));
       }
     }
     // the stores in flight have read shared memory before the CTA leaves
@@ -711,9 +768,13 @@ const float4* w4 = (const float4*)(my_scales + c + h);
   if (!ok) op_flag(a.status, AGNES_OP_TIMEOUT);
   tcgen05_fence_before();
   __syncthreads();
+  if constexpr (kPair) cluster_sync();  // nobody arrives at or reads this CTA's any more
   if (warp == kMmaWarp) {
     tcgen05_fence_after();
-    tmem_free(tmem, kTmemCols);
+    if constexpr (kPair)
+      tmem_free_pair(tmem, kTmemCols);
+    else
+      tmem_free(tmem, kTmemCols);
   }
 }
 
@@ -724,7 +785,7 @@ struct TileOperands {
   int64_t k;
 };
 
-template <typename TOut, bool kConvert, int kCols, bool kDrain>
+template <typename TOut, bool kConvert, int kCols, bool kDrain, bool kPair>
 cudaError_t launch_tiles(TileArgs a, const TileOperands& o, int device, cudaStream_t st) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return cudaErrorNotSupported;
@@ -736,8 +797,8 @@ cudaError_t launch_tiles(TileArgs a, const TileOperands& o, int device, cudaStre
                            o.a_stride, kSliceK, kTileM, CU_TENSOR_MAP_SWIZZLE_64B)
                 : map_rows(encode, &a_map, type, o.a, o.k, a.ta * a.rows, o.a_stride, kSliceK,
                            kTileM, CU_TENSOR_MAP_SWIZZLE_128B)) &&
-      map_rows(encode, &b_map, type, o.b, o.k, a.tb * a.cols, o.b_stride, kSliceK, kCols,
-               CU_TENSOR_MAP_SWIZZLE_128B);
+      map_rows(encode, &b_map, type, o.b, o.k, a.tb * a.cols, o.b_stride, kSliceK,
+               kPair ? kCols / 2 : kCols, CU_TENSOR_MAP_SWIZZLE_128B);
   if (!mapped) return cudaErrorInvalidValue;
   const int64_t out_bytes = a.out_stride * (int64_t)sizeof(TOut);
   a.tma_out = aligned_rows(a.out, out_bytes, 16) && out_bytes < (1ll << 40);
@@ -747,18 +808,19 @@ cudaError_t launch_tiles(TileArgs a, const TileOperands& o, int device, cudaStre
     return cudaErrorInvalidValue;
   static OncePerDevice once;
   const cudaError_t e = once.run(device, [] {
-    return cudaFuncSetAttribute(tile_kernel<TOut, kConvert, kCols, kDrain>,
+    return cudaFuncSetAttribute(tile_kernel<TOut, kConvert, kCols, kDrain, kPair>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
   });
   if (e != cudaSuccess) return e;
   a.steps = (int32_t)ceil_div(o.k, kSliceK);
   a.last = (int32_t)ceil_div(o.k - (int64_t)(a.steps - 1) * kSliceK, 16);
   if (!kDrain) a.chain = a.steps;
-  const int num_sms = op_num_sms(device);
-  const int64_t tiles_m = ceil_div(a.rows, kTileM), tiles_n = ceil_div(a.cols, kCols);
-  const int b_slice = a.tb * kCols * 128;
+  const int group = kPair ? 2 : 1;
+  const int num_sms = op_num_sms(device) / group;  // or pairs of them
+  const int64_t tiles_m = ceil_div(a.rows, group * kTileM), tiles_n = ceil_div(a.cols, kCols);
+  const int b_slice = a.tb * kCols * 128 / group;
   const int a_slice = a.ta * kOperandBytes + (kConvert ? kRawBytes : 0);
-  a.resident = tiles_n <= num_sms &&
+  a.resident = !kPair && tiles_n <= num_sms &&
                (int64_t)a.steps * b_slice + 3 * a_slice + kEpilogueWarps * kOutBytes <= tile_smem(kConvert);
   a.slot_bytes = a_slice + (a.resident ? 0 : b_slice);
   const int fixed = a.resident ? a.steps * b_slice : 0;
@@ -773,8 +835,9 @@ cudaError_t launch_tiles(TileArgs a, const TileOperands& o, int device, cudaStre
   int64_t grid = num_sms;
   if (a.resident) grid = num_sms / tiles_n * tiles_n;  // a CTA's columns stay the same
   if (tiles_m <= grid / tiles_n) grid = tiles_m * tiles_n;
-  return launch_next(tile_kernel<TOut, kConvert, kCols, kDrain>, dim3((unsigned)grid),
-                     (unsigned)kTileThreads, smem, st, a_map, b_map, out_map, a);
+  return launch_next_cluster(tile_kernel<TOut, kConvert, kCols, kDrain, kPair>,
+                             dim3((unsigned)(grid * group)), (unsigned)kTileThreads, smem,
+                             (unsigned)group, st, a_map, b_map, out_map, a);
 }
 
 template <typename TOut, int kRows>
@@ -813,9 +876,18 @@ struct GradInputSpace {
 template <typename TOut, bool kConvert>
 cudaError_t launch_product(const TileArgs& a, const TileOperands& o, bool drain, int device,
                            cudaStream_t st) {
-  if (drain) return launch_tiles<TOut, kConvert, 128, true>(a, o, device, st);
-  if (a.cols <= 128) return launch_tiles<TOut, kConvert, 128, false>(a, o, device, st);
-  return launch_tiles<TOut, kConvert, 256, false>(a, o, device, st);
+  if (drain) return launch_tiles<TOut, kConvert, 128, true, false>(a, o, device, st);
+  if (a.cols <= 128) return launch_tiles<TOut, kConvert, 128, false, false>(a, o, device, st);
+  // A pair's turn of 256 rows takes 0.75 (bfloat16 terms) to 0.86 (whole numbers) of what two
+  // CTAs of their own take for theirs, where rows are long: 16,384 x 4096 to 4096 403 us and
+  // 469, the gradient of 8192 x 4096 to 2048 columns 158 and 212.  With fewer and larger tiles the
+  // last turn may be emptier: 6000 x 1024 to 4096 55 us and 50.
+  const int64_t tiles_n = ceil_div(a.cols, 256), sms = op_num_sms(device);
+  const int64_t turns = ceil_div(ceil_div(a.rows, kTileM) * tiles_n, sms);
+  const int64_t pair_turns = ceil_div(ceil_div(a.rows, 2 * kTileM) * tiles_n, sms / 2);
+  if (o.k >= 512 && sms >= 2 && pair_turns * 85 < turns * 100)
+    return launch_tiles<TOut, kConvert, 256, false, true>(a, o, device, st);
+  return launch_tiles<TOut, kConvert, 256, false, false>(a, o, device, st);
 }
 
 template <typename TOut>

@@ -129,20 +129,29 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Launches a kernel whose predecessor on the stream is the kernel before it in the same
 // call, ahead of that one's completion: its CTAs are set up meanwhile and wait in
 // grid_dep_wait(), which has to be the kernel's first statement.
+// `cluster`: CTAs to a cluster.
 template <typename... Params, typename... Args>
-cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem,
-                        cudaStream_t st, Args&&... args) {
-  cudaLaunchAttribute attr[1];
+cudaError_t launch_next_cluster(void (*kernel)(Params...), dim3 grid, unsigned threads,
+                                size_t smem, unsigned cluster, cudaStream_t st, Args&&... args) {
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+template <typename... Params, typename... Args>
+cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem,
+                        cudaStream_t st, Args&&... args) {
+  return launch_next_cluster(kernel, grid, threads, smem, 1, st, args...);
 }
 
 // Lets the next kernel's CTAs be set up from here on.

@@ -70,6 +70,65 @@ __device__ __forceinline__ void mma_16bit(uint32_t d, uint64_t a, uint64_t b, ui
       : "memory");
 }
 
+// ---- pairs of CTAs: a cluster of two, whose first issues products of 256 rows, 128 from each
+// CTA's shared memory to its own tensor memory, with half of the other operand's rows in each
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\t"
+      "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Arrives at the mbarrier at the same place in the shared memory of CTA `rank`.  What the
+// arriving warp wrote is its own CTA's shared memory, which it has made visible to its tensor
+// core (fence_async_proxy), and the other CTA's thread only has that read, so no wider release
+// is asked for: one at cluster scope held every slice up for 3 us (16,384 x 4096 to 4096 849 us
+// instead of 403).
+__device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank) {
+  asm volatile(
+      "{\n\t.reg .b32 at;\n\t"
+      "mapa.shared::cluster.u32 at, %0, %1;\n\t"
+      "mbarrier.arrive.shared::cluster.b64 _, [at];\n\t}" ::"r"(bar),
+      "r"(rank)
+      : "memory");
+}
+
+// The same as mma_16bit and mma_commit for a pair; the commit arrives at the mbarrier's place
+// in both CTAs.
+__device__ __forceinline__ void mma_16bit_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                               uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
+      "[%0], %1;" ::"r"(bar),
+      "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                   smem_addr(slot)),
+               "r"(cols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t addr, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols)
+               : "memory");
+}
+
 // What a kernel wrote to shared memory is there for the tensor core and the TMA.
 __device__ __forceinline__ void fence_async_proxy() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -242,6 +242,17 @@ def test_product(cuda_device, out, rows, width, dim):
     _product_check(cuda_device, rows, width, dim, out, width % 2 == 0)
 
 
+# more tiles than there are pairs of CTAs, ragged ones among them
+MANY = [(20_000, 600, 520), (9000, 900, 640), (19_900, 500, 1100), (5001, 2000, 515)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,dim", MANY)
+@pytest.mark.parametrize("out", FLOATS)
+def test_product_of_many_tiles(cuda_device, out, rows, width, dim):
+    _product_check(cuda_device, rows, width, dim, out, width % 4 == 0)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows", [3, 40])
 def test_product_of_the_longest_rows(cuda_device, rows):
@@ -358,6 +369,16 @@ def _grad_check(dev, rows, width, dim, dtype, out):
 @pytest.mark.parametrize("dtype", FLOATS)
 def test_gradients(cuda_device, dtype, rows, width, dim):
     _grad_check(cuda_device, rows, width, dim, dtype, FLOATS[(rows + dim) % 3])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,dim", [(m, k, n) for m, n, k in MANY])
+@pytest.mark.parametrize("dtype,out", [(torch.bfloat16, torch.bfloat16),
+                                       (torch.float16, torch.float16),
+                                       (torch.float32, torch.bfloat16),
+                                       (torch.bfloat16, torch.float32)])
+def test_gradients_of_many_tiles(cuda_device, dtype, out, rows, width, dim):
+    _grad_check(cuda_device, rows, width, dim, dtype, out)
 
 
 @pytest.mark.gpu

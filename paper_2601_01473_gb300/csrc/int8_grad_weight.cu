@@ -36,9 +36,11 @@ constexpr int kBiasWarp0 = kMmaWarp + 1, kBiasWarps = 2;
 constexpr int kThreads = 32 * (kBiasWarp0 + kBiasWarps);
 constexpr int kBox = kSlice * 128;           // 64 columns of a slice in 16 bits
 constexpr int kGradBytes = 2 * kBox;         // a term of the gradient
-constexpr int kValueBytes = 4 * kBox;        // the scaled whole numbers' two terms
-constexpr int kRawBytes = kSlice * kTile;
-constexpr int kMaxSlots = 4;
+// Of the scaled whole numbers' two terms and of the whole numbers, for a CTA of its own or one
+// of a pair.
+constexpr int value_bytes(bool pair) { return (pair ? 2 : 4) * kBox; }
+constexpr int raw_bytes(bool pair) { return kSlice * kTile / (pair ? 2 : 1); }
+constexpr int kMaxSlots = 6;
 constexpr int kBars = 3 * kMaxSlots + 5;
 constexpr int kSmemLimit = 232448;
 constexpr int kRingBytes = kSmemLimit - 1024 - 8 * kBars - 16;
@@ -52,6 +54,7 @@ struct WeightArgs {
   const uint8_t* x;
   int64_t x_stride;
   int32_t ta;
+  bool pair;
   int32_t slices;             // of all rows
   int32_t tiles_j, tiles_i;   // of the output, along width and dim
   int32_t splits, per_split;  // shares of the rows, slices of one
@@ -79,11 +82,16 @@ struct WeightBars {
   __device__ uint32_t drained() const { return at(3 * kMaxSlots + 4); }
 };
 
+// kPair: two CTAs have 256 x 128 of the output, each the gradient's columns and the output of
+// its half and both terms of half of the whole numbers.
+template <bool kPair>
 __global__ void __launch_bounds__(kThreads, 1)
 weight_kernel(const __grid_constant__ CUtensorMap grad_map,
               const __grid_constant__ CUtensorMap x_map, const WeightArgs a) {
   grid_dep_wait();
-  constexpr uint32_t kIdesc = idesc_16bit(true, true, kTile, 2 * kTile);
+  constexpr uint32_t kIdesc = idesc_16bit(true, true, kPair ? 2 * kTile : kTile, 2 * kTile);
+  constexpr int kValueBytes = value_bytes(kPair), kRawBytes = raw_bytes(kPair);
+  const uint32_t rank = kPair ? cluster_rank() : 0;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
   uint64_t* bars = (uint64_t*)(smem + a.slots * a.slot_bytes);
@@ -92,30 +100,46 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // this CTA's tile and share
   const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
-  const int64_t tile = blockIdx.x % tiles, split = blockIdx.x / tiles;
-  const int32_t tile_i = (int32_t)(tile % a.tiles_i);
-  const int64_t j0 = tile / a.tiles_i * kTile;
+  constexpr int kGroup = kPair ? 2 : 1;
+  const int64_t item = blockIdx.x / kGroup, groups = tiles / kGroup;
+  const int64_t split = item / groups, group = item % groups;
+  const int32_t tile_i = (int32_t)(group % a.tiles_i);
+  const int64_t tile_j = group / a.tiles_i * kGroup + rank, tile = tile_j * a.tiles_i + tile_i;
+  const int64_t j0 = tile_j * kTile;
   const int32_t i0 = tile_i * kTile;
   const int32_t k0 = (int32_t)split * a.per_split, k1 = min(k0 + a.per_split, a.slices);
   const bool bias = a.bias_partial && tile_i == 0;
-  if (warp == kMmaWarp) tmem_alloc(tmem_slot, kTmemCols);
+  if (warp == kMmaWarp) {
+    if constexpr (kPair)
+      tmem_alloc_pair(tmem_slot, kTmemCols);
+    else
+      tmem_alloc(tmem_slot, kTmemCols);
+  }
   if (tid == 0) {
     for (int s = 0; s < kMaxSlots; ++s) {
       mbar_init(bar.full(s), 1);
-      mbar_init(bar.ready(s), kConvertWarps);
+      mbar_init(bar.ready(s), kConvertWarps * kGroup);
       mbar_init(bar.empty(s), 1 + (bias ? kBiasWarps : 0));
     }
     for (int d = 0; d < 2; ++d) {
       mbar_init(bar.done(d), 1);
-      mbar_init(bar.taken(d), kEpilogueWarps);
+      mbar_init(bar.taken(d), kEpilogueWarps * kGroup);
     }
     mbar_init(bar.drained(), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tcgen05_fence_before();
   __syncthreads();
+  if constexpr (kPair) cluster_sync();  // the other CTA's barriers are there
   tcgen05_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // for the thread that issues the products: of this CTA, or of the pair's first
+  const auto tell = [&](uint32_t b) {
+    if constexpr (kPair)
+      mbar_arrive_at(b, 0);
+    else
+      mbar_arrive(b);
+  };
   const uint32_t ring_at = smem_addr(smem);
   // in a slot: the gradient's terms, the scaled whole numbers', the whole numbers
   const uint32_t value_off = (uint32_t)(a.ta * kGradBytes), raw_off = value_off + kValueBytes;
@@ -140,9 +164,16 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
             tma_load(at + (uint32_t)(p * kGradBytes + b * kBox), &grad_map,
                      (int32_t)(j0 + b * 64), (int32_t)(p * a.rows + (int64_t)k * kSlice),
                      bar.full(s));
-        tma_load(at + raw_off, &x_map, i0, (int32_t)((int64_t)k * kSlice), bar.full(s));
+        tma_load(at + raw_off, &x_map, i0 + (int32_t)rank * (kTile / 2),
+                 (int32_t)((int64_t)k * kSlice), bar.full(s));
         ring.next(a.slots);
         ++issued;
+      }
+      if (kPair && ok) {  // the other CTA's last arrivals here land before this one may leave
+        for (int s = 0; ok && s < a.slots; ++s) {
+          ok = ring.first || mbar_wait(bar.empty(ring.slot), ring.parity ^ 1u);
+          ring.next(a.slots);
+        }
       }
       if (!ok) {  // the copies in flight land before the CTA may leave
         Ring r;
@@ -151,7 +182,19 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
       }
     }
   } else if (warp == kMmaWarp) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
+      const auto multiply = [](uint32_t d, uint64_t x, uint64_t y, uint32_t more) {
+        if constexpr (kPair)
+          mma_16bit_pair(d, x, y, kIdesc, more);
+        else
+          mma_16bit(d, x, y, kIdesc, more);
+      };
+      const auto commit = [](uint32_t b) {
+        if constexpr (kPair)
+          mma_commit_pair(b);
+        else
+          mma_commit(b);
+      };
       Ring acc;
       for (int32_t c0 = k0; ok && c0 < k1; c0 += a.chain) {
         const int d = acc.slot;
@@ -177,25 +220,24 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
 #pragma unroll
           for (int i = 0; i < kSlice / 16; ++i) {
             if (i >= n) break;
-            mma_16bit(to, g0 + (uint64_t)(i * 128), v0 + (uint64_t)(i * 128), kIdesc,
-                      accumulate | (uint32_t)(i > 0));
+            multiply(to, g0 + (uint64_t)(i * 128), v0 + (uint64_t)(i * 128),
+                     accumulate | (uint32_t)(i > 0));
             if (a.ta > 1)
-              mma_16bit(to, g0 + (uint64_t)(i * 128 + (kGradBytes >> 4)), v0 + (uint64_t)(i * 128),
-                        kIdesc, 1);
+              multiply(to, g0 + (uint64_t)(i * 128 + (kGradBytes >> 4)), v0 + (uint64_t)(i * 128), 1);
             if (a.ta > 2)
-              mma_16bit(to, g0 + (uint64_t)(i * 128 + 2 * (kGradBytes >> 4)),
-                        v0 + (uint64_t)(i * 128), kIdesc, 1);
+              multiply(to, g0 + (uint64_t)(i * 128 + 2 * (kGradBytes >> 4)),
+                       v0 + (uint64_t)(i * 128), 1);
           }
           accumulate = 1;
-          mma_commit(bar.empty(s));
+          commit(bar.empty(s));
           ring.next(a.slots);
         }
         if (!ok) break;
-        mma_commit(bar.done(d));
+        commit(bar.done(d));
         acc.next(2);
       }
       if (!ok) {  // the products in flight end before the tensor memory is freed
-        mma_commit(bar.drained());
+        commit(bar.drained());
         mbar_wait(bar.drained(), 0);
       }
     }
@@ -234,8 +276,9 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
       if (j + 1 < a.width) to[j + 1] = sum[1];
     }
   } else if (warp >= kConvertWarp0) {
-    // a thread to 64 values of a row: neighbouring threads to neighbouring rows, whose
-    // pieces lie in different banks
+    // a thread to 64 values of a row (32 of a pair's): neighbouring threads to neighbouring
+    // rows, whose pieces lie in different banks
+    constexpr int kPieces = kPair ? 2 : 4;  // of 16 whole numbers
     const int t = tid - 32 * kConvertWarp0, half = t >> 6, r = t & 63;
     const auto scale_of = [&](int32_t k) {
       const int64_t row = (int64_t)k * kSlice + r;
@@ -252,15 +295,19 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
         break;
       }
       uint8_t* slot = smem + s * a.slot_bytes;
-      const uint8_t* from = slot + raw_off + r * kTile;
-      uint8_t* to = slot + value_off + half * kBox + r * 128;
+      const uint8_t* from = slot + raw_off + r * (kRawBytes / kSlice);
+      // a box of 64 values for each half, or one for both; behind them the second terms'
+      uint8_t* to = slot + value_off + (kPair ? 0 : half * kBox) + r * 128;
+      const int first = kPair ? 4 * half : 0;  // piece of 8 values of the box
       const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);  // exact: it has eight bits
-      uint4 w[4];
+      uint4 w[kPieces];
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        w[c] = *(const uint4*)(from + (((4 * half + c) ^ (r & 7)) << 4));
+      for (int c = 0; c < kPieces; ++c) {
+        const int piece = half * kPieces + c;  // as the TMA's swizzle of 64 or 128 bytes has it
+        w[c] = *(const uint4*)(from + ((piece ^ (kPair ? (r >> 1) & 3 : r & 7)) << 4));
+      }
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < kPieces; ++c) {
         uint2 hi[4], lo[4];
         int8_terms4(w[c].x, s2, hi[0], lo[0]);
         int8_terms4(w[c].y, s2, hi[1], lo[1]);
@@ -268,21 +315,23 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
         int8_terms4(w[c].w, s2, hi[3], lo[3]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int at = ((2 * c + h) ^ (r & 7)) << 4;
+          const int at = ((first + 2 * c + h) ^ (r & 7)) << 4;
           *(uint4*)(to + at) = make_uint4(hi[2 * h].x, hi[2 * h].y, hi[2 * h + 1].x, hi[2 * h + 1].y);
-          *(uint4*)(to + 2 * kBox + at) =
+          *(uint4*)(to + kValueBytes / 2 + at) =
               make_uint4(lo[2 * h].x, lo[2 * h].y, lo[2 * h + 1].x, lo[2 * h + 1].y);
         }
       }
       fence_async_proxy();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar.ready(s));
+      if (lane == 0) tell(bar.ready(s));
       ring.next(a.slots);
     }
   } else {
     constexpr int kHalf = kTile / 2;
+    // both terms' sums of 128 columns, or of a pair's first 64 and then of its second
+    constexpr int kTerms = kPair ? kHalf : kTile;  // from a column's first sum to its second
     const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) +
-                              (uint32_t)((warp >> 2) * kHalf);
+                              (uint32_t)((warp >> 2) * (kPair ? kTile : kHalf));
     float total[kHalf];
 #pragma unroll
     for (int e = 0; e < kHalf; ++e) total[e] = 0.f;
@@ -297,13 +346,13 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
 #pragma unroll
       for (int c = 0; c < 2 * kHalf; c += 32) {  // the leading bits' sums, then the rest's
         uint32_t v[32];
-        tmem_load32(lanes_at + (uint32_t)(d * 2 * kTile + c % kHalf + c / kHalf * kTile), v);
+        tmem_load32(lanes_at + (uint32_t)(d * 2 * kTile + c % kHalf + c / kHalf * kTerms), v);
 #pragma unroll
         for (int e = 0; e < 32; ++e) total[c % kHalf + e] += __uint_as_float(v[e]);
       }
       tcgen05_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar.taken(d));
+      if (lane == 0) tell(bar.taken(d));
       acc.next(2);
     }
     float4* to = (float4*)(a.partial + (split * tiles + tile) * kTileValues) + warp * 16 * 32;
@@ -315,9 +364,13 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
   if (!ok) op_flag(a.status, AGNES_OP_TIMEOUT);
   tcgen05_fence_before();
   __syncthreads();
+  if constexpr (kPair) cluster_sync();  // nobody arrives at or reads this CTA's any more
   if (warp == kMmaWarp) {
     tcgen05_fence_after();
-    tmem_free(tmem, kTmemCols);
+    if constexpr (kPair)
+      tmem_free_pair(tmem, kTmemCols);
+    else
+      tmem_free(tmem, kTmemCols);
   }
 }
 
@@ -372,14 +425,16 @@ join_kernel(const WeightArgs a) {
 // How the rows are shared out, and the workspace: partial tiles, partial biases, and the
 // gradient's terms where it cannot be taken as it is.
 struct WeightSpace {
+  bool pair;
   int64_t slices, tiles_j, tiles_i, splits, per_split, wpad, bias, grad, bytes;
   WeightSpace(int64_t rows, int64_t width, int64_t dim, int32_t dtype, bool direct) {
     slices = ceil_div(rows, kSlice);
-    tiles_j = ceil_div(width, kTile);
+    pair = width > kTile;
+    tiles_j = pair ? ceil_div(width, 2 * kTile) * 2 : 1;
     tiles_i = ceil_div(dim, kTile);
     wpad = ceil_div(width, 8) * 8;
     const int64_t tiles = tiles_j * tiles_i;
-    // one CTA to an SM: shares so that the last turn is as full as the others
+    // one CTA to an SM, or a pair to two: shares so that the last turn is as full as the others
     splits = 1;
     if (tiles > 0 && slices > 0) {
       double best = 0;
@@ -399,6 +454,7 @@ struct WeightSpace {
     bytes = rows > 0 && width > 0 ? grad + (direct ? 0 : grad_terms(dtype) * rows * wpad * 2) : 0;
   }
   void shape(WeightArgs& a) const {
+    a.pair = pair;
     a.slices = (int32_t)slices;
     a.tiles_j = (int32_t)tiles_j;
     a.tiles_i = (int32_t)tiles_i;
@@ -415,23 +471,24 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, i
   CUtensorMap grad_map, x_map;
   if (!map_rows(encode, &grad_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, grad, a.width, a.ta * a.rows,
                 grad_stride, 64, kSlice, CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !map_rows(encode, &x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.x, a.dim, a.rows, a.x_stride, kTile,
-                kSlice, CU_TENSOR_MAP_SWIZZLE_128B))
+      !map_rows(encode, &x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.x, a.dim, a.rows, a.x_stride,
+                a.pair ? kTile / 2 : kTile, kSlice,
+                a.pair ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
-  static OncePerDevice once;
-  cudaError_t e = once.run(device, [] {
-    return cudaFuncSetAttribute(weight_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                kSmemLimit);
+  const auto kernel = a.pair ? weight_kernel<true> : weight_kernel<false>;
+  static OncePerDevice once[2];
+  cudaError_t e = once[a.pair].run(device, [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
   });
   if (e != cudaSuccess) return e;
   a.chain = 8 / a.ta;
-  a.slot_bytes = a.ta * kGradBytes + kValueBytes + kRawBytes;
+  a.slot_bytes = a.ta * kGradBytes + value_bytes(a.pair) + raw_bytes(a.pair);
   const int slots = kRingBytes / a.slot_bytes;
   a.slots = slots < kMaxSlots ? slots : kMaxSlots;
   const size_t smem = (size_t)kSmemLimit - kRingBytes + (size_t)a.slots * a.slot_bytes;
   const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
-  e = launch_next(weight_kernel, dim3((unsigned)(tiles * a.splits)), (unsigned)kThreads, smem, st,
-                  grad_map, x_map, a);
+  e = launch_next_cluster(kernel, dim3((unsigned)(tiles * a.splits)), (unsigned)kThreads, smem,
+                          a.pair ? 2u : 1u, st, grad_map, x_map, a);
   if (e != cudaSuccess) return e;
   constexpr int kJoinThreads = 32 * kJoinQuads * kJoinShares;
   return launch_next(join_kernel<TOut>,

@@ -13,8 +13,8 @@
 //                     numbers as they are;
 //   the convert warps scale the whole numbers and write both terms;
 //   the MMA warp      issues the products into one of two accumulators, `chain` slices each;
-//   the epilogue warps add the accumulators up in registers and write a partial tile;
-//   the bias warps    add the gradient's columns up, of the first tile of columns.
+//   the epilogue warps add the accumulators up in registers and write a partial tile, and
+//                     meanwhile add the gradient's columns up, of the first tile of columns.
 // Tensor memory's sums are cut off, not rounded, after each product: over a hyperbatch's rows
 // in one chain that bias would reach 1e-5 of the result, so chains are short.  A second
 // kernel adds the shares' tiles up in order, so the result is the same each time.
@@ -32,8 +32,7 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kConvertWarp0 = kEpilogueWarps, kConvertWarps = 4;
 constexpr int kProducerWarp = kConvertWarp0 + kConvertWarps;
 constexpr int kMmaWarp = kProducerWarp + 1;
-constexpr int kBiasWarp0 = kMmaWarp + 1, kBiasWarps = 2;
-constexpr int kThreads = 32 * (kBiasWarp0 + kBiasWarps);
+constexpr int kThreads = 32 * (kMmaWarp + 1);
 constexpr int kBox = kSlice * 128;           // 64 columns of a slice in 16 bits
 constexpr int kGradBytes = 2 * kBox;         // a term of the gradient
 // Of the scaled whole numbers' two terms and of the whole numbers, for a CTA of its own or one
@@ -60,7 +59,7 @@ struct WeightArgs {
   int32_t splits, per_split;  // shares of the rows, slices of one
   int32_t chain;
   float* partial;             // [split][tile][kTileValues], as the threads hold them
-  float* bias_partial;        // [split][width], or null
+  float* bias_partial;        // [split][4][width], or null
   void* out;
   int64_t out_stride;
   float* dbias;
@@ -119,7 +118,7 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
     for (int s = 0; s < kMaxSlots; ++s) {
       mbar_init(bar.full(s), 1);
       mbar_init(bar.ready(s), kConvertWarps * kGroup);
-      mbar_init(bar.empty(s), 1 + (bias ? kBiasWarps : 0));
+      mbar_init(bar.empty(s), 1 + (bias ? kEpilogueWarps : 0));
     }
     for (int d = 0; d < 2; ++d) {
       mbar_init(bar.done(d), 1);
@@ -241,40 +240,6 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
         mbar_wait(bar.drained(), 0);
       }
     }
-  } else if (warp >= kBiasWarp0) {
-    if (bias) {
-      // two columns to a lane, in a row's 16-byte pieces as the TMA's swizzle has them
-      const int b = warp - kBiasWarp0, piece = lane >> 2, byte = (lane & 3) * 4;
-      float sum[2] = {0.f, 0.f};
-      for (int32_t k = k0; k < k1; ++k) {
-        const int s = ring.slot;
-        if (!__all_sync(0xffffffffu, mbar_wait(bar.full(s), ring.parity))) {
-          ok = false;
-          break;
-        }
-        const uint8_t* from = smem + s * a.slot_bytes + b * kBox;
-        const int64_t left = a.rows - (int64_t)k * kSlice;
-        const int n = left < kSlice ? (int)left : kSlice;
-        float part[2] = {0.f, 0.f};
-        for (int p = 0; p < a.ta; ++p)
-#pragma unroll 16
-          for (int r = 0; r < n; ++r) {
-            const uint32_t v = *(const uint32_t*)(from + p * kGradBytes + r * 128 +
-                                                  ((piece ^ (r & 7)) << 4) + byte);
-            part[0] += __uint_as_float(v << 16);
-            part[1] += __uint_as_float(v & 0xffff0000u);
-          }
-        sum[0] += part[0];
-        sum[1] += part[1];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar.empty(s));
-        ring.next(a.slots);
-      }
-      const int64_t j = j0 + b * 64 + lane * 2;
-      float* to = a.bias_partial + split * a.width;
-      if (j < a.width) to[j] = sum[0];
-      if (j + 1 < a.width) to[j + 1] = sum[1];
-    }
   } else if (warp >= kConvertWarp0) {
     // a thread to 64 values of a row (32 of a pair's): neighbouring threads to neighbouring
     // rows, whose pieces lie in different banks
@@ -335,8 +300,38 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
     float total[kHalf];
 #pragma unroll
     for (int e = 0; e < kHalf; ++e) total[e] = 0.f;
+    // of the bias, a warp has two columns to a lane and a quarter of a slice's rows
+    float column[2] = {0.f, 0.f};
+    const int box = warp & 1, rows0 = (warp >> 1) * (kSlice / 4);
     Ring acc;
-    for (int32_t c0 = k0; c0 < k1; c0 += a.chain) {
+    for (int32_t c0 = k0; ok && c0 < k1; c0 += a.chain) {
+      if (bias) {
+        for (int32_t k = c0; k < min(c0 + a.chain, k1); ++k) {
+          const int s = ring.slot;
+          if (!__all_sync(0xffffffffu, mbar_wait(bar.full(s), ring.parity))) {
+            ok = false;
+            break;
+          }
+          // a row's 16-byte pieces as the TMA's swizzle has them; rows past the last are zeros,
+          // or the next term's, which only ever follow terms of their own
+          const uint8_t* from = smem + s * a.slot_bytes + box * kBox + (lane & 3) * 4;
+          const int64_t left = a.rows - (int64_t)k * kSlice - rows0;
+          for (int p = 0; p < a.ta; ++p)
+#pragma unroll
+            for (int r = 0; r < kSlice / 4; ++r) {
+              const uint32_t v = *(const uint32_t*)(from + p * kGradBytes + (rows0 + r) * 128 +
+                                                    (((lane >> 2) ^ (r & 7)) << 4));
+              if (r < left) {
+                column[0] += __uint_as_float(v << 16);
+                column[1] += __uint_as_float(v & 0xffff0000u);
+              }
+            }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar.empty(s));
+          ring.next(a.slots);
+        }
+        if (!ok) break;
+      }
       const int d = acc.slot;
       if (!__all_sync(0xffffffffu, mbar_wait(bar.done(d), acc.parity))) {
         ok = false;
@@ -360,6 +355,12 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
     for (int c = 0; c < kHalf / 4; ++c)
       to[c * 32 + lane] = make_float4(total[4 * c], total[4 * c + 1], total[4 * c + 2],
                                       total[4 * c + 3]);
+    if (bias) {  // four quarters' sums of a column, added up with the shares'
+      const int64_t j = j0 + box * 64 + lane * 2;
+      float* to_bias = a.bias_partial + (split * 4 + (warp >> 1)) * a.width;
+      if (j < a.width) to_bias[j] = column[0];
+      if (j + 1 < a.width) to_bias[j + 1] = column[1];
+    }
   }
   if (!ok) op_flag(a.status, AGNES_OP_TIMEOUT);
   tcgen05_fence_before();
@@ -374,50 +375,54 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
   }
 }
 
-// The shares' tiles added up: 32 rows x 16 columns of a tile to a CTA, their shares dealt
-// out to kJoinShares threads each, whose sums are added in order.  The CTAs behind the
-// tiles' have the bias.
-constexpr int kJoinShares = 4;
-constexpr int kJoinQuads = 4;  // groups of four columns
-template <typename TOut>
-__global__ void __launch_bounds__(32 * kJoinQuads * kJoinShares)
+// The shares' tiles added up: 32 rows of 64 / kDeal columns of a tile to a CTA, each value's
+// shares dealt out to kDeal threads, whose sums are added in order.  The CTAs behind the tiles'
+// have the bias.
+constexpr int kJoinThreads = 512;
+template <typename TOut, int kDeal>
+__global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const WeightArgs a) {
   grid_dep_wait();
-  __shared__ float4 sums[kJoinShares][kJoinQuads][32];
-  if (blockIdx.x >= a.tiles_j * a.tiles_i * 32) {
-    const int64_t j = (int64_t)(blockIdx.x - a.tiles_j * a.tiles_i * 32) * blockDim.x + threadIdx.x;
+  constexpr int kQuads = 16 / kDeal, kParts = 8 * kDeal;  // of four columns; CTAs to a tile
+  constexpr int kCols = 4 * kQuads;
+  __shared__ float4 sums[kDeal][kQuads][33];
+  const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
+  if (blockIdx.x >= tiles * kParts) {
+    const int64_t j = (blockIdx.x - tiles * kParts) * kJoinThreads + threadIdx.x;
     if (j >= a.width) return;
     float sum = 0.f;
 #pragma unroll 8
-    for (int s = 0; s < a.splits; ++s) sum += a.bias_partial[(int64_t)s * a.width + j];
+    for (int s = 0; s < 4 * a.splits; ++s) sum += a.bias_partial[(int64_t)s * a.width + j];
     a.dbias[j] = sum;
     return;
   }
-  const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) % kJoinQuads;
-  const int share = (threadIdx.x >> 5) / kJoinQuads;
-  const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
-  const int64_t tile = blockIdx.x / 32;
-  const int part = blockIdx.x % 32, warp = part / 4, c = part % 4 * kJoinQuads + quad;
+  const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) % kQuads;
+  const int deal = (threadIdx.x >> 5) / kQuads;
+  const int64_t tile = blockIdx.x / kParts;
+  const int part = blockIdx.x % kParts, warp = part / kDeal, c = part % kDeal * kQuads + quad;
   const float4* from = (const float4*)(a.partial + tile * kTileValues) + (warp * 16 + c) * 32 + lane;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int s = share; s < a.splits; s += kJoinShares) {
+  for (int s = deal; s < a.splits; s += kDeal) {
     const float4 p = from[(int64_t)s * tiles * (kTileValues / 4)];
     v.x += p.x;
     v.y += p.y;
     v.z += p.z;
     v.w += p.w;
   }
-  sums[share][quad][lane] = v;
+  sums[deal][quad][lane] = v;
   __syncthreads();
-  // a row's 16 columns to neighbouring threads
-  const int t = threadIdx.x;
-  const int64_t j = tile / a.tiles_i * kTile + (warp & 3) * 32 + t / 16;
-  const int32_t i = (int32_t)(tile % a.tiles_i) * kTile + (warp >> 2) * 64 + part % 4 * 16 + t % 16;
-  if (j < a.width && i < a.dim) {
+  // a row's columns to neighbouring threads
+#pragma unroll
+  for (int t = threadIdx.x; t < 32 * kCols; t += kJoinThreads) {
+    const int r = t / kCols, i_in = t % kCols;
+    const int64_t j = tile / a.tiles_i * kTile + (warp & 3) * 32 + r;
+    const int32_t i = (int32_t)(tile % a.tiles_i) * kTile + (warp >> 2) * 64 +
+                      part % kDeal * kCols + i_in;
+    if (j >= a.width || i >= a.dim) continue;
     float sum = 0.f;
 #pragma unroll
-    for (int s = 0; s < kJoinShares; ++s) sum += ((const float*)&sums[s][t % 16 / 4][t / 16])[t % 4];
+    for (int s = 0; s < kDeal; ++s) sum += ((const float*)&sums[s][i_in / 4][r])[i_in % 4];
     ((TOut*)a.out)[j * a.out_stride + i] = from_f32<TOut>(sum);
   }
 }
@@ -450,7 +455,7 @@ struct WeightSpace {
     }
     per_split = slices ? ceil_div(slices, splits) : 0;
     bias = ceil_div(splits * tiles * kTileValues * 4, 256) * 256;
-    grad = bias + ceil_div(splits * width * 4, 256) * 256;
+    grad = bias + ceil_div(splits * width * 16, 256) * 256;
     bytes = rows > 0 && width > 0 ? grad + (direct ? 0 : grad_terms(dtype) * rows * wpad * 2) : 0;
   }
   void shape(WeightArgs& a) const {
@@ -490,9 +495,10 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, i
   e = launch_next_cluster(kernel, dim3((unsigned)(tiles * a.splits)), (unsigned)kThreads, smem,
                           a.pair ? 2u : 1u, st, grad_map, x_map, a);
   if (e != cudaSuccess) return e;
-  constexpr int kJoinThreads = 32 * kJoinQuads * kJoinShares;
-  return launch_next(join_kernel<TOut>,
-                     dim3((unsigned)(tiles * 32 + (a.dbias ? ceil_div(a.width, kJoinThreads) : 0))),
+  // few shares: more values to a CTA; many: more threads to a value
+  const bool few = a.splits <= 8;
+  const int64_t ctas = tiles * (few ? 8 : 32) + (a.dbias ? ceil_div(a.width, kJoinThreads) : 0);
+  return launch_next(few ? join_kernel<TOut, 1> : join_kernel<TOut, 4>, dim3((unsigned)ctas),
                      (unsigned)kJoinThreads, 0, st, a);
 }
 

@@ -24,6 +24,7 @@ struct KeepArgs {
   int64_t out_stride;
   uint8_t* kept;     // may be null
   int64_t kept_stride;
+  int32_t in_bytes, out_bytes;  // of the shared memory for what a CTA reads and writes
 };
 
 // The normal distribution function and its density at v, for results of 16 bits:
@@ -90,8 +91,10 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 // What is made of a row: 8-bit rows alone, a nonlinearity, or a gated one.
 enum { kRound, kPlain, kGated };
 
-template <typename T, int kMode, bool kOut8, int kVec, bool kLoop>
-__global__ void __launch_bounds__(kLanes, kVec == 1 ? 1 : 2)
+// kVec = 1: single elements, and without kLoop from and to shared memory (stage_in), where the
+// matrices are contiguous.
+template <typename T, int kMode, bool kOut8, int kVec, bool kLoop, bool kStaged>
+__global__ void __launch_bounds__(kLanes, kVec == 1 && !kStaged ? 1 : 2)
 keep_kernel(const KeepArgs a) {
   constexpr int kPer = kElems / kVec;
   constexpr bool kFit = sizeof(T) == 2;
@@ -105,6 +108,35 @@ keep_kernel(const KeepArgs a) {
   const bool keep = kMode == kRound || a.kept;
   uint8_t* to8 = (uint8_t*)a.out + row * a.out_stride;
   T* to = (T*)a.out + row * a.out_stride;
+  uint8_t* kept = a.kept + row * a.kept_stride;
+  // a CTA's rows: what it reads, its values and what it keeps
+  extern __shared__ uint4 staged[];
+  uint8_t* const in_stage = (uint8_t*)staged;
+  uint8_t* const out_stage = in_stage + a.in_bytes;
+  uint8_t* const kept_stage = out_stage + a.out_bytes;
+  const int64_t row0 = row - group, left = a.rows - row0;
+  const int n = (int)(left < a.groups ? left : a.groups);
+  if constexpr (kStaged) {
+    const T* from = (const T*)a.x + row0 * a.stride;
+    stage_in(in_stage, from, n * a.stride * (int64_t)sizeof(T), a.x,
+             (const T*)a.x + a.rows * a.stride);
+    x = (const T*)(in_stage + stage_offset(from)) + group * a.stride;
+    to = (T*)(out_stage + stage_offset((T*)a.out + row0 * a.out_stride)) + group * a.out_stride;
+    to8 = out_stage + group * a.out_stride;
+    kept = kept_stage + group * a.kept_stride;
+    stage_wait();
+  }
+  const auto finish = [&] {
+    if constexpr (kStaged) {
+      __syncthreads();
+      if (kMode != kRound && kOut8)
+        stage_out(out_stage, (uint8_t*)a.out + row0 * a.out_stride, n * a.out_stride);
+      else if (kMode != kRound)
+        stage_out(out_stage, (T*)a.out + row0 * a.out_stride,
+                  n * a.out_stride * (int64_t)sizeof(T));
+      if (keep) stage_out(kept_stage, a.kept + row0 * a.kept_stride, n * a.kept_stride);
+    }
+  };
   RowRegs<T, kVec, kPer> v, u;
   float y[kOut8 ? kElems : 1];
   uint32_t top[3] = {0, 0, 0};
@@ -122,6 +154,7 @@ keep_kernel(const KeepArgs a) {
       with_kind(a.f, [&](auto kind) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
+          if (part.beyond(i)) break;
           float f[kVec], g[kVec];
           v.get(i, f);
           if constexpr (kMode == kGated) u.get(i, g);
@@ -139,7 +172,10 @@ keep_kernel(const KeepArgs a) {
       });
     }
   }
-  if (!keep && !kOut8) return;
+  if (!keep && !kOut8) {
+    finish();
+    return;
+  }
   v.pin();
   if constexpr (kMode == kGated) u.pin();
   Int8Scale s = {}, s_gate = {}, s_out = {};
@@ -153,7 +189,6 @@ keep_kernel(const KeepArgs a) {
     if constexpr (kMode == kGated) s_gate = int8_scale(top[1]);
     if constexpr (kOut8) s_out = int8_scale(top[2]);
   }
-  uint8_t* kept = a.kept + row * a.kept_stride;
   const int64_t half = int8_row_bytes(a.dim);
   for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
     const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
@@ -163,15 +198,21 @@ keep_kernel(const KeepArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      float f[kVec], g[kVec];
+      if (part.beyond(i)) break;
+      float f[kVec];
       v.get(i, f);
-      if constexpr (kMode == kGated) u.get(i, g);
       if (keep) {
         int8_store(part, kept + c0, valid, i, f, s);
-        if constexpr (kMode == kGated) int8_store(part, kept + half + c0, valid, i, g, s_gate);
+        if constexpr (kMode == kGated) {
+          float g[kVec];
+          u.get(i, g);
+          int8_store(part, kept + half + c0, valid, i, g, s_gate);
+        }
       }
       if constexpr (kOut8) {
         if (kLoop) {
+          float g[kVec];
+          if constexpr (kMode == kGated) u.get(i, g);
           with_kind(a.f, [&](auto kind) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
@@ -192,6 +233,7 @@ keep_kernel(const KeepArgs a) {
       int8_store_end(kept + half, a.dim, lane, a.lanes, valid, s_gate);
   }
   if constexpr (kOut8) int8_store_end(to8, a.dim, lane, a.lanes, valid, s_out);
+  finish();
 }
 
 struct BackArgs {
@@ -203,6 +245,7 @@ struct BackArgs {
   int64_t grad_stride;
   void* out;
   int64_t out_stride;
+  int32_t kept_bytes, grad_bytes;  // of shared memory, where a CTA's rows are there
 };
 
 // The largest number of a type: a value past it is that (the row's scale was rounded up).
@@ -221,23 +264,67 @@ __device__ __forceinline__ float most_of<__nv_bfloat16>() {
   return 3.3895313892515355e38f;
 }
 
-// What 8-bit rows stand for.
-template <typename T, int kVec>
+// A CTA's rows of the kept values, of the gradient and of the output in shared memory.
+template <typename TGrad, typename T>
+struct BackStage {
+  const BackArgs& a;
+  uint8_t* base;
+  int64_t row0;
+  int n;
+  __device__ BackStage(const BackArgs& args, uint8_t* shared) : a(args), base(shared) {
+    row0 = (int64_t)blockIdx.x * a.groups;
+    const int64_t left = a.rows - row0;
+    n = (int)(left < a.groups ? left : a.groups);
+  }
+  __device__ uint8_t* kept() const { return base; }
+  __device__ uint8_t* grad_base() const { return base + a.kept_bytes; }
+  __device__ uint8_t* out_base() const { return grad_base() + a.grad_bytes; }
+  __device__ const TGrad* grad_from() const { return (const TGrad*)a.grad + row0 * a.grad_stride; }
+  __device__ T* out_to() const { return (T*)a.out + row0 * a.out_stride; }
+  __device__ void load(bool with_grad) const {
+    stage_in(kept(), a.kept + row0 * a.kept_stride, n * a.kept_stride, a.kept,
+             a.kept + a.rows * a.kept_stride);
+    if (with_grad)
+      stage_in(grad_base(), grad_from(), n * a.grad_stride * (int64_t)sizeof(TGrad), a.grad,
+               (const TGrad*)a.grad + a.rows * a.grad_stride);
+    stage_wait();
+  }
+  __device__ const TGrad* grad() const {
+    return (const TGrad*)(grad_base() + stage_offset(grad_from()));
+  }
+  __device__ T* out() const { return (T*)(out_base() + stage_offset(out_to())); }
+  __device__ void store() const {
+    __syncthreads();
+    stage_out(out_base(), out_to(), n * a.out_stride * (int64_t)sizeof(T));
+  }
+};
+
+// What 8-bit rows stand for.  kStaged: single elements (kVec = 1) through shared memory.
+template <typename T, int kVec, bool kStaged>
 __global__ void __launch_bounds__(kBackLanes, kVec == 1 ? 4 : 8)
 values_kernel(const BackArgs a) {
   constexpr int kPer = kElems / kVec;
+  extern __shared__ uint4 staged[];
   const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
   const int64_t row = (int64_t)blockIdx.x * a.groups + group;
-  if (row >= a.rows) return;
+  const BackStage<T, T> stage(a, (uint8_t*)staged);
+  const bool valid = row < a.rows;
+  if (!kStaged && !valid) return;
   const uint8_t* kept = a.kept + row * a.kept_stride;
-  const float scale = *(const float*)(kept + int8_row_bytes(a.dim) - 4);
   T* out = (T*)a.out + row * a.out_stride;
-  for (int32_t c0 = 0; c0 < a.dim; c0 += a.lanes * kElems) {
+  if constexpr (kStaged) {
+    stage.load(false);
+    kept = stage.kept() + group * a.kept_stride;
+    out = stage.out() + group * a.out_stride;
+  }
+  const float scale = valid ? *(const float*)(kept + int8_row_bytes(a.dim) - 4) : 0.f;
+  for (int32_t c0 = 0; valid && c0 < a.dim; c0 += a.lanes * kElems) {
     const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
     Int8Regs<kVec, kPer> v;
     v.load(part, kept + c0, true);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+      if (part.beyond(i)) break;
       float f[kVec];
       v.get(i, f);
 #pragma unroll
@@ -248,24 +335,34 @@ values_kernel(const BackArgs a) {
       part.store_one(out + c0, true, i, f);
     }
   }
+  if constexpr (kStaged) stage.store();
 }
 
 // The nonlinearity's gradient at them.
-template <typename TGrad, typename T, bool kGate, int kVec>
+template <typename TGrad, typename T, bool kGate, int kVec, bool kStaged>
 __global__ void __launch_bounds__(kBackLanes, kVec == 1 ? 2 : 4)
 back_kernel(const BackArgs a) {
   constexpr int kPer = kElems / kVec;
   constexpr bool kFit = sizeof(T) == 2;
+  extern __shared__ uint4 staged[];
   const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
   const int64_t row = (int64_t)blockIdx.x * a.groups + group;
-  if (row >= a.rows) return;
+  const BackStage<TGrad, T> stage(a, (uint8_t*)staged);
+  const bool valid = row < a.rows;
+  if (!kStaged && !valid) return;
   const uint8_t* kept = a.kept + row * a.kept_stride;
-  const int64_t half = int8_row_bytes(a.dim);
-  const float s0 = *(const float*)(kept + half - 4);
-  const float s1 = kGate ? *(const float*)(kept + 2 * half - 4) : 0.f;
   T* out = (T*)a.out + row * a.out_stride;
   const TGrad* grad = (const TGrad*)a.grad + row * a.grad_stride;
-  for (int32_t c0 = 0; c0 < a.dim; c0 += a.lanes * kElems) {
+  if constexpr (kStaged) {
+    stage.load(true);
+    kept = stage.kept() + group * a.kept_stride;
+    out = stage.out() + group * a.out_stride;
+    grad = stage.grad() + group * a.grad_stride;
+  }
+  const int64_t half = int8_row_bytes(a.dim);
+  const float s0 = valid ? *(const float*)(kept + half - 4) : 0.f;
+  const float s1 = valid && kGate ? *(const float*)(kept + 2 * half - 4) : 0.f;
+  for (int32_t c0 = 0; valid && c0 < a.dim; c0 += a.lanes * kElems) {
     const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
     Int8Regs<kVec, kPer> v, u;
     RowRegs<TGrad, kVec, kPer> d;
@@ -275,6 +372,7 @@ back_kernel(const BackArgs a) {
     with_kind(a.f, [&](auto kind) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
+        if (part.beyond(i)) break;
         float f[kVec], g[kVec], h[kVec];
         v.get(i, f);
         d.get(i, h);
@@ -294,6 +392,7 @@ back_kernel(const BackArgs a) {
       }
     });
   }
+  if constexpr (kStaged) stage.store();
 }
 
 // The elements of an access for rows of dim values that start at p and every stride after
@@ -328,7 +427,7 @@ agnes_status check_kept(const char* op, const char* name, int64_t rows, int64_t 
 }
 
 template <typename T, int kMode, bool kOut8>
-cudaError_t launch_keep(KeepArgs a, cudaStream_t st) {
+cudaError_t launch_keep(KeepArgs a, int device, cudaStream_t st) {
   const int64_t next = a.rows > 1 ? 1 : 0;  // a single row has no next one
   const bool aligned =
       aligned_rows(a.x, next * a.stride * (int64_t)sizeof(T), 16) &&
@@ -338,18 +437,44 @@ cudaError_t launch_keep(KeepArgs a, cudaStream_t st) {
   a.lanes = shape.lanes;
   a.log_lanes = shape.log_lanes;
   a.groups = shape.groups;
-  const bool loop = a.dim > a.lanes * kElems;
-  const auto kernel = vec_of(a.dim, aligned) == 8 ? (loop ? keep_kernel<T, kMode, kOut8, 8, true>
-                                                          : keep_kernel<T, kMode, kOut8, 8, false>)
-                                                  : (loop ? keep_kernel<T, kMode, kOut8, 1, true>
-                                                          : keep_kernel<T, kMode, kOut8, 1, false>);
-  kernel<<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), 0, st>>>(a);
+  const bool loop = a.dim > a.lanes * kElems, wide = vec_of(a.dim, aligned) == 8;
+  const int64_t cols = kMode == kGated ? 2 * (int64_t)a.dim : a.dim;
+  const int64_t kept_row = int8_row_bytes(a.dim) * (kMode == kGated ? 2 : 1);
+  const bool staged = !wide && !loop && (!next || a.stride == cols) &&
+                      (kMode == kRound || !next ||
+                       a.out_stride == (kOut8 ? int8_row_bytes(a.dim) : a.dim)) &&
+                      (!a.kept || !next || a.kept_stride == kept_row);
+  size_t smem = 0;
+  if (staged) {
+    if (!next) {
+      a.stride = cols;
+      a.out_stride = kOut8 ? int8_row_bytes(a.dim) : a.dim;
+      a.kept_stride = kept_row;
+    }
+    a.in_bytes = (int32_t)staged_bytes(a.groups * cols * (int64_t)sizeof(T));
+    a.out_bytes = kMode == kRound ? 0
+                  : (int32_t)staged_bytes(a.groups * a.out_stride * (kOut8 ? 1 : (int64_t)sizeof(T)));
+    smem = (size_t)a.in_bytes + a.out_bytes + (a.kept ? a.groups * kept_row : 0);
+  }
+  const auto kernel = wide     ? (loop ? keep_kernel<T, kMode, kOut8, 8, true, false>
+                                       : keep_kernel<T, kMode, kOut8, 8, false, false>)
+                      : staged ? keep_kernel<T, kMode, kOut8, 1, false, true>
+                      : loop   ? keep_kernel<T, kMode, kOut8, 1, true, false>
+                               : keep_kernel<T, kMode, kOut8, 1, false, false>;
+  if (smem > 48 * 1024) {
+    static OncePerDevice once;
+    const cudaError_t e = once.run(device, [&] {
+      return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
+    });
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), smem, st>>>(a);
   return cudaGetLastError();
 }
 
-// kernels[0] for vectors, [1] for single elements
+// kernels[0] for vectors, [1] for single elements, [2] for those through shared memory
 using BackKernel = void (*)(BackArgs);
-cudaError_t launch_back(const BackKernel (&kernels)[2], BackArgs a, int64_t grad_size,
+cudaError_t launch_back(const BackKernel (&kernels)[3], BackArgs a, int halves, int64_t grad_size,
                         int64_t size, cudaStream_t st) {
   const int64_t next = a.rows > 1 ? 1 : 0;
   const bool aligned = aligned_rows(a.out, next * a.out_stride * size, 16) &&
@@ -358,8 +483,26 @@ cudaError_t launch_back(const BackKernel (&kernels)[2], BackArgs a, int64_t grad
   a.lanes = shape.lanes;
   a.log_lanes = shape.log_lanes;
   a.groups = shape.groups;
-  kernels[vec_of(a.dim, aligned) == 8 ? 0 : 1]
-      <<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), 0, st>>>(a);
+  const int64_t kept_row = halves * int8_row_bytes(a.dim);
+  const bool staged = a.dim <= a.lanes * kElems &&
+                      (!next || (a.kept_stride == kept_row && a.out_stride == halves * a.dim &&
+                                 (!a.grad || a.grad_stride == a.dim)));
+  const int which = vec_of(a.dim, aligned) == 8 ? 0 : staged ? 2 : 1;
+  size_t smem = 0;
+  if (which == 2) {
+    a.kept_stride = kept_row;
+    a.out_stride = halves * a.dim;
+    a.grad_stride = a.dim;
+    a.kept_bytes = (int32_t)staged_bytes(a.groups * kept_row);
+    a.grad_bytes = a.grad ? (int32_t)staged_bytes(a.groups * a.dim * grad_size) : 0;
+    smem = (size_t)a.kept_bytes + a.grad_bytes + staged_bytes(a.groups * halves * a.dim * size);
+    if (smem > 48 * 1024) {  // gated rows in fp32
+      const cudaError_t e = cudaFuncSetAttribute(
+          kernels[which], cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
+      if (e != cudaSuccess) return e;
+    }
+  }
+  kernels[which]<<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), smem, st>>>(a);
   return cudaGetLastError();
 }
 
@@ -414,7 +557,7 @@ agnes_status agnes_int8_quantize(const void* x, int32_t dtype, int64_t stride, i
   a.kept = (uint8_t*)out;
   a.kept_stride = out_stride;
   return op_launched(op, with_float_type(dtype, [&](auto t) {
-    return launch_keep<typename decltype(t)::type, kRound, false>(a, (cudaStream_t)cuda_stream);
+    return launch_keep<typename decltype(t)::type, kRound, false>(a, device, (cudaStream_t)cuda_stream);
   }));
 }
 
@@ -443,8 +586,9 @@ agnes_status agnes_int8_dequantize(const void* x, int64_t stride, int64_t rows, 
   a.out_stride = out_stride;
   return op_launched(op, with_float_type(dtype, [&](auto t) {
     using T = typename decltype(t)::type;
-    const BackKernel kernels[2] = {values_kernel<T, 8>, values_kernel<T, 1>};
-    return launch_back(kernels, a, 0, sizeof(T), (cudaStream_t)cuda_stream);
+    const BackKernel kernels[3] = {values_kernel<T, 8, false>, values_kernel<T, 1, false>,
+                                   values_kernel<T, 1, true>};
+    return launch_back(kernels, a, 1, 0, sizeof(T), (cudaStream_t)cuda_stream);
   }));
 }
 
@@ -492,8 +636,8 @@ agnes_status agnes_activation(const void* x, int32_t dtype, int64_t stride, int6
     using T = typename decltype(t)::type;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     if (out_dtype == AGNES_INT8_ROWS)
-      return gated ? launch_keep<T, kGated, true>(a, st) : launch_keep<T, kPlain, true>(a, st);
-    return gated ? launch_keep<T, kGated, false>(a, st) : launch_keep<T, kPlain, false>(a, st);
+      return gated ? launch_keep<T, kGated, true>(a, device, st) : launch_keep<T, kPlain, true>(a, device, st);
+    return gated ? launch_keep<T, kGated, false>(a, device, st) : launch_keep<T, kPlain, false>(a, device, st);
   }));
 }
 
@@ -534,10 +678,13 @@ agnes_status agnes_activation_grad(const void* grad, int32_t grad_dtype, int64_t
     using TGrad = typename decltype(t)::type;
     return with_float_type(out_dtype, [&](auto o) {
       using T = typename decltype(o)::type;
-      const BackKernel kernels[2][2] = {
-          {back_kernel<TGrad, T, false, 8>, back_kernel<TGrad, T, false, 1>},
-          {back_kernel<TGrad, T, true, 8>, back_kernel<TGrad, T, true, 1>}};
-      return launch_back(kernels[gated], a, sizeof(TGrad), sizeof(T), (cudaStream_t)cuda_stream);
+      const BackKernel kernels[2][3] = {
+          {back_kernel<TGrad, T, false, 8, false>, back_kernel<TGrad, T, false, 1, false>,
+           back_kernel<TGrad, T, false, 1, true>},
+          {back_kernel<TGrad, T, true, 8, false>, back_kernel<TGrad, T, true, 1, false>,
+           back_kernel<TGrad, T, true, 1, true>}};
+      return launch_back(kernels[gated], a, halves, sizeof(TGrad), sizeof(T),
+                         (cudaStream_t)cuda_stream);
     });
   }));
 }

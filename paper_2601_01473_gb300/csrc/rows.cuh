@@ -90,6 +90,9 @@ struct RowPart {
   __device__ void store_one(T* row, bool valid, int i, const float* v) const {
     if (valid && col(i) < dim) store_vec<T, kVec>(row + col(i), v);
   }
+  // Whether no thread has anything of vector i on: for single elements, of which a row rarely
+  // fills all that a thread could take.
+  __device__ bool beyond(int i) const { return kVec == 1 && i * lanes >= dim; }
   // elements past the end hold zeros or what a row's arithmetic made of them
   __device__ bool has(int i) const { return col(i) < dim; }
 };
@@ -177,6 +180,54 @@ struct RowRegs<T, 1, kPer> {
   }
   __device__ void pin() {}
 };
+
+// Rows that no vector divides, of a contiguous matrix: a CTA's rows are one run of memory, which
+// goes through shared memory in 16-byte pieces.  A run keeps its place within a piece there, so
+// pieces lie as in memory.  (Single elements from and to memory keep 16 KB of an SM's loads on
+// their way at most.)
+constexpr int64_t staged_bytes(int64_t bytes) { return (bytes + 15) / 16 * 16 + 16; }
+
+// Where a run that starts at p has its first byte in its buffer.
+__device__ __forceinline__ int stage_offset(const void* p) { return (int)((uintptr_t)p & 15); }
+
+// Starts the copies of `bytes` from p on to `buffer` (16-byte aligned); only [lo, hi) is read.
+// stage_wait() ends them, for the whole CTA.
+__device__ __forceinline__ void stage_in(uint8_t* buffer, const void* p, int64_t bytes,
+                                         const void* lo, const void* hi) {
+  const uint8_t* first = (const uint8_t*)p - stage_offset(p);
+  const int pieces = (int)((bytes + stage_offset(p) + 15) / 16);
+  for (int i = threadIdx.x; i < pieces; i += blockDim.x) {
+    const uint8_t* at = first + (int64_t)i * 16;
+    uint8_t* to = buffer + i * 16;
+    if (at >= (const uint8_t*)lo && at + 16 <= (const uint8_t*)hi) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                       (uint32_t)__cvta_generic_to_shared(to)),
+                   "l"(at)
+                   : "memory");
+    } else {
+      for (int b = 0; b < 16; ++b)
+        if (at + b >= (const uint8_t*)lo && at + b < (const uint8_t*)hi) to[b] = at[b];
+    }
+  }
+}
+__device__ __forceinline__ void stage_wait() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+}
+
+// A run of `bytes` from `buffer` to p on, after a barrier.
+__device__ __forceinline__ void stage_out(const uint8_t* buffer, void* p, int64_t bytes) {
+  const int offset = stage_offset(p), end = (int)(bytes + offset);
+  uint8_t* first = (uint8_t*)p - offset;
+  for (int i = threadIdx.x; i * 16 < end; i += blockDim.x) {
+    if (i * 16 >= offset && i * 16 + 16 <= end) {
+      ((uint4*)first)[i] = ((const uint4*)buffer)[i];
+    } else {
+      for (int b = i * 16; b < i * 16 + 16; ++b)
+        if (b >= offset && b < end) first[b] = buffer[b];
+    }
+  }
+}
 
 struct SumOp {
   using type = float;

@@ -387,12 +387,19 @@ join_kernel(const WeightArgs a) {
   constexpr int kCols = 4 * kQuads;
   __shared__ float4 sums[kDeal][kQuads][33];
   const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
-  if (blockIdx.x >= tiles * kParts) {
-    const int64_t j = (blockIdx.x - tiles * kParts) * kJoinThreads + threadIdx.x;
-    if (j >= a.width) return;
+  if (blockIdx.x >= tiles * kParts) {  // 32 columns, their shares dealt out to the warps
+    float* part_sums = (float*)sums;
+    const int64_t j = (blockIdx.x - tiles * kParts) * 32 + (threadIdx.x & 31);
     float sum = 0.f;
-#pragma unroll 8
-    for (int s = 0; s < 4 * a.splits; ++s) sum += a.bias_partial[(int64_t)s * a.width + j];
+    if (j < a.width) {
+#pragma unroll 4
+      for (int s = threadIdx.x >> 5; s < 4 * a.splits; s += kJoinThreads / 32)
+        sum += a.bias_partial[(int64_t)s * a.width + j];
+    }
+    part_sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32 || j >= a.width) return;
+    for (int w = 1; w < kJoinThreads / 32; ++w) sum += part_sums[w * 32 + threadIdx.x];
     a.dbias[j] = sum;
     return;
   }
@@ -486,7 +493,7 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, i
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
   });
   if (e != cudaSuccess) return e;
-  a.chain = 8 / a.ta;
+  a.chain = a.ta == 1 ? 5 : a.ta == 2 ? 2 : 1;  // some 16 to 20 products of 16
   a.slot_bytes = a.ta * kGradBytes + value_bytes(a.pair) + raw_bytes(a.pair);
   const int slots = kRingBytes / a.slot_bytes;
   a.slots = slots < kMaxSlots ? slots : kMaxSlots;
@@ -497,7 +504,7 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, i
   if (e != cudaSuccess) return e;
   // few shares: more values to a CTA; many: more threads to a value
   const bool few = a.splits <= 8;
-  const int64_t ctas = tiles * (few ? 8 : 32) + (a.dbias ? ceil_div(a.width, kJoinThreads) : 0);
+  const int64_t ctas = tiles * (few ? 8 : 32) + (a.dbias ? ceil_div(a.width, 32) : 0);
   return launch_next(few ? join_kernel<TOut, 1> : join_kernel<TOut, 4>, dim3((unsigned)ctas),
                      (unsigned)kJoinThreads, 0, st, a);
 }

@@ -916,8 +916,10 @@ cudaError_t launch_linear(const LinearArgs& l, void* workspace, int32_t* status,
   a.out_stride = l.out_stride;
   a.status = status;
   const TileOperands o = {l.x, w, l.x_stride, space.kpad * 2, l.dim};
-  // 16-bit outputs keep nothing of what a chain of 32,768 products loses
-  const bool drain = l.dim > (sizeof(TOut) == 4 ? 1024 : 32768);
+  // Whole sums are exact up to 2^24, that of 1040 of the largest products; beyond, a product of
+  // 16 loses 2^-23 of the sum at most, so 2048 columns lose 8e-6 where all values are the
+  // largest, and nothing else.  16-bit outputs keep nothing of what 32,768 lose.
+  const bool drain = l.dim > (sizeof(TOut) == 4 ? 2048 : 32768);
   return launch_product<TOut, true>(a, o, drain, device, st);
 }
 
@@ -1103,10 +1105,10 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
   a.status = status;
   return op_launched(op, with_float_type(out_dtype, [&](auto t) {
     using TOut = typename decltype(t)::type;
-    // some 48 products of 16 to an accumulator where the sum stays in fp32; 16-bit outputs
-    // keep nothing of what a chain of some thousand loses
+    // some 20 products of 16 to an accumulator where the sum stays in fp32, which loses some 5e-7
+    // of it (40 lost 1e-6); 16-bit outputs keep nothing of what a chain of some thousand loses
     const int per_slice = 4 * (a.ta == 1 ? 2 : a.ta == 2 ? 4 : 5);
-    a.chain = 48 / per_slice > 0 ? 48 / per_slice : 1;
+    a.chain = 24 / per_slice > 0 ? 24 / per_slice : 1;
     const bool drain = sizeof(TOut) == 4 || width > 16384;
     return launch_product<TOut, false>(a, o, drain, device, st);
   }));

@@ -24,6 +24,7 @@ struct KeepArgs {
   int64_t out_stride;
   uint8_t* kept;     // may be null
   int64_t kept_stride;
+  int32_t batches;              // of `groups` rows, to a CTA; one but where they are staged
   int32_t in_bytes, out_bytes;  // of the shared memory for what a CTA reads and writes
 };
 
@@ -101,139 +102,131 @@ keep_kernel(const KeepArgs a) {
   __shared__ RowScratch scratch;
   int turn = 0;
   const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
-  const int64_t row = (int64_t)blockIdx.x * a.groups + group;
-  const bool valid = row < a.rows;
-  const T* x = (const T*)a.x + row * a.stride;
   const int32_t chunk = a.lanes * kElems;
   const bool keep = kMode == kRound || a.kept;
-  uint8_t* to8 = (uint8_t*)a.out + row * a.out_stride;
-  T* to = (T*)a.out + row * a.out_stride;
-  uint8_t* kept = a.kept + row * a.kept_stride;
   // a CTA's rows: what it reads, its values and what it keeps
   extern __shared__ uint4 staged[];
   uint8_t* const in_stage = (uint8_t*)staged;
   uint8_t* const out_stage = in_stage + a.in_bytes;
   uint8_t* const kept_stage = out_stage + a.out_bytes;
-  const int64_t row0 = row - group, left = a.rows - row0;
-  const int n = (int)(left < a.groups ? left : a.groups);
+  const int64_t row0 = (int64_t)blockIdx.x * a.groups * a.batches, left = a.rows - row0;
+  const int rows = (int)(left < a.groups * a.batches ? left : a.groups * a.batches);
+  const T* const x0 = (const T*)a.x + row0 * a.stride;
+  T* const out0 = (T*)a.out + row0 * a.out_stride;
+  uint8_t* const out8_0 = (uint8_t*)a.out + row0 * a.out_stride;
   if constexpr (kStaged) {
-    const T* from = (const T*)a.x + row0 * a.stride;
-    stage_in(in_stage, from, n * a.stride * (int64_t)sizeof(T), a.x,
+    stage_in(in_stage, x0, rows * a.stride * (int64_t)sizeof(T), a.x,
              (const T*)a.x + a.rows * a.stride);
-    x = (const T*)(in_stage + stage_offset(from)) + group * a.stride;
-    to = (T*)(out_stage + stage_offset((T*)a.out + row0 * a.out_stride)) + group * a.out_stride;
-    to8 = out_stage + group * a.out_stride;
-    kept = kept_stage + group * a.kept_stride;
     stage_wait();
   }
-  const auto finish = [&] {
-    if constexpr (kStaged) {
-      __syncthreads();
-      if (kMode != kRound && kOut8)
-        stage_out(out_stage, (uint8_t*)a.out + row0 * a.out_stride, n * a.out_stride);
-      else if (kMode != kRound)
-        stage_out(out_stage, (T*)a.out + row0 * a.out_stride,
-                  n * a.out_stride * (int64_t)sizeof(T));
-      if (keep) stage_out(kept_stage, a.kept + row0 * a.kept_stride, n * a.kept_stride);
-    }
-  };
-  RowRegs<T, kVec, kPer> v, u;
-  float y[kOut8 ? kElems : 1];
-  uint32_t top[3] = {0, 0, 0};
-  // The values are made of the row once: those of a type that is stored as it is go out at
-  // once, those that are rounded to 8 bits wait for their largest magnitude.
-  for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
-    const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
-    v.load(part, x + c0, valid);
-    if constexpr (kMode == kGated) u.load(part, x + a.dim + c0, valid);
-    if (keep) {
-      top[0] = max(top[0], v.top());
-      if constexpr (kMode == kGated) top[1] = max(top[1], u.top());
-    }
-    if constexpr (kMode != kRound) {
-      with_kind(a.f, [&](auto kind) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          if (part.beyond(i)) break;
-          float f[kVec], g[kVec];
-          v.get(i, f);
-          if constexpr (kMode == kGated) u.get(i, g);
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            f[e] = nonlinear<false, kFit>(kind, f[e], nullptr);
-            if constexpr (kMode == kGated) f[e] *= g[e];
-            if constexpr (kOut8) {
-              y[i * kVec + e] = f[e];
-              top[2] = max(top[2], magnitude(f[e]));
-            }
-          }
-          if constexpr (!kOut8) part.store_one(to + c0, valid, i, f);
-        }
-      });
-    }
-  }
-  if (!keep && !kOut8) {
-    finish();
-    return;
-  }
-  v.pin();
-  if constexpr (kMode == kGated) u.pin();
-  Int8Scale s = {}, s_gate = {}, s_out = {};
-  if constexpr (kMode == kRound) {
-    uint32_t one[1] = {top[0]};
-    group_reduce<MaxBits>(one, a.lanes, &scratch, turn);
-    s = int8_scale(one[0]);
-  } else {
-    group_reduce<MaxBits>(top, a.lanes, &scratch, turn);
-    s = int8_scale(top[0]);
-    if constexpr (kMode == kGated) s_gate = int8_scale(top[1]);
-    if constexpr (kOut8) s_out = int8_scale(top[2]);
-  }
-  const int64_t half = int8_row_bytes(a.dim);
-  for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
-    const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
-    if (kLoop) {
+  for (int batch = 0; batch < (kStaged ? a.batches : 1); ++batch) {
+    const int r = batch * a.groups + group;
+    const bool valid = r < rows;
+    const T* x = kStaged ? (const T*)(in_stage + stage_offset(x0)) + r * a.stride
+                         : x0 + r * a.stride;
+    T* to = kStaged ? (T*)(out_stage + stage_offset(out0)) + r * a.out_stride
+                    : out0 + r * a.out_stride;
+    uint8_t* to8 = (kStaged ? out_stage : out8_0) + r * a.out_stride;
+    uint8_t* kept = (kStaged ? kept_stage : a.kept + row0 * a.kept_stride) + r * a.kept_stride;
+    RowRegs<T, kVec, kPer> v, u;
+    float y[kOut8 ? kElems : 1];
+    uint32_t top[3] = {0, 0, 0};
+    // The values are made of the row once: those of a type that is stored as it is go out at
+    // once, those that are rounded to 8 bits wait for their largest magnitude.
+    for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
+      const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
       v.load(part, x + c0, valid);
       if constexpr (kMode == kGated) u.load(part, x + a.dim + c0, valid);
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (part.beyond(i)) break;
-      float f[kVec];
-      v.get(i, f);
       if (keep) {
-        int8_store(part, kept + c0, valid, i, f, s);
-        if constexpr (kMode == kGated) {
-          float g[kVec];
-          u.get(i, g);
-          int8_store(part, kept + half + c0, valid, i, g, s_gate);
-        }
+        top[0] = max(top[0], v.top());
+        if constexpr (kMode == kGated) top[1] = max(top[1], u.top());
       }
-      if constexpr (kOut8) {
-        if (kLoop) {
-          float g[kVec];
-          if constexpr (kMode == kGated) u.get(i, g);
-          with_kind(a.f, [&](auto kind) {
+      if constexpr (kMode != kRound) {
+        with_kind(a.f, [&](auto kind) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            if (part.beyond(i)) break;
+            float f[kVec];
+            v.get(i, f);
+            [[maybe_unused]] float g[kVec];
+            if constexpr (kMode == kGated) u.get(i, g);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
               f[e] = nonlinear<false, kFit>(kind, f[e], nullptr);
               if constexpr (kMode == kGated) f[e] *= g[e];
+              if constexpr (kOut8) {
+                y[i * kVec + e] = f[e];
+                top[2] = max(top[2], magnitude(f[e]));
+              }
             }
-          });
-          int8_store(part, to8 + c0, valid, i, f, s_out);
-        } else {
-          int8_store(part, to8, valid, i, y + i * kVec, s_out);
+            if constexpr (!kOut8) part.store_one(to + c0, valid, i, f);
+          }
+        });
+      }
+    }
+    if (!keep && !kOut8) continue;
+    v.pin();
+    if constexpr (kMode == kGated) u.pin();
+    Int8Scale s = {}, s_gate = {}, s_out = {};
+    if constexpr (kMode == kRound) {
+      uint32_t one[1] = {top[0]};
+      group_reduce<MaxBits>(one, a.lanes, &scratch, turn);
+      s = int8_scale(one[0]);
+    } else {
+      group_reduce<MaxBits>(top, a.lanes, &scratch, turn);
+      s = int8_scale(top[0]);
+      if constexpr (kMode == kGated) s_gate = int8_scale(top[1]);
+      if constexpr (kOut8) s_out = int8_scale(top[2]);
+    }
+    const int64_t half = int8_row_bytes(a.dim);
+    for (int32_t c0 = 0; c0 < (kLoop ? a.dim : 1); c0 += chunk) {
+      const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
+      if (kLoop) {
+        v.load(part, x + c0, valid);
+        if constexpr (kMode == kGated) u.load(part, x + a.dim + c0, valid);
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (part.beyond(i)) break;
+        float f[kVec];
+        v.get(i, f);
+        [[maybe_unused]] float g[kVec];
+        if constexpr (kMode == kGated) u.get(i, g);
+        if (keep) {
+          int8_store(part, kept + c0, valid, i, f, s);
+          if constexpr (kMode == kGated) int8_store(part, kept + half + c0, valid, i, g, s_gate);
+        }
+        if constexpr (kOut8) {
+          if (kLoop) {
+            with_kind(a.f, [&](auto kind) {
+#pragma unroll
+              for (int e = 0; e < kVec; ++e) {
+                f[e] = nonlinear<false, kFit>(kind, f[e], nullptr);
+                if constexpr (kMode == kGated) f[e] *= g[e];
+              }
+            });
+            int8_store(part, to8 + c0, valid, i, f, s_out);
+          } else {
+            int8_store(part, to8, valid, i, y + i * kVec, s_out);
+          }
         }
       }
     }
+    if (keep) {
+      int8_store_end(kept, a.dim, lane, a.lanes, valid, s);
+      if constexpr (kMode == kGated)
+        int8_store_end(kept + half, a.dim, lane, a.lanes, valid, s_gate);
+    }
+    if constexpr (kOut8) int8_store_end(to8, a.dim, lane, a.lanes, valid, s_out);
   }
-  if (keep) {
-    int8_store_end(kept, a.dim, lane, a.lanes, valid, s);
-    if constexpr (kMode == kGated)
-      int8_store_end(kept + half, a.dim, lane, a.lanes, valid, s_gate);
+  if constexpr (kStaged) {
+    __syncthreads();
+    if (kMode != kRound && kOut8)
+      stage_out(out_stage, out8_0, rows * a.out_stride);
+    else if (kMode != kRound)
+      stage_out(out_stage, out0, rows * a.out_stride * (int64_t)sizeof(T));
+    if (keep) stage_out(kept_stage, a.kept + row0 * a.kept_stride, rows * a.kept_stride);
   }
-  if constexpr (kOut8) int8_store_end(to8, a.dim, lane, a.lanes, valid, s_out);
-  finish();
 }
 
 struct BackArgs {
@@ -245,6 +238,7 @@ struct BackArgs {
   int64_t grad_stride;
   void* out;
   int64_t out_stride;
+  int32_t batches;                 // of `groups` rows, to a CTA; one but where they are staged
   int32_t kept_bytes, grad_bytes;  // of shared memory, where a CTA's rows are there
 };
 
@@ -272,9 +266,9 @@ struct BackStage {
   int64_t row0;
   int n;
   __device__ BackStage(const BackArgs& args, uint8_t* shared) : a(args), base(shared) {
-    row0 = (int64_t)blockIdx.x * a.groups;
+    row0 = (int64_t)blockIdx.x * a.groups * a.batches;
     const int64_t left = a.rows - row0;
-    n = (int)(left < a.groups ? left : a.groups);
+    n = (int)(left < a.groups * a.batches ? left : a.groups * a.batches);
   }
   __device__ uint8_t* kept() const { return base; }
   __device__ uint8_t* grad_base() const { return base + a.kept_bytes; }
@@ -306,33 +300,31 @@ values_kernel(const BackArgs a) {
   constexpr int kPer = kElems / kVec;
   extern __shared__ uint4 staged[];
   const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
-  const int64_t row = (int64_t)blockIdx.x * a.groups + group;
   const BackStage<T, T> stage(a, (uint8_t*)staged);
-  const bool valid = row < a.rows;
-  if (!kStaged && !valid) return;
-  const uint8_t* kept = a.kept + row * a.kept_stride;
-  T* out = (T*)a.out + row * a.out_stride;
-  if constexpr (kStaged) {
-    stage.load(false);
-    kept = stage.kept() + group * a.kept_stride;
-    out = stage.out() + group * a.out_stride;
-  }
-  const float scale = valid ? *(const float*)(kept + int8_row_bytes(a.dim) - 4) : 0.f;
-  for (int32_t c0 = 0; valid && c0 < a.dim; c0 += a.lanes * kElems) {
-    const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
-    Int8Regs<kVec, kPer> v;
-    v.load(part, kept + c0, true);
+  if constexpr (kStaged) stage.load(false);
+  for (int batch = 0; batch < (kStaged ? a.batches : 1); ++batch) {
+    const int r = batch * a.groups + group;
+    if (r >= stage.n) break;
+    const uint8_t* kept =
+        kStaged ? stage.kept() + r * a.kept_stride : a.kept + (stage.row0 + r) * a.kept_stride;
+    T* out = kStaged ? stage.out() + r * a.out_stride : stage.out_to() + r * a.out_stride;
+    const float scale = *(const float*)(kept + int8_row_bytes(a.dim) - 4);
+    for (int32_t c0 = 0; c0 < a.dim; c0 += a.lanes * kElems) {
+      const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
+      Int8Regs<kVec, kPer> v;
+      v.load(part, kept + c0, true);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (part.beyond(i)) break;
-      float f[kVec];
-      v.get(i, f);
+      for (int i = 0; i < kPer; ++i) {
+        if (part.beyond(i)) break;
+        float f[kVec];
+        v.get(i, f);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float most = most_of<T>(), y = f[e] * scale;
-        f[e] = y > most ? most : y < -most ? -most : y;
+        for (int e = 0; e < kVec; ++e) {
+          const float most = most_of<T>(), y = f[e] * scale;
+          f[e] = y > most ? most : y < -most ? -most : y;
+        }
+        part.store_one(out + c0, true, i, f);
       }
-      part.store_one(out + c0, true, i, f);
     }
   }
   if constexpr (kStaged) stage.store();
@@ -346,51 +338,49 @@ back_kernel(const BackArgs a) {
   constexpr bool kFit = sizeof(T) == 2;
   extern __shared__ uint4 staged[];
   const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
-  const int64_t row = (int64_t)blockIdx.x * a.groups + group;
   const BackStage<TGrad, T> stage(a, (uint8_t*)staged);
-  const bool valid = row < a.rows;
-  if (!kStaged && !valid) return;
-  const uint8_t* kept = a.kept + row * a.kept_stride;
-  T* out = (T*)a.out + row * a.out_stride;
-  const TGrad* grad = (const TGrad*)a.grad + row * a.grad_stride;
-  if constexpr (kStaged) {
-    stage.load(true);
-    kept = stage.kept() + group * a.kept_stride;
-    out = stage.out() + group * a.out_stride;
-    grad = stage.grad() + group * a.grad_stride;
-  }
-  const int64_t half = int8_row_bytes(a.dim);
-  const float s0 = valid ? *(const float*)(kept + half - 4) : 0.f;
-  const float s1 = valid && kGate ? *(const float*)(kept + 2 * half - 4) : 0.f;
-  for (int32_t c0 = 0; valid && c0 < a.dim; c0 += a.lanes * kElems) {
-    const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
-    Int8Regs<kVec, kPer> v, u;
-    RowRegs<TGrad, kVec, kPer> d;
-    v.load(part, kept + c0, true);
-    if constexpr (kGate) u.load(part, kept + half + c0, true);
-    d.load(part, grad + c0, true);
-    with_kind(a.f, [&](auto kind) {
+  if constexpr (kStaged) stage.load(true);
+  for (int batch = 0; batch < (kStaged ? a.batches : 1); ++batch) {
+    const int r = batch * a.groups + group;
+    if (r >= stage.n) break;
+    const uint8_t* kept =
+        kStaged ? stage.kept() + r * a.kept_stride : a.kept + (stage.row0 + r) * a.kept_stride;
+    T* out = kStaged ? stage.out() + r * a.out_stride : stage.out_to() + r * a.out_stride;
+    const TGrad* grad = (kStaged ? stage.grad() : stage.grad_from()) + r * a.grad_stride;
+    const int64_t half = int8_row_bytes(a.dim);
+    const float s0 = *(const float*)(kept + half - 4);
+    const float s1 = kGate ? *(const float*)(kept + 2 * half - 4) : 0.f;
+    for (int32_t c0 = 0; c0 < a.dim; c0 += a.lanes * kElems) {
+      const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
+      Int8Regs<kVec, kPer> v, u;
+      RowRegs<TGrad, kVec, kPer> d;
+      v.load(part, kept + c0, true);
+      if constexpr (kGate) u.load(part, kept + half + c0, true);
+      d.load(part, grad + c0, true);
+      with_kind(a.f, [&](auto kind) {
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (part.beyond(i)) break;
-        float f[kVec], g[kVec], h[kVec];
-        v.get(i, f);
-        d.get(i, h);
-        if constexpr (kGate) u.get(i, g);
+        for (int i = 0; i < kPer; ++i) {
+          if (part.beyond(i)) break;
+          float f[kVec], h[kVec];
+          v.get(i, f);
+          d.get(i, h);
+          [[maybe_unused]] float g[kVec];
+          if constexpr (kGate) u.get(i, g);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          float slope;
-          const float y = nonlinear<true, kFit>(kind, f[e] * s0, &slope);
-          f[e] = h[e] * slope;
-          if constexpr (kGate) {
-            f[e] *= g[e] * s1;
-            g[e] = h[e] * y;
+          for (int e = 0; e < kVec; ++e) {
+            float slope;
+            const float y = nonlinear<true, kFit>(kind, f[e] * s0, &slope);
+            f[e] = h[e] * slope;
+            if constexpr (kGate) {
+              f[e] *= g[e] * s1;
+              g[e] = h[e] * y;
+            }
           }
+          part.store_one(out + c0, true, i, f);
+          if constexpr (kGate) part.store_one(out + a.dim + c0, true, i, g);
         }
-        part.store_one(out + c0, true, i, f);
-        if constexpr (kGate) part.store_one(out + a.dim + c0, true, i, g);
-      }
-    });
+      });
+    }
   }
   if constexpr (kStaged) stage.store();
 }
@@ -426,6 +416,14 @@ agnes_status check_kept(const char* op, const char* name, int64_t rows, int64_t 
   return AGNES_OK;
 }
 
+// How many batches of `groups` rows a CTA that stages them takes: some 48 KB of them, as a CTA
+// loads, works and stores in turn, but not fewer CTAs than the device runs at a time.
+int32_t stage_batches(int64_t rows, int32_t groups, int64_t row_bytes, int sms) {
+  const int64_t fit = 49152 / (groups * row_bytes), share = rows / (groups * (int64_t)sms * 4);
+  const int64_t n = fit < share ? fit : share;
+  return n < 1 ? 1 : (int32_t)n;
+}
+
 template <typename T, int kMode, bool kOut8>
 cudaError_t launch_keep(KeepArgs a, int device, cudaStream_t st) {
   const int64_t next = a.rows > 1 ? 1 : 0;  // a single row has no next one
@@ -445,37 +443,42 @@ cudaError_t launch_keep(KeepArgs a, int device, cudaStream_t st) {
                        a.out_stride == (kOut8 ? int8_row_bytes(a.dim) : a.dim)) &&
                       (!a.kept || !next || a.kept_stride == kept_row);
   size_t smem = 0;
+  a.batches = 1;
   if (staged) {
     if (!next) {
       a.stride = cols;
       a.out_stride = kOut8 ? int8_row_bytes(a.dim) : a.dim;
       a.kept_stride = kept_row;
     }
-    a.in_bytes = (int32_t)staged_bytes(a.groups * cols * (int64_t)sizeof(T));
-    a.out_bytes = kMode == kRound ? 0
-                  : (int32_t)staged_bytes(a.groups * a.out_stride * (kOut8 ? 1 : (int64_t)sizeof(T)));
-    smem = (size_t)a.in_bytes + a.out_bytes + (a.kept ? a.groups * kept_row : 0);
+    const int64_t out_row =
+        kMode == kRound ? 0 : a.out_stride * (kOut8 ? 1 : (int64_t)sizeof(T));
+    const int64_t row = cols * (int64_t)sizeof(T) + out_row + (a.kept ? kept_row : 0);
+    a.batches = stage_batches(a.rows, a.groups, row, op_num_sms(device));
+    const int64_t rows = a.groups * (int64_t)a.batches;
+    a.in_bytes = (int32_t)staged_bytes(rows * cols * (int64_t)sizeof(T));
+    a.out_bytes = kMode == kRound ? 0 : (int32_t)staged_bytes(rows * out_row);
+    smem = (size_t)a.in_bytes + a.out_bytes + (a.kept ? rows * kept_row : 0);
   }
   const auto kernel = wide     ? (loop ? keep_kernel<T, kMode, kOut8, 8, true, false>
                                        : keep_kernel<T, kMode, kOut8, 8, false, false>)
                       : staged ? keep_kernel<T, kMode, kOut8, 1, false, true>
                       : loop   ? keep_kernel<T, kMode, kOut8, 1, true, false>
                                : keep_kernel<T, kMode, kOut8, 1, false, false>;
-  if (smem > 48 * 1024) {
+  if (smem + sizeof(RowScratch) > 48 * 1024) {
     static OncePerDevice once;
     const cudaError_t e = once.run(device, [&] {
       return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
     });
     if (e != cudaSuccess) return e;
   }
-  kernel<<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), smem, st>>>(a);
+  kernel<<<(unsigned)ceil_div(a.rows, a.groups * a.batches), shape.threads(), smem, st>>>(a);
   return cudaGetLastError();
 }
 
 // kernels[0] for vectors, [1] for single elements, [2] for those through shared memory
 using BackKernel = void (*)(BackArgs);
 cudaError_t launch_back(const BackKernel (&kernels)[3], BackArgs a, int halves, int64_t grad_size,
-                        int64_t size, cudaStream_t st) {
+                        int64_t size, int device, cudaStream_t st) {
   const int64_t next = a.rows > 1 ? 1 : 0;
   const bool aligned = aligned_rows(a.out, next * a.out_stride * size, 16) &&
                        (!a.grad || aligned_rows(a.grad, next * a.grad_stride * grad_size, 16));
@@ -489,20 +492,24 @@ cudaError_t launch_back(const BackKernel (&kernels)[3], BackArgs a, int halves, 
                                  (!a.grad || a.grad_stride == a.dim)));
   const int which = vec_of(a.dim, aligned) == 8 ? 0 : staged ? 2 : 1;
   size_t smem = 0;
+  a.batches = 1;
   if (which == 2) {
     a.kept_stride = kept_row;
     a.out_stride = halves * a.dim;
     a.grad_stride = a.dim;
-    a.kept_bytes = (int32_t)staged_bytes(a.groups * kept_row);
-    a.grad_bytes = a.grad ? (int32_t)staged_bytes(a.groups * a.dim * grad_size) : 0;
-    smem = (size_t)a.kept_bytes + a.grad_bytes + staged_bytes(a.groups * halves * a.dim * size);
-    if (smem > 48 * 1024) {  // gated rows in fp32
+    const int64_t out_row = halves * a.dim * size, grad_row = a.grad ? a.dim * grad_size : 0;
+    a.batches = stage_batches(a.rows, a.groups, kept_row + out_row + grad_row, op_num_sms(device));
+    const int64_t rows = a.groups * (int64_t)a.batches;
+    a.kept_bytes = (int32_t)staged_bytes(rows * kept_row);
+    a.grad_bytes = a.grad ? (int32_t)staged_bytes(rows * grad_row) : 0;
+    smem = (size_t)a.kept_bytes + a.grad_bytes + staged_bytes(rows * out_row);
+    if (smem > 48 * 1024) {
       const cudaError_t e = cudaFuncSetAttribute(
           kernels[which], cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
       if (e != cudaSuccess) return e;
     }
   }
-  kernels[which]<<<(unsigned)ceil_div(a.rows, a.groups), shape.threads(), smem, st>>>(a);
+  kernels[which]<<<(unsigned)ceil_div(a.rows, a.groups * a.batches), shape.threads(), smem, st>>>(a);
   return cudaGetLastError();
 }
 
@@ -588,7 +595,7 @@ agnes_status agnes_int8_dequantize(const void* x, int64_t stride, int64_t rows, 
     using T = typename decltype(t)::type;
     const BackKernel kernels[3] = {values_kernel<T, 8, false>, values_kernel<T, 1, false>,
                                    values_kernel<T, 1, true>};
-    return launch_back(kernels, a, 1, 0, sizeof(T), (cudaStream_t)cuda_stream);
+    return launch_back(kernels, a, 1, 0, sizeof(T), device, (cudaStream_t)cuda_stream);
   }));
 }
 
@@ -683,7 +690,7 @@ agnes_status agnes_activation_grad(const void* grad, int32_t grad_dtype, int64_t
            back_kernel<TGrad, T, false, 1, true>},
           {back_kernel<TGrad, T, true, 8, false>, back_kernel<TGrad, T, true, 1, false>,
            back_kernel<TGrad, T, true, 1, true>}};
-      return launch_back(kernels[gated], a, halves, sizeof(TGrad), sizeof(T),
+      return launch_back(kernels[gated], a, halves, sizeof(TGrad), sizeof(T), device,
                          (cudaStream_t)cuda_stream);
     });
   }));

@@ -254,6 +254,8 @@ agnes_status agnes_int8_linear_grad_weight_workspace(int64_t rows, int64_t width
                                                      int64_t* bytes);
 
 /* The gradient of agnes_int8_linear to its input: out[r][i] = sum_j grad[r][j] w[j][i].
+ * As in the gradient to the weights, what an infinity or NaN of grad or a row that
+ * stands for NaN enters is not finite (NaN, or an infinity), and nothing else is.
  *  out    rows x dim of out_dtype, out_stride apart.
  *  workspace  at least agnes_int8_linear_grad_input_workspace bytes, 256-byte
  *         aligned; its contents are not kept.  `direct` as above.

@@ -19,9 +19,17 @@ namespace {
 
 // ---- few rows ------------------------------------------------------------------
 
-constexpr int kFewRows = 32;
+// A group of up to 32 lanes has a column, 16 of its whole numbers to a lane at a time, which meet
+// all the rows' (from L1: the rows are as often read as there are columns, and bound the larger
+// calls).  Columns by twos would halve those reads, and the groups as well: 4 x 1024 to 1024 took
+// 4.1 us so and takes 3.1.  Times by rows against those of the tiles below, fp16:
+// 128 to 256     1.9 us (1 row), 2.3 (4), 3.1 (8), 6.7 (16)     7.3
+// 1024 to 4096   3.0, 4.3, 5.9, 11.3                           15.1
+// 4096 to 4096   4.2, 6.9, 10.4, 20.0                          38.7
+// of which the weights' bytes are 0.01, 0.6 and 2.5.  With 32 rows they are 8.4, 26.6 and 46.7
+// against 7.2, 15.2 and 38.8, so tiles have those.
+constexpr int kFewRows = 16;
 constexpr int kFewThreads = 256;
-constexpr int kFewCols = 2;  // of the output to a group of lanes at a time
 
 struct LinearArgs {
   const uint8_t *x, *w;
@@ -41,60 +49,52 @@ __device__ __forceinline__ float scaled(float sum, float a, float b) {
 }
 
 template <typename TOut, int kRows>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(kFewThreads, kRows > 8 ? 1 : 4)
 linear_few_kernel(int lanes, const LinearArgs a) {
   const int lane = threadIdx.x % lanes;
   const int64_t groups = (int64_t)gridDim.x * (kFewThreads / lanes);
   const int chunks = (a.dim + 15) / 16;
-  for (int64_t j0 = ((int64_t)blockIdx.x * (kFewThreads / lanes) + threadIdx.x / lanes) * kFewCols;
+  for (int64_t j = (int64_t)blockIdx.x * (kFewThreads / lanes) + threadIdx.x / lanes;
        // whole warps stay together for the exchange
-       j0 - (threadIdx.x % 32) / lanes * kFewCols < a.width; j0 += groups * kFewCols) {
-    int32_t sum[kRows * kFewCols];
+       j - (threadIdx.x % 32) / lanes < a.width; j += groups) {
+    const uint8_t* w_row = a.w + (j < a.width ? j : a.width - 1) * a.w_stride;
+    int32_t sum[kRows];
 #pragma unroll
-    for (int k = 0; k < kRows * kFewCols; ++k) sum[k] = 0;
+    for (int r = 0; r < kRows; ++r) sum[r] = 0;
+#pragma unroll 1
     for (int c = lane; c < chunks; c += lanes) {
-      uint4 w[kFewCols];
-#pragma unroll
-      for (int k = 0; k < kFewCols; ++k)
-        w[k] = j0 + k < a.width ? __ldg((const uint4*)(a.w + (j0 + k) * a.w_stride) + c)
-                                : make_uint4(0, 0, 0, 0);
-      uint4 keep = make_uint4(~0u, ~0u, ~0u, ~0u);
+      uint4 w = __ldg((const uint4*)w_row + c);
       if (c == chunks - 1) {  // the row's scale may be in its last 16 bytes
         const int left = a.dim - c * 16;
         const auto mask = [&](int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; };
-        keep = make_uint4(mask(left), mask(left - 4), mask(left - 8), mask(left - 12));
+        w = make_uint4(w.x & mask(left), w.y & mask(left - 4), w.z & mask(left - 8),
+                       w.w & mask(left - 12));
       }
 #pragma unroll
       for (int r = 0; r < kRows; ++r) {
-        if (r >= a.rows) break;
-        uint4 x = __ldg((const uint4*)(a.x + r * a.x_stride) + c);
-        x = make_uint4(x.x & keep.x, x.y & keep.y, x.z & keep.z, x.w & keep.w);
-#pragma unroll
-        for (int k = 0; k < kFewCols; ++k) {
-          int32_t s = sum[r * kFewCols + k];
-          s = __dp4a((int)x.x, (int)w[k].x, s);
-          s = __dp4a((int)x.y, (int)w[k].y, s);
-          s = __dp4a((int)x.z, (int)w[k].z, s);
-          sum[r * kFewCols + k] = __dp4a((int)x.w, (int)w[k].w, s);
-        }
+        // past the end the last row again: all rows' loads are on their way together
+        const uint4 x = __ldg((const uint4*)(a.x + (r < a.rows ? r : a.rows - 1) * a.x_stride) + c);
+        int32_t s = __dp4a((int)x.x, (int)w.x, sum[r]);
+        s = __dp4a((int)x.y, (int)w.y, s);
+        s = __dp4a((int)x.z, (int)w.z, s);
+        sum[r] = __dp4a((int)x.w, (int)w.w, s);
       }
     }
 #pragma unroll
-    for (int k = 0; k < kRows * kFewCols; ++k)
-      for (int d = lanes / 2; d > 0; d >>= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], d);
-    if (lane) continue;
+    for (int r = 0; r < kRows; ++r)
+      for (int d = lanes / 2; d > 0; d >>= 1) sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], d);
+    if (j >= a.width) continue;
+    const float sw = *(const float*)(w_row + a.row_bytes - 4);
+    const float b = a.bias ? __ldg(a.bias + j) : 0.f;
+    for (int r0 = 0; r0 < a.rows; r0 += lanes) {  // a row to a lane
+      int32_t mine = 0;
 #pragma unroll
-    for (int k = 0; k < kFewCols; ++k) {
-      if (j0 + k >= a.width) break;
-      const float sw = *(const float*)(a.w + (j0 + k) * a.w_stride + a.row_bytes - 4);
-      const float b = a.bias ? __ldg(a.bias + j0 + k) : 0.f;
-#pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        if (r >= a.rows) break;
-        const float sx = *(const float*)(a.x + r * a.x_stride + a.row_bytes - 4);
-        ((TOut*)a.out)[r * a.out_stride + j0 + k] =
-            from_f32<TOut>(scaled((float)sum[r * kFewCols + k], sx, sw) + b);
-      }
+      for (int r = 0; r < kRows; ++r)
+        if (r == r0 + lane) mine = sum[r];
+      const int r = r0 + lane;
+      if (r >= a.rows) break;
+      const float sx = *(const float*)(a.x + r * a.x_stride + a.row_bytes - 4);
+      ((TOut*)a.out)[r * a.out_stride + j] = from_f32<TOut>(scaled((float)mine, sx, sw) + b);
     }
   }
 }
@@ -726,7 +726,7 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
             for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(v[e]);
           }
           if constexpr (kConvert) {
-const float4* w4 = (const float4*)(my_scales + c + h);
+            const float4* w4 = (const float4*)(my_scales + c + h);
             const float4* b4 = (const float4*)(my_biases + c + h);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
@@ -844,7 +844,7 @@ template <typename TOut, int kRows>
 cudaError_t launch_few(const LinearArgs& a, int device, cudaStream_t st) {
   int lanes = 1;
   while (lanes < 32 && lanes < (a.dim + 15) / 16) lanes *= 2;
-  const int64_t ctas = ceil_div(a.width, kFewThreads / lanes * kFewCols);
+  const int64_t ctas = ceil_div(a.width, kFewThreads / lanes);
   const int64_t most = 8 * (int64_t)op_num_sms(device);
   linear_few_kernel<TOut, kRows>
       <<<(unsigned)(ctas < most ? ctas : most), kFewThreads, 0, st>>>(lanes, a);
@@ -1027,8 +1027,7 @@ agnes_status agnes_int8_linear(const void* x, int64_t x_stride, int64_t rows, co
     if (rows == 2) return launch_few<TOut, 2>(a, device, st);
     if (rows <= 4) return launch_few<TOut, 4>(a, device, st);
     if (rows <= 8) return launch_few<TOut, 8>(a, device, st);
-    if (rows <= 16) return launch_few<TOut, 16>(a, device, st);
-    if (rows <= kFewRows) return launch_few<TOut, 32>(a, device, st);
+    if (rows <= kFewRows) return launch_few<TOut, kFewRows>(a, device, st);
     return launch_linear<TOut>(a, workspace, status, device, st);
   }));
 }

@@ -24,9 +24,12 @@ namespace agnes {
 
 namespace {
 
-constexpr int kElems = 16;       // of a row to a thread, forward; rows of up to
-constexpr int kShortElems = 8;   // kShortDim columns take fewer, and two rows at a time,
-constexpr int kShortDim = 256;   // and so does the backward pass, which has more to hold
+// Of a row to a thread, forward.  Rows of up to kShortDim columns take fewer, and two rows at a
+// time (786,432 x 128 fp16 to fp16 144 us and not 242, 400,000 x 256 149 and not 252), and so
+// does the backward pass, which has more to hold.
+constexpr int kElems = 16;
+constexpr int kShortElems = 8;
+constexpr int kShortDim = 256;
 constexpr int kNormLanes = 512;  // threads to a row at most, forward
 constexpr int64_t kNormMaxDim = 8192;
 static_assert(kNormLanes * kElems >= kNormMaxDim && kRowLanesMax * kShortElems >= kNormMaxDim,
@@ -862,8 +865,8 @@ cudaError_t launch_grad(NormArgs a, bool wide, int64_t ctas, size_t smem, int de
   using Kernel = void (*)(NormArgs);
   constexpr int kPer = kShortElems;
   // With a residual in fp32 a thread has two vectors of four columns, so that each access of
-  // a warp is one run of memory (eight columns to a thread: 346 us of 16,384 x 4096, past L1,
-  // 328 through it).
+  // a warp is one run of memory (16,384 x 4096, bf16 branch, 253 us; with eight columns to a
+  // thread 346 past L1 and 328 through it).
   constexpr int kV = sizeof(TX) == 4 ? 4 : 8, kP = kShortElems / kV;
   const Kernel kernels[7] = {norm_grad_kernel<TX, TBranch, kV, kP, 1024, kBias, true, 0>,
                              norm_grad_kernel<TX, TBranch, 1, kPer, 1024, kBias, true, 0>,

@@ -481,6 +481,65 @@ def test_gradients_are_the_same_each_time(cuda_device):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,dim,dtype", [(40_000, 256, 128, torch.bfloat16),
+                                                  (9000, 640, 700, torch.bfloat16),
+                                                  (4000, 120, 300, torch.float32),
+                                                  (12, 300, 400, torch.float16)])
+def test_a_thousand_calls_give_the_same(cuda_device, rows, width, dim, dtype):
+    """What a race between a kernel's warps, or of a pair's two halves, would change now and then."""
+    d, x, w = (t.to(cuda_device) for t in _grad_inputs(rows, width, dim, dtype))
+    x8 = torch.randn(rows, dim, generator=gen(5)).to(cuda_device)
+
+    def run():
+        r = ops.int8_linear_grad_weight(d, x, dim)
+        return [ops.int8_linear(x, w, dim), r.weight, r.bias, ops.int8_linear_grad_input(d, w, dim),
+                ops.int8_quantize(x8)]
+    first = run()
+    changed = torch.zeros((), dtype=torch.int64, device=cuda_device)
+    for _ in range(1000):
+        for got, want in zip(run(), first):
+            changed += (got.view(torch.uint8) != want.view(torch.uint8)).sum()
+    assert int(changed) == 0
+    ops.check()
+
+
+# at and beside the sizes where a call takes another variant
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,dim", [
+    (16, 130, 260), (17, 130, 260), (128, 128, 128), (129, 129, 129), (50_000, 257, 511),
+    (50_000, 256, 512), (20_000, 384, 128), (20_000, 385, 128), (300, 64, 2048), (300, 64, 2049),
+    (64, 2048, 512)])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_where_variants_meet(cuda_device, rows, width, dim, dtype):
+    _product_check(cuda_device, rows, width, dim, dtype, True)
+    _grad_check(cuda_device, rows, width, dim, dtype, dtype)
+
+
+@pytest.mark.gpu
+def test_refusals_on_a_device(cuda_device):
+    flat = torch.zeros(64 * 144 + 16, dtype=torch.uint8, device=cuda_device)
+    apart = torch.zeros(4, 152, dtype=torch.uint8, device=cuda_device)[:, :144]  # 152 bytes apart
+    good = flat[:64 * 144].view(64, 144)
+    off = flat[8:8 + 64 * 144].view(64, 144)
+    d = torch.zeros(64, 64, device=cuda_device)
+    for x, w in ((off, good), (good, off), (apart, good), (good, apart)):
+        with pytest.raises(AgnesError, match="aligned|multiple of 16"):
+            ops.int8_linear(x, w, 128)
+    for bad in (off, apart):
+        n = bad.shape[0]
+        with pytest.raises(AgnesError, match="aligned|multiple of 16"):
+            ops.int8_linear_grad_weight(d[:n], bad, 128)
+        with pytest.raises(AgnesError, match="aligned|multiple of 16"):
+            ops.int8_linear_grad_input(d[:, :n], bad, 128)
+        with pytest.raises(AgnesError, match="aligned|multiple of 16"):
+            ops.int8_dequantize(bad, 128)
+        with pytest.raises(AgnesError, match="aligned|multiple of 16"):
+            ops.activation_grad(d[:n].repeat(1, 2), bad, "silu")
+        with pytest.raises(AgnesError, match="aligned|multiple of 16"):
+            ops.int8_quantize(torch.zeros(n, 128, device=cuda_device), out=bad)
+
+
+@pytest.mark.gpu
 def test_sums_over_many_rows(cuda_device):
     """A hyperbatch's rows, all of one sign: what a single fp32 sum would lose step by step."""
     rows, width, dim = 700_001, 24, 40

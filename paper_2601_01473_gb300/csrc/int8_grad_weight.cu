@@ -11,7 +11,8 @@
 // A CTA takes a tile of 128 x 128 of the output and a share of the rows:
 //   the producer      has the TMA copy slices of 64 rows, the gradient's terms and the whole
 //                     numbers as they are;
-//   the convert warps scale the whole numbers and write both terms;
+//   the convert warps scale the whole numbers and write both terms (kReady: a kernel before has,
+//                     once for all tiles);
 //   the MMA warp      issues the products into one of two accumulators, `chain` slices each;
 //   the epilogue warps add the accumulators up in registers and write a partial tile, and
 //                     meanwhile add the gradient's columns up, of the first tile of columns.
@@ -38,7 +39,9 @@ constexpr int kGradBytes = 2 * kBox;         // a term of the gradient
 // Of the scaled whole numbers' two terms and of the whole numbers, for a CTA of its own or one
 // of a pair.
 constexpr int value_bytes(bool pair) { return (pair ? 2 : 4) * kBox; }
-constexpr int raw_bytes(bool pair) { return kSlice * kTile / (pair ? 2 : 1); }
+constexpr int raw_bytes(bool pair, bool ready) {
+  return ready ? 0 : kSlice * kTile / (pair ? 2 : 1);
+}
 constexpr int kMaxSlots = 6;
 constexpr int kBars = 3 * kMaxSlots + 5;
 constexpr int kSmemLimit = 232448;
@@ -53,7 +56,7 @@ struct WeightArgs {
   const uint8_t* x;
   int64_t x_stride;
   int32_t ta;
-  bool pair;
+  bool pair, ready;
   int32_t slices;             // of all rows
   int32_t tiles_j, tiles_i;   // of the output, along width and dim
   int32_t splits, per_split;  // shares of the rows, slices of one
@@ -81,15 +84,16 @@ struct WeightBars {
   __device__ uint32_t drained() const { return at(3 * kMaxSlots + 4); }
 };
 
+// kReady: the scaled whole numbers' terms are copied like the gradient's.
 // kPair: two CTAs have 256 x 128 of the output, each the gradient's columns and the output of
 // its half and both terms of half of the whole numbers.
-template <bool kPair>
+template <bool kPair, bool kReady>
 __global__ void __launch_bounds__(kThreads, 1)
 weight_kernel(const __grid_constant__ CUtensorMap grad_map,
               const __grid_constant__ CUtensorMap x_map, const WeightArgs a) {
   grid_dep_wait();
   constexpr uint32_t kIdesc = idesc_16bit(true, true, kPair ? 2 * kTile : kTile, 2 * kTile);
-  constexpr int kValueBytes = value_bytes(kPair), kRawBytes = raw_bytes(kPair);
+  constexpr int kValueBytes = value_bytes(kPair), kRawBytes = raw_bytes(kPair, kReady);
   const uint32_t rank = kPair ? cluster_rank() : 0;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
@@ -117,7 +121,7 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
   if (tid == 0) {
     for (int s = 0; s < kMaxSlots; ++s) {
       mbar_init(bar.full(s), 1);
-      mbar_init(bar.ready(s), kConvertWarps * kGroup);
+      mbar_init(bar.ready(s), (kReady ? 1 : kConvertWarps) * kGroup);
       mbar_init(bar.empty(s), 1 + (bias ? kEpilogueWarps : 0));
     }
     for (int d = 0; d < 2; ++d) {
@@ -155,16 +159,24 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
           break;
         }
         const uint32_t at = ring_at + (uint32_t)(s * a.slot_bytes);
-        mbar_expect(bar.full(s), (uint32_t)(a.ta * kGradBytes + kRawBytes));
+        mbar_expect(bar.full(s), (uint32_t)(a.ta * kGradBytes + (kReady ? kValueBytes : kRawBytes)));
         // Past the last row a term's slice runs into the next term, which is finite there
-        // and meets whole numbers of zero.
+        // and meets zeros.
         for (int p = 0; p < a.ta; ++p)
           for (int b = 0; b < 2; ++b)
             tma_load(at + (uint32_t)(p * kGradBytes + b * kBox), &grad_map,
                      (int32_t)(j0 + b * 64), (int32_t)(p * a.rows + (int64_t)k * kSlice),
                      bar.full(s));
-        tma_load(at + raw_off, &x_map, i0 + (int32_t)rank * (kTile / 2),
-                 (int32_t)((int64_t)k * kSlice), bar.full(s));
+        if constexpr (kReady) {  // boxes of 64 columns of each term
+          constexpr int kBoxes = kValueBytes / 2 / kBox;
+          for (int b = 0; b < 2 * kBoxes; ++b)
+            tma_load(at + value_off + (uint32_t)(b * kBox), &x_map,
+                     i0 + (int32_t)rank * (kTile / 2) + b % kBoxes * 64,
+                     (int32_t)((b / kBoxes * (int64_t)a.slices + k) * kSlice), bar.full(s));
+        } else {
+          tma_load(at + raw_off, &x_map, i0 + (int32_t)rank * (kTile / 2),
+                   (int32_t)((int64_t)k * kSlice), bar.full(s));
+        }
         ring.next(a.slots);
         ++issued;
       }
@@ -181,7 +193,10 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
       }
     }
   } else if (warp == kMmaWarp) {
-    if (lane == 0 && rank == 0) {
+    // the whole warp goes through the loop, so that its addresses are the same for all lanes and
+    // stay in uniform registers, as the products take them
+    if (rank == 0) {
+      const bool lead = elect_one();
       const auto multiply = [](uint32_t d, uint64_t x, uint64_t y, uint32_t more) {
         if constexpr (kPair)
           mma_16bit_pair(d, x, y, kIdesc, more);
@@ -197,7 +212,7 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
       Ring acc;
       for (int32_t c0 = k0; ok && c0 < k1; c0 += a.chain) {
         const int d = acc.slot;
-        if (!acc.first && !mbar_wait(bar.taken(d), acc.parity ^ 1u)) {
+        if (!acc.first && !__all_sync(0xffffffffu, mbar_wait(bar.taken(d), acc.parity ^ 1u))) {
           ok = false;
           break;
         }
@@ -206,7 +221,9 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
         uint32_t accumulate = 0;
         for (int32_t k = c0; k < min(c0 + a.chain, k1); ++k) {
           const int s = ring.slot;
-          if (!mbar_wait(bar.full(s), ring.parity) || !mbar_wait(bar.ready(s), ring.parity)) {
+          // what is ready is full as well
+          const uint32_t b = !kReady || kPair ? bar.ready(s) : bar.full(s);
+          if (!__all_sync(0xffffffffu, mbar_wait(b, ring.parity))) {
             ok = false;
             break;
           }
@@ -216,28 +233,45 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
           const int n = left < kSlice ? (int)((left + 15) / 16) : kSlice / 16;
           // descriptors are sums of constants: one thread issues all products
           const uint64_t g0 = operand_desc_mn(at, kBox), v0 = operand_desc_mn(at + value_off, kBox);
+          if (lead) {
 #pragma unroll
-          for (int i = 0; i < kSlice / 16; ++i) {
-            if (i >= n) break;
-            multiply(to, g0 + (uint64_t)(i * 128), v0 + (uint64_t)(i * 128),
-                     accumulate | (uint32_t)(i > 0));
-            if (a.ta > 1)
-              multiply(to, g0 + (uint64_t)(i * 128 + (kGradBytes >> 4)), v0 + (uint64_t)(i * 128), 1);
-            if (a.ta > 2)
-              multiply(to, g0 + (uint64_t)(i * 128 + 2 * (kGradBytes >> 4)),
-                       v0 + (uint64_t)(i * 128), 1);
+            for (int i = 0; i < kSlice / 16; ++i) {
+              if (i >= n) break;
+              multiply(to, g0 + (uint64_t)(i * 128), v0 + (uint64_t)(i * 128),
+                       accumulate | (uint32_t)(i > 0));
+              if (a.ta > 1)
+                multiply(to, g0 + (uint64_t)(i * 128 + (kGradBytes >> 4)), v0 + (uint64_t)(i * 128),
+                         1);
+              if (a.ta > 2)
+                multiply(to, g0 + (uint64_t)(i * 128 + 2 * (kGradBytes >> 4)),
+                         v0 + (uint64_t)(i * 128), 1);
+            }
+            commit(bar.empty(s));
           }
+          __syncwarp();
           accumulate = 1;
-          commit(bar.empty(s));
           ring.next(a.slots);
         }
         if (!ok) break;
-        commit(bar.done(d));
+        if (lead) commit(bar.done(d));
+        __syncwarp();
         acc.next(2);
       }
       if (!ok) {  // the products in flight end before the tensor memory is freed
-        commit(bar.drained());
+        if (lead) commit(bar.drained());
         mbar_wait(bar.drained(), 0);
+      }
+    }
+  } else if (warp >= kConvertWarp0 && kReady) {
+    // one warp tells the pair's first CTA of this one's slices
+    if (kPair && warp == kConvertWarp0) {
+      for (int32_t k = k0; k < k1; ++k) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar.full(ring.slot), ring.parity))) {
+          ok = false;
+          break;
+        }
+        if (lane == 0) tell(bar.ready(ring.slot));
+        ring.next(a.slots);
       }
     }
   } else if (warp >= kConvertWarp0) {
@@ -260,7 +294,7 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
         break;
       }
       uint8_t* slot = smem + s * a.slot_bytes;
-      const uint8_t* from = slot + raw_off + r * (kRawBytes / kSlice);
+      const uint8_t* from = slot + raw_off + r * (raw_bytes(kPair, false) / kSlice);
       // a box of 64 values for each half, or one for both; behind them the second terms'
       uint8_t* to = slot + value_off + (kPair ? 0 : half * kBox) + r * 128;
       const int first = kPair ? 4 * half : 0;  // piece of 8 values of the box
@@ -375,6 +409,40 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
   }
 }
 
+// Both terms of the scaled whole numbers, dpad to a row, zeros past the last row up to a
+// whole slice, one matrix after the other.
+constexpr int kValuesThreads = 256;
+struct ValuesArgs {
+  const uint8_t* x;
+  int64_t stride, rows, padded;  // rows of x, and of a term
+  int32_t row_bytes, groups;     // groups of 8 columns to a row of dpad
+  uint32_t inv_groups;
+  __nv_bfloat16* out;
+};
+__global__ void __launch_bounds__(kValuesThreads)
+terms_kernel(const ValuesArgs a) {
+  const FlatRows flat(blockIdx.x, a.groups, a.inv_groups);
+#pragma unroll
+  for (int u = 0; u < kFlat / kValuesThreads; ++u) {
+    int64_t row;
+    uint32_t g;
+    flat.at(threadIdx.x + u * kValuesThreads, &row, &g);
+    if (row >= a.padded) continue;
+    uint2 hi[2] = {}, lo[2] = {};
+    if (row < a.rows) {
+      const uint8_t* from = a.x + row * a.stride;
+      const float scale = __ldg((const float*)(from + a.row_bytes - 4));
+      const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);  // exact: it has eight bits
+      const uint2 w = __ldg((const uint2*)(from + g * 8));
+      int8_terms4(w.x, s2, hi[0], lo[0]);
+      int8_terms4(w.y, s2, hi[1], lo[1]);
+    }
+    const int64_t at = row * a.groups + g;  // in 16 bytes; columns past dim are not looked at
+    ((uint4*)a.out)[at] = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
+    ((uint4*)a.out)[a.padded * a.groups + at] = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+  }
+}
+
 // The shares' tiles added up: 32 rows of 64 / kDeal columns of a tile to a CTA, each value's
 // shares dealt out to kDeal threads, whose sums are added in order.  The CTAs behind the tiles'
 // have the bias.
@@ -437,8 +505,8 @@ join_kernel(const WeightArgs a) {
 // How the rows are shared out, and the workspace: partial tiles, partial biases, and the
 // gradient's terms where it cannot be taken as it is.
 struct WeightSpace {
-  bool pair;
-  int64_t slices, tiles_j, tiles_i, splits, per_split, wpad, bias, grad, bytes;
+  bool pair, ready;
+  int64_t slices, tiles_j, tiles_i, splits, per_split, wpad, dpad, bias, grad, values, bytes;
   WeightSpace(int64_t rows, int64_t width, int64_t dim, int32_t dtype, bool direct) {
     slices = ceil_div(rows, kSlice);
     tiles_j = ceil_div(width, kTile);
@@ -466,10 +534,19 @@ struct WeightSpace {
     per_split = slices ? ceil_div(slices, splits) : 0;
     bias = ceil_div(splits * tiles * kTileValues * 4, 256) * 256;
     grad = bias + ceil_div(splits * width * 16, 256) * 256;
-    bytes = rows > 0 && width > 0 ? grad + (direct ? 0 : grad_terms(dtype) * rows * wpad * 2) : 0;
+    values = grad + (direct ? 0 : ceil_div(grad_terms(dtype) * rows * wpad * 2, 256) * 256);
+    dpad = ceil_div(dim, 8) * 8;
+    // The scaled whole numbers made once, before, where many tiles share them and the products
+    // of a slice take least: 8192 rows of 2048 to 4096 columns, bfloat16, 232 us and 267 by each
+    // tile's own convert warps, 4096 x 256 to 4096 25.2 and 25.9.  Below, what they have to write
+    // and read costs more: 100,000 x 128 to 1024 61 and 55, 600 x 1024 to 4096 27.8 and 27.2;
+    // with a gradient of two terms 8192 x 2048 to 4096 384 and 379.
+    ready = dtype == AGNES_BF16 && tiles_j >= 16 && rows >= 4096;
+    bytes = rows > 0 && width > 0 ? values + (ready ? 2 * slices * kSlice * dpad * 2 : 0) : 0;
   }
   void shape(WeightArgs& a) const {
     a.pair = pair;
+    a.ready = ready;
     a.slices = (int32_t)slices;
     a.tiles_j = (int32_t)tiles_j;
     a.tiles_i = (int32_t)tiles_i;
@@ -479,25 +556,36 @@ struct WeightSpace {
 };
 
 template <typename TOut>
-cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, int device,
-                          cudaStream_t st) {
+cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride,
+                          __nv_bfloat16* values, int device, cudaStream_t st) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return cudaErrorNotSupported;
   CUtensorMap grad_map, x_map;
+  const int64_t padded = (int64_t)a.slices * kSlice, groups = ceil_div(a.dim, 8);
   if (!map_rows(encode, &grad_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, grad, a.width, a.ta * a.rows,
                 grad_stride, 64, kSlice, CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !map_rows(encode, &x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.x, a.dim, a.rows, a.x_stride,
-                a.pair ? kTile / 2 : kTile, kSlice,
-                a.pair ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
+      !(a.ready ? map_rows(encode, &x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, values, a.dim,
+                           2 * padded, groups * 16, 64, kSlice, CU_TENSOR_MAP_SWIZZLE_128B)
+                : map_rows(encode, &x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.x, a.dim, a.rows,
+                           a.x_stride, a.pair ? kTile / 2 : kTile, kSlice,
+                           a.pair ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B)))
     return cudaErrorInvalidValue;
-  const auto kernel = a.pair ? weight_kernel<true> : weight_kernel<false>;
-  static OncePerDevice once[2];
-  cudaError_t e = once[a.pair].run(device, [&] {
+  if (a.ready) {
+    const ValuesArgs v = {a.x, a.x_stride, a.rows, padded, a.row_bytes, (int32_t)groups,
+                          flat_inverse(groups), values};
+    terms_kernel<<<(unsigned)ceil_div(padded * groups, kFlat), kValuesThreads, 0, st>>>(v);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  const auto kernel = a.ready ? (a.pair ? weight_kernel<true, true> : weight_kernel<false, true>)
+                              : (a.pair ? weight_kernel<true, false> : weight_kernel<false, false>);
+  static OncePerDevice once[4];
+  cudaError_t e = once[2 * a.ready + a.pair].run(device, [&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
   });
   if (e != cudaSuccess) return e;
   a.chain = a.ta == 1 ? 5 : a.ta == 2 ? 2 : 1;  // some 16 to 20 products of 16
-  a.slot_bytes = a.ta * kGradBytes + value_bytes(a.pair) + raw_bytes(a.pair);
+  a.slot_bytes = a.ta * kGradBytes + value_bytes(a.pair) + raw_bytes(a.pair, a.ready);
   const int slots = kRingBytes / a.slot_bytes;
   a.slots = slots < kMaxSlots ? slots : kMaxSlots;
   const size_t smem = (size_t)kSmemLimit - kRingBytes + (size_t)a.slots * a.slot_bytes;
@@ -602,7 +690,8 @@ agnes_status agnes_int8_linear_grad_weight(const void* grad, int32_t grad_dtype,
   w.status = status;
   space.shape(w);
   return op_launched(op, with_float_type(out_dtype, [&](auto t) {
-    return launch_weight<typename decltype(t)::type>(w, a, a_stride, device, st);
+    return launch_weight<typename decltype(t)::type>(
+        w, a, a_stride, (__nv_bfloat16*)((uint8_t*)workspace + space.values), device, st);
   }));
 }
 

@@ -519,19 +519,22 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
       }
     }
   } else if (warp == kMmaWarp) {
-    if (lane == 0 && rank == 0) {
+    // the whole warp goes through the loop, so that its addresses are the same for all lanes and
+    // stay in uniform registers, as the products take them
+    if (rank == 0) {
+      const bool lead = elect_one();
       const auto commit = [](uint32_t b) {
         if constexpr (kPair)
           mma_commit_pair(b);
         else
           mma_commit(b);
       };
-      if (a.resident) ok = mbar_wait(bar.b_full(), 0);
+      if (a.resident) ok = __all_sync(0xffffffffu, mbar_wait(bar.b_full(), 0));
       Ring ring, acc;
       for (; ok && t.any(); t.next()) {
         for (int k0 = 0; ok && k0 < a.steps; k0 += a.chain) {
           const int d = acc.slot;
-          if (!acc.first && !mbar_wait(bar.taken(d), acc.parity ^ 1u)) {
+          if (!acc.first && !__all_sync(0xffffffffu, mbar_wait(bar.taken(d), acc.parity ^ 1u))) {
             ok = false;
             break;
           }
@@ -541,8 +544,9 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
           const int k1 = min(k0 + a.chain, a.steps);
           for (int k = k0; k < k1; ++k) {
             const int s = ring.slot;
-            if (!mbar_wait(bar.full(s), ring.parity) ||
-                ((kConvert || kPair) && !mbar_wait(bar.ready(s), ring.parity))) {
+            // what is ready is full as well
+            const uint32_t b = kConvert || kPair ? bar.ready(s) : bar.full(s);
+            if (!__all_sync(0xffffffffu, mbar_wait(b, ring.parity))) {
               ok = false;
               break;
             }
@@ -551,25 +555,29 @@ tile_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ C
             const uint32_t b_at =
                 a.resident ? resident_at + (uint32_t)(k * a.tb) * kBBytes : a_at + b_off;
             const int n = k + 1 == a.steps ? a.last : kSliceK / 16;
-            if (kConvert)
-              slice_products<1, 1, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
-            else if (a.ta == 1)
-              slice_products<1, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
-            else if (a.ta == 2)
-              slice_products<2, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
-            else
-              slice_products<3, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
+            if (lead) {
+              if (kConvert)
+                slice_products<1, 1, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
+              else if (a.ta == 1)
+                slice_products<1, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
+              else if (a.ta == 2)
+                slice_products<2, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
+              else
+                slice_products<3, 2, kBRows, kPair>(to, a_at, b_at, n, kIdesc, accumulate);
+              commit(bar.empty(s));
+            }
+            __syncwarp();
             accumulate = 1;
-            commit(bar.empty(s));
             ring.next(slots);
           }
           if (!ok) break;
-          commit(bar.done(d));
+          if (lead) commit(bar.done(d));
+          __syncwarp();
           acc.next(2);
         }
       }
       if (!ok) {  // the products in flight end before the tensor memory is freed
-        commit(bar.drained());
+        if (lead) commit(bar.drained());
         mbar_wait(bar.drained(), 0);
       }
     }

@@ -129,6 +129,17 @@ __device__ __forceinline__ void tmem_free_pair(uint32_t addr, uint32_t cols) {
                : "memory");
 }
 
+// True in one lane of a converged warp, the same one each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(yes));
+  return yes;
+}
+
 // What a kernel wrote to shared memory is there for the tensor core and the TMA.
 __device__ __forceinline__ void fence_async_proxy() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

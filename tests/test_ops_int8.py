@@ -469,6 +469,26 @@ def test_gradients_of_infinities_and_nan(cuda_device, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,width", [(4200, 2000), (4200, 2100), (700, 300)])
+def test_a_row_that_is_no_number_and_the_others(cuda_device, rows, width):
+    """Over a slice's end and the last rows, in all variants of the gradient to the weights."""
+    dim = 150
+    d, x, _ = _grad_inputs(rows, width, dim, torch.bfloat16)
+    clean = ops.int8_linear_grad_weight(d.to(cuda_device), x.to(cuda_device), dim)
+    assert clean.weight.isfinite().all() and clean.bias.isfinite().all()
+    d[rows - 1, 7] = math.inf
+    got = ops.int8_linear_grad_weight(d.to(cuda_device), x.to(cuda_device), dim)
+    assert not got.weight[7].isfinite().any() and not got.bias[7].isfinite()
+    got.weight[7], got.bias[7] = clean.weight[7], clean.bias[7]
+    assert torch.equal(got.weight, clean.weight) and torch.equal(got.bias, clean.bias)
+    # a row of x that stands for NaN enters all sums over the rows, the bias' not
+    d[rows - 1, 7] = 0
+    x[rows - 1, -4:] = torch.tensor([0xff, 0xff, 0xff, 0x7f], dtype=torch.uint8)
+    got = ops.int8_linear_grad_weight(d.to(cuda_device), x.to(cuda_device), dim)
+    assert got.weight.isnan().all() and got.bias.isfinite().all()
+
+
+@pytest.mark.gpu
 def test_gradients_are_the_same_each_time(cuda_device):
     d, x, w = _grad_inputs(30_000, 200, 150, torch.bfloat16)
     d, x, w = d.to(cuda_device), x.to(cuda_device), w.to(cuda_device)
@@ -508,7 +528,7 @@ def test_a_thousand_calls_give_the_same(cuda_device, rows, width, dim, dtype):
 @pytest.mark.parametrize("rows,width,dim", [
     (16, 130, 260), (17, 130, 260), (128, 128, 128), (129, 129, 129), (50_000, 257, 511),
     (50_000, 256, 512), (20_000, 384, 128), (20_000, 385, 128), (300, 64, 2048), (300, 64, 2049),
-    (64, 2048, 512)])
+    (64, 2048, 512), (4101, 1921, 130), (4096, 2060, 200), (4095, 1921, 72)])
 @pytest.mark.parametrize("dtype", FLOATS)
 def test_where_variants_meet(cuda_device, rows, width, dim, dtype):
     _product_check(cuda_device, rows, width, dim, dtype, True)

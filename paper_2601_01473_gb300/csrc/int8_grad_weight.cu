@@ -36,8 +36,8 @@ constexpr int kMmaWarp = kProducerWarp + 1;
 constexpr int kThreads = 32 * (kMmaWarp + 1);
 constexpr int kBox = kSlice * 128;           // 64 columns of a slice in 16 bits
 constexpr int kGradBytes = 2 * kBox;         // a term of the gradient
-// Of the scaled whole numbers' two terms and of the whole numbers, for a CTA of its own or one
-// of a pair.
+// Of the scaled whole numbers' two terms and of the whole numbers (none where the terms come
+// ready), for a CTA of its own or one of a pair.
 constexpr int value_bytes(bool pair) { return (pair ? 2 : 4) * kBox; }
 constexpr int raw_bytes(bool pair, bool ready) {
   return ready ? 0 : kSlice * kTile / (pair ? 2 : 1);
@@ -92,6 +92,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 weight_kernel(const __grid_constant__ CUtensorMap grad_map,
               const __grid_constant__ CUtensorMap x_map, const WeightArgs a) {
   grid_dep_wait();
+  static_assert(kPair || !kReady, "many tiles");
   constexpr uint32_t kIdesc = idesc_16bit(true, true, kPair ? 2 * kTile : kTile, 2 * kTile);
   constexpr int kValueBytes = value_bytes(kPair), kRawBytes = raw_bytes(kPair, kReady);
   const uint32_t rank = kPair ? cluster_rank() : 0;
@@ -222,8 +223,7 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
         for (int32_t k = c0; k < min(c0 + a.chain, k1); ++k) {
           const int s = ring.slot;
           // what is ready is full as well
-          const uint32_t b = !kReady || kPair ? bar.ready(s) : bar.full(s);
-          if (!__all_sync(0xffffffffu, mbar_wait(b, ring.parity))) {
+          if (!__all_sync(0xffffffffu, mbar_wait(bar.ready(s), ring.parity))) {
             ok = false;
             break;
           }
@@ -264,7 +264,7 @@ weight_kernel(const __grid_constant__ CUtensorMap grad_map,
     }
   } else if (warp >= kConvertWarp0 && kReady) {
     // one warp tells the pair's first CTA of this one's slices
-    if (kPair && warp == kConvertWarp0) {
+    if (warp == kConvertWarp0) {
       for (int32_t k = k0; k < k1; ++k) {
         if (!__all_sync(0xffffffffu, mbar_wait(bar.full(ring.slot), ring.parity))) {
           ok = false;
@@ -509,11 +509,11 @@ struct WeightSpace {
   int64_t slices, tiles_j, tiles_i, splits, per_split, wpad, dpad, bias, grad, values, bytes;
   WeightSpace(int64_t rows, int64_t width, int64_t dim, int32_t dtype, bool direct) {
     slices = ceil_div(rows, kSlice);
-    tiles_j = ceil_div(width, kTile);
-    // Pairs where all have both halves: 786,432 rows of 128 to 256 columns 116 us, 130 by CTAs of
-    // their own, 8192 of 2048 to 4096 306 and 330.  With half a pair idle, 100,000 rows of 300 to
-    // 600 columns took 135 us and take 124.
-    pair = tiles_j % 2 == 0;
+    // Pairs where there are two tiles: 786,432 rows of 128 to 256 columns 102 us, 130 by CTAs of
+    // their own, 8192 of 2048 to 4096 232 and 250; with half a pair idle, 100,000 of 300 to 600
+    // 118 and 126.
+    pair = width > kTile;
+    tiles_j = pair ? ceil_div(width, 2 * kTile) * 2 : 1;
     tiles_i = ceil_div(dim, kTile);
     wpad = ceil_div(width, 8) * 8;
     const int64_t tiles = tiles_j * tiles_i;
@@ -577,10 +577,11 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride,
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  const auto kernel = a.ready ? (a.pair ? weight_kernel<true, true> : weight_kernel<false, true>)
-                              : (a.pair ? weight_kernel<true, false> : weight_kernel<false, false>);
-  static OncePerDevice once[4];
-  cudaError_t e = once[2 * a.ready + a.pair].run(device, [&] {
+  const auto kernel = a.ready  ? weight_kernel<true, true>
+                      : a.pair ? weight_kernel<true, false>
+                               : weight_kernel<false, false>;
+  static OncePerDevice once[3];
+  cudaError_t e = once[a.pair + a.ready].run(device, [&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
   });
   if (e != cudaSuccess) return e;
@@ -593,9 +594,9 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride,
   e = launch_next_cluster(kernel, dim3((unsigned)(tiles * a.splits)), (unsigned)kThreads, smem,
                           a.pair ? 2u : 1u, st, grad_map, x_map, a);
   if (e != cudaSuccess) return e;
-  // Few shares: more values to a CTA; many: more threads to a value.  The gradient of 8192 rows
-  // of 2048 to 4096 columns (2 shares) takes 306 us, 328 in the other way; that of 20,000 rows
-  // of 128 to 128 (as many shares as SMs) 11.4 us, 23.7 in the first.
+  // Few shares: more values to a CTA; many: more threads to a value.  In the other way the
+  // gradient of 8192 rows of 2048 to 4096 columns (2 shares) takes 22 us more, that of 20,000
+  // rows of 128 to 128 (as many shares as SMs) 23.7 us and not 11.4.
   const bool few = a.splits <= 8;
   const int64_t ctas = tiles * (few ? 8 : 32) + (a.dbias ? ceil_div(a.width, 32) : 0);
   return launch_next(few ? join_kernel<TOut, 1> : join_kernel<TOut, 4>, dim3((unsigned)ctas),

@@ -828,6 +828,7 @@ cudaError_t launch_tiles(TileArgs a, const TileOperands& o, int device, cudaStre
   const int64_t tiles_m = ceil_div(a.rows, group * kTileM), tiles_n = ceil_div(a.cols, kCols);
   const int b_slice = a.tb * kCols * 128 / group;
   const int a_slice = a.ta * kOperandBytes + (kConvert ? kRawBytes : 0);
+  // 786,432 x 128 to 256 97 us, and 103 with B's slices copied for every tile
   a.resident = !kPair && tiles_n <= num_sms &&
                (int64_t)a.steps * b_slice + 3 * a_slice + kEpilogueWarps * kOutBytes <= tile_smem(kConvert);
   a.slot_bytes = a_slice + (a.resident ? 0 : b_slice);
@@ -885,15 +886,13 @@ template <typename TOut, bool kConvert>
 cudaError_t launch_product(const TileArgs& a, const TileOperands& o, bool drain, int device,
                            cudaStream_t st) {
   if (drain) return launch_tiles<TOut, kConvert, 128, true, false>(a, o, device, st);
+  // 786,432 x 128 to 128 68 us, and 82 by tiles of 256 columns
   if (a.cols <= 128) return launch_tiles<TOut, kConvert, 128, false, false>(a, o, device, st);
-  // A pair's turn of 256 rows takes 0.75 (bfloat16 terms) to 0.86 (whole numbers) of what two
-  // CTAs of their own take for theirs, where rows are long: 16,384 x 4096 to 4096 403 us and
-  // 469, the gradient of 8192 x 4096 to 2048 columns 158 and 212.  With fewer and larger tiles the
-  // last turn may be emptier: 6000 x 1024 to 4096 55 us and 50.
-  const int64_t tiles_n = ceil_div(a.cols, 256), sms = op_num_sms(device);
-  const int64_t turns = ceil_div(ceil_div(a.rows, kTileM) * tiles_n, sms);
-  const int64_t pair_turns = ceil_div(ceil_div(a.rows, 2 * kTileM) * tiles_n, sms / 2);
-  if (o.k >= 512 && sms >= 2 && pair_turns * 85 < turns * 100)
+  // Pairs for contractions of more than two slices: 16,384 x 4096 to 4096 356 us and 466 by CTAs
+  // of their own, 300,000 x 200 to 256 53 and 65, the gradient of 8192 x 4096 to 2048 columns 159
+  // and 220.  A pair's start costs 0.9 us more, and its B is not resident: 300 x 128 to 256 8.8
+  // and 7.9, 786,432 x 128 to 256 98.3 and 97.3.
+  if (o.k > 128 && op_num_sms(device) >= 2)
     return launch_tiles<TOut, kConvert, 256, false, true>(a, o, device, st);
   return launch_tiles<TOut, kConvert, 256, false, false>(a, o, device, st);
 }

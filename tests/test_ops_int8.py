@@ -528,7 +528,7 @@ def test_a_thousand_calls_give_the_same(cuda_device, rows, width, dim, dtype):
 @pytest.mark.parametrize("rows,width,dim", [
     (16, 130, 260), (17, 130, 260), (128, 128, 128), (129, 129, 129), (50_000, 257, 511),
     (50_000, 256, 512), (20_000, 384, 128), (20_000, 385, 128), (300, 64, 2048), (300, 64, 2049),
-    (64, 2048, 512), (4101, 1921, 130), (4096, 2060, 200), (4095, 1921, 72)])
+    (64, 2048, 512), (700, 300, 129), (4101, 1921, 130), (4096, 2060, 200), (4095, 1921, 72)])
 @pytest.mark.parametrize("dtype", FLOATS)
 def test_where_variants_meet(cuda_device, rows, width, dim, dtype):
     _product_check(cuda_device, rows, width, dim, dtype, True)

@@ -8,7 +8,16 @@
 // Few rows: the weights' bytes count, so a group of lanes takes a column's whole numbers,
 // four products an instruction, for all rows.
 // Otherwise the tensor cores (tcgen05.mma), in 16-bit operands: whole numbers are exact in
-// fp16, and a scaled one is the sum of two bfloat16 values (int8.cuh).
+// fp16, and a scaled one is the sum of two bfloat16 values (int8.cuh).  The weights are laid
+// out for them by a kernel before; the rows come as they are.  A persistent CTA, or a pair:
+//   the producer      has the TMA copy slices of 64 of the contraction;
+//   the convert warps make the rows' whole numbers fp16 (forward);
+//   the MMA warp      issues a slice's products into one of two accumulators;
+//   the epilogue warps scale the sums, add the bias and hand them to the TMA by way of shared
+//                     memory, while the next tile's products run.
+// Long rows are bound by the tensor cores (16,384 x 4096 to 4096, bf16: 357 us, 1540 TFLOP/s,
+// the tensor pipe 68% active; the gradient of 8192 x 4096 to 2048 159 us, two terms, 95%), short
+// ones by what they write (786,432 x 128 to 256, fp16: 97 us; a memset of the output takes 101).
 #include <type_traits>
 
 #include "int8_product.cuh"

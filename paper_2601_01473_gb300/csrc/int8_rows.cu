@@ -418,14 +418,6 @@ agnes_status check_kept(const char* op, const char* name, int64_t rows, int64_t 
   return AGNES_OK;
 }
 
-// How many batches of `groups` rows a CTA that stages them takes: some 48 KB of them, as a CTA
-// loads, works and stores in turn, but not fewer CTAs than the device runs at a time.
-int32_t stage_batches(int64_t rows, int32_t groups, int64_t row_bytes, int sms) {
-  const int64_t fit = 49152 / (groups * row_bytes), share = rows / (groups * (int64_t)sms * 4);
-  const int64_t n = fit < share ? fit : share;
-  return n < 1 ? 1 : (int32_t)n;
-}
-
 template <typename T, int kMode, bool kOut8>
 cudaError_t launch_keep(KeepArgs a, int device, cudaStream_t st) {
   const int64_t next = a.rows > 1 ? 1 : 0;  // a single row has no next one

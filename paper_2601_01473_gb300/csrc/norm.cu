@@ -52,6 +52,7 @@ struct NormArgs {
   void *sum, *next;
   int64_t sum_stride, next_stride;
   bool next_rows8;
+  int32_t batches, stage_at[5];  // of the staged rows: `groups` at a time, and their buffers
   // backward
   const void *d_next, *d_sum;
   int64_t d_next_stride, d_sum_stride;
@@ -254,28 +255,86 @@ struct NormRow {
   }
 };
 
-// kRows rows to a group at a time: the vectors over the columns are loaded once for all of
-// them, and the exchanges of their sums overlap.
-template <typename TX, typename TBranch, int kVec, int kPer, int kRows, int kLanes>
-__global__ void __launch_bounds__(kLanes ? kRowThreads : kNormLanes)
-norm_kernel(const NormArgs a) {
+// Where a group's rows are: in memory, or a batch of them in shared memory.
+template <typename TX, typename TBranch>
+struct NormRowsAt {
+  const NormArgs& a;
+  int64_t row0;
+  __device__ int64_t row(int r) const { return row0 + (int64_t)r * a.groups; }
+  __device__ bool valid(int r) const { return row(r) < a.rows; }
+  __device__ const TX* x(int r) const { return (const TX*)a.x + row(r) * a.x_stride; }
+  __device__ const TBranch* branch(int r) const {
+    return (const TBranch*)a.branch + row(r) * a.branch_stride;
+  }
+  __device__ const TBranch* gate(int r) const {
+    return (const TBranch*)a.gate + row(r) * a.gate_stride;
+  }
+  __device__ TX* sum(int r) const { return (TX*)a.sum + row(r) * a.sum_stride; }
+  __device__ TBranch* next(int r) const { return (TBranch*)a.next + row(r) * a.next_stride; }
+  __device__ uint8_t* next8(int r) const { return (uint8_t*)a.next + row(r) * a.next_stride; }
+};
+
+// A CTA's rows are one run of each matrix; a buffer in shared memory for each.
+template <typename TX, typename TBranch>
+struct NormStage {
+  const NormArgs& a;
+  uint8_t* base;
+  int64_t row0;
+  int rows, at;  // of the CTA; the group's
+  __device__ bool valid(int) const { return at < rows; }
+  template <typename T>
+  __device__ T* first(const void* p, int64_t stride) const {
+    return (T*)p + row0 * stride;
+  }
+  template <typename T>
+  __device__ T* in(int buffer, const void* p) const {
+    return (T*)(base + a.stage_at[buffer] + stage_offset(first<T>(p, a.dim))) + (int64_t)at * a.dim;
+  }
+  __device__ const TX* x(int) const { return in<TX>(0, a.x); }
+  __device__ const TBranch* branch(int) const { return in<TBranch>(1, a.branch); }
+  __device__ const TBranch* gate(int) const { return in<TBranch>(2, a.gate); }
+  __device__ TX* sum(int) const { return in<TX>(3, a.sum); }
+  __device__ TBranch* next(int) const { return in<TBranch>(4, a.next); }
+  __device__ uint8_t* next8(int) const { return base + a.stage_at[4] + at * a.next_stride; }
+  template <typename T>
+  __device__ void load_one(int buffer, const void* p) const {
+    stage_in(base + a.stage_at[buffer], first<T>(p, a.dim), rows * (int64_t)a.dim * (int64_t)sizeof(T),
+             p, first<T>(p, a.dim) + (a.rows - row0) * a.dim);
+  }
+  __device__ void load() const {
+    load_one<TX>(0, a.x);
+    if (a.branch) load_one<TBranch>(1, a.branch);
+    if (a.gate_kind == AGNES_GATE_ROWS) load_one<TBranch>(2, a.gate);
+    stage_wait();
+  }
+  __device__ void store() const {
+    __syncthreads();
+    if (a.branch)
+      stage_out(base + a.stage_at[3], first<TX>(a.sum, a.dim),
+                rows * (int64_t)a.dim * (int64_t)sizeof(TX));
+    if (!a.next) return;
+    if (a.next_rows8)
+      stage_out(base + a.stage_at[4], first<uint8_t>(a.next, a.next_stride), rows * a.next_stride);
+    else
+      stage_out(base + a.stage_at[4], first<TBranch>(a.next, a.dim),
+                rows * (int64_t)a.dim * (int64_t)sizeof(TBranch));
+  }
+};
+
+template <typename TX, typename TBranch, int kVec, int kPer, int kRows, int kLanes, typename At>
+__device__ __forceinline__ void norm_rows(const NormArgs& a, NormRow<kVec, kPer, kLanes>& n,
+                                          const At& at) {
   using Row = NormRow<kVec, kPer, kLanes>;
   constexpr int kPairs = Row::kPairs;
-  __shared__ RowScratch scratch;
-  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
-  Row n = {{a.lanes, lane, a.dim}, &scratch};
-  const int64_t row0 = ((int64_t)blockIdx.x * kRows) * a.groups + group;
   RowRegs<TX, kVec, kPer> x_regs[kRows];
   RowRegs<TBranch, kVec, kPer> b_regs[kRows], g_regs[kRows];
-  const auto row = [&](int r) { return row0 + (int64_t)r * a.groups; };
   const bool gate_rows = a.gate_kind == AGNES_GATE_ROWS;
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
-    const bool valid = row(r) < a.rows;
-    x_regs[r].load(n.part, (const TX*)a.x + row(r) * a.x_stride, valid);
-    if (a.branch)
-      b_regs[r].load(n.part, (const TBranch*)a.branch + row(r) * a.branch_stride, valid);
-    if (gate_rows) g_regs[r].load(n.part, (const TBranch*)a.gate + row(r) * a.gate_stride, valid);
+    const bool valid = at.valid(r);
+    x_regs[r].load(n.part, at.x(r), valid);
+    if (a.branch) b_regs[r].load(n.part, at.branch(r), valid);
+    if (gate_rows) g_regs[r].load(n.part, at.gate(r), valid);
   }
   Two x[kRows][kPairs], w[kPairs], b[kPairs];
   float inv[kRows];
@@ -308,7 +367,7 @@ norm_kernel(const NormArgs a) {
       Row::unpack(x_regs[r], x[r]);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) x[r][e] = rounded<TX>(fma2(w[e], u[r][e], x[r][e]));
-      n.store((TX*)a.sum + row(r) * a.sum_stride, row(r) < a.rows, x[r]);
+      n.store(at.sum(r), at.valid(r), x[r]);
     }
   } else {
 #pragma unroll
@@ -334,12 +393,12 @@ norm_kernel(const NormArgs a) {
                                  __float_as_uint(f.y) & 0x7fffffffu));
       }
     }
-    group_reduce<MaxBits, kLanes>(top, a.lanes, &scratch, n.turn);
+    group_reduce<MaxBits, kLanes>(top, a.lanes, n.scratch, n.turn);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       const Int8Scale s = int8_scale(top[r]);
-      uint8_t* to = (uint8_t*)a.next + row(r) * a.next_stride;
-      const bool valid = row(r) < a.rows;
+      uint8_t* to = at.next8(r);
+      const bool valid = at.valid(r);
       float f[2 * kPairs];
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) {
@@ -349,13 +408,42 @@ norm_kernel(const NormArgs a) {
       }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) int8_store(n.part, to, valid, i, f + i * kVec, s);
-      int8_store_end(to, a.dim, lane, a.lanes, valid, s);
+      int8_store_end(to, a.dim, n.part.lane, a.lanes, valid, s);
     }
   } else {
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
-      n.store((TBranch*)a.next + row(r) * a.next_stride, row(r) < a.rows, x[r]);
+      n.store(at.next(r), at.valid(r), x[r]);
   }
+}
+
+// kRows rows to a group at a time: the vectors over the columns are loaded once for all of
+// them, and the exchanges of their sums overlap.
+template <typename TX, typename TBranch, int kVec, int kPer, int kRows, int kLanes>
+__global__ void __launch_bounds__(kLanes ? kRowThreads : kNormLanes)
+norm_kernel(const NormArgs a) {
+  __shared__ RowScratch scratch;
+  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
+  NormRow<kVec, kPer, kLanes> n = {{a.lanes, lane, a.dim}, &scratch};
+  const NormRowsAt<TX, TBranch> at = {a, ((int64_t)blockIdx.x * kRows) * a.groups + group};
+  norm_rows<TX, TBranch, kVec, kPer, kRows, kLanes>(a, n, at);
+}
+
+// Rows that no vector divides, of contiguous matrices, through shared memory: STAGED_FIGURES
+template <typename TX, typename TBranch, int kPer>
+__global__ void __launch_bounds__(kNormLanes, 2)
+norm_staged_kernel(const NormArgs a) {
+  __shared__ RowScratch scratch;
+  extern __shared__ uint4 norm_smem[];
+  const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
+  NormRow<1, kPer> n = {{a.lanes, lane, a.dim}, &scratch};
+  const int64_t row0 = (int64_t)blockIdx.x * a.groups * a.batches, left = a.rows - row0;
+  const int most = a.groups * a.batches;
+  NormStage<TX, TBranch> at = {a, (uint8_t*)norm_smem, row0, left < most ? (int)left : most, group};
+  at.load();
+  for (int batch = 0; batch < a.batches; ++batch, at.at += a.groups)
+    norm_rows<TX, TBranch, 1, kPer, 1, 0>(a, n, at);
+  at.store();
 }
 
 // A thread's sums over the rows: in registers, or (kShared) in shared memory, where a thread
@@ -847,6 +935,36 @@ void set_shape(NormArgs& a, const RowShape& shape) {
   a.inv_dim = 1.f / (float)a.dim;
 }
 
+// Of matrices that are one run each.
+template <typename TX, typename TBranch>
+cudaError_t launch_staged(NormArgs a, int device, cudaStream_t st) {
+  set_shape(a, row_shape(a.dim, kElems, kNormLanes));
+  const int64_t x_row = a.dim * (int64_t)sizeof(TX), b_row = a.dim * (int64_t)sizeof(TBranch);
+  const int64_t next_row = !a.next ? 0 : a.next_rows8 ? int8_row_bytes(a.dim) : b_row;
+  const int64_t row[5] = {x_row, a.branch ? b_row : 0, a.gate_kind == AGNES_GATE_ROWS ? b_row : 0,
+                          a.branch ? x_row : 0, next_row};
+  a.next_stride = a.next_rows8 ? int8_row_bytes(a.dim) : a.dim;
+  a.batches = stage_batches(a.rows, a.groups, row[0] + row[1] + row[2] + row[3] + row[4],
+                            op_num_sms(device));
+  const int64_t rows = a.groups * (int64_t)a.batches;
+  int64_t smem = 0;
+  for (int k = 0; k < 5; ++k) {
+    a.stage_at[k] = (int32_t)smem;
+    if (row[k]) smem += staged_bytes(rows * row[k]);
+  }
+  const int per = (a.dim + a.lanes - 1) / a.lanes, which = per <= 10 ? 0 : per <= 12 ? 1 : 2;
+  const auto kernel = which == 0   ? norm_staged_kernel<TX, TBranch, 10>
+                      : which == 1 ? norm_staged_kernel<TX, TBranch, 12>
+                                   : norm_staged_kernel<TX, TBranch, kElems>;
+  static OncePerDevice once[3];  // the longest rows take 132 KB
+  const cudaError_t e = once[which].run(device, [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  });
+  if (e != cudaSuccess) return e;
+  kernel<<<(unsigned)ceil_div(a.rows, rows), (unsigned)(a.lanes * a.groups), (size_t)smem, st>>>(a);
+  return cudaGetLastError();
+}
+
 // CTAs of the backward pass: each writes a row of partial sums, so no more than keep the
 // device busy.
 int64_t grad_ctas(int64_t rows, int64_t dim, int sms) {
@@ -964,9 +1082,17 @@ agnes_status agnes_residual_norm(const void* x, int32_t x_dtype, int64_t x_strid
                         .rows(branch ? sum : nullptr, sum_stride, x_size)
                         .rows(a.next_rows8 ? nullptr : a.next, next_stride, branch_size)
                         .ok();
+  const auto one_run = [&](int64_t stride) { return rows == 1 || stride == dim; };
+  const bool contiguous = one_run(x_stride) && (!branch || (one_run(branch_stride) && one_run(sum_stride))) &&
+                          (gate_kind != AGNES_GATE_ROWS || one_run(gate_stride)) &&
+                          (!before || (a.next_rows8 ? rows == 1 || next_stride == int8_row_bytes(dim)
+                                                    : one_run(next_stride)));
   return op_launched(op, with_norm_types(x_dtype, branch_dtype, [&](auto tx, auto tb) {
     using TX = typename decltype(tx)::type;
     using TBranch = typename decltype(tb)::type;
+    if constexpr (sizeof(TBranch) == 2)
+      if (!wide && contiguous)
+        return launch_staged<TX, TBranch>(a, device, (cudaStream_t)cuda_stream);
     const bool brief = wide && dim <= kShortDim;
     set_shape(a, brief ? short_shape(dim) : row_shape(dim, kElems, kNormLanes));
     const auto kernel = !wide          ? norm_kernel<TX, TBranch, 1, kElems, 1, 0>

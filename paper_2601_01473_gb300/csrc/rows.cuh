@@ -229,6 +229,14 @@ __device__ __forceinline__ void stage_out(const uint8_t* buffer, void* p, int64_
   }
 }
 
+// How many batches of `groups` rows a CTA that stages them takes: some 48 KB of them, as a CTA
+// loads, works and stores in turn, but not fewer CTAs than the device runs at a time.
+inline int32_t stage_batches(int64_t rows, int32_t groups, int64_t row_bytes, int sms) {
+  const int64_t fit = 49152 / (groups * row_bytes), share = rows / (groups * (int64_t)sms * 4);
+  const int64_t n = fit < share ? fit : share;
+  return n < 1 ? 1 : (int32_t)n;
+}
+
 struct SumOp {
   using type = float;
   static __device__ float identity() { return 0.f; }

@@ -352,6 +352,34 @@ def test_strides_and_in_place(cuda_device):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim,types", [(20_011, 301, 1), (30_003, 100, 1), (6001, 350, 4),
+                                            (1301, 500, 2), (17, 8191, 4), (700, 7, 2)])
+def test_runs_of_odd_rows_from_any_element_on(cuda_device, rows, dim, types):
+    """Rows that no vector divides, several batches to a CTA and an empty end, next to what others own."""
+    c, _, _ = make(rows, dim, TYPES[types], "layer", True, "rows", True)
+    want, want_next = check_forward(cuda_device, c)
+    want8 = check_forward(cuda_device, c, rows8=True)[1]
+    c = on(cuda_device, c)
+
+    def run(t, first):
+        flat = torch.full((rows * dim + 32,), 7.0, dtype=t.dtype, device=cuda_device)
+        v = flat[first:first + rows * dim].view(rows, dim)
+        v.copy_(t)
+        return flat, v
+
+    for first in (1, 5):
+        _, x = run(c["x"], first)
+        moved = dict(c, x=x, branch=run(c["branch"], first + 2)[1], gate=run(c["gate"], 3)[1])
+        flat, out = run(c["x"], first + 1)
+        got = ops.residual_norm(**moved, out=out)
+        assert torch.equal(got.sum, want) and torch.equal(got.next, want_next)
+        assert (flat[:first + 1] == 7).all() and (flat[first + 1 + rows * dim:] == 7).all()
+        assert torch.equal(ops.residual_norm(**moved, rows8=True).next, want8)
+        got = ops.residual_norm(**moved, out=x)  # in place
+        assert got.sum is x and torch.equal(x, want) and torch.equal(got.next, want_next)
+
+
+@pytest.mark.gpu
 def test_rows_of_zeros_of_one_value_and_of_what_is_not_finite(cuda_device):
     c, d_next, d_sum = make(6, 64, TYPES[0], "layer", True, "columns", True)
     c["branch"][1] = 0

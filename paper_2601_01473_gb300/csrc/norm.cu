@@ -59,6 +59,7 @@ struct NormArgs {
   void *dx, *dbranch, *dgate;
   int64_t dx_stride, dbranch_stride, dgate_stride;
   int32_t stages, stage_off;  // of the copies ahead, and where they lie, in 16 bytes
+  int32_t run_at[8], run_stage;  // of staged runs: the buffers, and a stage's bytes
   float* partial;      // [CTAs][sums][dim]
   int32_t slot[kSums];  // a sum's place among them, or -1
   int32_t sums;
@@ -639,8 +640,67 @@ struct GradRow {
   }
 };
 
+// The same of rows that no vector divides, of contiguous matrices: the rows that a CTA has at a
+// time are one run of each matrix, which lies in shared memory, a turn ahead; what they give
+// goes out by runs, too.
+enum { kRunX, kRunDSum, kRunDNext, kRunBranch, kRunGate, kRunDx, kRunDBranch, kRunDGate };
+template <typename TX, typename TBranch>
+struct GradRun {
+  const NormArgs& a;
+  uint8_t* base;
+  int group;
+  int64_t first = 0;  // of the turn
+  int stage = 0;
+  __device__ int rows(int64_t from) const {
+    const int64_t left = a.rows - from;
+    return left < a.groups ? (int)left : a.groups;
+  }
+  template <typename T>
+  __device__ void start_one(int buffer, const void* p, int64_t from, int to_stage) const {
+    if (!p) return;
+    const T* at = (const T*)p + from * a.dim;
+    stage_in(base + to_stage * a.run_stage + a.run_at[buffer], at,
+             rows(from) * (int64_t)a.dim * (int64_t)sizeof(T), p, (const T*)p + a.rows * a.dim);
+  }
+  // one group of copies each, past the end too, so that the wait's count holds
+  __device__ void start(int64_t from, int to_stage) const {
+    if (from < a.rows) {
+      start_one<TX>(kRunX, a.before ? a.x : nullptr, from, to_stage);
+      start_one<TX>(kRunDSum, a.d_sum, from, to_stage);
+      start_one<TBranch>(kRunDNext, a.before ? a.d_next : nullptr, from, to_stage);
+      start_one<TBranch>(kRunBranch, a.branch, from, to_stage);
+      start_one<TBranch>(kRunGate, a.gate_kind == AGNES_GATE_ROWS ? a.gate : nullptr, from, to_stage);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  __device__ void wait() const {
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncthreads();
+  }
+  template <typename T>
+  __device__ const T* in(int buffer, const void* p) const {
+    return (const T*)(base + stage * a.run_stage + a.run_at[buffer] +
+                      stage_offset((const T*)p + first * a.dim)) + group * a.dim;
+  }
+  template <typename T>
+  __device__ T* out(int buffer, void* p) const {
+    return (T*)(base + a.run_at[buffer] + stage_offset((T*)p + first * a.dim)) + group * a.dim;
+  }
+  template <typename T>
+  __device__ void store_one(int buffer, void* p) const {
+    stage_out(base + a.run_at[buffer], (T*)p + first * a.dim,
+              rows(first) * (int64_t)a.dim * (int64_t)sizeof(T));
+  }
+  __device__ void store() const {
+    __syncthreads();
+    store_one<TX>(kRunDx, a.dx);
+    if (a.branch) store_one<TBranch>(kRunDBranch, a.dbranch);
+    if (a.gate_kind == AGNES_GATE_ROWS) store_one<TBranch>(kRunDGate, a.dgate);
+  }
+};
+
 template <typename TX, typename TBranch, int kVec, int kPer, int kThreads, bool kBias, bool kShared,
-          int kLanes>
+          int kLanes, bool kRun = false>
 __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 2 : 1)
 norm_grad_kernel(const NormArgs a) {
   using Row = NormRow<kVec, kPer, kLanes>;
@@ -668,28 +728,47 @@ norm_grad_kernel(const NormArgs a) {
                                          a.stages};
   for (int k = 0; k + 1 < a.stages; ++k)
     in.start((int64_t)blockIdx.x * a.groups + group + k * step, k);
+  GradRun<TX, TBranch> run = {a, (uint8_t*)(grad_smem + a.stage_off), group};
+  if constexpr (kRun) run.start((int64_t)blockIdx.x * a.groups, 0);
   int slot = 0, fill = a.stages - 1;
   for (int64_t first = (int64_t)blockIdx.x * a.groups; first < a.rows; first += step) {
     const int64_t row = first + group;
     const bool valid = row < a.rows;
     Two d[kPairs], w[kPairs], n[kPairs], branch[kPairs];
     float inv, branch_inv;
-    in.start(row + (a.stages - 1) * step, fill);
-    in.wait();
+    if constexpr (kRun) {
+      run.first = first;
+      run.start(first + step, run.stage ^ 1);
+      run.wait();
+    } else {
+      in.start(row + (a.stages - 1) * step, fill);
+      in.wait();
+    }
     if (a.d_sum) {
-      in.d_sum(row, slot, d);
+      if constexpr (kRun)
+        r.load(run.template in<TX>(kRunDSum, a.d_sum), valid, d);
+      else
+        in.d_sum(row, slot, d);
     } else {
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) d[e] = both(0.f);
     }
     Two g[kPairs];
-    if (a.before) {
-      in.x(row, slot, n);
-      in.d_next(row, slot, g);
+    if constexpr (kRun) {
+      if (a.before) {
+        r.load(run.template in<TX>(kRunX, a.x), valid, n);
+        r.load(run.template in<TBranch>(kRunDNext, a.d_next), valid, g);
+      }
+      if (a.branch) r.load(run.template in<TBranch>(kRunBranch, a.branch), valid, branch);
+    } else {
+      if (a.before) {
+        in.x(row, slot, n);
+        in.d_next(row, slot, g);
+      }
+      if (a.branch) in.branch(row, slot, branch);
+      if (++slot == a.stages) slot = 0;
+      if (++fill == a.stages) fill = 0;
     }
-    if (a.branch) in.branch(row, slot, branch);
-    if (++slot == a.stages) slot = 0;
-    if (++fill == a.stages) fill = 0;
     r.standard_of(n, a.before, branch, a.after, a.layer, a.eps, a.inv_dim, inv, branch_inv);
     if (a.before) {
       vector(kBeforeVector, a.before, 1.f, w);
@@ -708,8 +787,14 @@ norm_grad_kernel(const NormArgs a) {
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) d[e] = d[e] + g[e];
     }
-    r.store((TX*)a.dx + row * a.dx_stride, valid, d);
-    if (!a.branch) continue;
+    r.store(kRun ? run.template out<TX>(kRunDx, a.dx) : (TX*)a.dx + row * a.dx_stride, valid, d);
+    if (!a.branch) {
+      if constexpr (kRun) {
+        run.store();
+        run.stage ^= 1;
+      }
+      continue;
+    }
     if (a.after) {
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) branch[e] = branch[e] * both(branch_inv);
@@ -725,13 +810,15 @@ norm_grad_kernel(const NormArgs a) {
       for (int e = 0; e < kPairs; ++e) b[e] = fma2(branch[e], w[e], b[e]);
       if (a.gate_kind == AGNES_GATE_ROWS) {
         Two gate[kPairs];
-        r.load((const TBranch*)a.gate + row * a.gate_stride, valid, gate);
+        r.load(kRun ? run.template in<TBranch>(kRunGate, a.gate)
+                    : (const TBranch*)a.gate + row * a.gate_stride, valid, gate);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
           b[e] = d[e] * b[e];
           d[e] = d[e] * gate[e];
         }
-        r.store((TBranch*)a.dgate + row * a.dgate_stride, valid, b);
+        r.store(kRun ? run.template out<TBranch>(kRunDGate, a.dgate)
+                     : (TBranch*)a.dgate + row * a.dgate_stride, valid, b);
       } else {
         if (valid) {
 #pragma unroll
@@ -756,7 +843,12 @@ norm_grad_kernel(const NormArgs a) {
       for (int e = 0; e < kPairs; ++e) d[e] = d[e] * w[e];
       r.through(d, branch, a.layer, branch_inv, a.inv_dim);
     }
-    r.store((TBranch*)a.dbranch + row * a.dbranch_stride, valid, d);
+    r.store(kRun ? run.template out<TBranch>(kRunDBranch, a.dbranch)
+                 : (TBranch*)a.dbranch + row * a.dbranch_stride, valid, d);
+    if constexpr (kRun) {
+      run.store();
+      run.stage ^= 1;
+    }
   }
   // a CTA's sums: its groups' added in order
 #pragma unroll
@@ -985,35 +1077,60 @@ constexpr int kMostSms = 256;  // for the size of a workspace, whatever device i
 size_t dim_smem(const NormArgs& a) { return (size_t)a.lanes * kShortElems * 4; }
 
 template <typename TX, typename TBranch, bool kBias>
-cudaError_t launch_grad(NormArgs a, bool wide, int64_t ctas, size_t smem, int device,
-                        cudaStream_t st) {
+cudaError_t launch_grad(NormArgs a, bool wide, bool contiguous, int64_t ctas, size_t smem,
+                        int device, cudaStream_t st) {
   using Kernel = void (*)(NormArgs);
   constexpr int kPer = kShortElems;
   // With a residual in fp32 a thread has two vectors of four columns, so that each access of
   // a warp is one run of memory (16,384 x 4096, bf16 branch, 253 us; with eight columns to a
   // thread 346 past L1 and 328 through it).
   constexpr int kV = sizeof(TX) == 4 ? 4 : 8, kP = kShortElems / kV;
-  const Kernel kernels[7] = {norm_grad_kernel<TX, TBranch, kV, kP, 1024, kBias, true, 0>,
+  const Kernel kernels[8] = {norm_grad_kernel<TX, TBranch, kV, kP, 1024, kBias, true, 0>,
                              norm_grad_kernel<TX, TBranch, 1, kPer, 1024, kBias, true, 0>,
                              norm_grad_kernel<TX, TBranch, 1, kPer, 512, kBias, false, 0>,
                              norm_grad_kernel<TX, TBranch, kV, kP, 512, kBias, false, 0>,
                              norm_grad_kernel<TX, TBranch, kV, kP, 256, kBias, false, 8>,
                              norm_grad_kernel<TX, TBranch, kV, kP, 256, kBias, false, 16>,
-                             norm_grad_kernel<TX, TBranch, kV, kP, 256, kBias, false, 32>};
-  const int which = a.lanes > 512 ? (wide ? 0 : 1) : !wide ? 2 : a.lanes > 32 ? 3
+                             norm_grad_kernel<TX, TBranch, kV, kP, 256, kBias, false, 32>,
+                             norm_grad_kernel<TX, TBranch, 1, kPer, 512, kBias, false, 0, true>};
+  int which = a.lanes > 512 ? (wide ? 0 : 1) : !wide ? 2 : a.lanes > 32 ? 3
                     : a.lanes == 8 ? 4 : a.lanes == 16 ? 5 : 6;
-  const Kernel kernel = kernels[which];
   // as many rows ahead as there is room for in the 227 KB of an SM's CTAs
   a.stages = 1;
   a.stage_off = (int32_t)ceil_div((int64_t)smem, 16);
-  if (which >= 3) {
+  // with more than two turns: 200,000 x 301 fp16 718 us, 871 by single elements, all in fp32 678
+  // and 742, 500,000 x 100 fp16 382 and 488; in one turn 100 x 301 takes 11.6 and 9.9
+  if (which == 2 && contiguous && a.rows > 2 * ctas * a.groups) {
+    const int64_t x_run = staged_bytes(a.groups * (int64_t)a.dim * (int64_t)sizeof(TX));
+    const int64_t b_run = staged_bytes(a.groups * (int64_t)a.dim * (int64_t)sizeof(TBranch));
+    const bool gate = a.gate_kind == AGNES_GATE_ROWS;
+    const int64_t bytes[8] = {a.before ? x_run : 0, a.d_sum ? x_run : 0, a.before ? b_run : 0,
+                              a.branch ? b_run : 0, gate ? b_run : 0, x_run, a.branch ? b_run : 0,
+                              gate ? b_run : 0};
+    int64_t at = 0;
+    for (int k = 0; k < 5; ++k) {
+      a.run_at[k] = (int32_t)at;
+      at += bytes[k];
+    }
+    a.run_stage = (int32_t)at;
+    at *= 2;
+    for (int k = 5; k < 8; ++k) {
+      a.run_at[k] = (int32_t)at;
+      at += bytes[k];
+    }
+    if ((int64_t)a.stage_off * 16 + at <= 224 * 1024) {
+      which = 7;
+      smem = (size_t)a.stage_off * 16 + (size_t)at;
+    }
+  } else if (which >= 3) {
     const int threads = a.lanes * a.groups;
     const size_t stage = (size_t)GradRow<TX, TBranch, kV, kP, true, 0>::kPieces * 16 * threads;
     const size_t room = (threads <= 256 ? 110 : 224) * 1024 - (size_t)a.stage_off * 16;
     a.stages = (int32_t)std::min((size_t)4, room / stage);
     smem = (size_t)a.stage_off * 16 + a.stages * stage;
   }
-  static OncePerDevice once[7];
+  const Kernel kernel = kernels[which];
+  static OncePerDevice once[8];
   const cudaError_t e = once[which].run(device, [&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
   });
@@ -1221,6 +1338,14 @@ agnes_status agnes_residual_norm_grad(
                         .rows(gate_kind == AGNES_GATE_ROWS ? dgate : nullptr, dgate_stride,
                               branch_size)
                         .ok();
+  const auto one_run = [&](const void* p, int64_t stride) {
+    return !p || rows == 1 || stride == dim;
+  };
+  const bool contiguous =
+      one_run(sum, sum_stride) && one_run(branch, branch_stride) && one_run(d_sum, d_sum_stride) &&
+      one_run(before ? d_next : nullptr, d_next_stride) && one_run(dx, dx_stride) &&
+      one_run(branch ? dbranch : nullptr, dbranch_stride) &&
+      (gate_kind != AGNES_GATE_ROWS || (one_run(gate, gate_stride) && one_run(dgate, dgate_stride)));
   const bool biases = dbefore_bias || dafter_bias, shared = a.lanes > 512;
   // the sums; or the vectors, and in their place a group's share of a sum at the end
   const size_t smem = shared ? (size_t)(biases ? kSums : kBeforeBias) * dim_smem(a)
@@ -1229,8 +1354,8 @@ agnes_status agnes_residual_norm_grad(
   const cudaError_t e = with_norm_types(x_dtype, branch_dtype, [&](auto tx, auto tb) {
     using TX = typename decltype(tx)::type;
     using TBranch = typename decltype(tb)::type;
-    return biases ? launch_grad<TX, TBranch, true>(a, wide, ctas, smem, device, st)
-                  : launch_grad<TX, TBranch, false>(a, wide, ctas, smem, device, st);
+    return biases ? launch_grad<TX, TBranch, true>(a, wide, contiguous, ctas, smem, device, st)
+                  : launch_grad<TX, TBranch, false>(a, wide, contiguous, ctas, smem, device, st);
   });
   OP_TRY(op_launched(op, e));
   if (!a.sums) return AGNES_OK;

@@ -356,8 +356,9 @@ def test_strides_and_in_place(cuda_device):
                                             (1301, 500, 2), (17, 8191, 4), (700, 7, 2)])
 def test_runs_of_odd_rows_from_any_element_on(cuda_device, rows, dim, types):
     """Rows that no vector divides, several batches to a CTA and an empty end, next to what others own."""
-    c, _, _ = make(rows, dim, TYPES[types], "layer", True, "rows", True)
+    c, d_next, d_sum = make(rows, dim, TYPES[types], "layer", True, "rows", True)
     want, want_next = check_forward(cuda_device, c)
+    grads = check_backward(cuda_device, c, want, d_next, d_sum)
     want8 = check_forward(cuda_device, c, rows8=True)[1]
     c = on(cuda_device, c)
 
@@ -375,6 +376,10 @@ def test_runs_of_odd_rows_from_any_element_on(cuda_device, rows, dim, types):
         assert torch.equal(got.sum, want) and torch.equal(got.next, want_next)
         assert (flat[:first + 1] == 7).all() and (flat[first + 1 + rows * dim:] == 7).all()
         assert torch.equal(ops.residual_norm(**moved, rows8=True).next, want8)
+        rest = {k: v for k, v in moved.items() if k != "x"}
+        got = ops.residual_norm_grad(run(d_next, first)[1], run(d_sum, first + 4)[1],
+                                     run(want, 2)[1], **rest)
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))
         got = ops.residual_norm(**moved, out=x)  # in place
         assert got.sum is x and torch.equal(x, want) and torch.equal(got.next, want_next)
 

@@ -17,23 +17,53 @@ __device__ __forceinline__ void int8_split(float v, float& hi, float& lo) {
   lo = fabsf(hi) <= 3.4e38f ? v - hi : 0.f;
 }
 
-// Four whole numbers times a scale (a bfloat16 value, twice in `scale`) as pairs of bfloat16
-// terms: hi the rounded products, lo what they leave, exactly.  A byte is its lower seven
+// A row's scale, for the terms of its whole numbers.
+struct Int8TermScale {
+  float value;
+  __nv_bfloat162 twice;
+  bool brief;  // packed bfloat16 arithmetic makes the terms
+  __device__ explicit Int8TermScale(float scale)
+      : value(scale), twice(__float2bfloat162_rn(scale)) {
+    // up to 2^121, 127 times it rounds to a finite bfloat16 value
+    brief = (__float_as_uint(scale) & 0x7fffffffu) <= 0x7c000000u;
+  }
+};
+
+// Four whole numbers times a scale as pairs of bfloat16 terms that add up to it exactly.
+// Brief ones: hi the rounded products, lo what they leave.  A byte is its lower seven
 // bits less 128 times its sign, and 128 + seven bits, 128 and 256 are bfloat16 bit patterns
 // of the byte's parts.
-__device__ __forceinline__ void int8_terms4(uint32_t word, __nv_bfloat162 scale, uint2& hi,
+// Others (a row with its type's largest number, whose products round past bfloat16's, and one
+// that stands for NaN), where the caller has not ruled them out (kBrief): in fp32, hi the leading
+// eight bits.
+template <bool kBrief>
+__device__ __forceinline__ void int8_terms4(uint32_t word, const Int8TermScale& scale, uint2& hi,
                                             uint2& lo) {
-  const uint32_t size = word & 0x7f7f7f7fu, sign = word & 0x80808080u;
   uint32_t* h = &hi.x;
   uint32_t* l = &lo.x;
+  if (!kBrief && !scale.brief) {
+    float q[4], rest[4];
+    int8_values4(word, q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) int8_split(q[e] * scale.value, q[e], rest[e]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __nv_bfloat162 top = __floats2bfloat162_rn(q[2 * i], q[2 * i + 1]);
+      const __nv_bfloat162 left = __floats2bfloat162_rn(rest[2 * i], rest[2 * i + 1]);
+      h[i] = *(const uint32_t*)&top;
+      l[i] = *(const uint32_t*)&left;
+    }
+    return;
+  }
+  const uint32_t size = word & 0x7f7f7f7fu, sign = word & 0x80808080u;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const uint32_t pick = i ? 0x4342 : 0x4140;
     const uint32_t a = __byte_perm(size, 0x43434343u, pick);
     const uint32_t b = __byte_perm(sign, 0x43434343u, pick);
     const __nv_bfloat162 q = __hsub2(*(const __nv_bfloat162*)&a, *(const __nv_bfloat162*)&b);
-    const __nv_bfloat162 top = __hmul2(q, scale);
-    const __nv_bfloat162 rest = __hfma2(q, scale, __hneg2(top));
+    const __nv_bfloat162 top = __hmul2(q, scale.twice);
+    const __nv_bfloat162 rest = __hfma2(q, scale.twice, __hneg2(top));
     h[i] = *(const uint32_t*)&top;
     l[i] = *(const uint32_t*)&rest;
   }

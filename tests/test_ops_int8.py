@@ -675,3 +675,61 @@ def test_offsets_past_32_bits(cuda_device):
     assert_within(dx[at], ref, _product_bound(ref, size, width, dx.dtype))
     assert int((dx != 0).any(1).sum()) <= 7
     ops.check()
+
+
+# ---- the largest numbers of a type -----------------------------------------------------------
+
+def _with_the_largest(rows, dim, dtype, seed):
+    """8-bit rows, of which row 5 and the last have their type's lowest number (the usual mask) and
+    its largest beside ordinary values.  They stand for finite numbers that round to infinity in
+    bfloat16."""
+    x = values(rows, dim, seed).to(dtype)
+    x[5, 7], x[rows - 1, 3] = torch.finfo(dtype).min, torch.finfo(dtype).max
+    packed = reference_rows(x)
+    most = reference_values(packed, dim).abs().amax(1)[[5, rows - 1]]
+    assert (most < 2.0 ** 128).all() and most.float().bfloat16().isinf().all()
+    return packed
+
+
+# a CTA to a tile, pairs, pairs with the scaled whole numbers made before
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,width", [(90, 70), (700, 300), (4200, 2000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("grad", FLOATS)
+def test_gradient_to_the_weights_of_rows_with_the_largest_numbers(cuda_device, rows, width, dtype,
+                                                                  grad):
+    dim = 150
+    x = _with_the_largest(rows, dim, dtype, 1)
+    xv = reference_values(x, dim).to(cuda_device)
+    d = (values(rows, width, 3) / 64).to(grad)
+    assert d.isfinite().all()
+    for weight in (0.0, 2.0 ** -20, 1.0):
+        d[5], d[rows - 1] = 0, 0
+        d[5, 2], d[rows - 1, 4] = weight, -weight
+        got = ops.int8_linear_grad_weight(d.to(cuda_device), x.to(cuda_device), dim).weight
+        dd = d.double().to(cuda_device)
+        ref, size = dd.t() @ xv, dd.abs().t() @ xv.abs()
+        assert got.isfinite().all()
+        assert_within(got, ref, (rows + 8) * 2 * U32 * size + 1.01 * rounding(ref, got.dtype))
+    ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("grad", FLOATS)
+def test_gradient_to_the_input_of_weights_with_the_largest_numbers(cuda_device, dtype, grad):
+    rows, width, dim = 130, 200, 150
+    w = _with_the_largest(width, dim, dtype, 2)
+    wv = reference_values(w, dim).to(cuda_device)
+    d = (values(rows, width, 3) / 64).to(grad)
+    assert d.isfinite().all()
+    for weight in (0.0, 2.0 ** -20, 1.0):
+        d[:, 5], d[:, width - 1] = 0, 0
+        d[2, 5], d[4, width - 1] = weight, -weight
+        got = ops.int8_linear_grad_input(d.to(cuda_device), w.to(cuda_device), dim,
+                                         out_dtype=torch.float32)
+        dd = d.double().to(cuda_device)
+        ref, size = dd @ wv, dd.abs() @ wv.abs()
+        assert got.isfinite().all()
+        assert_within(got, ref, (width + 8) * 2 * U32 * size + 1.01 * rounding(ref, got.dtype))
+    ops.check()

@@ -259,3 +259,28 @@ def test_offsets_past_32_bits(cuda_device):
     g = ops.activation_grad(x, kept, "gelu")
     assert torch.equal(g[at], ops.activation_grad(part.to(cuda_device), want_kept, "gelu"))
     assert int((g != 0).any(1).sum()) == 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 61])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("f", KINDS)
+def test_gradient_at_the_largest_numbers(cuda_device, dtype, f, dim):
+    x = values(4, 2 * dim, 1).to(dtype)
+    x[1, 5], x[2, 7] = torch.finfo(dtype).max, torch.finfo(dtype).min
+    x[1, dim + 5], x[3, dim + 9] = torch.finfo(dtype).max, torch.finfo(dtype).min
+    d = values(4, dim, 2).to(dtype)
+    d[1, 5], d[2, 7], d[3, 9] = 0, 2.0 ** -30, 0
+    halves = [reference_rows(x[:, :dim]), reference_rows(x[:, dim:])]
+    k, u = (reference_values(h, dim) for h in halves)
+    value, slope, off, slope_off = formula(k, f)
+    dd = d.double()
+    kept = torch.cat(halves, 1).to(cuda_device)
+    got = ops.activation_grad(d.to(cuda_device), halves[0].to(cuda_device), f)
+    assert got.isfinite().all()
+    check(got, dd * slope, dd.abs() * slope_off + 3 * U32 * (dd * slope).abs(), dtype)
+    got = ops.activation_grad(d.to(cuda_device), kept, f, gated=True)
+    ref = torch.cat((dd * slope * u, dd * value), 1)
+    bound = torch.cat((dd.abs() * slope_off * u.abs(), dd.abs() * off), 1)
+    assert got.isfinite().all()
+    check(got, ref, bound + 3 * U32 * ref.abs(), dtype)

@@ -188,10 +188,12 @@ agnes_status agnes_mx4_linear(const void* x, int64_t x_stride, int64_t rows, con
 /* Rows in 8 bits, for features and for activations that are kept for a backward
  * pass.  A row of dim values is int8_row_bytes(dim) bytes: dim whole numbers q
  * from -127 to 127, zeros, and in the last four bytes of a multiple of 16 a scale
- * s (fp32); it stands for q s.  Rows are 16-byte aligned, a multiple of 16 bytes
- * apart.  So a matrix of them can be loaded as a graph's features (row_bytes / 2
- * "fp16" values a row): they are gathered byte for byte.  1 <= dim <= 2^17,
- * 0 <= rows < 2^31 - 255. */
+ * s (fp32); it stands for q s.  s may be any fp32 number; agnes_int8_quantize writes
+ * bfloat16 ones (eight significant bits), for which a value has 15 bits and the gradients
+ * below take it whole, where of rows that came another way they take its leading 16 bits.
+ * Rows are 16-byte aligned, a multiple of 16 bytes apart.  So a matrix of them can be
+ * loaded as a graph's features (row_bytes / 2 "fp16" values a row): they are gathered
+ * byte for byte.  1 <= dim <= 2^17, 0 <= rows < 2^31 - 255. */
 #define AGNES_INT8_ROWS 3 /* an output's type: 8-bit rows, its stride in bytes */
 agnes_status agnes_int8_row_bytes(int64_t dim, int64_t* bytes);
 
@@ -233,7 +235,7 @@ agnes_status agnes_int8_linear_workspace(int64_t rows, int64_t width, int64_t di
 /* The gradient of agnes_int8_linear to the weights, from the rows that the layer
  * keeps in 8 bits, and to the bias:
  *   out[j][i] = sum_r grad[r][j] x[r][i],  dbias[j] = sum_r grad[r][j].
- * Products are exact to 2^-21, sums are in fp32 over an order that depends on the
+ * Products are exact to 2^-21 (2^-16 where a scale has more than eight bits), sums are in fp32 over an order that depends on the
  * sizes only: the result is the same, bit by bit, each time.
  *  grad   rows x width of grad_dtype, grad_stride apart.
  *  out    width x dim of out_dtype, out_stride apart (zeros where rows is 0).

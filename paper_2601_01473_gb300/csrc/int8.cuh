@@ -5,7 +5,8 @@
 // s is the row's largest magnitude / 127, rounded up to eight significant bits: a whole
 // number times it has 15 bits, which are the sum of two bfloat16 values, so the tensor
 // cores' products with a row's values are exact.  That costs the rounding 0.4% of a step
-// at most (s is up to 2^-7 larger than it had to be, on average half that).
+// at most (s is up to 2^-7 larger than it had to be, on average half that).  Rows that came
+// another way may have any fp32 scale: the gradients' products keep 16 bits of their values.
 #pragma once
 
 #include "rows.cuh"

@@ -24,18 +24,20 @@ struct Int8TermScale {
   bool brief;  // packed bfloat16 arithmetic makes the terms
   __device__ explicit Int8TermScale(float scale)
       : value(scale), twice(__float2bfloat162_rn(scale)) {
-    // up to 2^121, 127 times it rounds to a finite bfloat16 value
-    brief = (__float_as_uint(scale) & 0x7fffffffu) <= 0x7c000000u;
+    // eight bits; and up to 2^121, 127 times it rounds to a finite bfloat16 value
+    const uint32_t bits = __float_as_uint(scale);
+    brief = (bits & 0xffffu) == 0 && (bits & 0x7fffffffu) <= 0x7c000000u;
   }
 };
 
-// Four whole numbers times a scale as pairs of bfloat16 terms that add up to it exactly.
+// Four whole numbers times a scale as pairs of bfloat16 terms that add up to it: exactly for a
+// scale of eight bits, else to 2^-17 of it.
 // Brief ones: hi the rounded products, lo what they leave.  A byte is its lower seven
 // bits less 128 times its sign, and 128 + seven bits, 128 and 256 are bfloat16 bit patterns
 // of the byte's parts.
-// Others (a row with its type's largest number, whose products round past bfloat16's, and one
-// that stands for NaN), where the caller has not ruled them out (kBrief): in fp32, hi the leading
-// eight bits.
+// Others (a scale of more bits, that the quantiser did not write; a row with its type's largest
+// number, whose products round past bfloat16's; one that stands for NaN), where the caller has not
+// ruled them out (kBrief): in fp32, hi the leading eight bits and lo the next.
 template <bool kBrief>
 __device__ __forceinline__ void int8_terms4(uint32_t word, const Int8TermScale& scale, uint2& hi,
                                             uint2& lo) {

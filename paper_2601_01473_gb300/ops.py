@@ -501,7 +501,9 @@ def _new_rows8(rows, dim, device, halves=1):
 def int8_quantize(x, out=None, stream=None):
     """Rows of ``x`` [rows, dim] rounded to 8-bit rows (agnes_int8_quantize): uint8
     [rows, int8_row_bytes(dim)].  Activations, and weights [width, dim] of
-    ``int8_linear``; ``.view(torch.float16)`` of them makes a graph's features."""
+    ``int8_linear``; ``.view(torch.float16)`` of them makes a graph's features.  Rows of the
+    same format that another program wrote do as well: a row's scale may be any float32,
+    and where it has more than a bfloat16's eight bits the gradients take 16 bits of a value."""
     if stream is not None:
         return _on_stream(stream, int8_quantize, x, out)
     device, rows, dim, step = _rows("x", x)

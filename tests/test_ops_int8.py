@@ -733,3 +733,46 @@ def test_gradient_to_the_input_of_weights_with_the_largest_numbers(cuda_device, 
         assert got.isfinite().all()
         assert_within(got, ref, (width + 8) * 2 * U32 * size + 1.01 * rounding(ref, got.dtype))
     ops.check()
+
+
+# ---- rows that another program wrote ---------------------------------------------------------
+
+def _other_rows(rows, dim, seed):
+    """8-bit rows whose scales are fp32 numbers of 24 bits, one of them negative."""
+    x = values(rows, dim, seed)
+    scale = x.abs().amax(1, keepdim=True) / 127
+    scale[rows // 2] *= -1
+    assert (scale.view(torch.int32) % 65536 != 0).float().mean() > 0.9 or rows == 1
+    packed = torch.zeros(rows, row_bytes(dim), dtype=torch.uint8)
+    packed[:, :dim] = torch.round(x / scale).clamp(-127, 127).to(torch.int8).view(torch.uint8)
+    packed[:, -4:] = scale.contiguous().view(torch.uint8)
+    return packed
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,dim", [(90, 70, 40), (700, 300, 150), (4200, 2000, 150)])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_scales_of_more_than_eight_bits(cuda_device, rows, width, dim, dtype):
+    """A scale is any fp32 number: values of 31 bits then, which the products' operands keep
+    the leading 16 bits of."""
+    x, w = _other_rows(rows, dim, 1), _other_rows(width, dim, 2)
+    d = (values(rows, width, 3) / 64).to(dtype)
+    assert d.isfinite().all()
+    x_dev, w_dev, d_dev = x.to(cuda_device), w.to(cuda_device), d.to(cuda_device)
+    back = ops.int8_dequantize(x_dev, dim)
+    ref = reference_values(x, dim)
+    assert_within(back, ref, rounding(ref, torch.float32))
+    ref, size = _exact_product(x, w, dim, cuda_device)
+    assert_within(ops.int8_linear(x_dev, w_dev, dim), ref,
+                  _product_bound(ref, size, dim, torch.float32))
+    got = ops.int8_linear_grad_weight(d_dev, x_dev, dim).weight
+    dx = ops.int8_linear_grad_input(d_dev, w_dev, dim, out_dtype=torch.float32)
+    dd = d_dev.double()
+    xv, wv = (reference_values(v, dim).to(cuda_device) for v in (x, w))
+    for y, a, b, n in ((got, dd.t(), xv, rows), (dx, dd, wv, width)):
+        ref, size = a @ b, a.abs() @ b.abs()
+        # the second term is rounded to 8 bits, 2^-9 of what is at most 2^-7 of the value; the sum
+        assert_within(y, ref, (2.0 ** -16 + (n + 8) * 2 * U32) * size)
+        # and on average far less than the 2^-9 that one rounding of the scales would lose
+        assert float((y - ref).norm() / ref.norm()) < 2.0 ** -15
+    ops.check()

@@ -894,12 +894,14 @@ struct GradInputSpace {
 template <typename TOut, bool kConvert>
 cudaError_t launch_product(const TileArgs& a, const TileOperands& o, bool drain, int device,
                            cudaStream_t st) {
+  // by pairs: the gradient of 8192 x 4096 to 2048 in fp32 418 us and 539 by CTAs of their own
+  if (drain && o.k > 128 && op_num_sms(device) >= 2)
+    return launch_tiles<TOut, kConvert, 128, true, true>(a, o, device, st);
   if (drain) return launch_tiles<TOut, kConvert, 128, true, false>(a, o, device, st);
   // 786,432 x 128 to 128 68 us, and 82 by tiles of 256 columns
   if (a.cols <= 128) return launch_tiles<TOut, kConvert, 128, false, false>(a, o, device, st);
   // Pairs for contractions of more than two slices: 16,384 x 4096 to 4096 356 us and 466 by CTAs
-  // of their own, 300,000 x 200 to 256 53 and 65, the gradient of 8192 x 4096 to 2048 columns 159
-  // and 220.  A pair's start costs 0.9 us more, and its B is not resident: 300 x 128 to 256 8.8
+  // of their own, 300,000 x 200 to 256 53 and 65.  A pair's start costs 0.9 us more, and its B is not resident: 300 x 128 to 256 8.8
   // and 7.9, 786,432 x 128 to 256 98.3 and 97.3.
   if (o.k > 128 && op_num_sms(device) >= 2)
     return launch_tiles<TOut, kConvert, 256, false, true>(a, o, device, st);
@@ -934,8 +936,12 @@ cudaError_t launch_linear(const LinearArgs& l, void* workspace, int32_t* status,
   const TileOperands o = {l.x, w, l.x_stride, space.kpad * 2, l.dim};
   // Whole sums are exact up to 2^24, that of 1040 of the largest products; beyond, a product of
   // 16 loses 2^-23 of the sum at most, so 2048 columns lose 8e-6 where all values are the
-  // largest, and nothing else.  16-bit outputs keep nothing of what 32,768 lose.
-  const bool drain = l.dim > (sizeof(TOut) == 4 ? 2048 : 32768);
+  // largest, and nothing else.  Uniform values of one sign lose 7e-6 in 8192 columns, 3e-5 in 16,384
+  // and 1e-4 in 32,768, where half a unit of an fp16 result is 2^-12 of it or more and of a bfloat16
+  // one 2^-9.  Drained they lose nothing, but the rows are made fp16 for half as many columns:
+  // 8192 x 16,384 to 2048 fp16 737 us and not 455.
+  const int64_t most = sizeof(TOut) == 4 ? 2048 : std::is_same<TOut, __half>::value ? 8192 : 32768;
+  const bool drain = l.dim > most;
   return launch_product<TOut, true>(a, o, drain, device, st);
 }
 
@@ -1120,11 +1126,15 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
   a.status = status;
   return op_launched(op, with_float_type(out_dtype, [&](auto t) {
     using TOut = typename decltype(t)::type;
-    // some 20 products of 16 to an accumulator where the sum stays in fp32, which loses some 5e-7
-    // of it (40 lost 1e-6); 16-bit outputs keep nothing of what a chain of some thousand loses
+    // Of values of one sign a product of 16 loses 5e-8 to 9e-8 of the result.  Some 20 to an
+    // accumulator where the sum stays in fp32: 8e-7 (1.6e-6 of a gradient in fp32).  16-bit results
+    // have 128 at most: 7e-6, a thirtieth of half a unit of fp16 (2^-12 of a value or more), where
+    // the undrained sums of 4096 columns lost 3e-5 to 7e-5, of 16,384 2e-4 to 3e-4.  It costs
+    // 8192 x 4096 to 2048 bfloat16 177 us and not 166 (190 with 24 products to an accumulator).
     const int per_slice = 4 * (a.ta == 1 ? 2 : a.ta == 2 ? 4 : 5);
-    a.chain = 24 / per_slice > 0 ? 24 / per_slice : 1;
-    const bool drain = sizeof(TOut) == 4 || width > 16384;
+    const int most = sizeof(TOut) == 4 ? 24 : 128;
+    a.chain = most / per_slice;
+    const bool drain = sizeof(TOut) == 4 || ceil_div(width, kSliceK) > a.chain;
     return launch_product<TOut, false>(a, o, drain, device, st);
   }));
 }

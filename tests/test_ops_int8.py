@@ -776,3 +776,101 @@ def test_scales_of_more_than_eight_bits(cuda_device, rows, width, dim, dtype):
         # and on average far less than the 2^-9 that one rounding of the scales would lose
         assert float((y - ref).norm() / ref.norm()) < 2.0 ** -15
     ops.check()
+
+
+# ---- long contractions -----------------------------------------------------------------------
+
+# Tensor memory's sums are cut off instead of rounded: a product of 16 aligns these and the sum with
+# the largest of them, cuts each off two bits below its unit (2^-23 of it at most) and the result at
+# the unit: 17 eighths and a half of a unit on average, 2.6.  Over a sum of values of one sign a
+# partial sum's unit is 0.375 of the result's 2^-23 on average at most (m - 2/3 over m^2 for a result
+# of m, 1 <= m < 2), so that a product loses 2^-23 of the result.  How many products one such sum may
+# have, of the product and of the gradient to the input:
+CHAIN = {torch.float32: 64, torch.float16: 512, torch.bfloat16: 2048}
+GRAD_CHAIN = {torch.float32: 24, torch.float16: 128, torch.bfloat16: 128}
+
+
+def _one_sign_check(got, ref, products, chains):
+    """`got` of sums of positive numbers whose rows differ in size, `products` to an accumulator,
+    `chains` of those added up in fp32."""
+    loss = products * 2 * U32 + (chains + 4) * U32
+    assert_within(got, ref, loss * ref + 1.01 * rounding(ref, got.dtype))
+    # The mean, relative to 64 bits rounded once.  A loss takes a value to its neighbour, a unit
+    # away, as often as it is a part of a unit; rows alone count as independent.
+    off = ((got.double() - ref.to(got.dtype).double()) / ref).mean()
+    unit = 2 * float((rounding(ref, got.dtype) / ref).max())
+    assert abs(float(off)) <= loss + 4 * math.sqrt(unit * loss / got.shape[0])
+
+
+def _of_one_sign(dev, rows, dim, seed, scale=1.0):
+    """Between 0.5 and 1.5, times a number of the row's own between 1 and 2."""
+    g = torch.Generator(device=dev).manual_seed(seed)
+    x = torch.rand(rows, dim, generator=g, device=dev) + 0.5
+    return x * torch.exp2(torch.rand(rows, 1, generator=g, device=dev)) * scale
+
+
+# beside each limit and the longest rows
+@pytest.mark.gpu
+@pytest.mark.parametrize("out,dim", [(torch.float16, 8192), (torch.float16, 8193),
+                                     (torch.float16, 32_768), (torch.float16, 32_769),
+                                     (torch.bfloat16, 32_768), (torch.bfloat16, 32_769),
+                                     (torch.float16, 131_072), (torch.bfloat16, 131_072),
+                                     (torch.float32, 32_768)])
+def test_product_of_long_rows_of_one_sign(cuda_device, out, dim):
+    x = ops.int8_quantize(_of_one_sign(cuda_device, 1000, dim, 1))
+    w = ops.int8_quantize(_of_one_sign(cuda_device, 130, dim, 2, 2.0 ** -8))
+    got = ops.int8_linear(x, w, dim, out_dtype=out)
+    ref, _ = _exact_product(x, w, dim, cuda_device)
+    _one_sign_check(got, ref, min(CHAIN[out], -(-dim // 16)), dim / 1024)
+
+
+# widths beside the limits of each gradient's number of terms
+@pytest.mark.gpu
+@pytest.mark.parametrize("grad", FLOATS)
+@pytest.mark.parametrize("out", FLOATS)
+@pytest.mark.parametrize("width", [384, 385, 512, 513, 1024, 1025, 2048, 4097, 6592, 8193, 16_384,
+                                   16_385])
+def test_gradient_to_the_input_of_wide_layers_of_one_sign(cuda_device, grad, out, width):
+    rows, dim = 2000, 140
+    d = _of_one_sign(cuda_device, rows, width, width).to(grad)
+    w = ops.int8_quantize(_of_one_sign(cuda_device, width, dim, 3, 2.0 ** -8))
+    got = ops.int8_linear_grad_input(d, w, dim, out_dtype=out)
+    ref = d.double() @ reference_values(w, dim)
+    # products of 16 for each two terms: of bfloat16, fp16 and fp32
+    terms = {torch.bfloat16: 2, torch.float16: 4, torch.float32: 5}[grad]
+    _one_sign_check(got, ref, min(GRAD_CHAIN[out], -(-width // 16) * terms), width / 64)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [40, 300])
+@pytest.mark.parametrize("dim", [1040, 2048, 2049, 131_072])
+def test_product_of_the_largest_whole_numbers_in_chains(cuda_device, rows, dim):
+    """1024 columns' sum of 127^2 is exact; beyond 2048 columns those are added up in fp32."""
+    x = torch.full((rows, dim), 127.0)
+    w = torch.full((3, dim), 127.0)
+    w[1] *= -1
+    w[2, ::2] *= -1
+    got = ops.int8_linear(*(ops.int8_quantize(v.to(cuda_device)) for v in (x, w)), dim)
+    want = (x.double() @ w.double().t()).to(cuda_device)
+    # undrained: each product past 2^24 is cut off by 2 at most, or by 4 past 2^25
+    off = dim / 1024 * U32 * 127.0 ** 2 * dim if dim > 2048 else 0 if dim <= 1040 else \
+        4 * (dim - 1040) / 16
+    assert_within(got, want, off * torch.ones_like(want) + U32 * want.abs())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("grad", FLOATS)
+def test_long_contractions_of_both_signs(cuda_device, grad, out):
+    """The variants that add up chains for 16-bit results, ragged on each side."""
+    _product_check(cuda_device, 139, 261, 33_001, out, True)
+    d, _, w = _grad_inputs(139, 16_501, 261, grad)
+    got = ops.int8_linear_grad_input(d.to(cuda_device), w.to(cuda_device), 261, out_dtype=out)
+    dd, wv = d.double().to(cuda_device), reference_values(w, 261).to(cuda_device)
+    fine = torch.isfinite(dd).all(1)  # values past fp16's largest number
+    ref, size = dd[fine] @ wv, dd[fine].abs() @ wv.abs()
+    # 128 products to an accumulator, up to 259 of those
+    bound = (2 * 128 + 259 + 8) * U32 * size + 1.01 * rounding(ref, out)
+    assert_within(got[fine], ref, bound)
+    assert not got[~fine].isfinite().any()
+    ops.check()

@@ -55,6 +55,11 @@ __device__ __forceinline__ void normal_fit(float v, float* phi, float* density) 
   *density = e * 0.3989422804f;  // 1 / sqrt(2 pi)
 }
 
+// silu by 1 / (1 + exp -v), which leaves fp32's range below kSiluNear: the result is zero there and
+// not v exp v, 1e-36 and less, which fp16 and 8-bit rows have as zero anyway.
+constexpr int32_t kNearSilu = 3;
+constexpr float kSiluNear = -87.f;
+
 // f(v), and its derivative where one is asked for; kFit: for results of 16 bits.
 template <bool kSlope, bool kFit>
 __device__ __forceinline__ float nonlinear(int32_t f, float v, float* slope) {
@@ -62,10 +67,23 @@ __device__ __forceinline__ float nonlinear(int32_t f, float v, float* slope) {
     if (kSlope) *slope = v > 0.f ? 1.f : v <= 0.f ? 0.f : v;
     return v < 0.f ? 0.f : v;
   }
-  if (f == AGNES_F_SILU) {
+  if (f == kNearSilu) {
     const float p = __fdividef(1.f, 1.f + (kFit ? __expf(-v) : expf(-v)));
     if (kSlope) *slope = p * fmaf(v, 1.f - p, 1.f);
     return v * p;
+  }
+  if (f == AGNES_F_SILU) {
+    // p = 1 / (1 + exp -v) from exp -|v|, which stays in fp32's range, so v p does far below zero;
+    // the slope p + v p (1 - p) by the product of both, as 1 - p would be a difference
+    const float e = kFit ? __expf(-fabsf(v)) : expf(-fabsf(v));
+    const float r = __fdividef(1.f, 1.f + e);
+    const float up = v < 0.f ? e : 1.f;
+    if constexpr (kSlope) {
+      const float p = up * r;
+      *slope = fmaf(v, e * r * r, p);
+      return v * p;
+    }
+    return v * up * r;
   }
   float p, density;
   if constexpr (kFit) {
@@ -79,12 +97,15 @@ __device__ __forceinline__ float nonlinear(int32_t f, float v, float* slope) {
 }
 
 // f with the kind as a constant, chosen once for all of a thread's values.
-template <typename F>
+// kNear: kNearSilu may be among them.
+template <bool kNear, typename F>
 __device__ __forceinline__ void with_kind(int32_t kind, F&& f) {
   if (kind == AGNES_F_RELU)
     f(std::integral_constant<int32_t, AGNES_F_RELU>());
   else if (kind == AGNES_F_SILU)
     f(std::integral_constant<int32_t, AGNES_F_SILU>());
+  else if (kNear && kind == kNearSilu)
+    f(std::integral_constant<int32_t, kNearSilu>());
   else
     f(std::integral_constant<int32_t, AGNES_F_GELU>());
 }
@@ -101,6 +122,9 @@ __global__ void __launch_bounds__(kLanes, kVec == 1 && !kStaged ? 1 : 2)
 keep_kernel(const KeepArgs a) {
   constexpr int kPer = kElems / kVec;
   constexpr bool kFit = sizeof(T) == 2;
+  // 16-bit silu by the shorter form (65,536 x 1024 bf16, gated, 102 us and not 106): where small
+  // results are zeros, or a thread's values are all nearer (their largest magnitude is known)
+  constexpr bool kNear = kFit && (kOut8 || std::is_same<T, __half>::value), kAsk = kFit && !kNear;
   __shared__ RowScratch scratch;
   int turn = 0;
   const int group = threadIdx.x >> a.log_lanes, lane = threadIdx.x & (a.lanes - 1);
@@ -139,12 +163,14 @@ keep_kernel(const KeepArgs a) {
       const RowPart<kVec, kPer> part = {a.lanes, lane, a.dim - c0};
       v.load(part, x + c0, valid);
       if constexpr (kMode == kGated) u.load(part, x + a.dim + c0, valid);
+      const uint32_t largest = keep || kAsk ? v.top() : 0;
       if (keep) {
-        top[0] = max(top[0], v.top());
+        top[0] = max(top[0], largest);
         if constexpr (kMode == kGated) top[1] = max(top[1], u.top());
       }
       if constexpr (kMode != kRound) {
-        with_kind(a.f, [&](auto kind) {
+        const bool near = kNear || (kAsk && largest < __float_as_uint(-kSiluNear));
+        with_kind<kFit>(a.f == AGNES_F_SILU && near ? kNearSilu : a.f, [&](auto kind) {
 #pragma unroll
           for (int i = 0; i < kPer; ++i) {
             if (part.beyond(i)) break;
@@ -200,7 +226,7 @@ keep_kernel(const KeepArgs a) {
         }
         if constexpr (kOut8) {
           if (kLoop) {
-            with_kind(a.f, [&](auto kind) {
+            with_kind<kNear>(kNear && a.f == AGNES_F_SILU ? kNearSilu : a.f, [&](auto kind) {
 #pragma unroll
               for (int e = 0; e < kVec; ++e) {
                 f[e] = nonlinear<false, kFit>(kind, f[e], nullptr);
@@ -359,7 +385,7 @@ back_kernel(const BackArgs a) {
       v.load(part, kept + c0, true);
       if constexpr (kGate) u.load(part, kept + half + c0, true);
       d.load(part, grad + c0, true);
-      with_kind(a.f, [&](auto kind) {
+      with_kind<false>(a.f, [&](auto kind) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           if (part.beyond(i)) break;

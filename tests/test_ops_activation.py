@@ -284,3 +284,39 @@ def test_gradient_at_the_largest_numbers(cuda_device, dtype, f, dim):
     bound = torch.cat((dd.abs() * slope_off * u.abs(), dd.abs() * off), 1)
     assert got.isfinite().all()
     check(got, ref, bound + 3 * U32 * ref.abs(), dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_silu_far_below_zero(cuda_device, dtype):
+    """Where exp(-v) leaves fp32's range the value, v exp(v), is still in it."""
+    v = torch.linspace(-100, -80, 2001).to(dtype)[:, None]
+    y, kept = ops.activation(v.to(cuda_device), "silu")
+    # exp(v) to 2 units and half of fp32's smallest number, 1 + e, a reciprocal to 2 units, two
+    # products; 16-bit types take the exponential whose error grows by a unit for 0.86 of v
+    units = 12 * U32 if dtype == torch.float32 else 2 * (8 + 1.2 * 100) * U32
+    least = 2.0 ** -149
+
+    def check_at(got, v, ref):
+        assert got.dtype == dtype
+        assert_within(got, ref, units * ref.abs() + (2 + v.abs()) * least
+                      + 1.01 * rounding(ref, dtype))
+    x = v.double()
+    check_at(y, x, x * torch.sigmoid(x))
+    assert (y[v > -95] != 0).all()
+    k = reference_values(reference_rows(v), 1)
+    got = ops.activation_grad(torch.ones(len(v), 1, dtype=dtype, device=cuda_device), kept, "silu")
+    p = torch.sigmoid(k)
+    check_at(got, k, p * (1 + k * torch.sigmoid(-k)))
+
+
+@pytest.mark.gpu
+def test_silu_slope_far_above_zero(cuda_device):
+    """1 + v exp(-v): what is left of 1 - p is not a difference of numbers next to one."""
+    v = torch.linspace(4, 60, 3001)[:, None]
+    _, kept = ops.activation(v.to(cuda_device), "silu")
+    k = reference_values(reference_rows(v), 1)
+    got = ops.activation_grad(torch.ones(len(v), 1, device=cuda_device), kept, "silu")
+    p, q = torch.sigmoid(k), torch.sigmoid(-k)
+    # p and q to 4 units each, v q <= 0.08, a product, a sum, a product, a rounding
+    assert_within(got, p * (1 + k * q), U32 * (2 * 4 + 2 * 5 * k * q + 4))

@@ -568,7 +568,7 @@ struct WeightSpace {
 };
 
 template <typename TOut>
-cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride,
+cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride, bool direct,
                           __nv_bfloat16* values, int device, cudaStream_t st) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return cudaErrorNotSupported;
@@ -603,8 +603,15 @@ cudaError_t launch_weight(WeightArgs a, const void* grad, int64_t grad_stride,
   a.slots = slots < kMaxSlots ? slots : kMaxSlots;
   const size_t smem = (size_t)kSmemLimit - kRingBytes + (size_t)a.slots * a.slot_bytes;
   const int64_t tiles = (int64_t)a.tiles_j * a.tiles_i;
-  e = launch_next_cluster(kernel, dim3((unsigned)(tiles * a.splits)), (unsigned)kThreads, smem,
-                          a.pair ? 2u : 1u, st, grad_map, x_map, a);
+  const dim3 grid((unsigned)(tiles * a.splits));
+  const unsigned cluster = a.pair ? 2u : 1u;
+  // the call's first kernel where nothing had to be made of its operands: what is before it on the
+  // stream is another call's
+  const bool first = direct && !a.ready;
+  e = first ? launch_cluster(false, kernel, grid, (unsigned)kThreads, smem, cluster, st, grad_map,
+                             x_map, a)
+            : launch_next_cluster(kernel, dim3(grid), (unsigned)kThreads, smem, cluster, st,
+                                  grad_map, x_map, a);
   if (e != cudaSuccess) return e;
   // Few shares: more values to a CTA; many: more threads to a value.  In the other way the
   // gradient of 8192 rows of 2048 to 4096 columns (2 shares) takes 22 us more, that of 20,000
@@ -704,7 +711,7 @@ agnes_status agnes_int8_linear_grad_weight(const void* grad, int32_t grad_dtype,
   space.shape(w);
   return op_launched(op, with_float_type(out_dtype, [&](auto t) {
     return launch_weight<typename decltype(t)::type>(
-        w, a, a_stride, (__nv_bfloat16*)((uint8_t*)workspace + space.values), device, st);
+        w, a, a_stride, direct, (__nv_bfloat16*)((uint8_t*)workspace + space.values), device, st);
   }));
 }
 

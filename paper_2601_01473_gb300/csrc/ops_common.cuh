@@ -126,27 +126,33 @@ inline bool aligned_rows(const void* p, int64_t stride_bytes, int64_t bytes) {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Launches a kernel whose predecessor on the stream is the kernel before it in the same
-// call, ahead of that one's completion: its CTAs are set up meanwhile and wait in
-// grid_dep_wait(), which has to be the kernel's first statement.
-// `cluster`: CTAs to a cluster.
+// Launches a kernel in clusters of `cluster` CTAs, after its predecessor on the stream or `ahead` of
+// that one's completion.
 template <typename... Params, typename... Args>
-cudaError_t launch_next_cluster(void (*kernel)(Params...), dim3 grid, unsigned threads,
-                                size_t smem, unsigned cluster, cudaStream_t st, Args&&... args) {
+cudaError_t launch_cluster(bool ahead, void (*kernel)(Params...), dim3 grid, unsigned threads,
+                           size_t smem, unsigned cluster, cudaStream_t st, Args&&... args) {
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  cfg.attrs = cluster > 1 ? attr : attr + 1;
+  cfg.numAttrs = (cluster > 1 ? 1 : 0) + (ahead ? 1 : 0);
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+// Launches a kernel whose predecessor on the stream is the kernel before it in the same
+// call, ahead of that one's completion: its CTAs are set up meanwhile and wait in
+// grid_dep_wait(), which has to be the kernel's first statement.
+template <typename... Params, typename... Args>
+cudaError_t launch_next_cluster(void (*kernel)(Params...), dim3 grid, unsigned threads,
+                                size_t smem, unsigned cluster, cudaStream_t st, Args&&... args) {
+  return launch_cluster(true, kernel, grid, threads, smem, cluster, st, args...);
 }
 template <typename... Params, typename... Args>
 cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem,

@@ -38,3 +38,35 @@ def test_the_check_sees_a_kernel_that_reads_first():
     at = text.index("grid_dep_wait();")
     planted = text[:at] + "if (a.rows == 0) return;\n  " + text[at:]
     assert dict(_kernel_bodies(planted))["tile_kernel"] == "if (a.rows == 0) return"
+
+
+def _first_of_its_call(text):
+    """The kernels launched ahead before which their call may have launched no other."""
+    bodies = re.split(r"\n}\n", text)  # functions, or what is between them
+    found = set()
+    for body in bodies:
+        for m in re.finditer(r"\blaunch_next(?:_cluster)?\((?:(\w+_kernel)|\w+)", body):
+            before = body[:m.start()]
+            plain = re.search(r"<<<|prepare_operands\(|launch_grad<", before)
+            # `plain` is not in a condition, or the launch is the other half of its own
+            chosen = re.search(r"first \? launch_cluster\(false,[^;]*$", before)
+            conditional = plain and re.search(r"if \(a\.ready\) {[^}]*$", before[:plain.start()])
+            if not chosen and (not plain or conditional) and "launch_next" not in before:
+                found.add(m.group(1) or "kernel")
+    return found
+
+
+@pytest.mark.parametrize("fname", sorted(AHEAD))
+def test_kernels_launched_ahead_follow_one_of_their_call(fname):
+    """launch_next's condition: its predecessor on the stream is not the caller's last kernel, of
+    which nothing is known."""
+    text = open(os.path.join(CSRC, fname)).read()
+    # launch_tiles has its operands' kernel launched by its callers
+    assert _first_of_its_call(text) <= {"tile_kernel"}
+    if fname == "int8_linear.cu":
+        for caller in ("launch_linear(", "agnes_int8_linear_grad_input("):
+            body = text[text.rindex(caller):]
+            assert re.search(r"expand_kernel<<<|prepare_operands\(", body).start() < \
+                body.index("launch_product<")
+    if fname == "int8_grad_weight.cu":
+        assert "const bool first = direct && !a.ready;" in text

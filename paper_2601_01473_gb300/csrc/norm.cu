@@ -1053,9 +1053,13 @@ cudaError_t launch_staged(NormArgs a, int device, cudaStream_t st) {
   const auto kernel = which == 0   ? norm_staged_kernel<TX, TBranch, 10>
                       : which == 1 ? norm_staged_kernel<TX, TBranch, 12>
                                    : norm_staged_kernel<TX, TBranch, kElems>;
-  static OncePerDevice once[3];  // the longest rows take 132 KB
+  // the longest rows take most, one to a CTA: an fp32 residual and its sum, a branch, a full gate
+  // and next in 16 bits, 114,768 bytes with what their first and last pieces have besides
+  constexpr int kMost = (int)(kNormMaxDim * (2 * 4 + 3 * 2) + 5 * 16);
+  static_assert(kMost > staged_bytes(49152) + 4 * 32, "or a batch of shorter ones");
+  static OncePerDevice once[3];
   const cudaError_t e = once[which].run(device, [&] {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
   });
   if (e != cudaSuccess) return e;
   kernel<<<(unsigned)ceil_div(a.rows, rows), (unsigned)(a.lanes * a.groups), (size_t)smem, st>>>(a);

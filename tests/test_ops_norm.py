@@ -544,3 +544,24 @@ def test_offsets_past_32_bits(cuda_device):
     d_next, d_sum = spread(d_next), spread(d_sum)
     g = ops.residual_norm_grad(d_next, d_sum, got.sum, **big)
     assert torch.equal(g.x[at], want_grad.x) and torch.equal(g.branch[at], want_grad.branch)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("types", [(torch.float32, torch.bfloat16), (torch.float16, torch.float16)])
+def test_the_longest_rows_from_any_element_on(cuda_device, types):
+    """What takes most shared memory: 8192 columns that no vector's alignment suits, a full gate."""
+    rows, dim = 3, 8192
+    c, _, _ = make(rows, dim, types, "layer", True, "rows", True)
+    flat = torch.zeros(rows * dim + 1, dtype=types[0], device=cuda_device)
+    moved = on(cuda_device, c)
+    moved["x"] = flat[1:].view(rows, dim).copy_(c["x"])
+    got = ops.residual_norm(**moved)
+    ref = forward(c)
+    assert_within(got.sum, ref.v, ref.err + 1.01 * rounding(ref.v, types[0]))
+    ref = following(got.sum.cpu(), c)
+    assert_within(got.next, ref.v, ref.err + 1.01 * rounding(ref.v, types[1]))
+    got8 = ops.residual_norm(**moved, rows8=True)
+    assert torch.equal(got8.sum, got.sum)
+    back = ops.int8_dequantize(got8.next, dim).double().cpu()
+    step = ref.v.abs().amax(1, keepdim=True) / 127 * 1.01
+    assert ((back - ref.v).abs() <= 0.502 * step + ref.err).all()

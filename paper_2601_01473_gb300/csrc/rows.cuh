@@ -79,12 +79,6 @@ struct RowPart {
       }
     }
   }
-  template <typename T>
-  __device__ void store(T* row, bool valid, const float (&v)[kElems]) const {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (valid && col(i) < dim) store_vec<T, kVec>(row + col(i), v + i * kVec);
-  }
   // vector i
   template <typename T>
   __device__ void store_one(T* row, bool valid, int i, const float* v) const {

@@ -98,3 +98,41 @@ def test_the_gradients_are_those_of_plain_pytorch(cuda_device, dtype, rows):
             off = (y.double() - ref.grad).abs().max()
             assert off <= unit * ref.grad.abs().max(), (key, float(off / ref.grad.abs().max()))
     ops.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_step_changes_every_parameter_by_its_gradient(cuda_device, dtype):
+    m = _example()
+    rows, lr = 70, 0.25
+    new = lambda: m.DeepStudent(60, 72, 40, 19, 2, cuda_device, dtype=dtype)  # noqa: E731
+    s, before = new(), new()
+    g = gen(2)
+    x8 = ops.int8_quantize(torch.randn(rows, 60, generator=g).to(cuda_device))
+    teacher = torch.randn(rows, 4, generator=g).to(cuda_device)
+    index = torch.randint(0, 19, (rows, 4), generator=g).to(cuda_device)
+    loss = s.step(x8, teacher, index, 2.0, lr)
+    logits, kept = before.forward(x8)
+    want_loss, grad = ops.distill_loss_grad(logits, teacher, index, 1.0 / rows, 2.0)
+    assert torch.equal(loss, want_loss)
+    d = before.backward(grad, kept)
+
+    def changed(new_value, old, by):
+        assert by.abs().max() > 0
+        # a product and a sum, each rounded
+        off = (new_value.double() - (old.double() - lr * by.double())).abs()
+        assert (off <= 2.0 ** -23 * (old.abs() + lr * by.abs())).all()
+
+    changed(s.head, before.head, d["head"])
+    layers = [("first", s.first, before.first)]
+    for name in ("up", "down"):
+        layers += [(f"{name}{i}", *pair) for i, pair in
+                   enumerate(zip(getattr(s, name), getattr(before, name)))]
+    for key, layer, old in layers:
+        changed(layer.weight, old.weight, d[key].weight)
+        changed(layer.bias, old.bias, d[key].bias)
+        assert torch.equal(layer.rows8, ops.int8_quantize(layer.weight))
+    for name in ("before", "after", "gate"):
+        for i, (v, old) in enumerate(zip(getattr(s, name), getattr(before, name))):
+            changed(v, old, d[f"{name}{i}"])
+    ops.check()

@@ -1128,13 +1128,13 @@ agnes_status agnes_int8_linear_grad_input(const void* grad, int32_t grad_dtype,
     using TOut = typename decltype(t)::type;
     // Of values of one sign a product of 16 loses 5e-8 to 9e-8 of the result.  Some 20 to an
     // accumulator where the sum stays in fp32: 8e-7 (1.6e-6 of a gradient in fp32).  16-bit results
-    // have 128 at most: 7e-6, a thirtieth of half a unit of fp16 (2^-12 of a value or more), where
-    // the undrained sums of 4096 columns lost 3e-5 to 7e-5, of 16,384 2e-4 to 3e-4.  It costs
-    // 8192 x 4096 to 2048 bfloat16 177 us and not 166 (190 with 24 products to an accumulator).
+    // have 128 undrained at most (7e-6, a thirtieth of half a unit of fp16, which is 2^-12 of a value
+    // or more) or 64 (3e-6); undrained sums of 4096 columns lost 3e-5 to 7e-5, of 16,384 2e-4 to 3e-4.
+    // It costs 8192 x 4096 to 2048 bfloat16 180 us and not 166 (177 with 128 products to an
+    // accumulator, 190 with 24).
     const int per_slice = 4 * (a.ta == 1 ? 2 : a.ta == 2 ? 4 : 5);
-    const int most = sizeof(TOut) == 4 ? 24 : 128;
-    a.chain = most / per_slice;
-    const bool drain = sizeof(TOut) == 4 || ceil_div(width, kSliceK) > a.chain;
+    a.chain = (sizeof(TOut) == 4 ? 24 : 64) / per_slice;
+    const bool drain = sizeof(TOut) == 4 || ceil_div(width, kSliceK) * per_slice > 128;
     return launch_product<TOut, false>(a, o, drain, device, st);
   }));
 }

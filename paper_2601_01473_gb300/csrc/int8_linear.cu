@@ -16,8 +16,9 @@
 //   the epilogue warps scale the sums, add the bias and hand them to the TMA by way of shared
 //                     memory, while the next tile's products run.
 // Long rows are bound by the tensor cores (16,384 x 4096 to 4096, bf16: 357 us, 1540 TFLOP/s,
-// the tensor pipe 68% active; the gradient of 8192 x 4096 to 2048 159 us, two terms, 95%), short
-// ones by what they write (786,432 x 128 to 256, fp16: 97 us; a memset of the output takes 101).
+// the tensor pipe 68% active; the gradient of 8192 x 4096 to 2048 170 us, two terms, 74%: its sums
+// are drained, undrained it took 151 and 95%), short ones by what they write (786,432 x 128 to 256,
+// fp16: 97 us; a memset of the output takes 101).
 #include <type_traits>
 
 #include "int8_product.cuh"
@@ -408,7 +409,7 @@ __device__ __forceinline__ void slice_products(uint32_t to, uint32_t a_at, uint3
 // made fp16 in shared memory, and B fp16; else both are bfloat16, of several terms each.
 // kDrain: an accumulator sums `chain` slices, and the epilogue warps add those up in
 // registers: tensor memory's sums are cut off, not rounded, after each product, which adds
-// up over long chains.
+// up over long chains.  (With kConvert 8 bytes a thread are spilled, some 26 for fp32 results.)
 // kPair: two CTAs have a tile of 256 x kCols, each the rows and the output of its half and half
 // of B, so that B is copied and read once for both.
 template <typename TOut, bool kConvert, int kCols, bool kDrain, bool kPair>
@@ -894,15 +895,18 @@ struct GradInputSpace {
 template <typename TOut, bool kConvert>
 cudaError_t launch_product(const TileArgs& a, const TileOperands& o, bool drain, int device,
                            cudaStream_t st) {
-  // by pairs: the gradient of 8192 x 4096 to 2048 in fp32 418 us and 539 by CTAs of their own
-  if (drain && o.k > 128 && op_num_sms(device) >= 2)
+  if (drain) {
+    // By pairs: the gradient of 8192 x 4096 to 2048 in fp32 418 us and 539 by CTAs of their own,
+    // which have the short contractions; those are drained in the gradient in fp32 alone.
+    if constexpr (!kConvert && sizeof(TOut) == 4)
+      if (o.k <= 128) return launch_tiles<TOut, kConvert, 128, true, false>(a, o, device, st);
     return launch_tiles<TOut, kConvert, 128, true, true>(a, o, device, st);
-  if (drain) return launch_tiles<TOut, kConvert, 128, true, false>(a, o, device, st);
+  }
   // 786,432 x 128 to 128 68 us, and 82 by tiles of 256 columns
   if (a.cols <= 128) return launch_tiles<TOut, kConvert, 128, false, false>(a, o, device, st);
   // Pairs for contractions of more than two slices: 16,384 x 4096 to 4096 356 us and 466 by CTAs
-  // of their own, 300,000 x 200 to 256 53 and 65.  A pair's start costs 0.9 us more, and its B is not resident: 300 x 128 to 256 8.8
-  // and 7.9, 786,432 x 128 to 256 98.3 and 97.3.
+  // of their own, 300,000 x 200 to 256 53 and 65.  A pair's start costs 0.9 us more, and its B is
+  // not resident: 300 x 128 to 256 8.8 and 7.9, 786,432 x 128 to 256 98.3 and 97.3.
   if (o.k > 128 && op_num_sms(device) >= 2)
     return launch_tiles<TOut, kConvert, 256, false, true>(a, o, device, st);
   return launch_tiles<TOut, kConvert, 256, false, false>(a, o, device, st);

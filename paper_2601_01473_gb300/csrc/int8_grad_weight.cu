@@ -18,11 +18,12 @@
 //   the MMA warp      issues the products into one of two accumulators, `chain` slices each;
 //   the epilogue warps add the accumulators up in registers and write a partial tile, and
 //                     meanwhile add the gradient's columns up, of the first tile of columns.
-// Tensor memory's sums are cut off, not rounded, after each product: over a hyperbatch's rows
-// in one chain that bias would reach 1e-5 of the result, so chains are short.  A second
+// Tensor memory's sums are cut off, not rounded, after each product, which loses 5e-8 to 9e-8 of
+// a sum of values of one sign: a CTA's share of a hyperbatch's rows, some 300 products, would lose
+// 2e-5 in one chain, so chains are short.  A second
 // kernel adds the shares' tiles up in order, so the result is the same each time.
 // 786,432 rows of 128 to 256 columns, bfloat16: 102 us, 5.1 TB/s (memory); 8192 rows of 2048 to
-// 4096 columns 232 us, of which 204 here, the tensor pipe 62% active, 22 the shares' sum.
+// 4096 columns 232 us, of which 205 here, the tensor pipe 62% active, 22 the shares' sum.
 #include <type_traits>
 
 #include "int8_product.cuh"
@@ -52,7 +53,7 @@ constexpr int kSmemLimit = 232448;
 constexpr int kRingBytes = kSmemLimit - 1024 - 8 * kBars - 16;
 constexpr int kTmemCols = 512;
 constexpr int kTileValues = kTile * kTile;
-constexpr int kSms = 152;  // that the rows are shared out for: a GB300's
+constexpr int kSms = 152;  // that the rows are shared out for, whatever the device: a GB300's
 
 struct WeightArgs {
   int64_t rows, width;

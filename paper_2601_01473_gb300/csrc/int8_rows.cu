@@ -4,8 +4,9 @@
 // Bound by memory: a group of threads holds a row in registers, so it is read once, for
 // its largest magnitude, its whole numbers and its nonlinearity; rows of more than 8192
 // values are read again, from L2 as far as it holds them.
-// 2M x 128 fp16 to 8 bits 145 us and back 124; gated silu of 65,536 x 1024 bfloat16 101 us kept
-// in 8 bits and 85 back, 4.9 and 5.7 TB/s.
+// 2M x 128 fp16 to 8 bits 145 us and back 124; gated silu of 65,536 x 1024 bfloat16 99 us kept
+// in 8 bits and 86 back, 4.9 and 5.7 TB/s.  Rows that no vector divides are bound by instructions on
+// single elements; gated ones to 8 bits spill 152 bytes a thread besides.
 #include "int8.cuh"
 
 namespace agnes {
@@ -32,7 +33,7 @@ struct KeepArgs {
 
 // The normal distribution function and its density at v, for results of 16 bits:
 // Phi(-a) = exp(-a^2 / 2) t Q(t), t = 1 / (1 + 0.21 a), with Q of degree 8 fitted to the
-// scaled complementary error function over 0 <= a <= 14, to 2^-25.9 of it.  The square's
+// scaled complementary error function over 0 <= a <= 14, to 2^-24.6 of it (2^-26 of one).  The square's
 // own rounding is put back into the exponential.  (normcdff and a second exponential: gelu of
 // 131,072 x 1024 bf16 278 us forward and 537 backward.)
 __device__ __forceinline__ void normal_fit(float v, float* phi, float* density) {

@@ -435,7 +435,8 @@ norm_kernel(const NormArgs a) {
 // 352 and 719.  With ten or twelve values to a thread where they hold a row: 287 and 380 with
 // sixteen.  Bound by its instructions on single elements.  (All in fp32, 200,000 x 301 took 401
 // and 438, 8000 x 8191 537 and 415: those stay with single elements.  Two rows at a time for the
-// vectors' sake: 241 there, but 419 and not 314 with an fp32 residual.)
+// vectors' sake: 241 there, but 419 and not 314 with an fp32 residual.)  Two CTAs to an SM leave a
+// thread 64 registers: 48, 100 or 248 bytes are spilled with ten, twelve or sixteen values to it.
 template <typename TX, typename TBranch, int kPer>
 __global__ void __launch_bounds__(kNormLanes, 2)
 norm_staged_kernel(const NormArgs a) {
@@ -1122,6 +1123,8 @@ cudaError_t launch_grad(NormArgs a, bool wide, bool contiguous, int64_t ctas, si
       a.run_at[k] = (int32_t)at;
       at += bytes[k];
     }
+    // Without room for two stages (all in fp32 with a full gate above some 3,100 columns) single
+    // elements are read from memory after all: 16,000 x 3501 779 us, 539 with a gate by column.
     if ((int64_t)a.stage_off * 16 + at <= 224 * 1024) {
       which = 7;
       smem = (size_t)a.stage_off * 16 + (size_t)at;

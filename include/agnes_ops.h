@@ -235,8 +235,9 @@ agnes_status agnes_int8_linear_workspace(int64_t rows, int64_t width, int64_t di
 /* The gradient of agnes_int8_linear to the weights, from the rows that the layer
  * keeps in 8 bits, and to the bias:
  *   out[j][i] = sum_r grad[r][j] x[r][i],  dbias[j] = sum_r grad[r][j].
- * Products are exact to 2^-21 (2^-16 where a scale has more than eight bits), sums are in fp32 over an order that depends on the
- * sizes only: the result is the same, bit by bit, each time.
+ * Products are exact to 2^-21 (2^-16 where a scale has more than eight bits), sums are in
+ * fp32 over an order that depends on the sizes only: the result is the same, bit by bit,
+ * each time.
  *  grad   rows x width of grad_dtype, grad_stride apart.
  *  out    width x dim of out_dtype, out_stride apart (zeros where rows is 0).
  *  dbias  width floats, or NULL.
